@@ -69,8 +69,9 @@ extern "C" {
 
 /* Raised with every entry point added and every change to the contents of a
  * buffer that a caller may keep (9: the weight spectrum in fragment order,
- * eqlinear_block.h; a spectrum written by a library of version 8 is not read). */
-#define EQLINEAR_ABI_VERSION 9
+ * eqlinear_block.h; a spectrum written by a library of version 8 is not read;
+ * 10: eqlinear_encoder.h). */
+#define EQLINEAR_ABI_VERSION 10
 #define EQLINEAR_MAX_T 16
 
 typedef enum { EQL_F32 = 0, EQL_F16 = 1, EQL_BF16 = 2 } eql_dtype_t;

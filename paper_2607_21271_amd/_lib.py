@@ -1,4 +1,4 @@
-"""ctypes binding of libeqlinear.so: the C ABI of include/eqlinear.h, same names.
+"""ctypes binding of libeqlinear.so: the C ABI of include/eqlinear.h, eqlinear_block.h and eqlinear_encoder.h, same names.
 
 Argument marshalling only.  Every function takes device addresses as Python
 ints (or None for NULL) and returns the library's status code; ``check``
@@ -30,8 +30,31 @@ EQL_ERR_SCRATCH = 7
 # (EQLINEAR_STATIC_SCRATCH_BYTES in include/eqlinear.h).
 STATIC_SCRATCH_BYTES = 64 << 20
 
-# Every function the header declares, with (restype, argtypes).
+EQL_ACT_NONE = 0
+EQL_ACT_RELU = 1
+EQL_ACT_SILU = 2
+EQL_ACT_GELU = 3
+
 _vp, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
+_f = ctypes.c_float
+
+
+class RotaryShape(ctypes.Structure):
+    """eqlinear_rotary_shape of include/eqlinear_encoder.h."""
+    _fields_ = [("B", _i64), ("L", _i64), ("heads", _i), ("dh", _i), ("T", _i), ("axes", _i), ("sections", _i * 4),
+                ("float_positions", _i), ("interleaved", _i), ("inverse", _i), ("dtype", _i), ("x_stride", _i64 * 3),
+                ("y_stride", _i64 * 3), ("pos_stride", _i64 * 2)]
+
+
+class WindowShape(ctypes.Structure):
+    """eqlinear_window_shape of include/eqlinear_encoder.h."""
+    _fields_ = [("B", _i64), ("Lq", _i64), ("Lk", _i64), ("left", _i64), ("right", _i64), ("sinks", _i64),
+                ("heads", _i), ("kv_heads", _i), ("head_dim", _i), ("dtype", _i), ("scale", _f), ("reserved", _i)] + [
+                    (n + "_stride", _i64 * 3) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")]
+
+
+# Every function the headers declare, with (restype, argtypes).
+_RS, _WS = ctypes.POINTER(RotaryShape), ctypes.POINTER(WindowShape)
 SIGNATURES = {
     "eqlinear_abi_version": (_i, []),
     "eqlinear_status_string": (ctypes.c_char_p, [_i]),
@@ -55,6 +78,15 @@ SIGNATURES = {
     "eqlinear_gconv_forward": (_i, [_vp, _vp, _vp, _vp, _i64, _i, _i, _i, _i, _i, _i, _i, _vp]),
     "eqlinear_group_norm": (_i, [_vp, _vp, _vp, _vp, _i64, _i, _i, ctypes.c_float, _i, _vp]),
     "eqlinear_attention": (_i, [_vp, _vp, _i64, _i, _i, _i, ctypes.c_float, _i, _vp]),
+    "eqlinear_rotary": (_i, [_RS, _vp, _vp, _vp, _vp, _vp]),
+    "eqlinear_window_attention_workspace_bytes": (_sz, [_WS]),
+    "eqlinear_window_attention": (_i, [_WS] + [_vp] * 8 + [_sz, _vp]),
+    "eqlinear_window_attention_backward_workspace_bytes": (_sz, [_WS]),
+    "eqlinear_window_attention_backward": (_i, [_WS] + [_vp] * 12 + [_sz, _vp]),
+    "eqlinear_group_norm_act_workspace_bytes": (_sz, [_i64, _i64, _i, _i, _i, _i]),
+    "eqlinear_group_norm_act": (_i, [_vp] * 6 + [_sz, _i64, _i64, _i, _i, _i, _f, _i, _i, _vp]),
+    "eqlinear_group_norm_act_backward_workspace_bytes": (_sz, [_i64, _i64, _i, _i, _i, _i]),
+    "eqlinear_group_norm_act_backward": (_i, [_vp] * 9 + [_sz, _i64, _i64, _i, _i, _i, _i, _i, _vp]),
 }
 
 
@@ -185,3 +217,45 @@ def eqlinear_group_norm(x, weight, bias, y, rows, T, C, eps, dtype, stream) -> i
 
 def eqlinear_attention(qkv, o, B, L, heads, head_dim, scale, dtype, stream) -> int:
     return lib().eqlinear_attention(qkv, o, B, L, heads, head_dim, scale, dtype, stream)
+
+
+def eqlinear_rotary(shape, x, positions, freqs, y, stream) -> int:
+    return lib().eqlinear_rotary(shape, x, positions, freqs, y, stream)
+
+
+def eqlinear_window_attention_workspace_bytes(shape) -> int:
+    return lib().eqlinear_window_attention_workspace_bytes(shape)
+
+
+def eqlinear_window_attention(shape, q, k, v, lengths, starts, o, lse, workspace, workspace_bytes, stream) -> int:
+    return lib().eqlinear_window_attention(shape, q, k, v, lengths, starts, o, lse, workspace, workspace_bytes, stream)
+
+
+def eqlinear_window_attention_backward_workspace_bytes(shape) -> int:
+    return lib().eqlinear_window_attention_backward_workspace_bytes(shape)
+
+
+def eqlinear_window_attention_backward(shape, q, k, v, lengths, starts, o, lse, d_o, dq, dk, dv, workspace,
+                                       workspace_bytes, stream) -> int:
+    return lib().eqlinear_window_attention_backward(shape, q, k, v, lengths, starts, o, lse, d_o, dq, dk, dv,
+                                                    workspace, workspace_bytes, stream)
+
+
+def eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype) -> int:
+    return lib().eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype)
+
+
+def eqlinear_group_norm_act(x, weight, bias, y, stats, workspace, workspace_bytes, B, S, T, C, groups, eps, act,
+                            dtype, stream) -> int:
+    return lib().eqlinear_group_norm_act(x, weight, bias, y, stats, workspace, workspace_bytes, B, S, T, C, groups,
+                                         eps, act, dtype, stream)
+
+
+def eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype) -> int:
+    return lib().eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype)
+
+
+def eqlinear_group_norm_act_backward(x, weight, bias, stats, dy, dx, dw, db, workspace, workspace_bytes, B, S, T, C,
+                                     groups, act, dtype, stream) -> int:
+    return lib().eqlinear_group_norm_act_backward(x, weight, bias, stats, dy, dx, dw, db, workspace, workspace_bytes,
+                                                  B, S, T, C, groups, act, dtype, stream)

@@ -1,0 +1,185 @@
+"""Attention with a sliding window and first tokens that stay visible, for long token sequences of an encoder.
+
+Token i of sequence b stands at position p = starts[b] + i among the lengths[b] keys of that sequence and sees key j iff
+
+    p < lengths[b],  j < lengths[b],  j <= p + right  and  (j >= p - left or j < sinks)
+
+(-1 is no limit).  One entry point serves training (autograd), whole sequences and single tokens over a cache: queries
+may be fewer than keys, and by default are the last of them.  Query heads may share key/value heads.  This module
+allocates and marshals; ``eqlinear_window_attention`` and its backward compute.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import _lib, ops, rotary
+
+
+def _ready(t: torch.Tensor) -> torch.Tensor:
+    """t itself where its heads start on whole 16-byte words, else a contiguous copy."""
+    w = 16 // t.element_size()
+    s, n = t.stride(), t.shape
+    if (s[3] == 1 and t.data_ptr() % 16 == 0
+            and all(n[i] <= 1 or s[i] % w == 0 for i in range(3))):
+        return t
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
+def _shape(q, k, left, right, sinks, scale, q_s, k_s, v_s, o_s, *grads):
+    B, Lq, H, D = q.shape
+    none = (0, 0, 0)
+    return _lib.WindowShape(B, Lq, k.shape[1], left, right, sinks, H, k.shape[2], D, ops._DT[q.dtype], scale, 0, q_s,
+                            k_s, v_s, o_s, *(grads or (none, none, none, none)))
+
+
+_strides = rotary._strides
+
+
+def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse, stream=None):
+    B, Lq, H, D = q.shape
+    o = torch.empty(B, Lq, H, D, dtype=q.dtype, device=q.device)
+    shape = _shape(q, k, left, right, sinks, scale, _strides(q), _strides(k), _strides(v), _strides(o))
+    ref = ctypes.byref(shape)
+    lse = torch.empty(B, k.shape[2], Lq, H // k.shape[2], dtype=torch.float32, device=q.device) if want_lse else None
+    need = _lib.eqlinear_window_attention_workspace_bytes(ref)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _lib.check(_lib.eqlinear_window_attention(ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
+                                              ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(ws), need,
+                                              ops._stream(stream)), "eqlinear_window_attention")
+    return o, lse
+
+
+def _backward(q, k, v, lengths, starts, o, lse, do, dq, dk, dv, left, right, sinks, scale, stream=None):
+    shape = _shape(q, k, left, right, sinks, scale, _strides(q), _strides(k), _strides(v), _strides(o), _strides(do),
+                   _strides(dq), _strides(dk), _strides(dv))
+    ref = ctypes.byref(shape)
+    need = _lib.eqlinear_window_attention_backward_workspace_bytes(ref)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _lib.check(_lib.eqlinear_window_attention_backward(
+        ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths), ops._ptr(starts), ops._ptr(o), ops._ptr(lse),
+        ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv), ops._ptr(ws), need, ops._stream(stream)),
+        "eqlinear_window_attention_backward")
+
+
+def _check_spans(B, dev_of, lengths, starts):
+    for name, t in (("lengths", lengths), ("starts", starts)):
+        if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (B,) or not t.is_contiguous()):
+            raise ValueError("%s must be a contiguous int32 [%d], got %s %s" % (name, B, t.dtype, tuple(t.shape)))
+    ops._check_dev(dev_of, lengths, starts)
+
+
+def _check_window(left, right, sinks):
+    if left < -1 or right < -1 or sinks < 0:
+        raise ValueError("left and right are -1 (no limit) or at least 0, sinks at least 0; got %d, %d, %d"
+                         % (left, right, sinks))
+
+
+def _check(q, k, v, lengths, starts, left, right, sinks):
+    ops._dtype_code(q)
+    ops._check_same_dtype(q, k=k, v=v)
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
+        raise ValueError("q must be [B, Lq, heads, D] and k, v [B, Lk, kv_heads, D], got %s, %s, %s"
+                         % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+    if q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3] or k.shape[2] < 1 or q.shape[2] % k.shape[2]:
+        raise ValueError("q %s and k %s differ in sequences or head size, or the heads do not divide"
+                         % (tuple(q.shape), tuple(k.shape)))
+    _check_window(left, right, sinks)
+    ops._check_dev(q, k, v)
+    _check_spans(q.shape[0], q, lengths, starts)
+
+
+class WindowAttentionFunction(torch.autograd.Function):
+    """Autograd: gradients of q, k and v; key/value gradients sum over the query heads that share a head."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, lengths, starts, left, right, sinks, scale):
+        q, k, v = _ready(q), _ready(k), _ready(v)
+        o, lse = _forward(q, k, v, lengths, starts, left, right, sinks, scale, True)
+        ctx.save_for_backward(q, k, v, lengths, starts, o, lse)
+        ctx.args = (left, right, sinks, scale)
+        return o
+
+    @staticmethod
+    def backward(ctx, go):
+        q, k, v, lengths, starts, o, lse = ctx.saved_tensors
+        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        _backward(q, k, v, lengths, starts, o, lse, _ready(go), dq, dk, dv, *ctx.args)
+        return dq, dk, dv, None, None, None, None, None, None
+
+
+def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, left: int = -1, right: int = -1, sinks: int = 0,
+                     scale: float | None = None, lengths: torch.Tensor | None = None,
+                     starts: torch.Tensor | None = None) -> torch.Tensor:
+    """o [B, Lq, heads, D] from q [B, Lq, heads, D] and k, v [B, Lk, kv_heads, D] (views with strides are read as they
+    are where heads start on 16-byte words).
+
+    ``lengths`` int32 [B]: keys of each sequence that hold data (None: Lk).  ``starts`` int32 [B]: position of the
+    first query (None: Lk - Lq, the queries are the last tokens).  A query past its sequence, or that sees no
+    key, gives zeros and no gradient.  ``scale`` defaults to D ** -0.5."""
+    left, right, sinks = int(left), int(right), int(sinks)
+    _check(q, k, v, lengths, starts, left, right, sinks)
+    scale = float(q.shape[3]) ** -0.5 if scale is None else float(scale)
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
+        return WindowAttentionFunction.apply(q, k, v, lengths, starts, left, right, sinks, scale)
+    return _forward(_ready(q), _ready(k), _ready(v), lengths, starts, left, right, sinks, scale, False)[0]
+
+
+class PackedAttentionFunction(torch.autograd.Function):
+    """Rotary positions and windowed attention on the packed output of one layer, qkv [B, L, heads + 2 kv_heads, D]:
+    the gradient comes back in one buffer of that shape, turned back in place."""
+
+    @staticmethod
+    def forward(ctx, qkv, kv_heads, positions, freqs, sections, T, interleaved, lengths, left, right, sinks, scale):
+        H = qkv.shape[2] - 2 * kv_heads
+        qkv = _ready(qkv)
+        qk = qkv[:, :, :H + kv_heads]
+        if positions is not None:
+            qk = rotary.rotary_axes(qk.detach(), positions, freqs, sections, T, interleaved)
+        q, k, v = qk[:, :, :H], qk[:, :, H:], qkv[:, :, H + kv_heads:]
+        starts = torch.zeros(qkv.shape[0], dtype=torch.int32, device=qkv.device) if lengths is not None else None
+        o, lse = _forward(q, k, v, lengths, starts, left, right, sinks, scale, ctx.needs_input_grad[0])
+        if ctx.needs_input_grad[0]:
+            ctx.save_for_backward(qk, v, lengths, starts, o, lse, positions, freqs)
+            ctx.args = (left, right, sinks, scale)
+            ctx.turn = (sections, T, interleaved)
+            ctx.heads = (H, kv_heads)
+        return o
+
+    @staticmethod
+    def backward(ctx, go):
+        qk, v, lengths, starts, o, lse, positions, freqs = ctx.saved_tensors
+        H, kv_heads = ctx.heads
+        B, L, _, D = qk.shape
+        g = torch.empty(B, L, H + 2 * kv_heads, D, dtype=qk.dtype, device=qk.device)
+        dqk = g[:, :, :H + kv_heads]
+        _backward(qk[:, :, :H], qk[:, :, H:], v, lengths, starts, o, lse, _ready(go), dqk[:, :, :H], dqk[:, :, H:],
+                  g[:, :, H + kv_heads:], *ctx.args)
+        if positions is not None:
+            rotary.rotary_axes_(dqk, positions, freqs, *ctx.turn, inverse=True)
+        return (g,) + (None,) * 11
+
+
+def packed_window_attention(qkv: torch.Tensor, kv_heads: int, positions: torch.Tensor | None = None,
+                            freqs: torch.Tensor | None = None, sections=(), T: int = 1, interleaved: bool = False,
+                            lengths: torch.Tensor | None = None, left: int = -1, right: int = -1, sinks: int = 0,
+                            scale: float | None = None) -> torch.Tensor:
+    """Self-attention on a layer's packed output qkv [B, L, heads + 2 kv_heads, D] (queries, keys, values): queries and
+    keys turned by ``rotary_axes`` where positions are given, then ``window_attention`` with every token at its own
+    place (tokens from lengths[b] on are padding)."""
+    left, right, sinks = int(left), int(right), int(sinks)
+    ops._dtype_code(qkv)
+    if qkv.dim() != 4 or kv_heads < 1 or qkv.shape[2] <= 2 * kv_heads or (qkv.shape[2] - 2 * kv_heads) % kv_heads:
+        raise ValueError("qkv must be [B, L, heads + 2 * kv_heads, D] with heads a multiple of kv_heads = %d, got %s"
+                         % (kv_heads, tuple(qkv.shape)))
+    _check_window(left, right, sinks)
+    ops._check_dev(qkv)
+    _check_spans(qkv.shape[0], qkv, lengths, None)
+    if positions is not None:
+        sections = tuple(int(s) for s in sections)
+        rotary._check(qkv, positions, freqs, sections, T)
+    scale = float(qkv.shape[3]) ** -0.5 if scale is None else float(scale)
+    return PackedAttentionFunction.apply(qkv, kv_heads, positions, freqs, sections, T, interleaved, lengths, left, right,
+                                         sinks, scale)

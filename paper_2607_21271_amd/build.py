@@ -20,10 +20,11 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeqlinear.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
-HOST_SOURCES = ["eql_api.cpp", "eql_dispatch.cpp"]
+HOST_SOURCES = ["eql_api.cpp", "eql_dispatch.cpp", "eql_encoder_api.cpp"]
 MAX_T = 16
 # (source, object stem, extra defines)
-UNITS = [("eql_big.hip", "eql_big", []), ("eql_block.hip", "eql_block", [])] + [(s, os.path.splitext(s)[0], []) for s in HOST_SOURCES] + [
+UNITS = [("eql_big.hip", "eql_big", []), ("eql_block.hip", "eql_block", []), ("eql_encoder.hip", "eql_encoder", [])] + [
+    ("eql_attn.hip", "attn_" + name, ["-DEQK_DT=%d" % dt]) for dt, name in ((1, "f16"), (0, "f32"), (2, "bf16"))] + [(s, os.path.splitext(s)[0], []) for s in HOST_SOURCES] + [
     ("eql_inst.hip", "inst_%s_t%02d" % (name, t), ["-DEQK_T=%d" % t, "-DEQK_DT=%d" % dt])
     for t in range(MAX_T, 0, -1) for dt, name in ((1, "f16"), (0, "f32"), (2, "bf16"))]
 
@@ -33,11 +34,12 @@ ARCH = "gfx950"
 # MFMA accumulators may live in arch VGPRs (gfx950 has a unified register
 # file); with this selection the kernels of two waves per SIMD allocate
 # without scratch.  The large-tile unit (one wave per SIMD, T * 64
-# accumulators per lane) keeps them in the accumulation registers instead.
+# accumulators per lane) and full-precision attention keep them in the
+# accumulation registers instead.
 LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 DEVICE_FLAGS = LINK_FLAGS + VGPR_FORM
-ACC_REG_UNITS = {"eql_big"}
+ACC_REG_UNITS = {"eql_big", "attn_f32"}
 COMMON_FLAGS = ["-O3", "-std=c++20", "-fPIC", "-Wall", "-Wno-unused-function",
                 "-I" + os.path.join(os.path.dirname(HERE), "include")]
 

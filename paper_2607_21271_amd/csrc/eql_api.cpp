@@ -10,6 +10,7 @@
 
 #include "../../include/eqlinear.h"
 #include "../../include/eqlinear_block.h"
+#include "eql_check.h"
 #include "eql_dihedral.h"
 #include "eql_gconv.h"
 #include "eql_launch.h"
@@ -564,36 +565,19 @@ FusedPlan fused_plan(int64_t N, int T, int Cin, int Cout, int dt) {
 
 }  // namespace eqk
 
+using eqk::align256;
+using eqk::aligned;
+using eqk::any_overlap;
+using eqk::check_device;
+using eqk::elem_bytes;
+using eqk::overlaps;
+using eqk::Range;
+using eqk::valid_dtype;
+
 namespace {
 
 constexpr int64_t kMaxN = (int64_t)1 << 36;
 constexpr int kMaxC = 65536;
-
-size_t elem_bytes(int dtype) { return dtype == EQL_F32 ? 4 : 2; }
-bool valid_dtype(int dtype) { return dtype == EQL_F32 || dtype == EQL_F16 || dtype == EQL_BF16; }
-
-size_t align256(size_t v) { return (v + 255) / 256 * 256; }
-
-struct Range {
-  const void* p;
-  size_t bytes;
-};
-
-bool overlaps(Range a, Range b) {
-  if (!a.p || !b.p || a.bytes == 0 || b.bytes == 0) return false;
-  const uintptr_t a0 = (uintptr_t)a.p, a1 = a0 + a.bytes;
-  const uintptr_t b0 = (uintptr_t)b.p, b1 = b0 + b.bytes;
-  return a0 < b1 && b0 < a1;
-}
-
-bool any_overlap(const Range* r, int n) {
-  for (int i = 0; i < n; ++i)
-    for (int j = i + 1; j < n; ++j)
-      if (overlaps(r[i], r[j])) return true;
-  return false;
-}
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 int check_shape(int64_t N, int T, int Cin, int Cout, int dtype) {
   if (!valid_dtype(dtype)) return EQL_ERR_INVALID_ARG;
@@ -611,6 +595,20 @@ std::once_flag g_once[kMaxDevices];
 int g_arch_ok[kMaxDevices];
 int g_cus[kMaxDevices];
 
+int launched(hipError_t e) { return e == hipSuccess ? EQL_OK : EQL_ERR_LAUNCH; }
+
+}  // namespace
+
+namespace eqk {
+// Read on every plan so that tests can switch it within one process.
+int gemm_big_forced() {
+  const char* v = getenv("EQL_GEMM_BIG");
+  return (v != nullptr && (v[0] == '0' || v[0] == '1') && v[1] == 0) ? v[0] - '0' : -1;
+}
+int gauss_forced() {
+  const char* v = getenv("EQL_GAUSS");
+  return (v != nullptr && (v[0] == '0' || v[0] == '1') && v[1] == 0) ? v[0] - '0' : -1;
+}
 int check_device() {
   int count = 0;
   if (hipGetDeviceCount(&count) != hipSuccess || count <= 0) {
@@ -636,20 +634,6 @@ int check_device() {
   return g_arch_ok[dev] ? EQL_OK : EQL_ERR_UNSUPPORTED;
 }
 
-int launched(hipError_t e) { return e == hipSuccess ? EQL_OK : EQL_ERR_LAUNCH; }
-
-}  // namespace
-
-namespace eqk {
-// Read on every plan so that tests can switch it within one process.
-int gemm_big_forced() {
-  const char* v = getenv("EQL_GEMM_BIG");
-  return (v != nullptr && (v[0] == '0' || v[0] == '1') && v[1] == 0) ? v[0] - '0' : -1;
-}
-int gauss_forced() {
-  const char* v = getenv("EQL_GAUSS");
-  return (v != nullptr && (v[0] == '0' || v[0] == '1') && v[1] == 0) ? v[0] - '0' : -1;
-}
 // Valid after check_device() succeeded on the current device.
 int device_cu_count() {
   int dev = 0;

@@ -1,0 +1,859 @@
+// eql_attn.h -- attention with a sliding window and first tokens that stay
+// visible, for gfx950: forward, forward over few rows split along the keys, and
+// the two backward passes.
+//
+// Rows.  The G query heads that share a key/value head are taken together:
+// packed row r of (sequence b, key/value head hk) is query token r / G of head
+// hk G + r % G, R = Lq G rows in all.  Token i stands at position p = start + i
+// and sees key j iff p < len, j < len, j <= p + right and (j >= p - left or
+// j < sinks); a row that sees nothing gives zeros.
+//
+// Products.  All kernels compute transposed tiles with one owner a lane: in a
+// 32 x 32 MFMA result a lane holds 16 entries of column lane % 32, entry e in
+// row 8 (e / 4) + 4 (lane / 32) + e % 4.  The owners (queries in the forward and
+// query-gradient kernels, keys in the key/value-gradient kernel) are the columns,
+// the streamed rows the result rows, so that a softmax statistic is a lane's own
+// sum and one exchange between the lane halves, and eight consecutive entries
+// of a score tile are the B operand of the product that follows: contraction
+// slot (half, j) stands for streamed row 16 s + 8 (j / 4) + 4 half + j % 4,
+// and the A operand reads its rows in the same order (col_frag).
+//
+// Streamed rows go through two LDS buffers, by way of registers: one barrier a
+// tile, the next tile's loads in flight during the products, rows past the
+// sequence and elements past the head dimension set to zero on the way.
+#pragma once
+#include "eql_attn_args.h"
+#include "eql_common.h"
+#include "eql_config.h"
+
+namespace eqk {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+
+// Bits as the other type.  By value: a bit cast of an element of a vector names
+// the vector's first element in this compiler.
+__device__ __forceinline__ float bits_f32(uint32_t v) { return __builtin_bit_cast(float, v); }
+__device__ __forceinline__ uint32_t f32_bits(float v) { return __builtin_bit_cast(uint32_t, v); }
+
+// Eight contraction values of one row: a lane's share of a 16-deep step.
+template <int DT>
+struct Frag8 {
+  uint32_t w[DT == kF32 ? 8 : 4];
+};
+
+template <int DT>
+__device__ __forceinline__ void mma32(floatx16& acc, const Frag8<DT>& a, const Frag8<DT>& b) {
+  if constexpr (DT == kF16) {
+    const u32x4 av = {a.w[0], a.w[1], a.w[2], a.w[3]}, bv = {b.w[0], b.w[1], b.w[2], b.w[3]};
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, av), __builtin_bit_cast(half8, bv), acc, 0,
+                                                 0, 0);
+  } else if constexpr (DT == kBF16) {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    const u32x4 av = {a.w[0], a.w[1], a.w[2], a.w[3]}, bv = {b.w[0], b.w[1], b.w[2], b.w[3]};
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, av), __builtin_bit_cast(bf16x8, bv), acc,
+                                                  0, 0, 0);
+  } else {
+    // step j of the eight contracts slot j of both lane halves
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__builtin_bit_cast(float, a.w[j]), __builtin_bit_cast(float, b.w[j]),
+                                                 acc, 0, 0, 0);
+  }
+}
+
+// Entries 8 s .. 8 s + 7 of a result tile, rounded to the element type, as the
+// operand of a 16-deep step.
+template <int DT>
+__device__ __forceinline__ Frag8<DT> tile_frag(const floatx16& t, int s) {
+  Frag8<DT> f;
+  if constexpr (DT == kF32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.w[j] = f32_bits(t[8 * s + j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.w[j] = pack2<DT>(t[8 * s + 2 * j], t[8 * s + 2 * j + 1]);
+  }
+  return f;
+}
+
+// LDS tile of rows of DP elements.  16-byte chunk c of a row lies at chunk
+// c ^ swz(row): sixteen consecutive rows put one chunk on sixteen places of the 256
+// bytes of all banks (row reads), and four consecutive rows put four
+// neighbouring chunks on sixteen (transposed reads).
+template <int DT, int DP>
+struct RowTile {
+  static constexpr int EB = DT == kF32 ? 4 : 2;
+  static constexpr int CE = 16 / EB;                        // elements of a chunk
+  static constexpr int NC = DP / CE;                        // chunks of a row
+  static constexpr int RB = (DP == 96 ? 128 : DP) * EB;     // bytes of a row
+  static constexpr int NCH = RB / 16;
+  __device__ static __forceinline__ int swz(int row) {
+    if constexpr (NCH == 4) return (row >> 2) & 3;
+    else if constexpr (NCH == 8) return ((row >> 1) & 1) * 4 + ((row >> 2) & 3);
+    else return (row & 3) * 4 + ((row >> 2) & 3);
+  }
+  __device__ static __forceinline__ int off(int row, int c) { return row * RB + ((c ^ swz(row)) << 4); }
+};
+
+// Row operand: elements 16 s + 8 half .. + 7 of tile row `row`.
+template <int DT, int DP>
+__device__ __forceinline__ Frag8<DT> row_frag(const char* t, int row, int s, int half) {
+  using RT = RowTile<DT, DP>;
+  Frag8<DT> f;
+  constexpr int N = DT == kF32 ? 2 : 1;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const u32x4 a = *reinterpret_cast<const u32x4*>(t + RT::off(row, (2 * s + half) * N + n));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) f.w[4 * n + j] = a[j];
+  }
+  return f;
+}
+
+// Column operand: element 32 d + lane % 32 of tile rows r0 + 8 (j / 4) + 4 half + j % 4.
+// 16 bits: two transposing LDS reads, in which sixteen lanes hand in the
+// addresses of four rows of sixteen elements and lane i takes column i.
+template <int DT, int DP>
+__device__ __forceinline__ Frag8<DT> col_frag(const char* t, int r0, int d, int lane) {
+  using RT = RowTile<DT, DP>;
+  Frag8<DT> f;
+  const int half = lane >> 5;
+  if constexpr (DT == kF32) {
+    const int e = d * 32 + (lane & 31);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int row = r0 + 8 * (j >> 2) + 4 * half + (j & 3);
+      f.w[j] = *reinterpret_cast<const uint32_t*>(t + RT::off(row, e >> 2) + (e & 3) * 4);
+    }
+  } else {
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    const int e = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int row = r0 + 8 * j + 4 * half + ((lane & 15) >> 2);
+      const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (__attribute__((address_space(3))) s16x4*)(t + RT::off(row, e >> 3) + (e & 7) * 2));
+      const u32x2 w = __builtin_bit_cast(u32x2, v);
+      f.w[2 * j] = w[0];
+      f.w[2 * j + 1] = w[1];
+    }
+  }
+  return f;
+}
+
+// Maximum and sum of the two lane halves' values.
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+  return fmaxf(bits_f32(r[0]), bits_f32(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+  return bits_f32(r[0]) + bits_f32(r[1]);
+}
+
+// Running maximum of the exponent fields of 16-byte chunks: equal to the mask in
+// some field iff an infinity or NaN went by.
+template <int DT>
+struct ExpMax {
+  static constexpr uint32_t kMask = DT == kF32 ? 0x7f800000u : DT == kF16 ? 0x7c007c00u : 0x7f807f80u;
+  uint32_t m = 0;
+  __device__ __forceinline__ void add(const u32x4& c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t e = c[j] & kMask;
+      if constexpr (DT == kF32) {
+        m = m > e ? m : e;
+      } else {
+        typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+        m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, m), __builtin_bit_cast(u16x2, e)));
+      }
+    }
+  }
+  __device__ __forceinline__ bool hit() const {
+    if constexpr (DT == kF32) return m == kMask;
+    else return (m & 0xffffu) == (kMask & 0xffffu) || (m >> 16) == (kMask >> 16);
+  }
+};
+
+// One 16-deep step of a product whose streamed rows hold infinities or NaN, and
+// of which some owners see only some: the finite elements as ever (an owner who
+// sees none of the others gets the very same bits), then the others row by row, each
+// into a tile of its own that only the owners who see the row add.  sees(k) tells
+// whether the lane's owner sees tile row k.
+template <int DT, int DP, typename F>
+__device__ __forceinline__ void mma_seen(floatx16 (&acc)[DP / 32], const char* t, int r0, const Frag8<DT>& b, int lane,
+                                         F&& sees) {
+  constexpr int NR = DT == kF32 ? 8 : 4;
+  constexpr uint32_t kMask = ExpMax<DT>::kMask;
+  const int half = lane >> 5;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) {
+    Frag8<DT> a = col_frag<DT, DP>(t, r0, d, lane), odd;
+    bool any = false;
+#pragma unroll
+    for (int w = 0; w < NR; ++w) {
+      const uint32_t e = a.w[w] & kMask;
+      uint32_t m;
+      if constexpr (DT == kF32) m = e == kMask ? 0xffffffffu : 0u;
+      else m = ((e & 0xffffu) == (kMask & 0xffffu) ? 0xffffu : 0u) | ((e >> 16) == (kMask >> 16) ? 0xffff0000u : 0u);
+      odd.w[w] = a.w[w] & m;
+      a.w[w] &= ~m;
+      any |= m != 0;
+    }
+    mma32<DT>(acc[d], a, b);
+    if (!__any(any)) continue;
+#pragma unroll 1
+    for (int slot = 0; slot < 16; ++slot) {
+      const int j = slot & 7;
+      const bool mine = (slot >> 3) == half;
+      const uint32_t keep = DT == kF32 ? 0xffffffffu : (j & 1) ? 0xffff0000u : 0x0000ffffu;
+      Frag8<DT> one;
+#pragma unroll
+      for (int w = 0; w < NR; ++w) one.w[w] = mine && w == (DT == kF32 ? j : j >> 1) ? odd.w[w] & keep : 0u;
+      floatx16 p{};
+      mma32<DT>(p, one, b);
+      const bool s = sees(r0 + 8 * (j >> 2) + 4 * (slot >> 3) + (j & 3));
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[d][e] += s ? p[e] : 0.0f;
+    }
+  }
+}
+
+// Loads of one streamed tile of TK rows by NT threads, held in registers between
+// the load and the LDS write.
+template <int DT, int DP, int TK, int NT>
+struct Stage {
+  using RT = RowTile<DT, DP>;
+  static constexpr int N = (TK * RT::NC + NT - 1) / NT;
+  static_assert(TK * RT::NC % NT == 0, "whole chunks");
+  u32x4 r[N];
+  // at(row) is the address of tile row `row`, ok(row) whether it holds data (its
+  // address must be readable either way)
+  template <typename A, typename K>
+  __device__ __forceinline__ void load(int tid, int D, A&& at, K&& ok) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = tid + i * NT, row = u / RT::NC, c = u % RT::NC;
+      const bool in = c * RT::CE < D;
+      const u32x4 v = *reinterpret_cast<const u32x4*>(at(row) + (in ? c * 16 : 0));
+      r[i] = in && ok(row) ? v : u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ void store(int tid, char* t) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = tid + i * NT;
+      *reinterpret_cast<u32x4*>(t + RT::off(u / RT::NC, u % RT::NC)) = r[i];
+    }
+  }
+  __device__ __forceinline__ void scan(ExpMax<DT>& m) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) m.add(r[i]);
+  }
+};
+
+// Owner operand: one row of D elements read straight from memory, steps of 16.
+template <int DT, int DP>
+__device__ __forceinline__ void load_owner(Frag8<DT> (&f)[DP / 16], const char* row, bool ok, int D, int half) {
+  constexpr int N = DT == kF32 ? 2 : 1, CE = RowTile<DT, DP>::CE;
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int c = (2 * s + half) * N + n;
+      u32x4 v{0, 0, 0, 0};
+      if (ok && c * CE < D) v = *reinterpret_cast<const u32x4*>(row + c * 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f[s].w[4 * n + j] = v[j];
+    }
+}
+
+// Writes an owner's row from result tiles acc[DP / 32] (entries in d), times
+// `mul`, rounded once, or zeros where it has no data: whole 16-byte words after
+// an exchange between the halves.  Every lane of the wave must come here.
+template <int DT, int DP>
+__device__ __forceinline__ void store_owner(const floatx16 (&acc)[DP / 32], float mul, bool data, char* row,
+                                            bool ok, int D, int half) {
+  auto val = [&](int d, int e) { return data ? acc[d][e] * mul : 0.0f; };
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) {
+    if constexpr (DT == kF32) {
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) {
+        const int at = 32 * d + 2 * e + 4 * half;
+        const floatx4 v = {val(d, e), val(d, e + 1), val(d, e + 2), val(d, e + 3)};
+        if (ok && at < D) *reinterpret_cast<floatx4*>(row + at * 4) = v;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; e += 8) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = pack2<DT>(val(d, e + 2 * j), val(d, e + 2 * j + 1));
+        const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+        const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+        const int at = 32 * d + 2 * e + 8 * half;
+        if (ok && at < D) *reinterpret_cast<u32x4*>(row + at * 2) = u32x4{a[0], b[0], a[1], b[1]};
+      }
+    }
+  }
+}
+
+// Length and start of one sequence, in the ranges the position arithmetic allows.
+__device__ __forceinline__ int seq_len(const AttnArgs& a, int b) {
+  return a.lengths ? min(max(a.lengths[b], 0), a.Lk) : a.Lk;
+}
+__device__ __forceinline__ int seq_start(const AttnArgs& a, int b) {
+  return a.starts ? min(max(a.starts[b], -kAttnMaxPos), kAttnMaxPos) : a.Lk - a.Lq;
+}
+
+// The keys that packed rows r0 .. r1 see, as key tiles of TK: `ns` tiles of first
+// tokens, then tiles t0 ...; n in all.  And per range the bounds of visibility.
+struct KeyRange {
+  int n, ns, t0;
+  int last, sink_end;     // no row sees past `last`; first tokens seen by some row
+  int first;              // no row sees before `first`, first tokens aside
+  int all_first, all_last, all_sink;  // keys every row sees: all_first .. all_last and below all_sink
+  __device__ __forceinline__ int tile(int i) const { return i < ns ? i : t0 + i - ns; }
+};
+__device__ __forceinline__ KeyRange key_range(const AttnArgs& a, int r0, int r1, int len, int start, int TK) {
+  KeyRange k{};
+  const int pa = start + r0 / a.G, pb = min(start + r1 / a.G, len - 1);
+  if (pa > pb) { k.last = -1; k.first = 1; return k; }
+  k.last = min(len - 1, pb + a.right);
+  k.first = max(0, pa - a.left);
+  k.sink_end = min(a.sinks, k.last + 1);
+  k.all_first = pb - a.left;
+  k.all_last = min(len - 1, pa + a.right);
+  k.all_sink = min(a.sinks, k.all_last + 1);
+  if (k.last < 0) return k;
+  k.t0 = k.first / TK;
+  k.ns = min((k.sink_end + TK - 1) / TK, k.t0);
+  k.n = k.ns + max(k.last / TK - k.t0 + 1, 0);
+  return k;
+}
+
+// Workgroup number -> (part, row tile, head pair): consecutive numbers of one XCD
+// (number % 8) take consecutive tiles, whose windows overlap in its L2.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n) {
+  const uint32_t q = n / 8, rest = n % 8, x = i % 8;
+  return x * q + min(x, rest) + i / 8;
+}
+
+// ---- forward ---------------------------------------------------------------
+// o = sum_j p_j v_j / sum_j p_j, p_j = exp2(c s_j - m), c = scale log2 e, with the
+// running maximum m of a row raised (and what was summed rescaled) only where
+// a tile's maximum exceeds it by 2^8: probabilities stay below 2^8, far inside
+// fp16's range.  Scores, maxima and sums in fp32; a probability is
+// rounded once to the element type, as the operand of the second product.
+template <int DT, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql_wattn_fwd_kernel(AttnArgs a) {
+  using RT = RowTile<DT, DP>;
+  constexpr int TK = attn_tile(DT), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // K 0, K 1, V 0, V 1, flags
+  int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+  const int part = id % a.parts;
+  const uint32_t rest = id / a.parts;
+  const int nrt = (a.R + 32 * NW - 1) / (32 * NW);
+  const int rt = nrt - 1 - (int)(rest % nrt), bh = (int)(rest / nrt);  // long causal rows first
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int len = seq_len(a, b), start = seq_start(a, b);
+
+  const int g0 = rt * 32 * NW, g1 = min(g0 + 32 * NW, a.R) - 1;  // rows of the workgroup
+  const int w0 = g0 + wave * 32, w1 = min(w0 + 31, a.R - 1);     // and of the wave
+  const KeyRange kg = key_range(a, g0, g1, len, start, TK);
+  KeyRange kw = key_range(a, w0, w1, len, start, TK);
+  if (w0 > w1) { kw.n = 0; kw.last = -1; kw.first = 1; kw.sink_end = 0; }
+  const int r = w0 + (lane & 31);
+  const int tok = min(r, a.R - 1) / a.G, pos = start + tok;
+  const int head = hk * a.G + min(r, a.R - 1) % a.G;
+  const bool row_ok = r < a.R && pos < len;
+  const int hi = row_ok ? min(len - 1, pos + a.right) : -1, lo = pos - a.left, sk = min(a.sinks, hi + 1);
+
+  const char* const kb = (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2]) * RT::EB;
+  const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
+  Frag8<DT> qf[DP / 16];
+  load_owner<DT, DP>(qf, (const char*)a.q + ((int64_t)b * a.qs[0] + (int64_t)tok * a.qs[1] + (int64_t)head * a.qs[2]) * RT::EB,
+                     row_ok, a.D, half);
+
+  const int i0 = (int)((int64_t)kg.n * part / a.parts), i1 = (int)((int64_t)kg.n * (part + 1) / a.parts);
+  Stage<DT, DP, TK, NT> sk_, sv_;
+  auto load = [&](int i) {
+    const int k0 = kg.tile(i) * TK;
+    auto ok = [&](int row) { return k0 + row < len; };
+    sk_.load(tid, a.D, [&](int row) { return kb + (int64_t)min(k0 + row, len - 1) * a.ks[1] * RT::EB; }, ok);
+    sv_.load(tid, a.D, [&](int row) { return vb + (int64_t)min(k0 + row, len - 1) * a.vs[1] * RT::EB; }, ok);
+  };
+
+  floatx16 acc[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+  float m = -__builtin_inff(), l = 0.0f;
+  const float c = a.scale_log2e;
+  if (i0 < i1) load(i0);
+  for (int i = i0; i < i1; ++i) {
+    char* const kt = smem + (i & 1) * TB;
+    char* const vt = smem + (2 + (i & 1)) * TB;
+    int* const flag = flags + (i & 1) * NW;
+    sk_.store(tid, kt);
+    sv_.store(tid, vt);
+    {
+      ExpMax<DT> e;
+      sv_.scan(e);
+      const bool any = __any(e.hit());
+      if (lane == 0) flag[wave] = any;
+    }
+    __syncthreads();
+    const int k0 = kg.tile(i) * TK;
+    if (i + 1 < i1) load(i + 1);
+    if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;  // no row of the wave sees the tile
+    floatx16 s[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      s[n] = floatx16{};
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) mma32<DT>(s[n], row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
+    }
+    const bool whole = k0 + TK - 1 <= kw.all_last && (k0 >= kw.all_first || k0 + TK <= kw.all_sink);
+    auto sees = [&](int k) {
+      const int j = k0 + k;
+      return j <= hi && (j >= lo || j < sk);
+    };
+    if (!whole) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[n][e] = -__builtin_inff();
+    }
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[n][e]);
+    mx = half_max(mx);
+    if (__any((mx - m) * c > 8.0f)) {
+      const float mn = fmaxf(m, mx);
+      const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * c);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] *= f;
+    }
+    const float mc = m == -__builtin_inff() ? 0.0f : m * c;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -mc));
+        l += s[n][e];
+      }
+    bool odd = false;
+    if (!whole) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) odd |= flag[w] != 0;
+    }
+    if (__builtin_amdgcn_readfirstlane(odd)) {
+#pragma unroll
+      for (int t = 0; t < 2 * NB; ++t)
+        mma_seen<DT, DP>(acc, vt, 16 * t, tile_frag<DT>(s[t / 2], t % 2), lane, sees);
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2 * NB; ++t) {
+        const Frag8<DT> p = tile_frag<DT>(s[t / 2], t % 2);
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(vt, 16 * t, d, lane), p);
+      }
+    }
+  }
+  l = half_sum(l);
+  if (!row_ok) l = 0.0f;
+  const float ml = m == -__builtin_inff() ? 0.0f : m * c;
+  const int64_t row = (int64_t)bh * a.R + r;
+  if (a.parts == 1) {
+    store_owner<DT, DP>(acc, 1.0f / l, l != 0.0f,
+                        (char*)a.o + ((int64_t)b * a.os[0] + (int64_t)tok * a.os[1] + (int64_t)head * a.os[2]) * RT::EB,
+                        r < a.R, a.D, half);
+    if (a.lse && half == 0 && r < a.R) a.lse[row] = l == 0.0f ? __builtin_inff() : ml + __builtin_amdgcn_logf(l);
+  } else {
+    // part of a row: the unscaled sums, then maximum and sum
+    const int64_t rows = (int64_t)a.B * a.Hkv * a.R, at = (int64_t)part * rows + row;
+    store_owner<kF32, DP>(acc, 1.0f, true, (char*)(a.part + at * a.D), r < a.R, a.D, half);
+    if (half == 0 && r < a.R) {
+      float* const st = a.part + rows * a.parts * a.D + at * 2;
+      st[0] = l == 0.0f ? -__builtin_inff() : ml;
+      st[1] = l;
+    }
+  }
+}
+
+// Joins the parts of each row, in their order: four rows a workgroup.
+template <int DT>
+__global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
+  constexpr int EB = DT == kF32 ? 4 : 2;
+  const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63;
+  const float* const st = a.part + rows * a.parts * a.D;
+  float m = -__builtin_inff();
+  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, st[(p * rows + row) * 2]);
+  const float mu = m == -__builtin_inff() ? 0.0f : m;
+  float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  const bool c0 = lane < a.D, c1 = lane + 64 < a.D;
+  for (int p = 0; p < a.parts; ++p) {
+    const int64_t at = p * rows + row;
+    const float lp = st[at * 2 + 1];
+    if (lp == 0.0f) continue;
+    const float f = __builtin_amdgcn_exp2f(st[at * 2] - mu);
+    l += lp * f;
+    if (c0) o0 += a.part[at * a.D + lane] * f;
+    if (c1) o1 += a.part[at * a.D + lane + 64] * f;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  const int bh = (int)(row / a.R), r = (int)(row % a.R);
+  using E = typename Elem<DT>::T;
+  E* const o = (E*)((char*)a.o + ((int64_t)(bh / a.Hkv) * a.os[0] + (int64_t)(r / a.G) * a.os[1] +
+                                  (int64_t)((bh % a.Hkv) * a.G + r % a.G) * a.os[2]) * EB);
+  if (c0) o[lane] = (E)(o0 * inv);
+  if (c1) o[lane + 64] = (E)(o1 * inv);
+  if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? __builtin_inff() : mu + __builtin_amdgcn_logf(l);
+}
+
+// ---- query gradient --------------------------------------------------------
+// dq = scale sum_j ds_j k_j, ds_j = p_j (do . v_j - delta), p_j = exp2(c s_j - lse),
+// delta = do . o, which it writes for the kernel that follows.
+template <int DT, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
+  using RT = RowTile<DT, DP>;
+  constexpr int TK = attn_tile(DT), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // K 0, K 1, V 0, V 1, flags
+  int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+  const int nrt = (a.R + 32 * NW - 1) / (32 * NW);
+  const int rt = nrt - 1 - (int)(id % nrt), bh = (int)(id / nrt);
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int len = seq_len(a, b), start = seq_start(a, b);
+  const int g0 = rt * 32 * NW, g1 = min(g0 + 32 * NW, a.R) - 1;
+  const int w0 = g0 + wave * 32, w1 = min(w0 + 31, a.R - 1);
+  const KeyRange kg = key_range(a, g0, g1, len, start, TK);
+  KeyRange kw = key_range(a, w0, w1, len, start, TK);
+  if (w0 > w1) { kw.n = 0; kw.last = -1; kw.first = 1; kw.sink_end = 0; }
+  const int r = w0 + (lane & 31);
+  const int tok = min(r, a.R - 1) / a.G, pos = start + tok;
+  const int head = hk * a.G + min(r, a.R - 1) % a.G;
+  const bool row_ok = r < a.R && pos < len;
+  const int hi = row_ok ? min(len - 1, pos + a.right) : -1, lo = pos - a.left, sk = min(a.sinks, hi + 1);
+  auto at = [&](const void* p, const int64_t (&s)[3]) {
+    return (char*)p + ((int64_t)b * s[0] + (int64_t)tok * s[1] + (int64_t)head * s[2]) * RT::EB;
+  };
+  const char* const kb = (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2]) * RT::EB;
+  const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
+  const int64_t row = (int64_t)bh * a.R + r;
+  const float lse = row_ok ? a.lse[row] : __builtin_inff();
+  float delta = 0.0f;
+  if (row_ok) {
+    // each half of the wave takes every second chunk of the row
+    const char *const po = at(a.o, a.os), *const pg = at(a.go, a.gos);
+#pragma unroll 1
+    for (int e = half * RT::CE; e < a.D; e += 2 * RT::CE) {
+      const u32x4 vo = *reinterpret_cast<const u32x4*>(po + e * RT::EB), vg = *reinterpret_cast<const u32x4*>(pg + e * RT::EB);
+      const uint32_t wo[4] = {vo[0], vo[1], vo[2], vo[3]}, wg[4] = {vg[0], vg[1], vg[2], vg[3]};
+      float x[RT::CE], y[RT::CE];
+      raw_to_floats<DT, 4>(wo, x);
+      raw_to_floats<DT, 4>(wg, y);
+#pragma unroll
+      for (int j = 0; j < RT::CE; ++j) delta = __builtin_fmaf(x[j], y[j], delta);
+    }
+  }
+  delta = half_sum(delta);
+  if (half == 0 && r < a.R) a.delta[row] = delta;
+  Frag8<DT> qf[DP / 16], gf[DP / 16];
+  load_owner<DT, DP>(qf, at(a.q, a.qs), row_ok, a.D, half);
+  load_owner<DT, DP>(gf, at(a.go, a.gos), row_ok, a.D, half);
+
+  Stage<DT, DP, TK, NT> sk_, sv_;
+  auto load = [&](int i) {
+    const int k0 = kg.tile(i) * TK;
+    auto ok = [&](int rr) { return k0 + rr < len; };
+    sk_.load(tid, a.D, [&](int rr) { return kb + (int64_t)min(k0 + rr, len - 1) * a.ks[1] * RT::EB; }, ok);
+    sv_.load(tid, a.D, [&](int rr) { return vb + (int64_t)min(k0 + rr, len - 1) * a.vs[1] * RT::EB; }, ok);
+  };
+  floatx16 acc[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+  const float c = a.scale_log2e;
+  if (kg.n > 0) load(0);
+  for (int i = 0; i < kg.n; ++i) {
+    char* const kt = smem + (i & 1) * TB;
+    char* const vt = smem + (2 + (i & 1)) * TB;
+    int* const flag = flags + (i & 1) * NW;
+    sk_.store(tid, kt);
+    sv_.store(tid, vt);
+    {
+      ExpMax<DT> e;
+      sk_.scan(e);
+      const bool any = __any(e.hit());
+      if (lane == 0) flag[wave] = any;
+    }
+    __syncthreads();
+    const int k0 = kg.tile(i) * TK;
+    if (i + 1 < kg.n) load(i + 1);
+    if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;
+    const bool whole = k0 + TK - 1 <= kw.all_last && (k0 >= kw.all_first || k0 + TK <= kw.all_sink);
+    auto sees = [&](int k) {
+      const int j = k0 + k;
+      return j <= hi && (j >= lo || j < sk);
+    };
+    bool odd = false;
+    if (!whole) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) odd |= flag[w] != 0;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      floatx16 s{}, g{};
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) {
+        mma32<DT>(s, row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
+        mma32<DT>(g, row_frag<DT, DP>(vt, n * 32 + (lane & 31), t, half), gf[t]);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * (g[e] - delta);
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = 0.0f;
+      }
+      if (__builtin_amdgcn_readfirstlane(odd)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          mma_seen<DT, DP>(acc, kt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const Frag8<DT> p = tile_frag<DT>(s, t);
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(kt, n * 32 + 16 * t, d, lane), p);
+        }
+      }
+    }
+  }
+  store_owner<DT, DP>(acc, a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
+}
+
+// ---- key and value gradient ------------------------------------------------
+// dv_j = sum_r p_rj do_r, dk_j = scale sum_r ds_rj q_r over the packed rows r, a
+// contiguous run for each key.  A wave owns 32 keys; key tiles that hold first
+// tokens (seen by every later row) and tiles of long runs are split into parts
+// along the rows, whose fp32 sums a second kernel adds in order.
+template <int DT, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
+  using RT = RowTile<DT, DP>;
+  constexpr int TQ = attn_tile(DT), NT = NW * 64, NB = TQ / 32, TB = TQ * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // Q 0, Q 1, dO 0, dO 1, lse 0 1, delta 0 1, flags
+  float* const stats = reinterpret_cast<float*>(smem + 4 * TB);
+  int* const flags = reinterpret_cast<int*>(stats + 4 * TQ);
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
+  // workgroups of one head pair: sink tiles in sink_parts parts, then the others in key_parts
+  const uint32_t per = (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts);
+  const int bh = (int)(id / per);
+  int w = (int)(id % per), kt_, part, parts;
+  if (w < a.sink_tiles * a.sink_parts) {
+    parts = a.sink_parts;
+    kt_ = w / parts;
+    part = w % parts;
+  } else {
+    parts = a.key_parts;
+    kt_ = a.sink_tiles + (w - a.sink_tiles * a.sink_parts) / parts;
+    part = (w - a.sink_tiles * a.sink_parts) % parts;
+  }
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int len = seq_len(a, b), start = seq_start(a, b);
+  const int ends = min(len - 1 - start, a.Lq - 1);  // last token with data
+  // tokens that see some key of ja .. jb, and tokens that see all of them
+  auto tokens = [&](int ja, int jb, int& t0, int& t1, int& all0, int& all1) {
+    t0 = min(max(ja - a.right - start, 0), a.Lq);
+    t1 = ja < len ? ja < a.sinks ? ends : min(ends, jb + a.left - start) : -1;
+    all0 = min(max(jb - a.right - start, 0), a.Lq);
+    all1 = jb < len ? jb < a.sinks ? ends : min(ends, ja + a.left - start) : -1;
+  };
+  const int j0 = kt_ * 32 * NW, jw = j0 + wave * 32, j = jw + (lane & 31);
+  int g0, g1, w0, w1, f0, f1, l0, l1, u0, u1;
+  tokens(j0, j0 + 32 * NW - 1, g0, g1, u0, u1);
+  tokens(jw, jw + 31, w0, w1, f0, f1);
+  tokens(j, j, l0, l1, u0, u1);
+  const int rlo = l0 * a.G, rhi = l1 < l0 ? -1 : l1 * a.G + a.G - 1;  // rows that see the lane's key
+  const int wlo = w0 * a.G, whi = w1 < w0 ? -1 : w1 * a.G + a.G - 1;
+  const int flo = f0 * a.G, fhi = f1 < f0 ? -1 : f1 * a.G + a.G - 1;
+
+  Frag8<DT> kf[DP / 16], vf[DP / 16];
+  {
+    const int jc = min(j, len - 1);
+    load_owner<DT, DP>(kf, (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)jc * a.ks[1] + (int64_t)hk * a.ks[2]) * RT::EB,
+                       j < len, a.D, half);
+    load_owner<DT, DP>(vf, (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)jc * a.vs[1] + (int64_t)hk * a.vs[2]) * RT::EB,
+                       j < len, a.D, half);
+  }
+  const int tq0 = g0 * a.G / TQ, nt = g1 < g0 ? 0 : (g1 * a.G + a.G - 1) / TQ - tq0 + 1;
+  const int i0 = (int)((int64_t)nt * part / parts), i1 = (int)((int64_t)nt * (part + 1) / parts);
+  const int rend = max(ends + 1, 0) * a.G;  // rows with data
+  const char* const qb = (const char*)a.q + ((int64_t)b * a.qs[0] + (int64_t)hk * a.G * a.qs[2]) * RT::EB;
+  const char* const gb = (const char*)a.go + ((int64_t)b * a.gos[0] + (int64_t)hk * a.G * a.gos[2]) * RT::EB;
+  Stage<DT, DP, TQ, NT> sq, sg;
+  float st_lse = 0.0f, st_delta = 0.0f;
+  auto load = [&](int i) {
+    const int r0 = (tq0 + i) * TQ;
+    auto ok = [&](int rr) { return r0 + rr < rend; };
+    auto addr = [&](const char* base, const int64_t (&s)[3], int rr) {
+      const unsigned x = (unsigned)min(r0 + rr, rend - 1), t = x / (unsigned)a.G;
+      return base + ((int64_t)t * s[1] + (int64_t)(x - t * a.G) * s[2]) * RT::EB;
+    };
+    sq.load(tid, a.D, [&](int rr) { return addr(qb, a.qs, rr); }, ok);
+    sg.load(tid, a.D, [&](int rr) { return addr(gb, a.gos, rr); }, ok);
+    if (tid < TQ) {
+      const int64_t at = (int64_t)bh * a.R + min(r0 + tid, rend - 1);
+      st_lse = ok(tid) ? a.lse[at] : __builtin_inff();
+      st_delta = ok(tid) ? a.delta[at] : 0.0f;
+    }
+  };
+  floatx16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = floatx16{};
+  const float c = a.scale_log2e;
+  if (i0 < i1) load(i0);
+  for (int i = i0; i < i1; ++i) {
+    char* const qt = smem + (i & 1) * TB;
+    char* const gt = smem + (2 + (i & 1)) * TB;
+    float* const ls = stats + (i & 1) * TQ;
+    float* const de = stats + (2 + (i & 1)) * TQ;
+    int* const flag = flags + (i & 1) * NW;
+    sq.store(tid, qt);
+    sg.store(tid, gt);
+    if (tid < TQ) {
+      ls[tid] = st_lse;
+      de[tid] = st_delta;
+    }
+    {
+      ExpMax<DT> e;
+      sq.scan(e);
+      sg.scan(e);
+      const bool any = __any(e.hit());
+      if (lane == 0) flag[wave] = any;
+    }
+    __syncthreads();
+    const int r0 = (tq0 + i) * TQ;
+    if (i + 1 < i1) load(i + 1);
+    if (r0 > whi || r0 + TQ <= wlo) continue;
+    const bool whole = r0 >= flo && r0 + TQ - 1 <= fhi;
+    auto sees = [&](int k) { return r0 + k >= rlo && r0 + k <= rhi; };
+    bool odd = false;
+    if (!whole) {
+#pragma unroll
+      for (int x = 0; x < NW; ++x) odd |= flag[x] != 0;
+    }
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+      floatx16 s{}, g{};
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t) {
+        mma32<DT>(s, row_frag<DT, DP>(qt, n * 32 + (lane & 31), t, half), kf[t]);
+        mma32<DT>(g, row_frag<DT, DP>(gt, n * 32 + (lane & 31), t, half), vf[t]);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const floatx4 le = *reinterpret_cast<const floatx4*>(ls + n * 32 + 8 * x + 4 * half);
+        const floatx4 dl = *reinterpret_cast<const floatx4*>(de + n * 32 + 8 * x + 4 * half);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int e = 4 * x + y;
+          s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -le[y]));
+          g[e] = s[e] * (g[e] - dl[y]);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = g[e] = 0.0f;
+      }
+      if (__builtin_amdgcn_readfirstlane(odd)) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          mma_seen<DT, DP>(dv, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
+          mma_seen<DT, DP>(dk, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), lane, sees);
+        }
+      } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const Frag8<DT> p = tile_frag<DT>(s, t), ds = tile_frag<DT>(g, t);
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) {
+            mma32<DT>(dv[d], col_frag<DT, DP>(gt, n * 32 + 16 * t, d, lane), p);
+            mma32<DT>(dk[d], col_frag<DT, DP>(qt, n * 32 + 16 * t, d, lane), ds);
+          }
+        }
+      }
+    }
+  }
+  if (parts == 1) {
+    const bool ok = j < a.Lk;
+    store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
+                        ok, a.D, half);
+    store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
+                        ok, a.D, half);
+  } else {
+    // slot of this workgroup among the split ones of its head pair: [slot][dk, dv][key][D]
+    const int64_t slots = (int64_t)a.sink_tiles * (a.sink_parts > 1 ? a.sink_parts : 0) +
+                          (int64_t)(a.key_tiles - a.sink_tiles) * (a.key_parts > 1 ? a.key_parts : 0);
+    const int slot = a.sink_parts > 1 ? w : w - a.sink_tiles;
+    float* const p = a.part + ((bh * slots + slot) * 2 * (32 * NW) + (j - j0)) * a.D;
+    store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
+    store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)32 * NW * a.D), true, a.D, half);
+  }
+}
+
+// Adds the parts of split key tiles in their order.  One workgroup a split tile,
+// head pair and gradient.
+template <int DT>
+__global__ __launch_bounds__(256) void eql_wattn_dkv_sum_kernel(AttnArgs a, int keys) {
+  using E = typename Elem<DT>::T;
+  const int split_sinks = a.sink_parts > 1 ? a.sink_tiles : 0;
+  const int split_keys = a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0;
+  const int per = split_sinks + split_keys;
+  const int which = blockIdx.x % 2;
+  const int x = (int)((blockIdx.x / 2) % per), bh = (int)((blockIdx.x / 2) / per);
+  const int64_t slots = (int64_t)split_sinks * a.sink_parts + (int64_t)split_keys * a.key_parts;
+  int tile, parts;
+  int64_t slot;
+  if (x < split_sinks) {
+    tile = x;
+    parts = a.sink_parts;
+    slot = (int64_t)x * parts;
+  } else {
+    tile = a.sink_tiles + x - split_sinks;
+    parts = a.key_parts;
+    slot = (int64_t)split_sinks * a.sink_parts + (int64_t)(x - split_sinks) * parts;
+  }
+  const int b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int64_t one = (int64_t)2 * keys * a.D;
+  const float* const src = a.part + (bh * slots + slot) * one + (int64_t)which * keys * a.D;
+  const int64_t* const st = which ? a.dvs : a.dks;
+  E* const dst = (E*)(which ? a.dv : a.dk) + (int64_t)b * st[0] + (int64_t)hk * st[2];
+  const int n = min(keys, a.Lk - tile * keys) * a.D;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    float s = 0.0f;
+    for (int p = 0; p < parts; ++p) s += src[p * one + i];
+    dst[(int64_t)(tile * keys + i / a.D) * st[1] + i % a.D] = (E)s;
+  }
+}
+
+}  // namespace eqk

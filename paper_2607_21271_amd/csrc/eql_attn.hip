@@ -1,0 +1,105 @@
+// eql_attn.hip -- windowed attention (eql_attn.h): instantiations, plans and
+// launches of one element type (EQK_DT).
+#include "eql_attn.h"
+#include "eql_launch.h"
+
+namespace eqk {
+namespace {
+
+constexpr int DT = EQK_DT;
+constexpr int kEB = DT == kF32 ? 4 : 2;
+
+constexpr int tile_bytes(int DP) { return attn_tile(DT) * (DP == 96 ? 128 : DP) * kEB; }
+constexpr int fwd_lds(int DP, int NW) { return 4 * tile_bytes(DP) + 2 * NW * 4; }
+constexpr int dkv_lds(int DP) { return 4 * tile_bytes(DP) + 4 * attn_tile(DT) * 4 + 2 * 4 * 4; }
+
+template <typename K>
+hipError_t launch(K k, int64_t blocks, int threads, int lds, hipStream_t stream, const AttnArgs& a) {
+  if (lds > 65536) {
+    const hipError_t e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(threads), lds, stream, a);
+  return hipGetLastError();
+}
+
+template <int DP>
+hipError_t fwd(const AttnArgs& a, int waves, hipStream_t stream) {
+  const int64_t n = (int64_t)a.B * a.Hkv * ((a.R + 32 * waves - 1) / (32 * waves)) * a.parts;
+  return waves == 1 ? launch(eql_wattn_fwd_kernel<DT, DP, 1>, n, 64, fwd_lds(DP, 1), stream, a)
+                    : launch(eql_wattn_fwd_kernel<DT, DP, 4>, n, 256, fwd_lds(DP, 4), stream, a);
+}
+
+template <int DP>
+hipError_t bwd(const AttnArgs& a, hipStream_t stream) {
+  const int64_t nq = (int64_t)a.B * a.Hkv * ((a.R + 127) / 128);
+  if (nq > 0) {
+    const hipError_t e = launch(eql_wattn_dq_kernel<DT, DP, 4>, nq, 256, fwd_lds(DP, 4), stream, a);
+    if (e != hipSuccess) return e;
+  }
+  const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
+  if (per == 0) return hipSuccess;
+  return launch(eql_wattn_dkv_kernel<DT, DP, kAttnDkvKeys / 32>, (int64_t)a.B * a.Hkv * per, 256, dkv_lds(DP), stream, a);
+}
+
+// The sequences of one launch: fewer than 2^32 threads.
+AttnArgs slice(const AttnArgs& a, int b0, int n) {
+  AttnArgs s = a;
+  auto in = [&](const void* p, const int64_t (&st)[3]) { return p ? (const char*)p + b0 * st[0] * kEB : nullptr; };
+  auto out = [&](void* p, const int64_t (&st)[3]) { return p ? (char*)p + b0 * st[0] * kEB : nullptr; };
+  s.q = in(a.q, a.qs); s.k = in(a.k, a.ks); s.v = in(a.v, a.vs); s.go = in(a.go, a.gos);
+  s.o = out(a.o, a.os); s.dq = out(a.dq, a.dqs); s.dk = out(a.dk, a.dks); s.dv = out(a.dv, a.dvs);
+  if (a.lengths) s.lengths = a.lengths + b0;
+  if (a.starts) s.starts = a.starts + b0;
+  if (a.lse) s.lse = a.lse + (int64_t)b0 * a.Hkv * a.R;
+  if (a.delta) s.delta = a.delta + (int64_t)b0 * a.Hkv * a.R;
+  s.B = n;
+  return s;
+}
+
+}  // namespace
+
+template <>
+hipError_t wattn_fwd<DT>(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
+  const int64_t per = (int64_t)a.Hkv * ((a.R + 32 * p.waves - 1) / (32 * p.waves)) * p.parts;
+  const int64_t most = p.parts > 1 ? a.B : launch_blocks(64 * p.waves) / per;  // parts are planned for small grids only
+  if (most < 1) return hipErrorInvalidValue;
+  for (int64_t b0 = 0; b0 < a.B; b0 += most) {
+    AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
+    s.parts = p.parts;
+    hipError_t e = a.D <= 32   ? fwd<32>(s, p.waves, stream)
+                   : a.D <= 64 ? fwd<64>(s, p.waves, stream)
+                   : a.D <= 96 ? fwd<96>(s, p.waves, stream)
+                               : fwd<128>(s, p.waves, stream);
+    if (e == hipSuccess && p.parts > 1)
+      e = launch(eql_wattn_join_kernel<DT>, ((int64_t)s.B * s.Hkv * s.R + 3) / 4, 256, 0, stream, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <>
+hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
+  const bool split = a.part != nullptr;
+  const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
+  const int64_t rows = (a.R + 127) / 128;
+  const int64_t most = split ? a.B : launch_blocks(256) / (a.Hkv * (per > rows ? per : rows));
+  if (most < 1) return hipErrorInvalidValue;
+  for (int64_t b0 = 0; b0 < a.B; b0 += most) {
+    const AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
+    hipError_t e = a.D <= 32   ? bwd<32>(s, stream)
+                   : a.D <= 64 ? bwd<64>(s, stream)
+                   : a.D <= 96 ? bwd<96>(s, stream)
+                               : bwd<128>(s, stream);
+    if (e == hipSuccess && split) {
+      const int64_t tiles = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0);
+      hipLaunchKernelGGL(eql_wattn_dkv_sum_kernel<DT>, dim3((unsigned)(2 * tiles * s.B * s.Hkv)), dim3(256), 0, stream, s,
+                         kAttnDkvKeys);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace eqk

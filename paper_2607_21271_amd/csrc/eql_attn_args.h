@@ -1,0 +1,56 @@
+// eql_attn_args.h -- arguments and launch plan of the windowed attention kernels,
+// shared by host and device code.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "eql_config.h"
+
+namespace eqk {
+
+// Lengths and first positions stay within 2^28 and packed rows below 2^29; a side
+// of the window without a limit is 2^29, past every key from every position.
+// Sums of three of them fit 32 bits.
+constexpr int kAttnMaxPos = 1 << 28;
+constexpr int kAttnNoLimit = 1 << 29;
+constexpr int kAttnMaxD = 128;
+
+struct AttnArgs {
+  const void *q, *k, *v, *go;
+  void *o, *dq, *dk, *dv;
+  const int *lengths, *starts;  // per sequence, or null
+  float *lse, *delta;           // [B, Hkv, R], log2 units
+  float* part;                  // fp32 parts of split rows or keys
+  int64_t qs[3], ks[3], vs[3], os[3], gos[3], dqs[3], dks[3], dvs[3];  // elements: sequence, token, head
+  int B, Lq, Lk, Hkv, G, R, D;
+  int left, right, sinks;
+  float scale, scale_log2e;
+  int parts;                                        // forward: parts of a row's keys
+  int key_tiles, sink_tiles, key_parts, sink_parts; // key/value gradient
+};
+
+// streamed rows of a tile
+constexpr int attn_tile(int dt) { return dt == kF32 ? 32 : 64; }
+
+// Waves of a forward workgroup over R packed rows, and the parts that the keys are split into.
+struct AttnPlan {
+  int waves, parts;
+};
+AttnPlan attn_plan(const AttnArgs& a, int dt, int cus);
+size_t attn_part_bytes(const AttnArgs& a, const AttnPlan& p);
+// Fills key_tiles .. sink_parts; returns the bytes of the parts.
+constexpr int kAttnDkvKeys = 128;  // keys of a workgroup
+size_t attn_dkv_plan(AttnArgs& a, int dt, int cus);
+
+template <int DT>
+hipError_t wattn_fwd(const AttnArgs& a, const AttnPlan& p, hipStream_t stream);
+template <int DT>
+hipError_t wattn_bwd(const AttnArgs& a, hipStream_t stream);
+template <> hipError_t wattn_fwd<kF32>(const AttnArgs&, const AttnPlan&, hipStream_t);
+template <> hipError_t wattn_fwd<kF16>(const AttnArgs&, const AttnPlan&, hipStream_t);
+template <> hipError_t wattn_fwd<kBF16>(const AttnArgs&, const AttnPlan&, hipStream_t);
+template <> hipError_t wattn_bwd<kF32>(const AttnArgs&, hipStream_t);
+template <> hipError_t wattn_bwd<kF16>(const AttnArgs&, hipStream_t);
+template <> hipError_t wattn_bwd<kBF16>(const AttnArgs&, hipStream_t);
+
+}  // namespace eqk

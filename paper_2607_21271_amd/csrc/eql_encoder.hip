@@ -1,0 +1,103 @@
+// eql_encoder.hip -- instantiations and launches of the rotary (eql_rotary.h) and
+// group-norm (eql_gnact.h) kernels.
+#include "eql_encoder.h"
+#include "eql_launch.h"
+
+namespace eqk {
+namespace {
+
+template <int DT, int VEC>
+hipError_t rotary_v(const RotaryArgs& a, hipStream_t stream) {
+  const int64_t blocks = (a.tokens + a.TB - 1) / a.TB;
+  if (blocks > launch_blocks(256)) return hipErrorInvalidValue;
+  if constexpr (VEC > 1) {
+    if (a.interleaved && a.T == 1) {
+      hipLaunchKernelGGL((eql_rotary_kernel<DT, VEC, true>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((eql_rotary_kernel<DT, VEC, false>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t rotary_dt(const RotaryArgs& a, int vec, hipStream_t stream) {
+  if constexpr (DT != kF32)
+    if (vec == 8) return rotary_v<DT, 8>(a, stream);
+  if (vec == 4) return rotary_v<DT, 4>(a, stream);
+  if (vec == 2) return rotary_v<DT, 2>(a, stream);
+  return rotary_v<DT, 1>(a, stream);
+}
+
+template <int DT, int VEC>
+hipError_t gn_fwd_v(const GnArgs& a, hipStream_t stream) {
+  const unsigned n = (unsigned)(a.B * a.chunks * a.cblocks);
+  hipLaunchKernelGGL((eql_gn_sums_kernel<DT, VEC>), dim3(n), dim3(256), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  auto k = a.act == kActRelu   ? eql_gn_map_kernel<DT, VEC, kActRelu>
+           : a.act == kActSilu ? eql_gn_map_kernel<DT, VEC, kActSilu>
+           : a.act == kActGelu ? eql_gn_map_kernel<DT, VEC, kActGelu>
+                               : eql_gn_map_kernel<DT, VEC, kActNone>;
+  hipLaunchKernelGGL(k, dim3(n), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+template <int DT, int VEC, int ACT>
+hipError_t gn_bwd_a(const GnArgs& a, hipStream_t stream) {
+  const unsigned n = (unsigned)(a.B * a.chunks * a.cblocks);
+  hipLaunchKernelGGL((eql_gn_bsums_kernel<DT, VEC, ACT>), dim3(n), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL((eql_gn_bmean_kernel<DT>), dim3((unsigned)((a.B * a.G + 3) / 4)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL((eql_gn_bmap_kernel<DT, VEC, ACT>), dim3(n + (unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+template <int DT, int VEC>
+hipError_t gn_bwd_v(const GnArgs& a, hipStream_t stream) {
+  if (a.act == kActRelu) return gn_bwd_a<DT, VEC, kActRelu>(a, stream);
+  if (a.act == kActSilu) return gn_bwd_a<DT, VEC, kActSilu>(a, stream);
+  if (a.act == kActGelu) return gn_bwd_a<DT, VEC, kActGelu>(a, stream);
+  return gn_bwd_a<DT, VEC, kActNone>(a, stream);
+}
+
+// Whole 16-byte vectors, or single elements where a row of K is none.
+template <int DT>
+hipError_t gn_dt(const GnArgs& a, int vec, bool bwd, hipStream_t stream) {
+  constexpr int W = DT == kF32 ? 4 : 8;
+  if (vec == W) return bwd ? gn_bwd_v<DT, W>(a, stream) : gn_fwd_v<DT, W>(a, stream);
+  return bwd ? gn_bwd_v<DT, 1>(a, stream) : gn_fwd_v<DT, 1>(a, stream);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(int dt, const RotaryArgs& a, int vec, hipStream_t stream) {
+  if (dt == kF32) return rotary_dt<kF32>(a, vec, stream);
+  if (dt == kF16) return rotary_dt<kF16>(a, vec, stream);
+  return rotary_dt<kBF16>(a, vec, stream);
+}
+
+// About four workgroups a CU over all sequences, and at least four positions for each thread.
+void gn_plan(GnArgs& a, int vec, int cus) {
+  const int nv = a.K / vec;
+  a.cblocks = (nv + 255) / 256;
+  const int step = nv >= 256 ? 1 : 256 / nv;
+  int64_t chunks = (4 * (int64_t)cus + a.B * a.cblocks - 1) / (a.B * a.cblocks);
+  const int64_t most = (a.S + 4 * step - 1) / (4 * step);
+  if (chunks > most) chunks = most;
+  if (chunks < 1) chunks = 1;
+  a.rows = (int)((a.S + chunks - 1) / chunks);
+  a.chunks = (int)((a.S + a.rows - 1) / a.rows);
+}
+
+hipError_t launch_gn_forward(int dt, const GnArgs& a, int vec, hipStream_t stream) {
+  if (dt == kF32) return gn_dt<kF32>(a, vec, false, stream);
+  if (dt == kF16) return gn_dt<kF16>(a, vec, false, stream);
+  return gn_dt<kBF16>(a, vec, false, stream);
+}
+
+hipError_t launch_gn_backward(int dt, const GnArgs& a, int vec, hipStream_t stream) {
+  if (dt == kF32) return gn_dt<kF32>(a, vec, true, stream);
+  if (dt == kF16) return gn_dt<kF16>(a, vec, true, stream);
+  return gn_dt<kBF16>(a, vec, true, stream);
+}
+
+}  // namespace eqk

@@ -1,0 +1,108 @@
+"""Group norm with an activation over channels-last equivariant features [B, ..., C, T].
+
+    z = (x - mean) / sqrt(var + eps) * weight[c] + bias[c],   y = act(z)
+
+with the statistics of each sequence (image) taken over its positions, the channels of a group and the group axis T, and
+one weight and bias per channel, shared over T: the map commutes with the group action, so it stands between the layers
+of ``gconv``.  This module allocates and marshals; ``eqlinear_group_norm_act`` and its backward compute.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import _lib, ops
+
+ACTIVATIONS = {"none": _lib.EQL_ACT_NONE, "relu": _lib.EQL_ACT_RELU, "silu": _lib.EQL_ACT_SILU,
+               "gelu": _lib.EQL_ACT_GELU}
+
+
+def _ready(t: torch.Tensor) -> torch.Tensor:
+    t = t.contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
+def _dims(x):
+    C, T = x.shape[-2:]
+    B = x.shape[0]
+    S = 1
+    for n in x.shape[1:-2]:
+        S *= n
+    return B, S, T, C
+
+
+def _forward(x, weight, bias, groups, act, eps, want_stats, stream=None):
+    B, S, T, C = _dims(x)
+    dt = ops._DT[x.dtype]
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty(B, groups, 2, dtype=torch.float32, device=x.device) if want_stats else None
+    need = _lib.eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dt)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    _lib.check(_lib.eqlinear_group_norm_act(ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(y), ops._ptr(stats),
+                                            ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt, ops._stream(stream)),
+               "eqlinear_group_norm_act")
+    return y, stats
+
+
+class GroupNormActFunction(torch.autograd.Function):
+    """Autograd: gradients of x, weight and bias in one call."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, groups, act, eps):
+        x, weight, bias = _ready(x), weight.contiguous(), bias.contiguous()
+        y, stats = _forward(x, weight, bias, groups, act, eps, True)
+        ctx.save_for_backward(x, weight, bias, stats)
+        ctx.args = (groups, act)
+        return y
+
+    @staticmethod
+    def backward(ctx, gy):
+        x, weight, bias, stats = ctx.saved_tensors
+        groups, act = ctx.args
+        B, S, T, C = _dims(x)
+        dt = ops._DT[x.dtype]
+        gy = _ready(gy)
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if x.numel() == 0:
+            return dx, torch.zeros_like(weight), torch.zeros_like(bias), None, None, None
+        dw, db = torch.empty_like(weight), torch.empty_like(bias)
+        need = _lib.eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dt)
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        _lib.check(_lib.eqlinear_group_norm_act_backward(
+            ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(stats), ops._ptr(gy), ops._ptr(dx), ops._ptr(dw),
+            ops._ptr(db), ops._ptr(ws), need, B, S, T, C, groups, act, dt, ops._stream(None)),
+            "eqlinear_group_norm_act_backward")
+        return dx, dw, db, None, None, None
+
+
+def group_norm_act(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, groups: int, activation: str = "none",
+                   eps: float = 1e-5) -> torch.Tensor:
+    """y of x's shape [B, ..., C, T]; weight and bias [C]; ``activation`` none, relu, silu or gelu (by erf)."""
+    ops._dtype_code(x)
+    ops._check_same_dtype(x, weight=weight, bias=bias)
+    if x.dim() < 3:
+        raise ValueError("x must be [B, ..., C, T], got %s" % (tuple(x.shape),))
+    C = x.shape[-2]
+    if tuple(weight.shape) != (C,) or tuple(bias.shape) != (C,):
+        raise ValueError("weight and bias must be [%d], got %s and %s" % (C, tuple(weight.shape), tuple(bias.shape)))
+    if groups < 1 or C % groups:
+        raise ValueError("%d channels do not divide into %d groups" % (C, groups))
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s, got %r" % (", ".join(ACTIVATIONS), activation))
+    ops._check_dev(x, weight, bias)
+    act = ACTIVATIONS[activation]
+    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias.requires_grad):
+        return GroupNormActFunction.apply(x, weight, bias, groups, act, float(eps))
+    return _forward(_ready(x), weight.contiguous(), bias.contiguous(), groups, act, float(eps), False)[0]
+
+
+class GroupNormAct(torch.nn.Module):
+    """Group norm with an activation: [B, ..., C, T] -> the same shape."""
+
+    def __init__(self, C: int, groups: int, activation: str = "none", eps: float = 1e-5, device=None, dtype=None):
+        super().__init__()
+        self.groups, self.activation, self.eps = groups, activation, eps
+        self.weight = torch.nn.Parameter(torch.ones(C, device=device, dtype=dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(C, device=device, dtype=dtype))
+
+    def forward(self, x):
+        return group_norm_act(x, self.weight, self.bias, self.groups, self.activation, self.eps)

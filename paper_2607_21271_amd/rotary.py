@@ -1,0 +1,125 @@
+"""Rotary positions with several axes (time, height, width) for the heads of an equivariant encoder.
+
+A token at positions p[a] turns channel pair c of every head by phi = p[axis(c)] * freqs[c]; the group elements of a
+channel turn alike, so the map commutes with the group action (rolling the T axis).  Scores of turned queries and
+keys then depend on the tokens' offsets along each axis only.  This module allocates and marshals;
+``eqlinear_rotary`` computes.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import _lib, ops
+
+
+def axis_frequencies(sections, theta=10000.0, device=None) -> torch.Tensor:
+    """Frequencies [sum(sections)], theta**(-i / n) for pair i of an axis of n pairs; ``theta`` a number or one per axis."""
+    thetas = [float(theta)] * len(sections) if not hasattr(theta, "__len__") else [float(t) for t in theta]
+    if len(thetas) != len(sections):
+        raise ValueError("theta has %d values for %d axes" % (len(thetas), len(sections)))
+    f = [t ** (-torch.arange(n, dtype=torch.float64) / max(n, 1)) for n, t in zip(sections, thetas)]
+    return torch.cat(f).float().to(device)
+
+
+def grid_positions(shape, prefix: int = 0, device=None) -> torch.Tensor:
+    """Positions [prefix + prod(shape), len(shape)] (int32) of a grid of tokens in raster order, the first axis slowest,
+    after ``prefix`` tokens (class and register tokens) at the origin, which do not turn."""
+    axes = torch.meshgrid(*(torch.arange(n, dtype=torch.int32) for n in shape), indexing="ij")
+    grid = torch.stack([a.reshape(-1) for a in axes], -1)
+    return torch.cat((torch.zeros(prefix, len(shape), dtype=torch.int32), grid)).to(device)
+
+
+def _strides(x):
+    """Strides of [B, L, N] with the axes of size 1 counted as 0."""
+    return tuple(x.stride(i) if x.shape[i] > 1 else 0 for i in range(3))
+
+
+def _launch(x, positions, freqs, sections, T, interleaved, inverse, y, stream=None):
+    B, L, N, D = x.shape
+    pos = positions.stride()
+    pst = (pos[0], pos[1]) if positions.dim() == 3 else (0, pos[0])
+    shape = _lib.RotaryShape(B, L, N, D // T, T, len(sections), tuple(sections), positions.dtype == torch.float32,
+                             interleaved, inverse, ops._DT[x.dtype], _strides(x), _strides(y), pst)
+    _lib.check(_lib.eqlinear_rotary(ctypes.byref(shape), ops._ptr(x), ops._ptr(positions), ops._ptr(freqs), ops._ptr(y),
+                                    ops._stream(stream)), "eqlinear_rotary")
+    return y
+
+
+def _rows(x):
+    """x itself where its heads are contiguous, in non-negative strides, else a contiguous copy."""
+    return x if x.stride(3) == 1 or x.shape[3] == 1 else x.contiguous()
+
+
+def _check(x, positions, freqs, sections, T):
+    ops._dtype_code(x)
+    if x.dim() != 4:
+        raise ValueError("x must be [B, L, heads, dh * T], got %s" % (tuple(x.shape),))
+    B, L, _, D = x.shape
+    if T < 1 or D % T:
+        raise ValueError("head size %d is not a multiple of T = %d" % (D, T))
+    if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) < 1 or 2 * sum(sections) > D // T:
+        raise ValueError("sections %s do not fit %d channels (two to a pair, at most 4 axes)" % (tuple(sections), D // T))
+    want = (L, len(sections))
+    if tuple(positions.shape) not in (want, (B,) + want):
+        raise ValueError("positions must be %s or %s, got %s" % (want, (B,) + want, tuple(positions.shape)))
+    if positions.dtype not in (torch.int32, torch.float32):
+        raise TypeError("positions must be int32 or float32, got %s" % positions.dtype)
+    if freqs.dtype != torch.float32 or tuple(freqs.shape) != (sum(sections),):
+        raise ValueError("freqs must be float32 [%d], got %s %s" % (sum(sections), freqs.dtype, tuple(freqs.shape)))
+    ops._check_dev(x, positions, freqs)
+
+
+class RotaryFunction(torch.autograd.Function):
+    """Autograd: the gradient of x is the inverse turn of the gradient of y; positions and frequencies get none."""
+
+    @staticmethod
+    def forward(ctx, x, positions, freqs, sections, T, interleaved, inverse):
+        ctx.save_for_backward(positions, freqs)
+        ctx.args = (sections, T, interleaved, inverse)
+        x = _rows(x)
+        return _launch(x, positions, freqs, sections, T, interleaved, inverse,
+                       torch.empty(x.shape, dtype=x.dtype, device=x.device))
+
+    @staticmethod
+    def backward(ctx, gy):
+        positions, freqs = ctx.saved_tensors
+        sections, T, interleaved, inverse = ctx.args
+        gy = _rows(gy)
+        gx = _launch(gy, positions, freqs, sections, T, interleaved, not inverse,
+                     torch.empty(gy.shape, dtype=gy.dtype, device=gy.device))
+        return gx, None, None, None, None, None, None
+
+
+def rotary_axes(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, sections, T: int = 1,
+                interleaved: bool = False, inverse: bool = False) -> torch.Tensor:
+    """x [B, L, heads, dh * T] with its first 2 * sum(sections) channels turned (a new tensor).
+
+    positions [L, axes] or [B, L, axes] (int32 or float32), freqs [sum(sections)] (``axis_frequencies``); sections[a]
+    pairs turn by axis a.  Pairs are channels (c, c + sum(sections)), or (2c, 2c + 1) where ``interleaved``.
+    x may be a view with strides (the queries and keys of a packed buffer).  Differentiable in x."""
+    sections = tuple(int(s) for s in sections)
+    _check(x, positions, freqs, sections, T)
+    if positions.stride(-1) != 1:
+        positions = positions.contiguous()
+    freqs = freqs.contiguous()
+    if x.requires_grad and torch.is_grad_enabled():
+        return RotaryFunction.apply(x, positions, freqs, sections, T, interleaved, inverse)
+    x = _rows(x)
+    return _launch(x, positions, freqs, sections, T, interleaved, inverse,
+                   torch.empty(x.shape, dtype=x.dtype, device=x.device))
+
+
+def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, sections, T: int = 1,
+                 interleaved: bool = False, inverse: bool = False) -> torch.Tensor:
+    """``rotary_axes`` in place, on x or on a view of it; not recorded by autograd, so x must not need a gradient."""
+    sections = tuple(int(s) for s in sections)
+    _check(x, positions, freqs, sections, T)
+    if x.requires_grad and torch.is_grad_enabled():
+        raise ValueError("rotary_axes_ is not differentiable; use rotary_axes")
+    if x.stride(3) != 1 and x.shape[3] != 1:
+        raise ValueError("the elements of a head must be contiguous to turn in place")
+    if positions.stride(-1) != 1:
+        positions = positions.contiguous()
+    return _launch(x, positions, freqs.contiguous(), sections, T, interleaved, inverse, x)
