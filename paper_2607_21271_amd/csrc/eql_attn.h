@@ -22,6 +22,8 @@
 // tile, the next tile's loads in flight during the products, rows past the
 // sequence and elements past the head dimension set to zero on the way.
 #pragma once
+#include <type_traits>
+
 #include "eql_attn_args.h"
 #include "eql_common.h"
 #include "eql_config.h"
@@ -185,6 +187,7 @@ __device__ __forceinline__ void mma_seen(floatx16 (&acc)[DP / 32], const char* t
                                          F&& sees) {
   constexpr int NR = DT == kF32 ? 8 : 4;
   constexpr uint32_t kMask = ExpMax<DT>::kMask;
+  asm volatile("" : "+v"(lane));  // keeps this rare path's addresses out of the registers of the common one
   const int half = lane >> 5;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) {
@@ -217,6 +220,18 @@ __device__ __forceinline__ void mma_seen(floatx16 (&acc)[DP / 32], const char* t
       for (int e = 0; e < 16; ++e) acc[d][e] += s ? p[e] : 0.0f;
     }
   }
+}
+
+// Whether a wave of the workgroup found infinities or NaN in the tile; the same in
+// every wave.  The kernels walk their tiles on the assumption that there are none where
+// they would matter (a tile that some owner sees in part) and, where it fails,
+// start over with mma_seen: the common loop then carries nothing for it.
+template <int NW>
+__device__ __forceinline__ bool any_flag(const int* flag) {
+  int f = 0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) f |= flag[w];
+  return __builtin_amdgcn_readfirstlane(f) != 0;
 }
 
 // Loads of one streamed tile of TK rows by NT threads, held in registers between
@@ -315,6 +330,10 @@ struct KeyRange {
   int first;              // no row sees before `first`, first tokens aside
   int all_first, all_last, all_sink;  // keys every row sees: all_first .. all_last and below all_sink
   __device__ __forceinline__ int tile(int i) const { return i < ns ? i : t0 + i - ns; }
+  // whether every row sees the whole tile from key k0 on
+  __device__ __forceinline__ bool whole(int k0, int TK) const {
+    return k0 + TK - 1 <= all_last && (k0 >= all_first || k0 + TK <= all_sink);
+  }
 };
 __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, int r0, int r1, int len, int start, int TK) {
   KeyRange k{};
@@ -346,12 +365,14 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n) {
 // a tile's maximum exceeds it by 2^8: probabilities stay below 2^8, far inside
 // fp16's range.  Scores, maxima and sums in fp32; a probability is
 // rounded once to the element type, as the operand of the second product.
+// Up to 32 rows take one wave to a workgroup (more parts, no wait for other waves):
+// it reads its LDS in order, so one buffer does.
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql_wattn_fwd_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
-  constexpr int TK = attn_tile(DT), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // K 0, K 1, V 0, V 1, flags
-  int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
+  constexpr int TK = attn_fwd_tile(DT, NW), NBUF = attn_fwd_bufs(NW), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // K buffers, V buffers, flags
+  int* const flags = reinterpret_cast<int*>(smem + 2 * NBUF * TB);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
   const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
@@ -389,87 +410,96 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
   };
 
   floatx16 acc[DP / 32];
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
-  float m = -__builtin_inff(), l = 0.0f;
+  float m, l;
   const float c = a.scale_log2e;
-  if (i0 < i1) load(i0);
-  for (int i = i0; i < i1; ++i) {
-    char* const kt = smem + (i & 1) * TB;
-    char* const vt = smem + (2 + (i & 1)) * TB;
-    int* const flag = flags + (i & 1) * NW;
-    sk_.store(tid, kt);
-    sv_.store(tid, vt);
-    {
-      ExpMax<DT> e;
-      sv_.scan(e);
-      const bool any = __any(e.hit());
-      if (lane == 0) flag[wave] = any;
-    }
-    __syncthreads();
-    const int k0 = kg.tile(i) * TK;
-    if (i + 1 < i1) load(i + 1);
-    if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;  // no row of the wave sees the tile
-    floatx16 s[NB];
+  auto walk = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      s[n] = floatx16{};
+    for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+    m = -__builtin_inff();
+    l = 0.0f;
+    if (i0 < i1) load(i0);
+    for (int i = i0; i < i1; ++i) {
+      const int buf = NBUF == 1 ? 0 : i & 1;
+      char* const kt = smem + buf * TB;
+      char* const vt = smem + (NBUF + buf) * TB;
+      int* const flag = flags + buf * NW;
+      sk_.store(tid, kt);
+      sv_.store(tid, vt);
+      {
+        ExpMax<DT> e;
+        sv_.scan(e);
+        const bool any = __any(e.hit());
+        if (lane == 0) flag[wave] = any;
+      }
+      __syncthreads();
+      const int k0 = kg.tile(i) * TK;
+      if (i + 1 < i1) load(i + 1);
+      if constexpr (!kCareful) {
+        if (!kg.whole(k0, TK) && any_flag<NW>(flag)) return false;
+      }
+      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;  // no row of the wave sees the tile
+      floatx16 s[NB];
 #pragma unroll
-      for (int t = 0; t < DP / 16; ++t) mma32<DT>(s[n], row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
-    }
-    const bool whole = k0 + TK - 1 <= kw.all_last && (k0 >= kw.all_first || k0 + TK <= kw.all_sink);
-    auto sees = [&](int k) {
-      const int j = k0 + k;
-      return j <= hi && (j >= lo || j < sk);
-    };
-    if (!whole) {
+      for (int n = 0; n < NB; ++n) {
+        s[n] = floatx16{};
+#pragma unroll
+        for (int t = 0; t < DP / 16; ++t) mma32<DT>(s[n], row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
+      }
+      const bool whole = kw.whole(k0, TK);
+      auto sees = [&](int k) {
+        const int j = k0 + k;
+        return j <= hi && (j >= lo || j < sk);
+      };
+      if (!whole) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[n][e] = -__builtin_inff();
+      }
+      float mx = -__builtin_inff();
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[n][e] = -__builtin_inff();
-    }
-    float mx = -__builtin_inff();
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[n][e]);
+      mx = half_max(mx);
+      if (__any((mx - m) * c > 8.0f)) {
+        const float mn = fmaxf(m, mx);
+        const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * c);
+        m = mn;
+        l *= f;
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[n][e]);
-    mx = half_max(mx);
-    if (__any((mx - m) * c > 8.0f)) {
-      const float mn = fmaxf(m, mx);
-      const float f = mn == m ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * c);
-      m = mn;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[d][e] *= f;
-    }
-    const float mc = m == -__builtin_inff() ? 0.0f : m * c;
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -mc));
-        l += s[n][e];
+          for (int e = 0; e < 16; ++e) acc[d][e] *= f;
       }
-    bool odd = false;
-    if (!whole) {
+      const float mc = m == -__builtin_inff() ? 0.0f : m * c;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) odd |= flag[w] != 0;
-    }
-    if (__builtin_amdgcn_readfirstlane(odd)) {
+      for (int n = 0; n < NB; ++n)
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t)
-        mma_seen<DT, DP>(acc, vt, 16 * t, tile_frag<DT>(s[t / 2], t % 2), lane, sees);
-    } else {
+        for (int e = 0; e < 16; ++e) {
+          s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -mc));
+          l += s[n][e];
+        }
+      if constexpr (kCareful) {
 #pragma unroll
-      for (int t = 0; t < 2 * NB; ++t) {
-        const Frag8<DT> p = tile_frag<DT>(s[t / 2], t % 2);
+        for (int t = 0; t < 2 * NB; ++t)
+          mma_seen<DT, DP>(acc, vt, 16 * t, tile_frag<DT>(s[t / 2], t % 2), lane, sees);
+      } else {
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(vt, 16 * t, d, lane), p);
+        for (int t = 0; t < 2 * NB; ++t) {
+          const Frag8<DT> p = tile_frag<DT>(s[t / 2], t % 2);
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(vt, 16 * t, d, lane), p);
+        }
       }
     }
+    return true;
+  };
+  if (!walk(std::false_type{})) {
+    __syncthreads();
+    walk(std::true_type{});
   }
   l = half_sum(l);
   if (!row_ok) l = 0.0f;
@@ -492,34 +522,43 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
   }
 }
 
-// Joins the parts of each row, in their order: four rows a workgroup.
+// Joins the parts of each row (64 at most), in their order: four rows a workgroup,
+// lane p of a wave holding part p's statistics.
 template <int DT>
 __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
-  constexpr int EB = DT == kF32 ? 4 : 2;
+  using E = typename Elem<DT>::T;
   const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= rows) return;
   const int lane = threadIdx.x & 63;
-  const float* const st = a.part + rows * a.parts * a.D;
-  float m = -__builtin_inff();
-  for (int p = 0; p < a.parts; ++p) m = fmaxf(m, st[(p * rows + row) * 2]);
-  const float mu = m == -__builtin_inff() ? 0.0f : m;
-  float l = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  float m = -__builtin_inff(), l = 0.0f;
+  if (lane < a.parts) {
+    const float* const st = a.part + rows * a.parts * a.D + ((int64_t)lane * rows + row) * 2;
+    m = st[0];
+    l = st[1];
+  }
+  float top = m;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  const float mu = top == -__builtin_inff() ? 0.0f : top;
+  const float f = __builtin_amdgcn_exp2f(m - mu);
+  l = l == 0.0f ? 0.0f : l * f;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+  float o0 = 0.0f, o1 = 0.0f;
   const bool c0 = lane < a.D, c1 = lane + 64 < a.D;
+#pragma unroll 8
   for (int p = 0; p < a.parts; ++p) {
-    const int64_t at = p * rows + row;
-    const float lp = st[at * 2 + 1];
-    if (lp == 0.0f) continue;
-    const float f = __builtin_amdgcn_exp2f(st[at * 2] - mu);
-    l += lp * f;
-    if (c0) o0 += a.part[at * a.D + lane] * f;
-    if (c1) o1 += a.part[at * a.D + lane + 64] * f;
+    const float* const x = a.part + (p * rows + row) * a.D + lane;
+    const float g = bits_f32(__builtin_amdgcn_readlane(f32_bits(f), p));
+    const float x0 = c0 ? x[0] : 0.0f, x1 = c1 ? x[64] : 0.0f;
+    o0 += g == 0.0f ? 0.0f : x0 * g;  // a part that saw nothing holds no numbers
+    o1 += g == 0.0f ? 0.0f : x1 * g;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int bh = (int)(row / a.R), r = (int)(row % a.R);
-  using E = typename Elem<DT>::T;
-  E* const o = (E*)((char*)a.o + ((int64_t)(bh / a.Hkv) * a.os[0] + (int64_t)(r / a.G) * a.os[1] +
-                                  (int64_t)((bh % a.Hkv) * a.G + r % a.G) * a.os[2]) * EB);
+  E* const o = (E*)a.o + ((int64_t)(bh / a.Hkv) * a.os[0] + (int64_t)(r / a.G) * a.os[1] +
+                          (int64_t)((bh % a.Hkv) * a.G + r % a.G) * a.os[2]);
   if (c0) o[lane] = (E)(o0 * inv);
   if (c1) o[lane + 64] = (E)(o1 * inv);
   if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? __builtin_inff() : mu + __builtin_amdgcn_logf(l);
@@ -587,64 +626,70 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     sv_.load(tid, a.D, [&](int rr) { return vb + (int64_t)min(k0 + rr, len - 1) * a.vs[1] * RT::EB; }, ok);
   };
   floatx16 acc[DP / 32];
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
   const float c = a.scale_log2e;
-  if (kg.n > 0) load(0);
-  for (int i = 0; i < kg.n; ++i) {
-    char* const kt = smem + (i & 1) * TB;
-    char* const vt = smem + (2 + (i & 1)) * TB;
-    int* const flag = flags + (i & 1) * NW;
-    sk_.store(tid, kt);
-    sv_.store(tid, vt);
-    {
-      ExpMax<DT> e;
-      sk_.scan(e);
-      const bool any = __any(e.hit());
-      if (lane == 0) flag[wave] = any;
-    }
-    __syncthreads();
-    const int k0 = kg.tile(i) * TK;
-    if (i + 1 < kg.n) load(i + 1);
-    if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;
-    const bool whole = k0 + TK - 1 <= kw.all_last && (k0 >= kw.all_first || k0 + TK <= kw.all_sink);
-    auto sees = [&](int k) {
-      const int j = k0 + k;
-      return j <= hi && (j >= lo || j < sk);
-    };
-    bool odd = false;
-    if (!whole) {
+  auto walk = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) odd |= flag[w] != 0;
-    }
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      floatx16 s{}, g{};
-#pragma unroll
-      for (int t = 0; t < DP / 16; ++t) {
-        mma32<DT>(s, row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
-        mma32<DT>(g, row_frag<DT, DP>(vt, n * 32 + (lane & 31), t, half), gf[t]);
+    for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+    if (kg.n > 0) load(0);
+    for (int i = 0; i < kg.n; ++i) {
+      char* const kt = smem + (i & 1) * TB;
+      char* const vt = smem + (2 + (i & 1)) * TB;
+      int* const flag = flags + (i & 1) * NW;
+      sk_.store(tid, kt);
+      sv_.store(tid, vt);
+      {
+        ExpMax<DT> e;
+        sk_.scan(e);
+        const bool any = __any(e.hit());
+        if (lane == 0) flag[wave] = any;
       }
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * (g[e] - delta);
-      if (!whole) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = 0.0f;
+      __syncthreads();
+      const int k0 = kg.tile(i) * TK;
+      if (i + 1 < kg.n) load(i + 1);
+      if constexpr (!kCareful) {
+        if (!kg.whole(k0, TK) && any_flag<NW>(flag)) return false;
       }
-      if (__builtin_amdgcn_readfirstlane(odd)) {
+      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;
+      const bool whole = kw.whole(k0, TK);
+      auto sees = [&](int k) {
+        const int j = k0 + k;
+        return j <= hi && (j >= lo || j < sk);
+      };
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          mma_seen<DT, DP>(acc, kt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
-      } else {
+      for (int n = 0; n < NB; ++n) {
+        floatx16 s{}, g{};
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const Frag8<DT> p = tile_frag<DT>(s, t);
+        for (int t = 0; t < DP / 16; ++t) {
+          mma32<DT>(s, row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
+          mma32<DT>(g, row_frag<DT, DP>(vt, n * 32 + (lane & 31), t, half), gf[t]);
+        }
 #pragma unroll
-          for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(kt, n * 32 + 16 * t, d, lane), p);
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * (g[e] - delta);
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = 0.0f;
+        }
+        if constexpr (kCareful) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            mma_seen<DT, DP>(acc, kt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const Frag8<DT> p = tile_frag<DT>(s, t);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(kt, n * 32 + 16 * t, d, lane), p);
+          }
         }
       }
     }
+    return true;
+  };
+  if (!walk(std::false_type{})) {
+    __syncthreads();
+    walk(std::true_type{});
   }
   store_owner<DT, DP>(acc, a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
 }
@@ -690,6 +735,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   const int j0 = kt_ * 32 * NW, jw = j0 + wave * 32, j = jw + (lane & 31);
   int g0, g1, w0, w1, f0, f1, l0, l1, u0, u1;
   tokens(j0, j0 + 32 * NW - 1, g0, g1, u0, u1);
+  const int all_lo = u0 * a.G, all_hi = u1 < u0 ? -1 : u1 * a.G + a.G - 1;  // rows that see every key of the workgroup
   tokens(jw, jw + 31, w0, w1, f0, f1);
   tokens(j, j, l0, l1, u0, u1);
   const int rlo = l0 * a.G, rhi = l1 < l0 ? -1 : l1 * a.G + a.G - 1;  // rows that see the lane's key
@@ -727,82 +773,88 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
     }
   };
   floatx16 dk[DP / 32], dv[DP / 32];
-#pragma unroll
-  for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = floatx16{};
   const float c = a.scale_log2e;
-  if (i0 < i1) load(i0);
-  for (int i = i0; i < i1; ++i) {
-    char* const qt = smem + (i & 1) * TB;
-    char* const gt = smem + (2 + (i & 1)) * TB;
-    float* const ls = stats + (i & 1) * TQ;
-    float* const de = stats + (2 + (i & 1)) * TQ;
-    int* const flag = flags + (i & 1) * NW;
-    sq.store(tid, qt);
-    sg.store(tid, gt);
-    if (tid < TQ) {
-      ls[tid] = st_lse;
-      de[tid] = st_delta;
-    }
-    {
-      ExpMax<DT> e;
-      sq.scan(e);
-      sg.scan(e);
-      const bool any = __any(e.hit());
-      if (lane == 0) flag[wave] = any;
-    }
-    __syncthreads();
-    const int r0 = (tq0 + i) * TQ;
-    if (i + 1 < i1) load(i + 1);
-    if (r0 > whi || r0 + TQ <= wlo) continue;
-    const bool whole = r0 >= flo && r0 + TQ - 1 <= fhi;
-    auto sees = [&](int k) { return r0 + k >= rlo && r0 + k <= rhi; };
-    bool odd = false;
-    if (!whole) {
+  auto walk = [&](auto careful) {
+    constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
-      for (int x = 0; x < NW; ++x) odd |= flag[x] != 0;
-    }
-#pragma unroll
-    for (int n = 0; n < NB; ++n) {
-      floatx16 s{}, g{};
-#pragma unroll
-      for (int t = 0; t < DP / 16; ++t) {
-        mma32<DT>(s, row_frag<DT, DP>(qt, n * 32 + (lane & 31), t, half), kf[t]);
-        mma32<DT>(g, row_frag<DT, DP>(gt, n * 32 + (lane & 31), t, half), vf[t]);
+    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = floatx16{};
+    if (i0 < i1) load(i0);
+    for (int i = i0; i < i1; ++i) {
+      char* const qt = smem + (i & 1) * TB;
+      char* const gt = smem + (2 + (i & 1)) * TB;
+      float* const ls = stats + (i & 1) * TQ;
+      float* const de = stats + (2 + (i & 1)) * TQ;
+      int* const flag = flags + (i & 1) * NW;
+      sq.store(tid, qt);
+      sg.store(tid, gt);
+      if (tid < TQ) {
+        ls[tid] = st_lse;
+        de[tid] = st_delta;
       }
+      {
+        ExpMax<DT> e;
+        sq.scan(e);
+        sg.scan(e);
+        const bool any = __any(e.hit());
+        if (lane == 0) flag[wave] = any;
+      }
+      __syncthreads();
+      const int r0 = (tq0 + i) * TQ;
+      if (i + 1 < i1) load(i + 1);
+      if constexpr (!kCareful) {
+        if (!(r0 >= all_lo && r0 + TQ - 1 <= all_hi) && any_flag<NW>(flag)) return false;
+      }
+      if (r0 > whi || r0 + TQ <= wlo) continue;
+      const bool whole = r0 >= flo && r0 + TQ - 1 <= fhi;
+      auto sees = [&](int k) { return r0 + k >= rlo && r0 + k <= rhi; };
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const floatx4 le = *reinterpret_cast<const floatx4*>(ls + n * 32 + 8 * x + 4 * half);
-        const floatx4 dl = *reinterpret_cast<const floatx4*>(de + n * 32 + 8 * x + 4 * half);
+      for (int n = 0; n < NB; ++n) {
+        floatx16 s{}, g{};
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int e = 4 * x + y;
-          s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -le[y]));
-          g[e] = s[e] * (g[e] - dl[y]);
+        for (int t = 0; t < DP / 16; ++t) {
+          mma32<DT>(s, row_frag<DT, DP>(qt, n * 32 + (lane & 31), t, half), kf[t]);
+          mma32<DT>(g, row_frag<DT, DP>(gt, n * 32 + (lane & 31), t, half), vf[t]);
         }
-      }
-      if (!whole) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = g[e] = 0.0f;
-      }
-      if (__builtin_amdgcn_readfirstlane(odd)) {
+        for (int x = 0; x < 4; ++x) {
+          const floatx4 le = *reinterpret_cast<const floatx4*>(ls + n * 32 + 8 * x + 4 * half);
+          const floatx4 dl = *reinterpret_cast<const floatx4*>(de + n * 32 + 8 * x + 4 * half);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          mma_seen<DT, DP>(dv, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
-          mma_seen<DT, DP>(dk, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), lane, sees);
+          for (int y = 0; y < 4; ++y) {
+            const int e = 4 * x + y;
+            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -le[y]));
+            g[e] = s[e] * (g[e] - dl[y]);
+          }
         }
-      } else {
+        if (!whole) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const Frag8<DT> p = tile_frag<DT>(s, t), ds = tile_frag<DT>(g, t);
+          for (int e = 0; e < 16; ++e)
+            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = g[e] = 0.0f;
+        }
+        if constexpr (kCareful) {
 #pragma unroll
-          for (int d = 0; d < DP / 32; ++d) {
-            mma32<DT>(dv[d], col_frag<DT, DP>(gt, n * 32 + 16 * t, d, lane), p);
-            mma32<DT>(dk[d], col_frag<DT, DP>(qt, n * 32 + 16 * t, d, lane), ds);
+          for (int t = 0; t < 2; ++t) {
+            mma_seen<DT, DP>(dv, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
+            mma_seen<DT, DP>(dk, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), lane, sees);
+          }
+        } else {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const Frag8<DT> p = tile_frag<DT>(s, t), ds = tile_frag<DT>(g, t);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+              mma32<DT>(dv[d], col_frag<DT, DP>(gt, n * 32 + 16 * t, d, lane), p);
+              mma32<DT>(dk[d], col_frag<DT, DP>(qt, n * 32 + 16 * t, d, lane), ds);
+            }
           }
         }
       }
     }
+    return true;
+  };
+  if (!walk(std::false_type{})) {
+    __syncthreads();
+    walk(std::true_type{});
   }
   if (parts == 1) {
     const bool ok = j < a.Lk;
@@ -821,16 +873,18 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   }
 }
 
-// Adds the parts of split key tiles in their order.  One workgroup a split tile,
-// head pair and gradient.
+// Adds the parts of split key tiles in their order: a thread four elements of one
+// tile's gradient; blockIdx.y the tile of a head pair and the gradient.
 template <int DT>
 __global__ __launch_bounds__(256) void eql_wattn_dkv_sum_kernel(AttnArgs a, int keys) {
   using E = typename Elem<DT>::T;
   const int split_sinks = a.sink_parts > 1 ? a.sink_tiles : 0;
   const int split_keys = a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0;
   const int per = split_sinks + split_keys;
-  const int which = blockIdx.x % 2;
-  const int x = (int)((blockIdx.x / 2) % per), bh = (int)((blockIdx.x / 2) / per);
+  const uint32_t chunks = (uint32_t)(keys * a.D + 1023) / 1024;
+  const uint32_t id = blockIdx.x / chunks;
+  const int which = id % 2;
+  const int x = (int)((id / 2) % per), bh = (int)((id / 2) / per);
   const int64_t slots = (int64_t)split_sinks * a.sink_parts + (int64_t)split_keys * a.key_parts;
   int tile, parts;
   int64_t slot;
@@ -843,17 +897,19 @@ __global__ __launch_bounds__(256) void eql_wattn_dkv_sum_kernel(AttnArgs a, int 
     parts = a.key_parts;
     slot = (int64_t)split_sinks * a.sink_parts + (int64_t)(x - split_sinks) * parts;
   }
+  const int i = (int)(blockIdx.x % chunks) * 1024 + threadIdx.x * 4;  // D is a multiple of 4
+  if (i >= min(keys, a.Lk - tile * keys) * a.D) return;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int64_t one = (int64_t)2 * keys * a.D;
-  const float* const src = a.part + (bh * slots + slot) * one + (int64_t)which * keys * a.D;
+  const float* const src = a.part + (bh * slots + slot) * one + (int64_t)which * keys * a.D + i;
+  floatx4 s = *reinterpret_cast<const floatx4*>(src);
+#pragma unroll 8
+  for (int p = 1; p < parts; ++p) s += *reinterpret_cast<const floatx4*>(src + p * one);
   const int64_t* const st = which ? a.dvs : a.dks;
-  E* const dst = (E*)(which ? a.dv : a.dk) + (int64_t)b * st[0] + (int64_t)hk * st[2];
-  const int n = min(keys, a.Lk - tile * keys) * a.D;
-  for (int i = threadIdx.x; i < n; i += 256) {
-    float s = 0.0f;
-    for (int p = 0; p < parts; ++p) s += src[p * one + i];
-    dst[(int64_t)(tile * keys + i / a.D) * st[1] + i % a.D] = (E)s;
-  }
+  E* const dst = (E*)(which ? a.dv : a.dk) + (int64_t)b * st[0] + (int64_t)hk * st[2] +
+                 (int64_t)(tile * keys + i / a.D) * st[1] + i % a.D;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) dst[k] = (E)s[k];
 }
 
 }  // namespace eqk

@@ -9,9 +9,11 @@ namespace {
 constexpr int DT = EQK_DT;
 constexpr int kEB = DT == kF32 ? 4 : 2;
 
-constexpr int tile_bytes(int DP) { return attn_tile(DT) * (DP == 96 ? 128 : DP) * kEB; }
-constexpr int fwd_lds(int DP, int NW) { return 4 * tile_bytes(DP) + 2 * NW * 4; }
-constexpr int dkv_lds(int DP) { return 4 * tile_bytes(DP) + 4 * attn_tile(DT) * 4 + 2 * 4 * 4; }
+constexpr int row_bytes(int DP) { return (DP == 96 ? 128 : DP) * kEB; }
+constexpr int fwd_lds(int DP, int NW) {
+  return attn_fwd_bufs(NW) * (2 * attn_fwd_tile(DT, NW) * row_bytes(DP) + NW * 4);
+}
+constexpr int dkv_lds(int DP) { return 2 * (2 * attn_tile(DT) * row_bytes(DP) + 2 * attn_tile(DT) * 4 + 4 * 4); }
 
 template <typename K>
 hipError_t launch(K k, int64_t blocks, int threads, int lds, hipStream_t stream, const AttnArgs& a) {
@@ -26,8 +28,10 @@ hipError_t launch(K k, int64_t blocks, int threads, int lds, hipStream_t stream,
 template <int DP>
 hipError_t fwd(const AttnArgs& a, int waves, hipStream_t stream) {
   const int64_t n = (int64_t)a.B * a.Hkv * ((a.R + 32 * waves - 1) / (32 * waves)) * a.parts;
-  return waves == 1 ? launch(eql_wattn_fwd_kernel<DT, DP, 1>, n, 64, fwd_lds(DP, 1), stream, a)
-                    : launch(eql_wattn_fwd_kernel<DT, DP, 4>, n, 256, fwd_lds(DP, 4), stream, a);
+  if constexpr (DT != kF32 || DP <= 64) {
+    if (waves == 1) return launch(eql_wattn_fwd_kernel<DT, DP, 1>, n, 64, fwd_lds(DP, 1), stream, a);
+  }
+  return launch(eql_wattn_fwd_kernel<DT, DP, 4>, n, 256, fwd_lds(DP, 4), stream, a);
 }
 
 template <int DP>
@@ -93,8 +97,8 @@ hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
                                : bwd<128>(s, stream);
     if (e == hipSuccess && split) {
       const int64_t tiles = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0);
-      hipLaunchKernelGGL(eql_wattn_dkv_sum_kernel<DT>, dim3((unsigned)(2 * tiles * s.B * s.Hkv)), dim3(256), 0, stream, s,
-                         kAttnDkvKeys);
+      const int64_t n = 2 * tiles * s.B * s.Hkv * ((kAttnDkvKeys * a.D + 1023) / 1024);
+      hipLaunchKernelGGL(eql_wattn_dkv_sum_kernel<DT>, dim3((unsigned)n), dim3(256), 0, stream, s, kAttnDkvKeys);
       e = hipGetLastError();
     }
     if (e != hipSuccess) return e;

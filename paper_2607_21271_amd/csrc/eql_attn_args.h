@@ -29,8 +29,10 @@ struct AttnArgs {
   int key_tiles, sink_tiles, key_parts, sink_parts; // key/value gradient
 };
 
-// streamed rows of a tile
+// streamed rows of a tile; a single wave stages by itself and holds half as many
 constexpr int attn_tile(int dt) { return dt == kF32 ? 32 : 64; }
+constexpr int attn_fwd_tile(int dt, int waves) { return waves == 1 ? 32 : attn_tile(dt); }
+constexpr int attn_fwd_bufs(int waves) { return waves == 1 ? 1 : 2; }
 
 // Waves of a forward workgroup over R packed rows, and the parts that the keys are split into.
 struct AttnPlan {

@@ -43,8 +43,7 @@ int64_t span(int64_t n0, int64_t n1, int64_t n2, int64_t inner, const int64_t* s
 namespace eqk {
 
 // Key tiles that a workgroup of `rows` packed rows may walk.
-static int64_t attn_tiles(const AttnArgs& a, int dt, int64_t rows) {
-  const int64_t tk = attn_tile(dt);
+static int64_t attn_tiles(const AttnArgs& a, int64_t tk, int64_t rows) {
   int64_t keys = (int64_t)a.left + a.right + (rows + a.G - 1) / a.G + a.sinks + 2 * tk;
   if (keys > a.Lk) keys = a.Lk;
   return (keys + tk - 1) / tk;
@@ -52,14 +51,15 @@ static int64_t attn_tiles(const AttnArgs& a, int dt, int64_t rows) {
 
 AttnPlan attn_plan(const AttnArgs& a, int dt, int cus) {
   AttnPlan p;
-  // one wave holds 32 rows; up to that many, waves of their own share nothing
-  p.waves = a.R <= 32 ? 1 : 4;
+  // one wave holds 32 rows; up to that many, waves of their own share nothing (a
+  // single wave has no registers for the tiles of wide heads in full precision)
+  p.waves = a.R <= 32 && (dt != kF32 || a.D <= 64) ? 1 : 4;
   const int64_t rows = 32 * p.waves;
   const int64_t blocks = (int64_t)a.B * a.Hkv * ((a.R + rows - 1) / rows);
-  const int64_t want = (p.waves == 1 ? 4 : 2) * (int64_t)cus;
+  const int64_t want = (p.waves == 1 ? 8 : 2) * (int64_t)cus;
   int64_t parts = 1;
   if (blocks * 2 <= want) {
-    const int64_t most = attn_tiles(a, dt, rows) / 2;  // at least two tiles each
+    const int64_t most = attn_tiles(a, attn_fwd_tile(dt, p.waves), rows) / 2;  // at least two tiles each
     parts = want / blocks;
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
