@@ -11,56 +11,70 @@ allocates and marshals; ``eqlinear_window_attention`` and its backward compute.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
 from . import _lib, ops, rotary
 
 
+@functools.lru_cache(maxsize=1024)
+def _whole_words(shape, stride, itemsize) -> bool:
+    w = 16 // itemsize
+    return stride[3] == 1 and all(shape[i] <= 1 or stride[i] % w == 0 for i in range(3))
+
+
 def _ready(t: torch.Tensor) -> torch.Tensor:
     """t itself where its heads start on whole 16-byte words, else a contiguous copy."""
-    w = 16 // t.element_size()
-    s, n = t.stride(), t.shape
-    if (s[3] == 1 and t.data_ptr() % 16 == 0
-            and all(n[i] <= 1 or s[i] % w == 0 for i in range(3))):
+    if t.data_ptr() % 16 == 0 and _whole_words(t.shape, t.stride(), t.element_size()):
         return t
     t = t.contiguous()
     return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
 
 
-def _shape(q, k, left, right, sinks, scale, q_s, k_s, v_s, o_s, *grads):
-    B, Lq, H, D = q.shape
-    none = (0, 0, 0)
-    return _lib.WindowShape(B, Lq, k.shape[1], left, right, sinks, H, k.shape[2], D, ops._DT[q.dtype], scale, 0, q_s,
-                            k_s, v_s, o_s, *(grads or (none, none, none, none)))
+def _dense(shape):
+    return shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3], 1
 
 
-_strides = rotary._strides
+def _outer(shape, stride):
+    """Strides of sequence, token and head, 0 for an axis of size 1."""
+    return tuple(stride[i] if shape[i] > 1 else 0 for i in range(3))
 
 
-def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse, stream=None):
-    B, Lq, H, D = q.shape
-    o = torch.empty(B, Lq, H, D, dtype=q.dtype, device=q.device)
-    shape = _shape(q, k, left, right, sinks, scale, _strides(q), _strides(k), _strides(v), _strides(o))
-    ref = ctypes.byref(shape)
-    lse = torch.empty(B, k.shape[2], Lq, H // k.shape[2], dtype=torch.float32, device=q.device) if want_lse else None
-    need = _lib.eqlinear_window_attention_workspace_bytes(ref)
+@functools.lru_cache(maxsize=1024)
+def _plan(dtype, qshape, kshape, q, k, v, do, dq, dk, dv, left, right, sinks, scale):
+    """The C shape of a call (a pointer that keeps it) and its workspace bytes; the strides are those of the tensors, the
+    output is dense.  One problem's calls differ in addresses only."""
+    o = lambda shape, stride: (0, 0, 0) if stride is None else _outer(shape, stride)
+    shape = _lib.WindowShape(qshape[0], qshape[1], kshape[1], left, right, sinks, qshape[2], kshape[2], qshape[3],
+                             ops._DT[dtype], scale, 0, o(qshape, q), o(kshape, k), o(kshape, v),
+                             o(qshape, _dense(qshape)), o(qshape, do), o(qshape, dq), o(kshape, dk), o(kshape, dv))
+    ref = ctypes.pointer(shape)
+    return ref, (_lib.eqlinear_window_attention_workspace_bytes(ref) if do is None
+                 else _lib.eqlinear_window_attention_backward_workspace_bytes(ref))
+
+
+def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse):
+    qshape, kshape = q.shape, k.shape
+    ref, need = _plan(q.dtype, qshape, kshape, q.stride(), k.stride(), v.stride(), None, None, None, None, left, right,
+                      sinks, scale)
+    o = torch.empty(qshape, dtype=q.dtype, device=q.device)
+    # lse [B, kv_heads, Lq, heads / kv_heads]
+    lse = torch.empty(qshape[0] * qshape[1] * qshape[2], dtype=torch.float32, device=q.device) if want_lse else None
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _lib.check(_lib.eqlinear_window_attention(ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
                                               ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(ws), need,
-                                              ops._stream(stream)), "eqlinear_window_attention")
+                                              ops._stream_of(q)), "eqlinear_window_attention")
     return o, lse
 
 
-def _backward(q, k, v, lengths, starts, o, lse, do, dq, dk, dv, left, right, sinks, scale, stream=None):
-    shape = _shape(q, k, left, right, sinks, scale, _strides(q), _strides(k), _strides(v), _strides(o), _strides(do),
-                   _strides(dq), _strides(dk), _strides(dv))
-    ref = ctypes.byref(shape)
-    need = _lib.eqlinear_window_attention_backward_workspace_bytes(ref)
+def _backward(q, k, v, lengths, starts, o, lse, do, dq, dk, dv, left, right, sinks, scale):
+    ref, need = _plan(q.dtype, q.shape, k.shape, q.stride(), k.stride(), v.stride(), do.stride(), dq.stride(),
+                      dk.stride(), dv.stride(), left, right, sinks, scale)
     ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     _lib.check(_lib.eqlinear_window_attention_backward(
         ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths), ops._ptr(starts), ops._ptr(o), ops._ptr(lse),
-        ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv), ops._ptr(ws), need, ops._stream(stream)),
+        ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv), ops._ptr(ws), need, ops._stream_of(q)),
         "eqlinear_window_attention_backward")
 
 

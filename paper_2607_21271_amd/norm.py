@@ -8,6 +8,9 @@ of ``gconv``.  This module allocates and marshals; ``eqlinear_group_norm_act`` a
 """
 from __future__ import annotations
 
+import functools
+import math
+
 import torch
 
 from . import _lib, ops
@@ -21,24 +24,23 @@ def _ready(t: torch.Tensor) -> torch.Tensor:
     return t if t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
 
 
-def _dims(x):
-    C, T = x.shape[-2:]
-    B = x.shape[0]
-    S = 1
-    for n in x.shape[1:-2]:
-        S *= n
-    return B, S, T, C
+@functools.lru_cache(maxsize=1024)
+def _plan(shape, groups, dtype):
+    """(B, S, T, C, dtype code) of a call and the workspace bytes of forward and backward."""
+    C, T = shape[-2:]
+    S = math.prod(shape[1:-2])
+    args = (shape[0], S, T, C, groups, ops._DT[dtype])
+    return args, _lib.eqlinear_group_norm_act_workspace_bytes(*args), \
+        _lib.eqlinear_group_norm_act_backward_workspace_bytes(*args)
 
 
-def _forward(x, weight, bias, groups, act, eps, want_stats, stream=None):
-    B, S, T, C = _dims(x)
-    dt = ops._DT[x.dtype]
+def _forward(x, weight, bias, groups, act, eps, want_stats):
+    (B, S, T, C, _, dt), need, _ = _plan(x.shape, groups, x.dtype)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty(B, groups, 2, dtype=torch.float32, device=x.device) if want_stats else None
-    need = _lib.eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dt)
+    stats = torch.empty(2 * B * groups, dtype=torch.float32, device=x.device) if want_stats else None  # [B, groups, 2]
     ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
     _lib.check(_lib.eqlinear_group_norm_act(ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(y), ops._ptr(stats),
-                                            ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt, ops._stream(stream)),
+                                            ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt, ops._stream_of(x)),
                "eqlinear_group_norm_act")
     return y, stats
 
@@ -58,18 +60,16 @@ class GroupNormActFunction(torch.autograd.Function):
     def backward(ctx, gy):
         x, weight, bias, stats = ctx.saved_tensors
         groups, act = ctx.args
-        B, S, T, C = _dims(x)
-        dt = ops._DT[x.dtype]
+        (B, S, T, C, _, dt), _, need = _plan(x.shape, groups, x.dtype)
         gy = _ready(gy)
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         if x.numel() == 0:
             return dx, torch.zeros_like(weight), torch.zeros_like(bias), None, None, None
         dw, db = torch.empty_like(weight), torch.empty_like(bias)
-        need = _lib.eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dt)
         ws = torch.empty(need, dtype=torch.uint8, device=x.device)
         _lib.check(_lib.eqlinear_group_norm_act_backward(
             ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(stats), ops._ptr(gy), ops._ptr(dx), ops._ptr(dw),
-            ops._ptr(db), ops._ptr(ws), need, B, S, T, C, groups, act, dt, ops._stream(None)),
+            ops._ptr(db), ops._ptr(ws), need, B, S, T, C, groups, act, dt, ops._stream_of(x)),
             "eqlinear_group_norm_act_backward")
         return dx, dw, db, None, None, None
 

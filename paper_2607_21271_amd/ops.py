@@ -45,6 +45,11 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_of(t: torch.Tensor) -> int:
+    """Handle of the current stream of t's device."""
+    return torch._C._cuda_getCurrentRawStream(t.device.index)
+
+
 def _check_dev(*ts):
     dev = None
     for t in ts:

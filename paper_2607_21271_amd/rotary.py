@@ -8,6 +8,7 @@ keys then depend on the tokens' offsets along each axis only.  This module alloc
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -31,24 +32,25 @@ def grid_positions(shape, prefix: int = 0, device=None) -> torch.Tensor:
     return torch.cat((torch.zeros(prefix, len(shape), dtype=torch.int32), grid)).to(device)
 
 
-def _strides(x):
-    """Strides of [B, L, N] with the axes of size 1 counted as 0."""
-    return tuple(x.stride(i) if x.shape[i] > 1 else 0 for i in range(3))
+@functools.lru_cache(maxsize=1024)
+def _plan(dtype, shape, x, y, pos, float_pos, sections, T, interleaved, inverse):
+    """The C shape of a call (a pointer that keeps it); x, y and pos are the tensors' strides."""
+    B, L, N, D = shape
+    outer = lambda st: tuple(st[i] if shape[i] > 1 else 0 for i in range(3))  # an axis of size 1 takes no step
+    return ctypes.pointer(_lib.RotaryShape(B, L, N, D // T, T, len(sections), sections, float_pos, interleaved, inverse,
+                                           ops._DT[dtype], outer(x), outer(y), pos[:2] if len(pos) == 3 else (0, pos[0])))
 
 
-def _launch(x, positions, freqs, sections, T, interleaved, inverse, y, stream=None):
-    B, L, N, D = x.shape
-    pos = positions.stride()
-    pst = (pos[0], pos[1]) if positions.dim() == 3 else (0, pos[0])
-    shape = _lib.RotaryShape(B, L, N, D // T, T, len(sections), tuple(sections), positions.dtype == torch.float32,
-                             interleaved, inverse, ops._DT[x.dtype], _strides(x), _strides(y), pst)
-    _lib.check(_lib.eqlinear_rotary(ctypes.byref(shape), ops._ptr(x), ops._ptr(positions), ops._ptr(freqs), ops._ptr(y),
-                                    ops._stream(stream)), "eqlinear_rotary")
+def _launch(x, positions, freqs, sections, T, interleaved, inverse, y):
+    ref = _plan(x.dtype, x.shape, x.stride(), y.stride(), positions.stride(), positions.dtype == torch.float32, sections,
+                T, interleaved, inverse)
+    _lib.check(_lib.eqlinear_rotary(ref, ops._ptr(x), ops._ptr(positions), ops._ptr(freqs), ops._ptr(y),
+                                    ops._stream_of(x)), "eqlinear_rotary")
     return y
 
 
 def _rows(x):
-    """x itself where its heads are contiguous, in non-negative strides, else a contiguous copy."""
+    """x itself where the elements of a head are contiguous, else a contiguous copy."""
     return x if x.stride(3) == 1 or x.shape[3] == 1 else x.contiguous()
 
 
