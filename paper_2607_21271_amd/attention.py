@@ -21,11 +21,14 @@ from . import _lib, ops, rotary
 @functools.lru_cache(maxsize=1024)
 def _whole_words(shape, stride, itemsize) -> bool:
     w = 16 // itemsize
-    return stride[3] == 1 and all(shape[i] <= 1 or stride[i] % w == 0 for i in range(3))
+    b, token, head = _outer(shape, stride)
+    return (stride[3] == 1 and b % w == 0 and token % w == 0 and head % w == 0
+            and (65 * token + shape[2] * head) * itemsize < 1 << 31)
 
 
 def _ready(t: torch.Tensor) -> torch.Tensor:
-    """t itself where its heads start on whole 16-byte words, else a contiguous copy."""
+    """t itself where its heads start on whole 16-byte words (and a tile of its rows spans less than 2 GiB), else a
+    contiguous copy."""
     if t.data_ptr() % 16 == 0 and _whole_words(t.shape, t.stride(), t.element_size()):
         return t
     t = t.contiguous()

@@ -27,6 +27,7 @@
 #include "eql_attn_args.h"
 #include "eql_common.h"
 #include "eql_config.h"
+#include "eql_gemm.h"
 
 namespace eqk {
 
@@ -63,6 +64,15 @@ __device__ __forceinline__ void mma32(floatx16& acc, const Frag8<DT>& a, const F
   }
 }
 
+// Two floats rounded to nearest even and packed by one instruction.
+template <int DT>
+__device__ __forceinline__ uint32_t pack_pair(float a, float b) {
+  using E = typename Elem<DT>::T;
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef E e16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), e16x2));
+}
+
 // Entries 8 s .. 8 s + 7 of a result tile, rounded to the element type, as the
 // operand of a 16-deep step.
 template <int DT>
@@ -73,9 +83,34 @@ __device__ __forceinline__ Frag8<DT> tile_frag(const floatx16& t, int s) {
     for (int j = 0; j < 8; ++j) f.w[j] = f32_bits(t[8 * s + j]);
   } else {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f.w[j] = pack2<DT>(t[8 * s + 2 * j], t[8 * s + 2 * j + 1]);
+    for (int j = 0; j < 4; ++j) f.w[j] = pack_pair<DT>(t[8 * s + 2 * j], t[8 * s + 2 * j + 1]);
   }
   return f;
+}
+
+// sum + the eight values of an operand, as rounded
+template <int DT>
+__device__ __forceinline__ float add_frag(float sum, const Frag8<DT>& f) {
+  if constexpr (DT == kF32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += bits_f32(f.w[j]);
+  } else if constexpr (DT == kF16) {
+    const half2v one = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = f.w[j];
+      sum = __builtin_amdgcn_fdot2(__builtin_bit_cast(half2v, w), one, sum, false);
+    }
+  } else {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 one = {(__bf16)1.0f, (__bf16)1.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t w = f.w[j];
+      sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), one, sum, false);
+    }
+  }
+  return sum;
 }
 
 // LDS tile of rows of DP elements.  16-byte chunk c of a row lies at chunk
@@ -97,51 +132,70 @@ struct RowTile {
   __device__ static __forceinline__ int off(int row, int c) { return row * RB + ((c ^ swz(row)) << 4); }
 };
 
-// Row operand: elements 16 s + 8 half .. + 7 of tile row `row`.
+// A lane's places in a tile.  16 bits: offsets formed once, to which a tile's
+// place in LDS and a row block are compile-time constants of the instruction (rows
+// 16 apart share their swizzle).
 template <int DT, int DP>
-__device__ __forceinline__ Frag8<DT> row_frag(const char* t, int row, int s, int half) {
+struct LdsMap {
   using RT = RowTile<DT, DP>;
-  Frag8<DT> f;
-  constexpr int N = DT == kF32 ? 2 : 1;
+  int lane;
+  uint32_t row_at[DT == kF32 ? 1 : DP / 16], col_at[2][DT == kF32 ? 1 : DP / 32];
+  __device__ __forceinline__ explicit LdsMap(int lane_) : lane(lane_) {
+    if constexpr (DT != kF32) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const u32x4 a = *reinterpret_cast<const u32x4*>(t + RT::off(row, (2 * s + half) * N + n));
+      for (int s = 0; s < DP / 16; ++s) row_at[s] = RT::off(lane & 31, 2 * s + (lane >> 5));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) f.w[4 * n + j] = a[j];
-  }
-  return f;
-}
-
-// Column operand: element 32 d + lane % 32 of tile rows r0 + 8 (j / 4) + 4 half + j % 4.
-// 16 bits: two transposing LDS reads, in which sixteen lanes hand in the
-// addresses of four rows of sixteen elements and lane i takes column i.
-template <int DT, int DP>
-__device__ __forceinline__ Frag8<DT> col_frag(const char* t, int r0, int d, int lane) {
-  using RT = RowTile<DT, DP>;
-  Frag8<DT> f;
-  const int half = lane >> 5;
-  if constexpr (DT == kF32) {
-    const int e = d * 32 + (lane & 31);
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int row = r0 + 8 * (j >> 2) + 4 * half + (j & 3);
-      f.w[j] = *reinterpret_cast<const uint32_t*>(t + RT::off(row, e >> 2) + (e & 3) * 4);
-    }
-  } else {
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    const int e = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int row = r0 + 8 * j + 4 * half + ((lane & 15) >> 2);
-      const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (__attribute__((address_space(3))) s16x4*)(t + RT::off(row, e >> 3) + (e & 7) * 2));
-      const u32x2 w = __builtin_bit_cast(u32x2, v);
-      f.w[2 * j] = w[0];
-      f.w[2 * j + 1] = w[1];
+        for (int d = 0; d < DP / 32; ++d) {
+          const int e = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+          col_at[j][d] = RT::off(8 * j + 4 * (lane >> 5) + ((lane & 15) >> 2), e >> 3) + (e & 7) * 2;
+        }
     }
   }
-  return f;
-}
+  // Row operand: elements 16 s + 8 half .. + 7 of tile row 32 n + lane % 32.
+  __device__ __forceinline__ Frag8<DT> row(const char* t, int n, int s) const {
+    Frag8<DT> f;
+    if constexpr (DT == kF32) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(t + RT::off(n * 32 + (lane & 31), (2 * s + (lane >> 5)) * 2 + q));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f.w[4 * q + j] = a[j];
+      }
+    } else {
+      const u32x4 a = *reinterpret_cast<const u32x4*>(t + n * 32 * RT::RB + row_at[s]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f.w[j] = a[j];
+    }
+    return f;
+  }
+  // Column operand: element 32 d + lane % 32 of tile rows r0 + 8 (j / 4) + 4 half + j % 4,
+  // r0 a multiple of 16.  16 bits: two transposing LDS reads, in which sixteen lanes
+  // hand in the addresses of four rows of sixteen elements and lane i takes column i.
+  __device__ __forceinline__ Frag8<DT> col(const char* t, int r0, int d) const {
+    Frag8<DT> f;
+    if constexpr (DT == kF32) {
+      const int e = d * 32 + (lane & 31);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = r0 + 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3);
+        f.w[j] = *reinterpret_cast<const uint32_t*>(t + RT::off(row, e >> 2) + (e & 3) * 4);
+      }
+    } else {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4*)(t + r0 * RT::RB + col_at[j][d]));
+        const u32x2 w = __builtin_bit_cast(u32x2, v);
+        f.w[2 * j] = w[0];
+        f.w[2 * j + 1] = w[1];
+      }
+    }
+    return f;
+  }
+};
 
 // Maximum and sum of the two lane halves' values.
 __device__ __forceinline__ float half_max(float v) {
@@ -151,6 +205,14 @@ __device__ __forceinline__ float half_max(float v) {
 __device__ __forceinline__ float half_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
   return bits_f32(r[0]) + bits_f32(r[1]);
+}
+
+// Visibility of 32 streamed rows as bits.  below(x): bits 0 .. x - 1.
+__device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1u; }
+// All ones where the lane's owner sees entry e of a result tile, else zero; `bits`
+// shifted right by 4 for the upper lane half.
+__device__ __forceinline__ uint32_t entry_mask(uint32_t bits, int e) {
+  return (uint32_t)__builtin_amdgcn_sbfe((int)bits, 8 * (e >> 2) + (e & 3), 1);
 }
 
 // Running maximum of the exponent fields of 16-byte chunks: equal to the mask in
@@ -183,15 +245,14 @@ struct ExpMax {
 // into a tile of its own that only the owners who see the row add.  sees(k) tells
 // whether the lane's owner sees tile row k.
 template <int DT, int DP, typename F>
-__device__ __forceinline__ void mma_seen(floatx16 (&acc)[DP / 32], const char* t, int r0, const Frag8<DT>& b, int lane,
-                                         F&& sees) {
+__device__ __forceinline__ void mma_seen(floatx16 (&acc)[DP / 32], const LdsMap<DT, DP>& map, const char* t, int r0,
+                                         const Frag8<DT>& b, F&& sees) {
   constexpr int NR = DT == kF32 ? 8 : 4;
   constexpr uint32_t kMask = ExpMax<DT>::kMask;
-  asm volatile("" : "+v"(lane));  // keeps this rare path's addresses out of the registers of the common one
-  const int half = lane >> 5;
+  const int half = map.lane >> 5;
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) {
-    Frag8<DT> a = col_frag<DT, DP>(t, r0, d, lane), odd;
+    Frag8<DT> a = map.col(t, r0, d), odd;
     bool any = false;
 #pragma unroll
     for (int w = 0; w < NR; ++w) {
@@ -235,24 +296,35 @@ __device__ __forceinline__ bool any_flag(const int* flag) {
 }
 
 // Loads of one streamed tile of TK rows by NT threads, held in registers between
-// the load and the LDS write.
+// the load and the LDS write.  Buffer loads: an offset past the resource
+// (kDropOffset, or a row past its end) reads as zero, so a row needs no arithmetic
+// but its offset, the same in every tile.
 template <int DT, int DP, int TK, int NT>
 struct Stage {
   using RT = RowTile<DT, DP>;
-  static constexpr int N = (TK * RT::NC + NT - 1) / NT;
+  static constexpr int N = TK * RT::NC / NT;
   static_assert(TK * RT::NC % NT == 0, "whole chunks");
   u32x4 r[N];
-  // at(row) is the address of tile row `row`, ok(row) whether it holds data (its
-  // address must be readable either way)
-  template <typename A, typename K>
-  __device__ __forceinline__ void load(int tid, int D, A&& at, K&& ok) {
+  uint32_t off[N];
+  // at(row): byte offset of tile row `row`; elements from D on are zero
+  template <typename A>
+  __device__ __forceinline__ void place(int tid, int D, A&& at) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int u = tid + i * NT, row = u / RT::NC, c = u % RT::NC;
-      const bool in = c * RT::CE < D;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(at(row) + (in ? c * 16 : 0));
-      r[i] = in && ok(row) ? v : u32x4{0, 0, 0, 0};
+      const int u = tid + i * NT, c = u % RT::NC;
+      off[i] = c * RT::CE < D ? (uint32_t)at(u / RT::NC) + c * 16 : kDropOffset;
     }
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off[i], 0, 0));
+  }
+  // the tile rows from `rows` on as zero, whatever their offset
+  __device__ __forceinline__ void load_first(__amdgpu_buffer_rsrc_t rs, int tid, int rows) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      r[i] = __builtin_bit_cast(
+          u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, (tid + i * NT) / RT::NC < rows ? off[i] : kDropOffset, 0, 0));
   }
   __device__ __forceinline__ void store(int tid, char* t) const {
 #pragma unroll
@@ -266,6 +338,12 @@ struct Stage {
     for (int i = 0; i < N; ++i) m.add(r[i]);
   }
 };
+// Rows k0 .. of one sequence's keys or values (`base`, `stride` bytes a row), those
+// below len, as a resource for one tile.
+template <int TK>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_rsrc(const char* base, int64_t stride, int k0, int len, int row_bytes) {
+  return make_rsrc(base + k0 * stride, (uint32_t)((min(len - k0, TK) - 1) * (int)stride + row_bytes));
+}
 
 // Owner operand: one row of D elements read straight from memory, steps of 16.
 template <int DT, int DP>
@@ -304,7 +382,7 @@ __device__ __forceinline__ void store_owner(const floatx16 (&acc)[DP / 32], floa
       for (int e = 0; e < 16; e += 8) {
         uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = pack2<DT>(val(d, e + 2 * j), val(d, e + 2 * j + 1));
+        for (int j = 0; j < 4; ++j) w[j] = pack_pair<DT>(val(d, e + 2 * j), val(d, e + 2 * j + 1));
         const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
         const auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
         const int at = 32 * d + 2 * e + 8 * half;
@@ -368,7 +446,7 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n) {
 // Up to 32 rows take one wave to a workgroup (more parts, no wait for other waves):
 // it reads its LDS in order, so one buffer does.
 template <int DT, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql_wattn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 3) void eql_wattn_fwd_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
   constexpr int TK = attn_fwd_tile(DT, NW), NBUF = attn_fwd_bufs(NW), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // K buffers, V buffers, flags
@@ -394,6 +472,8 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
   const bool row_ok = r < a.R && pos < len;
   const int hi = row_ok ? min(len - 1, pos + a.right) : -1, lo = pos - a.left, sk = min(a.sinks, hi + 1);
 
+  // bit k: whether the lane's row sees key k0 + k
+  auto seen_bits = [&](int k0) { return below(hi - k0 + 1) & (~below(lo - k0) | below(sk - k0)); };
   const char* const kb = (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2]) * RT::EB;
   const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
   Frag8<DT> qf[DP / 16];
@@ -402,16 +482,19 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
 
   const int i0 = (int)((int64_t)kg.n * part / a.parts), i1 = (int)((int64_t)kg.n * (part + 1) / a.parts);
   Stage<DT, DP, TK, NT> sk_, sv_;
+  const int64_t kst = a.ks[1] * RT::EB, vst = a.vs[1] * RT::EB;
+  sk_.place(tid, a.D, [&](int row) { return row * (int)kst; });
+  sv_.place(tid, a.D, [&](int row) { return row * (int)vst; });
   auto load = [&](int i) {
     const int k0 = kg.tile(i) * TK;
-    auto ok = [&](int row) { return k0 + row < len; };
-    sk_.load(tid, a.D, [&](int row) { return kb + (int64_t)min(k0 + row, len - 1) * a.ks[1] * RT::EB; }, ok);
-    sv_.load(tid, a.D, [&](int row) { return vb + (int64_t)min(k0 + row, len - 1) * a.vs[1] * RT::EB; }, ok);
+    sk_.load(row_rsrc<TK>(kb, kst, k0, len, a.D * RT::EB));
+    sv_.load(row_rsrc<TK>(vb, vst, k0, len, a.D * RT::EB));
   };
 
   floatx16 acc[DP / 32];
   float m, l;
   const float c = a.scale_log2e;
+  const LdsMap<DT, DP> map(lane);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
@@ -419,44 +502,46 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
     m = -__builtin_inff();
     l = 0.0f;
     if (i0 < i1) load(i0);
-    for (int i = i0; i < i1; ++i) {
-      const int buf = NBUF == 1 ? 0 : i & 1;
+    auto step = [&](int i, auto which) {
+      constexpr int buf = decltype(which)::value;
       char* const kt = smem + buf * TB;
       char* const vt = smem + (NBUF + buf) * TB;
       int* const flag = flags + buf * NW;
       sk_.store(tid, kt);
       sv_.store(tid, vt);
-      {
+      const int k0 = kg.tile(i) * TK;
+      const bool part_seen = !kg.whole(k0, TK);  // some row sees the tile in part
+      if (part_seen) {
         ExpMax<DT> e;
         sv_.scan(e);
         const bool any = __any(e.hit());
         if (lane == 0) flag[wave] = any;
       }
       __syncthreads();
-      const int k0 = kg.tile(i) * TK;
       if (i + 1 < i1) load(i + 1);
       if constexpr (!kCareful) {
-        if (!kg.whole(k0, TK) && any_flag<NW>(flag)) return false;
+        if (part_seen && any_flag<NW>(flag)) return false;
       }
-      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;  // no row of the wave sees the tile
+      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) return true;  // no row of the wave sees the tile
       floatx16 s[NB];
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         s[n] = floatx16{};
 #pragma unroll
-        for (int t = 0; t < DP / 16; ++t) mma32<DT>(s[n], row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
+        for (int t = 0; t < DP / 16; ++t) mma32<DT>(s[n], map.row(kt, n, t), qf[t]);
       }
       const bool whole = kw.whole(k0, TK);
-      auto sees = [&](int k) {
-        const int j = k0 + k;
-        return j <= hi && (j >= lo || j < sk);
-      };
+      auto sees = [&](int k) { return bool((seen_bits(k0 + (k & 32)) >> (k & 31)) & 1u); };
       if (!whole) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int n = 0; n < NB; ++n) {
+          const uint32_t bits = seen_bits(k0 + 32 * n) >> (4 * half);
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[n][e] = -__builtin_inff();
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t k = entry_mask(bits, e);
+            s[n][e] = bits_f32((f32_bits(s[n][e]) & k) | (0xff800000u & ~k));  // -inf
+          }
+        }
       }
       float mx = -__builtin_inff();
 #pragma unroll
@@ -478,22 +563,24 @@ __global__ __launch_bounds__(NW * 64, NW == 1 ? 1 : DT == kF32 ? 1 : 2) void eql
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -mc));
-          l += s[n][e];
-        }
-      if constexpr (kCareful) {
+        for (int e = 0; e < 16; ++e) s[n][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][e], c, -mc));
 #pragma unroll
-        for (int t = 0; t < 2 * NB; ++t)
-          mma_seen<DT, DP>(acc, vt, 16 * t, tile_frag<DT>(s[t / 2], t % 2), lane, sees);
-      } else {
+      for (int t = 0; t < 2 * NB; ++t) {
+        const Frag8<DT> p = tile_frag<DT>(s[t / 2], t % 2);
+        l = add_frag<DT>(l, p);  // of the rounded probabilities, as the numerator
+        if constexpr (kCareful) {
+          mma_seen<DT, DP>(acc, map, vt, 16 * t, p, sees);
+        } else {
 #pragma unroll
-        for (int t = 0; t < 2 * NB; ++t) {
-          const Frag8<DT> p = tile_frag<DT>(s[t / 2], t % 2);
-#pragma unroll
-          for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(vt, 16 * t, d, lane), p);
+          for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], map.col(vt, 16 * t, d), p);
         }
       }
+      return true;
+    };
+    for (int i = i0; i < i1; i += NBUF) {
+      if (!step(i, std::integral_constant<int, 0>{})) return false;
+      if constexpr (NBUF == 2)
+        if (i + 1 < i1 && !step(i + 1, std::integral_constant<int, 1>{})) return false;
     }
     return true;
   };
@@ -570,7 +657,7 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
-  constexpr int TK = attn_tile(DT), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
+  constexpr int TK = attn_tile(DT), NBUF = 2, NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // K 0, K 1, V 0, V 1, flags
   int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -593,6 +680,8 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   auto at = [&](const void* p, const int64_t (&s)[3]) {
     return (char*)p + ((int64_t)b * s[0] + (int64_t)tok * s[1] + (int64_t)head * s[2]) * RT::EB;
   };
+  // bit k: whether the lane's row sees key k0 + k
+  auto seen_bits = [&](int k0) { return below(hi - k0 + 1) & (~below(lo - k0) | below(sk - k0)); };
   const char* const kb = (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2]) * RT::EB;
   const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
   const int64_t row = (int64_t)bh * a.R + r;
@@ -619,71 +708,79 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   load_owner<DT, DP>(gf, at(a.go, a.gos), row_ok, a.D, half);
 
   Stage<DT, DP, TK, NT> sk_, sv_;
+  const int64_t kst = a.ks[1] * RT::EB, vst = a.vs[1] * RT::EB;
+  sk_.place(tid, a.D, [&](int row) { return row * (int)kst; });
+  sv_.place(tid, a.D, [&](int row) { return row * (int)vst; });
   auto load = [&](int i) {
     const int k0 = kg.tile(i) * TK;
-    auto ok = [&](int rr) { return k0 + rr < len; };
-    sk_.load(tid, a.D, [&](int rr) { return kb + (int64_t)min(k0 + rr, len - 1) * a.ks[1] * RT::EB; }, ok);
-    sv_.load(tid, a.D, [&](int rr) { return vb + (int64_t)min(k0 + rr, len - 1) * a.vs[1] * RT::EB; }, ok);
+    sk_.load(row_rsrc<TK>(kb, kst, k0, len, a.D * RT::EB));
+    sv_.load(row_rsrc<TK>(vb, vst, k0, len, a.D * RT::EB));
   };
   floatx16 acc[DP / 32];
   const float c = a.scale_log2e;
+  const LdsMap<DT, DP> map(lane);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
     if (kg.n > 0) load(0);
-    for (int i = 0; i < kg.n; ++i) {
-      char* const kt = smem + (i & 1) * TB;
-      char* const vt = smem + (2 + (i & 1)) * TB;
-      int* const flag = flags + (i & 1) * NW;
+    auto step = [&](int i, auto which) {
+      constexpr int buf = decltype(which)::value;
+      char* const kt = smem + buf * TB;
+      char* const vt = smem + (2 + buf) * TB;
+      int* const flag = flags + buf * NW;
       sk_.store(tid, kt);
       sv_.store(tid, vt);
-      {
+      const int k0 = kg.tile(i) * TK;
+      const bool part_seen = !kg.whole(k0, TK);  // some row sees the tile in part
+      if (part_seen) {
         ExpMax<DT> e;
         sk_.scan(e);
         const bool any = __any(e.hit());
         if (lane == 0) flag[wave] = any;
       }
       __syncthreads();
-      const int k0 = kg.tile(i) * TK;
       if (i + 1 < kg.n) load(i + 1);
       if constexpr (!kCareful) {
-        if (!kg.whole(k0, TK) && any_flag<NW>(flag)) return false;
+        if (part_seen && any_flag<NW>(flag)) return false;
       }
-      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) continue;
+      if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) return true;
       const bool whole = kw.whole(k0, TK);
-      auto sees = [&](int k) {
-        const int j = k0 + k;
-        return j <= hi && (j >= lo || j < sk);
-      };
+      auto sees = [&](int k) { return bool((seen_bits(k0 + (k & 32)) >> (k & 31)) & 1u); };
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         floatx16 s{}, g{};
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
-          mma32<DT>(s, row_frag<DT, DP>(kt, n * 32 + (lane & 31), t, half), qf[t]);
-          mma32<DT>(g, row_frag<DT, DP>(vt, n * 32 + (lane & 31), t, half), gf[t]);
+          mma32<DT>(s, map.row(kt, n, t), qf[t]);
+          mma32<DT>(g, map.row(vt, n, t), gf[t]);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * (g[e] - delta);
         if (!whole) {
+          const uint32_t bits = seen_bits(k0 + 32 * n) >> (4 * half);
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = 0.0f;
+          for (int e = 0; e < 16; ++e) s[e] = bits_f32(f32_bits(s[e]) & entry_mask(bits, e));
         }
         if constexpr (kCareful) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            mma_seen<DT, DP>(acc, kt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
+            mma_seen<DT, DP>(acc, map, kt, n * 32 + 16 * t, tile_frag<DT>(s, t), sees);
         } else {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const Frag8<DT> p = tile_frag<DT>(s, t);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], col_frag<DT, DP>(kt, n * 32 + 16 * t, d, lane), p);
+            for (int d = 0; d < DP / 32; ++d) mma32<DT>(acc[d], map.col(kt, n * 32 + 16 * t, d), p);
           }
         }
       }
+      return true;
+    };
+    for (int i = 0; i < kg.n; i += NBUF) {
+      if (!step(i, std::integral_constant<int, 0>{})) return false;
+      if constexpr (NBUF == 2)
+        if (i + 1 < kg.n && !step(i + 1, std::integral_constant<int, 1>{})) return false;
     }
     return true;
   };
@@ -702,7 +799,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
-  constexpr int TQ = attn_tile(DT), NT = NW * 64, NB = TQ / 32, TB = TQ * RT::RB;
+  constexpr int TQ = attn_tile(DT), NBUF = 2, NT = NW * 64, NB = TQ / 32, TB = TQ * RT::RB;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // Q 0, Q 1, dO 0, dO 1, lse 0 1, delta 0 1, flags
   float* const stats = reinterpret_cast<float*>(smem + 4 * TB);
   int* const flags = reinterpret_cast<int*>(stats + 4 * TQ);
@@ -739,6 +836,8 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   tokens(jw, jw + 31, w0, w1, f0, f1);
   tokens(j, j, l0, l1, u0, u1);
   const int rlo = l0 * a.G, rhi = l1 < l0 ? -1 : l1 * a.G + a.G - 1;  // rows that see the lane's key
+  // bit k: whether row r0 + k sees the lane's key
+  auto seen_bits = [&](int r0) { return below(rhi - r0 + 1) & ~below(rlo - r0); };
   const int wlo = w0 * a.G, whi = w1 < w0 ? -1 : w1 * a.G + a.G - 1;
   const int flo = f0 * a.G, fhi = f1 < f0 ? -1 : f1 * a.G + a.G - 1;
 
@@ -757,41 +856,57 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   const char* const gb = (const char*)a.go + ((int64_t)b * a.gos[0] + (int64_t)hk * a.G * a.gos[2]) * RT::EB;
   Stage<DT, DP, TQ, NT> sq, sg;
   float st_lse = 0.0f, st_delta = 0.0f;
-  auto load = [&](int i) {
-    const int r0 = (tq0 + i) * TQ;
-    auto ok = [&](int rr) { return r0 + rr < rend; };
-    auto addr = [&](const char* base, const int64_t (&s)[3], int rr) {
-      const unsigned x = (unsigned)min(r0 + rr, rend - 1), t = x / (unsigned)a.G;
-      return base + ((int64_t)t * s[1] + (int64_t)(x - t * a.G) * s[2]) * RT::EB;
+  // offsets of a tile's rows from its first token; the same in every tile where the
+  // head group divides the tile
+  auto place = [&](int first) {
+    auto at = [&](const int64_t (&s)[3], int rr) {
+      const unsigned x = (unsigned)(first + rr), t = x / (unsigned)a.G;
+      return (int)t * (int)(s[1] * RT::EB) + (int)(x - t * a.G) * (int)(s[2] * RT::EB);
     };
-    sq.load(tid, a.D, [&](int rr) { return addr(qb, a.qs, rr); }, ok);
-    sg.load(tid, a.D, [&](int rr) { return addr(gb, a.gos, rr); }, ok);
+    sq.place(tid, a.D, [&](int rr) { return at(a.qs, rr); });
+    sg.place(tid, a.D, [&](int rr) { return at(a.gos, rr); });
+  };
+  const bool even = TQ % a.G == 0;
+  place(0);
+  const float inv_c = 1.0f / a.scale_log2e;
+  auto load = [&](int i) {
+    const int r0 = (tq0 + i) * TQ, t0 = r0 / a.G;
+    if (!even) place(r0 - t0 * a.G);
+    const auto rq = make_rsrc(qb + t0 * a.qs[1] * RT::EB, 0x7fffffffu), rg = make_rsrc(gb + t0 * a.gos[1] * RT::EB, 0x7fffffffu);
+    sq.load_first(rq, tid, rend - r0);
+    sg.load_first(rg, tid, rend - r0);
     if (tid < TQ) {
-      const int64_t at = (int64_t)bh * a.R + min(r0 + tid, rend - 1);
-      st_lse = ok(tid) ? a.lse[at] : __builtin_inff();
-      st_delta = ok(tid) ? a.delta[at] : 0.0f;
+      const bool ok = r0 + tid < rend;
+      const int64_t at = (int64_t)bh * a.R + (ok ? r0 + tid : rend - 1);
+      st_lse = ok ? -a.lse[at] * inv_c : -__builtin_inff();
+      st_delta = ok ? -a.delta[at] : 0.0f;
     }
   };
   floatx16 dk[DP / 32], dv[DP / 32];
   const float c = a.scale_log2e;
+  // the products start from -lse / c and -delta of their rows: p = exp2(c s), ds = p g
+  const LdsMap<DT, DP> map(lane);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = floatx16{};
     if (i0 < i1) load(i0);
-    for (int i = i0; i < i1; ++i) {
-      char* const qt = smem + (i & 1) * TB;
-      char* const gt = smem + (2 + (i & 1)) * TB;
-      float* const ls = stats + (i & 1) * TQ;
-      float* const de = stats + (2 + (i & 1)) * TQ;
-      int* const flag = flags + (i & 1) * NW;
+    auto step = [&](int i, auto which) {
+      constexpr int buf = decltype(which)::value;
+      char* const qt = smem + buf * TB;
+      char* const gt = smem + (2 + buf) * TB;
+      float* const ls = stats + buf * TQ;
+      float* const de = stats + (2 + buf) * TQ;
+      int* const flag = flags + buf * NW;
       sq.store(tid, qt);
       sg.store(tid, gt);
       if (tid < TQ) {
         ls[tid] = st_lse;
         de[tid] = st_delta;
       }
-      {
+      const int r0 = (tq0 + i) * TQ;
+      const bool part_seen = !(r0 >= all_lo && r0 + TQ - 1 <= all_hi);  // some key is seen by a part of the tile
+      if (part_seen) {
         ExpMax<DT> e;
         sq.scan(e);
         sg.scan(e);
@@ -799,43 +914,50 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
         if (lane == 0) flag[wave] = any;
       }
       __syncthreads();
-      const int r0 = (tq0 + i) * TQ;
       if (i + 1 < i1) load(i + 1);
       if constexpr (!kCareful) {
-        if (!(r0 >= all_lo && r0 + TQ - 1 <= all_hi) && any_flag<NW>(flag)) return false;
+        if (part_seen && any_flag<NW>(flag)) return false;
       }
-      if (r0 > whi || r0 + TQ <= wlo) continue;
+      if (r0 > whi || r0 + TQ <= wlo) return true;
       const bool whole = r0 >= flo && r0 + TQ - 1 <= fhi;
-      auto sees = [&](int k) { return r0 + k >= rlo && r0 + k <= rhi; };
+      auto sees = [&](int k) { return bool((seen_bits(r0 + (k & 32)) >> (k & 31)) & 1u); };
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
-        floatx16 s{}, g{};
-#pragma unroll
-        for (int t = 0; t < DP / 16; ++t) {
-          mma32<DT>(s, row_frag<DT, DP>(qt, n * 32 + (lane & 31), t, half), kf[t]);
-          mma32<DT>(g, row_frag<DT, DP>(gt, n * 32 + (lane & 31), t, half), vf[t]);
-        }
+        floatx16 s, g;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const floatx4 le = *reinterpret_cast<const floatx4*>(ls + n * 32 + 8 * x + 4 * half);
           const floatx4 dl = *reinterpret_cast<const floatx4*>(de + n * 32 + 8 * x + 4 * half);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const int e = 4 * x + y;
-            s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -le[y]));
-            g[e] = s[e] * (g[e] - dl[y]);
+            s[4 * x + y] = le[y];
+            g[4 * x + y] = dl[y];
           }
         }
-        if (!whole) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!sees(n * 32 + 8 * (e >> 2) + 4 * half + (e & 3))) s[e] = g[e] = 0.0f;
+        for (int t = 0; t < DP / 16; ++t) {
+          mma32<DT>(s, map.row(qt, n, t), kf[t]);
+          mma32<DT>(g, map.row(gt, n, t), vf[t]);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[e] = __builtin_amdgcn_exp2f(s[e] * c);
+          g[e] *= s[e];
+        }
+        if (!whole) {
+          const uint32_t bits = seen_bits(r0 + 32 * n) >> (4 * half);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t k = entry_mask(bits, e);
+            s[e] = bits_f32(f32_bits(s[e]) & k);
+            g[e] = bits_f32(f32_bits(g[e]) & k);
+          }
         }
         if constexpr (kCareful) {
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
-            mma_seen<DT, DP>(dv, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), lane, sees);
-            mma_seen<DT, DP>(dk, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), lane, sees);
+            mma_seen<DT, DP>(dv, map, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), sees);
+            mma_seen<DT, DP>(dk, map, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), sees);
           }
         } else {
 #pragma unroll
@@ -843,12 +965,18 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
             const Frag8<DT> p = tile_frag<DT>(s, t), ds = tile_frag<DT>(g, t);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
-              mma32<DT>(dv[d], col_frag<DT, DP>(gt, n * 32 + 16 * t, d, lane), p);
-              mma32<DT>(dk[d], col_frag<DT, DP>(qt, n * 32 + 16 * t, d, lane), ds);
+              mma32<DT>(dv[d], map.col(gt, n * 32 + 16 * t, d), p);
+              mma32<DT>(dk[d], map.col(qt, n * 32 + 16 * t, d), ds);
             }
           }
         }
       }
+      return true;
+    };
+    for (int i = i0; i < i1; i += NBUF) {
+      if (!step(i, std::integral_constant<int, 0>{})) return false;
+      if constexpr (NBUF == 2)
+        if (i + 1 < i1 && !step(i + 1, std::integral_constant<int, 1>{})) return false;
     }
     return true;
   };

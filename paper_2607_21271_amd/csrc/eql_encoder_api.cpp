@@ -164,6 +164,9 @@ int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
     if (b > 0 && !t[i].p) return EQL_ERR_INVALID_ARG;
     for (int k = 0; k < 3; ++k)
       if (t[i].st[k] % ce != 0) return EQL_ERR_ALIGNMENT;
+    // a tile's rows are addressed by 31 bits from its first: 64 tokens and the heads
+    if ((double)(65 * (double)t[i].st[1] + (double)(t[i].query ? s->heads : 0) * (double)t[i].st[2]) * e >= 2147483648.0)
+      return EQL_ERR_UNSUPPORTED;
     if (!aligned(t[i].p, 16)) return EQL_ERR_ALIGNMENT;
     r[i] = Range{t[i].p, (size_t)b};
   }
