@@ -430,11 +430,33 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, int r0, int r1,
   return k;
 }
 
-// Workgroup number -> (part, row tile, head pair): consecutive numbers of one XCD
-// (number % 8) take consecutive tiles, whose windows overlap in its L2.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t i, uint32_t n) {
-  const uint32_t q = n / 8, rest = n % 8, x = i % 8;
-  return x * q + min(x, rest) + i / 8;
+// Workgroup number -> (sequence and key/value head, item of its n).  Workgroup i runs
+// on XCD i % 8.  From 16 items on, every XCD takes two runs of n / 16 neighbouring
+// items of each head pair, the k-th and the (15 - k)-th, k turning with the pair:
+// neighbours share what they stream in one L2, and every XCD has its share of a ragged
+// batch's long sequences and of work that grows along the sequence.  Fewer items: one
+// XCD takes whole head pairs.
+struct Item {
+  int bh, at;
+  bool ok;
+};
+__device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t n) {
+  Item r;
+  const uint32_t x = i % 8, s = i / 8;
+  if (n < kAttnFold) {
+    const uint32_t q = blocks / 8, rest = blocks % 8, id = x * q + min(x, rest) + s;
+    r.bh = (int)(id / n);
+    r.at = (int)(id % n);
+    r.ok = true;
+  } else {
+    const uint32_t c = n / kAttnFold + 1, j = s % (2 * c);
+    r.bh = (int)(s / (2 * c));
+    const uint32_t k = (x + r.bh) % 8, run = j < c ? 15 - k : k, in = j < c ? j : j - c;
+    const uint32_t lo = (uint32_t)((uint64_t)run * n / kAttnFold), hi = (uint32_t)((uint64_t)(run + 1) * n / kAttnFold);
+    r.at = (int)(lo + in);
+    r.ok = lo + in < hi;
+  }
+  return r;
 }
 
 // ---- forward ---------------------------------------------------------------
@@ -453,11 +475,10 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 
   int* const flags = reinterpret_cast<int*>(smem + 2 * NBUF * TB);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
-  const int part = id % a.parts;
-  const uint32_t rest = id / a.parts;
   const int nrt = (a.R + 32 * NW - 1) / (32 * NW);
-  const int rt = nrt - 1 - (int)(rest % nrt), bh = (int)(rest / nrt);  // long causal rows first
+  const Item item = attn_item(blockIdx.x, gridDim.x, (uint32_t)nrt * a.parts);
+  if (!item.ok) return;
+  const int part = item.at % a.parts, rt = item.at / a.parts, bh = item.bh;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int len = seq_len(a, b), start = seq_start(a, b);
 
@@ -662,9 +683,9 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
-  const int nrt = (a.R + 32 * NW - 1) / (32 * NW);
-  const int rt = nrt - 1 - (int)(id % nrt), bh = (int)(id / nrt);
+  const Item item = attn_item(blockIdx.x, gridDim.x, (uint32_t)((a.R + 32 * NW - 1) / (32 * NW)));
+  if (!item.ok) return;
+  const int rt = item.at, bh = item.bh;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int len = seq_len(a, b), start = seq_start(a, b);
   const int g0 = rt * 32 * NW, g1 = min(g0 + 32 * NW, a.R) - 1;
@@ -796,8 +817,8 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 // contiguous run for each key.  A wave owns 32 keys; key tiles that hold first
 // tokens (seen by every later row) and tiles of long runs are split into parts
 // along the rows, whose fp32 sums a second kernel adds in order.
-template <int DT, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
+template <int DT, int DP, int NW, bool DK, bool DV>
+__device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
   using RT = RowTile<DT, DP>;
   constexpr int TQ = attn_tile(DT), NBUF = 2, NT = NW * 64, NB = TQ / 32, TB = TQ * RT::RB;
   extern __shared__ __attribute__((aligned(16))) char smem[];  // Q 0, Q 1, dO 0, dO 1, lse 0 1, delta 0 1, flags
@@ -805,11 +826,9 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   int* const flags = reinterpret_cast<int*>(stats + 4 * TQ);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t id = xcd_order(blockIdx.x, gridDim.x);
-  // workgroups of one head pair: sink tiles in sink_parts parts, then the others in key_parts
-  const uint32_t per = (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts);
-  const int bh = (int)(id / per);
-  int w = (int)(id % per), kt_, part, parts;
+  // items of one head pair: sink tiles in sink_parts parts, then the others in key_parts
+  const int bh = item.bh;
+  int w = item.at, kt_, part, parts;
   if (w < a.sink_tiles * a.sink_parts) {
     parts = a.sink_parts;
     kt_ = w / parts;
@@ -846,8 +865,9 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
     const int jc = min(j, len - 1);
     load_owner<DT, DP>(kf, (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)jc * a.ks[1] + (int64_t)hk * a.ks[2]) * RT::EB,
                        j < len, a.D, half);
-    load_owner<DT, DP>(vf, (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)jc * a.vs[1] + (int64_t)hk * a.vs[2]) * RT::EB,
-                       j < len, a.D, half);
+    if constexpr (DK)
+      load_owner<DT, DP>(vf, (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)jc * a.vs[1] + (int64_t)hk * a.vs[2]) * RT::EB,
+                         j < len, a.D, half);
   }
   const int tq0 = g0 * a.G / TQ, nt = g1 < g0 ? 0 : (g1 * a.G + a.G - 1) / TQ - tq0 + 1;
   const int i0 = (int)((int64_t)nt * part / parts), i1 = (int)((int64_t)nt * (part + 1) / parts);
@@ -869,8 +889,17 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   const bool even = TQ % a.G == 0;
   place(0);
   const float inv_c = 1.0f / a.scale_log2e;
+  // The tiles in a rotated order: workgroups whose runs overlap come to a tile at about
+  // the same time, tile numbers equal modulo the length of a run, and find it in their
+  // XCD's L2.  From the run's start on, 64 runs of one head pair side by side touch
+  // 64 places, more than the L2 holds.
+  const int turn = i1 > i0 ? (int)((unsigned)(2 * a.run_tiles - (tq0 + i0) % a.run_tiles) % (unsigned)(i1 - i0)) : 0;
+  auto tile_of = [&](int i) {
+    const int x = i + turn;
+    return x < i1 ? x : x - (i1 - i0);
+  };
   auto load = [&](int i) {
-    const int r0 = (tq0 + i) * TQ, t0 = r0 / a.G;
+    const int r0 = (tq0 + tile_of(i)) * TQ, t0 = r0 / a.G;
     if (!even) place(r0 - t0 * a.G);
     const auto rq = make_rsrc(qb + t0 * a.qs[1] * RT::EB, 0x7fffffffu), rg = make_rsrc(gb + t0 * a.gos[1] * RT::EB, 0x7fffffffu);
     sq.load_first(rq, tid, rend - r0);
@@ -889,7 +918,10 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = floatx16{};
+    for (int d = 0; d < DP / 32; ++d) {
+      if constexpr (DK) dk[d] = floatx16{};
+      if constexpr (DV) dv[d] = floatx16{};
+    }
     if (i0 < i1) load(i0);
     auto step = [&](int i, auto which) {
       constexpr int buf = decltype(which)::value;
@@ -904,7 +936,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
         ls[tid] = st_lse;
         de[tid] = st_delta;
       }
-      const int r0 = (tq0 + i) * TQ;
+      const int r0 = (tq0 + tile_of(i)) * TQ;
       const bool part_seen = !(r0 >= all_lo && r0 + TQ - 1 <= all_hi);  // some key is seen by a part of the tile
       if (part_seen) {
         ExpMax<DT> e;
@@ -931,18 +963,18 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             s[4 * x + y] = le[y];
-            g[4 * x + y] = dl[y];
+            if constexpr (DK) g[4 * x + y] = dl[y];
           }
         }
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
           mma32<DT>(s, map.row(qt, n, t), kf[t]);
-          mma32<DT>(g, map.row(gt, n, t), vf[t]);
+          if constexpr (DK) mma32<DT>(g, map.row(gt, n, t), vf[t]);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s[e] = __builtin_amdgcn_exp2f(s[e] * c);
-          g[e] *= s[e];
+          if constexpr (DK) g[e] *= s[e];
         }
         if (!whole) {
           const uint32_t bits = seen_bits(r0 + 32 * n) >> (4 * half);
@@ -950,23 +982,22 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
           for (int e = 0; e < 16; ++e) {
             const uint32_t k = entry_mask(bits, e);
             s[e] = bits_f32(f32_bits(s[e]) & k);
-            g[e] = bits_f32(f32_bits(g[e]) & k);
+            if constexpr (DK) g[e] = bits_f32(f32_bits(g[e]) & k);
           }
         }
-        if constexpr (kCareful) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            mma_seen<DT, DP>(dv, map, gt, n * 32 + 16 * t, tile_frag<DT>(s, t), sees);
-            mma_seen<DT, DP>(dk, map, qt, n * 32 + 16 * t, tile_frag<DT>(g, t), sees);
-          }
-        } else {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const Frag8<DT> p = tile_frag<DT>(s, t), ds = tile_frag<DT>(g, t);
+        for (int t = 0; t < 2; ++t) {
+          Frag8<DT> p, ds;
+          if constexpr (DV) p = tile_frag<DT>(s, t);
+          if constexpr (DK) ds = tile_frag<DT>(g, t);
+          if constexpr (kCareful) {
+            if constexpr (DV) mma_seen<DT, DP>(dv, map, gt, n * 32 + 16 * t, p, sees);
+            if constexpr (DK) mma_seen<DT, DP>(dk, map, qt, n * 32 + 16 * t, ds, sees);
+          } else {
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
-              mma32<DT>(dv[d], map.col(gt, n * 32 + 16 * t, d), p);
-              mma32<DT>(dk[d], map.col(qt, n * 32 + 16 * t, d), ds);
+              if constexpr (DV) mma32<DT>(dv[d], map.col(gt, n * 32 + 16 * t, d), p);
+              if constexpr (DK) mma32<DT>(dk[d], map.col(qt, n * 32 + 16 * t, d), ds);
             }
           }
         }
@@ -986,19 +1017,28 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wa
   }
   if (parts == 1) {
     const bool ok = j < a.Lk;
-    store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
-                        ok, a.D, half);
-    store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
-                        ok, a.D, half);
+    if constexpr (DK)
+      store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
+                          ok, a.D, half);
+    if constexpr (DV)
+      store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
+                          ok, a.D, half);
   } else {
     // slot of this workgroup among the split ones of its head pair: [slot][dk, dv][key][D]
     const int64_t slots = (int64_t)a.sink_tiles * (a.sink_parts > 1 ? a.sink_parts : 0) +
                           (int64_t)(a.key_tiles - a.sink_tiles) * (a.key_parts > 1 ? a.key_parts : 0);
     const int slot = a.sink_parts > 1 ? w : w - a.sink_tiles;
     float* const p = a.part + ((bh * slots + slot) * 2 * (32 * NW) + (j - j0)) * a.D;
-    store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
-    store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)32 * NW * a.D), true, a.D, half);
+    if constexpr (DK) store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
+    if constexpr (DV) store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)32 * NW * a.D), true, a.D, half);
   }
+}
+
+template <int DT, int DP, int NW>
+__global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
+  const uint32_t per = (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts);
+  const Item item = attn_item(blockIdx.x, gridDim.x, per);
+  if (item.ok) dkv_body<DT, DP, NW, true, true>(a, item);
 }
 
 // Adds the parts of split key tiles in their order: a thread four elements of one

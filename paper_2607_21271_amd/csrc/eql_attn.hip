@@ -27,7 +27,7 @@ hipError_t launch(K k, int64_t blocks, int threads, int lds, hipStream_t stream,
 
 template <int DP>
 hipError_t fwd(const AttnArgs& a, int waves, hipStream_t stream) {
-  const int64_t n = (int64_t)a.B * a.Hkv * ((a.R + 32 * waves - 1) / (32 * waves)) * a.parts;
+  const int64_t n = attn_blocks((int64_t)a.B * a.Hkv, (int64_t)((a.R + 32 * waves - 1) / (32 * waves)) * a.parts);
   if constexpr (DT != kF32 || DP <= 64) {
     if (waves == 1) return launch(eql_wattn_fwd_kernel<DT, DP, 1>, n, 64, fwd_lds(DP, 1), stream, a);
   }
@@ -36,14 +36,15 @@ hipError_t fwd(const AttnArgs& a, int waves, hipStream_t stream) {
 
 template <int DP>
 hipError_t bwd(const AttnArgs& a, hipStream_t stream) {
-  const int64_t nq = (int64_t)a.B * a.Hkv * ((a.R + 127) / 128);
+  const int64_t nq = attn_blocks((int64_t)a.B * a.Hkv, (a.R + 127) / 128);
   if (nq > 0) {
     const hipError_t e = launch(eql_wattn_dq_kernel<DT, DP, 4>, nq, 256, fwd_lds(DP, 4), stream, a);
     if (e != hipSuccess) return e;
   }
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
   if (per == 0) return hipSuccess;
-  return launch(eql_wattn_dkv_kernel<DT, DP, kAttnDkvKeys / 32>, (int64_t)a.B * a.Hkv * per, 256, dkv_lds(DP), stream, a);
+  return launch(eql_wattn_dkv_kernel<DT, DP, kAttnDkvKeys / 32>, attn_blocks((int64_t)a.B * a.Hkv, per), 256,
+                dkv_lds(DP), stream, a);
 }
 
 // The sequences of one launch: fewer than 2^32 threads.
@@ -65,7 +66,7 @@ AttnArgs slice(const AttnArgs& a, int b0, int n) {
 
 template <>
 hipError_t wattn_fwd<DT>(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
-  const int64_t per = (int64_t)a.Hkv * ((a.R + 32 * p.waves - 1) / (32 * p.waves)) * p.parts;
+  const int64_t per = attn_blocks(a.Hkv, (int64_t)((a.R + 32 * p.waves - 1) / (32 * p.waves)) * p.parts);
   const int64_t most = p.parts > 1 ? a.B : launch_blocks(64 * p.waves) / per;  // parts are planned for small grids only
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
@@ -87,7 +88,7 @@ hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
   const bool split = a.part != nullptr;
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
   const int64_t rows = (a.R + 127) / 128;
-  const int64_t most = split ? a.B : launch_blocks(256) / (a.Hkv * (per > rows ? per : rows));
+  const int64_t most = split ? a.B : launch_blocks(256) / attn_blocks(a.Hkv, per > rows ? per : rows);
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
     const AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));

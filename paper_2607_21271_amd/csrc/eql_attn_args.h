@@ -15,6 +15,12 @@ constexpr int kAttnMaxPos = 1 << 28;
 constexpr int kAttnNoLimit = 1 << 29;
 constexpr int kAttnMaxD = 128;
 
+// Workgroups of a grid over `pairs` head pairs of n items each (attn_item).
+constexpr int kAttnFold = 16;
+constexpr int64_t attn_blocks(int64_t pairs, int64_t n) {
+  return n < kAttnFold ? pairs * n : pairs * 16 * (n / kAttnFold + 1);
+}
+
 struct AttnArgs {
   const void *q, *k, *v, *go;
   void *o, *dq, *dk, *dv;
@@ -27,6 +33,7 @@ struct AttnArgs {
   float scale, scale_log2e;
   int parts;                                        // forward: parts of a row's keys
   int key_tiles, sink_tiles, key_parts, sink_parts; // key/value gradient
+  int run_tiles;                                    // row tiles that see a key tile
 };
 
 // streamed rows of a tile; a single wave stages by itself and holds half as many

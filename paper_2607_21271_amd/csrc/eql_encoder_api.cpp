@@ -94,6 +94,7 @@ size_t attn_dkv_plan(AttnArgs& a, int dt, int cus) {
     if (parts < 1) parts = 1;
   }
   a.key_parts = (int)parts;
+  a.run_tiles = (int)(run > 1 ? run : 1);
   int64_t sp = st ? (all * parts + run - 1) / run : 1;
   if (sp > 128) sp = 128;
   a.sink_parts = (int)sp;
