@@ -134,37 +134,34 @@ struct RowTile {
 
 // A lane's places in a tile.  16 bits: offsets formed once, to which a tile's
 // place in LDS and a row block are compile-time constants of the instruction (rows
-// 16 apart share their swizzle).
+// 16 apart share their swizzle), a step or column block flips bits of the chunk.
 template <int DT, int DP>
 struct LdsMap {
   using RT = RowTile<DT, DP>;
-  int lane;
-  uint32_t row_at[DT == kF32 ? 1 : DP / 16], col_at[2][DT == kF32 ? 1 : DP / 32];
-  __device__ __forceinline__ explicit LdsMap(int lane_) : lane(lane_) {
-    if constexpr (DT != kF32) {
+  int lane, first;  // first tile row, a multiple of 32
+  uint32_t row0, col0[2];
+  __device__ __forceinline__ explicit LdsMap(int lane_, int first_ = 0) : lane(lane_), first(first_) {
+    row0 = RT::off(first + (lane & 31), lane >> 5);
+    const int e = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s) row_at[s] = RT::off(lane & 31, 2 * s + (lane >> 5));
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d) {
-          const int e = d * 32 + ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
-          col_at[j][d] = RT::off(8 * j + 4 * (lane >> 5) + ((lane & 15) >> 2), e >> 3) + (e & 7) * 2;
-        }
-    }
+    for (int j = 0; j < 2; ++j)
+      col0[j] = RT::off(first + 8 * j + 4 * (lane >> 5) + ((lane & 15) >> 2), e / RT::CE) + e % RT::CE * RT::EB;
   }
+  // The compiler forms the flipped offsets anew from here on instead of keeping them
+  // all: a kernel short of registers calls it once a tile.
+  __device__ __forceinline__ void renew() { asm volatile("" : "+v"(row0), "+v"(col0[0]), "+v"(col0[1])); }
   // Row operand: elements 16 s + 8 half .. + 7 of tile row 32 n + lane % 32.
   __device__ __forceinline__ Frag8<DT> row(const char* t, int n, int s) const {
     Frag8<DT> f;
     if constexpr (DT == kF32) {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(t + RT::off(n * 32 + (lane & 31), (2 * s + (lane >> 5)) * 2 + q));
+        const u32x4 a = *reinterpret_cast<const u32x4*>(t + RT::off(first + n * 32 + (lane & 31), (2 * s + (lane >> 5)) * 2 + q));
 #pragma unroll
         for (int j = 0; j < 4; ++j) f.w[4 * q + j] = a[j];
       }
     } else {
-      const u32x4 a = *reinterpret_cast<const u32x4*>(t + n * 32 * RT::RB + row_at[s]);
+      const u32x4 a = *reinterpret_cast<const u32x4*>(t + n * 32 * RT::RB + (row0 ^ (s << 5)));
 #pragma unroll
       for (int j = 0; j < 4; ++j) f.w[j] = a[j];
     }
@@ -179,7 +176,7 @@ struct LdsMap {
       const int e = d * 32 + (lane & 31);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int row = r0 + 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3);
+        const int row = first + r0 + 8 * (j >> 2) + 4 * (lane >> 5) + (j & 3);
         f.w[j] = *reinterpret_cast<const uint32_t*>(t + RT::off(row, e >> 2) + (e & 3) * 4);
       }
     } else {
@@ -187,7 +184,7 @@ struct LdsMap {
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) s16x4*)(t + r0 * RT::RB + col_at[j][d]));
+            (__attribute__((address_space(3))) s16x4*)(t + r0 * RT::RB + (col0[j] ^ (d << 6))));
         const u32x2 w = __builtin_bit_cast(u32x2, v);
         f.w[2 * j] = w[0];
         f.w[2 * j + 1] = w[1];
@@ -817,16 +814,25 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 // contiguous run for each key.  A wave owns 32 keys; key tiles that hold first
 // tokens (seen by every later row) and tiles of long runs are split into parts
 // along the rows, whose fp32 sums a second kernel adds in order.
-template <int DT, int DP, int NW, bool DK, bool DV>
-__device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
+// Wave groups of a workgroup, each taking its share of every tile's rows for the same
+// keys.  Heads of more than 96 16-bit elements take two: their accumulators leave no
+// room for a second workgroup on a CU, and one wave a SIMD waits for each of its reads.
+constexpr int dkv_groups(int DT, int DP) { return DT != kF32 && DP > 96 ? 2 : 1; }
+
+template <int DT, int DP>
+__global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
-  constexpr int TQ = attn_tile(DT), NBUF = 2, NT = NW * 64, NB = TQ / 32, TB = TQ * RT::RB;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // Q 0, Q 1, dO 0, dO 1, lse 0 1, delta 0 1, flags
+  constexpr int TQ = attn_tile(DT), NBUF = 2, GR = dkv_groups(DT, DP), NW = 4 * GR, NT = NW * 64, NB = TQ / 32 / GR, TB = TQ * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem[];  // Q 0, Q 1, dO 0, dO 1, lse 0 1, delta 0 1, flags, V
   float* const stats = reinterpret_cast<float*>(smem + 4 * TB);
   int* const flags = reinterpret_cast<int*>(stats + 4 * TQ);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int group = wave / 4, g32 = group * 32 * NB;  // first tile row of the wave
   // items of one head pair: sink tiles in sink_parts parts, then the others in key_parts
+  const Item item = attn_item(blockIdx.x, gridDim.x,
+                              (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts));
+  if (!item.ok) return;
   const int bh = item.bh;
   int w = item.at, kt_, part, parts;
   if (w < a.sink_tiles * a.sink_parts) {
@@ -848,9 +854,9 @@ __device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
     all0 = min(max(jb - a.right - start, 0), a.Lq);
     all1 = jb < len ? jb < a.sinks ? ends : min(ends, ja + a.left - start) : -1;
   };
-  const int j0 = kt_ * 32 * NW, jw = j0 + wave * 32, j = jw + (lane & 31);
+  const int j0 = kt_ * kAttnDkvKeys, jw = j0 + wave % 4 * 32, j = jw + (lane & 31);
   int g0, g1, w0, w1, f0, f1, l0, l1, u0, u1;
-  tokens(j0, j0 + 32 * NW - 1, g0, g1, u0, u1);
+  tokens(j0, j0 + kAttnDkvKeys - 1, g0, g1, u0, u1);
   const int all_lo = u0 * a.G, all_hi = u1 < u0 ? -1 : u1 * a.G + a.G - 1;  // rows that see every key of the workgroup
   tokens(jw, jw + 31, w0, w1, f0, f1);
   tokens(j, j, l0, l1, u0, u1);
@@ -860,15 +866,37 @@ __device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
   const int wlo = w0 * a.G, whi = w1 < w0 ? -1 : w1 * a.G + a.G - 1;
   const int flo = f0 * a.G, fhi = f1 < f0 ? -1 : f1 * a.G + a.G - 1;
 
-  Frag8<DT> kf[DP / 16], vf[DP / 16];
+  // the owners' operands: keys in registers, values too or, with two wave groups, in LDS
+  Frag8<DT> kf[DP / 16], vf[GR == 2 ? 1 : DP / 16];
+  char* const vt = reinterpret_cast<char*>(flags + 2 * NW);
+  uint32_t v0 = 0;  // the lane's first value chunk there
   {
     const int jc = min(j, len - 1);
     load_owner<DT, DP>(kf, (const char*)a.k + ((int64_t)b * a.ks[0] + (int64_t)jc * a.ks[1] + (int64_t)hk * a.ks[2]) * RT::EB,
                        j < len, a.D, half);
-    if constexpr (DK)
-      load_owner<DT, DP>(vf, (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)jc * a.vs[1] + (int64_t)hk * a.vs[2]) * RT::EB,
-                         j < len, a.D, half);
+    const char* const vrow = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)jc * a.vs[1] + (int64_t)hk * a.vs[2]) * RT::EB;
+    if constexpr (GR == 1) {
+      load_owner<DT, DP>(vf, vrow, j < len, a.D, half);
+    } else {
+      Frag8<DT> f[DP / 16];
+      load_owner<DT, DP>(f, vrow, j < len, a.D, half);
+      v0 = RT::off(j - j0, half);
+#pragma unroll
+      for (int t = 0; t < DP / 16; ++t)
+        if (group == 0) *reinterpret_cast<u32x4*>(vt + (v0 ^ (t << 5))) = u32x4{f[t].w[0], f[t].w[1], f[t].w[2], f[t].w[3]};
+    }
   }
+  auto values = [&](int t) {
+    if constexpr (GR == 1) {
+      return vf[t];
+    } else {
+      Frag8<DT> f;
+      const u32x4 x = *reinterpret_cast<const u32x4*>(vt + (v0 ^ (t << 5)));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) f.w[k] = x[k];
+      return f;
+    }
+  };
   const int tq0 = g0 * a.G / TQ, nt = g1 < g0 ? 0 : (g1 * a.G + a.G - 1) / TQ - tq0 + 1;
   const int i0 = (int)((int64_t)nt * part / parts), i1 = (int)((int64_t)nt * (part + 1) / parts);
   const int rend = max(ends + 1, 0) * a.G;  // rows with data
@@ -914,13 +942,13 @@ __device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
   floatx16 dk[DP / 32], dv[DP / 32];
   const float c = a.scale_log2e;
   // the products start from -lse / c and -delta of their rows: p = exp2(c s), ds = p g
-  const LdsMap<DT, DP> map(lane);
+  LdsMap<DT, DP> map(lane, g32);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) {
-      if constexpr (DK) dk[d] = floatx16{};
-      if constexpr (DV) dv[d] = floatx16{};
+      dk[d] = floatx16{};
+      dv[d] = floatx16{};
     }
     if (i0 < i1) load(i0);
     auto step = [&](int i, auto which) {
@@ -951,53 +979,57 @@ __device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
         if (part_seen && any_flag<NW>(flag)) return false;
       }
       if (r0 > whi || r0 + TQ <= wlo) return true;
+      if constexpr (GR == 2) {
+        map.renew();
+        asm volatile("" : "+v"(v0));
+      }
       const bool whole = r0 >= flo && r0 + TQ - 1 <= fhi;
-      auto sees = [&](int k) { return bool((seen_bits(r0 + (k & 32)) >> (k & 31)) & 1u); };
+      auto sees = [&](int k) { return bool((seen_bits(r0 + g32 + (k & 32)) >> (k & 31)) & 1u); };
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
         floatx16 s, g;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const floatx4 le = *reinterpret_cast<const floatx4*>(ls + n * 32 + 8 * x + 4 * half);
-          const floatx4 dl = *reinterpret_cast<const floatx4*>(de + n * 32 + 8 * x + 4 * half);
+          const floatx4 le = *reinterpret_cast<const floatx4*>(ls + g32 + n * 32 + 8 * x + 4 * half);
+          const floatx4 dl = *reinterpret_cast<const floatx4*>(de + g32 + n * 32 + 8 * x + 4 * half);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             s[4 * x + y] = le[y];
-            if constexpr (DK) g[4 * x + y] = dl[y];
+            g[4 * x + y] = dl[y];
           }
         }
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
           mma32<DT>(s, map.row(qt, n, t), kf[t]);
-          if constexpr (DK) mma32<DT>(g, map.row(gt, n, t), vf[t]);
+          mma32<DT>(g, map.row(gt, n, t), values(t));
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s[e] = __builtin_amdgcn_exp2f(s[e] * c);
-          if constexpr (DK) g[e] *= s[e];
+          g[e] *= s[e];
         }
         if (!whole) {
-          const uint32_t bits = seen_bits(r0 + 32 * n) >> (4 * half);
+          const uint32_t bits = seen_bits(r0 + g32 + 32 * n) >> (4 * half);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const uint32_t k = entry_mask(bits, e);
             s[e] = bits_f32(f32_bits(s[e]) & k);
-            if constexpr (DK) g[e] = bits_f32(f32_bits(g[e]) & k);
+            g[e] = bits_f32(f32_bits(g[e]) & k);
           }
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           Frag8<DT> p, ds;
-          if constexpr (DV) p = tile_frag<DT>(s, t);
-          if constexpr (DK) ds = tile_frag<DT>(g, t);
+          p = tile_frag<DT>(s, t);
+          ds = tile_frag<DT>(g, t);
           if constexpr (kCareful) {
-            if constexpr (DV) mma_seen<DT, DP>(dv, map, gt, n * 32 + 16 * t, p, sees);
-            if constexpr (DK) mma_seen<DT, DP>(dk, map, qt, n * 32 + 16 * t, ds, sees);
+            mma_seen<DT, DP>(dv, map, gt, n * 32 + 16 * t, p, sees);
+            mma_seen<DT, DP>(dk, map, qt, n * 32 + 16 * t, ds, sees);
           } else {
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
-              if constexpr (DV) mma32<DT>(dv[d], map.col(gt, n * 32 + 16 * t, d), p);
-              if constexpr (DK) mma32<DT>(dk[d], map.col(qt, n * 32 + 16 * t, d), ds);
+              mma32<DT>(dv[d], map.col(gt, n * 32 + 16 * t, d), p);
+              mma32<DT>(dk[d], map.col(qt, n * 32 + 16 * t, d), ds);
             }
           }
         }
@@ -1015,30 +1047,42 @@ __device__ __forceinline__ void dkv_body(const AttnArgs& a, const Item& item) {
     __syncthreads();
     walk(std::true_type{});
   }
+  if constexpr (GR == 2) {
+    // the second group's sums to the first, one gradient after the other
+    float* const x = reinterpret_cast<float*>(smem) + (wave % 4 * (DP / 2)) * 64 + lane;
+    auto join = [&](floatx16 (&acc)[DP / 32]) {
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (group == 1) x[(d * 16 + e) * 64] = acc[d][e];
+      __syncthreads();
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (group == 0) acc[d][e] += x[(d * 16 + e) * 64];
+    };
+    join(dk);
+    join(dv);
+    if (group == 1) return;
+  }
   if (parts == 1) {
     const bool ok = j < a.Lk;
-    if constexpr (DK)
-      store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
+    store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
                           ok, a.D, half);
-    if constexpr (DV)
-      store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
+    store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
                           ok, a.D, half);
   } else {
     // slot of this workgroup among the split ones of its head pair: [slot][dk, dv][key][D]
     const int64_t slots = (int64_t)a.sink_tiles * (a.sink_parts > 1 ? a.sink_parts : 0) +
                           (int64_t)(a.key_tiles - a.sink_tiles) * (a.key_parts > 1 ? a.key_parts : 0);
     const int slot = a.sink_parts > 1 ? w : w - a.sink_tiles;
-    float* const p = a.part + ((bh * slots + slot) * 2 * (32 * NW) + (j - j0)) * a.D;
-    if constexpr (DK) store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
-    if constexpr (DV) store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)32 * NW * a.D), true, a.D, half);
+    float* const p = a.part + ((bh * slots + slot) * 2 * kAttnDkvKeys + (j - j0)) * a.D;
+    store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
+    store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)kAttnDkvKeys * a.D), true, a.D, half);
   }
-}
-
-template <int DT, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DT == kF32 || DP > 64 ? 1 : 2) void eql_wattn_dkv_kernel(AttnArgs a) {
-  const uint32_t per = (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts);
-  const Item item = attn_item(blockIdx.x, gridDim.x, per);
-  if (item.ok) dkv_body<DT, DP, NW, true, true>(a, item);
 }
 
 // Adds the parts of split key tiles in their order: a thread four elements of one

@@ -13,7 +13,10 @@ constexpr int row_bytes(int DP) { return (DP == 96 ? 128 : DP) * kEB; }
 constexpr int fwd_lds(int DP, int NW) {
   return attn_fwd_bufs(NW) * (2 * attn_fwd_tile(DT, NW) * row_bytes(DP) + NW * 4);
 }
-constexpr int dkv_lds(int DP) { return 2 * (2 * attn_tile(DT) * row_bytes(DP) + 2 * attn_tile(DT) * 4 + 4 * 4); }
+constexpr int dkv_lds(int DP) {
+  return 2 * (2 * attn_tile(DT) * row_bytes(DP) + 2 * attn_tile(DT) * 4 + 4 * dkv_groups(DT, DP) * 4) +
+         (dkv_groups(DT, DP) == 2 ? kAttnDkvKeys * row_bytes(DP) : 0);
+}
 
 template <typename K>
 hipError_t launch(K k, int64_t blocks, int threads, int lds, hipStream_t stream, const AttnArgs& a) {
@@ -43,8 +46,8 @@ hipError_t bwd(const AttnArgs& a, hipStream_t stream) {
   }
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
   if (per == 0) return hipSuccess;
-  return launch(eql_wattn_dkv_kernel<DT, DP, kAttnDkvKeys / 32>, attn_blocks((int64_t)a.B * a.Hkv, per), 256,
-                dkv_lds(DP), stream, a);
+  return launch(eql_wattn_dkv_kernel<DT, DP>, attn_blocks((int64_t)a.B * a.Hkv, per),
+                256 * dkv_groups(DT, DP), dkv_lds(DP), stream, a);
 }
 
 // The sequences of one launch: fewer than 2^32 threads.
@@ -88,7 +91,7 @@ hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
   const bool split = a.part != nullptr;
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
   const int64_t rows = (a.R + 127) / 128;
-  const int64_t most = split ? a.B : launch_blocks(256) / attn_blocks(a.Hkv, per > rows ? per : rows);
+  const int64_t most = split ? a.B : launch_blocks(512) / attn_blocks(a.Hkv, per > rows ? per : rows);
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
     const AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
