@@ -88,7 +88,7 @@ int eqlinear_window_attention_backward(const eqlinear_window_shape* shape, const
  * x, y [B, S, C, T] contiguous, weight, bias [C], one dtype.  Mean and variance
  * (mean squared deviation) over the S positions, the C / groups channels of a
  * group and T:  y = act((x - mean) / sqrt(var + eps) * weight[c] + bias[c]).
- * stats (fp32 [B, groups, 2]: mean, 1 / sqrt(var + eps)) may be NULL; the backward
+ * stats (fp32 [B, groups, 2], 8-byte aligned: mean, 1 / sqrt(var + eps)) may be NULL; the backward
  * reads it.  Sums in fp32, one rounding.  C is a multiple of groups, T <= 16,
  * C <= 65536, groups <= 1024 (EQL_ERR_UNSUPPORTED). */
 enum { EQL_ACT_NONE = 0, EQL_ACT_RELU = 1, EQL_ACT_SILU = 2, EQL_ACT_GELU = 3 /* by erf */ };

@@ -47,7 +47,7 @@ template <int DT, int VEC, int ACT>
 hipError_t gn_bwd_a(const GnArgs& a, hipStream_t stream) {
   const unsigned n = (unsigned)(a.B * a.chunks * a.cblocks);
   hipLaunchKernelGGL((eql_gn_bsums_kernel<DT, VEC, ACT>), dim3(n), dim3(256), 0, stream, a);
-  hipLaunchKernelGGL((eql_gn_bmean_kernel<DT>), dim3((unsigned)((a.B * a.G + 3) / 4)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(eql_gn_bchunks_kernel, dim3((unsigned)(a.B * ((a.C + 63) / 64))), dim3(256), 0, stream, a);
   hipLaunchKernelGGL((eql_gn_bmap_kernel<DT, VEC, ACT>), dim3(n + (unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
@@ -75,13 +75,19 @@ hipError_t launch_rotary(int dt, const RotaryArgs& a, int vec, hipStream_t strea
   return rotary_dt<kBF16>(a, vec, stream);
 }
 
-// About four workgroups a CU over all sequences, and at least four positions for each thread.
+// About four workgroups a CU over all sequences (128 images of 3,136 positions: two a CU
+// take 20 + 30 us, four 17 + 28), and at least eight positions for each thread where
+// there are enough (a thread's start costs as much as several positions).
 void gn_plan(GnArgs& a, int vec, int cus) {
   const int nv = a.K / vec;
-  a.cblocks = (nv + 255) / 256;
-  const int step = nv >= 256 ? 1 : 256 / nv;
+  // vectors that hold whole channels: T / gcd(T, vec) of them, or a multiple
+  int whole = a.T;
+  for (int v = vec; v > 1 && whole % 2 == 0; v /= 2) whole /= 2;
+  a.width = 256 / whole * whole;
+  a.cblocks = (nv + a.width - 1) / a.width;
+  const int step = nv >= a.width ? 1 : 256 / nv;
   int64_t chunks = (4 * (int64_t)cus + a.B * a.cblocks - 1) / (a.B * a.cblocks);
-  const int64_t most = (a.S + 4 * step - 1) / (4 * step);
+  const int64_t most = (a.S + 8 * step - 1) / (8 * step);
   if (chunks > most) chunks = most;
   if (chunks < 1) chunks = 1;
   a.rows = (int)((a.S + chunks - 1) / chunks);

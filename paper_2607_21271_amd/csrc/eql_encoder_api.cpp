@@ -374,7 +374,7 @@ int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias,
   const bool empty = B == 0 || S == 0;
   if (!empty && (!x || !y)) return EQL_ERR_INVALID_ARG;
   const size_t e = elem_bytes(dtype), n = (size_t)B * S * a.K * e;
-  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, e) || !aligned(bias, e) || !aligned(stats, 4) ||
+  if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, e) || !aligned(bias, e) || !aligned(stats, 8) ||
       !aligned(workspace, 16))
     return EQL_ERR_ALIGNMENT;
   const Range out{y, n}, in[3] = {{x, n}, {weight, C * e}, {bias, C * e}};
@@ -402,7 +402,7 @@ size_t eqlinear_group_norm_act_backward_workspace_bytes(int64_t B, int64_t S, in
   eqk::GnArgs a;
   if (gn_args(B, S, T, C, groups, dtype, a) || B == 0 || S == 0) return 0;
   eqk::gn_plan(a, gn_vec(a, dtype), kPlanCus);
-  return align256((size_t)B * a.chunks * a.K * 2 * sizeof(float)) + align256((size_t)B * (C + groups) * 2 * sizeof(float));
+  return align256((size_t)B * a.chunks * C * 2 * sizeof(float)) + align256((size_t)B * C * 2 * sizeof(float));
 }
 
 int eqlinear_group_norm_act_backward(const void* x, const void* weight, const void* bias, const float* stats,
@@ -416,7 +416,7 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   if (!empty && (!x || !dy || !dx || !stats || !dw || !db)) return EQL_ERR_INVALID_ARG;
   const size_t e = elem_bytes(dtype), n = (size_t)B * S * a.K * e;
   if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16) || !aligned(weight, e) || !aligned(bias, e) ||
-      !aligned(dw, e) || !aligned(db, e) || !aligned(stats, 4) || !aligned(workspace, 16))
+      !aligned(dw, e) || !aligned(db, e) || !aligned(stats, 8) || !aligned(workspace, 16))
     return EQL_ERR_ALIGNMENT;
   const Range out[3] = {{dx, n}, {dw, C * e}, {db, C * e}}, in[4] = {{x, n}, {dy, n}, {weight, C * e}, {bias, C * e}};
   for (int i = 0; i < 3; ++i) {
@@ -428,7 +428,7 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
   eqk::gn_plan(a, vec, kPlanCus);
-  if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * groups * 64 >= 4294967296.0)
+  if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * (C + 64) * 4 >= 4294967296.0)
     return EQL_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype))
     return EQL_ERR_WORKSPACE;
@@ -442,7 +442,7 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   a.db = db;
   a.stats = const_cast<float*>(stats);
   a.part = (float*)workspace;
-  a.sums = (float*)((char*)workspace + align256((size_t)B * a.chunks * a.K * 2 * sizeof(float)));
+  a.sums = (float*)((char*)workspace + align256((size_t)B * a.chunks * C * 2 * sizeof(float)));
   a.act = act;
   return launched(eqk::launch_gn_backward(dtype, a, vec, (hipStream_t)stream));
 }

@@ -9,8 +9,8 @@
 // and column sums need no exchange until the end.  Forward: sums of x - x0 and its
 // square per chunk and group (x0 the group's first element: no cancellation
 // however far the mean lies from zero), then the map, whose workgroups add the
-// chunks' sums in order.  Backward: column sums of dz and dz xhat, one small kernel for
-// the sums per sequence, then dx together with dw and db.
+// chunks' sums in order.  Backward: channel sums of dz and dz xhat per chunk, one
+// small kernel that adds the chunks, then dx together with dw and db.
 #pragma once
 #include "eql_common.h"
 #include "eql_config.h"
@@ -24,29 +24,33 @@ struct GnArgs {
   const void *x, *w, *b, *dy;
   void *y, *dx, *dw, *db;
   float* stats;   // [B, G, 2] mean, rstd
-  float* part;    // forward [B, P, G, 2]; backward [B, P, K, 2]
-  float* sums;    // backward [B, C, 2] sums of dz xhat and dz, then [B, G, 2] means
+  float* part;    // forward [B, P, G, 2]; backward [B, chunks, C, 2]
+  float* sums;    // backward [B, C, 2]: sums of dz xhat and dz
   int64_t B, S;
   int C, T, G, K, act;
   float eps;
-  int chunks, cblocks, rows;  // chunks of `rows` positions, column blocks of 256 VEC
+  int chunks, cblocks, rows;  // chunks of `rows` positions, blocks of `width` vectors of columns
+  int width;                  // at most 256, whole channels
 };
 
-// erf by Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7: below half a unit of any
-// 16-bit result.  Full precision takes the library function.
+// The normal distribution's cdf and exp(-z^2 / 2) at z.  16-bit types: erf by
+// Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7, below half a unit of any 16-bit
+// result; its exponential is the density's.  Full precision takes the library function.
 template <int DT>
-__device__ __forceinline__ float gn_erf(float v) {
+__device__ __forceinline__ void gn_normal(float z, float& cdf, float& e) {
   if constexpr (DT == kF32) {
-    return erff(v);
+    e = expf(-0.5f * z * z);
+    cdf = 0.5f * (1.0f + erff(z * 0.70710678118654752f));
   } else {
-    const float x = __builtin_fabsf(v);
+    const float x = __builtin_fabsf(z) * 0.70710678118654752f;
     const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+    e = __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
     float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
     p = __builtin_fmaf(p, t, 1.421413741f);
     p = __builtin_fmaf(p, t, -0.284496736f);
     p = __builtin_fmaf(p, t, 0.254829592f);
-    const float r = 1.0f - p * t * __builtin_amdgcn_exp2f(-1.4426950408889634f * x * x);
-    return __builtin_copysignf(r, v);
+    const float tail = 0.5f * p * t * e;  // of |z|
+    cdf = z < 0.0f ? tail : 1.0f - tail;
   }
 }
 template <int DT>
@@ -58,8 +62,11 @@ template <int DT, int ACT>
 __device__ __forceinline__ float gn_act(float z) {
   if constexpr (ACT == kActRelu) return z > 0.0f ? z : z < 0.0f ? 0.0f : z;  // NaN stays
   else if constexpr (ACT == kActSilu) return z * gn_sigmoid<DT>(z);
-  else if constexpr (ACT == kActGelu) return 0.5f * z * (1.0f + gn_erf<DT>(z * 0.70710678118654752f));
-  else return z;
+  else if constexpr (ACT == kActGelu) {
+    float cdf, e;
+    gn_normal<DT>(z, cdf, e);
+    return z * cdf;
+  } else return z;
 }
 template <int DT, int ACT>
 __device__ __forceinline__ float gn_dact(float z) {
@@ -69,8 +76,9 @@ __device__ __forceinline__ float gn_dact(float z) {
     const float s = gn_sigmoid<DT>(z);
     return s * __builtin_fmaf(z, 1.0f - s, 1.0f);
   } else if constexpr (ACT == kActGelu) {
-    const float g = DT == kF32 ? expf(-0.5f * z * z) : __builtin_amdgcn_exp2f(-0.72134752044448170f * z * z);
-    return __builtin_fmaf(z * 0.39894228040143268f, g, 0.5f * (1.0f + gn_erf<DT>(z * 0.70710678118654752f)));
+    float cdf, e;
+    gn_normal<DT>(z, cdf, e);
+    return __builtin_fmaf(z * 0.39894228040143268f, e, cdf);
   } else {
     return 1.0f;
   }
@@ -83,10 +91,11 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // Where a workgroup and its threads stand: threads take columns col0 .. + VEC of
-// rows first, first + step, ... below last.
+// rows first, first + step, ... below last; ch, t and grp are those of col0.
 struct GnPlace {
   int64_t b, first, last;
   int chunk, cb, step, rr, cv, col0, cols;  // cols: columns of the block
+  int ch, t, grp;
   bool on;
 };
 template <int VEC>
@@ -97,16 +106,36 @@ __device__ __forceinline__ GnPlace gn_place(const GnArgs& a, uint32_t id) {
   id /= a.cblocks;
   p.chunk = id % a.chunks;
   p.b = id / a.chunks;
-  const int nvb = min(nv - p.cb * 256, 256);
+  const int nvb = min(nv - p.cb * a.width, a.width);
   p.step = 256 / nvb;
   p.rr = threadIdx.x / nvb;
   p.cv = threadIdx.x % nvb;
   p.on = p.rr < p.step;
-  p.col0 = (p.cb * 256 + p.cv) * VEC;
+  p.col0 = (p.cb * a.width + p.cv) * VEC;
   p.cols = nvb * VEC;
+  p.ch = (unsigned)p.col0 / (unsigned)a.T;
+  p.t = p.col0 - p.ch * a.T;
+  p.grp = (unsigned)p.ch / (unsigned)(a.C / a.G);
   p.first = (int64_t)p.chunk * a.rows + p.rr;
   p.last = min((int64_t)(p.chunk + 1) * a.rows, a.S);
   return p;
+}
+// f(k, channel, group) for the thread's columns col0 + k
+template <int VEC, typename F>
+__device__ __forceinline__ void gn_columns(const GnArgs& a, const GnPlace& p, F&& f) {
+  const int cg = a.C / a.G;
+  int ch = p.ch, t = p.t, g = p.grp, next = (g + 1) * cg;
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) {
+    f(k, ch, g);
+    if (++t == a.T) {
+      t = 0;
+      if (++ch == next) {
+        ++g;
+        next += cg;
+      }
+    }
+  }
 }
 
 template <int DT, int VEC>
@@ -126,11 +155,9 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
   float s1[VEC], s2[VEC], x0[VEC];
 #pragma unroll
-  for (int k = 0; k < VEC; ++k) {
-    s1[k] = s2[k] = 0.0f;
-    x0[k] = p.on ? (float)xb[(p.col0 + k) / gw * gw] : 0.0f;
-  }
+  for (int k = 0; k < VEC; ++k) s1[k] = s2[k] = x0[k] = 0.0f;
   if (p.on) {
+    gn_columns<VEC>(a, p, [&](int k, int, int g) { x0[k] = (float)xb[g * gw]; });
 #pragma unroll 4
     for (int64_t r = p.first; r < p.last; r += p.step) {
       const V v = *(const V*)(xb + r * a.K + p.col0);
@@ -150,7 +177,7 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
     }
   }
   __syncthreads();
-  const int lane = threadIdx.x & 63, c0 = p.cb * 256 * VEC;
+  const int lane = threadIdx.x & 63, c0 = p.cb * a.width * VEC;
   float* const out = a.part + ((p.b * a.chunks + p.chunk) * a.cblocks + p.cb) * a.G * 2;
   for (int g = threadIdx.x >> 6; g < a.G; g += 4) {
     const int lo = max(g * gw, c0) - c0, hi = min((g + 1) * gw, c0 + p.cols) - c0;
@@ -180,19 +207,52 @@ __global__ __launch_bounds__(256) void eql_gn_map_kernel(GnArgs a) {
   const int gw = a.K / a.G, parts = a.chunks * a.cblocks;
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
   {
-    const int lane = threadIdx.x & 63;
+    // the parts' sums: `lanes` threads a group each add every lanes-th part, then the threads of
+    // a group in order
     const float inv = 1.0f / ((float)a.S * (float)gw);
-    const float* const part = a.part + p.b * parts * a.G * 2;
-    for (int g = threadIdx.x >> 6; g < a.G; g += 4) {
+    const float2* const part = (const float2*)a.part + p.b * parts * a.G;
+    __shared__ float2 add[256];
+    const int gs = min(a.G, 256), lanes = 256 / gs;
+    for (int g0 = 0; g0 < a.G; g0 += gs) {
+      const int g = g0 + (int)threadIdx.x % gs, l = threadIdx.x / gs;
       float t1 = 0.0f, t2 = 0.0f;
-      for (int i = lane; i < parts; i += 64) {
-        t1 += part[((int64_t)i * a.G + g) * 2];
-        t2 += part[((int64_t)i * a.G + g) * 2 + 1];
+      if (g < a.G && l < lanes) {
+#pragma unroll 4
+        for (int i = l; i < parts; i += lanes) {
+          const float2 v = part[i * a.G + g];
+          t1 += v.x;
+          t2 += v.y;
+        }
+        add[threadIdx.x] = make_float2(t1, t2);
       }
-      t1 = wave_sum(t1) * inv;
-      t2 = wave_sum(t2) * inv;
-      const float var = __builtin_fmaf(-t1, t1, t2);
-      if (lane == 0) {
+      __syncthreads();
+      // sixteen neighbours of a group's threads at a time where there are many
+      for (int w = 16; w < lanes; w *= 16) {
+        if (g < a.G && l < lanes && l % w == 0) {
+          const int s = w / 16;
+          t1 = t2 = 0.0f;
+          for (int i = 0; i < 16 && l + i * s < lanes; ++i) {
+            const float2 v = add[(l + i * s) * gs + (int)threadIdx.x % gs];
+            t1 += v.x;
+            t2 += v.y;
+          }
+        }
+        __syncthreads();
+        if (g < a.G && l < lanes && l % w == 0) add[threadIdx.x] = make_float2(t1, t2);
+        __syncthreads();
+      }
+      if (g < a.G && l == 0) {
+        int w = 1;
+        while (w * 16 < lanes) w *= 16;
+        t1 = t2 = 0.0f;
+        for (int i = 0; i < lanes; i += w) {
+          const float2 v = add[i * gs + threadIdx.x];
+          t1 += v.x;
+          t2 += v.y;
+        }
+        t1 *= inv;
+        t2 *= inv;
+        const float var = __builtin_fmaf(-t1, t1, t2);
         const float mean = (float)xb[g * gw] + t1, rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);
         st[g] = make_float2(mean, rstd);
         if (a.stats && p.chunk == 0 && p.cb == 0) {
@@ -200,21 +260,20 @@ __global__ __launch_bounds__(256) void eql_gn_map_kernel(GnArgs a) {
           a.stats[(p.b * a.G + g) * 2 + 1] = rstd;
         }
       }
+      __syncthreads();
     }
   }
   __syncthreads();
   if (!p.on) return;
   float mu[VEC], m[VEC], c[VEC];
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) {
-    const int col = p.col0 + k, ch = col / a.T;
-    const float2 s = st[col / gw];
+  gn_columns<VEC>(a, p, [&](int k, int ch, int g) {
+    const float2 s = st[g];
     mu[k] = s.x;
     m[k] = s.y * (float)((const E*)a.w)[ch];
     c[k] = (float)((const E*)a.b)[ch];
-  }
+  });
   E* const yb = (E*)a.y + p.b * a.S * a.K;
-#pragma unroll 2
+#pragma unroll 4
   for (int64_t r = p.first; r < p.last; r += p.step) {
     V v = *(const V*)(xb + r * a.K + p.col0);
 #pragma unroll
@@ -230,7 +289,6 @@ __global__ __launch_bounds__(256) void eql_gn_bsums_kernel(GnArgs a) {
   using V = typename GnVec<DT, VEC>::V;
   __shared__ float red[2][256 * VEC];
   const GnPlace p = gn_place<VEC>(a, blockIdx.x);
-  const int gw = a.K / a.G;
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
   const E* const gb = (const E*)a.dy + p.b * a.S * a.K;
   float s1[VEC], s2[VEC];
@@ -238,16 +296,14 @@ __global__ __launch_bounds__(256) void eql_gn_bsums_kernel(GnArgs a) {
   for (int k = 0; k < VEC; ++k) s1[k] = s2[k] = 0.0f;
   if (p.on) {
     float mu[VEC], rs[VEC], w[VEC], c[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-      const int col = p.col0 + k, ch = col / a.T;
-      const float* const s = a.stats + (p.b * a.G + col / gw) * 2;
-      mu[k] = s[0];
-      rs[k] = s[1];
+    gn_columns<VEC>(a, p, [&](int k, int ch, int g) {
+      const float2 s = ((const float2*)a.stats)[p.b * a.G + g];
+      mu[k] = s.x;
+      rs[k] = s.y;
       w[k] = (float)((const E*)a.w)[ch];
       c[k] = (float)((const E*)a.b)[ch];
-    }
-#pragma unroll 2
+    });
+#pragma unroll 4
     for (int64_t r = p.first; r < p.last; r += p.step) {
       const V v = *(const V*)(xb + r * a.K + p.col0), g = *(const V*)(gb + r * a.K + p.col0);
 #pragma unroll
@@ -265,47 +321,45 @@ __global__ __launch_bounds__(256) void eql_gn_bsums_kernel(GnArgs a) {
     }
   }
   __syncthreads();
-  float* const out = a.part + (p.b * a.chunks + p.chunk) * a.K * 2 + (int64_t)p.cb * 256 * VEC * 2;
-  for (int i = threadIdx.x; i < p.cols * 2; i += 256) {
-    float t = 0.0f;
-    for (int r = 0; r < p.step; ++r) t += red[i & 1][r * p.cols + (i >> 1)];
-    out[i] = t;
+  // a block holds whole channels: every thread adds one channel's rows and group elements
+  const int nch = p.cols / a.T, ch0 = p.cb * a.width * VEC / a.T;
+  float2* const out = (float2*)a.part + (p.b * a.chunks + p.chunk) * a.C + ch0;
+  for (int i = threadIdx.x; i < nch; i += 256) {
+    float t1 = 0.0f, t2 = 0.0f;
+    for (int r = 0; r < p.step; ++r)
+      for (int t = 0; t < a.T; ++t) {
+        t1 += red[0][r * p.cols + i * a.T + t];
+        t2 += red[1][r * p.cols + i * a.T + t];
+      }
+    out[i] = make_float2(t1, t2);
   }
 }
 
-// Sums over the chunks and T of one sequence's channels, and from them the
-// group's means of w dz and w dz xhat: one wave a group.
-template <int DT>
-__global__ __launch_bounds__(256) void eql_gn_bmean_kernel(GnArgs a) {
-  using E = typename Elem<DT>::T;
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= a.B * a.G) return;
-  const int64_t b = i / a.G;
-  const int g = (int)(i % a.G), cg = a.C / a.G;
-  const float* const part = a.part + b * a.chunks * a.K * 2;
-  float m1 = 0.0f, m2 = 0.0f;
-  for (int c = g * cg + lane; c < (g + 1) * cg; c += 64) {
-    float t1 = 0.0f, t2 = 0.0f;
-    for (int q = 0; q < a.chunks; ++q)
-      for (int t = 0; t < a.T; ++t) {
-        t1 += part[((int64_t)q * a.K + c * a.T + t) * 2];
-        t2 += part[((int64_t)q * a.K + c * a.T + t) * 2 + 1];
-      }
-    a.sums[(b * a.C + c) * 2] = t1;
-    a.sums[(b * a.C + c) * 2 + 1] = t2;
-    const float w = (float)((const E*)a.w)[c];
-    m1 = __builtin_fmaf(w, t1, m1);
-    m2 = __builtin_fmaf(w, t2, m2);
+// Adds the chunks of one sequence's channels: 64 channels a workgroup, each by four
+// threads that take every fourth chunk.
+static __global__ __launch_bounds__(256) void eql_gn_bchunks_kernel(GnArgs a) {
+  __shared__ float2 add[256];
+  const uint32_t tiles = (uint32_t)(a.C + 63) / 64;
+  const int64_t b = blockIdx.x / tiles;
+  const int c = (int)(blockIdx.x % tiles) * 64 + (threadIdx.x & 63);
+  const float2* const part = (const float2*)a.part + b * a.chunks * a.C + c;
+  float t1 = 0.0f, t2 = 0.0f;
+  if (c < a.C) {
+#pragma unroll 8
+    for (int q = threadIdx.x >> 6; q < a.chunks; q += 4) {
+      const float2 v = part[(int64_t)q * a.C];
+      t1 += v.x;
+      t2 += v.y;
+    }
   }
-  m1 = wave_sum(m1);
-  m2 = wave_sum(m2);
-  if (lane == 0) {
-    const float inv = 1.0f / ((float)a.S * (float)(a.K / a.G));
-    float* const o = a.sums + a.B * a.C * 2 + i * 2;
-    o[0] = m1 * inv;
-    o[1] = m2 * inv;
+  add[threadIdx.x] = make_float2(t1, t2);
+  __syncthreads();
+  if (threadIdx.x >= 64 || c >= a.C) return;
+  for (int i = 64; i < 256; i += 64) {
+    t1 += add[i + threadIdx.x].x;
+    t2 += add[i + threadIdx.x].y;
   }
+  ((float2*)a.sums)[b * a.C + c] = make_float2(t1, t2);
 }
 
 // dx = rstd (w dz - mean(w dz) - xhat mean(w dz xhat)); the last workgroups add
@@ -332,24 +386,47 @@ __global__ __launch_bounds__(256) void eql_gn_bmap_kernel(GnArgs a) {
     return;
   }
   const GnPlace p = gn_place<VEC>(a, blockIdx.x);
+  __shared__ float2 means[kGnMaxGroups];  // of w dz xhat and w dz
+  {
+    const int lane = threadIdx.x & 63, cg = a.C / a.G;
+    const float inv = 1.0f / ((float)a.S * (float)(a.K / a.G));
+    const float2* const sums = (const float2*)a.sums + p.b * a.C;
+    // `lanes` neighbours of a wave a group: a power of two, at least the channels where they fit
+    int lanes = 1;
+    while (lanes < cg && lanes < 64) lanes *= 2;
+    for (int g0 = 0; g0 < a.G; g0 += 256 / lanes) {
+      const int g = g0 + (int)threadIdx.x / lanes;
+      float t1 = 0.0f, t2 = 0.0f;
+      if (g < a.G)
+        for (int i = lane % lanes; i < cg; i += lanes) {
+          const float2 v = sums[g * cg + i];
+          const float w = (float)((const E*)a.w)[g * cg + i];
+          t1 = __builtin_fmaf(w, v.x, t1);
+          t2 = __builtin_fmaf(w, v.y, t2);
+        }
+      for (int d = 1; d < lanes; d *= 2) {
+        t1 += __shfl_xor(t1, d);
+        t2 += __shfl_xor(t2, d);
+      }
+      if (g < a.G && lane % lanes == 0) means[g] = make_float2(t1 * inv, t2 * inv);
+    }
+  }
+  __syncthreads();
   if (!p.on) return;
-  const int gw = a.K / a.G;
   const int64_t base = p.b * a.S * a.K;
   const E *const xb = (const E*)a.x + base, *const gb = (const E*)a.dy + base;
   E* const ob = (E*)a.dx + base;
   float mu[VEC], rs[VEC], w[VEC], c[VEC], m1[VEC], m2[VEC];
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) {
-    const int col = p.col0 + k, ch = col / a.T;
-    const int64_t gi = p.b * a.G + col / gw;
-    mu[k] = a.stats[gi * 2];
-    rs[k] = a.stats[gi * 2 + 1];
-    m1[k] = a.sums[a.B * a.C * 2 + gi * 2];
-    m2[k] = a.sums[a.B * a.C * 2 + gi * 2 + 1];
+  gn_columns<VEC>(a, p, [&](int k, int ch, int g) {
+    const float2 s = ((const float2*)a.stats)[p.b * a.G + g], m = means[g];
+    mu[k] = s.x;
+    rs[k] = s.y;
+    m1[k] = m.x;
+    m2[k] = m.y;
     w[k] = (float)((const E*)a.w)[ch];
     c[k] = (float)((const E*)a.b)[ch];
-  }
-#pragma unroll 2
+  });
+#pragma unroll 4
   for (int64_t r = p.first; r < p.last; r += p.step) {
     V v = *(const V*)(xb + r * a.K + p.col0);
     const V g = *(const V*)(gb + r * a.K + p.col0);
