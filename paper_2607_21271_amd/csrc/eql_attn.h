@@ -671,7 +671,10 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
 
 // ---- query gradient --------------------------------------------------------
 // dq = scale sum_j ds_j k_j, ds_j = p_j (do . v_j - delta), p_j = exp2(c s_j - lse),
-// delta = do . o, which it writes for the kernel that follows.
+// delta = do . o, which it writes for the kernel that follows.  fp16: ds is rounded
+// at a power of two of its row that takes the row's largest |do| to about one, so that
+// small gradients keep their bits (a row of 1e-5 would lie below fp16's normal
+// range); the largest |do| of every wave's rows is written too.
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
@@ -704,7 +707,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
   const int64_t row = (int64_t)bh * a.R + r;
   const float lse = row_ok ? a.lse[row] : __builtin_inff();
-  float delta = 0.0f;
+  float delta = 0.0f, top = 0.0f;
   if (row_ok) {
     // each half of the wave takes every second chunk of the row
     const char *const po = at(a.o, a.os), *const pg = at(a.go, a.gos);
@@ -716,11 +719,23 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
       raw_to_floats<DT, 4>(wo, x);
       raw_to_floats<DT, 4>(wg, y);
 #pragma unroll
-      for (int j = 0; j < RT::CE; ++j) delta = __builtin_fmaf(x[j], y[j], delta);
+      for (int j = 0; j < RT::CE; ++j) {
+        delta = __builtin_fmaf(x[j], y[j], delta);
+        if constexpr (DT == kF16) top = fmaxf(top, __builtin_fabsf(y[j]) < 65536.0f ? __builtin_fabsf(y[j]) : 0.0f);  // of the finite
+      }
     }
   }
   delta = half_sum(delta);
   if (half == 0 && r < a.R) a.delta[row] = delta;
+  int raise = 0;  // ds is rounded times 2^raise, do . v - delta formed so
+  if constexpr (DT == kF16) {
+    top = half_max(top);
+    raise = -__builtin_amdgcn_frexp_expf(top);
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) a.top[((int64_t)bh * ((a.R + 32 * NW - 1) / (32 * NW)) + rt) * NW + wave] = top;
+  }
+  const float up = __builtin_ldexpf(1.0f, raise), delta_up = delta * up;
   Frag8<DT> qf[DP / 16], gf[DP / 16];
   load_owner<DT, DP>(qf, at(a.q, a.qs), row_ok, a.D, half);
   load_owner<DT, DP>(gf, at(a.go, a.gos), row_ok, a.D, half);
@@ -774,7 +789,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
           mma32<DT>(g, map.row(vt, n, t), gf[t]);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * (g[e] - delta);
+        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * __builtin_fmaf(g[e], up, -delta_up);
         if (!whole) {
           const uint32_t bits = seen_bits(k0 + 32 * n) >> (4 * half);
 #pragma unroll
@@ -806,12 +821,14 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     __syncthreads();
     walk(std::true_type{});
   }
-  store_owner<DT, DP>(acc, a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
+  store_owner<DT, DP>(acc, DT == kF16 ? __builtin_ldexpf(a.scale, -raise) : a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
 }
 
 // ---- key and value gradient ------------------------------------------------
 // dv_j = sum_r p_rj do_r, dk_j = scale sum_r ds_rj q_r over the packed rows r, a
-// contiguous run for each key.  A wave owns 32 keys; key tiles that hold first
+// contiguous run for each key.  fp16: p is rounded times 2^10 (the probabilities of a
+// row of 100,000 keys would lie below its normal range) and ds times the power of two
+// that takes the largest |do| of the head pair to about one.  A wave owns 32 keys; key tiles that hold first
 // tokens (seen by every later row) and tiles of long runs are split into parts
 // along the rows, whose fp32 sums a second kernel adds in order.
 // Wave groups of a workgroup, each taking its share of every tile's rows for the same
@@ -917,6 +934,22 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
   const bool even = TQ % a.G == 0;
   place(0);
   const float inv_c = 1.0f / a.scale_log2e;
+  int raise = 0;
+  if constexpr (DT == kF16) {
+    const int n = (a.R + 127) / 128 * 4;
+    float top = 0.0f;
+    for (int i = tid; i < n; i += NT) top = fmaxf(top, a.top[(int64_t)bh * n + i]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) stats[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[w]);
+    raise = -__builtin_amdgcn_frexp_expf(top);
+    __syncthreads();
+  }
+  constexpr float kRaiseP = DT == kF16 ? 10.0f : 0.0f;
+  const float raise_ds = __builtin_ldexpf(1.0f, raise - (int)kRaiseP);
   // The tiles in a rotated order: workgroups whose runs overlap come to a tile at about
   // the same time, tile numbers equal modulo the length of a run, and find it in their
   // XCD's L2.  From the run's start on, 64 runs of one head pair side by side touch
@@ -935,13 +968,14 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
     if (tid < TQ) {
       const bool ok = r0 + tid < rend;
       const int64_t at = (int64_t)bh * a.R + (ok ? r0 + tid : rend - 1);
-      st_lse = ok ? -a.lse[at] * inv_c : -__builtin_inff();
+      st_lse = ok ? (kRaiseP - a.lse[at]) * inv_c : -__builtin_inff();
       st_delta = ok ? -a.delta[at] : 0.0f;
     }
   };
   floatx16 dk[DP / 32], dv[DP / 32];
   const float c = a.scale_log2e;
   // the products start from -lse / c and -delta of their rows: p = exp2(c s), ds = p g
+  const float mul_k = DT == kF16 ? __builtin_ldexpf(a.scale, -raise) : a.scale, mul_v = DT == kF16 ? 0x1p-10f : 1.0f;
   LdsMap<DT, DP> map(lane, g32);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
@@ -1006,7 +1040,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s[e] = __builtin_amdgcn_exp2f(s[e] * c);
-          g[e] *= s[e];
+          g[e] *= DT == kF16 ? s[e] * raise_ds : s[e];
         }
         if (!whole) {
           const uint32_t bits = seen_bits(r0 + g32 + 32 * n) >> (4 * half);
@@ -1070,9 +1104,9 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
   }
   if (parts == 1) {
     const bool ok = j < a.Lk;
-    store_owner<DT, DP>(dk, a.scale, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
+    store_owner<DT, DP>(dk, mul_k, j < len, (char*)a.dk + ((int64_t)b * a.dks[0] + (int64_t)j * a.dks[1] + (int64_t)hk * a.dks[2]) * RT::EB,
                           ok, a.D, half);
-    store_owner<DT, DP>(dv, 1.0f, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
+    store_owner<DT, DP>(dv, mul_v, j < len, (char*)a.dv + ((int64_t)b * a.dvs[0] + (int64_t)j * a.dvs[1] + (int64_t)hk * a.dvs[2]) * RT::EB,
                           ok, a.D, half);
   } else {
     // slot of this workgroup among the split ones of its head pair: [slot][dk, dv][key][D]
@@ -1080,8 +1114,8 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
                           (int64_t)(a.key_tiles - a.sink_tiles) * (a.key_parts > 1 ? a.key_parts : 0);
     const int slot = a.sink_parts > 1 ? w : w - a.sink_tiles;
     float* const p = a.part + ((bh * slots + slot) * 2 * kAttnDkvKeys + (j - j0)) * a.D;
-    store_owner<kF32, DP>(dk, a.scale, j < len, (char*)p, true, a.D, half);
-    store_owner<kF32, DP>(dv, 1.0f, j < len, (char*)(p + (int64_t)kAttnDkvKeys * a.D), true, a.D, half);
+    store_owner<kF32, DP>(dk, mul_k, j < len, (char*)p, true, a.D, half);
+    store_owner<kF32, DP>(dv, mul_v, j < len, (char*)(p + (int64_t)kAttnDkvKeys * a.D), true, a.D, half);
   }
 }
 

@@ -229,6 +229,24 @@ def test_gradient_against_differences():
         assert abs(diff - dot) <= (h * h + 2.0 ** -22 / h) * size + 1e-3, (n, diff, dot)
 
 
+@pytest.mark.parametrize("power", [-12, 9])
+def test_fp16_gradients_far_from_one(power):
+    """Gradients of 2^-12 and 2^9 times as large are the same numbers up to the result's own rounding: no product in
+    between loses bits to fp16's range."""
+    L, D = 300, 64
+    q, k, v, do = (draw(s, "f16", 1, L, 2, D) for s in (141, 142, 143, 144))
+    k, v = k[:, :, :1].contiguous(), v[:, :, :1].contiguous()
+    do = do.clamp(-4, 4)
+    a, b = run(q, k, v, do, right=0), run(q, k, v, (do.double() * 2.0 ** power).half(), right=0)
+    for n in ("dq", "dk", "dv"):
+        x, y = a[n].double(), b[n].double() * 2.0 ** -power
+        # the scaled do is exact (or rounded by 2^-25 where it is subnormal: that error passes on like do's own size);
+        # either result is rounded once, the smaller one by 2^-25 at least
+        scale = x.abs().max()
+        bound = 2 * 2.0 ** -11 * x.abs() + 2.0 ** (-25 - min(power, 0)) * 4 + 2.0 ** -14 * scale
+        assert ((x - y).abs() <= bound).all(), (n, ((x - y).abs() - bound).max())
+
+
 def test_packed_attention_with_positions():
     """Rotary and attention in one call on a packed buffer against the two operators apart, with its gradient."""
     from paper_2607_21271_amd import attention, rotary
