@@ -61,10 +61,10 @@ def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse):
     qshape, kshape = q.shape, k.shape
     ref, need = _plan(q.dtype, qshape, kshape, q.stride(), k.stride(), v.stride(), None, None, None, None, left, right,
                       sinks, scale)
-    o = torch.empty(qshape, dtype=q.dtype, device=q.device)
+    o = torch.empty_like(q, memory_format=torch.contiguous_format)
     # lse [B, kv_heads, Lq, heads / kv_heads]
-    lse = torch.empty(qshape[0] * qshape[1] * qshape[2], dtype=torch.float32, device=q.device) if want_lse else None
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    lse = q.new_empty(qshape[:3], dtype=torch.float32) if want_lse else None
+    ws = q.new_empty((need,), dtype=torch.uint8) if need else None
     _lib.check(_lib.eqlinear_window_attention(ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
                                               ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(ws), need,
                                               ops._stream_of(q)), "eqlinear_window_attention")
@@ -74,7 +74,7 @@ def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse):
 def _backward(q, k, v, lengths, starts, o, lse, do, dq, dk, dv, left, right, sinks, scale):
     ref, need = _plan(q.dtype, q.shape, k.shape, q.stride(), k.stride(), v.stride(), do.stride(), dq.stride(),
                       dk.stride(), dv.stride(), left, right, sinks, scale)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    ws = q.new_empty((need,), dtype=torch.uint8) if need else None
     _lib.check(_lib.eqlinear_window_attention_backward(
         ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths), ops._ptr(starts), ops._ptr(o), ops._ptr(lse),
         ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv), ops._ptr(ws), need, ops._stream_of(q)),
@@ -94,18 +94,23 @@ def _check_window(left, right, sinks):
                          % (left, right, sinks))
 
 
+@functools.lru_cache(maxsize=1024)
+def _check_shapes(q, k, v, left, right, sinks):
+    if len(q) != 4 or len(k) != 4 or v != k:
+        raise ValueError("q must be [B, Lq, heads, D] and k, v [B, Lk, kv_heads, D], got %s, %s, %s"
+                         % (tuple(q), tuple(k), tuple(v)))
+    if q[0] != k[0] or q[3] != k[3] or k[2] < 1 or q[2] % k[2]:
+        raise ValueError("q %s and k %s differ in sequences or head size, or the heads do not divide" % (tuple(q), tuple(k)))
+    _check_window(left, right, sinks)
+
+
 def _check(q, k, v, lengths, starts, left, right, sinks):
     ops._dtype_code(q)
     ops._check_same_dtype(q, k=k, v=v)
-    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape:
-        raise ValueError("q must be [B, Lq, heads, D] and k, v [B, Lk, kv_heads, D], got %s, %s, %s"
-                         % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
-    if q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3] or k.shape[2] < 1 or q.shape[2] % k.shape[2]:
-        raise ValueError("q %s and k %s differ in sequences or head size, or the heads do not divide"
-                         % (tuple(q.shape), tuple(k.shape)))
-    _check_window(left, right, sinks)
+    _check_shapes(q.shape, k.shape, v.shape, left, right, sinks)
     ops._check_dev(q, k, v)
-    _check_spans(q.shape[0], q, lengths, starts)
+    if lengths is not None or starts is not None:
+        _check_spans(q.shape[0], q, lengths, starts)
 
 
 class WindowAttentionFunction(torch.autograd.Function):
@@ -122,7 +127,7 @@ class WindowAttentionFunction(torch.autograd.Function):
     @staticmethod
     def backward(ctx, go):
         q, k, v, lengths, starts, o, lse = ctx.saved_tensors
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
         _backward(q, k, v, lengths, starts, o, lse, _ready(go), dq, dk, dv, *ctx.args)
         return dq, dk, dv, None, None, None, None, None, None
 
@@ -170,7 +175,7 @@ class PackedAttentionFunction(torch.autograd.Function):
         qk, v, lengths, starts, o, lse, positions, freqs = ctx.saved_tensors
         H, kv_heads = ctx.heads
         B, L, _, D = qk.shape
-        g = torch.empty(B, L, H + 2 * kv_heads, D, dtype=qk.dtype, device=qk.device)
+        g = qk.new_empty((B, L, H + 2 * kv_heads, D))
         dqk = g[:, :, :H + kv_heads]
         _backward(qk[:, :, :H], qk[:, :, H:], v, lengths, starts, o, lse, _ready(go), dqk[:, :, :H], dqk[:, :, H:],
                   g[:, :, H + kv_heads:], *ctx.args)

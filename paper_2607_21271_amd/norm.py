@@ -25,6 +25,19 @@ def _ready(t: torch.Tensor) -> torch.Tensor:
 
 
 @functools.lru_cache(maxsize=1024)
+def _check_shapes(x, weight, bias, groups, activation):
+    if len(x) < 3:
+        raise ValueError("x must be [B, ..., C, T], got %s" % (tuple(x),))
+    C = x[-2]
+    if tuple(weight) != (C,) or tuple(bias) != (C,):
+        raise ValueError("weight and bias must be [%d], got %s and %s" % (C, tuple(weight), tuple(bias)))
+    if groups < 1 or C % groups:
+        raise ValueError("%d channels do not divide into %d groups" % (C, groups))
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation must be one of %s, got %r" % (", ".join(ACTIVATIONS), activation))
+
+
+@functools.lru_cache(maxsize=1024)
 def _plan(shape, groups, dtype):
     """(B, S, T, C, dtype code) of a call and the workspace bytes of forward and backward."""
     C, T = shape[-2:]
@@ -36,9 +49,9 @@ def _plan(shape, groups, dtype):
 
 def _forward(x, weight, bias, groups, act, eps, want_stats):
     (B, S, T, C, _, dt), need, _ = _plan(x.shape, groups, x.dtype)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty(2 * B * groups, dtype=torch.float32, device=x.device) if want_stats else None  # [B, groups, 2]
-    ws = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    y = torch.empty_like(x)
+    stats = x.new_empty((B, groups, 2), dtype=torch.float32) if want_stats else None
+    ws = x.new_empty((need,), dtype=torch.uint8) if need else None
     _lib.check(_lib.eqlinear_group_norm_act(ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(y), ops._ptr(stats),
                                             ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt, ops._stream_of(x)),
                "eqlinear_group_norm_act")
@@ -62,11 +75,11 @@ class GroupNormActFunction(torch.autograd.Function):
         groups, act = ctx.args
         (B, S, T, C, _, dt), _, need = _plan(x.shape, groups, x.dtype)
         gy = _ready(gy)
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = torch.empty_like(x)
         if x.numel() == 0:
             return dx, torch.zeros_like(weight), torch.zeros_like(bias), None, None, None
         dw, db = torch.empty_like(weight), torch.empty_like(bias)
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        ws = x.new_empty((need,), dtype=torch.uint8)
         _lib.check(_lib.eqlinear_group_norm_act_backward(
             ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(stats), ops._ptr(gy), ops._ptr(dx), ops._ptr(dw),
             ops._ptr(db), ops._ptr(ws), need, B, S, T, C, groups, act, dt, ops._stream_of(x)),
@@ -79,15 +92,7 @@ def group_norm_act(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, gr
     """y of x's shape [B, ..., C, T]; weight and bias [C]; ``activation`` none, relu, silu or gelu (by erf)."""
     ops._dtype_code(x)
     ops._check_same_dtype(x, weight=weight, bias=bias)
-    if x.dim() < 3:
-        raise ValueError("x must be [B, ..., C, T], got %s" % (tuple(x.shape),))
-    C = x.shape[-2]
-    if tuple(weight.shape) != (C,) or tuple(bias.shape) != (C,):
-        raise ValueError("weight and bias must be [%d], got %s and %s" % (C, tuple(weight.shape), tuple(bias.shape)))
-    if groups < 1 or C % groups:
-        raise ValueError("%d channels do not divide into %d groups" % (C, groups))
-    if activation not in ACTIVATIONS:
-        raise ValueError("activation must be one of %s, got %r" % (", ".join(ACTIVATIONS), activation))
+    _check_shapes(x.shape, weight.shape, bias.shape, groups, activation)
     ops._check_dev(x, weight, bias)
     act = ACTIVATIONS[activation]
     if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias.requires_grad):

@@ -54,22 +54,29 @@ def _rows(x):
     return x if x.stride(3) == 1 or x.shape[3] == 1 else x.contiguous()
 
 
-def _check(x, positions, freqs, sections, T):
-    ops._dtype_code(x)
-    if x.dim() != 4:
-        raise ValueError("x must be [B, L, heads, dh * T], got %s" % (tuple(x.shape),))
-    B, L, _, D = x.shape
+@functools.lru_cache(maxsize=1024)
+def _check_shapes(x, positions, freqs, sections, T):
+    if len(x) != 4:
+        raise ValueError("x must be [B, L, heads, dh * T], got %s" % (tuple(x),))
+    B, L, _, D = x
     if T < 1 or D % T:
         raise ValueError("head size %d is not a multiple of T = %d" % (D, T))
     if not 1 <= len(sections) <= 4 or min(sections) < 0 or sum(sections) < 1 or 2 * sum(sections) > D // T:
-        raise ValueError("sections %s do not fit %d channels (two to a pair, at most 4 axes)" % (tuple(sections), D // T))
+        raise ValueError("sections %s do not fit %d channels (two to a pair, at most 4 axes)" % (sections, D // T))
     want = (L, len(sections))
-    if tuple(positions.shape) not in (want, (B,) + want):
-        raise ValueError("positions must be %s or %s, got %s" % (want, (B,) + want, tuple(positions.shape)))
+    if tuple(positions) not in (want, (B,) + want):
+        raise ValueError("positions must be %s or %s, got %s" % (want, (B,) + want, tuple(positions)))
+    if tuple(freqs) != (sum(sections),):
+        raise ValueError("freqs must be [%d], got %s" % (sum(sections), tuple(freqs)))
+
+
+def _check(x, positions, freqs, sections, T):
+    ops._dtype_code(x)
+    _check_shapes(x.shape, positions.shape, freqs.shape, sections, T)
     if positions.dtype not in (torch.int32, torch.float32):
         raise TypeError("positions must be int32 or float32, got %s" % positions.dtype)
-    if freqs.dtype != torch.float32 or tuple(freqs.shape) != (sum(sections),):
-        raise ValueError("freqs must be float32 [%d], got %s %s" % (sum(sections), freqs.dtype, tuple(freqs.shape)))
+    if freqs.dtype != torch.float32:
+        raise ValueError("freqs must be float32, got %s" % freqs.dtype)
     ops._check_dev(x, positions, freqs)
 
 
@@ -82,7 +89,7 @@ class RotaryFunction(torch.autograd.Function):
         ctx.args = (sections, T, interleaved, inverse)
         x = _rows(x)
         return _launch(x, positions, freqs, sections, T, interleaved, inverse,
-                       torch.empty(x.shape, dtype=x.dtype, device=x.device))
+                       torch.empty_like(x, memory_format=torch.contiguous_format))
 
     @staticmethod
     def backward(ctx, gy):
@@ -90,7 +97,7 @@ class RotaryFunction(torch.autograd.Function):
         sections, T, interleaved, inverse = ctx.args
         gy = _rows(gy)
         gx = _launch(gy, positions, freqs, sections, T, interleaved, not inverse,
-                     torch.empty(gy.shape, dtype=gy.dtype, device=gy.device))
+                     torch.empty_like(gy, memory_format=torch.contiguous_format))
         return gx, None, None, None, None, None, None
 
 
@@ -110,7 +117,7 @@ def rotary_axes(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, s
         return RotaryFunction.apply(x, positions, freqs, sections, T, interleaved, inverse)
     x = _rows(x)
     return _launch(x, positions, freqs, sections, T, interleaved, inverse,
-                   torch.empty(x.shape, dtype=x.dtype, device=x.device))
+                   torch.empty_like(x, memory_format=torch.contiguous_format))
 
 
 def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, sections, T: int = 1,
