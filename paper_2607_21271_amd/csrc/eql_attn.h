@@ -292,6 +292,14 @@ __device__ __forceinline__ bool any_flag(const int* flag) {
   return __builtin_amdgcn_readfirstlane(f) != 0;
 }
 
+// Orders a wave's LDS writes before its reads by other lanes, and the other way round:
+// the hardware runs them in order, the compiler has to keep them so.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // Loads of one streamed tile of TK rows by NT threads, held in registers between
 // the load and the LDS write.  Buffer loads: an offset past the resource
 // (kDropOffset, or a row past its end) reads as zero, so a row needs no arithmetic
@@ -462,24 +470,31 @@ __device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t 
 // a tile's maximum exceeds it by 2^8: probabilities stay below 2^8, far inside
 // fp16's range.  Scores, maxima and sums in fp32; a probability is
 // rounded once to the element type, as the operand of the second product.
-// Up to 32 rows take one wave to a workgroup (more parts, no wait for other waves):
-// it reads its LDS in order, so one buffer does.
-template <int DT, int DP, int NW>
-__global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 3) void eql_wattn_fwd_kernel(AttnArgs a) {
+// Two forms.  RW = 4 waves of 32 rows each share the staged tiles.  Up to 32 rows (new
+// tokens over a cache): KEYS = 8 waves hold the same rows and take every eighth tile each,
+// in LDS of their own, without waiting for one another (a wave's LDS operations
+// run in order, so one buffer does), and join at the end.
+template <int DT, int DP, int RW, int KEYS>
+__global__ __launch_bounds__(RW * KEYS * 64, KEYS > 1 ? 2 : DT == kF32 ? 1 : DP > 64 ? 2 : 3) void eql_wattn_fwd_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
-  constexpr int TK = attn_fwd_tile(DT, NW), NBUF = attn_fwd_bufs(NW), NT = NW * 64, NB = TK / 32, TB = TK * RT::RB;
-  extern __shared__ __attribute__((aligned(16))) char smem[];  // K buffers, V buffers, flags
-  int* const flags = reinterpret_cast<int*>(smem + 2 * NBUF * TB);
-  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
-  const int wave = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int nrt = (a.R + 32 * NW - 1) / (32 * NW);
+  static_assert(RW == 1 || KEYS == 1, "waves share rows or tiles");
+  constexpr int TK = attn_fwd_tile(DT, RW), NBUF = RW == 1 ? 1 : 2, NT = RW * 64, NB = TK / 32, TB = TK * RT::RB;
+  extern __shared__ __attribute__((aligned(16))) char smem_[];  // per key wave: K buffers, V buffers; flags or statistics
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave_ = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = RW == 1 ? 0 : wave_, kwave = KEYS == 1 ? 0 : wave_;
+  const int tid = RW == 1 ? lane : threadIdx.x;  // among the threads that stage a tile
+  char* const smem = smem_ + kwave * 2 * NBUF * TB;
+  char* const tail = smem_ + KEYS * 2 * NBUF * TB;
+  int* const flags = reinterpret_cast<int*>(tail);
+  const int nrt = (a.R + 32 * RW - 1) / (32 * RW);
   const Item item = attn_item(blockIdx.x, gridDim.x, (uint32_t)nrt * a.parts);
   if (!item.ok) return;
   const int part = item.at % a.parts, rt = item.at / a.parts, bh = item.bh;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
   const int len = seq_len(a, b), start = seq_start(a, b);
 
-  const int g0 = rt * 32 * NW, g1 = min(g0 + 32 * NW, a.R) - 1;  // rows of the workgroup
+  const int g0 = rt * 32 * RW, g1 = min(g0 + 32 * RW, a.R) - 1;  // rows of the workgroup
   const int w0 = g0 + wave * 32, w1 = min(w0 + 31, a.R - 1);     // and of the wave
   const KeyRange kg = key_range(a, g0, g1, len, start, TK);
   KeyRange kw = key_range(a, w0, w1, len, start, TK);
@@ -519,26 +534,28 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 
     for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
     m = -__builtin_inff();
     l = 0.0f;
-    if (i0 < i1) load(i0);
+    if (i0 + kwave < i1) load(i0 + kwave);
     auto step = [&](int i, auto which) {
       constexpr int buf = decltype(which)::value;
       char* const kt = smem + buf * TB;
       char* const vt = smem + (NBUF + buf) * TB;
-      int* const flag = flags + buf * NW;
+      int* const flag = flags + buf * RW;
       sk_.store(tid, kt);
       sv_.store(tid, vt);
       const int k0 = kg.tile(i) * TK;
       const bool part_seen = !kg.whole(k0, TK);  // some row sees the tile in part
+      bool odd = false;
       if (part_seen) {
         ExpMax<DT> e;
         sv_.scan(e);
-        const bool any = __any(e.hit());
-        if (lane == 0) flag[wave] = any;
+        odd = __any(e.hit());
+        if (KEYS == 1 && lane == 0) flag[wave] = odd;
       }
-      __syncthreads();
-      if (i + 1 < i1) load(i + 1);
+      if constexpr (KEYS == 1) __syncthreads();
+      else wave_lds_fence();
+      if (i + KEYS < i1) load(i + KEYS);
       if constexpr (!kCareful) {
-        if (part_seen && any_flag<NW>(flag)) return false;
+        if (part_seen && (KEYS == 1 ? any_flag<RW>(flag) : odd)) return false;
       }
       if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) return true;  // no row of the wave sees the tile
       floatx16 s[NB];
@@ -595,16 +612,48 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 
       }
       return true;
     };
-    for (int i = i0; i < i1; i += NBUF) {
+    for (int i = i0 + kwave; i < i1; i += NBUF * KEYS) {
       if (!step(i, std::integral_constant<int, 0>{})) return false;
+      if constexpr (KEYS > 1) wave_lds_fence();
       if constexpr (NBUF == 2)
         if (i + 1 < i1 && !step(i + 1, std::integral_constant<int, 1>{})) return false;
     }
     return true;
   };
   if (!walk(std::false_type{})) {
-    __syncthreads();
+    if constexpr (KEYS == 1) __syncthreads();
     walk(std::true_type{});
+  }
+  if constexpr (KEYS > 1) {
+    // the waves' sums to the first wave, each through its own part of the LDS
+    float* const x = reinterpret_cast<float*>(smem_) + lane;
+    float2* const st = reinterpret_cast<float2*>(tail) + lane;
+    constexpr int kWave = 2 * NBUF * TB / 4;
+    wave_lds_fence();
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[kwave * kWave + (d * 16 + e) * 64] = acc[d][e];
+    st[kwave * 64] = make_float2(m, l);
+    __syncthreads();
+    if (kwave != 0) return;
+#pragma unroll
+    for (int w = 1; w < KEYS; ++w) m = fmaxf(m, st[w * 64].x);
+    l = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+    for (int w = 0; w < KEYS; ++w) {
+      const float2 v = st[w * 64];
+      const float f = v.x == -__builtin_inff() ? 0.0f : v.x == m ? 1.0f : __builtin_amdgcn_exp2f((v.x - m) * c);
+      l += v.y * f;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float y = x[w * kWave + (d * 16 + e) * 64];
+          acc[d][e] += f == 0.0f ? 0.0f : y * f;  // a wave that saw nothing holds no numbers
+        }
+    }
   }
   l = half_sum(l);
   if (!row_ok) l = 0.0f;
@@ -627,20 +676,24 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : DP > 64 || NW == 1 ? 2 : 
   }
 }
 
-// Joins the parts of each row (64 at most), in their order: four rows a workgroup,
-// lane p of a wave holding part p's statistics.
+// Joins the parts of each row (64 at most): lane p of a wave holds part p's statistics.
+// Up to 8 parts a wave adds a row's parts in their order; more are dealt to the four
+// waves of a workgroup, whose sums are added in theirs (32 parts of 1,024 rows of 128
+// one after another 18 us).
 template <int DT>
 __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
   using E = typename Elem<DT>::T;
+  __shared__ float add[4][2][64];
   const int64_t rows = (int64_t)a.B * a.Hkv * a.R;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= rows) return;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int deal = attn_join_waves(a.parts), first = deal == 1 ? 0 : wave;
+  const int64_t row = deal == 1 ? (int64_t)blockIdx.x * 4 + wave : blockIdx.x;
+  if (row >= rows) return;  // only where a wave has a row of its own
   float m = -__builtin_inff(), l = 0.0f;
   if (lane < a.parts) {
-    const float* const st = a.part + rows * a.parts * a.D + ((int64_t)lane * rows + row) * 2;
-    m = st[0];
-    l = st[1];
+    const float2 v = ((const float2*)(a.part + rows * a.parts * a.D))[(int64_t)lane * rows + row];
+    m = v.x;
+    l = v.y;
   }
   float top = m;
 #pragma unroll
@@ -653,12 +706,22 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
   float o0 = 0.0f, o1 = 0.0f;
   const bool c0 = lane < a.D, c1 = lane + 64 < a.D;
 #pragma unroll 8
-  for (int p = 0; p < a.parts; ++p) {
+  for (int p = first; p < a.parts; p += deal) {
     const float* const x = a.part + (p * rows + row) * a.D + lane;
-    const float g = bits_f32(__builtin_amdgcn_readlane(f32_bits(f), p));
+    const float g = __shfl(f, p);
     const float x0 = c0 ? x[0] : 0.0f, x1 = c1 ? x[64] : 0.0f;
     o0 += g == 0.0f ? 0.0f : x0 * g;  // a part that saw nothing holds no numbers
     o1 += g == 0.0f ? 0.0f : x1 * g;
+  }
+  if (deal > 1) {
+    add[wave][0][lane] = o0;
+    add[wave][1][lane] = o1;
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = 1; w < 4; ++w) {
+      o0 += add[w][0][lane];
+      o1 += add[w][1][lane];
+    }
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int bh = (int)(row / a.R), r = (int)(row % a.R);

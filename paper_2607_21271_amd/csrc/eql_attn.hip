@@ -10,9 +10,8 @@ constexpr int DT = EQK_DT;
 constexpr int kEB = DT == kF32 ? 4 : 2;
 
 constexpr int row_bytes(int DP) { return (DP == 96 ? 128 : DP) * kEB; }
-constexpr int fwd_lds(int DP, int NW) {
-  return attn_fwd_bufs(NW) * (2 * attn_fwd_tile(DT, NW) * row_bytes(DP) + NW * 4);
-}
+constexpr int fwd_lds(int DP) { return 2 * (2 * attn_tile(DT) * row_bytes(DP) + 4 * 4); }
+constexpr int few_lds(int DP, int keys) { return keys * (2 * attn_fwd_tile(DT, 1) * row_bytes(DP) + 64 * 8); }
 constexpr int dkv_lds(int DP) {
   return 2 * (2 * attn_tile(DT) * row_bytes(DP) + 2 * attn_tile(DT) * 4 + 4 * dkv_groups(DT, DP) * 4) +
          (dkv_groups(DT, DP) == 2 ? kAttnDkvKeys * row_bytes(DP) : 0);
@@ -32,16 +31,18 @@ template <int DP>
 hipError_t fwd(const AttnArgs& a, int waves, hipStream_t stream) {
   const int64_t n = attn_blocks((int64_t)a.B * a.Hkv, (int64_t)((a.R + 32 * waves - 1) / (32 * waves)) * a.parts);
   if constexpr (DT != kF32 || DP <= 64) {
-    if (waves == 1) return launch(eql_wattn_fwd_kernel<DT, DP, 1>, n, 64, fwd_lds(DP, 1), stream, a);
+    if (waves == 1 && attn_key_waves(a.parts) == 8)
+      return launch(eql_wattn_fwd_kernel<DT, DP, 1, 8>, n, 512, few_lds(DP, 8), stream, a);
+    if (waves == 1) return launch(eql_wattn_fwd_kernel<DT, DP, 1, 4>, n, 256, few_lds(DP, 4), stream, a);
   }
-  return launch(eql_wattn_fwd_kernel<DT, DP, 4>, n, 256, fwd_lds(DP, 4), stream, a);
+  return launch(eql_wattn_fwd_kernel<DT, DP, 4, 1>, n, 256, fwd_lds(DP), stream, a);
 }
 
 template <int DP>
 hipError_t bwd(const AttnArgs& a, hipStream_t stream) {
   const int64_t nq = attn_blocks((int64_t)a.B * a.Hkv, (a.R + 127) / 128);
   if (nq > 0) {
-    const hipError_t e = launch(eql_wattn_dq_kernel<DT, DP, 4>, nq, 256, fwd_lds(DP, 4), stream, a);
+    const hipError_t e = launch(eql_wattn_dq_kernel<DT, DP, 4>, nq, 256, fwd_lds(DP), stream, a);
     if (e != hipSuccess) return e;
   }
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
@@ -71,7 +72,7 @@ AttnArgs slice(const AttnArgs& a, int b0, int n) {
 template <>
 hipError_t wattn_fwd<DT>(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   const int64_t per = attn_blocks(a.Hkv, (int64_t)((a.R + 32 * p.waves - 1) / (32 * p.waves)) * p.parts);
-  const int64_t most = p.parts > 1 ? a.B : launch_blocks(64 * p.waves) / per;  // parts are planned for small grids only
+  const int64_t most = p.parts > 1 ? a.B : launch_blocks(64 * (p.waves == 1 ? attn_key_waves(p.parts) : p.waves)) / per;  // parts are planned for small grids only
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
     AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
@@ -81,7 +82,7 @@ hipError_t wattn_fwd<DT>(const AttnArgs& a, const AttnPlan& p, hipStream_t strea
                    : a.D <= 96 ? fwd<96>(s, p.waves, stream)
                                : fwd<128>(s, p.waves, stream);
     if (e == hipSuccess && p.parts > 1)
-      e = launch(eql_wattn_join_kernel<DT>, ((int64_t)s.B * s.Hkv * s.R + 3) / 4, 256, 0, stream, s);
+      e = launch(eql_wattn_join_kernel<DT>, ((int64_t)s.B * s.Hkv * s.R * attn_join_waves(p.parts) + 3) / 4, 256, 0, stream, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -21,6 +21,9 @@ constexpr int64_t attn_blocks(int64_t pairs, int64_t n) {
   return n < kAttnFold ? pairs * n : pairs * 16 * (n / kAttnFold + 1);
 }
 
+// Waves that add a row's parts.
+constexpr int attn_join_waves(int parts) { return parts > 8 ? 4 : 1; }
+
 struct AttnArgs {
   const void *q, *k, *v, *go;
   void *o, *dq, *dk, *dv;
@@ -39,10 +42,14 @@ struct AttnArgs {
 
 // streamed rows of a tile; a single wave stages by itself and holds half as many
 constexpr int attn_tile(int dt) { return dt == kF32 ? 32 : 64; }
-constexpr int attn_fwd_tile(int dt, int waves) { return waves == 1 ? 32 : attn_tile(dt); }
-constexpr int attn_fwd_bufs(int waves) { return waves == 1 ? 1 : 2; }
+constexpr int attn_fwd_tile(int dt, int row_waves) { return row_waves == 1 ? 32 : attn_tile(dt); }
+// Key waves of a workgroup of up to 32 rows: eight where they take all keys of their rows
+// (8 sequences of 12 heads, 1,028 keys: 12 us, in parts and a join 19), four where
+// the keys are split in parts (two workgroups a CU cover each other's joins).
+constexpr int attn_key_waves(int parts) { return parts == 1 ? 8 : 4; }
 
-// Waves of a forward workgroup over R packed rows, and the parts that the keys are split into.
+// Row waves of a forward workgroup (4, or 1 beside several key waves), and the parts
+// that the keys are split into.
 struct AttnPlan {
   int waves, parts;
 };

@@ -51,15 +51,17 @@ static int64_t attn_tiles(const AttnArgs& a, int64_t tk, int64_t rows) {
 
 AttnPlan attn_plan(const AttnArgs& a, int dt, int cus) {
   AttnPlan p;
-  // one wave holds 32 rows; up to that many, waves of their own share nothing (a
-  // single wave has no registers for the tiles of wide heads in full precision)
+  // Up to 32 rows the waves of a workgroup share the rows and split the keys (a wave has no
+  // registers for that with wide heads in full precision).
   p.waves = a.R <= 32 && (dt != kF32 || a.D <= 64) ? 1 : 4;
   const int64_t rows = 32 * p.waves;
   const int64_t blocks = (int64_t)a.B * a.Hkv * ((a.R + rows - 1) / rows);
-  const int64_t want = (p.waves == 1 ? 8 : 2) * (int64_t)cus;
+  // workgroups that fill the device, and the tiles that are worth a part and its join: eight of
+  // each of four waves, or two of a workgroup that shares its tiles
+  const int64_t want = (p.waves == 1 ? 8 : 2) * (int64_t)cus, least = p.waves == 1 ? 32 : 2;
   int64_t parts = 1;
   if (blocks * 2 <= want) {
-    const int64_t most = attn_tiles(a, attn_fwd_tile(dt, p.waves), rows) / 2;  // at least two tiles each
+    const int64_t most = attn_tiles(a, attn_fwd_tile(dt, p.waves), rows) / least;
     parts = want / blocks;
     if (parts > most) parts = most;
     if (parts > 64) parts = 64;
