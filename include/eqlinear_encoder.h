@@ -55,8 +55,8 @@ int eqlinear_rotary(const eqlinear_rotary_shape* shape, const void* x, const voi
  * Keys, values and gradients that a query does not see have no effect on it,
  * infinities and NaN among them.  Scores, softmax and sums in fp32, a probability
  * (and its gradient) rounded once to the dtype as the operand of the next product.
- * head_dim <= 128 and a multiple of 16 bytes; Lk <= 2^28, Lq * heads / kv_heads
- * < 2^29; 65 token strides and, of queries, all head strides within 2 GiB
+ * head_dim <= 128 and a multiple of 16 bytes; kv_heads * Lk <= 2^27 - 2^14, heads * Lq
+ * <= 2^25 - 2^14; 65 token strides and, of queries, all head strides within 2 GiB
  * (EQL_ERR_UNSUPPORTED); strides of whole 16-byte words (EQL_ERR_ALIGNMENT).
  * lse (fp32 [B, kv_heads, Lq, heads / kv_heads], logarithm to base 2, +inf for
  * a query that sees nothing) may be NULL; the backward reads it. */

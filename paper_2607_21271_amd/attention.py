@@ -14,6 +14,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib, ops, rotary
 
@@ -125,6 +126,7 @@ class WindowAttentionFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, go):
         q, k, v, lengths, starts, o, lse = ctx.saved_tensors
         dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
@@ -171,6 +173,7 @@ class PackedAttentionFunction(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, go):
         qk, v, lengths, starts, o, lse, positions, freqs = ctx.saved_tensors
         H, kv_heads = ctx.heads

@@ -72,7 +72,8 @@ AttnArgs slice(const AttnArgs& a, int b0, int n) {
 template <>
 hipError_t wattn_fwd<DT>(const AttnArgs& a, const AttnPlan& p, hipStream_t stream) {
   const int64_t per = attn_blocks(a.Hkv, (int64_t)((a.R + 32 * p.waves - 1) / (32 * p.waves)) * p.parts);
-  const int64_t most = p.parts > 1 ? a.B : launch_blocks(64 * (p.waves == 1 ? attn_key_waves(p.parts) : p.waves)) / per;  // parts are planned for small grids only
+  const int64_t join = p.parts > 1 ? ((int64_t)a.Hkv * a.R * attn_join_waves(p.parts) + 3) / 4 : 0;
+  const int64_t most = launch_blocks(512) / (per > join ? per : join);
   if (most < 1) return hipErrorInvalidValue;
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
     AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
@@ -93,8 +94,13 @@ hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
   const bool split = a.part != nullptr;
   const int64_t per = (int64_t)a.sink_tiles * a.sink_parts + (int64_t)(a.key_tiles - a.sink_tiles) * a.key_parts;
   const int64_t rows = (a.R + 127) / 128;
-  const int64_t most = split ? a.B : launch_blocks(512) / attn_blocks(a.Hkv, per > rows ? per : rows);
+  const int64_t tiles = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0);
+  const int64_t sums = 2 * tiles * ((kAttnDkvKeys * a.D + 1023) / 1024);  // workgroups that add a head pair's parts
+  int64_t grid = attn_blocks(a.Hkv, per > rows ? per : rows);
+  if (grid < sums * a.Hkv) grid = sums * a.Hkv;
+  const int64_t most = launch_blocks(512) / grid;
   if (most < 1) return hipErrorInvalidValue;
+  // (the slices use the same parts, one after another on the stream)
   for (int64_t b0 = 0; b0 < a.B; b0 += most) {
     const AttnArgs s = slice(a, (int)b0, (int)(a.B - b0 < most ? a.B - b0 : most));
     hipError_t e = a.D <= 32   ? bwd<32>(s, stream)
@@ -102,9 +108,8 @@ hipError_t wattn_bwd<DT>(const AttnArgs& a, hipStream_t stream) {
                    : a.D <= 96 ? bwd<96>(s, stream)
                                : bwd<128>(s, stream);
     if (e == hipSuccess && split) {
-      const int64_t tiles = (a.sink_parts > 1 ? a.sink_tiles : 0) + (a.key_parts > 1 ? a.key_tiles - a.sink_tiles : 0);
-      const int64_t n = 2 * tiles * s.B * s.Hkv * ((kAttnDkvKeys * a.D + 1023) / 1024);
-      hipLaunchKernelGGL(eql_wattn_dkv_sum_kernel<DT>, dim3((unsigned)n), dim3(256), 0, stream, s, kAttnDkvKeys);
+      hipLaunchKernelGGL(eql_wattn_dkv_sum_kernel<DT>, dim3((unsigned)(sums * s.B * s.Hkv)), dim3(256), 0, stream, s,
+                         kAttnDkvKeys);
       e = hipGetLastError();
     }
     if (e != hipSuccess) return e;

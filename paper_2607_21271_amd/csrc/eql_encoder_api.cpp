@@ -119,9 +119,9 @@ int window_args(const eqlinear_window_shape* s, eqk::AttnArgs& a) {
   if (s->B > (1 << 24) || s->Lk > eqk::kAttnMaxPos || s->heads > 65536 || s->Lq >= ((int64_t)1 << 29) / g ||
       s->head_dim > eqk::kAttnMaxD || (size_t)s->head_dim * e % 16 != 0)
     return EQL_ERR_UNSUPPORTED;
-  // one launch's grid holds at least one sequence
-  if (s->kv_heads * ((s->Lq * g + 31) / 32) >= ((int64_t)1 << 24) ||
-      s->kv_heads * ((s->Lk + eqk::kAttnDkvKeys - 1) / eqk::kAttnDkvKeys) >= ((int64_t)1 << 23))
+  // one launch's grid holds at least one sequence: parts included, well below 2^32 threads
+  if (s->kv_heads * ((s->Lq * g + 31) / 32) >= ((int64_t)1 << 20) ||
+      s->kv_heads * ((s->Lk + eqk::kAttnDkvKeys - 1) / eqk::kAttnDkvKeys) >= ((int64_t)1 << 20))
     return EQL_ERR_UNSUPPORTED;
   auto lim = [](int64_t v) { return v < 0 || v > eqk::kAttnNoLimit ? eqk::kAttnNoLimit : (int)v; };
   a = eqk::AttnArgs{};

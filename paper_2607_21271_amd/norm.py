@@ -12,6 +12,7 @@ import functools
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib, ops
 
@@ -70,6 +71,7 @@ class GroupNormActFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         x, weight, bias, stats = ctx.saved_tensors
         groups, act = ctx.args

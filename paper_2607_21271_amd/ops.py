@@ -46,8 +46,11 @@ def _stream(stream):
 
 
 def _stream_of(t: torch.Tensor) -> int:
-    """Handle of the current stream of t's device."""
-    return torch._C._cuda_getCurrentRawStream(t.device.index)
+    """Handle of the current stream of t's device, which has to be the current device (a launch goes there)."""
+    index = t.device.index
+    if index != torch._C._cuda_getDevice():
+        raise ValueError("tensors on cuda:%d, current device cuda:%d" % (index, torch._C._cuda_getDevice()))
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _check_dev(*ts):

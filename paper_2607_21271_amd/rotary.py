@@ -11,6 +11,7 @@ import ctypes
 import functools
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib, ops
 
@@ -92,6 +93,7 @@ class RotaryFunction(torch.autograd.Function):
                        torch.empty_like(x, memory_format=torch.contiguous_format))
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, gy):
         positions, freqs = ctx.saved_tensors
         sections, T, interleaved, inverse = ctx.args
