@@ -845,6 +845,8 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
       auto sees = [&](int k) { return bool((seen_bits(k0 + (k & 32)) >> (k & 31)) & 1u); };
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
+        // a half of the tile that no row of the wave sees
+        if (NB > 1 && (k0 + 32 * n > kw.last || (k0 + 32 * n + 32 <= kw.first && k0 + 32 * n >= kw.sink_end))) continue;
         floatx16 s{}, g{};
 #pragma unroll
         for (int t = 0; t < DP / 16; ++t) {
@@ -1084,6 +1086,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
       auto sees = [&](int k) { return bool((seen_bits(r0 + g32 + (k & 32)) >> (k & 31)) & 1u); };
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
+        if (NB > 1 && (r0 + 32 * n > whi || r0 + 32 * n + 32 <= wlo)) continue;  // no key of the wave is seen by these rows
         floatx16 s, g;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
