@@ -439,13 +439,15 @@ __device__ __forceinline__ KeyRange key_range(const AttnArgs& a, int r0, int r1,
 // on XCD i % 8.  From 16 items on, every XCD takes two runs of n / 16 neighbouring
 // items of each head pair, the k-th and the (15 - k)-th, k turning with the pair:
 // neighbours share what they stream in one L2, and every XCD has its share of a ragged
-// batch's long sequences and of work that grows along the sequence.  Fewer items: one
-// XCD takes whole head pairs.
+// batch's long sequences and of work that grows along the sequence.  The runs of the
+// half where the work is come first, of all head pairs, the others fill the end.
+// Fewer items: one XCD takes whole head pairs.
 struct Item {
   int bh, at;
   bool ok;
 };
-__device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t n) {
+template <bool LATE>
+__device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t pairs, uint32_t n) {
   Item r;
   const uint32_t x = i % 8, s = i / 8;
   if (n < kAttnFold) {
@@ -454,9 +456,11 @@ __device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t 
     r.at = (int)(id % n);
     r.ok = true;
   } else {
-    const uint32_t c = n / kAttnFold + 1, j = s % (2 * c);
-    r.bh = (int)(s / (2 * c));
-    const uint32_t k = (x + r.bh) % 8, run = j < c ? 15 - k : k, in = j < c ? j : j - c;
+    const uint32_t c = n / kAttnFold + 1;
+    const bool second = s >= pairs * c;
+    const uint32_t j = second ? s - pairs * c : s, in = j % c;
+    r.bh = (int)(j / c);
+    const uint32_t k = (x + r.bh) % 8, run = LATE != second ? 15 - k : k;
     const uint32_t lo = (uint32_t)((uint64_t)run * n / kAttnFold), hi = (uint32_t)((uint64_t)(run + 1) * n / kAttnFold);
     r.at = (int)(lo + in);
     r.ok = lo + in < hi;
@@ -488,7 +492,7 @@ __global__ __launch_bounds__(RW * KEYS * 64, KEYS > 1 ? 2 : DT == kF32 ? 1 : DP 
   char* const tail = smem_ + KEYS * 2 * NBUF * TB;
   int* const flags = reinterpret_cast<int*>(tail);
   const int nrt = (a.R + 32 * RW - 1) / (32 * RW);
-  const Item item = attn_item(blockIdx.x, gridDim.x, (uint32_t)nrt * a.parts);
+  const Item item = attn_item<true>(blockIdx.x, gridDim.x, (uint32_t)(a.B * a.Hkv), (uint32_t)nrt * a.parts);
   if (!item.ok) return;
   const int part = item.at % a.parts, rt = item.at / a.parts, bh = item.bh;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -746,7 +750,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   int* const flags = reinterpret_cast<int*>(smem + 4 * TB);
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Item item = attn_item(blockIdx.x, gridDim.x, (uint32_t)((a.R + 32 * NW - 1) / (32 * NW)));
+  const Item item = attn_item<true>(blockIdx.x, gridDim.x, (uint32_t)(a.B * a.Hkv), (uint32_t)((a.R + 32 * NW - 1) / (32 * NW)));
   if (!item.ok) return;
   const int rt = item.at, bh = item.bh;
   const int b = bh / a.Hkv, hk = bh % a.Hkv;
@@ -912,8 +916,8 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int group = wave / 4, g32 = group * 32 * NB;  // first tile row of the wave
   // items of one head pair: sink tiles in sink_parts parts, then the others in key_parts
-  const Item item = attn_item(blockIdx.x, gridDim.x,
-                              (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts));
+  const Item item = attn_item<false>(blockIdx.x, gridDim.x, (uint32_t)(a.B * a.Hkv),
+                                     (uint32_t)(a.sink_tiles * a.sink_parts + (a.key_tiles - a.sink_tiles) * a.key_parts));
   if (!item.ok) return;
   const int bh = item.bh;
   int w = item.at, kt_, part, parts;
