@@ -59,10 +59,34 @@ hipError_t gn_bwd_v(const GnArgs& a, hipStream_t stream) {
   return gn_bwd_a<DT, VEC, kActNone>(a, stream);
 }
 
+template <int DT, int ACT>
+hipError_t gn_hold_a(const GnArgs& a, bool bwd, hipStream_t stream) {
+  const dim3 n((unsigned)(a.B * a.G));
+  if (!bwd) {
+    if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, a);
+    else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 1024, 16>), n, dim3(1024), 0, stream, a);
+    return hipGetLastError();
+  }
+  if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, a);
+  else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 512, 16>), n, dim3(512), 0, stream, a);
+  hipLaunchKernelGGL((eql_gn_params_kernel<DT>), dim3((unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t gn_hold_dt(const GnArgs& a, bool bwd, hipStream_t stream) {
+  if (a.act == kActRelu) return gn_hold_a<DT, kActRelu>(a, bwd, stream);
+  if (a.act == kActSilu) return gn_hold_a<DT, kActSilu>(a, bwd, stream);
+  if (a.act == kActGelu) return gn_hold_a<DT, kActGelu>(a, bwd, stream);
+  return gn_hold_a<DT, kActNone>(a, bwd, stream);
+}
+
 // Whole 16-byte vectors, or single elements where a row of K is none.
 template <int DT>
 hipError_t gn_dt(const GnArgs& a, int vec, bool bwd, hipStream_t stream) {
   constexpr int W = DT == kF32 ? 4 : 8;
+  if (a.hold) return gn_hold_dt<DT>(a, bwd, stream);
   if (vec == W) return bwd ? gn_bwd_v<DT, W>(a, stream) : gn_fwd_v<DT, W>(a, stream);
   return bwd ? gn_bwd_v<DT, 1>(a, stream) : gn_fwd_v<DT, 1>(a, stream);
 }
@@ -78,7 +102,23 @@ hipError_t launch_rotary(int dt, const RotaryArgs& a, int vec, hipStream_t strea
 // About four workgroups a CU over all sequences (128 images of 3,136 positions: two a CU
 // take 20 + 30 us, four 17 + 28), and at least eight positions for each thread where
 // there are enough (a thread's start costs as much as several positions).
-void gn_plan(GnArgs& a, int vec, int cus) {
+void gn_plan(GnArgs& a, int vec, int cus, bool bwd) {
+  // A group in one workgroup: whole vectors of a group's columns, at most a quarter of
+  // the threads, and the fewest threads whose registers hold its rows.
+  const int gw = a.K / a.G;
+  a.hold = 0;
+  if (vec > 1 && gw % vec == 0) {
+    const int most = bwd ? 512 : 1024;
+    for (int t = 256; t <= most; t = t == 256 ? most : 2 * most) {
+      const int vpg = gw / vec;
+      if (4 * vpg > t) continue;
+      const int64_t r = (a.S + t / vpg - 1) / (t / vpg);
+      if (r > 16) continue;
+      a.hold = (int)r;
+      a.threads = t;
+      break;
+    }
+  }
   const int nv = a.K / vec;
   // vectors that hold whole channels: T / gcd(T, vec) of them, or a multiple
   int whole = a.T;

@@ -367,8 +367,8 @@ extern "C" {
 size_t eqlinear_group_norm_act_workspace_bytes(int64_t B, int64_t S, int T, int C, int groups, int dtype) {
   eqk::GnArgs a;
   if (gn_args(B, S, T, C, groups, dtype, a) || B == 0 || S == 0) return 0;
-  eqk::gn_plan(a, gn_vec(a, dtype), kPlanCus);
-  return align256((size_t)B * a.chunks * a.cblocks * groups * 2 * sizeof(float));
+  eqk::gn_plan(a, gn_vec(a, dtype), kPlanCus, false);
+  return a.hold ? 0 : align256((size_t)B * a.chunks * a.cblocks * groups * 2 * sizeof(float));
 }
 
 int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias, void* y, float* stats,
@@ -388,10 +388,11 @@ int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias,
     if (overlaps(out, r)) return EQL_ERR_INVALID_ARG;
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
-  eqk::gn_plan(a, vec, kPlanCus);
-  if ((double)B * a.chunks * a.cblocks * 256 >= 4294967296.0) return EQL_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype))
-    return EQL_ERR_WORKSPACE;
+  eqk::gn_plan(a, vec, kPlanCus, false);
+  if ((double)B * (a.hold ? (double)groups * a.threads : (double)a.chunks * a.cblocks * 256) >= 4294967296.0)
+    return EQL_ERR_UNSUPPORTED;
+  const size_t need = eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.x = x;
   a.w = weight;
@@ -407,8 +408,8 @@ int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias,
 size_t eqlinear_group_norm_act_backward_workspace_bytes(int64_t B, int64_t S, int T, int C, int groups, int dtype) {
   eqk::GnArgs a;
   if (gn_args(B, S, T, C, groups, dtype, a) || B == 0 || S == 0) return 0;
-  eqk::gn_plan(a, gn_vec(a, dtype), kPlanCus);
-  return align256((size_t)B * a.chunks * C * 2 * sizeof(float)) + align256((size_t)B * C * 2 * sizeof(float));
+  eqk::gn_plan(a, gn_vec(a, dtype), kPlanCus, true);
+  return (a.hold ? 0 : align256((size_t)B * a.chunks * C * 2 * sizeof(float))) + align256((size_t)B * C * 2 * sizeof(float));
 }
 
 int eqlinear_group_norm_act_backward(const void* x, const void* weight, const void* bias, const float* stats,
@@ -433,8 +434,9 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   }
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
-  eqk::gn_plan(a, vec, kPlanCus);
-  if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * (C + 64) * 4 >= 4294967296.0)
+  eqk::gn_plan(a, vec, kPlanCus, true);
+  if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * (C + 64) * 4 >= 4294967296.0 ||
+      (double)B * groups * 512 >= 4294967296.0)
     return EQL_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype))
     return EQL_ERR_WORKSPACE;
@@ -448,7 +450,7 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   a.db = db;
   a.stats = const_cast<float*>(stats);
   a.part = (float*)workspace;
-  a.sums = (float*)((char*)workspace + align256((size_t)B * a.chunks * C * 2 * sizeof(float)));
+  a.sums = (float*)((char*)workspace + (a.hold ? 0 : align256((size_t)B * a.chunks * C * 2 * sizeof(float))));
   a.act = act;
   return launched(eqk::launch_gn_backward(dtype, a, vec, (hipStream_t)stream));
 }

@@ -4,6 +4,8 @@
 // mean and variance of a sequence's S positions, C / G channels and T group
 // elements, so that the map commutes with the group action.
 //
+// Groups that fit the registers of a workgroup (up to 128 K 16-bit values forward, 64 K
+// backward) take one kernel that reads everything once; the others two passes.
 // Every pass gives a thread VEC fixed columns of the K and lets it walk the
 // positions of its workgroup's chunk, so weights and statistics are registers
 // and column sums need no exchange until the end.  Forward: sums of x - x0 and its
@@ -31,6 +33,8 @@ struct GnArgs {
   float eps;
   int chunks, cblocks, rows;  // chunks of `rows` positions, blocks of `width` vectors of columns
   int width;                  // at most 256, whole channels
+  int hold;                   // vectors a thread holds where a workgroup holds a group, else 0
+  int threads;                // of such a workgroup
 };
 
 // The normal distribution's cdf and exp(-z^2 / 2) at z.  16-bit types: erf by
@@ -362,6 +366,25 @@ static __global__ __launch_bounds__(256) void eql_gn_bchunks_kernel(GnArgs a) {
   ((float2*)a.sums)[b * a.C + c] = make_float2(t1, t2);
 }
 
+// dw and db: the sequences' sums of a channel, one wave each.
+template <int DT>
+__device__ __forceinline__ void gn_params(const GnArgs& a, int c) {
+  using E = typename Elem<DT>::T;
+  const int lane = threadIdx.x & 63;
+  if (c >= a.C) return;
+  float t1 = 0.0f, t2 = 0.0f;
+  for (int64_t b = lane; b < a.B; b += 64) {
+    const float2 v = ((const float2*)a.sums)[b * a.C + c];
+    t1 += v.x;
+    t2 += v.y;
+  }
+  t1 = wave_sum(t1);
+  t2 = wave_sum(t2);
+  if (lane == 0) {
+    ((E*)a.dw)[c] = (E)t1;
+    ((E*)a.db)[c] = (E)t2;
+  }
+}
 // dx = rstd (w dz - mean(w dz) - xhat mean(w dz xhat)); the last workgroups add
 // the channels' sums over the batch: dw, db, one wave a channel.
 template <int DT, int VEC, int ACT>
@@ -370,19 +393,7 @@ __global__ __launch_bounds__(256) void eql_gn_bmap_kernel(GnArgs a) {
   using V = typename GnVec<DT, VEC>::V;
   const uint32_t main = (uint32_t)(a.B * a.chunks * a.cblocks);
   if (blockIdx.x >= main) {
-    const int c = (int)(blockIdx.x - main) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (c >= a.C) return;
-    float t1 = 0.0f, t2 = 0.0f;
-    for (int64_t b = lane; b < a.B; b += 64) {
-      t1 += a.sums[(b * a.C + c) * 2];
-      t2 += a.sums[(b * a.C + c) * 2 + 1];
-    }
-    t1 = wave_sum(t1);
-    t2 = wave_sum(t2);
-    if (lane == 0) {
-      ((E*)a.dw)[c] = (E)t1;
-      ((E*)a.db)[c] = (E)t2;
-    }
+    gn_params<DT>(a, (int)(blockIdx.x - main) * 4 + (threadIdx.x >> 6));
     return;
   }
   const GnPlace p = gn_place<VEC>(a, blockIdx.x);
@@ -438,6 +449,220 @@ __global__ __launch_bounds__(256) void eql_gn_bmap_kernel(GnArgs a) {
     }
     *(V*)(ob + r * a.K + p.col0) = v;
   }
+}
+
+// ---- groups that one workgroup holds -----------------------------------------
+// A workgroup keeps its group of one sequence in registers: NT threads, each at most R
+// 16-byte vectors of fixed columns, so x (and dy) are read once and statistics are two
+// passes over registers.  Consecutive workgroups of an XCD take the groups of one
+// sequence, whose rows share cache lines.
+struct GnHold {
+  int64_t b;
+  int g, vpg, rpp, c, r0;
+  int64_t at;  // element of the thread's first vector
+  bool on;
+};
+template <int VEC, int NT>
+__device__ __forceinline__ GnHold gn_hold(const GnArgs& a) {
+  GnHold h;
+  const uint32_t n = gridDim.x, q = n / 8, rest = n % 8, xcd = blockIdx.x % 8;
+  const uint32_t id = xcd * q + min(xcd, rest) + blockIdx.x / 8;
+  h.b = id / (uint32_t)a.G;
+  h.g = (int)(id % (uint32_t)a.G);
+  h.vpg = a.K / a.G / VEC;
+  h.rpp = NT / h.vpg;
+  h.c = (int)threadIdx.x % h.vpg;
+  h.r0 = (int)threadIdx.x / h.vpg;
+  h.on = h.r0 < h.rpp;
+  h.at = (h.b * a.S + h.r0) * a.K + (int64_t)h.g * (a.K / a.G) + h.c * VEC;
+  return h;
+}
+// Sum over the workgroup, the same in every thread; `red` of NT / 64 floats of its own.
+template <int NT>
+__device__ __forceinline__ float gn_total(float v, float* red) {
+  v = wave_sum(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float t = red[0];
+#pragma unroll
+  for (int w = 1; w < NT / 64; ++w) t += red[w];
+  return t;
+}
+// f(k, channel of column k of the thread) where T elements make a channel
+template <int VEC, typename F>
+__device__ __forceinline__ void gn_hold_columns(const GnArgs& a, const GnHold& h, F&& f) {
+  int ch = h.c * VEC / a.T, t = h.c * VEC - ch * a.T;
+  ch += h.g * (a.C / a.G);
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) {
+    f(k, ch);
+    if (++t == a.T) {
+      t = 0;
+      ++ch;
+    }
+  }
+}
+
+// The elements of a held vector.  The compiler may not keep their conversions from one
+// pass over the registers to the next: twice the registers, spilled.
+template <typename V>
+__device__ __forceinline__ V gn_words(u32x4& w) {
+  asm volatile("" : "+v"(w));
+  return __builtin_bit_cast(V, w);
+}
+
+template <int DT, int ACT, int NT, int R>
+__global__ __launch_bounds__(NT) void eql_gn_hold_kernel(GnArgs a) {
+  using E = typename Elem<DT>::T;
+  constexpr int VEC = DT == kF32 ? 4 : 8;
+  using V = typename GnVec<DT, VEC>::V;
+  __shared__ float red[2][NT / 64];
+  const GnHold h = gn_hold<VEC, NT>(a);
+  const int64_t step = (int64_t)h.rpp * a.K;
+  const int rows = h.on ? (int)((a.S - h.r0 + h.rpp - 1) / h.rpp) : 0;  // of the thread
+  const E* const x = (const E*)a.x + h.at;
+  // sums of x - x0, x0 the group's first element: exact however far the mean lies from zero
+  const float x0 = (float)((const E*)a.x)[h.b * a.S * a.K + (int64_t)h.g * (a.K / a.G)];
+  u32x4 v[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) v[i] = *(const u32x4*)(x + i * step);
+  const float inv = 1.0f / ((float)a.S * (float)(a.K / a.G));
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      const V e = gn_words<V>(v[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) s += (float)e.e[k] - x0;
+    }
+  const float mean = x0 + gn_total<NT>(s, red[0]) * inv;
+  s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      const V e = gn_words<V>(v[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const float d = (float)e.e[k] - mean;
+        s = __builtin_fmaf(d, d, s);
+      }
+    }
+  const float rstd = 1.0f / sqrtf(gn_total<NT>(s, red[1]) * inv + a.eps);
+  if (a.stats && threadIdx.x == 0) ((float2*)a.stats)[h.b * a.G + h.g] = make_float2(mean, rstd);
+  float m[VEC], c[VEC];
+  gn_hold_columns<VEC>(a, h, [&](int k, int ch) {
+    m[k] = h.on ? rstd * (float)((const E*)a.w)[ch] : 0.0f;
+    c[k] = h.on ? (float)((const E*)a.b)[ch] : 0.0f;
+  });
+  E* const y = (E*)a.y + h.at;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      V e = gn_words<V>(v[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) e.e[k] = (E)gn_act<DT, ACT>(__builtin_fmaf((float)e.e[k] - mean, m[k], c[k]));
+      *(V*)(y + i * step) = e;
+    }
+}
+
+template <int DT, int ACT, int NT, int R>
+__global__ __launch_bounds__(NT) void eql_gn_bhold_kernel(GnArgs a) {
+  using E = typename Elem<DT>::T;
+  constexpr int VEC = DT == kF32 ? 4 : 8;
+  using V = typename GnVec<DT, VEC>::V;
+  __shared__ float col[2][NT * VEC];
+  __shared__ float red[2][NT / 64];
+  const GnHold h = gn_hold<VEC, NT>(a);
+  const int64_t step = (int64_t)h.rpp * a.K;
+  const int rows = h.on ? (int)((a.S - h.r0 + h.rpp - 1) / h.rpp) : 0;
+  const E *const x = (const E*)a.x + h.at, *const gy = (const E*)a.dy + h.at;
+  u32x4 v[R], g[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      v[i] = *(const u32x4*)(x + i * step);
+      g[i] = *(const u32x4*)(gy + i * step);
+    }
+  const float2 st = ((const float2*)a.stats)[h.b * a.G + h.g];
+  const float mu = st.x, rs = st.y;
+  float w[VEC], c[VEC], s1[VEC], s2[VEC];
+  gn_hold_columns<VEC>(a, h, [&](int k, int ch) {
+    w[k] = h.on ? (float)((const E*)a.w)[ch] : 0.0f;
+    c[k] = h.on ? (float)((const E*)a.b)[ch] : 0.0f;
+    s1[k] = s2[k] = 0.0f;
+  });
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      const V e = gn_words<V>(v[i]), d = gn_words<V>(g[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const float xh = ((float)e.e[k] - mu) * rs;
+        const float dz = (float)d.e[k] * gn_dact<DT, ACT>(__builtin_fmaf(xh, w[k], c[k]));
+        s1[k] = __builtin_fmaf(dz, xh, s1[k]);
+        s2[k] += dz;
+      }
+    }
+  // columns over the rows of threads, halves onto halves
+  const int width = h.vpg * VEC, me = h.r0 * width + h.c * VEC;
+  int half = 1;
+  while (half < h.rpp) half *= 2;
+  if (h.on) {
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) {
+      col[0][me + k] = s1[k];
+      col[1][me + k] = s2[k];
+    }
+  }
+  for (half /= 2; half > 0; half /= 2) {
+    __syncthreads();
+    if (h.r0 < half && h.r0 + half < h.rpp) {
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        col[0][me + k] += col[0][me + half * width + k];
+        col[1][me + k] += col[1][me + half * width + k];
+      }
+    }
+  }
+  __syncthreads();
+  // channels over T, and the group's means
+  const int cg = a.C / a.G;
+  float m1 = 0.0f, m2 = 0.0f;
+  for (int i = threadIdx.x; i < cg; i += NT) {
+    float t1 = 0.0f, t2 = 0.0f;
+    for (int t = 0; t < a.T; ++t) {
+      t1 += col[0][i * a.T + t];
+      t2 += col[1][i * a.T + t];
+    }
+    const int ch = h.g * cg + i;
+    ((float2*)a.sums)[h.b * a.C + ch] = make_float2(t1, t2);
+    const float wc = (float)((const E*)a.w)[ch];
+    m1 = __builtin_fmaf(wc, t1, m1);
+    m2 = __builtin_fmaf(wc, t2, m2);
+  }
+  const float inv = 1.0f / ((float)a.S * (float)(a.K / a.G));
+  m1 = gn_total<NT>(m1, red[0]) * inv;
+  m2 = gn_total<NT>(m2, red[1]) * inv;
+  E* const dx = (E*)a.dx + h.at;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (i < rows) {
+      V e = gn_words<V>(v[i]);
+      const V d = gn_words<V>(g[i]);
+#pragma unroll
+      for (int k = 0; k < VEC; ++k) {
+        const float xh = ((float)e.e[k] - mu) * rs;
+        const float dz = (float)d.e[k] * gn_dact<DT, ACT>(__builtin_fmaf(xh, w[k], c[k]));
+        e.e[k] = (E)(rs * (__builtin_fmaf(-xh, m1, __builtin_fmaf(w[k], dz, -m2))));
+      }
+      *(V*)(dx + i * step) = e;
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void eql_gn_params_kernel(GnArgs a) {
+  gn_params<DT>(a, (int)blockIdx.x * 4 + (threadIdx.x >> 6));
 }
 
 }  // namespace eqk

@@ -113,7 +113,7 @@ def gnb(x=P, w=Q, b=Q + 4096, stats=Q + 8192, dy=R, dx=S, dw=Q + 16384, db=Q + 2
     (dict(B=-1), L.EQL_ERR_INVALID_ARG), (dict(act=4), L.EQL_ERR_INVALID_ARG), (dict(x=None), L.EQL_ERR_INVALID_ARG),
     (dict(w=None), L.EQL_ERR_INVALID_ARG), (dict(T=17), L.EQL_ERR_UNSUPPORTED), (dict(C=2050, G=1025), L.EQL_ERR_UNSUPPORTED),
     (dict(x=P + 8), L.EQL_ERR_ALIGNMENT), (dict(b=Q + 4097), L.EQL_ERR_ALIGNMENT),
-    (dict(ws=None), L.EQL_ERR_WORKSPACE), (dict(nws=8), L.EQL_ERR_WORKSPACE)])
+    (dict(ws=None, S_=1 << 16), L.EQL_ERR_WORKSPACE), (dict(nws=8, S_=1 << 16), L.EQL_ERR_WORKSPACE)])
 def test_group_norm_arguments(kw, status):
     assert gn(**kw) == status
     assert gnb(**kw) == status
@@ -125,4 +125,4 @@ def test_group_norm_own_arguments():
     assert gnb(dx=P + 16) == L.EQL_ERR_INVALID_ARG and gnb(dw=Q) == L.EQL_ERR_INVALID_ARG
     assert gnb(db=Q + 16384) == L.EQL_ERR_INVALID_ARG and gnb(stats=None) == L.EQL_ERR_INVALID_ARG
     ws = L.eqlinear_group_norm_act_workspace_bytes
-    assert ws(2, 9, 4, 24, 4, L.EQL_F16) > 0 and ws(0, 9, 4, 24, 4, L.EQL_F16) == 0 and ws(2, 9, 4, 24, 5, L.EQL_F16) == 0
+    assert ws(2, 1 << 16, 4, 24, 4, L.EQL_F16) > 0 and ws(0, 1 << 16, 4, 24, 4, L.EQL_F16) == 0 and ws(2, 9, 4, 24, 5, L.EQL_F16) == 0

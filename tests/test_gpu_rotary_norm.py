@@ -86,7 +86,8 @@ def test_rotary_commutes_with_the_group_and_other_stream():
 
 # B, S, C, T, groups
 NORM = [(1, 1, 8, 4, 1), (2, 3, 24, 4, 4), (1, 196, 24, 4, 6), (3, 50, 5, 3, 5), (2, 64, 64, 4, 16), (1, 7, 300, 8, 10),
-        (2, 17, 1030, 2, 103), (5, 129, 16, 1, 2), (1, 2000, 12, 2, 3), (70, 9, 8, 2, 2)]
+        (2, 17, 1030, 2, 103), (5, 129, 16, 1, 2), (1, 2000, 12, 2, 3), (70, 9, 8, 2, 2),
+        (2, 300, 24, 4, 4), (1, 1500, 16, 8, 2), (1, 5300, 24, 4, 4), (3, 700, 64, 4, 1), (1, 21000, 8, 2, 2)]
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
