@@ -475,9 +475,16 @@ __device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t 
 // fp16's range.  Scores, maxima and sums in fp32; a probability is
 // rounded once to the element type, as the operand of the second product.
 // Two forms.  RW = 4 waves of 32 rows each share the staged tiles.  Up to 32 rows (new
-// tokens over a cache): KEYS = 8 waves hold the same rows and take every eighth tile each,
-// in LDS of their own, without waiting for one another (a wave's LDS operations
+// tokens over a cache): KEYS = 4 or 8 waves hold the same rows and take every KEYS-th tile
+// each, in LDS of their own, without waiting for one another (a wave's LDS operations
 // run in order, so one buffer does), and join at the end.
+//
+// Bound: heads of 64 by the vector pipe (130 instructions a wave and tile, 32 of them
+// exponentials at a quarter rate, against 16 products of 32 cycles), wider ones by
+// both pipes; few rows by memory.  16,389 tokens, 12 heads of 64, window +-1024, fp16:
+// 160 us, 620 TFLOP/s (vector pipe 49% busy, products 30%, no LDS conflict, 2.1 waves a
+// SIMD on average: the last of 6 workgroups a CU run alone).  One token over 16
+// caches of up to 65,536 keys, 4 heads of 128, bf16: 240 us with the join, 5.5 TB/s.
 template <int DT, int DP, int RW, int KEYS>
 __global__ __launch_bounds__(RW * KEYS * 64, KEYS > 1 ? 2 : DT == kF32 ? 1 : DP > 64 ? 2 : 3) void eql_wattn_fwd_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
@@ -741,7 +748,13 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
 // delta = do . o, which it writes for the kernel that follows.  fp16: ds is rounded
 // at a power of two of its row that takes the row's largest |do| to about one, so that
 // small gradients keep their bits (a row of 1e-5 would lie below fp16's normal
-// range); the largest |do| of every wave's rows is written too.
+// range); the largest |do| of every wave's rows is written too.  delta is taken
+// from the rounded o: an error of u |do| |o| in a difference of numbers sqrt(keys)
+// larger, seen only where a row sees a handful of keys (dq 1.5 - 1.8 times as far
+// from the exact one as a result rounded once, else 1.4 by the rounded ds).
+//
+// Three products where the forward has two, and bound like it.  2 ragged clips of up to
+// 8,197 tokens, 16 heads of 128 on 4, window 2047, bf16: 310 - 340 us.
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
@@ -895,11 +908,17 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 
 // ---- key and value gradient ------------------------------------------------
 // dv_j = sum_r p_rj do_r, dk_j = scale sum_r ds_rj q_r over the packed rows r, a
-// contiguous run for each key.  fp16: p is rounded times 2^10 (the probabilities of a
-// row of 100,000 keys would lie below its normal range) and ds times the power of two
-// that takes the largest |do| of the head pair to about one.  A wave owns 32 keys; key tiles that hold first
-// tokens (seen by every later row) and tiles of long runs are split into parts
-// along the rows, whose fp32 sums a second kernel adds in order.
+// contiguous run for each key.  A wave owns 32 keys; key tiles that hold first tokens
+// (seen by every later row) and tiles of long runs are split into parts along the rows,
+// whose fp32 sums a second kernel adds in order.  fp16: p is rounded times 2^10 (the
+// probabilities of a row of 100,000 keys would lie below its normal range) and ds times
+// the power of two that takes the largest |do| of the head pair to about one.
+//
+// Bound: heads of 128 by waiting (1.3 waves a SIMD; products 25% busy, LDS 30%): a key
+// tile streams the rows that see it, 4.4 MB for a window of 2047 over 4 heads, and 58%
+// of that comes from the L2.  The clips above: 600 us (dk and dv in workgroups of their
+// own, which stream twice as much: 1145).  64 x 197 tokens, 12 heads of 64, fp16: 50 us.
+
 // Wave groups of a workgroup, each taking its share of every tile's rows for the same
 // keys.  Heads of more than 96 16-bit elements take two: their accumulators leave no
 // room for a second workgroup on a CU, and one wave a SIMD waits for each of its reads.

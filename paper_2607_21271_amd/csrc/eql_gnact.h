@@ -13,6 +13,12 @@
 // however far the mean lies from zero), then the map, whose workgroups add the
 // chunks' sums in order.  Backward: channel sums of dz and dz xhat per chunk, one
 // small kernel that adds the chunks, then dx together with dw and db.
+//
+// Bound: memory, and with gelu in 16 bits the vector pipe as much (about 30 operations
+// an element, twice in the backward).  Held groups, 128 x 3136 x 96 fp16, silu: 42 us, 3.7 TB/s (two
+// workgroups of 1,024 threads a CU load, compute and store at the same time as one
+// another; in two passes over memory 45 us); 32 x 784 x 256 bf16, gelu: forward 15 us, backward 27 + 4
+// (in passes 22 and 33).
 #pragma once
 #include "eql_common.h"
 #include "eql_config.h"
