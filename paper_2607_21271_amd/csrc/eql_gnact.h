@@ -8,10 +8,11 @@
 // backward) take one kernel that reads everything once; the others two passes.
 // Every pass gives a thread VEC fixed columns of the K and lets it walk the
 // positions of its workgroup's chunk, so weights and statistics are registers
-// and column sums need no exchange until the end.  Forward: sums of x - x0 and its
-// square per chunk and group (x0 the group's first element: no cancellation
-// however far the mean lies from zero), then the map, whose workgroups add the
-// chunks' sums in order.  Backward: channel sums of dz and dz xhat per chunk, one
+// and column sums need no exchange until the end.  Forward: mean and squared deviations
+// per chunk and group, then the map, whose workgroups join the chunks' in order.  Every
+// sum of squares is taken about a value of its own few elements (a column's first, then a
+// mean) and moved to the mean of what it joins: one value far from all others, the first
+// of a padded image say, costs no more than its own column's last bits.  Backward: channel sums of dz and dz xhat per chunk, one
 // small kernel that adds the chunks, then dx together with dw and db.
 //
 // Bound: memory, and with gelu in 16 bits the vector pipe as much (about 30 operations
@@ -32,7 +33,7 @@ struct GnArgs {
   const void *x, *w, *b, *dy;
   void *y, *dx, *dw, *db;
   float* stats;   // [B, G, 2] mean, rstd
-  float* part;    // forward [B, P, G, 2]; backward [B, chunks, C, 2]
+  float* part;    // forward [B, P, G, 2] mean, squared deviations; backward [B, chunks, C, 2]
   float* sums;    // backward [B, C, 2]: sums of dz xhat and dz
   int64_t B, S;
   int C, T, G, K, act;
@@ -44,8 +45,10 @@ struct GnArgs {
 };
 
 // The normal distribution's cdf and exp(-z^2 / 2) at z.  16-bit types: erf by
-// Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7, below half a unit of any 16-bit
-// result; its exponential is the density's.  Full precision takes the library function.
+// Abramowitz and Stegun 7.1.26, |error| <= 1.5e-7; its exponential is the density's.
+// z cdf is then at most 2.1e-7 off: below a quarter of a unit of a 16-bit result from 2e-3
+// on, in the tail of negative z up to one unit of fp16 and four of bf16.  Full precision
+// takes the library function.
 template <int DT>
 __device__ __forceinline__ void gn_normal(float z, float& cdf, float& e) {
   if constexpr (DT == kF32) {
@@ -163,11 +166,16 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
   const GnPlace p = gn_place<VEC>(a, blockIdx.x);
   const int gw = a.K / a.G;
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
+  // a column of the thread: its sums of x - x0 and the square, x0 its first element
+  const int have = (int)(p.last - (int64_t)p.chunk * a.rows);  // rows of the chunk
+  auto rows_of = [&](int rr) { return rr < have ? (have - rr + p.step - 1) / p.step : 0; };
   float s1[VEC], s2[VEC], x0[VEC];
 #pragma unroll
   for (int k = 0; k < VEC; ++k) s1[k] = s2[k] = x0[k] = 0.0f;
-  if (p.on) {
-    gn_columns<VEC>(a, p, [&](int k, int, int g) { x0[k] = (float)xb[g * gw]; });
+  if (p.on && p.first < p.last) {
+    const V v0 = *(const V*)(xb + p.first * a.K + p.col0);
+#pragma unroll
+    for (int k = 0; k < VEC; ++k) x0[k] = (float)v0.e[k];
 #pragma unroll 4
     for (int64_t r = p.first; r < p.last; r += p.step) {
       const V v = *(const V*)(xb + r * a.K + p.col0);
@@ -180,10 +188,12 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
     }
   }
   if (p.on) {
+    const float inv = p.first < p.last ? 1.0f / (float)rows_of(p.rr) : 0.0f;
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
-      red[0][p.rr * p.cols + p.cv * VEC + k] = s1[k];
-      red[1][p.rr * p.cols + p.cv * VEC + k] = s2[k];
+      const float d = s1[k] * inv;
+      red[0][p.rr * p.cols + p.cv * VEC + k] = x0[k] + d;
+      red[1][p.rr * p.cols + p.cv * VEC + k] = __builtin_fmaf(-d, s1[k], s2[k]);
     }
   }
   __syncthreads();
@@ -193,16 +203,21 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
     const int lo = max(g * gw, c0) - c0, hi = min((g + 1) * gw, c0 + p.cols) - c0;
     float t1 = 0.0f, t2 = 0.0f;
     const int w = hi - lo;
+    const float ref = w > 0 ? red[0][lo] : 0.0f;
     for (int i = lane; i < w * p.step; i += 64) {
-      const int at = i / w * p.cols + lo + i % w;
-      t1 += red[0][at];
-      t2 += red[1][at];
+      const int rr = i / w, at = rr * p.cols + lo + i % w;
+      const float d = red[0][at] - ref, n = (float)rows_of(rr);
+      if (n > 0.0f) {
+        t1 = __builtin_fmaf(n, d, t1);
+        t2 += __builtin_fmaf(n * d, d, red[1][at]);
+      }
     }
     t1 = wave_sum(t1);
     t2 = wave_sum(t2);
     if (lane == 0) {
-      out[2 * g] = t1;
-      out[2 * g + 1] = t2;
+      const float d = w > 0 ? t1 / ((float)have * (float)w) : 0.0f;
+      out[2 * g] = ref + d;
+      out[2 * g + 1] = __builtin_fmaf(-d, t1, t2);
     }
   }
 }
@@ -217,21 +232,26 @@ __global__ __launch_bounds__(256) void eql_gn_map_kernel(GnArgs a) {
   const int gw = a.K / a.G, parts = a.chunks * a.cblocks;
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
   {
-    // the parts' sums: `lanes` threads a group each add every lanes-th part, then the threads of
-    // a group in order
+    // the parts' sums about the group's first part: `lanes` threads a group each add every
+    // lanes-th part, then the threads of a group in order
     const float inv = 1.0f / ((float)a.S * (float)gw);
     const float2* const part = (const float2*)a.part + p.b * parts * a.G;
     __shared__ float2 add[256];
-    const int gs = min(a.G, 256), lanes = 256 / gs;
+    const int gs = min(a.G, 256), lanes = 256 / gs, bw = a.width * VEC;
     for (int g0 = 0; g0 < a.G; g0 += gs) {
       const int g = g0 + (int)threadIdx.x % gs, l = threadIdx.x / gs;
-      float t1 = 0.0f, t2 = 0.0f;
+      float t1 = 0.0f, t2 = 0.0f, ref = 0.0f;
       if (g < a.G && l < lanes) {
+        ref = part[g * gw / bw * a.G + g].x;
 #pragma unroll 4
         for (int i = l; i < parts; i += lanes) {
           const float2 v = part[i * a.G + g];
-          t1 += v.x;
-          t2 += v.y;
+          const int chunk = (unsigned)i / (unsigned)a.cblocks, c0 = (i - chunk * a.cblocks) * bw;
+          const int w = min((g + 1) * gw, c0 + bw) - max(g * gw, c0);  // columns of the group in the part
+          const float n = w > 0 ? (float)w * (float)(min((int64_t)(chunk + 1) * a.rows, a.S) - (int64_t)chunk * a.rows) : 0.0f;
+          const float d = w > 0 ? v.x - ref : 0.0f;
+          t1 = __builtin_fmaf(n, d, t1);
+          t2 += __builtin_fmaf(n * d, d, v.y);
         }
         add[threadIdx.x] = make_float2(t1, t2);
       }
@@ -263,7 +283,7 @@ __global__ __launch_bounds__(256) void eql_gn_map_kernel(GnArgs a) {
         t1 *= inv;
         t2 *= inv;
         const float var = __builtin_fmaf(-t1, t1, t2);
-        const float mean = (float)xb[g * gw] + t1, rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);
+        const float mean = ref + t1, rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);
         st[g] = make_float2(mean, rstd);
         if (a.stats && p.chunk == 0 && p.cb == 0) {
           a.stats[(p.b * a.G + g) * 2] = mean;
