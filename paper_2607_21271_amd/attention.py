@@ -90,7 +90,7 @@ def _check_spans(B, dev_of, lengths, starts):
 
 
 def _check_window(left, right, sinks):
-    if left < -1 or right < -1 or sinks < 0:
+    if left < -1 or right < -1 or sinks < 0 or max(left, right, sinks) >= 1 << 63:
         raise ValueError("left and right are -1 (no limit) or at least 0, sinks at least 0; got %d, %d, %d"
                          % (left, right, sinks))
 
@@ -100,7 +100,7 @@ def _check_shapes(q, k, v, left, right, sinks):
     if len(q) != 4 or len(k) != 4 or v != k:
         raise ValueError("q must be [B, Lq, heads, D] and k, v [B, Lk, kv_heads, D], got %s, %s, %s"
                          % (tuple(q), tuple(k), tuple(v)))
-    if q[0] != k[0] or q[3] != k[3] or k[2] < 1 or q[2] % k[2]:
+    if q[0] != k[0] or q[3] != k[3] or q[3] < 1 or k[2] < 1 or q[2] % k[2]:
         raise ValueError("q %s and k %s differ in sequences or head size, or the heads do not divide" % (tuple(q), tuple(k)))
     _check_window(left, right, sinks)
 
@@ -196,7 +196,7 @@ def packed_window_attention(qkv: torch.Tensor, kv_heads: int, positions: torch.T
     place (tokens from lengths[b] on are padding)."""
     left, right, sinks = int(left), int(right), int(sinks)
     ops._dtype_code(qkv)
-    if qkv.dim() != 4 or kv_heads < 1 or qkv.shape[2] <= 2 * kv_heads or (qkv.shape[2] - 2 * kv_heads) % kv_heads:
+    if qkv.dim() != 4 or kv_heads < 1 or qkv.shape[3] < 1 or qkv.shape[2] <= 2 * kv_heads or (qkv.shape[2] - 2 * kv_heads) % kv_heads:
         raise ValueError("qkv must be [B, L, heads + 2 * kv_heads, D] with heads a multiple of kv_heads = %d, got %s"
                          % (kv_heads, tuple(qkv.shape)))
     _check_window(left, right, sinks)

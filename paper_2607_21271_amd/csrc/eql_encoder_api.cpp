@@ -38,6 +38,24 @@ int64_t span(int64_t n0, int64_t n1, int64_t n2, int64_t inner, const int64_t* s
   return s > kMaxElems ? -1 : s * (int64_t)e;
 }
 
+// Whether no two elements of [n0, n1, n2, inner] share a place: every stride at least what
+// the smaller ones span.  An output that is written twice would depend on the order.
+bool distinct(int64_t n0, int64_t n1, int64_t n2, int64_t inner, const int64_t* st) {
+  const int64_t n[3] = {n0, n1, n2};
+  bool done[3] = {n0 <= 1, n1 <= 1, n2 <= 1};
+  int64_t extent = inner;
+  for (int i = 0; i < 3; ++i) {
+    int at = -1;
+    for (int k = 0; k < 3; ++k)
+      if (!done[k] && (at < 0 || st[k] < st[at])) at = k;
+    if (at < 0) break;
+    if (st[at] < extent) return false;
+    extent += (n[at] - 1) * st[at];
+    done[at] = true;
+  }
+  return true;
+}
+
 }  // namespace
 
 namespace eqk {
@@ -165,6 +183,8 @@ int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
     const int64_t b = span(s->B, L, t[i].query ? s->heads : s->kv_heads, s->head_dim, t[i].st, e);
     if (b < 0) return EQL_ERR_INVALID_ARG;
     if (b > 0 && !t[i].p) return EQL_ERR_INVALID_ARG;
+    if (b > 0 && t[i].written && !distinct(s->B, L, t[i].query ? s->heads : s->kv_heads, s->head_dim, t[i].st))
+      return EQL_ERR_INVALID_ARG;
     for (int k = 0; k < 3; ++k)
       if (t[i].st[k] % ce != 0) return EQL_ERR_ALIGNMENT;
     // a tile's rows are addressed by 31 bits from its first: 64 tokens and the heads
@@ -216,6 +236,7 @@ int eqlinear_rotary(const eqlinear_rotary_shape* s, const void* x, const void* p
   const int64_t pst[3] = {s->pos_stride[0], s->pos_stride[1], 0};
   const int64_t pb = span(s->B, s->L, 1, s->axes, pst, 4);
   if (xb < 0 || yb < 0 || pb < 0 || !freqs || (xb > 0 && (!x || !y || !positions))) return EQL_ERR_INVALID_ARG;
+  if (yb > 0 && !distinct(s->B, s->L, s->heads, D, s->y_stride)) return EQL_ERR_INVALID_ARG;
   if (!aligned(x, e) || !aligned(y, e) || !aligned(positions, 4) || !aligned(freqs, 4)) return EQL_ERR_ALIGNMENT;
   bool in_place = x == y;
   for (int i = 0; i < 3; ++i) in_place = in_place && s->x_stride[i] == s->y_stride[i];

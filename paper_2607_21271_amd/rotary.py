@@ -124,7 +124,8 @@ def rotary_axes(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, s
 
 def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, sections, T: int = 1,
                  interleaved: bool = False, inverse: bool = False) -> torch.Tensor:
-    """``rotary_axes`` in place, on x or on a view of it; not recorded by autograd, so x must not need a gradient."""
+    """``rotary_axes`` in place, on x or on a view of it whose elements lie apart (no expanded tensor); not recorded by
+    autograd, so x must not need a gradient, but a graph that saved x is told of the change."""
     sections = tuple(int(s) for s in sections)
     _check(x, positions, freqs, sections, T)
     if x.requires_grad and torch.is_grad_enabled():
@@ -133,4 +134,7 @@ def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, 
         raise ValueError("the elements of a head must be contiguous to turn in place")
     if positions.stride(-1) != 1:
         positions = positions.contiguous()
-    return _launch(x, positions, freqs.contiguous(), sections, T, interleaved, inverse, x)
+    _launch(x, positions, freqs.contiguous(), sections, T, interleaved, inverse, x)
+    if not x.is_inference():
+        torch.autograd.graph.increment_version(x)
+    return x
