@@ -168,7 +168,8 @@ __global__ __launch_bounds__(256) void eql_gn_sums_kernel(GnArgs a) {
   const E* const xb = (const E*)a.x + p.b * a.S * a.K;
   // a column of the thread: its sums of x - x0 and the square, x0 its first element
   const int have = (int)(p.last - (int64_t)p.chunk * a.rows);  // rows of the chunk
-  auto rows_of = [&](int rr) { return rr < have ? (have - rr + p.step - 1) / p.step : 0; };
+  const int each = have / p.step, more = have - each * p.step;
+  auto rows_of = [&](int rr) { return each + (rr < more ? 1 : 0); };
   float s1[VEC], s2[VEC], x0[VEC];
 #pragma unroll
   for (int k = 0; k < VEC; ++k) s1[k] = s2[k] = x0[k] = 0.0f;
@@ -243,12 +244,17 @@ __global__ __launch_bounds__(256) void eql_gn_map_kernel(GnArgs a) {
       float t1 = 0.0f, t2 = 0.0f, ref = 0.0f;
       if (g < a.G && l < lanes) {
         ref = part[g * gw / bw * a.G + g].x;
+        // part i is block cb of its chunk; the parts of the last chunk, from `short_from` on, hold fewer rows
+        int cb = l % a.cblocks;
+        const int turn = lanes % a.cblocks, short_from = parts - a.cblocks;
+        const float full = (float)a.rows, rest = (float)(int)(a.S - (int64_t)(a.chunks - 1) * a.rows);
 #pragma unroll 4
         for (int i = l; i < parts; i += lanes) {
           const float2 v = part[i * a.G + g];
-          const int chunk = (unsigned)i / (unsigned)a.cblocks, c0 = (i - chunk * a.cblocks) * bw;
-          const int w = min((g + 1) * gw, c0 + bw) - max(g * gw, c0);  // columns of the group in the part
-          const float n = w > 0 ? (float)w * (float)(min((int64_t)(chunk + 1) * a.rows, a.S) - (int64_t)chunk * a.rows) : 0.0f;
+          const int c0 = cb * bw, w = min((g + 1) * gw, c0 + bw) - max(g * gw, c0);  // columns of the group in the part
+          const float n = w > 0 ? (float)w * (i < short_from ? full : rest) : 0.0f;
+          cb += turn;
+          cb -= cb >= a.cblocks ? a.cblocks : 0;
           const float d = w > 0 ? v.x - ref : 0.0f;
           t1 = __builtin_fmaf(n, d, t1);
           t2 += __builtin_fmaf(n * d, d, v.y);
