@@ -482,7 +482,7 @@ __device__ __forceinline__ Item attn_item(uint32_t i, uint32_t blocks, uint32_t 
 // Bound: heads of 64 by the vector pipe (130 instructions a wave and tile, 32 of them
 // exponentials at a quarter rate, against 16 products of 32 cycles), wider ones by
 // both pipes; few rows by memory.  16,389 tokens, 12 heads of 64, window +-1024, fp16:
-// 160 us, 620 TFLOP/s (vector pipe 49% busy, products 30%, no LDS conflict, 2.1 waves a
+// 157 us, 640 TFLOP/s (vector pipe 49% busy, products 30%, no LDS conflict, 2.1 waves a
 // SIMD on average: the last of 6 workgroups a CU run alone).  One token over 16
 // caches of up to 65,536 keys, 4 heads of 128, bf16: 240 us with the join, 5.5 TB/s.
 template <int DT, int DP, int RW, int KEYS>
@@ -754,7 +754,7 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
 // from the exact one as a result rounded once, else 1.4 by the rounded ds).
 //
 // Three products where the forward has two, and bound like it.  2 ragged clips of up to
-// 8,197 tokens, 16 heads of 128 on 4, window 2047, bf16: 310 - 340 us.
+// 8,197 tokens, 16 heads of 128 on 4, window 2047, bf16: 295 - 340 us.
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
@@ -916,7 +916,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 //
 // Bound: heads of 128 by waiting (1.3 waves a SIMD; products 25% busy, LDS 30%): a key
 // tile streams the rows that see it, 4.4 MB for a window of 2047 over 4 heads, and 58%
-// of that comes from the L2.  The clips above: 600 us (dk and dv in workgroups of their
+// of that comes from the L2.  The clips above: 560 - 600 us (dk and dv in workgroups of their
 // own, which stream twice as much: 1145).  64 x 197 tokens, 12 heads of 64, fp16: 50 us.
 
 // Wave groups of a workgroup, each taking its share of every tile's rows for the same

@@ -19,7 +19,7 @@
 // an element, twice in the backward).  Held groups, 128 x 3136 x 96 fp16, silu: 42 us, 3.7 TB/s (two
 // workgroups of 1,024 threads a CU load, compute and store at the same time as one
 // another; in two passes over memory 45 us); 32 x 784 x 256 bf16, gelu: forward 15 us, backward 27 + 4
-// (in passes 22 and 33).
+// (in passes 22 and 33).  In passes, silu in fp16: 8 x 50,176 x 24 x 4 46 us, 3.4 TB/s with the host.
 #pragma once
 #include "eql_common.h"
 #include "eql_config.h"
