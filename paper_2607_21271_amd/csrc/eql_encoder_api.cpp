@@ -107,7 +107,7 @@ size_t attn_dkv_plan(AttnArgs& a, int dt, int cus) {
   // the others are split only to fill the device, the first ones down to the others' length
   const int64_t blocks = (int64_t)a.B * a.Hkv * kt;
   int64_t parts = 1;
-  if (blocks * 2 <= cus) {
+  if (blocks > 0 && blocks * 2 <= cus) {  // (no keys: no blocks)
     parts = cus / blocks;
     if (parts > run / 4) parts = run / 4;
     if (parts > 32) parts = 32;
