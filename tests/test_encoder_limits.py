@@ -20,3 +20,18 @@ def test_workspace_without_keys_or_queries(dt):
     assert rows <= need(window(2, 3, 0, 4, 2, 64, dt=dt)) <= 4096
     assert need(window(2, 0, 0, 4, 2, 64, dt=dt)) == need(window(2, 0, 5, 4, 2, 64, dt=dt)) == 0
     assert L.eqlinear_window_attention_workspace_bytes(window(2, 3, 0, 4, 2, 64, dt=dt)) == 0
+
+
+@pytest.mark.parametrize("B,L_,H,D,left,sinks", [
+    (4, 8192, 8, 128, 63, 4096), (8, 65536, 8, 128, 63, 1024), (8, 65536, 8, 128, 63, 16384), (1, 1 << 20, 8, 64, 100, 1 << 19),
+    (64, 2048, 12, 64, 31, 4), (1, 600, 1, 80, 15, 3), (3, 5000, 5, 96, 0, 700)])
+def test_parts_of_the_key_gradient_are_bounded(B, L_, H, D, left, sinks):
+    """Parts exist to fill 256 CUs: eight a CU of first tokens and one of other keys, each two fp32 tiles of 128 keys, are
+    enough for any shape.  (Beside them two fp32 values a row at most.)"""
+    got = L.eqlinear_window_attention_backward_workspace_bytes(window(B, L_, L_, H, H, D, left, 0, sinks))
+    assert 0 < got <= 9 * 256 * 2 * 128 * D * 4 + 8 * B * H * (L_ + 128) + 1024
+
+
+def test_first_tokens_of_few_sequences_are_split():
+    need = L.eqlinear_window_attention_backward_workspace_bytes
+    assert need(window(1, 8192, 8192, 2, 2, 64, 100, 0, 4)) > need(window(1, 8192, 8192, 2, 2, 64, 100, 0, 0))
