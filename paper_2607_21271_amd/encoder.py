@@ -32,8 +32,12 @@ class EQWindowBlock(EQViTBlock):
         self.register_buffer("freqs", rotary.axis_frequencies(self.sections, device=device), persistent=False)
 
     def _apply(self, fn, recurse=True):
+        # the frequencies follow the weights to another device, not to another type: rounded to 16 bits they would turn a
+        # token at position 2,048 wrong by tenths of a radian (fp16) or by radians (bf16)
+        freqs = self.freqs
         super()._apply(fn, recurse)
-        self.freqs = self.freqs.float()  # whatever type the weights are cast to
+        device = self.freqs.device
+        self.freqs = rotary.axis_frequencies(self.sections, device=device) if freqs.is_meta else freqs.to(device)
         return self
 
     def heads_of(self, h):
