@@ -743,12 +743,36 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
   if (a.lse && lane == 0) a.lse[row] = l == 0.0f ? __builtin_inff() : mu + __builtin_amdgcn_logf(l);
 }
 
+// fp16: score gradients are rounded as the operand of a product times a power of two of
+// their owner (a query's row, a key's column), so that neither large values overflow fp16's
+// range nor small gradients fall below it.  The power starts where a product of fp16's two smallest
+// numbers counts, and comes down as a running maximum goes up: where a tile holds an entry
+// of more than 2^15, the owner's largest is taken to about 2^kRaised, and what was summed with it.
+// An entry 2^17 times smaller than its owner's largest keeps all its bits.  Infinities stay.
+// The maximum costs up to 3% of a gradient (16,389 tokens, 12 heads of 64, window +-1024: 490 -> 504 us).
+constexpr float kRaiseStart = 0x1p60f, kRaiseLimit = 0x1p15f;
+constexpr int kRaised = 4;
+template <int DP>
+__device__ __forceinline__ void lower_raise(floatx16& t, floatx16 (&acc)[DP / 32], float& up) {
+  float mx = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) mx = fmaxf(mx, __builtin_fabsf(t[e]));
+  if (!__any(mx > kRaiseLimit)) return;
+  mx = half_max(mx);
+  const int low = mx > kRaiseLimit && mx < __builtin_inff() ? __builtin_amdgcn_frexp_expf(mx) - kRaised : 0;
+  const float f = __builtin_ldexpf(1.0f, -low);
+  up *= f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) t[e] *= f;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[d][e] *= f;
+}
+
 // ---- query gradient --------------------------------------------------------
 // dq = scale sum_j ds_j k_j, ds_j = p_j (do . v_j - delta), p_j = exp2(c s_j - lse),
-// delta = do . o, which it writes for the kernel that follows.  fp16: ds is rounded
-// at a power of two of its row that takes the row's largest |do| to about one, so that
-// small gradients keep their bits (a row of 1e-5 would lie below fp16's normal
-// range); the largest |do| of every wave's rows is written too.  delta is taken
+// delta = do . o, which it writes for the kernel that follows.  delta is taken
 // from the rounded o: an error of u |do| |o| in a difference of numbers sqrt(keys)
 // larger, seen only where a row sees a handful of keys (dq 1.5 - 1.8 times as far
 // from the exact one as a result rounded once, else 1.4 by the rounded ds).
@@ -787,7 +811,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
   const int64_t row = (int64_t)bh * a.R + r;
   const float lse = row_ok ? a.lse[row] : __builtin_inff();
-  float delta = 0.0f, top = 0.0f;
+  float delta = 0.0f;
   if (row_ok) {
     // each half of the wave takes every second chunk of the row
     const char *const po = at(a.o, a.os), *const pg = at(a.go, a.gos);
@@ -799,23 +823,11 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
       raw_to_floats<DT, 4>(wo, x);
       raw_to_floats<DT, 4>(wg, y);
 #pragma unroll
-      for (int j = 0; j < RT::CE; ++j) {
-        delta = __builtin_fmaf(x[j], y[j], delta);
-        if constexpr (DT == kF16) top = fmaxf(top, __builtin_fabsf(y[j]) < 65536.0f ? __builtin_fabsf(y[j]) : 0.0f);  // of the finite
-      }
+      for (int j = 0; j < RT::CE; ++j) delta = __builtin_fmaf(x[j], y[j], delta);
     }
   }
   delta = half_sum(delta);
   if (half == 0 && r < a.R) a.delta[row] = delta;
-  int raise = 0;  // ds is rounded times 2^raise, do . v - delta formed so
-  if constexpr (DT == kF16) {
-    top = half_max(top);
-    raise = -__builtin_amdgcn_frexp_expf(top);
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) a.top[((int64_t)bh * ((a.R + 32 * NW - 1) / (32 * NW)) + rt) * NW + wave] = top;
-  }
-  const float up = __builtin_ldexpf(1.0f, raise), delta_up = delta * up;
   Frag8<DT> qf[DP / 16], gf[DP / 16];
   load_owner<DT, DP>(qf, at(a.q, a.qs), row_ok, a.D, half);
   load_owner<DT, DP>(gf, at(a.go, a.gos), row_ok, a.D, half);
@@ -830,12 +842,14 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     sv_.load(row_rsrc<TK>(vb, vst, k0, len, a.D * RT::EB));
   };
   floatx16 acc[DP / 32];
+  float up;  // the power of two that ds is formed times
   const float c = a.scale_log2e;
   const LdsMap<DT, DP> map(lane);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
+    up = DT == kF16 ? kRaiseStart : 1.0f;
     if (kg.n > 0) load(0);
     auto step = [&](int i, auto which) {
       constexpr int buf = decltype(which)::value;
@@ -871,12 +885,16 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
           mma32<DT>(g, map.row(vt, n, t), gf[t]);
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse)) * __builtin_fmaf(g[e], up, -delta_up);
+        for (int e = 0; e < 16; ++e) {
+          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse));
+          s[e] = p * (DT == kF16 ? __builtin_fmaf(g[e], up, -delta * up) : g[e] - delta);
+        }
         if (!whole) {
           const uint32_t bits = seen_bits(k0 + 32 * n) >> (4 * half);
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e] = bits_f32(f32_bits(s[e]) & entry_mask(bits, e));
         }
+        if constexpr (DT == kF16) lower_raise<DP>(s, acc, up);
         if constexpr (kCareful) {
 #pragma unroll
           for (int t = 0; t < 2; ++t)
@@ -903,7 +921,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     __syncthreads();
     walk(std::true_type{});
   }
-  store_owner<DT, DP>(acc, DT == kF16 ? __builtin_ldexpf(a.scale, -raise) : a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
+  store_owner<DT, DP>(acc, DT == kF16 ? a.scale / up : a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
 }
 
 // ---- key and value gradient ------------------------------------------------
@@ -911,8 +929,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 // contiguous run for each key.  A wave owns 32 keys; key tiles that hold first tokens
 // (seen by every later row) and tiles of long runs are split into parts along the rows,
 // whose fp32 sums a second kernel adds in order.  fp16: p is rounded times 2^10 (the
-// probabilities of a row of 100,000 keys would lie below its normal range) and ds times
-// the power of two that takes the largest |do| of the head pair to about one.
+// probabilities of a row of 100,000 keys would lie below its normal range).
 //
 // Bound: heads of 128 by waiting (1.3 waves a SIMD; products 25% busy, LDS 30%): a key
 // tile streams the rows that see it, 4.4 MB for a window of 2047 over 4 heads, and 58%
@@ -1022,22 +1039,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
   const bool even = TQ % a.G == 0;
   place(0);
   const float inv_c = 1.0f / a.scale_log2e;
-  int raise = 0;
-  if constexpr (DT == kF16) {
-    const int n = (a.R + 127) / 128 * 4;
-    float top = 0.0f;
-    for (int i = tid; i < n; i += NT) top = fmaxf(top, a.top[(int64_t)bh * n + i]);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) stats[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, stats[w]);
-    raise = -__builtin_amdgcn_frexp_expf(top);
-    __syncthreads();
-  }
   constexpr float kRaiseP = DT == kF16 ? 10.0f : 0.0f;
-  const float raise_ds = __builtin_ldexpf(1.0f, raise - (int)kRaiseP);
   // The tiles in a rotated order: workgroups whose runs overlap come to a tile at about
   // the same time, tile numbers equal modulo the length of a run, and find it in their
   // XCD's L2.  From the run's start on, 64 runs of one head pair side by side touch
@@ -1061,9 +1063,9 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
     }
   };
   floatx16 dk[DP / 32], dv[DP / 32];
+  float up;  // the power of two that ds is formed times, over that of p
   const float c = a.scale_log2e;
   // the products start from -lse / c and -delta of their rows: p = exp2(c s), ds = p g
-  const float mul_k = DT == kF16 ? __builtin_ldexpf(a.scale, -raise) : a.scale, mul_v = DT == kF16 ? 0x1p-10f : 1.0f;
   LdsMap<DT, DP> map(lane, g32);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
@@ -1072,6 +1074,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
       dk[d] = floatx16{};
       dv[d] = floatx16{};
     }
+    up = DT == kF16 ? kRaiseStart * 0x1p-10f : 1.0f;
     if (i0 < i1) load(i0);
     auto step = [&](int i, auto which) {
       constexpr int buf = decltype(which)::value;
@@ -1129,7 +1132,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           s[e] = __builtin_amdgcn_exp2f(s[e] * c);
-          g[e] *= DT == kF16 ? s[e] * raise_ds : s[e];
+          g[e] *= DT == kF16 ? s[e] * up : s[e];
         }
         if (!whole) {
           const uint32_t bits = seen_bits(r0 + g32 + 32 * n) >> (4 * half);
@@ -1140,6 +1143,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
             g[e] = bits_f32(f32_bits(g[e]) & k);
           }
         }
+        if constexpr (DT == kF16) lower_raise<DP>(g, dk, up);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           Frag8<DT> p, ds;
@@ -1170,7 +1174,16 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
     __syncthreads();
     walk(std::true_type{});
   }
+  const float scale_k = DT == kF16 ? a.scale * 0x1p-10f / up : a.scale, mul_v = DT == kF16 ? 0x1p-10f : 1.0f;
+  constexpr bool kScaleFirst = GR == 2 && DT == kF16;  // a key's two groups have powers of their own
+  const float mul_k = kScaleFirst ? 1.0f : scale_k;
   if constexpr (GR == 2) {
+    if constexpr (kScaleFirst) {
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) dk[d][e] *= scale_k;
+    }
     // the second group's sums to the first, one gradient after the other
     float* const x = reinterpret_cast<float*>(smem) + (wave % 4 * (DP / 2)) * 64 + lane;
     auto join = [&](floatx16 (&acc)[DP / 32]) {

@@ -62,7 +62,6 @@ AttnArgs slice(const AttnArgs& a, int b0, int n) {
   if (a.starts) s.starts = a.starts + b0;
   if (a.lse) s.lse = a.lse + (int64_t)b0 * a.Hkv * a.R;
   if (a.delta) s.delta = a.delta + (int64_t)b0 * a.Hkv * a.R;
-  if (a.top) s.top = a.top + (int64_t)b0 * a.Hkv * ((a.R + 127) / 128 * 4);
   s.B = n;
   return s;
 }

@@ -29,7 +29,6 @@ struct AttnArgs {
   void *o, *dq, *dk, *dv;
   const int *lengths, *starts;  // per sequence, or null
   float *lse, *delta;           // [B, Hkv, R], log2 units
-  float* top;                   // fp16 backward: largest |do| of every 32 rows, [B, Hkv, R up to 128s]
   float* part;                  // fp32 parts of split rows or keys
   int64_t qs[3], ks[3], vs[3], os[3], gos[3], dqs[3], dks[3], dvs[3];  // elements: sequence, token, head
   int B, Lq, Lk, Hkv, G, R, D;

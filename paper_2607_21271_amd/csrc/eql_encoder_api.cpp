@@ -212,9 +212,6 @@ int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
 constexpr int kPlanCus = 256;
 
 size_t delta_bytes(const eqk::AttnArgs& a) { return align256((size_t)a.B * a.Hkv * a.R * sizeof(float)); }
-size_t top_bytes(const eqk::AttnArgs& a, int dt) {
-  return dt == EQL_F16 ? align256((size_t)a.B * a.Hkv * ((a.R + 127) / 128 * 4) * sizeof(float)) : 0;
-}
 
 }  // namespace
 
@@ -324,7 +321,7 @@ int eqlinear_window_attention(const eqlinear_window_shape* s, const void* q, con
 size_t eqlinear_window_attention_backward_workspace_bytes(const eqlinear_window_shape* s) {
   eqk::AttnArgs a;
   if (window_args(s, a) || a.B == 0) return 0;
-  return delta_bytes(a) + top_bytes(a, s->dtype) + eqk::attn_dkv_plan(a, s->dtype, kPlanCus);
+  return delta_bytes(a) + eqk::attn_dkv_plan(a, s->dtype, kPlanCus);
 }
 
 int eqlinear_window_attention_backward(const eqlinear_window_shape* s, const void* q, const void* k, const void* v,
@@ -340,7 +337,7 @@ int eqlinear_window_attention_backward(const eqlinear_window_shape* s, const voi
   if (!aligned(lengths, 4) || !aligned(starts, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return EQL_ERR_ALIGNMENT;
   if (a.B == 0 || (a.R == 0 && a.Lk == 0)) return check_device();
   if (a.R > 0 && !lse) return EQL_ERR_INVALID_ARG;
-  const size_t part = eqk::attn_dkv_plan(a, s->dtype, kPlanCus), head = delta_bytes(a) + top_bytes(a, s->dtype), need = head + part;
+  const size_t part = eqk::attn_dkv_plan(a, s->dtype, kPlanCus), head = delta_bytes(a), need = head + part;
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.q = q;
@@ -355,7 +352,6 @@ int eqlinear_window_attention_backward(const eqlinear_window_shape* s, const voi
   a.starts = starts;
   a.lse = const_cast<float*>(lse);
   a.delta = (float*)workspace;
-  a.top = (float*)((char*)workspace + delta_bytes(a));
   a.part = part ? (float*)((char*)workspace + head) : nullptr;
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::wattn_bwd<eqk::kF32>(a, st));

@@ -21,3 +21,46 @@ def test_gradient_without_keys(dt):
     k = torch.zeros(2, 0, 2, 64, dtype=R.DT[dt], device="cuda")
     got = gradients(q, k, k.clone(), do, sinks=2)
     assert (got["o"] == 0).all() and (got["dq"] == 0).all() and got["dk"].shape == got["dv"].shape == k.shape
+
+
+def f16(seed, *shape, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).half().cuda()
+
+
+def compare(q, k, v, do, **kw):
+    got, want = gradients(q, k, v, do, **kw), R.attention(q, k, v, do, **kw)
+    for n, t in got.items():
+        assert torch.isfinite(t).all(), n
+        R.within(n, t, *want[n])
+
+
+@pytest.mark.parametrize("D", [40, 64, 128])
+@pytest.mark.parametrize("L,kw", [(2, {}), (150, dict(right=0)), (333, dict(left=40, right=7, sinks=2))])
+def test_fp16_large_values(L, kw, D):
+    """Values of 4,000 and small gradients: score gradients of hundreds of thousands times the largest |do|."""
+    v = torch.sign(f16(13, 1, L, 1, D)) * 4000.0
+    if L == 2:
+        v[0, 0], v[0, 1] = 4000.0, -4000.0
+        do = torch.full((1, L, 2, D), 1e-3, dtype=torch.float16, device="cuda")
+    else:
+        do = f16(14, 1, L, 2, D, scale=1e-3)
+    compare(f16(11, 1, L, 2, D, scale=0.5), f16(12, 1, L, 1, D, scale=0.5), v, do, **kw)
+
+
+@pytest.mark.parametrize("D", [40, 64, 128])
+@pytest.mark.parametrize("row", [0, 70, 199])
+def test_fp16_one_large_gradient_beside_small_ones(row, D):
+    """A row of 30,000 among rows of 0.01: keys that it does not see keep the bits of their gradients, and so do rows."""
+    do = f16(24, 1, 200, 2, D, scale=0.01)
+    do[0, row, 1] = 30000.0 * torch.sign(do[0, row, 1])
+    compare(f16(21, 1, 200, 2, D), f16(22, 1, 200, 1, D), f16(23, 1, 200, 1, D), do, left=20, right=0)
+
+
+def test_fp16_gradients_grow_along_the_rows():
+    """Rows whose gradients grow by 2^20 from first to last, and shrink: the power of two of a key moves with them."""
+    L = 256
+    size = torch.logspace(-10, 10, L, base=2.0).cuda()[None, :, None, None]
+    for s in (size, size.flip(1)):
+        do = (f16(34, 1, L, 1, 64).float() * s).half()
+        compare(f16(31, 1, L, 1, 64), f16(32, 1, L, 1, 64), f16(33, 1, L, 1, 64), do, left=50, right=50)
