@@ -1040,6 +1040,10 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
   place(0);
   const float inv_c = 1.0f / a.scale_log2e;
   constexpr float kRaiseP = DT == kF16 ? 10.0f : 0.0f;
+  // 16 bits: the score product starts from -lse / c of its row, and p = exp2(c s).  Full precision: p =
+  // exp2(c s - lse), formed at the end; a sum that starts at 10 or 100 loses the last bits of
+  // scores of about one in each of its steps (errors of dk and dv 2 - 3 times the plain form's).
+  constexpr bool kLseFirst = DT != kF32;
   // The tiles in a rotated order: workgroups whose runs overlap come to a tile at about
   // the same time, tile numbers equal modulo the length of a run, and find it in their
   // XCD's L2.  From the run's start on, 64 runs of one head pair side by side touch
@@ -1058,14 +1062,14 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
     if (tid < TQ) {
       const bool ok = r0 + tid < rend;
       const int64_t at = (int64_t)bh * a.R + (ok ? r0 + tid : rend - 1);
-      st_lse = ok ? (kRaiseP - a.lse[at]) * inv_c : -__builtin_inff();
+      st_lse = ok ? (kRaiseP - a.lse[at]) * (kLseFirst ? inv_c : 1.0f) : -__builtin_inff();
       st_delta = ok ? -a.delta[at] : 0.0f;
     }
   };
   floatx16 dk[DP / 32], dv[DP / 32];
   float up;  // the power of two that ds is formed times, over that of p
   const float c = a.scale_log2e;
-  // the products start from -lse / c and -delta of their rows: p = exp2(c s), ds = p g
+  // (the gradients' products start from -delta of their rows: ds = p g)
   LdsMap<DT, DP> map(lane, g32);
   auto walk = [&](auto careful) {
     constexpr bool kCareful = decltype(careful)::value;
@@ -1120,7 +1124,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
           const floatx4 dl = *reinterpret_cast<const floatx4*>(de + g32 + n * 32 + 8 * x + 4 * half);
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            s[4 * x + y] = le[y];
+            s[4 * x + y] = kLseFirst ? le[y] : 0.0f;
             g[4 * x + y] = dl[y];
           }
         }
@@ -1131,7 +1135,8 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          s[e] = __builtin_amdgcn_exp2f(s[e] * c);
+          if constexpr (kLseFirst) s[e] = __builtin_amdgcn_exp2f(s[e] * c);
+          else s[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, ls[g32 + n * 32 + 8 * (e >> 2) + 4 * half + (e & 3)]));
           g[e] *= DT == kF16 ? s[e] * up : s[e];
         }
         if (!whole) {

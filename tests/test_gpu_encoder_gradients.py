@@ -64,3 +64,18 @@ def test_fp16_gradients_grow_along_the_rows():
     for s in (size, size.flip(1)):
         do = (f16(34, 1, L, 1, 64).float() * s).half()
         compare(f16(31, 1, L, 1, 64), f16(32, 1, L, 1, 64), f16(33, 1, L, 1, 64), do, left=50, right=50)
+
+
+@pytest.mark.parametrize("L,H,D,kw", [(700, 2, 64, {}), (2000, 1, 128, {}), (1500, 1, 96, dict(left=900, right=900)), (509, 3, 40, dict(left=100, right=20))])
+def test_full_precision_gradients(L, H, D, kw):
+    """2-norm errors of full-precision gradients.  A probability is exp2(c s - lse): below 2^m the logarithm and the
+    difference are each rounded by 2^(m - 25) at most, so it is off by 2 ln 2 2^(m - 25) of itself; the sums of products
+    add 2^-21 (random signs: sqrt(2000) roundings of 2^-24 of terms, and of D / 2 in the scores)."""
+    g = torch.Generator().manual_seed(41)
+    q, k, v, do = (torch.randn(1, L, H, D, generator=g).cuda() for _ in range(4))
+    got, want = gradients(q, k, v, do, **kw), R.attention(q, k, v, do, **kw)
+    bits = 3 if min(L, sum(kw.values()) or L) < 200 else 4  # lse of that many keys and scores of spread one
+    bound = 2 * 0.6932 * 2.0 ** (bits - 25) + 2.0 ** -21
+    for n in ("o", "dq", "dk", "dv"):
+        err = ((got[n].double().cpu() - want[n][0]).norm() / want[n][0].norm()).item()
+        assert err <= bound, (n, err, bound)
