@@ -146,9 +146,9 @@ def window_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, left: in
     left, right, sinks = int(left), int(right), int(sinks)
     _check(q, k, v, lengths, starts, left, right, sinks)
     scale = float(q.shape[3]) ** -0.5 if scale is None else float(scale)
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad):
-        return WindowAttentionFunction.apply(q, k, v, lengths, starts, left, right, sinks, scale)
-    return _forward(_ready(q), _ready(k), _ready(v), lengths, starts, left, right, sinks, scale, False)[0]
+    if ops._no_node(q, k, v):
+        return _forward(_ready(q), _ready(k), _ready(v), lengths, starts, left, right, sinks, scale, False)[0]
+    return WindowAttentionFunction.apply(q, k, v, lengths, starts, left, right, sinks, scale)
 
 
 class PackedAttentionFunction(torch.autograd.Function):

@@ -97,9 +97,9 @@ def group_norm_act(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor, gr
     _check_shapes(x.shape, weight.shape, bias.shape, groups, activation)
     ops._check_dev(x, weight, bias)
     act = ACTIVATIONS[activation]
-    if torch.is_grad_enabled() and (x.requires_grad or weight.requires_grad or bias.requires_grad):
-        return GroupNormActFunction.apply(x, weight, bias, groups, act, float(eps))
-    return _forward(_ready(x), weight.contiguous(), bias.contiguous(), groups, act, float(eps), False)[0]
+    if ops._no_node(x, weight, bias):
+        return _forward(_ready(x), weight.contiguous(), bias.contiguous(), groups, act, float(eps), False)[0]
+    return GroupNormActFunction.apply(x, weight, bias, groups, act, float(eps))
 
 
 class GroupNormAct(torch.nn.Module):

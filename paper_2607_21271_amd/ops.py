@@ -45,6 +45,22 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _watched() -> bool:
+    """Whether torch records or transforms the operations of this thread: a trace, a forward-mode level, a functorch
+    transform.  An autograd function is part of that (or refuses it); a bare launch would leave no mark."""
+    return (torch.jit.is_tracing() or torch.autograd.forward_ad._current_level >= 0
+            or torch._C._functorch.peek_interpreter_stack() is not None)
+
+
+def _no_node(*ts) -> bool:
+    """Whether a call on these tensors needs no autograd function: no gradient is wanted and nothing looks on."""
+    if torch.is_grad_enabled():
+        for t in ts:
+            if t.requires_grad:
+                return False
+    return not _watched()
+
+
 def _stream_of(t: torch.Tensor) -> int:
     """Handle of the current stream of t's device, which has to be the current device (a launch goes there)."""
     index = t.device.index

@@ -115,7 +115,7 @@ def rotary_axes(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, s
     if positions.stride(-1) != 1:
         positions = positions.contiguous()
     freqs = freqs.contiguous()
-    if x.requires_grad and torch.is_grad_enabled():
+    if not ops._no_node(x):
         return RotaryFunction.apply(x, positions, freqs, sections, T, interleaved, inverse)
     x = _rows(x)
     return _launch(x, positions, freqs, sections, T, interleaved, inverse,
@@ -130,6 +130,9 @@ def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, 
     _check(x, positions, freqs, sections, T)
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("rotary_axes_ is not differentiable; use rotary_axes")
+    if ops._watched() and (torch.jit.is_tracing() or torch._C._functorch.peek_interpreter_stack() is not None
+                           or torch.autograd.forward_ad.unpack_dual(x).tangent is not None):
+        raise ValueError("rotary_axes_ cannot be traced or transformed; use rotary_axes")
     if x.stride(3) != 1 and x.shape[3] != 1:
         raise ValueError("the elements of a head must be contiguous to turn in place")
     if positions.stride(-1) != 1:
