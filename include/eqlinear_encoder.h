@@ -7,7 +7,9 @@
  * no synchronisation, outputs overwritten, bitwise reproducible (no atomics,
  * fixed orders of summation).  Sizes of 0 in B, L, Lq or S are no-ops.  An
  * address plus its strides must lie inside memory that the caller owns; strides
- * are counted in elements, and an output's keep its elements apart. */
+ * are counted in elements, and an output's keep its elements apart.  What is written
+ * (outputs, statistics, workspace) overlaps nothing else of the call; outputs with
+ * strides may lie between one another's elements where their strides agree. */
 #ifndef EQLINEAR_ENCODER_H
 #define EQLINEAR_ENCODER_H
 

@@ -12,6 +12,7 @@
 
 using eqk::align256;
 using eqk::aligned;
+using eqk::any_overlap;
 using eqk::check_device;
 using eqk::elem_bytes;
 using eqk::overlaps;
@@ -54,6 +55,32 @@ bool distinct(int64_t n0, int64_t n1, int64_t n2, int64_t inner, const int64_t* 
     done[at] = true;
   }
   return true;
+}
+
+// One axis of two outputs with the same stride.
+struct Axis {
+  int64_t na, nb, stride;
+};
+// Whether some element of an output (`inner` elements at every step of its axes) lies on one of
+// another, whose first element is `delta` elements behind.  Axes from the largest stride
+// on: only displacements at which what the smaller ones span could meet are looked at, two or
+// three where elements lie apart (more than 64 count as meeting).
+bool meet(const Axis* ax, int n, int64_t delta, int64_t inner) {
+  if (n == 0) return delta < inner && delta > -inner;
+  int64_t ea = inner, eb = inner;
+  for (int i = 1; i < n; ++i) {
+    ea += (ax[i].na - 1) * ax[i].stride;
+    eb += (ax[i].nb - 1) * ax[i].stride;
+  }
+  auto floor_div = [](int64_t a, int64_t b) { return a / b - (a % b < 0); };
+  const int64_t s = ax[0].stride;
+  int64_t lo = floor_div(-eb - delta, s) + 1, hi = -floor_div(delta - ea, s) - 1;  // -eb < delta + d s < ea
+  if (lo < 1 - ax[0].na) lo = 1 - ax[0].na;
+  if (hi > ax[0].nb - 1) hi = ax[0].nb - 1;
+  if (hi - lo >= 64) return true;
+  for (int64_t d = lo; d <= hi; ++d)
+    if (meet(ax + 1, n - 1, delta + d * s, inner)) return true;
+  return false;
 }
 
 }  // namespace
@@ -175,13 +202,37 @@ int window_args(const eqlinear_window_shape* s, eqk::AttnArgs& a) {
   return EQL_OK;
 }
 
-// One tensor of the attention: its span, or an error.
+// One tensor of the attention, and one buffer without strides.
 struct Operand {
   const void* p;
   const int64_t* st;
   bool query, written;
 };
-int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
+struct Buffer {
+  Range r;
+  bool written;
+};
+
+// Whether two outputs whose spans overlap share a place.  Their strides have to agree (on
+// axes where both take a step) for them to lie between one another's elements.
+bool outputs_meet(const eqlinear_window_shape* s, const Operand& x, const Operand& y) {
+  const int64_t nx[3] = {s->B, x.query ? s->Lq : s->Lk, x.query ? s->heads : s->kv_heads};
+  const int64_t ny[3] = {s->B, y.query ? s->Lq : s->Lk, y.query ? s->heads : s->kv_heads};
+  const int64_t e = (int64_t)elem_bytes(s->dtype);
+  Axis ax[3];
+  int n = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (nx[i] == 1 && ny[i] == 1) continue;
+    if (nx[i] > 1 && ny[i] > 1 && x.st[i] != y.st[i]) return true;
+    const Axis a{nx[i], ny[i], nx[i] > 1 ? x.st[i] : y.st[i]};
+    int at = n++;
+    for (; at > 0 && ax[at - 1].stride < a.stride; --at) ax[at] = ax[at - 1];
+    ax[at] = a;
+  }
+  return meet(ax, n, ((intptr_t)y.p - (intptr_t)x.p) / e, s->head_dim);
+}
+
+int window_operands(const eqlinear_window_shape* s, const Operand* t, int n, const Buffer* buf, int nbuf) {
   const size_t e = elem_bytes(s->dtype);
   const int64_t ce = (int64_t)(16 / e);
   Range r[8];
@@ -200,10 +251,17 @@ int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
     if (!aligned(t[i].p, 16)) return EQL_ERR_ALIGNMENT;
     r[i] = Range{t[i].p, (size_t)b};
   }
-  // an output overlaps no input; outputs may interleave in one buffer
-  for (int i = 0; i < n; ++i)
+  // nothing that is written overlaps anything else; strided outputs may interleave in one buffer
+  for (int i = 0; i < n; ++i) {
     for (int j = 0; j < n; ++j)
-      if (t[i].written && !t[j].written && overlaps(r[i], r[j])) return EQL_ERR_INVALID_ARG;
+      if (t[i].written && j != i && overlaps(r[i], r[j]) && (!t[j].written || (j < i && outputs_meet(s, t[i], t[j]))))
+        return EQL_ERR_INVALID_ARG;
+    for (int j = 0; j < nbuf; ++j)
+      if ((t[i].written || buf[j].written) && overlaps(r[i], buf[j].r)) return EQL_ERR_INVALID_ARG;
+  }
+  for (int i = 0; i < nbuf; ++i)
+    for (int j = 0; j < i; ++j)
+      if ((buf[i].written || buf[j].written) && overlaps(buf[i].r, buf[j].r)) return EQL_ERR_INVALID_ARG;
   return EQL_OK;
 }
 
@@ -211,7 +269,8 @@ int window_operands(const eqlinear_window_shape* s, const Operand* t, int n) {
 // query and the call agree and results do not depend on the device.
 constexpr int kPlanCus = 256;
 
-size_t delta_bytes(const eqk::AttnArgs& a) { return align256((size_t)a.B * a.Hkv * a.R * sizeof(float)); }
+size_t lse_bytes(const eqk::AttnArgs& a) { return (size_t)a.B * a.Hkv * a.R * sizeof(float); }
+size_t delta_bytes(const eqk::AttnArgs& a) { return align256(lse_bytes(a)); }
 
 }  // namespace
 
@@ -297,11 +356,14 @@ int eqlinear_window_attention(const eqlinear_window_shape* s, const void* q, con
   eqk::AttnArgs a;
   if (int st = window_args(s, a)) return st;
   const Operand t[4] = {{q, a.qs, true, false}, {k, a.ks, false, false}, {v, a.vs, false, false}, {o, a.os, true, true}};
-  if (int st = window_operands(s, t, 4)) return st;
   if (!aligned(lengths, 4) || !aligned(starts, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return EQL_ERR_ALIGNMENT;
-  if (a.B == 0 || a.R == 0) return check_device();
-  const eqk::AttnPlan p = eqk::attn_plan(a, s->dtype, kPlanCus);
-  const size_t need = eqk::attn_part_bytes(a, p);
+  const bool empty = a.B == 0 || a.R == 0;
+  const eqk::AttnPlan p = empty ? eqk::AttnPlan{} : eqk::attn_plan(a, s->dtype, kPlanCus);
+  const size_t need = empty ? 0 : eqk::attn_part_bytes(a, p);
+  const Buffer buf[4] = {{{lengths, a.B * sizeof(int32_t)}, false}, {{starts, a.B * sizeof(int32_t)}, false},
+                         {{lse, lse_bytes(a)}, true}, {{workspace, workspace_bytes < need ? workspace_bytes : need}, true}};
+  if (int st = window_operands(s, t, 4, buf, 4)) return st;
+  if (empty) return check_device();
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.q = q;
@@ -333,11 +395,14 @@ int eqlinear_window_attention_backward(const eqlinear_window_shape* s, const voi
   const Operand t[8] = {{q, a.qs, true, false},  {k, a.ks, false, false},   {v, a.vs, false, false},
                         {o, a.os, true, false},  {d_o, a.gos, true, false}, {dq, a.dqs, true, true},
                         {dk, a.dks, false, true}, {dv, a.dvs, false, true}};
-  if (int st = window_operands(s, t, 8)) return st;
   if (!aligned(lengths, 4) || !aligned(starts, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return EQL_ERR_ALIGNMENT;
-  if (a.B == 0 || (a.R == 0 && a.Lk == 0)) return check_device();
+  const bool empty = a.B == 0 || (a.R == 0 && a.Lk == 0);
+  const size_t part = empty ? 0 : eqk::attn_dkv_plan(a, s->dtype, kPlanCus), head = delta_bytes(a), need = head + part;
+  const Buffer buf[4] = {{{lengths, a.B * sizeof(int32_t)}, false}, {{starts, a.B * sizeof(int32_t)}, false},
+                         {{lse, lse_bytes(a)}, false}, {{workspace, workspace_bytes < need ? workspace_bytes : need}, true}};
+  if (int st = window_operands(s, t, 8, buf, 4)) return st;
+  if (empty) return check_device();
   if (a.R > 0 && !lse) return EQL_ERR_INVALID_ARG;
-  const size_t part = eqk::attn_dkv_plan(a, s->dtype, kPlanCus), head = delta_bytes(a), need = head + part;
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.q = q;
@@ -378,6 +443,14 @@ int gn_args(int64_t B, int64_t S, int T, int C, int groups, int dtype, eqk::GnAr
   return EQL_OK;
 }
 
+// Whether every output is apart from the inputs and the other outputs.
+bool apart(const Range* out, int n, const Range* in, int nin) {
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < nin; ++j)
+      if (overlaps(out[i], in[j])) return false;
+  return !any_overlap(out, n);
+}
+
 // Whole 16-byte vectors where every row starts on one.
 int gn_vec(const eqk::GnArgs& a, int dtype) {
   const int w = (int)(16 / elem_bytes(dtype));
@@ -407,15 +480,14 @@ int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias,
   if (!aligned(x, 16) || !aligned(y, 16) || !aligned(weight, e) || !aligned(bias, e) || !aligned(stats, 8) ||
       !aligned(workspace, 16))
     return EQL_ERR_ALIGNMENT;
-  const Range out{y, n}, in[3] = {{x, n}, {weight, C * e}, {bias, C * e}};
-  for (const Range& r : in)
-    if (overlaps(out, r)) return EQL_ERR_INVALID_ARG;
+  const size_t need = eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype);
+  const Range out[3] = {{y, n}, {stats, (size_t)B * groups * 8}, {workspace, workspace_bytes < need ? workspace_bytes : need}}, in[3] = {{x, n}, {weight, C * e}, {bias, C * e}};
+  if (!apart(out, 3, in, 3)) return EQL_ERR_INVALID_ARG;
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
   eqk::gn_plan(a, vec, kPlanCus, false);
   if ((double)B * (a.hold ? (double)groups * a.threads : (double)a.chunks * a.cblocks * 256) >= 4294967296.0)
     return EQL_ERR_UNSUPPORTED;
-  const size_t need = eqlinear_group_norm_act_workspace_bytes(B, S, T, C, groups, dtype);
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.x = x;
@@ -449,21 +521,17 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   if (!aligned(x, 16) || !aligned(dy, 16) || !aligned(dx, 16) || !aligned(weight, e) || !aligned(bias, e) ||
       !aligned(dw, e) || !aligned(db, e) || !aligned(stats, 8) || !aligned(workspace, 16))
     return EQL_ERR_ALIGNMENT;
-  const Range out[3] = {{dx, n}, {dw, C * e}, {db, C * e}}, in[4] = {{x, n}, {dy, n}, {weight, C * e}, {bias, C * e}};
-  for (int i = 0; i < 3; ++i) {
-    for (const Range& r : in)
-      if (overlaps(out[i], r)) return EQL_ERR_INVALID_ARG;
-    for (int j = 0; j < i; ++j)
-      if (overlaps(out[i], out[j])) return EQL_ERR_INVALID_ARG;
-  }
+  const size_t need = eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype);
+  const Range out[4] = {{dx, n}, {dw, C * e}, {db, C * e}, {workspace, workspace_bytes < need ? workspace_bytes : need}};
+  const Range in[5] = {{x, n}, {dy, n}, {weight, C * e}, {bias, C * e}, {stats, (size_t)B * groups * 8}};
+  if (!apart(out, 4, in, 5)) return EQL_ERR_INVALID_ARG;
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
   eqk::gn_plan(a, vec, kPlanCus, true);
   if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * (C + 64) * 4 >= 4294967296.0 ||
       (double)B * groups * 512 >= 4294967296.0)
     return EQL_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < eqlinear_group_norm_act_backward_workspace_bytes(B, S, T, C, groups, dtype))
-    return EQL_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < need) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.x = x;
   a.w = weight;

@@ -35,3 +35,103 @@ def test_parts_of_the_key_gradient_are_bounded(B, L_, H, D, left, sinks):
 def test_first_tokens_of_few_sequences_are_split():
     need = L.eqlinear_window_attention_backward_workspace_bytes
     assert need(window(1, 8192, 8192, 2, 2, 64, 100, 0, 4)) > need(window(1, 8192, 8192, 2, 2, 64, 100, 0, 0))
+
+
+# ---- buffers that lie on one another (addresses are never dereferenced) ----------------------------------------------
+
+P, S, W = 1 << 20, 1 << 36, 1 << 41
+STEP = 1 << 28
+
+
+def dense(n, heads, D, T=0):
+    return (T or n) * heads * D, heads * D, D
+
+
+def forward(B=2, L_=64, H=4, Hkv=2, D=64, o=S, lse=None, ws=None, lengths=None, starts=None, Lq=None):
+    Lq = Lq or L_
+    sh = L.WindowShape(B, Lq, L_, -1, -1, 0, H, Hkv, D, L.EQL_F16, 0.125, 0, dense(Lq, H, D), dense(L_, Hkv, D),
+                       dense(L_, Hkv, D), dense(Lq, H, D), *(NONE,) * 4)
+    need = L.eqlinear_window_attention_workspace_bytes(ctypes.byref(sh))
+    return L.eqlinear_window_attention(ctypes.byref(sh), P, P + STEP, P + 2 * STEP, lengths, starts, o, lse, ws, need, None)
+
+
+def backward(B=2, L_=64, H=4, Hkv=2, D=64, dq=S, dk=S + STEP, dv=S + 2 * STEP, st=None, lse=W, ws=W + STEP, o=P + 3 * STEP,
+             lengths=None, starts=None):
+    st = st or (dense(L_, H, D), dense(L_, Hkv, D), dense(L_, Hkv, D))
+    sh = L.WindowShape(B, L_, L_, -1, -1, 0, H, Hkv, D, L.EQL_F16, 0.125, 0, dense(L_, H, D), dense(L_, Hkv, D),
+                       dense(L_, Hkv, D), dense(L_, H, D), dense(L_, H, D), *st)
+    need = L.eqlinear_window_attention_backward_workspace_bytes(ctypes.byref(sh))
+    return L.eqlinear_window_attention_backward(ctypes.byref(sh), P, P + STEP, P + 2 * STEP, lengths, starts, o, lse,
+                                                P + 4 * STEP, dq, dk, dv, ws, need, None)
+
+
+PASSED = (L.EQL_ERR_NO_DEVICE,)  # the next thing that is looked at; where there is a GPU these are not called
+needs_no_gpu = pytest.mark.skipif(__import__("torch").cuda.device_count() > 0, reason="addresses that hold nothing")
+E2 = 2  # bytes of an element
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dk=S + STEP, dv=S + STEP), dict(dq=S, dk=S), dict(dq=S, dv=S + 128), dict(dk=S + STEP, dv=S + STEP + 16),
+    dict(ws=P + STEP), dict(ws=S), dict(ws=W), dict(lse=S + 64), dict(lengths=S + 8), dict(starts=S + STEP + 4),
+    dict(lengths=W + STEP), dict(o=W + STEP),
+    # dq and dk of one packed buffer, one head too close; with a last head on the next token's first
+    dict(st=((64 * 8 * 64, 8 * 64, 64),) * 3, dq=S, dk=S + 3 * 64 * E2, dv=S + 6 * 64 * E2),
+    dict(st=((64 * 8 * 64, 8 * 64, 64),) * 3, dq=S, dk=S + 4 * 64 * E2, dv=S + 7 * 64 * E2),
+    # overlapping spans of other strides
+    dict(st=(dense(64, 4, 64), (64 * 512, 512, 64), dense(64, 2, 64)), dk=S + 64)])
+def test_gradient_outputs_apart(kw):
+    assert backward(**kw) == L.EQL_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(o=S, lse=S), dict(lse=P), dict(lse=P + 2 * STEP + 16), dict(lengths=S), dict(starts=S + 4),
+                                dict(lse=W, lengths=W + 4), dict(B=1, L_=100000, Lq=1, ws=S), dict(B=1, L_=100000, Lq=1, ws=P + STEP),
+                                dict(B=1, L_=100000, Lq=1, ws=W, lse=W + 32)])
+def test_outputs_apart(kw):
+    assert forward(**kw) == L.EQL_ERR_INVALID_ARG
+
+
+@needs_no_gpu
+@pytest.mark.parametrize("kw", [
+    {}, dict(lengths=W - 4096, starts=W - 2048),
+    # one packed buffer: tokens of queries, keys, values; sequences padded; heads before tokens; tokens before sequences
+    dict(st=((64 * 8 * 64, 8 * 64, 64),) * 3, dq=S, dk=S + 4 * 64 * E2, dv=S + 6 * 64 * E2),
+    dict(st=((64 * 8 * 64 + 24, 8 * 64, 64),) * 3, dq=S, dk=S + 4 * 64 * E2, dv=S + 6 * 64 * E2),
+    dict(st=((64 * 8 * 64, 64, 64 * 64),) * 3, dq=S, dk=S + 4 * 64 * 64 * E2, dv=S + 6 * 64 * 64 * E2),
+    dict(st=((8 * 64, 2 * 8 * 64, 64),) * 3, dq=S, dk=S + 4 * 64 * E2, dv=S + 6 * 64 * E2),
+    dict(st=((8 * 64, 0, 64),) * 3, L_=1, dq=S, dk=S + 4 * 64 * E2, dv=S + 6 * 64 * E2),
+    dict(st=((64 * 4 * 64, 4 * 64, 64), (64 * 4 * 64, 4 * 64, 0), (64 * 4 * 64, 4 * 64, 0)), H=2, Hkv=1, dq=S,
+         dk=S + 2 * 64 * E2, dv=S + 3 * 64 * E2)])
+def test_gradients_may_interleave(kw):
+    assert backward(**kw) in PASSED
+
+
+@needs_no_gpu
+def test_outputs_that_are_apart():
+    assert forward() in PASSED and forward(lse=W, lengths=W + STEP, starts=W + 2 * STEP) in PASSED
+    assert forward(B=1, L_=100000, Lq=1, ws=W, lse=W + STEP) in PASSED
+
+
+def norm(f, **kw):
+    a = dict(x=P, w=P + STEP, b=P + STEP + 4096, y=S, stats=W, ws=W + STEP, B=2, S_=1 << 16, T=4, C=24, G=4)
+    a.update(kw)
+    shape = (a["B"], a["S_"], a["T"], a["C"], a["G"])
+    if f == "forward":
+        return L.eqlinear_group_norm_act(a["x"], a["w"], a["b"], a["y"], a["stats"], a["ws"], 1 << 26, *shape, 1e-5, 1,
+                                         L.EQL_F16, None)
+    g = dict(dy=P + 2 * STEP, dx=S + STEP, dw=S + 2 * STEP, db=S + 2 * STEP + 4096)
+    g.update({n: v for n, v in kw.items() if n in g})
+    return L.eqlinear_group_norm_act_backward(a["x"], a["w"], a["b"], a["stats"], g["dy"], g["dx"], g["dw"], g["db"], a["ws"],
+                                              1 << 26, *shape, 1, L.EQL_F16, None)
+
+
+@pytest.mark.parametrize("f,kw", [
+    ("forward", dict(stats=S)), ("forward", dict(stats=P + STEP)), ("forward", dict(ws=S + 4096)), ("forward", dict(ws=P)),
+    ("forward", dict(ws=W)), ("backward", dict(stats=S + STEP + 8)), ("backward", dict(ws=S + 2 * STEP)),
+    ("backward", dict(ws=W)), ("backward", dict(ws=P + 2 * STEP)), ("backward", dict(stats=S + 2 * STEP))])
+def test_group_norm_buffers_apart(f, kw):
+    assert norm(f, **kw) == L.EQL_ERR_INVALID_ARG
+
+
+@needs_no_gpu
+def test_group_norm_buffers_that_are_apart():
+    assert norm("forward") in PASSED and norm("backward") in PASSED
