@@ -91,8 +91,8 @@ int eqlinear_window_attention_backward(const eqlinear_window_shape* shape, const
  * (mean squared deviation) over the S positions, the C / groups channels of a
  * group and T:  y = act((x - mean) / sqrt(var + eps) * weight[c] + bias[c]).
  * stats (fp32 [B, groups, 2], 8-byte aligned: mean, 1 / sqrt(var + eps)) may be NULL; the backward
- * reads it.  Sums in fp32, one rounding.  C is a multiple of groups, T <= 16,
- * C <= 65536, groups <= 1024 (EQL_ERR_UNSUPPORTED). */
+ * reads it.  Sums in fp32, one rounding.  C is a multiple of groups, T <= 16, C <= 65536,
+ * groups <= 1024, B <= 2^20, S <= 2^30, 2^46 elements (EQL_ERR_UNSUPPORTED above). */
 enum { EQL_ACT_NONE = 0, EQL_ACT_RELU = 1, EQL_ACT_SILU = 2, EQL_ACT_GELU = 3 /* by erf */ };
 
 size_t eqlinear_group_norm_act_workspace_bytes(int64_t B, int64_t S, int T, int C, int groups, int dtype);

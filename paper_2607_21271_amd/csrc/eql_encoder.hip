@@ -29,27 +29,65 @@ hipError_t rotary_dt(const RotaryArgs& a, int vec, hipStream_t stream) {
   return rotary_v<DT, 1>(a, stream);
 }
 
+// The sequences b0 .. b0 + n of a call.  The parts are those of either pass (bwd), the sums stay
+// the call's: dw and db add them over all sequences.
+template <int DT>
+GnArgs gn_slice(const GnArgs& a, int64_t b0, int64_t n, bool bwd) {
+  const int64_t at = b0 * a.S * a.K * (int64_t)sizeof(typename Elem<DT>::T);
+  GnArgs s = a;
+  s.B = n;
+  s.x = (const char*)a.x + at;
+  if (a.y) s.y = (char*)a.y + at;
+  if (a.dy) s.dy = (const char*)a.dy + at;
+  if (a.dx) s.dx = (char*)a.dx + at;
+  if (a.stats) s.stats = a.stats + b0 * a.G * 2;
+  if (a.part) s.part = a.part + (bwd ? b0 * a.chunks * a.C : b0 * a.chunks * a.cblocks * a.G) * 2;
+  if (a.sums) s.sums = a.sums + b0 * a.C * 2;
+  return s;
+}
+// f(slice) for slices of at most `most` sequences, until one fails
+template <int DT, typename F>
+hipError_t gn_slices(const GnArgs& a, int64_t most, bool bwd, F&& f) {
+  for (int64_t b0 = 0; b0 < a.B; b0 += most) {
+    f(gn_slice<DT>(a, b0, a.B - b0 < most ? a.B - b0 : most, bwd));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+template <int DT>
+hipError_t gn_params_launch(const GnArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL((eql_gn_params_kernel<DT>), dim3((unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
 template <int DT, int VEC>
 hipError_t gn_fwd_v(const GnArgs& a, hipStream_t stream) {
-  const unsigned n = (unsigned)(a.B * a.chunks * a.cblocks);
-  hipLaunchKernelGGL((eql_gn_sums_kernel<DT, VEC>), dim3(n), dim3(256), 0, stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
   auto k = a.act == kActRelu   ? eql_gn_map_kernel<DT, VEC, kActRelu>
            : a.act == kActSilu ? eql_gn_map_kernel<DT, VEC, kActSilu>
            : a.act == kActGelu ? eql_gn_map_kernel<DT, VEC, kActGelu>
                                : eql_gn_map_kernel<DT, VEC, kActNone>;
-  hipLaunchKernelGGL(k, dim3(n), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  const int64_t per = (int64_t)a.chunks * a.cblocks;
+  return gn_slices<DT>(a, launch_blocks(256) / per, false, [&](const GnArgs& s) {
+    const dim3 n((unsigned)(s.B * per));
+    hipLaunchKernelGGL((eql_gn_sums_kernel<DT, VEC>), n, dim3(256), 0, stream, s);
+    hipLaunchKernelGGL(k, n, dim3(256), 0, stream, s);
+  });
 }
 
 template <int DT, int VEC, int ACT>
 hipError_t gn_bwd_a(const GnArgs& a, hipStream_t stream) {
-  const unsigned n = (unsigned)(a.B * a.chunks * a.cblocks);
-  hipLaunchKernelGGL((eql_gn_bsums_kernel<DT, VEC, ACT>), dim3(n), dim3(256), 0, stream, a);
-  hipLaunchKernelGGL(eql_gn_bchunks_kernel, dim3((unsigned)(a.B * ((a.C + 63) / 64))), dim3(256), 0, stream, a);
-  hipLaunchKernelGGL((eql_gn_bmap_kernel<DT, VEC, ACT>), dim3(n + (unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  const int64_t per = (int64_t)a.chunks * a.cblocks, tiles = (a.C + 63) / 64, params = (a.C + 3) / 4;
+  const int64_t most = (launch_blocks(256) - params) / (per > tiles ? per : tiles);
+  const bool whole = a.B <= most;  // the map's last workgroups form dw and db where one launch holds every sequence
+  const hipError_t e = gn_slices<DT>(a, most, true, [&](const GnArgs& s) {
+    const int64_t n = s.B * per;
+    hipLaunchKernelGGL((eql_gn_bsums_kernel<DT, VEC, ACT>), dim3((unsigned)n), dim3(256), 0, stream, s);
+    hipLaunchKernelGGL(eql_gn_bchunks_kernel, dim3((unsigned)(s.B * tiles)), dim3(256), 0, stream, s);
+    hipLaunchKernelGGL((eql_gn_bmap_kernel<DT, VEC, ACT>), dim3((unsigned)(n + (whole ? params : 0))), dim3(256), 0,
+                       stream, s);
+  });
+  return e != hipSuccess || whole ? e : gn_params_launch<DT>(a, stream);
 }
 template <int DT, int VEC>
 hipError_t gn_bwd_v(const GnArgs& a, hipStream_t stream) {
@@ -61,18 +99,19 @@ hipError_t gn_bwd_v(const GnArgs& a, hipStream_t stream) {
 
 template <int DT, int ACT>
 hipError_t gn_hold_a(const GnArgs& a, bool bwd, hipStream_t stream) {
-  const dim3 n((unsigned)(a.B * a.G));
-  if (!bwd) {
-    if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, a);
-    else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, a);
-    else hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 1024, 16>), n, dim3(1024), 0, stream, a);
-    return hipGetLastError();
-  }
-  if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, a);
-  else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 512, 16>), n, dim3(512), 0, stream, a);
-  hipLaunchKernelGGL((eql_gn_params_kernel<DT>), dim3((unsigned)((a.C + 3) / 4)), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  const hipError_t e = gn_slices<DT>(a, launch_blocks(a.threads) / a.G, bwd, [&](const GnArgs& s) {
+    const dim3 n((unsigned)(s.B * a.G));
+    if (!bwd) {
+      if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, s);
+      else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, s);
+      else hipLaunchKernelGGL((eql_gn_hold_kernel<DT, ACT, 1024, 16>), n, dim3(1024), 0, stream, s);
+    } else {
+      if (a.threads == 256 && a.hold <= 4) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 4>), n, dim3(256), 0, stream, s);
+      else if (a.threads == 256) hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 256, 16>), n, dim3(256), 0, stream, s);
+      else hipLaunchKernelGGL((eql_gn_bhold_kernel<DT, ACT, 512, 16>), n, dim3(512), 0, stream, s);
+    }
+  });
+  return e != hipSuccess || !bwd ? e : gn_params_launch<DT>(a, stream);
 }
 template <int DT>
 hipError_t gn_hold_dt(const GnArgs& a, bool bwd, hipStream_t stream) {

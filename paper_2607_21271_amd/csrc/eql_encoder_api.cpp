@@ -486,8 +486,6 @@ int eqlinear_group_norm_act(const void* x, const void* weight, const void* bias,
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
   eqk::gn_plan(a, vec, kPlanCus, false);
-  if ((double)B * (a.hold ? (double)groups * a.threads : (double)a.chunks * a.cblocks * 256) >= 4294967296.0)
-    return EQL_ERR_UNSUPPORTED;
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.x = x;
@@ -528,9 +526,6 @@ int eqlinear_group_norm_act_backward(const void* x, const void* weight, const vo
   if (empty) return check_device();
   const int vec = gn_vec(a, dtype);
   eqk::gn_plan(a, vec, kPlanCus, true);
-  if (((double)B * a.chunks * a.cblocks + C) * 256 >= 4294967296.0 || (double)B * (C + 64) * 4 >= 4294967296.0 ||
-      (double)B * groups * 512 >= 4294967296.0)
-    return EQL_ERR_UNSUPPORTED;
   if (!workspace || workspace_bytes < need) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
   a.x = x;

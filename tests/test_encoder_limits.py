@@ -135,3 +135,21 @@ def test_group_norm_buffers_apart(f, kw):
 @needs_no_gpu
 def test_group_norm_buffers_that_are_apart():
     assert norm("forward") in PASSED and norm("backward") in PASSED
+
+
+# B, S, C, T, groups: groups of one channel in passes; held groups, 2^24 of them; many channels of many sequences
+LARGE = [(262144, 16, 32, 1, 32), ((1 << 18) + 5, 1, 512, 1, 64), (16384, 1, 65536, 1, 1024), (1 << 20, 1, 3843, 1, 3),
+         (1 << 20, 3, 1024, 2, 1024)]
+
+
+@needs_no_gpu
+@pytest.mark.parametrize("B,S_,C,T,G", LARGE)
+def test_group_norm_of_large_batches(B, S_, C, T, G):
+    """What the forward takes, the gradient takes; more workgroups than one launch holds are no limit."""
+    n = L.eqlinear_group_norm_act_workspace_bytes(B, S_, T, C, G, L.EQL_F16)
+    m = L.eqlinear_group_norm_act_backward_workspace_bytes(B, S_, T, C, G, L.EQL_F16)
+    T_ = [i << 40 for i in range(1, 11)]
+    assert L.eqlinear_group_norm_act(T_[0], T_[1], T_[2], T_[3], T_[4], T_[5], n, B, S_, T, C, G, 1e-5, 0, L.EQL_F16,
+                                     None) in PASSED
+    assert L.eqlinear_group_norm_act_backward(T_[0], T_[1], T_[2], T_[3], T_[4], T_[5], T_[6], T_[7], T_[8], m, B, S_, T, C,
+                                              G, 0, L.EQL_F16, None) in PASSED
