@@ -8,16 +8,18 @@ namespace {
 
 template <int DT, int VEC>
 hipError_t rotary_v(const RotaryArgs& a, hipStream_t stream) {
-  const int64_t blocks = (a.tokens + a.TB - 1) / a.TB;
-  if (blocks > launch_blocks(256)) return hipErrorInvalidValue;
-  if constexpr (VEC > 1) {
-    if (a.interleaved && a.T == 1) {
-      hipLaunchKernelGGL((eql_rotary_kernel<DT, VEC, true>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-      return hipGetLastError();
-    }
+  auto k = eql_rotary_kernel<DT, VEC, false>;
+  if constexpr (VEC > 1)
+    if (a.interleaved && a.T == 1) k = eql_rotary_kernel<DT, VEC, true>;
+  RotaryArgs s = a;
+  for (s.first = 0; s.first < a.tokens; s.first += launch_blocks(256) * a.TB) {
+    int64_t blocks = (a.tokens - s.first + a.TB - 1) / a.TB;
+    if (blocks > launch_blocks(256)) blocks = launch_blocks(256);
+    hipLaunchKernelGGL(k, dim3((unsigned)blocks), dim3(256), 0, stream, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((eql_rotary_kernel<DT, VEC, false>), dim3((unsigned)blocks), dim3(256), 0, stream, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 template <int DT>

@@ -21,7 +21,7 @@ struct RotaryArgs {
   void* y;
   const void* positions;
   const float* freqs;
-  int64_t tokens, L;         // B * L, L
+  int64_t first, tokens, L;  // first token of a launch, B * L, L
   int64_t xs[3], ys[3];      // elements: sequence, token, head
   int64_t ps[2];             // positions: sequence, token
   int N, T, n, D;
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void eql_rotary_kernel(RotaryArgs a) {
   struct alignas(VEC * sizeof(E)) V { E e[VEC]; };
   __shared__ float2 cs[kRotaryAngles];
   __shared__ int64_t xo[kRotaryMaxTokens], yo[kRotaryMaxTokens];
-  const int64_t g0 = (int64_t)blockIdx.x * a.TB;
+  const int64_t g0 = a.first + (int64_t)blockIdx.x * a.TB;
   const int nt = (int)(a.tokens - g0 < a.TB ? a.tokens - g0 : a.TB);
   if ((int)threadIdx.x < nt) {
     const int64_t g = g0 + threadIdx.x, b = g / a.L, l = g % a.L;
