@@ -58,6 +58,8 @@ class EQWindowBlock(EQViTBlock):
         values [B, capacity, heads, D]); lengths and starts are filled + n and filled for every sequence, int32 [B]."""
         B, n = x.shape[:2]
         H = self.heads
+        if filled < 0 or any(filled + n > c.shape[1] for c in cache):
+            raise ValueError("%d tokens from place %d on do not fit a cache of %d" % (n, filled, cache[0].shape[1]))
         qkv = self.heads_of(self.qkv(self.norm1(x)))
         rotary.rotary_axes_(qkv[:, :, :2 * H], positions, self.freqs, self.sections, self.T)
         for c, new in zip(cache, (qkv[:, :, H:2 * H], qkv[:, :, 2 * H:])):

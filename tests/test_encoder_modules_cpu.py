@@ -89,3 +89,13 @@ def test_turning_in_place_is_refused_where_it_would_be_missed(monkeypatch):
     with pytest.raises(ValueError):
         torch.jit.trace(turn, x, check_trace=False)
     assert (turn(x) == 3.0).all()
+
+
+@pytest.mark.parametrize("filled,n", [(4, 1), (3, 2), (5, 1), (-1, 1)])
+def test_tokens_past_the_end_of_a_cache_are_refused(filled, n):
+    """One token past a full cache would broadcast into an empty slice: dropped, and its attention zeros."""
+    block = EQWindowBlock(2, 8, 2, (1,), right=0)
+    cache = tuple(torch.zeros(3, 4, 2, 8) for _ in range(2))
+    spans = torch.full((2, 3), filled, dtype=torch.int32)
+    with pytest.raises(ValueError, match="cache"):
+        block.extend(torch.zeros(3, n, 8, 2), torch.zeros(n, 1, dtype=torch.int32), cache, filled, spans[0] + n, spans[1])
