@@ -200,6 +200,8 @@ def packed_window_attention(qkv: torch.Tensor, kv_heads: int, positions: torch.T
         raise ValueError("qkv must be [B, L, heads + 2 * kv_heads, D] with heads a multiple of kv_heads = %d, got %s"
                          % (kv_heads, tuple(qkv.shape)))
     _check_window(left, right, sinks)
+    if positions is not None and freqs is None:
+        raise ValueError("positions need freqs (rotary.axis_frequencies)")
     ops._check_dev(qkv)
     _check_spans(qkv.shape[0], qkv, lengths, None)
     if positions is not None:

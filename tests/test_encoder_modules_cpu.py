@@ -99,3 +99,10 @@ def test_tokens_past_the_end_of_a_cache_are_refused(filled, n):
     spans = torch.full((2, 3), filled, dtype=torch.int32)
     with pytest.raises(ValueError, match="cache"):
         block.extend(torch.zeros(3, n, 8, 2), torch.zeros(n, 1, dtype=torch.int32), cache, filled, spans[0] + n, spans[1])
+
+
+def test_packed_attention_with_positions_needs_frequencies():
+    from paper_2607_21271_amd import attention
+    x = torch.zeros(2, 5, 3, 8)
+    with pytest.raises(ValueError, match="freqs"):
+        attention.packed_window_attention(x, 1, torch.zeros(5, 1, dtype=torch.int32), sections=(2,))
