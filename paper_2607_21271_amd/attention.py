@@ -66,9 +66,8 @@ def _forward(q, k, v, lengths, starts, left, right, sinks, scale, want_lse):
     # lse [B, kv_heads, Lq, heads / kv_heads]
     lse = q.new_empty(qshape[:3], dtype=torch.float32) if want_lse else None
     ws = q.new_empty((need,), dtype=torch.uint8) if need else None
-    _lib.check(_lib.eqlinear_window_attention(ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
-                                              ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(ws), need,
-                                              ops._stream_of(q)), "eqlinear_window_attention")
+    ops._launch("eqlinear_window_attention", q, ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
+                ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(ws), need)
     return o, lse
 
 
@@ -76,10 +75,9 @@ def _backward(q, k, v, lengths, starts, o, lse, do, dq, dk, dv, left, right, sin
     ref, need = _plan(q.dtype, q.shape, k.shape, q.stride(), k.stride(), v.stride(), do.stride(), dq.stride(),
                       dk.stride(), dv.stride(), left, right, sinks, scale)
     ws = q.new_empty((need,), dtype=torch.uint8) if need else None
-    _lib.check(_lib.eqlinear_window_attention_backward(
-        ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths), ops._ptr(starts), ops._ptr(o), ops._ptr(lse),
-        ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv), ops._ptr(ws), need, ops._stream_of(q)),
-        "eqlinear_window_attention_backward")
+    ops._launch("eqlinear_window_attention_backward", q, ref, ops._ptr(q), ops._ptr(k), ops._ptr(v), ops._ptr(lengths),
+                ops._ptr(starts), ops._ptr(o), ops._ptr(lse), ops._ptr(do), ops._ptr(dq), ops._ptr(dk), ops._ptr(dv),
+                ops._ptr(ws), need)
 
 
 def _check_spans(B, dev_of, lengths, starts):

@@ -53,9 +53,8 @@ def _forward(x, weight, bias, groups, act, eps, want_stats):
     y = torch.empty_like(x)
     stats = x.new_empty((B, groups, 2), dtype=torch.float32) if want_stats else None
     ws = x.new_empty((need,), dtype=torch.uint8) if need else None
-    _lib.check(_lib.eqlinear_group_norm_act(ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(y), ops._ptr(stats),
-                                            ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt, ops._stream_of(x)),
-               "eqlinear_group_norm_act")
+    ops._launch("eqlinear_group_norm_act", x, ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(y), ops._ptr(stats),
+                ops._ptr(ws), need, B, S, T, C, groups, eps, act, dt)
     return y, stats
 
 
@@ -82,10 +81,9 @@ class GroupNormActFunction(torch.autograd.Function):
             return dx, torch.zeros_like(weight), torch.zeros_like(bias), None, None, None
         dw, db = torch.empty_like(weight), torch.empty_like(bias)
         ws = x.new_empty((need,), dtype=torch.uint8)
-        _lib.check(_lib.eqlinear_group_norm_act_backward(
-            ops._ptr(x), ops._ptr(weight), ops._ptr(bias), ops._ptr(stats), ops._ptr(gy), ops._ptr(dx), ops._ptr(dw),
-            ops._ptr(db), ops._ptr(ws), need, B, S, T, C, groups, act, dt, ops._stream_of(x)),
-            "eqlinear_group_norm_act_backward")
+        ops._launch("eqlinear_group_norm_act_backward", x, ops._ptr(x), ops._ptr(weight), ops._ptr(bias),
+                    ops._ptr(stats), ops._ptr(gy), ops._ptr(dx), ops._ptr(dw), ops._ptr(db), ops._ptr(ws), need, B, S, T,
+                    C, groups, act, dt)
         return dx, dw, db, None, None, None
 
 

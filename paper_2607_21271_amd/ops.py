@@ -23,8 +23,13 @@ from __future__ import annotations
 import weakref
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
+
+# looked up once: a call over a single token takes some microseconds of Python
+_is_grad_enabled, _is_tracing = torch.is_grad_enabled, torch._C._is_tracing
+_transforms = torch._C._functorch.peek_interpreter_stack
 
 _DT = {torch.float32: _lib.EQL_F32, torch.float16: _lib.EQL_F16, torch.bfloat16: _lib.EQL_BF16}
 
@@ -48,25 +53,32 @@ def _stream(stream):
 def _watched() -> bool:
     """Whether torch records or transforms the operations of this thread: a trace, a forward-mode level, a functorch
     transform.  An autograd function is part of that (or refuses it); a bare launch would leave no mark."""
-    return (torch.jit.is_tracing() or torch.autograd.forward_ad._current_level >= 0
-            or torch._C._functorch.peek_interpreter_stack() is not None)
+    return _is_tracing() or forward_ad._current_level >= 0 or _transforms() is not None
 
 
 def _no_node(*ts) -> bool:
     """Whether a call on these tensors needs no autograd function: no gradient is wanted and nothing looks on."""
-    if torch.is_grad_enabled():
+    if _is_grad_enabled():
         for t in ts:
             if t.requires_grad:
                 return False
-    return not _watched()
+    return not (_is_tracing() or forward_ad._current_level >= 0 or _transforms() is not None)
 
 
-def _stream_of(t: torch.Tensor) -> int:
-    """Handle of the current stream of t's device, which has to be the current device (a launch goes there)."""
-    index = t.device.index
-    if index != torch._C._cuda_getDevice():
-        raise ValueError("tensors on cuda:%d, current device cuda:%d" % (index, torch._C._cuda_getDevice()))
-    return torch._C._cuda_getCurrentRawStream(index)
+def _stream_of(t: torch.Tensor):
+    """Handle of the current stream of t's device; None where that is not the current device (a launch goes there)."""
+    index, c = t.device.index, torch._C
+    return c._cuda_getCurrentRawStream(index) if index == c._cuda_getDevice() else None
+
+
+def _launch(entry: str, t: torch.Tensor, *args):
+    """The library's entry point on t's device and its current stream."""
+    stream = _stream_of(t)
+    if stream is None:
+        with torch.cuda.device(t.device):
+            _lib.check(getattr(_lib, entry)(*args, torch._C._cuda_getCurrentRawStream(t.device.index)), entry)
+    else:
+        _lib.check(getattr(_lib, entry)(*args, stream), entry)
 
 
 def _check_dev(*ts):

@@ -45,8 +45,7 @@ def _plan(dtype, shape, x, y, pos, float_pos, sections, T, interleaved, inverse)
 def _launch(x, positions, freqs, sections, T, interleaved, inverse, y):
     ref = _plan(x.dtype, x.shape, x.stride(), y.stride(), positions.stride(), positions.dtype == torch.float32, sections,
                 T, interleaved, inverse)
-    _lib.check(_lib.eqlinear_rotary(ref, ops._ptr(x), ops._ptr(positions), ops._ptr(freqs), ops._ptr(y),
-                                    ops._stream_of(x)), "eqlinear_rotary")
+    ops._launch("eqlinear_rotary", x, ref, ops._ptr(x), ops._ptr(positions), ops._ptr(freqs), ops._ptr(y))
     return y
 
 
@@ -130,7 +129,7 @@ def rotary_axes_(x: torch.Tensor, positions: torch.Tensor, freqs: torch.Tensor, 
     _check(x, positions, freqs, sections, T)
     if x.requires_grad and torch.is_grad_enabled():
         raise ValueError("rotary_axes_ is not differentiable; use rotary_axes")
-    if ops._watched() and (torch.jit.is_tracing() or torch._C._functorch.peek_interpreter_stack() is not None
+    if ops._watched() and (ops._is_tracing() or ops._transforms() is not None
                            or torch.autograd.forward_ad.unpack_dual(x).tangent is not None):
         raise ValueError("rotary_axes_ cannot be traced or transformed; use rotary_axes")
     if x.stride(3) != 1 and x.shape[3] != 1:

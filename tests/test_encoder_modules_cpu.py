@@ -106,3 +106,28 @@ def test_packed_attention_with_positions_needs_frequencies():
     x = torch.zeros(2, 5, 3, 8)
     with pytest.raises(ValueError, match="freqs"):
         attention.packed_window_attention(x, 1, torch.zeros(5, 1, dtype=torch.int32), sections=(2,))
+
+
+def test_launches_go_to_the_tensors_device(monkeypatch):
+    """Tensors of another device than the current one: the call runs on theirs, on its current stream."""
+    import contextlib
+    from types import SimpleNamespace
+
+    from paper_2607_21271_amd import _lib, ops
+    log, current = [], [0]
+
+    @contextlib.contextmanager
+    def device(d):
+        before, current[0] = current[0], getattr(d, "index", d)
+        yield
+        current[0] = before
+    monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda i: 100 + i, raising=False)
+    monkeypatch.setattr(_lib, "eqlinear_rotary", lambda *a: log.append((current[0], *a)) or 0)
+    for index in (0, 1):
+        ops._launch("eqlinear_rotary", SimpleNamespace(device=SimpleNamespace(type="cuda", index=index)), 7, 8)
+    assert log == [(0, 7, 8, 100), (1, 7, 8, 101)] and current == [0]
+    monkeypatch.setattr(_lib, "eqlinear_rotary", lambda *a: _lib.EQL_ERR_INVALID_ARG)
+    with pytest.raises(_lib.EqlError):
+        ops._launch("eqlinear_rotary", SimpleNamespace(device=SimpleNamespace(type="cuda", index=1)), 7, 8)
