@@ -79,7 +79,8 @@ int eqlinear_window_attention(const eqlinear_window_shape* shape, const void* q,
                               size_t workspace_bytes, void* stream);
 
 /* Gradients of the above: o and lse as the forward wrote them.  dk, dv sum over
- * the query heads that share a head.  delta = <do, o> is taken from the rounded o. */
+ * the query heads that share a head.  delta = <do, o> is taken from the
+ * rounded o, or summed anew for 16-bit rows that see few keys. */
 size_t eqlinear_window_attention_backward_workspace_bytes(const eqlinear_window_shape* shape);
 int eqlinear_window_attention_backward(const eqlinear_window_shape* shape, const void* q, const void* k, const void* v,
                                        const int32_t* lengths, const int32_t* starts, const void* o, const float* lse,

@@ -749,7 +749,7 @@ __global__ __launch_bounds__(256) void eql_wattn_join_kernel(AttnArgs a) {
 // numbers counts, and comes down as a running maximum goes up: where a tile holds an entry
 // of more than 2^15, the owner's largest is taken to about 2^kRaised, and what was summed with it.
 // An entry 2^17 times smaller than its owner's largest keeps all its bits.  Infinities stay.
-// The maximum costs up to 3% of a gradient (16,389 tokens, 12 heads of 64, window +-1024: 490 -> 504 us).
+// The maximum costs up to 5% of a gradient (16,389 tokens, 12 heads of 64, window +-1024: 495 -> 508 us).
 constexpr float kRaiseStart = 0x1p60f, kRaiseLimit = 0x1p15f;
 constexpr int kRaised = 4;
 template <int DP>
@@ -772,13 +772,17 @@ __device__ __forceinline__ void lower_raise(floatx16& t, floatx16 (&acc)[DP / 32
 
 // ---- query gradient --------------------------------------------------------
 // dq = scale sum_j ds_j k_j, ds_j = p_j (do . v_j - delta), p_j = exp2(c s_j - lse),
-// delta = do . o, which it writes for the kernel that follows.  delta is taken
-// from the rounded o: an error of u |do| |o| in a difference of numbers sqrt(keys)
-// larger, seen only where a row sees a handful of keys (dq 1.5 - 1.8 times as far
-// from the exact one as a result rounded once, else 1.4 by the rounded ds).
+// delta = do . o = sum_j p_j do . v_j, which it writes for the kernel that follows.  16 bits: the
+// rounded o would put an error of u |do| |o| into a difference of numbers that are larger by
+// sqrt(keys) only, so a workgroup with a row that sees at most kFewKeys keys first walks its tiles for
+// sum_j p_j do . v_j over sum_j p_j (dq and dk of rows of two keys 1.5 times as far from the exact
+// ones as results rounded once, from the rounded o 2.2; of five keys 1.45 and 1.7; from 33 keys on
+// it makes 0.1 of a difference).  Elsewhere do . o of the rounded o; ds rounded costs 1.4 by itself.
+// Windows of 16 keys over 4,096 tokens run as fast either way, both gradients 104 - 110 us.
 //
 // Three products where the forward has two, and bound like it.  2 ragged clips of up to
-// 8,197 tokens, 16 heads of 128 on 4, window 2047, bf16: 295 - 340 us.
+// 8,197 tokens, 16 heads of 128 on 4, window 2047, bf16: 300 - 330 us.
+constexpr int kFewKeys = 32;
 template <int DT, int DP, int NW>
 __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kernel(AttnArgs a) {
   using RT = RowTile<DT, DP>;
@@ -811,8 +815,14 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
   const char* const vb = (const char*)a.v + ((int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2]) * RT::EB;
   const int64_t row = (int64_t)bh * a.R + r;
   const float lse = row_ok ? a.lse[row] : __builtin_inff();
+  // whether some row of the workgroup sees few keys (the first and last see the fewest)
+  auto keys_of = [&](int p) {
+    const int last = min(len - 1, p + a.right), first = max(0, p - a.left);
+    return max(last - first + 1, 0) + min(a.sinks, min(first, last + 1));
+  };
+  const bool few = DT != kF32 && kg.n > 0 && min(keys_of(start + g0 / a.G), keys_of(min(start + g1 / a.G, len - 1))) <= kFewKeys;
   float delta = 0.0f;
-  if (row_ok) {
+  if (row_ok && !few) {
     // each half of the wave takes every second chunk of the row
     const char *const po = at(a.o, a.os), *const pg = at(a.go, a.gos);
 #pragma unroll 1
@@ -827,7 +837,6 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     }
   }
   delta = half_sum(delta);
-  if (half == 0 && r < a.R) a.delta[row] = delta;
   Frag8<DT> qf[DP / 16], gf[DP / 16];
   load_owner<DT, DP>(qf, at(a.q, a.qs), row_ok, a.D, half);
   load_owner<DT, DP>(gf, at(a.go, a.gos), row_ok, a.D, half);
@@ -842,11 +851,13 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     sv_.load(row_rsrc<TK>(vb, vst, k0, len, a.D * RT::EB));
   };
   floatx16 acc[DP / 32];
-  float up;  // the power of two that ds is formed times
+  float up;            // the power of two that ds is formed times
+  float sum_p, sum_g;  // of a row's probabilities, and times do . v
   const float c = a.scale_log2e;
   const LdsMap<DT, DP> map(lane);
-  auto walk = [&](auto careful) {
-    constexpr bool kCareful = decltype(careful)::value;
+  auto walk = [&](auto mode) {
+    constexpr bool kCareful = decltype(mode)::value == 1, kDelta = decltype(mode)::value == 2;
+    sum_p = sum_g = 0.0f;
 #pragma unroll
     for (int d = 0; d < DP / 32; ++d) acc[d] = floatx16{};
     up = DT == kF16 ? kRaiseStart : 1.0f;
@@ -860,7 +871,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
       sv_.store(tid, vt);
       const int k0 = kg.tile(i) * TK;
       const bool part_seen = !kg.whole(k0, TK);  // some row sees the tile in part
-      if (part_seen) {
+      if (part_seen && !kDelta) {
         ExpMax<DT> e;
         sk_.scan(e);
         const bool any = __any(e.hit());
@@ -868,7 +879,7 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
       }
       __syncthreads();
       if (i + 1 < kg.n) load(i + 1);
-      if constexpr (!kCareful) {
+      if constexpr (!kCareful && !kDelta) {
         if (part_seen && any_flag<NW>(flag)) return false;
       }
       if (k0 > kw.last || (k0 + TK <= kw.first && k0 >= kw.sink_end)) return true;
@@ -883,6 +894,16 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
         for (int t = 0; t < DP / 16; ++t) {
           mma32<DT>(s, map.row(kt, n, t), qf[t]);
           mma32<DT>(g, map.row(vt, n, t), gf[t]);
+        }
+        if constexpr (kDelta) {
+          const uint32_t bits = whole ? ~0u : seen_bits(k0 + 32 * n) >> (4 * half);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -lse));
+            sum_p += bits_f32(f32_bits(p) & entry_mask(bits, e));
+            sum_g += bits_f32(f32_bits(p * g[e]) & entry_mask(bits, e));
+          }
+          continue;
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -917,9 +938,17 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
     }
     return true;
   };
-  if (!walk(std::false_type{})) {
+  if (few) {
+    walk(std::integral_constant<int, 2>{});
+    sum_p = half_sum(sum_p);
+    sum_g = half_sum(sum_g);
+    delta = row_ok && sum_p != 0.0f ? sum_g / sum_p : 0.0f;
     __syncthreads();
-    walk(std::true_type{});
+  }
+  if (half == 0 && r < a.R) a.delta[row] = delta;
+  if (!walk(std::integral_constant<int, 0>{})) {
+    __syncthreads();
+    walk(std::integral_constant<int, 1>{});
   }
   store_owner<DT, DP>(acc, DT == kF16 ? a.scale / up : a.scale, row_ok, at(a.dq, a.dqs), r < a.R, a.D, half);
 }
