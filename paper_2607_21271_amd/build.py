@@ -33,7 +33,9 @@ ARCH = "gfx950"
 # Packed-fp32 instructions are switched off for all device code.
 # MFMA accumulators may live in arch VGPRs (gfx950 has a unified register
 # file); with this selection the kernels of two waves per SIMD allocate
-# without scratch.  The large-tile unit (one wave per SIMD, T * 64
+# without scratch, but for the weight gradient of T = 11 and 12 (24 to 112
+# bytes a lane) and the attention's key gradient at heads above 96 (64 in bf16,
+# 352 in fp16; 164 in full precision, one wave).  The large-tile unit (one wave per SIMD, T * 64
 # accumulators per lane) and full-precision attention keep them in the
 # accumulation registers instead.
 LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

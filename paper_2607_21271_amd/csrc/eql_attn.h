@@ -962,8 +962,9 @@ __global__ __launch_bounds__(NW * 64, DT == kF32 ? 1 : 2) void eql_wattn_dq_kern
 //
 // Bound: heads of 128 by waiting (1.3 waves a SIMD; products 25% busy, LDS 30%): a key
 // tile streams the rows that see it, 4.4 MB for a window of 2047 over 4 heads, and 58%
-// of that comes from the L2.  The clips above: 560 - 600 us (dk and dv in workgroups of their
-// own, which stream twice as much: 1145).  64 x 197 tokens, 12 heads of 64, fp16: 50 us.
+// of that comes from the L2.  The clips above: 570 - 610 us (dk and dv in workgroups of their
+// own, which stream twice as much: 1145); of full length both gradients 1.14 ms, in fp16, which
+// spills more, 1.37.  64 x 197 tokens, 12 heads of 64, fp16: 48 us.
 
 // Wave groups of a workgroup, each taking its share of every tile's rows for the same
 // keys.  Heads of more than 96 16-bit elements take two: their accumulators leave no
@@ -1256,7 +1257,7 @@ __global__ __launch_bounds__(256 * dkv_groups(DT, DP), DT == kF32 || DP == 96 ? 
 }
 
 // Adds the parts of split key tiles in their order: a thread four elements of one
-// tile's gradient; blockIdx.y the tile of a head pair and the gradient.
+// tile's gradient.
 template <int DT>
 __global__ __launch_bounds__(256) void eql_wattn_dkv_sum_kernel(AttnArgs a, int keys) {
   using E = typename Elem<DT>::T;
