@@ -40,8 +40,8 @@ _BLOCK_END = re.compile(r"^\.LBB|^\s*s_cbranch|^\s*s_branch|^; %bb")
 _CVT = re.compile(r"^\s*v_cvt_f32_f16\S*\s+v(\d+),\s*v(\d+)\b")
 _F32_DEF = re.compile(r"^\s*(v_cvt_f32_f16\S*|v_add_f32\S*|v_sub_f32\S*|v_subrev_f32\S*|v_mul_f32\S*"
                       r"|v_fma_f32\S*|v_fmac_f32\S*|v_fmamk_f32\S*|v_fmaak_f32\S*)\s+v(\d+),")
-_DEF_RANGE = re.compile(r"^\s*(v_\S+|buffer_load\S*|global_load\S*|ds_read\S*)\s+v\[(\d+):(\d+)\]")
-_DEF_ONE = re.compile(r"^\s*(v_\S+|buffer_load\S*|global_load\S*|ds_read\S*)\s+v(\d+)\b")
+_DEF_RANGE = re.compile(r"^\s*(v_\S+|buffer_load\S*|global_load\S*|scratch_load\S*|ds_read\S*)\s+v\[(\d+):(\d+)\]")
+_DEF_ONE = re.compile(r"^\s*(v_\S+|buffer_load\S*|global_load\S*|scratch_load\S*|ds_read\S*)\s+v(\d+)\b")
 _UNPACK_FIRST = re.compile(r"^\s*v_cvt_f32_f16_e32 v(\d+), v(\d+)\s*$")
 _SCRATCH = re.compile(r"^; ScratchSize: (\d+)")
 _MFMA = re.compile(r"^\s*v_mfma\S*\s+([va])\[(\d+):(\d+)\],\s*[^,]+,\s*[^,]+,\s*([va])\[(\d+):(\d+)\]")
