@@ -7,7 +7,7 @@ an autograd Function and ``EQLinear`` module.  Submodules load lazily, and
 using them without the built library raises.
 """
 
-__all__ = ["_lib", "attention", "encoder", "norm", "ops", "roofline", "rotary"]
+__all__ = ["_lib", "attention", "encoder", "norm", "ops", "roofline", "rotary", "scan"]
 
 
 def __getattr__(name):

@@ -1,4 +1,5 @@
-"""ctypes binding of libeqlinear.so: the C ABI of include/eqlinear.h, eqlinear_block.h and eqlinear_encoder.h, same names.
+"""ctypes binding of libeqlinear.so: the C ABI of include/eqlinear.h, eqlinear_block.h, eqlinear_encoder.h and
+eqlinear_recurrent.h, same names.
 
 Argument marshalling only.  Every function takes device addresses as Python
 ints (or None for NULL) and returns the library's status code; ``check``
@@ -35,6 +36,9 @@ EQL_ACT_RELU = 1
 EQL_ACT_SILU = 2
 EQL_ACT_GELU = 3
 
+EQL_NORM_LAYER = 0
+EQL_NORM_RMS = 1
+
 _vp, _i, _i64, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_size_t
 _f = ctypes.c_float
 
@@ -53,8 +57,27 @@ class WindowShape(ctypes.Structure):
                     (n + "_stride", _i64 * 3) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")]
 
 
+class ScanShape(ctypes.Structure):
+    """eqlinear_scan_shape of include/eqlinear_recurrent.h."""
+    _fields_ = [("B", _i64), ("L", _i64), ("C", _i), ("T", _i), ("N", _i), ("groups", _i), ("softplus", _i), ("dtype", _i),
+                ("x_stride", _i64 * 2), ("delta_stride", _i64 * 2), ("z_stride", _i64 * 2), ("b_stride", _i64 * 3),
+                ("c_stride", _i64 * 3)]
+
+
+class ConvShape(ctypes.Structure):
+    """eqlinear_conv_shape of include/eqlinear_recurrent.h."""
+    _fields_ = [("B", _i64), ("L", _i64), ("C", _i), ("T", _i), ("W", _i), ("act", _i), ("dtype", _i), ("reserved", _i),
+                ("x_stride", _i64 * 2)]
+
+
+class ResidualShape(ctypes.Structure):
+    """eqlinear_residual_shape of include/eqlinear_recurrent.h."""
+    _fields_ = [("B", _i64), ("L", _i64), ("C", _i), ("T", _i), ("kind", _i), ("dtype", _i), ("eps", _f), ("reserved", _i)]
+
+
 # Every function the headers declare, with (restype, argtypes).
 _RS, _WS = ctypes.POINTER(RotaryShape), ctypes.POINTER(WindowShape)
+_SS, _CS, _NS = ctypes.POINTER(ScanShape), ctypes.POINTER(ConvShape), ctypes.POINTER(ResidualShape)
 SIGNATURES = {
     "eqlinear_abi_version": (_i, []),
     "eqlinear_status_string": (ctypes.c_char_p, [_i]),
@@ -87,6 +110,17 @@ SIGNATURES = {
     "eqlinear_group_norm_act": (_i, [_vp] * 6 + [_sz, _i64, _i64, _i, _i, _i, _f, _i, _i, _vp]),
     "eqlinear_group_norm_act_backward_workspace_bytes": (_sz, [_i64, _i64, _i, _i, _i, _i]),
     "eqlinear_group_norm_act_backward": (_i, [_vp] * 9 + [_sz, _i64, _i64, _i, _i, _i, _i, _i, _vp]),
+    "eqlinear_selective_scan_workspace_bytes": (_sz, [_SS]),
+    "eqlinear_selective_scan_states_bytes": (_sz, [_SS]),
+    "eqlinear_selective_scan": (_i, [_SS] + [_vp] * 14 + [_sz, _vp]),
+    "eqlinear_selective_scan_backward_workspace_bytes": (_sz, [_SS]),
+    "eqlinear_selective_scan_backward": (_i, [_SS] + [_vp] * 22 + [_sz, _vp]),
+    "eqlinear_causal_conv": (_i, [_CS] + [_vp] * 8),
+    "eqlinear_causal_conv_backward_workspace_bytes": (_sz, [_CS]),
+    "eqlinear_causal_conv_backward": (_i, [_CS] + [_vp] * 12 + [_sz, _vp]),
+    "eqlinear_residual_norm": (_i, [_NS] + [_vp] * 11),
+    "eqlinear_residual_norm_backward_workspace_bytes": (_sz, [_NS]),
+    "eqlinear_residual_norm_backward": (_i, [_NS] + [_vp] * 18 + [_sz, _vp]),
 }
 
 
@@ -259,3 +293,59 @@ def eqlinear_group_norm_act_backward(x, weight, bias, stats, dy, dx, dw, db, wor
                                      groups, act, dtype, stream) -> int:
     return lib().eqlinear_group_norm_act_backward(x, weight, bias, stats, dy, dx, dw, db, workspace, workspace_bytes,
                                                   B, S, T, C, groups, act, dtype, stream)
+
+
+def eqlinear_selective_scan_workspace_bytes(shape) -> int:
+    return lib().eqlinear_selective_scan_workspace_bytes(shape)
+
+
+def eqlinear_selective_scan_states_bytes(shape) -> int:
+    return lib().eqlinear_selective_scan_states_bytes(shape)
+
+
+def eqlinear_selective_scan(shape, x, delta, A, b, c, D, z, delta_bias, lengths, state_in, y, state_out, states, workspace,
+                            workspace_bytes, stream) -> int:
+    return lib().eqlinear_selective_scan(shape, x, delta, A, b, c, D, z, delta_bias, lengths, state_in, y, state_out,
+                                         states, workspace, workspace_bytes, stream)
+
+
+def eqlinear_selective_scan_backward_workspace_bytes(shape) -> int:
+    return lib().eqlinear_selective_scan_backward_workspace_bytes(shape)
+
+
+def eqlinear_selective_scan_backward(shape, x, delta, A, b, c, D, z, delta_bias, lengths, states, dy, d_state_out, dx,
+                                     ddelta, dA, db, dc, dD, dz, ddelta_bias, d_state_in, workspace, workspace_bytes,
+                                     stream) -> int:
+    return lib().eqlinear_selective_scan_backward(shape, x, delta, A, b, c, D, z, delta_bias, lengths, states, dy,
+                                                  d_state_out, dx, ddelta, dA, db, dc, dD, dz, ddelta_bias, d_state_in,
+                                                  workspace, workspace_bytes, stream)
+
+
+def eqlinear_causal_conv(shape, x, weight, bias, lengths, state_in, y, state_out, stream) -> int:
+    return lib().eqlinear_causal_conv(shape, x, weight, bias, lengths, state_in, y, state_out, stream)
+
+
+def eqlinear_causal_conv_backward_workspace_bytes(shape) -> int:
+    return lib().eqlinear_causal_conv_backward_workspace_bytes(shape)
+
+
+def eqlinear_causal_conv_backward(shape, x, weight, bias, lengths, state_in, dy, d_state_out, dx, dweight, dbias,
+                                  d_state_in, workspace, workspace_bytes, stream) -> int:
+    return lib().eqlinear_causal_conv_backward(shape, x, weight, bias, lengths, state_in, dy, d_state_out, dx, dweight,
+                                               dbias, d_state_in, workspace, workspace_bytes, stream)
+
+
+def eqlinear_residual_norm(shape, x, branch, weight, bias, scale, gate, post_weight, post_bias, r, h, stream) -> int:
+    return lib().eqlinear_residual_norm(shape, x, branch, weight, bias, scale, gate, post_weight, post_bias, r, h, stream)
+
+
+def eqlinear_residual_norm_backward_workspace_bytes(shape) -> int:
+    return lib().eqlinear_residual_norm_backward_workspace_bytes(shape)
+
+
+def eqlinear_residual_norm_backward(shape, x, branch, weight, scale, gate, post_weight, post_bias, dr, dh, dx, dbranch,
+                                    dweight, dbias, dscale, dgate, dpost_weight, dpost_bias, workspace, workspace_bytes,
+                                    stream) -> int:
+    return lib().eqlinear_residual_norm_backward(shape, x, branch, weight, scale, gate, post_weight, post_bias, dr, dh, dx,
+                                                 dbranch, dweight, dbias, dscale, dgate, dpost_weight, dpost_bias,
+                                                 workspace, workspace_bytes, stream)

@@ -20,11 +20,13 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libeqlinear.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 
-HOST_SOURCES = ["eql_api.cpp", "eql_dispatch.cpp", "eql_encoder_api.cpp"]
+HOST_SOURCES = ["eql_api.cpp", "eql_dispatch.cpp", "eql_encoder_api.cpp", "eql_recurrent_api.cpp"]
 MAX_T = 16
 # (source, object stem, extra defines)
 UNITS = [("eql_big.hip", "eql_big", []), ("eql_block.hip", "eql_block", []), ("eql_encoder.hip", "eql_encoder", [])] + [
-    ("eql_attn.hip", "attn_" + name, ["-DEQK_DT=%d" % dt]) for dt, name in ((1, "f16"), (0, "f32"), (2, "bf16"))] + [(s, os.path.splitext(s)[0], []) for s in HOST_SOURCES] + [
+    (src, stem + name, ["-DEQK_DT=%d" % dt])
+    for src, stem in (("eql_attn.hip", "attn_"), ("eql_scan.hip", "scan_"), ("eql_recurrent.hip", "recurrent_"))
+    for dt, name in ((1, "f16"), (0, "f32"), (2, "bf16"))] + [(s, os.path.splitext(s)[0], []) for s in HOST_SOURCES] + [
     ("eql_inst.hip", "inst_%s_t%02d" % (name, t), ["-DEQK_T=%d" % t, "-DEQK_DT=%d" % dt])
     for t in range(MAX_T, 0, -1) for dt, name in ((1, "f16"), (0, "f32"), (2, "bf16"))]
 

@@ -1,0 +1,111 @@
+// eql_recurrent.h -- arguments, plans and launches of the scan, causal convolution and
+// residual-norm kernels, shared by host and device code.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "eql_config.h"
+
+namespace eqk {
+
+// ---- selective scan ----
+// A wave takes `scan_cols(NL)` neighbouring columns (channel, group element) of one group:
+// NL lanes share four columns and hold four states of each.
+constexpr int kScanMaxN = 64;
+constexpr int scan_lanes(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
+constexpr int scan_cols(int NL) { return 256 / NL; }
+// tokens of a tile, whose first state training keeps
+constexpr int scan_tile(int NL) { return NL == 1 ? 4 : NL == 2 ? 8 : 16; }
+constexpr int scan_ept(int NL) { return scan_tile(NL) * scan_cols(NL) / 64; }  // elements of a lane
+constexpr int scan_vec(int dt, int NL) {
+  return (dt == kF32 ? 4 : 8) < scan_ept(NL) ? (dt == kF32 ? 4 : 8) : scan_ept(NL);
+}
+constexpr int kScanWaves = 4;  // of a workgroup
+
+struct ScanArgs {
+  const void *x, *delta, *z, *b, *c, *dy;
+  const float *A, *D, *bias, *h0, *dhT;
+  void *y, *dx, *ddelta, *dz, *db, *dc;
+  float *hT, *dh0, *dA, *dD, *dbias;
+  const int* lengths;
+  float* states;  // [B, tiles, cols, NP]: the state before each tile
+  float* carry;   // [B, K, cols, NP]: the state before each chunk (backward: the gradient behind it)
+  float* sums;    // [B, K, cols]: the chunk's sum of d
+  float* part;    // [B * K, N + 2, cols]: sums of dA, dD, ddelta_bias
+  float* bcpart;  // [B, L, groups, P, 2, NP]: db and dc of each workgroup's columns
+  int64_t xs[2], ds[2], zs[2], bs[3], cs[3];
+  int64_t B, L, first;   // first: workgroup of the call that this launch starts with
+  int64_t chunk, tiles;  // tokens of a chunk (whole tiles), tiles of a sequence
+  int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
+  int whole;  // every vector of a wave's columns is aligned and inside its group
+};
+
+// Fills CT .. P, chunk and tiles for the forward or the backward pass.
+void scan_plan(ScanArgs& a, int cus, bool bwd);
+template <int DT>
+hipError_t scan_forward(const ScanArgs& a, hipStream_t stream);
+template <int DT>
+hipError_t scan_backward(const ScanArgs& a, hipStream_t stream);
+template <> hipError_t scan_forward<kF32>(const ScanArgs&, hipStream_t);
+template <> hipError_t scan_forward<kF16>(const ScanArgs&, hipStream_t);
+template <> hipError_t scan_forward<kBF16>(const ScanArgs&, hipStream_t);
+template <> hipError_t scan_backward<kF32>(const ScanArgs&, hipStream_t);
+template <> hipError_t scan_backward<kF16>(const ScanArgs&, hipStream_t);
+template <> hipError_t scan_backward<kBF16>(const ScanArgs&, hipStream_t);
+
+// ---- causal convolution ----
+constexpr int kConvMaxW = 8;
+
+struct ConvArgs {
+  const void *x, *w, *bias, *h0, *dy, *dhT;
+  void *y, *hT, *dx, *dw, *db, *dh0;
+  const int* lengths;
+  float* part;  // [B * strips, W + 1, CT]
+  int64_t xs[2];
+  int64_t B, L, strips, first;
+  int C, T, W, CT, rows, silu, vec;  // rows: tokens of a strip
+};
+
+constexpr int conv_vec(int dt, int W, bool bwd) { return dt == kF32 ? 4 : bwd && W > 4 ? 4 : 8; }
+void conv_plan(ConvArgs& a, int dt, int cus, bool bwd);
+template <int DT>
+hipError_t conv_forward(const ConvArgs& a, hipStream_t stream);
+template <int DT>
+hipError_t conv_backward(const ConvArgs& a, hipStream_t stream);
+template <> hipError_t conv_forward<kF32>(const ConvArgs&, hipStream_t);
+template <> hipError_t conv_forward<kF16>(const ConvArgs&, hipStream_t);
+template <> hipError_t conv_forward<kBF16>(const ConvArgs&, hipStream_t);
+template <> hipError_t conv_backward<kF32>(const ConvArgs&, hipStream_t);
+template <> hipError_t conv_backward<kF16>(const ConvArgs&, hipStream_t);
+template <> hipError_t conv_backward<kBF16>(const ConvArgs&, hipStream_t);
+
+// ---- residual norm ----
+constexpr int kResMaxRow = 8192;
+
+struct ResArgs {
+  const void *x, *u, *w, *b, *scale, *gate, *pw, *pb, *dr, *dh;
+  void *r, *h, *dx, *du, *dw, *db, *dscale, *dgate, *dpw, *dpb;
+  float* part;  // [seqs, strips, J, K]: column sums of each workgroup
+  float* sums;  // [seqs, J, C]
+  int64_t B, L;
+  int64_t seqs, rows;    // sequences with a gate of their own (else one), tokens of each
+  int64_t strips, strip; // workgroups of a sequence and tokens of each
+  int64_t first;
+  int C, T, K, rms, J;
+  float eps;
+  int whole, lanes, ept;  // threads of a row and elements of each
+};
+
+void res_plan(ResArgs& a, int dt, int cus, bool bwd);
+template <int DT>
+hipError_t res_forward(const ResArgs& a, hipStream_t stream);
+template <int DT>
+hipError_t res_backward(const ResArgs& a, hipStream_t stream);
+template <> hipError_t res_forward<kF32>(const ResArgs&, hipStream_t);
+template <> hipError_t res_forward<kF16>(const ResArgs&, hipStream_t);
+template <> hipError_t res_forward<kBF16>(const ResArgs&, hipStream_t);
+template <> hipError_t res_backward<kF32>(const ResArgs&, hipStream_t);
+template <> hipError_t res_backward<kF16>(const ResArgs&, hipStream_t);
+template <> hipError_t res_backward<kBF16>(const ResArgs&, hipStream_t);
+
+}  // namespace eqk

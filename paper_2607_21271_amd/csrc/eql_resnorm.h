@@ -1,0 +1,363 @@
+// eql_resnorm.h -- the residual sum between two norms, forward and gradients, for gfx950.
+//   v = norm(u) pw + pb (or u);  r = x + k v, k = scale[c] gate[b, c];  h = norm(r) w + b
+// over the K = C T elements of a token, per-channel parameters shared over T.  With rh, uh the normalised rows and
+// fr, fu their factors:
+//   dr' = dr + fr (q - mean(q) - rh mean(q rh)), q = dh w  (rms: without mean(q));  dx = dr'
+//   du = k dr', or through the norm before: fu (p - mean(p) - uh mean(p uh)), p = k dr' pw
+//   dw = sum dh rh, db = sum dh;  with E = sum dr' v, P = sum dr' uh, S = sum dr' over a sequence's tokens and T:
+//   E = pw P + pb S where there is a norm before, dgate = scale E, dscale = sum_b gate E, dpw = sum_b k P,
+//   dpb = sum_b k S.
+// LANES threads hold a row, EPT elements each, and walk the rows of their strip; means are two-pass, from
+// registers.  The backward forms r again from x and u: what it reads is the inputs and the two gradients, and
+// no rounding of r enters.  Column sums stay in registers over a strip, then one row of sums a workgroup goes to
+// memory, and two small kernels add them in a fixed order.
+// Bound: memory (forward 4, backward 6 rows an element).
+#pragma once
+#include "eql_common.h"
+#include "eql_config.h"
+#include "eql_recurrent.h"
+
+namespace eqk {
+
+template <int DT, int LANES, int EPT, bool WHOLE>
+struct ResRow {
+  using E = typename Elem<DT>::T;
+  static constexpr int EB = Elem<DT>::bytes, VEC = WHOLE ? 16 / EB : 1, NV = EPT / VEC;
+  static constexpr int W = WHOLE ? 4 : 1;
+  static constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at a time
+  static constexpr int THREADS = LANES < 256 ? 256 : LANES;
+  struct Raw {
+    uint32_t w[NV * W];
+  };
+  // first element of vector v
+  static __device__ __forceinline__ int at(int v) { return (v * LANES + (int)(threadIdx.x % LANES)) * VEC; }
+  static __device__ __forceinline__ void load(Raw& r, const void* base, int64_t row, int K, bool on) {
+    const E* p = reinterpret_cast<const E*>(base) + row * K;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const bool ok = on && at(v) < K;
+      if constexpr (WHOLE) {
+        const u32x4 q = ok ? *reinterpret_cast<const u32x4*>(p + at(v)) : u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[v * 4 + i] = q[i];
+      } else if constexpr (EB == 4) {
+        r.w[v] = ok ? __builtin_bit_cast(uint32_t, p[at(v)]) : 0u;
+      } else {
+        r.w[v] = ok ? __builtin_bit_cast(uint16_t, p[at(v)]) : 0u;
+      }
+    }
+  }
+  static __device__ __forceinline__ void floats(const Raw& r, float (&f)[EPT]) {
+    if constexpr (WHOLE) {
+      raw_to_floats<DT, NV * 4>(r.w, f);
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if constexpr (EB == 4) f[v] = __builtin_bit_cast(float, r.w[v]);
+        else f[v] = (float)__builtin_bit_cast(E, (uint16_t)r.w[v]);
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(const float (&f)[EPT], void* base, int64_t row, int K) {
+    E* p = reinterpret_cast<E*>(base) + row * K;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (at(v) >= K) continue;
+      if constexpr (WHOLE) {
+        u32x4 q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = pack2<DT>(f[v * VEC + i * (4 / EB)], f[v * VEC + i * (4 / EB) + (EB == 2)]);
+        *reinterpret_cast<u32x4*>(p + at(v)) = q;
+      } else {
+        p[at(v)] = (E)f[v];
+      }
+    }
+  }
+  // a parameter of the thread's columns, `none` outside and where p is NULL
+  static __device__ __forceinline__ void param(const void* p, int T, int K, float none, float (&f)[EPT]) {
+    const E* q = reinterpret_cast<const E*>(p);
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      const int c = at(e / VEC) + e % VEC;
+      f[e] = p && c < K ? (float)q[c / T] : none;
+    }
+  }
+  // the sum over a row's threads
+  static __device__ __forceinline__ float total(float s, float* red, int& slot) {
+#pragma unroll
+    for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) s += __shfl_xor(s, d);
+    if constexpr (LANES > 64) {
+      constexpr int NW = LANES / 64;
+      float* const q = red + slot * NW;  // alternating, so that one barrier a sum is enough
+      slot ^= 1;
+      if ((threadIdx.x & 63) == 0) q[threadIdx.x >> 6] = s;
+      __syncthreads();
+      s = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NW; w += 2) s += q[w] + q[w + 1];
+    }
+    return s;
+  }
+  // f normalised in place (0 outside the row); returns the factor
+  static __device__ __forceinline__ float normed(float (&f)[EPT], const ResArgs& a, float* red, int& slot) {
+    float s = 0.0f;
+    if (!a.rms) {
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) s += f[e];
+      const float mean = total(s, red, slot) / (float)a.K;
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) f[e] = at(e / VEC) + e % VEC < a.K ? f[e] - mean : 0.0f;
+      s = 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) s = __builtin_fmaf(f[e], f[e], s);
+    const float k = 1.0f / sqrtf(total(s, red, slot) / (float)a.K + a.eps);
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) f[e] *= k;
+    return k;
+  }
+  // the gradient g of a normalised row through the norm, in place (0 outside the row)
+  static __device__ __forceinline__ void back(float (&g)[EPT], const float (&f)[EPT], float k, const ResArgs& a, float* red,
+                                              int& slot) {
+    float s = 0.0f, m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) {
+      s = __builtin_fmaf(g[e], f[e], s);
+      m += g[e];
+    }
+    s = total(s, red, slot) / (float)a.K;
+    m = a.rms ? 0.0f : total(m, red, slot) / (float)a.K;
+#pragma unroll
+    for (int e = 0; e < EPT; ++e)
+      g[e] = at(e / VEC) + e % VEC < a.K ? k * (g[e] - __builtin_fmaf(f[e], s, m)) : 0.0f;
+  }
+};
+
+// Strip of a workgroup: rows first + its own .. last of sequence q.
+struct ResPlace {
+  int64_t q, strip, first, last;
+};
+__device__ __forceinline__ ResPlace res_place(const ResArgs& a) {
+  ResPlace p;
+  const int64_t id = a.first + blockIdx.x;
+  p.q = id / a.strips;
+  p.strip = id % a.strips;
+  p.first = p.strip * a.strip;
+  p.last = min(p.first + a.strip, a.rows);
+  return p;
+}
+
+template <int DT, int LANES, int EPT, bool WHOLE>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_res_fwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, WHOLE>;
+  __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
+  const ResPlace p = res_place(a);
+  int slot = 0;
+  float k[EPT], w[EPT], b[EPT], pw[EPT], pb[EPT];
+  R::param(a.scale, a.T, a.K, 1.0f, k);
+  if (a.gate) {
+    float g[EPT];
+    R::param(reinterpret_cast<const typename R::E*>(a.gate) + p.q * a.C, a.T, a.K, 1.0f, g);
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) k[e] *= g[e];
+  }
+  R::param(a.w, a.T, a.K, 0.0f, w);
+  R::param(a.b, a.T, a.K, 0.0f, b);
+  R::param(a.pw, a.T, a.K, 0.0f, pw);
+  R::param(a.pb, a.T, a.K, 0.0f, pb);
+  const int mine = LANES < 256 ? threadIdx.x / LANES : 0;
+  typename R::Raw xr, ur;
+  auto fetch = [&](int64_t row) {
+    R::load(xr, a.x, p.q * a.rows + row, a.K, row < p.last);
+    if (a.u) R::load(ur, a.u, p.q * a.rows + row, a.K, row < p.last);
+  };
+  fetch(p.first + mine);
+  // (LANES > 64: one row a workgroup, so every thread takes every turn)
+  for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
+    const int64_t row = p.q * a.rows + i;
+    float x[EPT], u[EPT];
+    R::floats(xr, x);
+    if (a.u) R::floats(ur, u);
+    if (i + R::ROWS < p.last) fetch(i + R::ROWS);
+    if (a.u) {
+      if (a.pw) {
+        R::normed(u, a, red, slot);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) u[e] = __builtin_fmaf(u[e], pw[e], pb[e]);
+      }
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e], u[e], x[e]);
+      R::store(x, a.r, row, a.K);
+    }
+    if (a.w) {
+      R::normed(x, a, red, slot);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(x[e], w[e], b[e]);
+      R::store(x, a.h, row, a.K);
+    }
+  }
+}
+
+// Rows of column sums: dw, db (where there is a norm after), then E, or P and S.
+template <int DT, int LANES, int EPT, bool WHOLE>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_res_bwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, WHOLE>;
+  __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
+  __shared__ float cols[R::ROWS > 1 ? R::ROWS * LANES * EPT : 1];
+  const ResPlace p = res_place(a);
+  int slot = 0;
+  float k[EPT], w[EPT], pw[EPT], pb[EPT];
+  R::param(a.scale, a.T, a.K, 1.0f, k);
+  if (a.gate) {
+    float g[EPT];
+    R::param(reinterpret_cast<const typename R::E*>(a.gate) + p.q * a.C, a.T, a.K, 1.0f, g);
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) k[e] *= g[e];
+  }
+  R::param(a.w, a.T, a.K, 0.0f, w);
+  R::param(a.pw, a.T, a.K, 0.0f, pw);
+  R::param(a.pb, a.T, a.K, 0.0f, pb);
+  float s0[EPT], s1[EPT], s2[EPT], s3[EPT];
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) s0[e] = s1[e] = s2[e] = s3[e] = 0.0f;
+  const int mine = LANES < 256 ? threadIdx.x / LANES : 0;
+  for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
+    const int64_t row = p.q * a.rows + i;
+    typename R::Raw xr, ur, rr, hr;
+    R::load(xr, a.x, row, a.K, true);
+    if (a.u) R::load(ur, a.u, row, a.K, true);
+    if (a.dr) R::load(rr, a.dr, row, a.K, true);
+    if (a.dh) R::load(hr, a.dh, row, a.K, true);
+    float x[EPT], u[EPT], g[EPT], fu = 1.0f;
+    R::floats(xr, x);
+    if (a.u) {
+      R::floats(ur, u);
+      if (a.pw) fu = R::normed(u, a, red, slot);  // u: uh
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e], a.pw ? __builtin_fmaf(u[e], pw[e], pb[e]) : u[e], x[e]);
+    }
+    if (a.dh) {
+      const float fr = R::normed(x, a, red, slot);  // x: rh
+      R::floats(hr, g);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        s0[e] = __builtin_fmaf(g[e], x[e], s0[e]);
+        s1[e] += g[e];
+        g[e] *= w[e];
+      }
+      R::back(g, x, fr, a, red, slot);
+    } else {
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) g[e] = 0.0f;
+    }
+    if (a.dr) {
+      float d[EPT];
+      R::floats(rr, d);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) g[e] += d[e];
+    }
+    if (a.dx) R::store(g, a.dx, row, a.K);
+    if (a.u) {
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        s2[e] = __builtin_fmaf(g[e], u[e], s2[e]);
+        s3[e] += g[e];
+        g[e] *= a.pw ? k[e] * pw[e] : k[e];
+      }
+      if (a.du) {
+        if (a.pw) R::back(g, u, fu, a, red, slot);
+        R::store(g, a.du, row, a.K);
+      }
+    }
+  }
+  float* const part = a.part + (p.q * a.strips + p.strip) * a.J * a.K;
+  int j = 0;
+  auto put = [&](const float (&s)[EPT]) {
+    if constexpr (R::ROWS > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        const int c = R::at(e / R::VEC) + e % R::VEC;
+        if (c < a.K) cols[mine * (LANES * EPT) + c] = s[e];
+      }
+      __syncthreads();
+      for (int c = threadIdx.x; c < a.K; c += R::THREADS) {
+        float v = cols[c];
+#pragma unroll
+        for (int m = 1; m < R::ROWS; ++m) v += cols[m * (LANES * EPT) + c];
+        part[(int64_t)j * a.K + c] = v;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) {
+        const int c = R::at(e / R::VEC) + e % R::VEC;
+        if (c < a.K) part[(int64_t)j * a.K + c] = s[e];
+      }
+    }
+    ++j;
+  };
+  if (a.w) {
+    put(s0);
+    put(s1);
+  }
+  if (a.u) {
+    put(s2);
+    if (a.pw) put(s3);
+  }
+}
+
+// sums[q, j, c]: the strips and group elements of a sequence's column sums, and the sequence's gate.  A
+// workgroup takes one channel of one row j.
+template <int UNUSED = 0>
+__global__ __launch_bounds__(256) void eql_res_strips_kernel(const ResArgs a) {
+  int64_t id = a.first + blockIdx.x;
+  const int c = (int)(id % a.C);
+  id /= a.C;
+  const int j = (int)(id % a.J);
+  const int64_t q = id / a.J, n = a.strips * a.T;
+  float v = 0.0f;
+  for (int64_t i = threadIdx.x; i < n; i += 256) v += a.part[((q * a.strips + i / a.T) * a.J + j) * a.K + c * a.T + i % a.T];
+  __shared__ float red[4];
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) a.sums[(q * a.J + j) * a.C + c] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+// The parameters' gradients: a wave adds the sequences of a channel.
+template <int DT>
+__global__ __launch_bounds__(256) void eql_res_params_kernel(const ResArgs a) {
+  using E = typename Elem<DT>::T;
+  const int c = (int)(a.first + blockIdx.x) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (c >= a.C) return;
+  auto at = [&](const void* p, int64_t i) { return (float)reinterpret_cast<const E*>(p)[i]; };
+  const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
+  float dw = 0.0f, db = 0.0f, ds = 0.0f, dpw = 0.0f, dpb = 0.0f;
+  for (int64_t q = lane; q < a.seqs; q += 64) {
+    const float* s = a.sums + q * a.J * a.C + c;
+    if (a.w) {
+      dw += s[0];
+      db += s[a.C];
+      s += 2 * a.C;
+    }
+    if (!a.u) continue;
+    const float gate = a.gate ? at(a.gate, q * a.C + c) : 1.0f, P = s[0], S = a.pw ? s[a.C] : 0.0f;
+    const float e = a.pw ? __builtin_fmaf(pw, P, pb * S) : P;
+    if (a.dgate) reinterpret_cast<E*>(a.dgate)[q * a.C + c] = (E)(scale * e);
+    ds = __builtin_fmaf(gate, e, ds);
+    dpw = __builtin_fmaf(gate * scale, P, dpw);
+    dpb = __builtin_fmaf(gate * scale, S, dpb);
+  }
+  auto out = [&](void* p, float v) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    if (p && lane == 0) reinterpret_cast<E*>(p)[c] = (E)v;
+  };
+  out(a.dw, dw);
+  out(a.db, db);
+  out(a.dscale, ds);
+  out(a.dpw, dpw);
+  out(a.dpb, dpb);
+}
+
+}  // namespace eqk

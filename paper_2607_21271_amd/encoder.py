@@ -3,23 +3,28 @@
     stem     rotation-equivariant 3 x 3 convolutions (``gconv``) with group norm and activation between (``norm``)
     tokens   the features of p x p pixels averaged, a frame in raster order, frames after one another, after a few
              register tokens
-    blocks   ``EQViTBlock`` with rotary positions (time, height, width) and windowed attention (``attention``)
+    blocks   ``EQViTBlock`` with rotary positions (time, height, width) and windowed attention (``attention``), or
+             recurrent ones: a short causal convolution and a selective scan (``scan``) between fused norms
 
 Every part commutes with the group action on the T axis.  Without a limit to the right every token sees as far ahead as
 back; with ``right = 0`` a video can also be encoded frame by frame over caches (``EQEncoder.stream``), whose tokens are
-those of the whole clip.
+those of the whole clip; recurrent blocks see earlier tokens only and stream with a state of fixed size.
 
-``python -m paper_2607_21271_amd.encoder`` trains a small encoder on synthetic clips for a few steps and streams one.
+``python -m paper_2607_21271_amd.encoder [attention|scan]`` trains a small encoder on synthetic clips for a few steps and
+streams one.
 """
 from __future__ import annotations
+
+import sys
 
 import torch
 import torch.nn.functional as F
 
-from . import attention, rotary
-from .blocks import EQViTBlock
+from . import attention, rotary, scan
+from .blocks import EQViTBlock, GroupLayerNorm
 from .gconv import GroupConv2d
-from .norm import GroupNormAct
+from .norm import GroupNormAct, residual_norm
+from .ops import EQLinear
 
 
 class EQWindowBlock(EQViTBlock):
@@ -70,22 +75,104 @@ class EQWindowBlock(EQViTBlock):
         return x + self.fc2(F.gelu(self.fc1(self.norm2(x))))
 
 
+class EQScanBlock(torch.nn.Module):
+    """A recurrent block on tokens x [B, L, C, T], each of which sees itself and the tokens before:
+
+        x = x + scale1 * gate * mix(norm1(x)),  x = x + scale2 * gate * fc2(gelu(fc1(norm2(x))))
+
+    ``mix`` projects to 2 x ``expand`` x C channels, half of them the gate, runs a causal convolution of ``width`` tokens and a
+    selective scan of ``states`` states a channel, and projects back.  The steps come from an equivariant layer of rank
+    ``rank``, Bt and Ct from the mean over the group, so the block commutes with the group action.  ``layer_scale``: first value
+    of scale1 and scale2 (None: without); ``post_norm``: both branches are normalised before they are added."""
+
+    def __init__(self, T: int, C: int, expand: int = 2, states: int = 16, width: int = 4, groups: int = 1,
+                 rank: int | None = None, mlp_ratio: int = 4, kind: str = "layer", layer_scale: float | None = None,
+                 post_norm: bool = False, device=None, dtype=None):
+        super().__init__()
+        kw = {"device": device, "dtype": dtype}
+        wide = {"device": device, "dtype": torch.float32}
+        E = expand * C
+        rank = max(1, -(-C // 16)) if rank is None else rank
+        self.T, self.C, self.E, self.states, self.width, self.groups, self.kind = T, C, E, states, width, groups, kind
+        self.norm1, self.norm2 = GroupLayerNorm(C, **kw), GroupLayerNorm(C, **kw)
+        self.post1, self.post2 = (GroupLayerNorm(C, **kw) if post_norm else None for _ in range(2))
+        for name in ("scale1", "scale2"):
+            self.register_parameter(name, None if layer_scale is None else
+                                    torch.nn.Parameter(torch.full((C,), float(layer_scale), **kw)))
+        self.in_proj = EQLinear(T, C, 2 * E, **kw)
+        self.conv_weight = torch.nn.Parameter(torch.rand(E, width, **kw).mul_(2).sub_(1).mul_(width ** -0.5))
+        self.conv_bias = torch.nn.Parameter(torch.zeros(E, **kw))
+        self.bc = torch.nn.Linear(E, 2 * groups * states, bias=False, **kw)
+        self.delta_down, self.delta_up = EQLinear(T, E, rank, bias=False, **kw), EQLinear(T, rank, E, bias=False, **kw)
+        # decays of 1, 2, .. states a unit of step, steps between 0.001 and 0.1 at first; held in float32 whatever the
+        # block's type: what a state keeps over thousands of tokens goes by their last digits
+        self.A_log = torch.nn.Parameter(torch.arange(1, states + 1, **wide).log().repeat(E, 1))
+        self.D = torch.nn.Parameter(torch.ones(E, **wide))
+        step = torch.exp(torch.rand(E, **wide) * 4.605 - 6.908)
+        self.delta_bias = torch.nn.Parameter(torch.log(torch.expm1(step)))
+        self.out_proj = EQLinear(T, E, C, **kw)
+        self.fc1, self.fc2 = EQLinear(T, C, mlp_ratio * C, **kw), EQLinear(T, mlp_ratio * C, C, **kw)
+
+    def _apply(self, fn, recurse=True):
+        wide = [t for p in (self.A_log, self.D, self.delta_bias) for t in (p, p.grad) if t is not None]
+
+        def keep(t):
+            out = fn(t)
+            return t.to(out.device) if out.dtype != t.dtype and any(t is w for w in wide) else out
+
+        return super()._apply(keep, recurse)
+
+    def new_cache(self, B: int):
+        """What ``extend`` carries from call to call: the last tokens of the convolution and the states, zeros at first."""
+        w = self.conv_weight
+        return (w.new_zeros((B, self.width - 1, self.E, self.T)),
+                self.A_log.new_zeros((B, self.E, self.T, self.states)))
+
+    def mix(self, h, lengths=None, cache=None):
+        B, L = h.shape[:2]
+        x, z = self.in_proj(h).chunk(2, 2)
+        last, state = cache or (None, None)
+        x = scan.causal_conv(x, self.conv_weight, self.conv_bias, "silu", lengths, last, state_out=last)
+        x = x if cache is None else x[0]
+        bc = self.bc(x.mean(3)).view(B, L, 2 * self.groups, self.states)
+        y = scan.selective_scan(x, self.delta_up(self.delta_down(x)), -torch.exp(self.A_log), bc[:, :, :self.groups],
+                                bc[:, :, self.groups:], self.D, z, self.delta_bias, lengths=lengths, state=state,
+                                state_out=state)
+        return self.out_proj(y if cache is None else y[0])
+
+    def forward(self, x, lengths=None, gate=None, cache=None):
+        """``gate`` [B, C]: of both branches, 0 where a sequence drops them."""
+        post = lambda n: {} if n is None else {"post_weight": n.weight, "post_bias": n.bias}
+        kw = {"kind": self.kind, "eps": self.norm1.eps}
+        _, h = residual_norm(x, weight=self.norm1.weight, bias=self.norm1.bias, **kw)
+        x, h = residual_norm(x, self.mix(h, lengths, cache), self.norm2.weight, self.norm2.bias, scale=self.scale1, gate=gate,
+                             **post(self.post1), **kw)
+        return residual_norm(x, self.fc2(F.gelu(self.fc1(h))), scale=self.scale2, gate=gate, **post(self.post2), **kw)[0]
+
+    @torch.no_grad()
+    def extend(self, x, cache):
+        """``forward`` of the next tokens x [B, n, C, T], which carries on from the cache (``new_cache``) and updates it."""
+        return self.forward(x, cache=cache)
+
+
 class EQEncoder(torch.nn.Module):
     """Clips [B, frames, H, W, Cin, T] -> tokens [B, registers + frames * H/p * W/p, C, T]."""
 
     def __init__(self, T: int, Cin: int, C: int, heads: int, depth: int, sections, patch: int = 4, registers: int = 4,
                  left: int = -1, right: int = -1, stem: int = 2, groups: int = 4, activation: str = "silu", device=None,
-                 dtype=None):
+                 dtype=None, mixer: str = "attention"):
         super().__init__()
+        if mixer not in ("attention", "scan"):
+            raise ValueError("mixer must be attention or scan, got %r" % (mixer,))
         kw = {"device": device, "dtype": dtype}
-        self.T, self.C, self.patch = T, C, patch
+        self.T, self.C, self.patch, self.mixer = T, C, patch, mixer
         self.stem = torch.nn.ModuleList(torch.nn.ModuleList((GroupConv2d(T, Cin if i == 0 else C, C, **kw),
                                                              GroupNormAct(C, groups, activation, **kw)))
                                         for i in range(stem))
         # one value per channel, the same for every group element
         self.registers = torch.nn.Parameter(torch.randn(registers, C, 1, **kw) * 0.02)
         self.blocks = torch.nn.ModuleList(EQWindowBlock(T, C, heads, sections, left, right, registers, **kw)
-                                          for _ in range(depth))
+                                          if mixer == "attention" else EQScanBlock(T, C, **kw) for _ in range(depth))
 
     def positions(self, frames, H, W, device, first: int = 0):
         """Of the tokens of frames first .. first + frames - 1, after the registers where first is 0."""
@@ -112,6 +199,10 @@ class EQEncoder(torch.nn.Module):
 
     def forward(self, clip):
         x = self._with_registers(self.tokens(clip))
+        if self.mixer == "scan":
+            for block in self.blocks:
+                x = block(x)
+            return x
         pos = self.positions(*clip.shape[1:4], clip.device)
         for block in self.blocks:
             x = block(x, pos)
@@ -119,7 +210,19 @@ class EQEncoder(torch.nn.Module):
 
     @torch.no_grad()
     def stream(self, clip):
-        """The same tokens, frame by frame: every frame's tokens attend over the caches of the frames before."""
+        """The same tokens, frame by frame: every frame's tokens attend over the caches of the frames before, or carry on
+        from the states behind them."""
+        if self.mixer == "scan":
+            caches = [b.new_cache(clip.shape[0]) for b in self.blocks]
+            out = []
+            for t in range(clip.shape[1]):
+                x = self.tokens(clip[:, t:t + 1])
+                if t == 0:
+                    x = self._with_registers(x)
+                for block, cache in zip(self.blocks, caches):
+                    x = block.extend(x, cache)
+                out.append(x)
+            return torch.cat(out, 1)
         if any(b.right != 0 for b in self.blocks):
             raise ValueError("streaming needs right = 0: a token may not see later ones")
         B, N, H, W = clip.shape[:4]
@@ -143,11 +246,11 @@ class EQEncoder(torch.nn.Module):
         return torch.cat(out, 1)
 
 
-def main(steps: int = 20, device: str = "cuda") -> None:
+def main(steps: int = 20, device: str = "cuda", mixer: str = "attention") -> None:
     """Trains a small encoder to tell the direction in which a pattern drifts, then streams a clip."""
     torch.manual_seed(0)
     T, frames, size = 4, 4, 32
-    enc = EQEncoder(T, 4, 32, heads=4, depth=2, sections=(2, 1, 1), left=200, right=0, device=device)
+    enc = EQEncoder(T, 4, 32, heads=4, depth=2, sections=(2, 1, 1), left=200, right=0, device=device, mixer=mixer)
     head = torch.nn.Linear(32, 2, device=device)
     opt = torch.optim.AdamW([*enc.parameters(), *head.parameters()], lr=3e-4)
 
@@ -172,4 +275,4 @@ def main(steps: int = 20, device: str = "cuda") -> None:
 
 
 if __name__ == "__main__":
-    main()
+    main(mixer=sys.argv[1] if len(sys.argv) > 1 else "attention")

@@ -1,4 +1,5 @@
-"""Group norm with an activation over channels-last equivariant features [B, ..., C, T].
+"""Norms of channels-last equivariant features [B, ..., C, T]: group norm with an activation, and the residual sum between
+two norms (``residual_norm``, below).
 
     z = (x - mean) / sqrt(var + eps) * weight[c] + bias[c],   y = act(z)
 
@@ -8,6 +9,7 @@ of ``gconv``.  This module allocates and marshals; ``eqlinear_group_norm_act`` a
 """
 from __future__ import annotations
 
+import ctypes
 import functools
 import math
 
@@ -111,3 +113,107 @@ class GroupNormAct(torch.nn.Module):
 
     def forward(self, x):
         return group_norm_act(x, self.weight, self.bias, self.groups, self.activation, self.eps)
+
+
+# ---- the residual sum between two norms -------------------------------------------------------------------------------
+
+KINDS = {"layer": _lib.EQL_NORM_LAYER, "rms": _lib.EQL_NORM_RMS}
+
+
+@functools.lru_cache(maxsize=1024)
+def _residual_plan(shape, kind, eps, dtype):
+    """The C shape of a call (a pointer that keeps it) and the bytes of its backward workspace."""
+    ref = ctypes.pointer(_lib.ResidualShape(shape[0], math.prod(shape[1:-2]), shape[-2], shape[-1], kind, ops._DT[dtype], eps, 0))
+    return ref, _lib.eqlinear_residual_norm_backward_workspace_bytes(ref)
+
+
+def _residual_forward(x, branch, weight, bias, scale, gate, post_weight, post_bias, kind, eps):
+    ref, _ = _residual_plan(x.shape, kind, eps, x.dtype)
+    r = None if branch is None else torch.empty_like(x)
+    h = None if weight is None else torch.empty_like(x)
+    p = ops._ptr
+    ops._launch("eqlinear_residual_norm", x, ref, p(x), p(branch), p(weight), p(bias), p(scale), p(gate), p(post_weight),
+                p(post_bias), p(r), p(h))
+    return r, h
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    """Autograd: gradients of x, the branch and every parameter; r is formed again from x and the branch."""
+
+    @staticmethod
+    def forward(ctx, x, branch, weight, bias, scale, gate, post_weight, post_bias, kind, eps):
+        ctx.set_materialize_grads(False)
+        given = tuple(None if t is None else t.contiguous()
+                      for t in (x, branch, weight, bias, scale, gate, post_weight, post_bias))
+        ctx.save_for_backward(*given)
+        ctx.args = (kind, eps)
+        r, h = _residual_forward(*given, kind, eps)
+        return h if r is None else r if h is None else (r, h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *grads):
+        given = ctx.saved_tensors
+        x, branch, weight, bias, scale, gate, post_weight, post_bias = given
+        ref, need = _residual_plan(x.shape, *ctx.args, x.dtype)
+        if all(g is None for g in grads):
+            return (None,) * 10
+        gr, gh = grads if len(grads) == 2 else (None, grads[0]) if branch is None else (grads[0], None)
+        gr, gh = (None if g is None else g.contiguous() for g in (gr, gh))
+        new = torch.empty_like if x.numel() else torch.zeros_like
+        dx, du, dw, db, ds, dg, dpw, dpb = (new(t) if t is not None and need else None
+                                            for t, need in zip(given, ctx.needs_input_grad))
+        if x.numel():
+            ws = x.new_empty((need,), dtype=torch.uint8)
+            p = ops._ptr
+            ops._launch("eqlinear_residual_norm_backward", x, ref, p(x), p(branch), p(weight), p(scale), p(gate),
+                        p(post_weight), p(post_bias), p(gr), p(gh), p(dx), p(du), p(dw), p(db), p(ds), p(dg), p(dpw), p(dpb),
+                        p(ws), need)
+        return dx, du, dw, db, ds, dg, dpw, dpb, None, None
+
+
+@functools.lru_cache(maxsize=1024)
+def _check_residual_shapes(x, branch, weight, bias, scale, gate, post_weight, post_bias, kind):
+    if len(x) < 3 or x[-1] < 1 or x[-2] < 1:
+        raise ValueError("x must be [B, ..., C, T], got %s" % (tuple(x),))
+    if kind not in KINDS:
+        raise ValueError("kind must be one of %s, got %r" % (", ".join(KINDS), kind))
+    if branch is None and not (scale is gate is post_weight is None and weight is not None):
+        raise ValueError("without a branch there is the norm of x alone: weight, and no scale, gate or post_weight")
+    if branch is not None and branch != x:
+        raise ValueError("branch must be %s, got %s" % (tuple(x), tuple(branch)))
+    if (bias is not None and weight is None) or (post_bias is not None and post_weight is None):
+        raise ValueError("a bias needs the weight of its norm")
+    for name, s, want in (("weight", weight, x[-2:-1]), ("bias", bias, x[-2:-1]), ("scale", scale, x[-2:-1]),
+                          ("gate", gate, (x[0], x[-2])), ("post_weight", post_weight, x[-2:-1]),
+                          ("post_bias", post_bias, x[-2:-1])):
+        if s is not None and tuple(s) != tuple(want):
+            raise ValueError("%s must be %s, got %s" % (name, list(want), tuple(s)))
+
+
+def residual_norm(x: torch.Tensor, branch: torch.Tensor | None = None, weight: torch.Tensor | None = None,
+                  bias: torch.Tensor | None = None, scale: torch.Tensor | None = None, gate: torch.Tensor | None = None,
+                  post_weight: torch.Tensor | None = None, post_bias: torch.Tensor | None = None, kind: str = "layer",
+                  eps: float = 1e-6):
+    """The end of one branch of a block and the norm before the next, on x and branch [B, ..., C, T]:
+
+        v = norm(branch) * post_weight[c] + post_bias[c]   (branch itself without post_weight)
+        r = x + scale[c] * gate[b, c] * v
+        h = norm(r) * weight[c] + bias[c]
+
+    Gives (r, h); h is None without ``weight``; without ``branch`` r is x and h its norm.  Norms go over the (C, T) of each token:
+    ``kind`` layer (mean and variance) or rms.  Parameters are per channel, shared over T, of x's type; ``gate`` [B, C] is per
+    sequence (a conditioned gate, or 0 and 1 / (1 - p) of a branch dropped at random).  Either result may be the one that has
+    a gradient."""
+    ops._dtype_code(x)
+    ops._check_same_dtype(x, branch=branch, weight=weight, bias=bias, scale=scale, gate=gate, post_weight=post_weight,
+                          post_bias=post_bias)
+    given = (x, branch, weight, bias, scale, gate, post_weight, post_bias)
+    _check_residual_shapes(*(None if t is None else t.shape for t in given), kind)
+    ops._check_dev(*given)
+    if ops._no_node(*(t for t in given if t is not None)):
+        r, h = _residual_forward(*(None if t is None else t.contiguous() for t in given), KINDS[kind], float(eps))
+    else:
+        out = ResidualNormFunction.apply(*given, KINDS[kind], float(eps))
+        r, h = (None, out) if branch is None else (out, None) if weight is None else out
+    return x if branch is None else r, h

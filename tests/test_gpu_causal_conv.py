@@ -1,0 +1,144 @@
+"""The short causal convolution on the GPU against its 64-bit definition (tests/recurrent_ref.py)."""
+import pytest
+import torch
+
+import recurrent_ref as R
+from encoder_ref import DT
+
+pytestmark = pytest.mark.gpu
+
+NAMES, GRADS = ("x", "weight", "bias", "state"), ("dx", "dw", "db", "dstate")
+
+
+def make(seed, B, L, C, T, W, dt, bias=True, state=True):
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *s: torch.randn(*s, generator=g).to(DT[dt]).cuda()
+    return dict(x=n(B, L, C, T), weight=n(C, W), bias=n(C) if bias else None, state=n(B, W - 1, C, T) if state else None)
+
+
+def run(t, dy=None, dstate=None, **kw):
+    from paper_2607_21271_amd.scan import causal_conv
+    if dy is None and dstate is None:
+        with torch.no_grad():
+            return dict(zip(("y", "state"), causal_conv(**t, return_state=True, **kw)))
+    t = {k: None if v is None else v.detach().requires_grad_() for k, v in t.items()}
+    y, h = causal_conv(**t, return_state=True, **kw)
+    outs, given = zip(*((o, g) for o, g in ((y, dy), (h, dstate)) if g is not None))
+    want = [k for k in NAMES if t[k] is not None]
+    return {"y": y, "state": h,
+            **{GRADS[NAMES.index(k)]: g for k, g in zip(want, torch.autograd.grad(outs, [t[k] for k in want], given))}}
+
+
+def check(t, dy=None, dstate=None, **kw):
+    got, want = run(t, dy, dstate, **kw), R.conv(**t, dy=dy, dstate=dstate, **kw)
+    for n, v in got.items():
+        R.within(n, v, *want[n])
+    return got
+
+
+def grads(seed, t):
+    g = torch.Generator().manual_seed(seed)
+    B, _, C, T = t["x"].shape
+    return (torch.randn(t["x"].shape, generator=g).to(t["x"].dtype).cuda(),
+            torch.randn(B, t["weight"].shape[1] - 1, C, T, generator=g).to(t["x"].dtype).cuda())
+
+
+@pytest.mark.parametrize("W", range(1, 9))
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_widths(W, dt):
+    for B, L, C, T in ((2, 1, 8, 4), (1, 3, 5, 3), (2, 70, 24, 8), (3, 130, 7, 1)):
+        t = make(W + L, B, L, C, T, W, dt)
+        for act in ("none", "silu"):
+            check(t, activation=act)
+            check(t, *grads(W, t), activation=act)
+
+
+@pytest.mark.parametrize("bias,state", [(0, 0), (0, 1), (1, 0)])
+def test_what_may_be_left_out(bias, state):
+    t = make(3, 2, 40, 8, 4, 4, "f16", bias, state)
+    dy, ds = grads(1, t)
+    for given in ((None, None), (dy, ds), (dy, None), (None, ds)):
+        if given == (None, ds) and not bias:
+            continue
+        check(t, *given, activation="silu")
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16"])
+@pytest.mark.parametrize("L", [1, 2, 40, 300])
+def test_lengths(dt, L):
+    """No token, one, all but one, all; NaN behind them."""
+    lengths = torch.tensor([0, 1, L - 1, L, -2, L + 3], dtype=torch.int32)
+    t = make(5, 6, L, 6, 2, 4, dt)
+    dy, ds = grads(2, t)
+    for b, n in enumerate(lengths.clamp(0, L).tolist()):
+        t["x"][b, n:] = float("nan")
+        dy[b, n:] = float("nan")
+    for act in ("none", "silu"):
+        got = check(t, dy, ds, activation=act, lengths=lengths.cuda())
+        for b, n in enumerate(lengths.clamp(0, L).tolist()):
+            assert (got["y"][b, n:] == 0).all() and (got["dx"][b, n:] == 0).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("cut", ["packed", "offset", "odd", "broadcast", "turned"])
+def test_layouts(dt, cut):
+    B, L, C, T = 2, 50, 12, 4
+    t = make(7, B, L, C, T, 4, dt)
+    v = t["x"]
+    if cut == "packed":
+        t["x"] = torch.cat((v + 1, v), 2)[:, :, C:]
+    elif cut == "offset":
+        flat = torch.empty(v.numel() + 1, dtype=v.dtype, device="cuda")
+        flat[1:] = v.reshape(-1)
+        t["x"] = flat[1:].view(v.shape)
+    elif cut == "odd":
+        wide = torch.zeros(B, L, C * T + 3, dtype=v.dtype, device="cuda")
+        wide[:, :, 2:-1] = v.flatten(2)
+        t["x"] = wide[:, :, 2:-1].unflatten(2, (C, T))
+    elif cut == "broadcast":
+        t["x"] = v[:1].expand(B, L, C, T)
+    else:
+        t["x"] = v.transpose(0, 1).contiguous().transpose(0, 1)
+    check(t, *grads(3, t), activation="silu")
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16"])
+@pytest.mark.parametrize("W", [2, 4, 8])
+def test_carrying_on(dt, W):
+    """Pieces of 1, 2, 17 and 60 tokens with the state updated in place, against the whole sequence."""
+    from paper_2607_21271_amd.scan import causal_conv
+    t = make(9, 2, 80, 6, 4, W, dt)
+    want = R.conv(**t, activation="silu")
+    state, at, ys = t["state"].clone(), 0, []
+    for n in (1, 2, 17, 60):
+        y, out = causal_conv(t["x"][:, at:at + n], t["weight"], t["bias"], "silu", state=state, state_out=state)
+        assert out is state
+        ys.append(y)
+        at += n
+    R.within("y", torch.cat(ys, 1), *want["y"])
+    assert torch.equal(state.double().cpu(), want["state"][0])
+
+
+def test_empty():
+    t = make(1, 2, 0, 4, 2, 4, "f32")
+    got = run(t, torch.zeros_like(t["x"]), torch.ones(2, 3, 4, 2, device="cuda"))
+    assert torch.equal(got["state"], t["state"]) and (got["dstate"] == 1).all() and (got["dw"] == 0).all() and (got["db"] == 0).all()
+    t = make(1, 0, 5, 4, 2, 4, "f32")
+    got = run(t, torch.zeros_like(t["x"]), torch.ones(0, 3, 4, 2, device="cuda"))
+    assert (got["dw"] == 0).all() and (got["db"] == 0).all()
+
+
+def test_same_bits_every_time():
+    t = make(11, 2, 900, 24, 4, 4, "f16")
+    g = grads(4, t)
+    first = run(t, *g, activation="silu")
+    for _ in range(3):
+        for k, v in run(t, *g, activation="silu").items():
+            assert torch.equal(v, first[k]), k
+
+
+def test_large_values():
+    """silu and its gradient where the exponential overflows or vanishes."""
+    t = make(13, 1, 40, 8, 2, 2, "f32")
+    t["x"] = t["x"] * 60
+    check(t, *grads(5, t), activation="silu")
