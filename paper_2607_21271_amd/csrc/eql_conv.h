@@ -1,44 +1,56 @@
 // eql_conv.h -- short causal convolution along the tokens, forward and gradients, for gfx950.
 //   u_l = bias[c] + sum_w weight[c, w] x_{l - W + 1 + w},  y = act(u)
 //   du = dy act'(u);  dx_l = sum_w weight[c, w] du_{l + W - 1 - w};  dweight[c, w] = sum du_l x_{l - W + 1 + w}
-// A thread takes VEC neighbouring columns (channel, group element) of a strip of tokens and keeps the window
-// of W tokens in registers; what a strip needs of its neighbours is read again (W - 1 tokens, from the caches).
-// Bound: memory.
+// A thread takes VEC neighbouring columns (channel, group element) of a strip of tokens.  What a strip needs
+// of its neighbours, W - 1 tokens, is read again, from the caches.  Runs of GR columns that share a channel share their
+// weights and their sums for dweight and dbias.
+// Bound: memory, and the loads that a thread has in flight: the forward reads its whole strip before it starts, the
+// backward eight tokens while it works on the eight before.
 #pragma once
+#include "eql_colsum.h"
 #include "eql_common.h"
 #include "eql_config.h"
 #include "eql_recurrent.h"
 
 namespace eqk {
 
-template <int DT>
-__device__ __forceinline__ float conv_sigmoid(float v) {
-  const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * __builtin_fabsf(v));
-  const float r = __builtin_amdgcn_rcpf(1.0f + e);
-  return v < 0.0f ? e * r : r;
+__device__ __forceinline__ float conv_sigmoid(float v) {  // (exp(-v) of inf gives 0)
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
 }
 
-// VEC elements at p, as floats; WHOLE: one aligned vector, else `n` single ones (the others 0).
+// VEC elements as raw words; WHOLE: one aligned vector, else the first n of them, the others 0.
+template <int DT, int VEC>
+struct ConvVec {
+  static constexpr int EB = Elem<DT>::bytes, W = VEC * EB / 4;
+  uint32_t w[W];
+};
 template <int DT, int VEC, bool WHOLE>
-__device__ __forceinline__ void conv_load(const void* p, int n, float (&f)[VEC]) {
-  using E = typename Elem<DT>::T;
-  if constexpr (WHOLE) {
-    constexpr int W = VEC * Elem<DT>::bytes / 4;
-    uint32_t w[W];
-    if constexpr (W == 4) {
-      const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ void conv_load(const void* p, int n, ConvVec<DT, VEC>& r) {
+  constexpr int W = ConvVec<DT, VEC>::W;
+  if constexpr (WHOLE && W == 4) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = v[i];
-    } else {
-      const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-      w[0] = v[0];
-      w[1] = v[1];
-    }
-    raw_to_floats<DT, W>(w, f);
+    for (int i = 0; i < 4; ++i) r.w[i] = v[i];
+  } else if constexpr (WHOLE) {
+    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+    r.w[0] = v[0];
+    r.w[1] = v[1];
+  } else if constexpr (DT == kF32) {
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) r.w[i] = i < n ? q[i] : 0u;
   } else {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = i < n ? (float)reinterpret_cast<const E*>(p)[i] : 0.0f;
+    for (int i = 0; i < W; ++i) {
+      const uint32_t lo = 2 * i < n ? q[2 * i] : 0u, hi = 2 * i + 1 < n ? q[2 * i + 1] : 0u;
+      r.w[i] = lo | hi << 16;
+    }
   }
+}
+template <int DT, int VEC>
+__device__ __forceinline__ void conv_floats(const ConvVec<DT, VEC>& r, float (&f)[VEC]) {
+  raw_to_floats<DT, ConvVec<DT, VEC>::W>(r.w, f);
 }
 template <int DT, int VEC, bool WHOLE>
 __device__ __forceinline__ void conv_store(void* p, int n, const float (&f)[VEC]) {
@@ -57,183 +69,267 @@ __device__ __forceinline__ void conv_store(void* p, int n, const float (&f)[VEC]
   }
 }
 
-// Where a thread stands: columns col .. col + n, tokens l0 .. l1 of sequence b.
+// Where a thread stands: columns col .. col + n, tokens l0 .. l1 of sequence b (none where it has no work).
 struct ConvPlace {
-  int64_t b, strip, l0, l1, len;
-  int col, n;
+  int64_t b, group, l0, l1, len;
+  int col, n, vector, turn;  // vector: among its workgroup's; turn: strip of the workgroup's
+  bool on;
 };
 template <int VEC>
-__device__ __forceinline__ bool conv_place(const ConvArgs& a, ConvPlace& p) {
+__device__ __forceinline__ ConvPlace conv_place(const ConvArgs& a) {
+  ConvPlace p;
   const int nv = (a.CT + VEC - 1) / VEC;
-  const int64_t i = (a.first + blockIdx.x) * 256 + threadIdx.x;
-  p.col = (int)(i % nv) * VEC;
+  unsigned id = blockIdx.x;
+  const int cb = (int)(id % (unsigned)a.cblocks);
+  id /= (unsigned)a.cblocks;
+  p.group = id % (unsigned)a.groups;
+  p.b = a.first + id / (unsigned)a.groups;
+  p.vector = (int)threadIdx.x % a.width;
+  p.turn = (int)threadIdx.x / a.width;
+  p.col = (cb * a.width + p.vector) * VEC;
   p.n = min(VEC, a.CT - p.col);
-  p.strip = i / nv % a.strips;
-  p.b = i / nv / a.strips;
-  if (p.b >= a.B) return false;
+  const int64_t strip = p.group * a.turns + p.turn;
+  p.on = p.turn < a.turns && strip < a.strips && cb * a.width + p.vector < nv;
   p.len = a.lengths ? min(max((int64_t)a.lengths[p.b], (int64_t)0), a.L) : a.L;
-  p.l0 = p.strip * a.rows;
-  p.l1 = min(p.l0 + a.rows, a.L);
-  return true;
+  p.l0 = p.on ? strip * a.rows : 0;
+  p.l1 = p.on ? min(p.l0 + a.rows, a.L) : 0;
+  return p;
 }
-template <int DT, int W, int VEC>
-__device__ __forceinline__ void conv_weights(const ConvArgs& a, const ConvPlace& p, float (&w)[W][VEC], float (&bias)[VEC]) {
+template <int DT, int W, int VEC, int GR>
+__device__ __forceinline__ void conv_weights(const ConvArgs& a, const ConvPlace& p, float (&w)[W][VEC / GR], float (&bias)[VEC / GR]) {
   using E = typename Elem<DT>::T;
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-    const int c = min(p.col + i, a.CT - 1) / a.T;
+  for (int i = 0; i < VEC / GR; ++i) {
+    const unsigned col = (unsigned)min(p.col + i * GR, a.CT - 1);
+    const int c = a.mT ? (int)__umulhi(col, a.mT) : (int)col;
     bias[i] = a.bias ? (float)reinterpret_cast<const E*>(a.bias)[c] : 0.0f;
 #pragma unroll
     for (int j = 0; j < W; ++j) w[j][i] = (float)reinterpret_cast<const E*>(a.w)[c * W + j];
   }
 }
-// Token l of sequence b, from the state before token 0; 0 from len on and before the state.
+// Token l of sequence b, from the state before token 0; 0 from len on, before the state, and for a thread without work.
 template <int DT, int W, int VEC, bool WHOLE>
-__device__ __forceinline__ void conv_token(const ConvArgs& a, const ConvPlace& p, int64_t l, float (&f)[VEC]) {
+__device__ __forceinline__ void conv_token(const ConvArgs& a, const ConvPlace& p, int64_t l, ConvVec<DT, VEC>& r) {
   constexpr int EB = Elem<DT>::bytes;
-  if (l >= 0 && l < p.len) {
-    conv_load<DT, VEC, WHOLE>((const char*)a.x + (p.b * a.xs[0] + l * a.xs[1] + p.col) * EB, p.n, f);
-  } else if (l < 0 && a.h0) {
-    conv_load<DT, VEC, WHOLE>((const char*)a.h0 + ((p.b * (W - 1) + l + W - 1) * a.CT + p.col) * EB, p.n, f);
+  if (p.on && l >= 0 && l < p.len) {
+    conv_load<DT, VEC, WHOLE>((const char*)a.x + (p.b * a.xs[0] + l * a.xs[1] + p.col) * EB, p.n, r);
+  } else if (p.on && l < 0 && a.h0) {
+    conv_load<DT, VEC, WHOLE>((const char*)a.h0 + ((p.b * (W - 1) + l + W - 1) * a.CT + p.col) * EB, p.n, r);
   } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) f[i] = 0.0f;
+    for (int i = 0; i < ConvVec<DT, VEC>::W; ++i) r.w[i] = 0u;
   }
 }
 
-template <int DT, int W, int VEC, bool WHOLE>
+constexpr int kConvRows = 16;  // of a forward strip
+
+template <int DT, int W, int VEC, int GR, bool WHOLE>
 __global__ __launch_bounds__(256) void eql_conv_fwd_kernel(const ConvArgs a) {
   constexpr int EB = Elem<DT>::bytes;
-  ConvPlace p;
-  if (!conv_place<VEC>(a, p)) return;
-  float w[W][VEC], bias[VEC], x[W][VEC];  // x[W - 1]: the newest token
-  conv_weights<DT, W, VEC>(a, p, w, bias);
+  const ConvPlace p = conv_place<VEC>(a);
+  if (!p.on) return;
+  ConvVec<DT, VEC> raw[kConvRows + W - 1];  // tokens l0 - (W - 1) ..
+  const bool inner = p.l0 >= W - 1 && p.l0 + kConvRows <= p.len;
+  if (inner) {
+    const char* q = (const char*)a.x + (p.b * a.xs[0] + (p.l0 - (W - 1)) * a.xs[1] + p.col) * EB;
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, x[j + 1]);
-#pragma unroll 4
-  for (int64_t l = p.l0; l < p.l1; ++l) {
+    for (int j = 0; j < kConvRows + W - 1; ++j) conv_load<DT, VEC, WHOLE>(q + j * a.xs[1] * EB, p.n, raw[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kConvRows + W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, raw[j]);
+  }
+  float w[W][VEC / GR], bias[VEC / GR], x[W][VEC];  // x[W - 1]: the newest token
+  conv_weights<DT, W, VEC, GR>(a, p, w, bias);
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) conv_floats(raw[j], x[j + 1]);
+  char* out = (char*)a.y + ((p.b * a.L + p.l0) * a.CT + p.col) * EB;
+#pragma unroll
+  for (int r = 0; r < kConvRows; ++r) {
+    if (p.l0 + r >= p.l1) break;
     float y[VEC];
 #pragma unroll
     for (int j = 0; j + 1 < W; ++j)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) x[j][i] = x[j + 1][i];
-    conv_token<DT, W, VEC, WHOLE>(a, p, l, x[W - 1]);
+    conv_floats(raw[r + W - 1], x[W - 1]);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
-      y[i] = bias[i];
+      y[i] = bias[i / GR];
 #pragma unroll
-      for (int j = 0; j < W; ++j) y[i] = __builtin_fmaf(w[j][i], x[j][i], y[i]);
-      if (a.silu) y[i] *= conv_sigmoid<DT>(y[i]);
-      if (l >= p.len) y[i] = 0.0f;
+      for (int j = 0; j < W; ++j) y[i] = __builtin_fmaf(w[j][i / GR], x[j][i], y[i]);
+      if (a.silu) y[i] *= conv_sigmoid(y[i]);
     }
-    conv_store<DT, VEC, WHOLE>((char*)a.y + ((p.b * a.L + l) * a.CT + p.col) * EB, p.n, y);
+    if (p.l0 + r >= p.len)
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) y[i] = 0.0f;
+    conv_store<DT, VEC, WHOLE>(out + (int64_t)r * a.CT * EB, p.n, y);
   }
   // the last W - 1 tokens: the first strip alone reads the state, so it may be updated in place
-  if (W > 1 && a.hT && p.strip == 0) {
-    float s[W][VEC];
+  if (W > 1 && a.hT && p.l0 == 0) {
+    ConvVec<DT, VEC> s[W];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.len - (W - 1) + j, s[j]);
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j)
-      conv_store<DT, VEC, WHOLE>((char*)a.hT + ((p.b * (W - 1) + j) * a.CT + p.col) * EB, p.n, s[j]);
+    for (int j = 0; j < W - 1; ++j) {
+      float f[VEC];
+      conv_floats(s[j], f);
+      conv_store<DT, VEC, WHOLE>((char*)a.hT + ((p.b * (W - 1) + j) * a.CT + p.col) * EB, p.n, f);
+    }
   }
 }
 
-// dx of the strip's tokens; its sums for dweight and dbias.  du of the W - 1 tokens behind the strip is formed again.
-template <int DT, int W, int VEC, bool WHOLE>
+// dx of the strip's tokens; its sums for dweight and dbias.  du of the W - 1 tokens behind the strip is formed again:
+// rows + W - 1 tokens are walked, a multiple of eight.
+constexpr int kConvBatch = 8;
+
+template <int DT, int W, int VEC, int GR, bool WHOLE>
 __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
-  constexpr int EB = Elem<DT>::bytes;
-  ConvPlace p;
-  if (!conv_place<VEC>(a, p)) return;
-  float w[W][VEC], bias[VEC], x[W][VEC], du[W][VEC], dw[W][VEC], db[VEC];
-  conv_weights<DT, W, VEC>(a, p, w, bias);
+  constexpr int EB = Elem<DT>::bytes, NG = VEC / GR;
+  const ConvPlace p = conv_place<VEC>(a);
+  const int steps = a.rows + W - 1;
+  const bool inner = p.on && p.l0 >= W - 1 && p.l0 + steps <= p.len;
+  ConvVec<DT, VEC> xr[kConvBatch], gr[kConvBatch], before[W];
+  const char* const xp = (const char*)a.x + (p.b * a.xs[0] + p.l0 * a.xs[1] + p.col) * EB;
+  const char* const gp = (const char*)a.dy + ((p.b * a.L + p.l0) * a.CT + p.col) * EB;
+  auto fetch = [&](int s) {
+    if (inner) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-    db[i] = 0.0f;
-#pragma unroll
-    for (int j = 0; j < W; ++j) dw[j][i] = du[j][i] = 0.0f;
-  }
-#pragma unroll
-  for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, x[j + 1]);
-  // du[j]: of token l - (W - 1) + j
-#pragma unroll 2
-  for (int64_t l = p.l0; l < p.l1 + W - 1; ++l) {
-#pragma unroll
-    for (int j = 0; j + 1 < W; ++j)
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) {
-        x[j][i] = x[j + 1][i];
-        du[j][i] = du[j + 1][i];
+      for (int j = 0; j < kConvBatch; ++j) {
+        conv_load<DT, VEC, WHOLE>(xp + (int64_t)(s + j) * a.xs[1] * EB, p.n, xr[j]);
+        conv_load<DT, VEC, WHOLE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
       }
-    conv_token<DT, W, VEC, WHOLE>(a, p, l, x[W - 1]);
-    float g[VEC];
-    if (l < p.len) conv_load<DT, VEC, WHOLE>((const char*)a.dy + ((p.b * a.L + l) * a.CT + p.col) * EB, p.n, g);
+    } else {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-      if (l >= p.len) {
-        g[i] = 0.0f;
-      } else if (a.silu) {
-        float u = bias[i];
+      for (int j = 0; j < kConvBatch; ++j) {
+        conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 + s + j, xr[j]);
+        if (p.on && p.l0 + s + j < p.len) conv_load<DT, VEC, WHOLE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
+        else
 #pragma unroll
-        for (int j = 0; j < W; ++j) u = __builtin_fmaf(w[j][i], x[j][i], u);
-        const float s = conv_sigmoid<DT>(u);
-        g[i] *= s * __builtin_fmaf(u, 1.0f - s, 1.0f);
-      }
-      du[W - 1][i] = g[i];
-      if (l < p.l1) {
-        db[i] += g[i];
-#pragma unroll
-        for (int j = 0; j < W; ++j) dw[j][i] = __builtin_fmaf(g[i], x[j][i], dw[j][i]);
+          for (int i = 0; i < ConvVec<DT, VEC>::W; ++i) gr[j].w[i] = 0u;
       }
     }
-    // token l - (W - 1) has its last du; of the strip before, what falls before token 0 is the state's
-    const int64_t at = l - (W - 1);
-    const bool mine = at >= p.l0 || (at < 0 && a.dh0);
-    if (mine) {
+  };
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, before[j]);
+  fetch(0);
+  float w[W][NG], bias[NG], x[W][VEC], du[W][VEC], dw[W][NG], db[NG];
+  conv_weights<DT, W, VEC, GR>(a, p, w, bias);
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    db[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) dw[j][i] = 0.0f;
+  }
+#pragma unroll
+  for (int j = 0; j < W; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) du[j][i] = 0.0f;
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) conv_floats(before[j], x[j + 1]);
+  // du[j]: of token l - (W - 1) + j
+  for (int s = 0; s < steps; s += kConvBatch) {
+    ConvVec<DT, VEC> xc[kConvBatch], gc[kConvBatch];
+#pragma unroll
+    for (int j = 0; j < kConvBatch; ++j) {
+      xc[j] = xr[j];
+      gc[j] = gr[j];
+    }
+    if (s + kConvBatch < steps) fetch(s + kConvBatch);
+#pragma unroll
+    for (int r = 0; r < kConvBatch; ++r) {
+      const int64_t l = p.l0 + s + r;
+#pragma unroll
+      for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          x[j][i] = x[j + 1][i];
+          du[j][i] = du[j + 1][i];
+        }
+      conv_floats(xc[r], x[W - 1]);
+      float g[VEC];
+      conv_floats(gc[r], g);
+      if (a.silu) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          float u = bias[i / GR];
+#pragma unroll
+          for (int j = 0; j < W; ++j) u = __builtin_fmaf(w[j][i / GR], x[j][i], u);
+          const float sg = conv_sigmoid(u);
+          g[i] *= sg * __builtin_fmaf(u, 1.0f - sg, 1.0f);
+        }
+      }
+      if (!inner && l >= p.len)  // (a gradient of 0 behind the sequence, whatever the weights)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) g[i] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) du[W - 1][i] = g[i];
+      if (l < p.l1) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          db[i / GR] += g[i];
+#pragma unroll
+          for (int j = 0; j < W; ++j) dw[j][i / GR] = __builtin_fmaf(g[i], x[j][i], dw[j][i / GR]);
+        }
+      }
+      // token l - (W - 1) has its last du; what falls before token 0 is the state's
+      const int64_t at = l - (W - 1);
+      if (!p.on || at >= p.l1 || !(at >= p.l0 || (at < 0 && a.dh0))) continue;
       float d[VEC];
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         d[i] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < W; ++j) d[i] = __builtin_fmaf(w[W - 1 - j][i], du[j][i], d[i]);
+        for (int j = 0; j < W; ++j) d[i] = __builtin_fmaf(w[W - 1 - j][i / GR], du[j][i], d[i]);
       }
-      if (W > 1 && a.dhT && at >= p.len - (W - 1) && at < p.len) {  // a token of the last ones
-        float h[VEC];
-        conv_load<DT, VEC, WHOLE>((const char*)a.dhT + ((p.b * (W - 1) + at - p.len + W - 1) * a.CT + p.col) * EB, p.n, h);
+      if (!inner) {
+        if (W > 1 && a.dhT && at >= p.len - (W - 1) && at < p.len) {  // a token of the last ones
+          ConvVec<DT, VEC> hr;
+          float h[VEC];
+          conv_load<DT, VEC, WHOLE>((const char*)a.dhT + ((p.b * (W - 1) + at - p.len + W - 1) * a.CT + p.col) * EB, p.n, hr);
+          conv_floats(hr, h);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) d[i] += h[i];
+          for (int i = 0; i < VEC; ++i) d[i] += h[i];
+        }
+        if (at >= p.len)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) d[i] = 0.0f;
       }
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) d[i] = at < p.len ? d[i] : 0.0f;
       if (at >= 0) conv_store<DT, VEC, WHOLE>((char*)a.dx + ((p.b * a.L + at) * a.CT + p.col) * EB, p.n, d);
       else conv_store<DT, VEC, WHOLE>((char*)a.dh0 + ((p.b * (W - 1) + at + W - 1) * a.CT + p.col) * EB, p.n, d);
     }
   }
-  float* const part = a.part + (p.b * a.strips + p.strip) * (W + 1) * a.CT + p.col;
+  // the sums of the workgroup's strips, in order
+  __shared__ float red[256][NG];
+  const int K = a.CT / GR;
+  float* const part = a.part + (p.b * a.groups + p.group) * (W + 1) * K + p.col / GR;
 #pragma unroll
-  for (int j = 0; j <= W; ++j)
+  for (int j = 0; j <= W; ++j) {
+    if (j) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (i < p.n) part[(int64_t)j * a.CT + i] = j < W ? dw[j < W ? j : 0][i] : db[i];
+    for (int i = 0; i < NG; ++i) red[threadIdx.x][i] = j < W ? dw[j < W ? j : 0][i] : db[i];
+    __syncthreads();
+    if (p.turn == 0 && p.col < a.CT) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        if (i * GR >= p.n) break;
+        float v = red[p.vector][i];
+        for (int t = 1; t < a.turns; ++t) v += red[t * a.width + p.vector][i];
+        part[(int64_t)j * K + i] = v;
+      }
+    }
+  }
 }
 
-// dweight and dbias: a workgroup adds the parts of one channel and weight.
+// dweight and dbias from the workgroups' sums.
 template <int DT>
-__global__ __launch_bounds__(256) void eql_conv_params_kernel(const ConvArgs a) {
+__global__ __launch_bounds__(256) void eql_conv_params_kernel(const ConvArgs a, int GR) {
   using E = typename Elem<DT>::T;
-  const int64_t id = a.first + blockIdx.x;
-  const int ch = (int)(id / (a.W + 1)), j = (int)(id % (a.W + 1));
-  E* const dst = j < a.W ? reinterpret_cast<E*>(a.dw) + (int64_t)ch * a.W + j : a.db ? reinterpret_cast<E*>(a.db) + ch : nullptr;
-  if (!dst) return;
-  const int64_t n = a.B * a.strips * a.T;
-  float v = 0.0f;
-  for (int64_t i = threadIdx.x; i < n; i += 256) v += a.part[(i / a.T * (a.W + 1) + j) * a.CT + ch * a.T + i % a.T];
-  __shared__ float red[4];
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  if (threadIdx.x == 0) *dst = (E)((red[0] + red[1]) + (red[2] + red[3]));
+  const int j = (int)(blockIdx.x % (a.W + 1)), block = (int)(blockIdx.x / (a.W + 1));
+  const int T = a.T / GR, K = a.C * T;
+  column_sums(a.part + (int64_t)j * K, a.B * a.groups, (int64_t)(a.W + 1) * K, a.C, T, block, [&](int c, float v) {
+    if (j < a.W) reinterpret_cast<E*>(a.dw)[(int64_t)c * a.W + j] = (E)v;
+    else if (a.db) reinterpret_cast<E*>(a.db)[c] = (E)v;
+  });
 }
 
 }  // namespace eqk

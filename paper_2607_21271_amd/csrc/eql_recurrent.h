@@ -34,7 +34,10 @@ struct ScanArgs {
   float* part;    // [B * K, N + 2, cols]: sums of dA, dD, ddelta_bias
   float* bcpart;  // [B, L, groups, P, 2, NP]: db and dc of each workgroup's columns
   int64_t xs[2], ds[2], zs[2], bs[3], cs[3];
-  int64_t B, L, first;   // first: workgroup of the call that this launch starts with
+  int64_t B, L;
+  int64_t first;         // what a launch starts with: a sequence (an element or workgroup of the small kernels)
+  unsigned tasks;        // waves of a launch
+  unsigned mT;           // ceil(2^32 / T), 0 for T = 1: the high half of column * mT is the channel
   int64_t chunk, tiles;  // tokens of a chunk (whole tiles), tiles of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
   int whole;  // every vector of a wave's columns is aligned and inside its group
@@ -60,10 +63,16 @@ struct ConvArgs {
   const void *x, *w, *bias, *h0, *dy, *dhT;
   void *y, *hT, *dx, *dw, *db, *dh0;
   const int* lengths;
-  float* part;  // [B * strips, W + 1, CT]
+  float* part;  // [B * groups, W + 1, CT / GR]
   int64_t xs[2];
-  int64_t B, L, strips, first;
-  int C, T, W, CT, rows, silu, vec;  // rows: tokens of a strip
+  int64_t B, L, strips, groups;
+  int64_t seq;           // what a launch starts with: a sequence, and a workgroup from it on
+  unsigned first;
+  unsigned mT;           // ceil(2^32 / T), 0 for T = 1: the high half of column * mT is the channel
+  int C, T, W, CT, silu, vec;
+  int rows;              // tokens of a strip
+  int width, cblocks;    // vectors of columns of a workgroup, workgroups side by side
+  int turns;             // strips of a workgroup; `groups` of them are a sequence's
 };
 
 constexpr int conv_vec(int dt, int W, bool bwd) { return dt == kF32 ? 4 : bwd && W > 4 ? 4 : 8; }
@@ -85,12 +94,14 @@ constexpr int kResMaxRow = 8192;
 struct ResArgs {
   const void *x, *u, *w, *b, *scale, *gate, *pw, *pb, *dr, *dh;
   void *r, *h, *dx, *du, *dw, *db, *dscale, *dgate, *dpw, *dpb;
-  float* part;  // [seqs, strips, J, K]: column sums of each workgroup
+  float* part;  // [seqs, strips, J, K / GR]: column sums of each workgroup
   float* sums;  // [seqs, J, C]
   int64_t B, L;
   int64_t seqs, rows;    // sequences with a gate of their own (else one), tokens of each
   int64_t strips, strip; // workgroups of a sequence and tokens of each
-  int64_t first;
+  int64_t seq;     // what a launch starts with: a sequence, and a workgroup from it on
+  unsigned first;
+  unsigned mT;     // ceil(2^32 / T), 0 for T = 1
   int C, T, K, rms, J;
   float eps;
   int whole, lanes, ept;  // threads of a row and elements of each

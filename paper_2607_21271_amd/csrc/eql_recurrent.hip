@@ -9,56 +9,86 @@ namespace {
 
 constexpr int DT = EQK_DT;
 
-// f(slice of the call that one launch takes, its workgroups)
+// f(slice of the call that one launch takes, its workgroups) for `per` workgroups a sequence: fewer than 2^32
+// threads a launch, and numbers of workgroups below 2^31 from its first sequence on.
 template <typename A, typename F>
-hipError_t launches(const A& a, int64_t blocks, int threads, F&& f) {
+hipError_t launches(const A& a, int64_t seqs, int64_t per, int threads, F&& f) {
   A s = a;
-  const int64_t most = launch_blocks(threads);
-  for (s.first = 0; s.first < blocks; s.first += most) {
-    f(s, dim3((unsigned)(blocks - s.first < most ? blocks - s.first : most)));
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  const int64_t some = ((int64_t)1 << 31) - 1, most = launch_blocks(threads);
+  if (per < 1 || per > some) return hipErrorInvalidValue;
+  const int64_t step = some / per;
+  for (s.seq = 0; s.seq < seqs; s.seq += step) {
+    const int64_t n = (seqs - s.seq < step ? seqs - s.seq : step) * per;
+    for (int64_t first = 0; first < n; first += most) {
+      s.first = (unsigned)first;
+      f(s, dim3((unsigned)(n - first < most ? n - first : most)));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
   }
   return hipSuccess;
 }
 
-template <int W, bool BACK, bool WHOLE>
+template <int W, bool BACK, int GR, bool WHOLE>
+hipError_t conv_gr(const ConvArgs& a, hipStream_t stream) {
+  constexpr int VEC = conv_vec(DT, W, BACK);
+  if constexpr (GR > VEC) {
+    return hipErrorInvalidValue;
+  } else {
+    const hipError_t e = launches(a, a.B, a.groups * a.cblocks, 256, [&](const ConvArgs& s, dim3 n) {
+      if constexpr (BACK) hipLaunchKernelGGL((eql_conv_bwd_kernel<DT, W, VEC, GR, WHOLE>), n, dim3(256), 0, stream, s);
+      else hipLaunchKernelGGL((eql_conv_fwd_kernel<DT, W, VEC, GR, WHOLE>), n, dim3(256), 0, stream, s);
+    });
+    if (e != hipSuccess || !BACK) return e;
+    hipLaunchKernelGGL(eql_conv_params_kernel<DT>, dim3((unsigned)((W + 1) * colsum_blocks(a.C, a.T / GR))), dim3(256), 0, stream, a, GR);
+    return hipGetLastError();
+  }
+}
+template <int W, bool BACK>
 hipError_t conv_w(const ConvArgs& a, hipStream_t stream) {
   constexpr int VEC = conv_vec(DT, W, BACK);
-  const int64_t threads = a.B * a.strips * ((a.CT + VEC - 1) / VEC);
-  const hipError_t e = launches(a, (threads + 255) / 256, 256, [&](const ConvArgs& s, dim3 n) {
-    if constexpr (BACK) hipLaunchKernelGGL((eql_conv_bwd_kernel<DT, W, VEC, WHOLE>), n, dim3(256), 0, stream, s);
-    else hipLaunchKernelGGL((eql_conv_fwd_kernel<DT, W, VEC, WHOLE>), n, dim3(256), 0, stream, s);
-  });
-  if (e != hipSuccess || !BACK) return e;
-  return launches(a, (int64_t)a.C * (W + 1), 256, [&](const ConvArgs& s, dim3 n) {
-    hipLaunchKernelGGL(eql_conv_params_kernel<DT>, n, dim3(256), 0, stream, s);
-  });
+  if (a.vec == 1) return conv_gr<W, BACK, 1, false>(a, stream);
+  if (a.T % VEC == 0) return conv_gr<W, BACK, VEC, true>(a, stream);
+  if constexpr (VEC == 8)
+    if (a.T % 4 == 0) return conv_gr<W, BACK, 4, true>(a, stream);
+  return conv_gr<W, BACK, 1, true>(a, stream);
 }
 template <bool BACK, int W = 1>
 hipError_t conv(const ConvArgs& a, hipStream_t stream) {
   if constexpr (W > kConvMaxW) {
     return hipErrorInvalidValue;
   } else {
-    if (a.W != W) return conv<BACK, W + 1>(a, stream);
-    return a.vec > 1 ? conv_w<W, BACK, true>(a, stream) : conv_w<W, BACK, false>(a, stream);
+    return a.W == W ? conv_w<W, BACK>(a, stream) : conv<BACK, W + 1>(a, stream);
   }
 }
 
-template <int LANES, int EPT, bool WHOLE>
+template <int LANES, int EPT, bool WHOLE, int GR>
 hipError_t res_row(const ResArgs& a, bool back, hipStream_t stream) {
-  constexpr int threads = ResRow<DT, LANES, EPT, WHOLE>::THREADS;
-  return launches(a, a.seqs * a.strips, threads, [&](const ResArgs& s, dim3 n) {
-    if (back) hipLaunchKernelGGL((eql_res_bwd_kernel<DT, LANES, EPT, WHOLE>), n, dim3(threads), 0, stream, s);
-    else hipLaunchKernelGGL((eql_res_fwd_kernel<DT, LANES, EPT, WHOLE>), n, dim3(threads), 0, stream, s);
+  constexpr int threads = ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS;
+  return launches(a, a.seqs, a.strips, threads, [&](const ResArgs& s, dim3 n) {
+    if (back) hipLaunchKernelGGL((eql_res_bwd_kernel<DT, LANES, EPT, WHOLE, GR>), n, dim3(threads), 0, stream, s);
+    else hipLaunchKernelGGL((eql_res_fwd_kernel<DT, LANES, EPT, WHOLE, GR>), n, dim3(threads), 0, stream, s);
   });
 }
-template <bool WHOLE>
+template <bool WHOLE, int GR>
 hipError_t res_lanes(const ResArgs& a, bool back, hipStream_t stream) {
-  if (a.lanes == 16) return res_row<16, 8, WHOLE>(a, back, stream);
-  if (a.lanes == 64) return a.ept == 8 ? res_row<64, 8, WHOLE>(a, back, stream) : res_row<64, 16, WHOLE>(a, back, stream);
-  if (a.lanes == 256) return a.ept == 8 ? res_row<256, 8, WHOLE>(a, back, stream) : res_row<256, 16, WHOLE>(a, back, stream);
-  return res_row<512, 16, WHOLE>(a, back, stream);
+  if (a.lanes == 16) return res_row<16, 8, WHOLE, GR>(a, back, stream);
+  if (a.lanes == 64) return a.ept == 8 ? res_row<64, 8, WHOLE, GR>(a, back, stream) : res_row<64, 16, WHOLE, GR>(a, back, stream);
+  if (a.lanes == 256) return a.ept == 8 ? res_row<256, 8, WHOLE, GR>(a, back, stream) : res_row<256, 16, WHOLE, GR>(a, back, stream);
+  return res_row<512, 16, WHOLE, GR>(a, back, stream);
+}
+// columns that share a channel, of a vector
+int res_gr(const ResArgs& a) {
+  if (!a.whole) return 1;
+  if (DT != kF32 && a.T % 8 == 0) return 8;
+  return a.T % 4 == 0 ? 4 : 1;
+}
+hipError_t res(const ResArgs& a, bool back, hipStream_t stream) {
+  const int gr = res_gr(a);
+  if constexpr (DT != kF32)
+    if (gr == 8) return res_lanes<true, 8>(a, back, stream);
+  if (gr == 4) return res_lanes<true, 4>(a, back, stream);
+  return a.whole ? res_lanes<true, 1>(a, back, stream) : res_lanes<false, 1>(a, back, stream);
 }
 
 }  // namespace
@@ -73,19 +103,19 @@ hipError_t conv_backward<DT>(const ConvArgs& a, hipStream_t stream) {
 }
 template <>
 hipError_t res_forward<DT>(const ResArgs& a, hipStream_t stream) {
-  return a.whole ? res_lanes<true>(a, false, stream) : res_lanes<false>(a, false, stream);
+  return res(a, false, stream);
 }
 template <>
 hipError_t res_backward<DT>(const ResArgs& a, hipStream_t stream) {
-  const hipError_t e = a.seqs * a.rows == 0 ? hipSuccess : a.whole ? res_lanes<true>(a, true, stream) : res_lanes<false>(a, true, stream);
+  const hipError_t e = res(a, true, stream);
   if (e != hipSuccess || a.J == 0) return e;
-  const hipError_t f = launches(a, a.seqs * a.J * a.C, 256, [&](const ResArgs& s, dim3 n) {
-    hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(256), 0, stream, s);
+  const int gr = res_gr(a), blocks = colsum_blocks(a.C, a.T / gr);
+  const hipError_t f = launches(a, a.seqs, (int64_t)a.J * blocks, 256, [&](const ResArgs& s, dim3 n) {
+    hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(256), 0, stream, s, gr, blocks);
   });
   if (f != hipSuccess) return f;
-  return launches(a, (a.C + 3) / 4, 256, [&](const ResArgs& s, dim3 n) {
-    hipLaunchKernelGGL(eql_res_params_kernel<DT>, n, dim3(256), 0, stream, s);
-  });
+  hipLaunchKernelGGL(eql_res_params_kernel<DT>, dim3((unsigned)((a.C + 63) / 64)), dim3(256), 0, stream, a);
+  return hipGetLastError();
 }
 
 }  // namespace eqk

@@ -134,6 +134,11 @@ int scan_whole(const eqk::ScanArgs& a, int dtype) {
   const int vec = eqk::scan_vec(dtype, eqk::scan_lanes(a.N));
   const size_t e = elem_bytes(dtype);
   const int64_t none[1] = {0};
+  // a tile's tokens are addressed by 31 bits from its first
+  const int64_t steps[6] = {a.CT, a.xs[1], a.ds[1], a.z ? a.zs[1] : 0, a.bs[1], a.cs[1]};
+  for (int64_t st : steps)
+    if (st >= ((int64_t)1 << 31) / 128) return 0;
+  if (a.N % 4 != 0 || !vectors(a.b, a.bs, 3, e, 4) || !vectors(a.c, a.cs, 3, e, 4)) return 0;
   return a.CTg % vec == 0 && vectors(a.x, a.xs, 2, e, vec) && vectors(a.delta, a.ds, 2, e, vec) &&
          vectors(a.z, a.zs, 2, e, vec) && vectors(a.y, none, 1, e, vec) && vectors(a.dy, none, 1, e, vec) &&
          vectors(a.dx, none, 1, e, vec) && vectors(a.ddelta, none, 1, e, vec) && vectors(a.dz, none, 1, e, vec);
@@ -143,8 +148,15 @@ int scan_whole(const eqk::ScanArgs& a, int dtype) {
 
 namespace eqk {
 
-// Chunks of tokens that fill the device where the columns alone do not: two waves a SIMD, no
-// chunk shorter than 8 tiles.
+// Time of `waves` waves that walk `tiles` tiles each, in tiles of a wave alone on its SIMD: the forward's kernels fit two on
+// one, which hide each other's waiting (a tile of one wave 0.37 us, of two 0.55 us together), the gradients' one.
+static double scan_time(int64_t waves, int64_t tiles, int64_t simds, bool bwd) {
+  const int64_t w = (waves + simds - 1) / simds;
+  return (double)(tiles + 1) * (bwd ? (double)w : 0.75 * w + (w % 2 ? 0.25 : 0.0));
+}
+
+// Chunks of tokens where the columns alone do not fill the device: the number of waves (one to four a SIMD) for
+// which the pass over the states or gradients, half to three quarters of the main one, and the main one take least.
 void scan_plan(ScanArgs& a, int cus, bool bwd) {
   const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL);
   a.CT = a.C * a.T;
@@ -152,13 +164,28 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.nblk = (a.CTg + CH - 1) / CH;
   a.cols = a.G * a.nblk * CH;
   a.tiles = (a.L + TT - 1) / TT;
+  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
   const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves;
   a.P = (a.nblk + waves - 1) / waves;
-  const int64_t one = a.B * a.G * (bwd ? (int64_t)a.P * waves : a.nblk), want = 8 * (int64_t)cus;
-  int64_t K = one > 0 && one * 2 <= want ? want / one : 1;
-  if (K > a.tiles / 8) K = a.tiles / 8;
-  if (K < 1) K = 1;
-  const int64_t per = a.tiles > 0 ? (a.tiles + K - 1) / K : 1;
+  const int64_t simds = 4 * (int64_t)cus, one = a.B * a.G * (bwd ? (int64_t)a.P * waves : a.nblk);
+  int64_t per = a.tiles > 0 ? a.tiles : 1;
+  if (one > 0 && one < simds && a.tiles > 1) {
+    const int64_t whole = per;
+    double least = scan_time(one, whole, simds, bwd);
+    for (int w = 1; w <= 4; ++w) {
+      int64_t K = w * simds / one;
+      if (K > whole) K = whole;
+      if (K < 2) continue;
+      const int64_t n = (whole + K - 1) / K;
+      K = (whole + n - 1) / n;
+      // (two more launches, and the states between the passes: about ten microseconds)
+      const double t = scan_time(one * K, n, simds, bwd) * (bwd ? 1.3 : 1.7) + (bwd ? 8.0 : 25.0);
+      if (t < least) {
+        least = t;
+        per = n;
+      }
+    }
+  }
   a.chunk = per * TT;
   a.K = (int)(a.tiles > 0 ? (a.tiles + per - 1) / per : 1);
 }
@@ -166,33 +193,40 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
 void conv_plan(ConvArgs& a, int dt, int cus, bool bwd) {
   const int vec = conv_vec(dt, a.W, bwd);
   a.CT = a.C * a.T;
-  // strips of 16 tokens, longer ones (fewer halo tokens) where the device is full anyway
-  const int64_t cols = a.B * ((a.CT + vec - 1) / vec);
-  int64_t rows = cols * a.L / ((int64_t)cus * 2048);
-  const int64_t least = bwd ? 32 : 16, most = bwd ? 128 : 64;
-  rows = rows < least ? least : rows > most ? most : rows;
-  a.rows = (int)rows;
-  a.strips = (a.L + rows - 1) / rows;
+  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
+  const int nv = (a.CT + vec - 1) / vec;
+  a.width = nv < 256 ? nv : 256;
+  a.cblocks = (nv + a.width - 1) / a.width;
+  a.turns = 256 / a.width;
+  a.rows = 16;
+  if (bwd) {
+    // strips of 8 m tokens with their halo: longer ones where the device is full of waves anyway
+    int64_t m = a.B * nv * a.L / (8 * 64 * 8 * (int64_t)cus);
+    m = m < 2 ? 2 : m > 8 ? 8 : m;
+    a.rows = (int)(8 * m) - (a.W - 1);
+  }
+  a.strips = (a.L + a.rows - 1) / a.rows;
   if (a.strips < 1) a.strips = 1;
+  a.groups = (a.strips + a.turns - 1) / a.turns;
 }
 
 void res_plan(ResArgs& a, int dt, int cus, bool bwd) {
   (void)dt;
   a.K = a.C * a.T;
+  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
   a.lanes = a.K <= 128 ? 16 : a.K <= 1024 ? 64 : a.K <= 4096 ? 256 : 512;
   a.ept = a.K <= 8 * a.lanes ? 8 : 16;
   a.seqs = a.gate ? a.B : 1;
   a.rows = a.gate ? a.L : a.B * a.L;
   const int64_t turn = a.lanes < 256 ? 256 / a.lanes : 1;  // rows of a workgroup at a time
-  // about eight workgroups a CU, each at least four turns long
-  int64_t strips = a.seqs > 0 ? (8 * (int64_t)cus + a.seqs - 1) / a.seqs : 1;
-  const int64_t most = (a.rows + 4 * turn - 1) / (4 * turn);
+  // four workgroups a CU (two in the backward, whose sums take registers), each at least two turns long
+  int64_t strips = a.seqs > 0 ? ((bwd ? 2 : 4) * (int64_t)cus + a.seqs - 1) / a.seqs : 1;
+  const int64_t most = (a.rows + 2 * turn - 1) / (2 * turn);
   if (strips > most) strips = most;
   if (strips < 1) strips = 1;
   a.strip = (a.rows + strips - 1) / strips;
   if (a.strip < 1) a.strip = 1;
   a.strips = a.rows > 0 ? (a.rows + a.strip - 1) / a.strip : 0;
-  (void)bwd;
 }
 
 }  // namespace eqk
@@ -344,7 +378,7 @@ int conv_args(const eqlinear_conv_shape* s, eqk::ConvArgs& a, bool bwd) {
   return EQL_OK;
 }
 
-size_t conv_part(const eqk::ConvArgs& a) { return align256((size_t)a.B * a.strips * (a.W + 1) * a.CT * sizeof(float)); }
+size_t conv_part(const eqk::ConvArgs& a) { return align256((size_t)a.B * a.groups * (a.W + 1) * a.CT * sizeof(float)); }
 
 // The inputs of both passes: x, weight, bias, lengths, state.
 int conv_inputs(const eqlinear_conv_shape* s, const eqk::ConvArgs& a, const void* x, const void* weight, const void* bias,
@@ -586,6 +620,7 @@ int eqlinear_residual_norm_backward(const eqlinear_residual_shape* s, const void
   if (!apart(out, 9, in, 9)) return EQL_ERR_INVALID_ARG;
   if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
+  if (n == 0) return EQL_OK;
   a.part = (float*)workspace;
   a.sums = (float*)((char*)workspace + align256((size_t)a.seqs * a.strips * a.J * a.K * sizeof(float)));
   a.whole = res_whole(a, s->dtype);

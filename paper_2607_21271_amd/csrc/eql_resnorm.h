@@ -13,16 +13,19 @@
 // memory, and two small kernels add them in a fixed order.
 // Bound: memory (forward 4, backward 6 rows an element).
 #pragma once
+#include "eql_colsum.h"
 #include "eql_common.h"
 #include "eql_config.h"
+#include "eql_lanes.h"
 #include "eql_recurrent.h"
 
 namespace eqk {
 
-template <int DT, int LANES, int EPT, bool WHOLE>
+template <int DT, int LANES, int EPT, bool WHOLE, int GR>
 struct ResRow {
   using E = typename Elem<DT>::T;
   static constexpr int EB = Elem<DT>::bytes, VEC = WHOLE ? 16 / EB : 1, NV = EPT / VEC;
+  static constexpr int NP = EPT / GR;  // parameters of a thread: of runs of GR columns that share a channel
   static constexpr int W = WHOLE ? 4 : 1;
   static constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at a time
   static constexpr int THREADS = LANES < 256 ? 256 : LANES;
@@ -74,18 +77,28 @@ struct ResRow {
     }
   }
   // a parameter of the thread's columns, `none` outside and where p is NULL
-  static __device__ __forceinline__ void param(const void* p, int T, int K, float none, float (&f)[EPT]) {
+  static __device__ __forceinline__ void param(const void* p, const ResArgs& a, float none, float (&f)[NP]) {
     const E* q = reinterpret_cast<const E*>(p);
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      const int c = at(e / VEC) + e % VEC;
-      f[e] = p && c < K ? (float)q[c / T] : none;
+    for (int i = 0; i < NP; ++i) {
+      const int c = at(i * GR / VEC) + i * GR % VEC;
+      f[i] = p && c < a.K ? (float)q[a.mT ? (int)__umulhi((unsigned)c, a.mT) : c] : none;
     }
   }
   // the sum over a row's threads
   static __device__ __forceinline__ float total(float s, float* red, int& slot) {
-#pragma unroll
-    for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) s += __shfl_xor(s, d);
+    s += dpp<0x128>(s);  // rows of 16 lanes rotated by 8, 4, 2, 1
+    s += dpp<0x124>(s);
+    s += dpp<0x122>(s);
+    s += dpp<0x121>(s);
+    if constexpr (LANES >= 64) {
+      float t = s;
+      swap16(s, t);
+      s += t;
+      t = s;
+      swap32(s, t);
+      s += t;
+    }
     if constexpr (LANES > 64) {
       constexpr int NW = LANES / 64;
       float* const q = red + slot * NW;  // alternating, so that one barrier a sum is enough
@@ -139,32 +152,30 @@ struct ResPlace {
 };
 __device__ __forceinline__ ResPlace res_place(const ResArgs& a) {
   ResPlace p;
-  const int64_t id = a.first + blockIdx.x;
-  p.q = id / a.strips;
-  p.strip = id % a.strips;
+  const unsigned id = a.first + blockIdx.x;
+  p.q = a.seq + id / (unsigned)a.strips;
+  p.strip = id % (unsigned)a.strips;
   p.first = p.strip * a.strip;
   p.last = min(p.first + a.strip, a.rows);
   return p;
 }
+// scale[c] gate[q, c] of the thread's columns
+template <typename R>
+__device__ __forceinline__ void res_scale(const ResArgs& a, const ResPlace& p, float (&k)[R::NP]) {
+  R::param(a.scale, a, 1.0f, k);
+  if (!a.gate) return;
+  float g[R::NP];
+  R::param(reinterpret_cast<const typename R::E*>(a.gate) + p.q * a.C, a, 1.0f, g);
+#pragma unroll
+  for (int i = 0; i < R::NP; ++i) k[i] *= g[i];
+}
 
-template <int DT, int LANES, int EPT, bool WHOLE>
-__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_res_fwd_kernel(const ResArgs a) {
-  using R = ResRow<DT, LANES, EPT, WHOLE>;
+template <int DT, int LANES, int EPT, bool WHOLE, int GR>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void eql_res_fwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, WHOLE, GR>;
   __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
   const ResPlace p = res_place(a);
   int slot = 0;
-  float k[EPT], w[EPT], b[EPT], pw[EPT], pb[EPT];
-  R::param(a.scale, a.T, a.K, 1.0f, k);
-  if (a.gate) {
-    float g[EPT];
-    R::param(reinterpret_cast<const typename R::E*>(a.gate) + p.q * a.C, a.T, a.K, 1.0f, g);
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) k[e] *= g[e];
-  }
-  R::param(a.w, a.T, a.K, 0.0f, w);
-  R::param(a.b, a.T, a.K, 0.0f, b);
-  R::param(a.pw, a.T, a.K, 0.0f, pw);
-  R::param(a.pb, a.T, a.K, 0.0f, pb);
   const int mine = LANES < 256 ? threadIdx.x / LANES : 0;
   typename R::Raw xr, ur;
   auto fetch = [&](int64_t row) {
@@ -172,6 +183,12 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_
     if (a.u) R::load(ur, a.u, p.q * a.rows + row, a.K, row < p.last);
   };
   fetch(p.first + mine);
+  float k[R::NP], w[R::NP], b[R::NP], pw[R::NP], pb[R::NP];
+  res_scale<R>(a, p, k);
+  R::param(a.w, a, 0.0f, w);
+  R::param(a.b, a, 0.0f, b);
+  R::param(a.pw, a, 0.0f, pw);
+  R::param(a.pb, a, 0.0f, pb);
   // (LANES > 64: one row a workgroup, so every thread takes every turn)
   for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
     const int64_t row = p.q * a.rows + i;
@@ -183,115 +200,124 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_
       if (a.pw) {
         R::normed(u, a, red, slot);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) u[e] = __builtin_fmaf(u[e], pw[e], pb[e]);
+        for (int e = 0; e < EPT; ++e) u[e] = __builtin_fmaf(u[e], pw[e / GR], pb[e / GR]);
       }
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e], u[e], x[e]);
+      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e / GR], u[e], x[e]);
       R::store(x, a.r, row, a.K);
     }
     if (a.w) {
       R::normed(x, a, red, slot);
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(x[e], w[e], b[e]);
+      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(x[e], w[e / GR], b[e / GR]);
       R::store(x, a.h, row, a.K);
     }
   }
 }
 
 // Rows of column sums: dw, db (where there is a norm after), then E, or P and S.
-template <int DT, int LANES, int EPT, bool WHOLE>
-__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_res_bwd_kernel(const ResArgs a) {
-  using R = ResRow<DT, LANES, EPT, WHOLE>;
+template <int DT, int LANES, int EPT, bool WHOLE, int GR>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void eql_res_bwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, WHOLE, GR>;
+  constexpr int NP = R::NP;
   __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
-  __shared__ float cols[R::ROWS > 1 ? R::ROWS * LANES * EPT : 1];
+  __shared__ float cols[R::ROWS > 1 ? R::ROWS * LANES * NP : 1];
   const ResPlace p = res_place(a);
   int slot = 0;
-  float k[EPT], w[EPT], pw[EPT], pb[EPT];
-  R::param(a.scale, a.T, a.K, 1.0f, k);
-  if (a.gate) {
-    float g[EPT];
-    R::param(reinterpret_cast<const typename R::E*>(a.gate) + p.q * a.C, a.T, a.K, 1.0f, g);
-#pragma unroll
-    for (int e = 0; e < EPT; ++e) k[e] *= g[e];
-  }
-  R::param(a.w, a.T, a.K, 0.0f, w);
-  R::param(a.pw, a.T, a.K, 0.0f, pw);
-  R::param(a.pb, a.T, a.K, 0.0f, pb);
-  float s0[EPT], s1[EPT], s2[EPT], s3[EPT];
-#pragma unroll
-  for (int e = 0; e < EPT; ++e) s0[e] = s1[e] = s2[e] = s3[e] = 0.0f;
   const int mine = LANES < 256 ? threadIdx.x / LANES : 0;
+  typename R::Raw xr, ur, rr, hr;
+  auto fetch = [&](int64_t i) {
+    const int64_t row = p.q * a.rows + i;
+    const bool on = i < p.last;
+    R::load(xr, a.x, row, a.K, on);
+    if (a.u) R::load(ur, a.u, row, a.K, on);
+    if (a.dh) R::load(hr, a.dh, row, a.K, on);
+    if (a.dr) R::load(rr, a.dr, row, a.K, on);
+  };
+  fetch(p.first + mine);
+  float k[NP], w[NP], pw[NP], pb[NP];
+  res_scale<R>(a, p, k);
+  R::param(a.w, a, 0.0f, w);
+  R::param(a.pw, a, 0.0f, pw);
+  R::param(a.pb, a, 0.0f, pb);
+  float s0[NP], s1[NP], s2[NP], s3[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) s0[i] = s1[i] = s2[i] = s3[i] = 0.0f;
   for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
     const int64_t row = p.q * a.rows + i;
-    typename R::Raw xr, ur, rr, hr;
-    R::load(xr, a.x, row, a.K, true);
-    if (a.u) R::load(ur, a.u, row, a.K, true);
-    if (a.dr) R::load(rr, a.dr, row, a.K, true);
-    if (a.dh) R::load(hr, a.dh, row, a.K, true);
-    float x[EPT], u[EPT], g[EPT], fu = 1.0f;
+    float x[EPT], u[EPT], g[EPT], d[EPT], fu = 1.0f;
     R::floats(xr, x);
+    if (a.u) R::floats(ur, u);
+    if (a.dh) R::floats(hr, g);
+    if (a.dr) R::floats(rr, d);
+    if (i + R::ROWS < p.last) fetch(i + R::ROWS);
     if (a.u) {
-      R::floats(ur, u);
-      if (a.pw) fu = R::normed(u, a, red, slot);  // u: uh
+      if (a.pw) {
+        fu = R::normed(u, a, red, slot);  // u: uh
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e], a.pw ? __builtin_fmaf(u[e], pw[e], pb[e]) : u[e], x[e]);
+        for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e / GR], __builtin_fmaf(u[e], pw[e / GR], pb[e / GR]), x[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e / GR], u[e], x[e]);
+      }
     }
     if (a.dh) {
       const float fr = R::normed(x, a, red, slot);  // x: rh
-      R::floats(hr, g);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
-        s0[e] = __builtin_fmaf(g[e], x[e], s0[e]);
-        s1[e] += g[e];
-        g[e] *= w[e];
+        s0[e / GR] = __builtin_fmaf(g[e], x[e], s0[e / GR]);
+        s1[e / GR] += g[e];
+        g[e] *= w[e / GR];
       }
       R::back(g, x, fr, a, red, slot);
+      if (a.dr)
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) g[e] += d[e];
     } else {
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) g[e] = 0.0f;
-    }
-    if (a.dr) {
-      float d[EPT];
-      R::floats(rr, d);
-#pragma unroll
-      for (int e = 0; e < EPT; ++e) g[e] += d[e];
+      for (int e = 0; e < EPT; ++e) g[e] = a.dr ? d[e] : 0.0f;
     }
     if (a.dx) R::store(g, a.dx, row, a.K);
     if (a.u) {
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        s2[e] = __builtin_fmaf(g[e], u[e], s2[e]);
-        s3[e] += g[e];
-        g[e] *= a.pw ? k[e] * pw[e] : k[e];
+      for (int e = 0; e < EPT; ++e) s2[e / GR] = __builtin_fmaf(g[e], u[e], s2[e / GR]);
+      if (a.pw) {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) {
+          s3[e / GR] += g[e];
+          g[e] *= k[e / GR] * pw[e / GR];
+        }
+        if (a.du) R::back(g, u, fu, a, red, slot);
+      } else {
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) g[e] *= k[e / GR];
       }
-      if (a.du) {
-        if (a.pw) R::back(g, u, fu, a, red, slot);
-        R::store(g, a.du, row, a.K);
-      }
+      if (a.du) R::store(g, a.du, row, a.K);
     }
   }
-  float* const part = a.part + (p.q * a.strips + p.strip) * a.J * a.K;
+  const int K = a.K / GR;  // columns of the sums
+  float* const part = a.part + (p.q * a.strips + p.strip) * a.J * K;
   int j = 0;
-  auto put = [&](const float (&s)[EPT]) {
+  auto put = [&](const float (&s)[NP]) {
     if constexpr (R::ROWS > 1) {
-      __syncthreads();
+      if (j) __syncthreads();
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        const int c = R::at(e / R::VEC) + e % R::VEC;
-        if (c < a.K) cols[mine * (LANES * EPT) + c] = s[e];
+      for (int i = 0; i < NP; ++i) {
+        const int c = (R::at(i * GR / R::VEC) + i * GR % R::VEC) / GR;
+        if (c < K) cols[mine * (LANES * NP) + c] = s[i];
       }
       __syncthreads();
-      for (int c = threadIdx.x; c < a.K; c += R::THREADS) {
+      for (int c = threadIdx.x; c < K; c += R::THREADS) {
         float v = cols[c];
 #pragma unroll
-        for (int m = 1; m < R::ROWS; ++m) v += cols[m * (LANES * EPT) + c];
-        part[(int64_t)j * a.K + c] = v;
+        for (int m = 1; m < R::ROWS; ++m) v += cols[m * (LANES * NP) + c];
+        part[(int64_t)j * K + c] = v;
       }
     } else {
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        const int c = R::at(e / R::VEC) + e % R::VEC;
-        if (c < a.K) part[(int64_t)j * a.K + c] = s[e];
+      for (int i = 0; i < NP; ++i) {
+        const int c = (R::at(i * GR / R::VEC) + i * GR % R::VEC) / GR;
+        if (c < K) part[(int64_t)j * K + c] = s[i];
       }
     }
     ++j;
@@ -306,58 +332,51 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE>::THREADS)) void eql_
   }
 }
 
-// sums[q, j, c]: the strips and group elements of a sequence's column sums, and the sequence's gate.  A
-// workgroup takes one channel of one row j.
+// sums[q, j, c]: the strips and group elements of a sequence's column sums.
 template <int UNUSED = 0>
-__global__ __launch_bounds__(256) void eql_res_strips_kernel(const ResArgs a) {
-  int64_t id = a.first + blockIdx.x;
-  const int c = (int)(id % a.C);
-  id /= a.C;
-  const int j = (int)(id % a.J);
-  const int64_t q = id / a.J, n = a.strips * a.T;
-  float v = 0.0f;
-  for (int64_t i = threadIdx.x; i < n; i += 256) v += a.part[((q * a.strips + i / a.T) * a.J + j) * a.K + c * a.T + i % a.T];
-  __shared__ float red[4];
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  if (threadIdx.x == 0) a.sums[(q * a.J + j) * a.C + c] = (red[0] + red[1]) + (red[2] + red[3]);
+__global__ __launch_bounds__(256) void eql_res_strips_kernel(const ResArgs a, int GR, int blocks) {
+  unsigned id = a.first + blockIdx.x;
+  const int block = (int)(id % (unsigned)blocks);
+  id /= (unsigned)blocks;
+  const int j = (int)(id % (unsigned)a.J), T = a.T / GR, K = a.K / GR;
+  const int64_t q = a.seq + id / (unsigned)a.J;
+  column_sums(a.part + (q * a.strips * a.J + j) * K, a.strips, (int64_t)a.J * K, a.C, T, block,
+              [&](int c, float v) { a.sums[(q * a.J + j) * a.C + c] = v; });
 }
-// The parameters' gradients: a wave adds the sequences of a channel.
+// The parameters' gradients: a workgroup takes 64 channels, its waves every fourth sequence.
 template <int DT>
 __global__ __launch_bounds__(256) void eql_res_params_kernel(const ResArgs a) {
   using E = typename Elem<DT>::T;
-  const int c = (int)(a.first + blockIdx.x) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (c >= a.C) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
+  __shared__ float red[5][4][64];
   auto at = [&](const void* p, int64_t i) { return (float)reinterpret_cast<const E*>(p)[i]; };
-  const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
-  float dw = 0.0f, db = 0.0f, ds = 0.0f, dpw = 0.0f, dpb = 0.0f;
-  for (int64_t q = lane; q < a.seqs; q += 64) {
-    const float* s = a.sums + q * a.J * a.C + c;
-    if (a.w) {
-      dw += s[0];
-      db += s[a.C];
-      s += 2 * a.C;
+  float sum[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // dw, db, dscale, dpw, dpb
+  if (c < a.C) {
+    const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
+    for (int64_t q = wave; q < a.seqs; q += 4) {
+      const float* s = a.sums + q * a.J * a.C + c;
+      if (a.w) {
+        sum[0] += s[0];
+        sum[1] += s[a.C];
+        s += 2 * a.C;
+      }
+      if (!a.u) continue;
+      const float gate = a.gate ? at(a.gate, q * a.C + c) : 1.0f, P = s[0], S = a.pw ? s[a.C] : 0.0f;
+      const float e = a.pw ? __builtin_fmaf(pw, P, pb * S) : P;
+      if (a.dgate) reinterpret_cast<E*>(a.dgate)[q * a.C + c] = (E)(scale * e);
+      sum[2] = __builtin_fmaf(gate, e, sum[2]);
+      sum[3] = __builtin_fmaf(gate * scale, P, sum[3]);
+      sum[4] = __builtin_fmaf(gate * scale, S, sum[4]);
     }
-    if (!a.u) continue;
-    const float gate = a.gate ? at(a.gate, q * a.C + c) : 1.0f, P = s[0], S = a.pw ? s[a.C] : 0.0f;
-    const float e = a.pw ? __builtin_fmaf(pw, P, pb * S) : P;
-    if (a.dgate) reinterpret_cast<E*>(a.dgate)[q * a.C + c] = (E)(scale * e);
-    ds = __builtin_fmaf(gate, e, ds);
-    dpw = __builtin_fmaf(gate * scale, P, dpw);
-    dpb = __builtin_fmaf(gate * scale, S, dpb);
   }
-  auto out = [&](void* p, float v) {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    if (p && lane == 0) reinterpret_cast<E*>(p)[c] = (E)v;
-  };
-  out(a.dw, dw);
-  out(a.db, db);
-  out(a.dscale, ds);
-  out(a.dpw, dpw);
-  out(a.dpb, dpb);
+  for (int i = 0; i < 5; ++i) red[i][wave][lane] = sum[i];
+  __syncthreads();
+  if (c >= a.C || wave != 0) return;
+  void* const dst[5] = {a.dw, a.db, a.dscale, a.dpw, a.dpb};
+#pragma unroll
+  for (int i = 0; i < 5; ++i)
+    if (dst[i]) reinterpret_cast<E*>(dst[i])[c] = (E)((red[i][0][lane] + red[i][1][lane]) + (red[i][2][lane] + red[i][3][lane]));
 }
 
 }  // namespace eqk

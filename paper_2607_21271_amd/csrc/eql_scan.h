@@ -18,12 +18,15 @@
 // comes in by exp(A sum d)), and the main pass starts every chunk from its own.
 #pragma once
 #include "eql_common.h"
+#include "eql_colsum.h"
 #include "eql_config.h"
+#include "eql_lanes.h"
 #include "eql_recurrent.h"
 
 namespace eqk {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+constexpr float kAtanh1 = 0.333333198f, kAtanh2 = 0.200038354f, kAtanh3 = 0.141169781f, kAtanh4 = 0.134337737f;
 
 // Reads and writes of LDS by lanes of one wave stay in program order; the compiler must keep it.
 __device__ __forceinline__ void wave_order() {
@@ -31,10 +34,6 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
-}
 // Sum over the NL neighbouring lanes that share columns.
 template <int NL>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -43,16 +42,6 @@ __device__ __forceinline__ float lanes_sum(float v) {
   if constexpr (NL >= 8) v += dpp<0x141>(v);   // half row mirrored: the other quad
   if constexpr (NL >= 16) v += dpp<0x140>(v);  // row mirrored: the other half
   return v;
-}
-__device__ __forceinline__ void swap16(float& u, float& v) {  // odd rows of u with even rows of v
-  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, u), __builtin_bit_cast(unsigned, v), false, false);
-  u = __builtin_bit_cast(float, (unsigned)r[0]);
-  v = __builtin_bit_cast(float, (unsigned)r[1]);
-}
-__device__ __forceinline__ void swap32(float& u, float& v) {  // upper half of u with lower half of v
-  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, u), __builtin_bit_cast(unsigned, v), false, false);
-  u = __builtin_bit_cast(float, (unsigned)r[0]);
-  v = __builtin_bit_cast(float, (unsigned)r[1]);
 }
 // Sums of v0 .. v3 over the lanes with the same place among NL, value r in row r (16 lanes) of the result.
 template <int NL>
@@ -69,45 +58,50 @@ __device__ __forceinline__ float columns_sum(float v0, float v1, float v2, float
   return s;
 }
 
-// log(1 + e) for 0 <= e <= 1 as 2 atanh(e / (2 + e)), the series to the 13th power: 2e-8 of its value.
-__device__ __forceinline__ float log1p_unit(float e) {
+// log(1 + e) / 2 for 0 <= e <= 1: atanh(s) of s = e / (2 + e) <= 1/3 is s p(s^2); p in five terms, economised from the
+// series by Chebyshev polynomials over [0, 1/9], is 1.5e-8 off.
+__device__ __forceinline__ float atanh_unit(float e) {
   const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-  float p = __builtin_fmaf(q, 1.0f / 13.0f, 1.0f / 11.0f);
-  p = __builtin_fmaf(q, p, 1.0f / 9.0f);
-  p = __builtin_fmaf(q, p, 1.0f / 7.0f);
-  p = __builtin_fmaf(q, p, 1.0f / 5.0f);
-  p = __builtin_fmaf(q, p, 1.0f / 3.0f);
+  float p = __builtin_fmaf(q, kAtanh4, kAtanh3);
+  p = __builtin_fmaf(q, p, kAtanh2);
+  p = __builtin_fmaf(q, p, kAtanh1);
   p = __builtin_fmaf(q, p, 1.0f);
-  return 2.0f * s * p;
+  return s * p;
 }
+// NaN stays: it is one of exp(-|v|) too.
 __device__ __forceinline__ float softplus(float v) {
   const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(v));
-  return (v > 0.0f ? v : v < 0.0f ? 0.0f : v) + log1p_unit(e);  // NaN stays
+  return __builtin_fmaf(2.0f, atanh_unit(e), fmaxf(v, 0.0f));
 }
-__device__ __forceinline__ float sigmoid(float v) {
+// softplus and its derivative from one exponential
+__device__ __forceinline__ float softplus(float v, float& slope) {
   const float e = __builtin_amdgcn_exp2f(-kLog2e * __builtin_fabsf(v));
   const float r = __builtin_amdgcn_rcpf(1.0f + e);
-  return v < 0.0f ? e * r : r;
+  slope = v < 0.0f ? e * r : r;
+  return __builtin_fmaf(2.0f, atanh_unit(e), fmaxf(v, 0.0f));
+}
+__device__ __forceinline__ float sigmoid(float v) {  // (exp(-v) of inf gives 0)
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kLog2e * v));
 }
 
-// Where a wave stands.
+// Where a wave stands; the same for all its lanes.
 struct ScanPlace {
-  int64_t b, k;    // sequence, chunk
-  int g, blk;      // group, block of its columns
+  int64_t b;       // sequence
+  int k, g, blk;   // chunk, group, block of its columns
   int col0;        // first column among the padded ones
   int ct0, left;   // first column of the features, columns of the group from it on
   int64_t len;     // tokens that hold data
   int64_t begin, end;
 };
 template <int NL>
-__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int64_t id) {
+__device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, unsigned id) {
   ScanPlace p;
-  p.blk = (int)(id % a.nblk);
-  id /= a.nblk;
-  p.g = (int)(id % a.G);
-  id /= a.G;
-  p.k = id % a.K;
-  p.b = id / a.K;
+  p.blk = (int)(id % (unsigned)a.nblk);
+  id /= (unsigned)a.nblk;
+  p.g = (int)(id % (unsigned)a.G);
+  id /= (unsigned)a.G;
+  p.k = (int)(id % (unsigned)a.K);
+  p.b = a.first + id / (unsigned)a.K;
   p.col0 = (p.g * a.nblk + p.blk) * scan_cols(NL);
   p.ct0 = p.g * a.CTg + p.blk * scan_cols(NL);
   p.left = a.CTg - p.blk * scan_cols(NL);
@@ -116,15 +110,19 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, int64_t id) {
   p.end = min(p.begin + a.chunk, a.L);
   return p;
 }
+__device__ __forceinline__ int scan_channel(const ScanArgs& a, int ct) { return a.mT ? (int)__umulhi((unsigned)ct, a.mT) : ct; }
+
+constexpr uint32_t kScanDrop = 0x80000000u;  // an offset past every resource: loads give 0, stores go nowhere
 
 // The lane's elements of a tile of [TT][CH]: NV vectors of VEC, vector v at token tok(v), column at.
-template <int DT, int NL>
+// WHOLE: vectors through a buffer resource that ends behind the tile's last token, else single elements.
+template <int DT, int NL, bool WHOLE>
 struct ScanTile {
   static constexpr int CH = scan_cols(NL), TT = scan_tile(NL), EPT = scan_ept(NL), VEC = scan_vec(DT, NL);
   static constexpr int NV = EPT / VEC, VT = CH / VEC, EB = DT == kF32 ? 4 : 2;
   static constexpr int W = VEC * EB / 4;  // 32-bit words of a vector
   static constexpr int NP = 4 * NL;
-  static constexpr int NBC = (TT * NP + 63) / 64;  // elements of b, and of c, that a lane loads
+  static constexpr int NB = (TT * NL + 63) / 64;  // runs of four of b, and of c, that a lane loads
   using E = typename Elem<DT>::T;
   struct Raw {
     uint32_t w[NV * W];
@@ -132,61 +130,94 @@ struct ScanTile {
   static __device__ __forceinline__ int at() { return (threadIdx.x & 63) % VT * VEC; }
   static __device__ __forceinline__ int tok(int v) { return v * (64 / VT) + (threadIdx.x & 63) / VT; }
 
-  template <bool WHOLE>
-  static __device__ __forceinline__ void load(Raw& r, const void* base, int64_t stride, int nt, int left) {
-    const E* p = reinterpret_cast<const E*>(base);
+  // A tensor's place in the tile: the lane's byte offsets and the tokens' stride.
+  struct View {
+    const char* p;  // of the wave's first column, sequence and token 0
+    int64_t stride;
+    uint32_t off[WHOLE ? NV : 1];
+  };
+  static __device__ __forceinline__ View view(const void* p, int64_t first, int64_t stride, int left) {
+    View r;
+    r.p = reinterpret_cast<const char*>(p) + first * EB;
+    r.stride = stride;
+    if constexpr (WHOLE) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int t = tok(v);
-      const bool on = t < nt;
-      const E* q = p + t * stride + at();
-      if constexpr (WHOLE) {
-        const bool ok = on && at() < left;
+      for (int v = 0; v < NV; ++v) r.off[v] = at() < left ? (uint32_t)((tok(v) * (int)stride + at()) * EB) : kScanDrop;
+    }
+    return r;
+  }
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const View& w, int64_t l, int rows, int left) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(w.p + l * w.stride * EB), (short)0,
+                                             ((rows - 1) * (int)w.stride + left) * EB, 0x00020000);
+  }
+  // tokens l .. l + nt (nt > 0); what lies behind them may be anything
+  static __device__ __forceinline__ void load(Raw& r, const View& w, int64_t l, int nt, int left) {
+    if constexpr (WHOLE) {
+      const auto rs = resource(w, l, nt, left);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
         if constexpr (W == 4) {
-          const u32x4 x = ok ? *reinterpret_cast<const u32x4*>(q) : u32x4{0, 0, 0, 0};
+          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, w.off[v], 0, 0));
 #pragma unroll
           for (int i = 0; i < 4; ++i) r.w[v * W + i] = x[i];
         } else {
-          const u32x2 x = ok ? *reinterpret_cast<const u32x2*>(q) : u32x2{0, 0};
-#pragma unroll
-          for (int i = 0; i < W; ++i) r.w[v * W + i] = x[i];
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, w.off[v], 0, 0));
+          r.w[v * W] = x[0];
+          r.w[v * W + 1] = x[1];
         }
-      } else if constexpr (EB == 4) {
+      }
+    } else {
+      const E* p = reinterpret_cast<const E*>(w.p) + l * w.stride;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i)
-          r.w[v * W + i] = on && at() + i < left ? __builtin_bit_cast(uint32_t, q[i]) : 0u;
-      } else {
-        const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+      for (int v = 0; v < NV; ++v) {
+        const E* q = p + tok(v) * w.stride + at();
+        const int n = tok(v) < nt ? left - at() : 0;
+        if constexpr (EB == 4) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          const uint32_t lo = on && at() + 2 * i < left ? h[2 * i] : 0u, hi = on && at() + 2 * i + 1 < left ? h[2 * i + 1] : 0u;
-          r.w[v * W + i] = lo | hi << 16;
+          for (int i = 0; i < VEC; ++i) r.w[v * W + i] = i < n ? __builtin_bit_cast(uint32_t, q[i]) : 0u;
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const uint32_t lo = 2 * i < n ? h[2 * i] : 0u, hi = 2 * i + 1 < n ? h[2 * i + 1] : 0u;
+            r.w[v * W + i] = lo | hi << 16;
+          }
         }
       }
     }
   }
   static __device__ __forceinline__ void floats(const Raw& r, float (&f)[EPT]) { raw_to_floats<DT, NV * W>(r.w, f); }
+  // the same words, whose conversion is not kept from an earlier one
+  static __device__ __forceinline__ void again(Raw& r) {
+#pragma unroll
+    for (int i = 0; i < NV * W; ++i) asm volatile("" : "+v"(r.w[i]));
+  }
+  static __device__ __forceinline__ void behind(float (&f)[EPT], int nt) {  // 0 from token nt on
+#pragma unroll
+    for (int e = 0; e < EPT; ++e) f[e] = tok(e / VEC) < nt ? f[e] : 0.0f;
+  }
 
-  // stores the elements of tokens below `rows`
-  template <bool WHOLE>
-  static __device__ __forceinline__ void store(const float (&f)[EPT], void* base, int64_t stride, int rows, int left) {
-    E* p = reinterpret_cast<E*>(base);
+  // stores tokens l .. l + rows
+  static __device__ __forceinline__ void store(const float (&f)[EPT], const View& w, int64_t l, int rows, int left) {
+    if constexpr (WHOLE) {
+      const auto rs = resource(w, l, rows, left);
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int t = tok(v);
-      if (t >= rows) continue;
-      E* q = p + t * stride + at();
-      if constexpr (WHOLE) {
-        if (at() >= left) continue;
-        uint32_t w[W];
+      for (int v = 0; v < NV; ++v) {
+        uint32_t q[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = pack2<DT>(f[v * VEC + i * (4 / EB)], f[v * VEC + i * (4 / EB) + (EB == 2)]);
-        if constexpr (W == 4) *reinterpret_cast<u32x4*>(q) = u32x4{w[0], w[1], w[2], w[3]};
-        else *reinterpret_cast<u32x2*>(q) = u32x2{w[0], w[1]};
-      } else {
+        for (int i = 0; i < W; ++i) q[i] = pack2<DT>(f[v * VEC + i * (4 / EB)], f[v * VEC + i * (4 / EB) + (EB == 2)]);
+        if constexpr (W == 4) __builtin_amdgcn_raw_buffer_store_b128(u32x4{q[0], q[1], q[2], q[3]}, rs, w.off[v], 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b64(u32x2{q[0], q[1]}, rs, w.off[v], 0, 0);
+      }
+    } else {
+      E* p = reinterpret_cast<E*>(const_cast<char*>(w.p)) + l * w.stride;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        E* q = p + tok(v) * w.stride + at();
+        const int n = tok(v) < rows ? left - at() : 0;
 #pragma unroll
         for (int i = 0; i < VEC; ++i)
-          if (at() + i < left) q[i] = (E)f[v * VEC + i];
+          if (i < n) q[i] = (E)f[v * VEC + i];
       }
     }
   }
@@ -209,23 +240,52 @@ struct ScanTile {
         for (int j = 0; j < 4; ++j) f[v * VEC + i + j] = q[j];
       }
   }
-  // b or c of a tile: element i * 64 + lane of [TT][NP]
+  // b or c of a tile: runs of four, i * 64 + lane of [TT][NP / 4]
   struct Bc {
-    E e[NBC];
+    uint32_t w[NB * EB];
   };
-  static __device__ __forceinline__ void load_bc(Bc& r, const void* base, int64_t stride, int nt, int N) {
-    const E* p = reinterpret_cast<const E*>(base);
+  static __device__ __forceinline__ void load_bc(Bc& r, const void* base, int64_t first, int64_t stride, int nt, int N) {
+    const char* p = reinterpret_cast<const char*>(base) + first * EB;
 #pragma unroll
-    for (int i = 0; i < NBC; ++i) {
-      const int j = i * 64 + (threadIdx.x & 63), t = j / NP, n = j % NP;
-      r.e[i] = t < nt && n < N ? p[t * stride + n] : (E)0.0f;
+    for (int i = 0; i < NB; ++i) {
+      const int j = i * 64 + (threadIdx.x & 63), t = j / NL, n = j % NL * 4;
+      if constexpr (WHOLE) {
+        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, ((nt - 1) * (int)stride + N) * EB, 0x00020000);
+        const uint32_t off = n < N && t < nt ? (uint32_t)((t * (int)stride + n) * EB) : kScanDrop;
+        if constexpr (EB == 4) {
+          const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
+#pragma unroll
+          for (int q = 0; q < 4; ++q) r.w[i * 4 + q] = x[q];
+        } else {
+          const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
+          r.w[i * 2] = x[0];
+          r.w[i * 2 + 1] = x[1];
+        }
+      } else {
+        const E* q = reinterpret_cast<const E*>(p) + t * stride + n;
+        const int m = t < nt ? N - n : 0;
+        if constexpr (EB == 4) {
+#pragma unroll
+          for (int o = 0; o < 4; ++o) r.w[i * 4 + o] = o < m ? __builtin_bit_cast(uint32_t, q[o]) : 0u;
+        } else {
+          const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
+#pragma unroll
+          for (int o = 0; o < 2; ++o) {
+            const uint32_t lo = 2 * o < m ? h[2 * o] : 0u, hi = 2 * o + 1 < m ? h[2 * o + 1] : 0u;
+            r.w[i * 2 + o] = lo | hi << 16;
+          }
+        }
+      }
     }
   }
   static __device__ __forceinline__ void put_bc(float* tile, const Bc& r) {
+    float f[NB * 4];
+    raw_to_floats<DT, NB * EB>(r.w, f);
 #pragma unroll
-    for (int i = 0; i < NBC; ++i) {
+    for (int i = 0; i < NB; ++i) {
       const int j = i * 64 + (threadIdx.x & 63);
-      if (TT * NP >= 64 || j < TT * NP) tile[j] = (float)r.e[i];
+      if (TT * NL >= 64 || j < TT * NL)
+        *reinterpret_cast<floatx4*>(tile + j * 4) = floatx4{f[i * 4], f[i * 4 + 1], f[i * 4 + 2], f[i * 4 + 3]};
     }
   }
 };
@@ -235,14 +295,14 @@ template <int NL>
 __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < 4; ++q) {
+    const float* s = a.A + (int64_t)scan_channel(a, p.ct0 + c0 + q) * a.N + n0;
+    const int m = c0 + q < p.left ? a.N - n0 : 0;
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const bool ok = c0 + q < p.left && n0 + n < a.N;
-      A2[q][n] = ok ? a.A[(int64_t)((p.ct0 + c0 + q) / a.T) * a.N + n0 + n] * kLog2e : 0.0f;
-    }
+    for (int n = 0; n < 4; ++n) A2[q][n] = n < m ? s[n] * kLog2e : 0.0f;
+  }
 }
-// The lane's states in [cols][NP] (whole) or [CT][N].
+// The lane's states in [cols][NP] or, for the caller, [CT][N].
 template <int NL>
 __device__ __forceinline__ void load_padded(const float* base, float (&h)[4][4]) {
   const int lane = threadIdx.x & 63;
@@ -264,11 +324,12 @@ __device__ __forceinline__ void store_padded(float* base, const float (&h)[4][4]
 template <int NL>
 __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* base, float (&h)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
+  const bool whole = a.N == 4 * NL && ((uintptr_t)base & 15) == 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
-    if (c0 + q < p.left && a.N == 4 * NL && ((uintptr_t)base & 15) == 0) {
-      const floatx4 v = *reinterpret_cast<const floatx4*>(s);
+    if (whole) {
+      const floatx4 v = c0 + q < p.left ? *reinterpret_cast<const floatx4*>(s) : floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[q][n] = v[n];
     } else {
@@ -280,11 +341,12 @@ __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p
 template <int NL>
 __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& p, float* base, const float (&h)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
+  const bool whole = a.N == 4 * NL && ((uintptr_t)base & 15) == 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     if (c0 + q >= p.left) continue;
     float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
-    if (a.N == 4 * NL && ((uintptr_t)base & 15) == 0) {
+    if (whole) {
       *reinterpret_cast<floatx4*>(s) = floatx4{h[q][0], h[q][1], h[q][2], h[q][3]};
     } else {
 #pragma unroll
@@ -293,22 +355,30 @@ __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& 
     }
   }
 }
-// The parameter of the channels of the lane's vector, v where p is NULL.
+// The parameter of the channels of the lane's vector, 0 outside and where src is NULL.
 template <int VEC>
 __device__ __forceinline__ void scan_param(const ScanArgs& a, const ScanPlace& p, const float* src, int at, float (&f)[VEC]) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) f[i] = src && at + i < p.left ? src[(p.ct0 + at + i) / a.T] : 0.0f;
+  for (int i = 0; i < VEC; ++i) f[i] = src && at + i < p.left ? src[scan_channel(a, p.ct0 + at + i)] : 0.0f;
 }
 
-// One token: a = exp(d A), h = a h + (d x) b.
-__device__ __forceinline__ void scan_step(float (&h)[4][4], const float (&A2)[4][4], const floatx4& d, const floatx4& dx,
-                                          const floatx4& bb) {
+// The decays of a token: exp(d A).
+__device__ __forceinline__ void scan_exp(float (&e)[4][4], const float (&A2)[4][4], const floatx4& d) {
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
-    for (int n = 0; n < 4; ++n)
-      h[q][n] = __builtin_fmaf(__builtin_amdgcn_exp2f(d[q] * A2[q][n]), h[q][n], dx[q] * bb[n]);
+    for (int n = 0; n < 4; ++n) e[q][n] = __builtin_amdgcn_exp2f(d[q] * A2[q][n]);
 }
+__device__ __forceinline__ void scan_step(float (&h)[4][4], const float (&e)[4][4], const floatx4& dx, const floatx4& bb) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) h[q][n] = __builtin_fmaf(e[q][n], h[q][n], dx[q] * bb[n]);
+}
+// End of a token in the loops over them: the next one's decays and words from LDS are on their way by then, so that one
+// wave on a SIMD waits for neither (left to itself the compiler uses an exponential two instructions
+// after it is issued: 980 cycles a token instead of SCAN_CYCLES).
+__device__ __forceinline__ void token_end() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---- forward ---------------------------------------------------------------
 // STATES: only the state that a chunk forms from zero and its sum of d (chunks 0 .. K - 2).
@@ -317,13 +387,13 @@ constexpr int scan_fwd_lds() {  // floats of a wave
   return 2 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
 }
 template <int DT, int NL, bool WHOLE, bool STATES>
-__global__ __launch_bounds__(64 * kScanWaves) void eql_scan_fwd_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL>;
-  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP, EB = TL::EB;
+__global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const ScanArgs a) {
+  using TL = ScanTile<DT, NL, WHOLE>;
+  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t id = (a.first + blockIdx.x) * kScanWaves + wave;
-  if (id >= a.B * a.K * a.G * a.nblk) return;  // (no barrier follows)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned id = blockIdx.x * kScanWaves + wave;
+  if (id >= a.tasks) return;  // (no barrier follows)
   const ScanPlace p = scan_place<NL>(a, id);
   if (STATES && p.k == a.K - 1) return;
   float* const ds = lds + wave * scan_fwd_lds<NL>();
@@ -331,6 +401,22 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_fwd_kernel(const Sca
   float* const bs = us + TT * CH;
   float* const cs = bs + TT * NP;
   const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int64_t stop = min(p.len, p.end);
+  const auto xv = TL::view(a.x, p.b * a.xs[0] + p.ct0, a.xs[1], p.left), dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left);
+  const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left), yv = TL::view(a.y, p.b * a.L * a.CT + p.ct0, a.CT, p.left);
+  typename TL::Raw xr, dr, zr;
+  typename TL::Bc br, cr;
+  auto fetch = [&](int64_t l0) {
+    const int nt = (int)min(stop - l0, (int64_t)TT);
+    TL::load(dr, dv, l0, nt, p.left);
+    TL::load(xr, xv, l0, nt, p.left);
+    TL::load_bc(br, a.b, p.b * a.bs[0] + l0 * a.bs[1] + p.g * a.bs[2], a.bs[1], nt, a.N);
+    if constexpr (!STATES) {
+      TL::load_bc(cr, a.c, p.b * a.cs[0] + l0 * a.cs[1] + p.g * a.cs[2], a.cs[1], nt, a.N);
+      if (a.z) TL::load(zr, zv, l0, nt, p.left);
+    }
+  };
+  if (p.begin < stop) fetch(p.begin);
   float A2[4][4], h[4][4], bias[VEC], skip[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
   scan_decay<NL>(a, p, A2);
   scan_param<VEC>(a, p, a.bias, at, bias);
@@ -343,59 +429,52 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_fwd_kernel(const Sca
     for (int q = 0; q < 4; ++q)
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[q][n] = 0.0f;
-  const int64_t stop = min(p.len, p.end);
-  // addresses of the wave's first token and column
-  auto base = [&](const void* q, const int64_t (&st)[2], int64_t l) { return (const char*)q + (p.b * st[0] + l * st[1] + p.ct0) * EB; };
-  auto bcbase = [&](const void* q, const int64_t (&st)[3], int64_t l) { return (const char*)q + (p.b * st[0] + l * st[1] + p.g * st[2]) * EB; };
-  typename TL::Raw xr, dr, zr;
-  typename TL::Bc br, cr;
-  auto fetch = [&](int64_t l0) {
-    const int nt = (int)min(stop - l0, (int64_t)TT);
-    TL::template load<WHOLE>(xr, base(a.x, a.xs, l0), a.xs[1], nt, p.left);
-    TL::template load<WHOLE>(dr, base(a.delta, a.ds, l0), a.ds[1], nt, p.left);
-    TL::load_bc(br, bcbase(a.b, a.bs, l0), a.bs[1], nt, a.N);
-    if constexpr (!STATES) {
-      if (a.z) TL::template load<WHOLE>(zr, base(a.z, a.zs, l0), a.zs[1], nt, p.left);
-      TL::load_bc(cr, bcbase(a.c, a.cs, l0), a.cs[1], nt, a.N);
-    }
-  };
-  if (p.begin < stop) fetch(p.begin);
   for (int64_t l0 = p.begin; l0 < stop; l0 += TT) {
     const int nt = (int)min(stop - l0, (int64_t)TT);
-    float xf[EPT], df[EPT], zf[EPT];
-    TL::floats(xr, xf);
-    TL::floats(dr, df);
-    if constexpr (!STATES) {
-      if (a.z) TL::floats(zr, zf);
-    }
+    typename TL::Raw xc = xr, zc = zr;  // of this tile, while the next one's are on their way
+    {
+      float xf[EPT], df[EPT];
+      TL::floats(dr, df);
+      TL::floats(xr, xf);
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      df[e] += bias[e % VEC];
-      if (a.softplus) df[e] = softplus(df[e]);
-      if (TL::tok(e / VEC) >= nt) df[e] = 0.0f;
-    }
-    wave_order();  // the tile before has been read
-    TL::put(ds, df);
+      for (int e = 0; e < EPT; ++e) df[e] += bias[e % VEC];
+      if (a.softplus)
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) df[e] = TL::tok(e / VEC) >= nt ? 0.0f : df[e] * xf[e];
-    TL::put(us, df);
-    TL::put_bc(bs, br);
-    if constexpr (!STATES) TL::put_bc(cs, cr);
+        for (int e = 0; e < EPT; ++e) df[e] = softplus(df[e]);
+      if (nt < TT) {
+        TL::behind(df, nt);
+        TL::behind(xf, nt);
+      }
+      wave_order();  // the tile before has been read
+      TL::put(ds, df);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) df[e] *= xf[e];
+      TL::put(us, df);
+      TL::put_bc(bs, br);
+      if constexpr (!STATES) TL::put_bc(cs, cr);
+    }
     if (l0 + TT < stop) fetch(l0 + TT);
     if constexpr (!STATES)
       if (a.states) store_padded<NL>(a.states + ((p.b * a.tiles + l0 / TT) * a.cols + p.col0) * NP, h);
     wave_order();
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * CH + c0); };
+    auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * NP + n0); };
+    float part[4] = {0.f, 0.f, 0.f, 0.f}, e0[4][4], e1[4][4];
+    floatx4 d = cols(ds, 0), u = cols(us, 0), bb = rows(bs, 0), cc = {};
+    if constexpr (!STATES) cc = rows(cs, 0);
+    scan_exp(e0, A2, d);
+    floatx4 d1 = cols(ds, 1);
+#pragma unroll
     for (int t = 0; t < TT; ++t) {
-      const floatx4 d = *reinterpret_cast<const floatx4*>(ds + t * CH + c0), u = *reinterpret_cast<const floatx4*>(us + t * CH + c0);
-      const floatx4 bb = *reinterpret_cast<const floatx4*>(bs + t * NP + n0);
-      scan_step(h, A2, d, u, bb);
+      const floatx4 d2 = cols(ds, t + 2), u1 = cols(us, t + 1), b1 = rows(bs, t + 1);
+      floatx4 c1 = {};
+      if constexpr (!STATES) c1 = rows(cs, t + 1);
+      if (t + 1 < TT) scan_exp(e1, A2, d1);
+      scan_step(h, e0, u, bb);
       if constexpr (STATES) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) part[q] += d[q];
       } else {
-        const floatx4 cc = *reinterpret_cast<const floatx4*>(cs + t * NP + n0);
         floatx4 y;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -404,24 +483,40 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_fwd_kernel(const Sca
           for (int n = 1; n < 4; ++n) s = __builtin_fmaf(h[q][n], cc[n], s);
           y[q] = lanes_sum<NL>(s);
         }
-        // in place of d x, which every lane of these columns has read
-        if (lane % NL == 0) *reinterpret_cast<floatx4*>(us + t * CH + c0) = y;
+        // in place of d x, which every lane of these columns has read; all of them write what all of them hold (a
+        // branch here would keep the next token's reads behind it)
+        *reinterpret_cast<floatx4*>(us + t * CH + c0) = y;
       }
+      d = d1;
+      d1 = d2;
+      u = u1;
+      bb = b1;
+      cc = c1;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
+      token_end();
     }
     if constexpr (STATES) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) total[q] += part[q];
     } else {
       wave_order();
-      float yf[EPT];
+      float xf[EPT], yf[EPT];
       TL::get(us, yf);
+      TL::again(xc);
+      TL::floats(xc, xf);
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        yf[e] = __builtin_fmaf(skip[e % VEC], xf[e], yf[e]);
-        if (a.z) yf[e] *= zf[e] * sigmoid(zf[e]);
-        if (TL::tok(e / VEC) >= nt) yf[e] = 0.0f;
+      for (int e = 0; e < EPT; ++e) yf[e] = __builtin_fmaf(skip[e % VEC], xf[e], yf[e]);
+      if (a.z) {
+        TL::again(zc);
+        TL::floats(zc, xf);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) yf[e] *= xf[e] * sigmoid(xf[e]);
       }
-      TL::template store<WHOLE>(yf, (char*)a.y + ((p.b * a.L + l0) * a.CT + p.ct0) * EB, a.CT, (int)min(p.end - l0, (int64_t)TT), p.left);
+      if (nt < TT) TL::behind(yf, nt);
+      TL::store(yf, yv, l0, (int)min(p.end - l0, (int64_t)TT), p.left);
     }
   }
   if constexpr (STATES) {
@@ -432,60 +527,83 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_fwd_kernel(const Sca
 #pragma unroll
     for (int e = 0; e < EPT; ++e) zero[e] = 0.0f;
     const int64_t from = p.begin + (max(stop - p.begin, (int64_t)0) + TT - 1) / TT * TT;  // tiles of padding alone
-    for (int64_t l0 = from; l0 < p.end; l0 += TT)
-      TL::template store<WHOLE>(zero, (char*)a.y + ((p.b * a.L + l0) * a.CT + p.ct0) * EB, a.CT, (int)min(p.end - l0, (int64_t)TT), p.left);
+    for (int64_t l0 = from; l0 < p.end; l0 += TT) TL::store(zero, yv, l0, (int)min(p.end - l0, (int64_t)TT), p.left);
     if (a.hT && p.k == a.K - 1) store_state<NL>(a, p, a.hT, h);
   }
 }
 
 // Carries the states over the chunks of a sequence, in place: what a chunk formed from zero becomes what it
-// starts from.  BACK: from the last chunk to the first, the gradient behind a chunk.  A thread takes one column's state.
+// starts from.  BACK: from the last chunk to the first, the gradient behind a chunk.  A thread takes one
+// column's state and reads kScanAhead chunks before it needs the first.
+constexpr int kScanAhead = 32;
 template <bool BACK>
-__global__ __launch_bounds__(256) void eql_scan_carry_kernel(const ScanArgs a, int NP) {
-  const int64_t i = (a.first + blockIdx.x) * 256 + threadIdx.x, per = (int64_t)a.cols * NP;
-  if (i >= a.B * per) return;
-  const int64_t b = i / per;
+__global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, int NP) {
+  const unsigned per = (unsigned)a.cols * NP, i = blockIdx.x * 64 + threadIdx.x;
+  const int64_t b = a.first + i / per;
   const int col = (int)(i % per / NP), n = (int)(i % NP);
   const int CH = 1024 / NP;  // columns of a wave's block
   const int g = col / (a.nblk * CH), in = col - g * a.nblk * CH;
   const bool real = in < a.CTg && n < a.N;
   const int ct = g * a.CTg + in;
-  const float A2 = real ? a.A[(int64_t)(ct / a.T) * a.N + n] * kLog2e : 0.0f;
+  const float A2 = real ? a.A[(int64_t)scan_channel(a, ct) * a.N + n] * kLog2e : 0.0f;
   const float* first = BACK ? a.dhT : a.h0;
   float h = first && real ? first[(b * a.CT + ct) * a.N + n] : 0.0f;
-  float* c = a.carry + (b * a.K * a.cols + col) * NP + n;
-  const float* s = a.sums + b * a.K * a.cols + col;
-  const int64_t cstep = (int64_t)a.cols * NP;
+  const int64_t cstep = (BACK ? -1 : 1) * (int64_t)a.cols * NP, sstep = (BACK ? -1 : 1) * (int64_t)a.cols;
+  const int from = BACK ? a.K - 1 : 0;
+  float* c = a.carry + ((b * a.K + from) * a.cols + col) * NP + n;
+  const float* s = a.sums + (b * a.K + from) * a.cols + col;
   // the first chunk of the way has nothing before it; the last one's own result is not wanted
-  float v = c[(BACK ? a.K - 1 : 0) * cstep], d = s[(int64_t)(BACK ? a.K - 1 : 0) * a.cols];
-  for (int j = 0; j < a.K - 1; ++j) {
-    const int64_t k = BACK ? a.K - 1 - j : j, next = BACK ? k - 1 : k + 1;
-    const bool more = j + 1 < a.K - 1;
-    const float v1 = more ? c[next * cstep] : 0.0f, d1 = more ? s[next * a.cols] : 0.0f;
-    c[k * cstep] = h;
-    h = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2), h, v);
-    v = v1;
-    d = d1;
+  for (int j = 0; j < a.K - 1; j += kScanAhead) {
+    float v[kScanAhead], d[kScanAhead];
+    const int m = min(a.K - 1 - j, kScanAhead);
+#pragma unroll
+    for (int k = 0; k < kScanAhead; ++k)
+      if (k < m) {
+        v[k] = c[k * cstep];
+        d[k] = s[k * sstep];
+      }
+#pragma unroll
+    for (int k = 0; k < kScanAhead; ++k)
+      if (k < m) {
+        c[k * cstep] = h;
+        h = __builtin_fmaf(__builtin_amdgcn_exp2f(d[k] * A2), h, v[k]);
+      }
+    c += m * cstep;
+    s += m * sstep;
   }
-  c[(BACK ? 0 : a.K - 1) * cstep] = h;
+  *c = h;
 }
 
 // ---- gradients ---------------------------------------------------------------
 // r behind a chunk from zero, and its sum of d (chunks 1 .. K - 1): r = a (c s + r) from the last token to the first.
 template <int DT, int NL, bool WHOLE>
-__global__ __launch_bounds__(64 * kScanWaves) void eql_scan_back_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL>;
-  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP, EB = TL::EB;
+__global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const ScanArgs a) {
+  using TL = ScanTile<DT, NL, WHOLE>;
+  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t id = (a.first + blockIdx.x) * kScanWaves + wave;
-  if (id >= a.B * a.K * a.G * a.nblk) return;  // (no barrier follows)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned id = blockIdx.x * kScanWaves + wave;
+  if (id >= a.tasks) return;  // (no barrier follows)
   const ScanPlace p = scan_place<NL>(a, id);
   if (p.k == 0) return;
   float* const ds = lds + wave * scan_fwd_lds<NL>();
   float* const ss = ds + TT * CH;
   float* const cs = ss + TT * CH;
   const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int64_t stop = min(p.len, p.end);
+  const auto dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left), gv = TL::view(a.dy, p.b * a.L * a.CT + p.ct0, a.CT, p.left);
+  const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left);
+  typename TL::Raw yr, dr, zr;
+  typename TL::Bc cr;
+  auto fetch = [&](int64_t l0) {
+    const int nt = (int)min(stop - l0, (int64_t)TT);
+    TL::load(dr, dv, l0, nt, p.left);
+    TL::load(yr, gv, l0, nt, p.left);
+    if (a.z) TL::load(zr, zv, l0, nt, p.left);
+    TL::load_bc(cr, a.c, p.b * a.cs[0] + l0 * a.cs[1] + p.g * a.cs[2], a.cs[1], nt, a.N);
+  };
+  const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
+  if (tiles > 0) fetch(p.begin + (tiles - 1) * TT);
   float A2[4][4], r[4][4], bias[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
   scan_decay<NL>(a, p, A2);
   scan_param<VEC>(a, p, a.bias, at, bias);
@@ -493,54 +611,58 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_back_kernel(const Sc
   for (int q = 0; q < 4; ++q)
 #pragma unroll
     for (int n = 0; n < 4; ++n) r[q][n] = 0.0f;
-  const int64_t stop = min(p.len, p.end);
-  auto base = [&](const void* q, const int64_t (&st)[2], int64_t l) { return (const char*)q + (p.b * st[0] + l * st[1] + p.ct0) * EB; };
-  typename TL::Raw yr, dr, zr;
-  typename TL::Bc cr;
-  auto fetch = [&](int64_t l0) {
-    const int nt = (int)min(stop - l0, (int64_t)TT);
-    TL::template load<WHOLE>(yr, (const char*)a.dy + ((p.b * a.L + l0) * a.CT + p.ct0) * EB, a.CT, nt, p.left);
-    TL::template load<WHOLE>(dr, base(a.delta, a.ds, l0), a.ds[1], nt, p.left);
-    if (a.z) TL::template load<WHOLE>(zr, base(a.z, a.zs, l0), a.zs[1], nt, p.left);
-    TL::load_bc(cr, (const char*)a.c + (p.b * a.cs[0] + l0 * a.cs[1] + p.g * a.cs[2]) * EB, a.cs[1], nt, a.N);
-  };
-  const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
-  if (tiles > 0) fetch(p.begin + (tiles - 1) * TT);
   for (int64_t tile = tiles - 1; tile >= 0; --tile) {
     const int64_t l0 = p.begin + tile * TT;
     const int nt = (int)min(stop - l0, (int64_t)TT);
-    float sf[EPT], df[EPT], zf[EPT];
-    TL::floats(yr, sf);
-    TL::floats(dr, df);
-    if (a.z) {
-      TL::floats(zr, zf);
+    {
+      float sf[EPT], df[EPT];
+      TL::floats(yr, sf);
+      TL::floats(dr, df);
+      if (a.z) {
+        float zf[EPT];
+        TL::floats(zr, zf);
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
-    }
+        for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
+      }
 #pragma unroll
-    for (int e = 0; e < EPT; ++e) {
-      df[e] += bias[e % VEC];
-      if (a.softplus) df[e] = softplus(df[e]);
-      if (TL::tok(e / VEC) >= nt) df[e] = sf[e] = 0.0f;
+      for (int e = 0; e < EPT; ++e) df[e] += bias[e % VEC];
+      if (a.softplus)
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) df[e] = softplus(df[e]);
+      if (nt < TT) {
+        TL::behind(df, nt);
+        TL::behind(sf, nt);
+      }
+      wave_order();
+      TL::put(ds, df);
+      TL::put(ss, sf);
+      TL::put_bc(cs, cr);
     }
-    wave_order();
-    TL::put(ds, df);
-    TL::put(ss, sf);
-    TL::put_bc(cs, cr);
     if (tile > 0) fetch(l0 - TT);
     wave_order();
-    float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + max(t, 0) * CH + c0); };
+    auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + max(t, 0) * NP + n0); };
+    float part[4] = {0.f, 0.f, 0.f, 0.f}, e0[4][4], e1[4][4];
+    floatx4 d = cols(ds, TT - 1), s = cols(ss, TT - 1), cc = rows(cs, TT - 1), d1 = cols(ds, TT - 2);
+    scan_exp(e0, A2, d);
+#pragma unroll
     for (int t = TT - 1; t >= 0; --t) {
-      const floatx4 d = *reinterpret_cast<const floatx4*>(ds + t * CH + c0), s = *reinterpret_cast<const floatx4*>(ss + t * CH + c0);
-      const floatx4 cc = *reinterpret_cast<const floatx4*>(cs + t * NP + n0);
+      const floatx4 d2 = cols(ds, t - 2), s1 = cols(ss, t - 1), c1 = rows(cs, t - 1);
+      if (t > 0) scan_exp(e1, A2, d1);
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         part[q] += d[q];
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-          r[q][n] = __builtin_amdgcn_exp2f(d[q] * A2[q][n]) * __builtin_fmaf(cc[n], s[q], r[q][n]);
+        for (int n = 0; n < 4; ++n) {
+          r[q][n] = e0[q][n] * __builtin_fmaf(cc[n], s[q], r[q][n]);
+          e0[q][n] = e1[q][n];
+        }
       }
+      d = d1;
+      d1 = d2;
+      s = s1;
+      cc = c1;
+      token_end();
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) total[q] += part[q];
@@ -566,18 +688,16 @@ constexpr int scan_bwd_bytes(int waves) {
   return waves * (scan_bwd_lds<NL>() + scan_red_lds<NL>()) * 4;
 }
 template <int DT, int NL, bool WHOLE, int SUB>
-__global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
-  using TL = ScanTile<DT, NL>;
-  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP, EB = TL::EB;
+__global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
+  using TL = ScanTile<DT, NL, WHOLE>;
+  constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   using E = typename TL::E;
   extern __shared__ __attribute__((aligned(16))) float smem[];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // workgroup: (sequence, chunk, group, run of `waves` blocks)
-  int64_t id = a.first + blockIdx.x;
-  const int run = (int)(id % a.P);
-  id /= a.P;
+  const int run = (int)(blockIdx.x % (unsigned)a.P);
   const bool on = run * waves + wave < a.nblk;
-  ScanPlace p = scan_place<NL>(a, id * a.nblk + min(run * waves + wave, a.nblk - 1));
+  ScanPlace p = scan_place<NL>(a, blockIdx.x / (unsigned)a.P * (unsigned)a.nblk + (unsigned)min(run * waves + wave, a.nblk - 1));
   if (!on) p.left = 0;
   float* const ds = smem + wave * scan_bwd_lds<NL>();
   float* const us = ds + TT * CH;
@@ -586,6 +706,15 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
   float* const cs = bs + TT * NP;
   float* const red = smem + waves * scan_bwd_lds<NL>();  // [2][waves][TT][2][NP]
   const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int64_t stop = min(p.len, p.end);
+  const auto xv = TL::view(a.x, p.b * a.xs[0] + p.ct0, a.xs[1], p.left), dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left);
+  const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left);
+  auto gv = TL::view(a.dy, p.b * a.L * a.CT + p.ct0, a.CT, p.left);  // the dense tensors
+  auto dense = [&](const void* q) {
+    auto v = gv;
+    v.p = (const char*)q + (p.b * a.L * a.CT + p.ct0) * TL::EB;
+    return v;
+  };
   float A2[4][4], g[4][4], dA[4][4], bias[VEC], skip[VEC], dskip[VEC], dbias[VEC];
   scan_decay<NL>(a, p, A2);
   scan_param<VEC>(a, p, a.bias, at, bias);
@@ -598,12 +727,7 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
     for (int n = 0; n < 4; ++n) g[q][n] = dA[q][n] = 0.0f;
   const int64_t slot = (p.b * a.K + p.k) * a.cols + p.col0;
   if (a.K > 1 && on) load_padded<NL>(a.carry + slot * NP, g);
-  else if (a.dhT) load_state<NL>(a, p, a.dhT, g);
-  const int64_t stop = min(p.len, p.end);
-  auto base = [&](const void* q, const int64_t (&st)[2], int64_t l) { return (const char*)q + (p.b * st[0] + l * st[1] + p.ct0) * EB; };
-  auto dense = [&](const void* q, int64_t l) { return (char*)q + ((p.b * a.L + l) * a.CT + p.ct0) * EB; };
-  auto bcbase = [&](const void* q, const int64_t (&st)[3], int64_t l) { return (const char*)q + (p.b * st[0] + l * st[1] + p.g * st[2]) * EB; };
-  const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
+  else if (a.K == 1 && a.dhT) load_state<NL>(a, p, a.dhT, g);
   float* const part = a.part + (p.b * a.K + p.k) * (a.N + 2) * a.cols + p.col0;
   int odd = 0, turns = 0;
   bool flushed = false;
@@ -623,18 +747,32 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
 #pragma unroll
       for (int n = 0; n < 4; ++n) dA[q][n] = 0.0f;
   };
+  // the tile's elements: read ahead for the scan, and again, from the caches, for what follows it
+  typename TL::Raw xr, dr, zr, yr;
+  typename TL::Bc br, cr;
+  auto fetch = [&](int64_t l0) {
+    const int nt = (int)min(stop - l0, (int64_t)TT);
+    TL::load(xr, xv, l0, nt, p.left);
+    TL::load(dr, dv, l0, nt, p.left);
+    TL::load(yr, gv, l0, nt, p.left);
+    if (a.z) TL::load(zr, zv, l0, nt, p.left);
+  };
+  auto fetch_bc = [&](int64_t l0) {
+    const int nt = (int)min(stop - l0, (int64_t)TT);
+    TL::load_bc(br, a.b, p.b * a.bs[0] + l0 * a.bs[1] + p.g * a.bs[2], a.bs[1], nt, a.N);
+    TL::load_bc(cr, a.c, p.b * a.cs[0] + l0 * a.cs[1] + p.g * a.cs[2], a.cs[1], nt, a.N);
+  };
+  const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
+  auto start = [&](int64_t tile) { return a.states + ((p.b * a.tiles + p.begin / TT + tile) * a.cols + p.col0) * NP; };
+  float hs[4][4] = {};  // the state before the tile
+  if (tiles > 0) {
+    fetch(p.begin + (tiles - 1) * TT);
+    fetch_bc(p.begin + (tiles - 1) * TT);
+    if (on) load_padded<NL>(start(tiles - 1), hs);
+  }
   for (int64_t tile = tiles - 1; tile >= 0; --tile, odd ^= 1) {
     const int64_t l0 = p.begin + tile * TT;
     const int nt = (int)min(stop - l0, (int64_t)TT);
-    // the tile's elements: read here for the scan and again, from the caches, for what follows it
-    typename TL::Raw xr, dr, zr, yr;
-    auto fetch = [&] {
-      TL::template load<WHOLE>(xr, base(a.x, a.xs, l0), a.xs[1], nt, p.left);
-      TL::template load<WHOLE>(dr, base(a.delta, a.ds, l0), a.ds[1], nt, p.left);
-      TL::template load<WHOLE>(yr, dense(a.dy, l0), a.CT, nt, p.left);
-      if (a.z) TL::template load<WHOLE>(zr, base(a.z, a.zs, l0), a.zs[1], nt, p.left);
-    };
-    fetch();
     {
       float xf[EPT], df[EPT], sf[EPT];
       TL::floats(xr, xf);
@@ -647,45 +785,70 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
         for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
       }
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        df[e] += bias[e % VEC];
-        if (a.softplus) df[e] = softplus(df[e]);
-        if (TL::tok(e / VEC) >= nt) df[e] = sf[e] = 0.0f;
-        dskip[e % VEC] = __builtin_fmaf(sf[e], xf[e], dskip[e % VEC]);
+      for (int e = 0; e < EPT; ++e) df[e] += bias[e % VEC];
+      if (a.softplus)
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) df[e] = softplus(df[e]);
+      if (nt < TT) {
+        TL::behind(df, nt);
+        TL::behind(xf, nt);
+        TL::behind(sf, nt);
       }
-      typename TL::Bc br, cr;
-      TL::load_bc(br, bcbase(a.b, a.bs, l0), a.bs[1], nt, a.N);
-      TL::load_bc(cr, bcbase(a.c, a.cs, l0), a.cs[1], nt, a.N);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) dskip[e % VEC] = __builtin_fmaf(sf[e], xf[e], dskip[e % VEC]);
       wave_order();
       TL::put(ds, df);
       TL::put(ss, sf);
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) df[e] = TL::tok(e / VEC) >= nt ? 0.0f : df[e] * xf[e];
+      for (int e = 0; e < EPT; ++e) df[e] *= xf[e];
       TL::put(us, df);
       TL::put_bc(bs, br);
       TL::put_bc(cs, cr);
     }
+    if (tile > 0) fetch_bc(l0 - TT);
     wave_order();
     float* const mine = red + ((odd * waves + wave) * TT * 2) * NP;
-    const float* const start = a.states + ((p.b * a.tiles + l0 / TT) * a.cols + p.col0) * NP;
+    auto token = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * CH + c0); };
+    auto states = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * NP + n0); };
 #pragma unroll 1
     for (int s0 = TT - SUB; s0 >= 0; s0 -= SUB) {
-      float h[4][4] = {}, H[SUB][4][4];  // H[i]: the state before token s0 + i
-      if (on) load_padded<NL>(start, h);
-#pragma unroll 4
-      for (int t = 0; t < s0; ++t)
-        scan_step(h, A2, *reinterpret_cast<const floatx4*>(ds + t * CH + c0), *reinterpret_cast<const floatx4*>(us + t * CH + c0),
-                  *reinterpret_cast<const floatx4*>(bs + t * NP + n0));
+      float h[4][4], H[SUB][4][4], e0[4][4], e1[4][4];  // H[i]: the state before token s0 + i
 #pragma unroll
-      for (int i = 0; i < SUB; ++i) {
-        const int t = s0 + i;
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) h[q][n] = hs[q][n];
+      if (s0 == 0 && tile > 0 && on) load_padded<NL>(start(tile - 1), hs);  // for the next tile, while this run is worked on
+      scan_exp(e0, A2, token(ds, 0));
+#pragma unroll 2
+      for (int t = 0; t < s0; ++t) {
+        scan_exp(e1, A2, token(ds, t + 1));
+        scan_step(h, e0, token(us, t), states(bs, t));
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int n = 0; n < 4; ++n) H[i][q][n] = h[q][n];
-        scan_step(h, A2, *reinterpret_cast<const floatx4*>(ds + t * CH + c0), *reinterpret_cast<const floatx4*>(us + t * CH + c0),
-                  *reinterpret_cast<const floatx4*>(bs + t * NP + n0));
-        __builtin_amdgcn_sched_barrier(0);
+          for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
+      }
+      {
+        floatx4 u = token(us, s0), bb = states(bs, s0), d1 = token(ds, s0 + 1);
+#pragma unroll
+        for (int i = 0; i < SUB; ++i) {
+          const int t1 = s0 + (i + 1 < SUB ? i + 1 : i), t2 = s0 + (i + 2 < SUB ? i + 2 : SUB - 1);
+          const floatx4 u1 = token(us, t1), b1 = states(bs, t1), d2 = token(ds, t2);
+          if (i + 1 < SUB) scan_exp(e1, A2, d1);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) H[i][q][n] = h[q][n];
+          scan_step(h, e0, u, bb);
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
+          u = u1;
+          bb = b1;
+          d1 = d2;
+          token_end();
+        }
       }
       // the way back reads the tokens and forms the exponentials again: kept, they would take as many registers
       // as the states
@@ -694,14 +857,37 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
       for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int n = 0; n < 4; ++n) asm volatile("" : "+v"(A2[q][n]));
+      floatx4 d = token(ds, s0 + SUB - 1), u = token(us, s0 + SUB - 1), s = token(ss, s0 + SUB - 1);
+      floatx4 bb = states(bs, s0 + SUB - 1), cc = states(cs, s0 + SUB - 1), d1 = token(ds, s0 + SUB - 2);
+      scan_exp(e0, A2, d);
+      floatx4 gb = {}, ga = {}, ch = {};
+      float db[4] = {}, dc[4] = {};
+      // the sums over lanes of a token are taken beside the next one's products
+      auto sums = [&](int t) {
+        floatx4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(gb[q]);
+        // d, d x and s of this token have been read by every lane of these columns; lanes that hold the same sums write
+        // them alike, without a branch
+        *reinterpret_cast<floatx4*>(us + t * CH + c0) = v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ga[q]);
+        *reinterpret_cast<floatx4*>(ds + t * CH + c0) = v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ch[q]);
+        *reinterpret_cast<floatx4*>(ss + t * CH + c0) = v;
+        mine[(t * 2) * NP + n0 + lane / 16] = columns_sum<NL>(db[0], db[1], db[2], db[3]);  // state n0 + row
+        mine[(t * 2 + 1) * NP + n0 + lane / 16] = columns_sum<NL>(dc[0], dc[1], dc[2], dc[3]);
+      };
 #pragma unroll
       for (int i = SUB - 1; i >= 0; --i) {
-        const int t = s0 + i;
-        const floatx4 d = *reinterpret_cast<const floatx4*>(ds + t * CH + c0), u = *reinterpret_cast<const floatx4*>(us + t * CH + c0);
-        const floatx4 s = *reinterpret_cast<const floatx4*>(ss + t * CH + c0);
-        const floatx4 bb = *reinterpret_cast<const floatx4*>(bs + t * NP + n0), cc = *reinterpret_cast<const floatx4*>(cs + t * NP + n0);
-        float db[4] = {0.f, 0.f, 0.f, 0.f}, dc[4] = {0.f, 0.f, 0.f, 0.f};
-        floatx4 gb, ga, ch;
+        const int t = s0 + i, before = i ? t - 1 : t, before2 = i > 1 ? t - 2 : s0;
+        // the tokens before are read while this one is worked on
+        const floatx4 d2 = token(ds, before2), u1 = token(us, before), s1 = token(ss, before), b1 = states(bs, before), c1 = states(cs, before);
+        if (i > 0) scan_exp(e1, A2, d1);
+        if (i + 1 < SUB) sums(t + 1);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) db[n] = dc[n] = 0.0f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           float sb = 0.0f, sa = 0.0f, sc = 0.0f;
@@ -713,68 +899,76 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
             sc = __builtin_fmaf(cc[n], now, sc);
             db[n] = __builtin_fmaf(g[q][n], u[q], db[n]);
             sb = __builtin_fmaf(g[q][n], bb[n], sb);
-            g[q][n] *= __builtin_amdgcn_exp2f(d[q] * A2[q][n]);
+            g[q][n] *= e0[q][n];
             const float m = g[q][n] * H[i][q][n];
             sa = __builtin_fmaf(A2[q][n], m, sa);
             dA[q][n] = __builtin_fmaf(d[q], m, dA[q][n]);
+            e0[q][n] = e1[q][n];
           }
-          gb[q] = lanes_sum<NL>(sb);
-          ga[q] = lanes_sum<NL>(sa);
-          ch[q] = lanes_sum<NL>(sc);
+          gb[q] = sb;
+          ga[q] = sa;
+          ch[q] = sc;
         }
-        // d, d x and s of this token have been read by every lane of these columns
-        if (lane % NL == 0) {
-          *reinterpret_cast<floatx4*>(us + t * CH + c0) = gb;
-          *reinterpret_cast<floatx4*>(ds + t * CH + c0) = ga;
-          *reinterpret_cast<floatx4*>(ss + t * CH + c0) = ch;
-        }
-        const float rb = columns_sum<NL>(db[0], db[1], db[2], db[3]), rc = columns_sum<NL>(dc[0], dc[1], dc[2], dc[3]);
-        if (lane % 16 < NL) {  // state n0 + row
-          mine[(t * 2) * NP + n0 + lane / 16] = rb;
-          mine[(t * 2 + 1) * NP + n0 + lane / 16] = rc;
-        }
-        __builtin_amdgcn_sched_barrier(0);  // bounds what is read ahead: the states take the registers
+        d = d1;
+        d1 = d2;
+        u = u1;
+        s = s1;
+        bb = b1;
+        cc = c1;
+        token_end();
       }
+      sums(s0);
     }
     if (++turns == 32) {  // sums of no more than 32 tiles in registers, so that long ones lose no digits
       turns = 0;
       flush();
     }
     wave_order();
-    fetch();
     {
-      float xf[EPT], df[EPT], sf[EPT], f[EPT], o[EPT];
+      float xf[EPT], f[EPT], o[EPT];
+      TL::again(xr);
+      TL::again(dr);
+      TL::again(yr);
       TL::floats(xr, xf);
-      TL::floats(dr, df);
-      TL::floats(yr, sf);
-      TL::get(us, f);  // sum_n g b
       const int rows = (int)min(p.end - l0, (int64_t)TT);
+      float sf[EPT];
+      TL::floats(yr, sf);
       if (a.z) {
         float zf[EPT], ch[EPT];
+        TL::again(zr);
         TL::floats(zr, zf);
         TL::get(ss, ch);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
           const float sg = sigmoid(zf[e]), y0 = __builtin_fmaf(skip[e % VEC], xf[e], ch[e]);
-          ch[e] = TL::tok(e / VEC) >= nt ? 0.0f : sf[e] * y0 * sg * __builtin_fmaf(zf[e], 1.0f - sg, 1.0f);
+          ch[e] = sf[e] * y0 * sg * __builtin_fmaf(zf[e], 1.0f - sg, 1.0f);
           sf[e] *= zf[e] * sg;
         }
-        if (a.dz) TL::template store<WHOLE>(ch, dense(a.dz, l0), a.CT, rows, p.left);
+        if (nt < TT) TL::behind(ch, nt);
+        if (a.dz) TL::store(ch, dense(a.dz), l0, rows, p.left);
       }
-      TL::get(ds, o);  // sum_n A a g h, times log2(e)
+      TL::floats(dr, o);
+      TL::get(us, f);  // sum_n g b
+      float sa[EPT];
+      TL::get(ds, sa);  // sum_n A a g h, times log2(e)
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
-        const bool in = TL::tok(e / VEC) < nt;
-        const float v = df[e] + bias[e % VEC];
-        const float d = a.softplus ? softplus(v) : v, dd = __builtin_fmaf(kLn2, o[e], xf[e] * f[e]);
-        const float dv = a.softplus ? dd * sigmoid(v) : dd;
-        o[e] = in ? dv : 0.0f;
-        dbias[e % VEC] += o[e];
-        f[e] = in ? __builtin_fmaf(skip[e % VEC], sf[e], d * f[e]) : 0.0f;
+        const float v = o[e] + bias[e % VEC];
+        float slope = 1.0f;
+        const float d = a.softplus ? softplus(v, slope) : v;
+        o[e] = __builtin_fmaf(kLn2, sa[e], xf[e] * f[e]) * slope;
+        f[e] = __builtin_fmaf(skip[e % VEC], sf[e], d * f[e]);
       }
-      TL::template store<WHOLE>(o, dense(a.ddelta, l0), a.CT, rows, p.left);
-      TL::template store<WHOLE>(f, dense(a.dx, l0), a.CT, rows, p.left);
+      if (nt < TT) {
+        TL::behind(o, nt);
+        TL::behind(f, nt);
+      }
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) dbias[e % VEC] += o[e];
+      TL::store(o, dense(a.ddelta), l0, rows, p.left);
+      TL::store(f, dense(a.dx), l0, rows, p.left);
     }
+    if (tile > 0) fetch(l0 - TT);
     __syncthreads();  // (every wave of the workgroup walks the same tiles)
     for (int i = threadIdx.x; i < nt * 2 * NP; i += 64 * waves) {
       float v = red[odd * waves * TT * 2 * NP + i];
@@ -792,9 +986,9 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
     for (int e = 0; e < EPT; ++e) zero[e] = 0.0f;
     for (int64_t l0 = p.begin + tiles * TT; l0 < p.end; l0 += TT) {
       const int rows = (int)min(p.end - l0, (int64_t)TT);
-      TL::template store<WHOLE>(zero, dense(a.dx, l0), a.CT, rows, p.left);
-      TL::template store<WHOLE>(zero, dense(a.ddelta, l0), a.CT, rows, p.left);
-      if (a.dz) TL::template store<WHOLE>(zero, dense(a.dz, l0), a.CT, rows, p.left);
+      TL::store(zero, dense(a.dx), l0, rows, p.left);
+      TL::store(zero, dense(a.ddelta), l0, rows, p.left);
+      if (a.dz) TL::store(zero, dense(a.dz), l0, rows, p.left);
     }
     if (a.P == 1) {
       const int64_t from = max(p.begin, stop), n = max(p.end - from, (int64_t)0) * a.N;
@@ -827,9 +1021,9 @@ __global__ __launch_bounds__(64 * kScanWaves, SUB > 8 ? 1 : 2) void eql_scan_bwd
 template <int DT>
 __global__ __launch_bounds__(256) void eql_scan_bc_kernel(const ScanArgs a, int NP) {
   using E = typename Elem<DT>::T;
-  const int64_t i = (a.first + blockIdx.x) * 256 + threadIdx.x;
+  const int64_t i = a.first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= a.B * a.L * a.G * 2 * NP) return;
-  const int64_t at = i / (2 * NP), l = at / a.G % a.L, b = at / a.G / a.L;
+  const int64_t at = i / (2 * NP), token = at / a.G, b = token / a.L, l = token - b * a.L;
   const int j = (int)(i % (2 * NP));
   if (j % NP >= a.N) return;
   const int64_t len = a.lengths ? (int64_t)a.lengths[b] : a.L;
@@ -845,15 +1039,17 @@ __global__ __launch_bounds__(256) void eql_scan_bc_kernel(const ScanArgs a, int 
 // group elements, each thread its own, then the threads in pairs.
 template <int UNUSED = 0>
 __global__ __launch_bounds__(256) void eql_scan_params_kernel(const ScanArgs a, int CH) {
-  const int64_t id = a.first + blockIdx.x;
+  const unsigned id = (unsigned)a.first + blockIdx.x;
   const int ch = (int)(id / (a.N + 2)), j = (int)(id % (a.N + 2));
   float* const dst = j < a.N ? a.dA + (int64_t)ch * a.N + j : j == a.N ? (a.dD ? a.dD + ch : nullptr) : (a.dbias ? a.dbias + ch : nullptr);
   if (!dst) return;
   const int64_t n = a.B * a.K * a.T;
   float v = 0.0f;
+  const int ct = ch * a.T, g = ct / a.CTg;
+  const float* const from = a.part + (int64_t)j * a.cols + g * a.nblk * CH + (ct - g * a.CTg);
   for (int64_t i = threadIdx.x; i < n; i += 256) {
-    const int ct = ch * a.T + (int)(i % a.T), g = ct / a.CTg;
-    v += a.part[(i / a.T * (a.N + 2) + j) * a.cols + g * a.nblk * CH + (ct - g * a.CTg)];
+    const int64_t k = n < (1 << 27) ? scan_channel(a, (int)i) : i / a.T;
+    v += from[k * (a.N + 2) * a.cols + (i - k * a.T)];
   }
   __shared__ float red[4];
 #pragma unroll

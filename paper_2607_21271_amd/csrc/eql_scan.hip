@@ -8,34 +8,53 @@ namespace {
 
 constexpr int DT = EQK_DT;
 
-// f(slice of the call that one launch takes, its workgroups)
+// f(slice of the sequences that one launch takes, its number of sequences); `waves`: of a sequence
 template <typename F>
-hipError_t launches(const ScanArgs& a, int64_t blocks, int threads, F&& f) {
+hipError_t sequences(const ScanArgs& a, int64_t waves, F&& f) {
   ScanArgs s = a;
-  const int64_t most = launch_blocks(threads);
-  for (s.first = 0; s.first < blocks; s.first += most) {
-    f(s, dim3((unsigned)(blocks - s.first < most ? blocks - s.first : most)));
+  const int64_t most = ((int64_t)1 << 30) / (64 * waves);  // (below 2^32 threads, and numbers of 31 bits)
+  if (most < 1) return hipErrorInvalidValue;
+  for (s.first = 0; s.first < a.B; s.first += most) {
+    f(s, a.B - s.first < most ? a.B - s.first : most);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
+// f(the call from `first` on, workgroups of 256) for `n` elements, or workgroups where per is 1
+template <typename F>
+hipError_t elements(const ScanArgs& a, int64_t n, int per, F&& f) {
+  ScanArgs s = a;
+  const int64_t most = launch_blocks(256) * per;
+  for (s.first = 0; s.first < n; s.first += most) {
+    f(s, dim3((unsigned)(((n - s.first < most ? n - s.first : most) + per - 1) / per)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+dim3 wave_blocks(ScanArgs& s, int64_t seqs) {
+  s.tasks = (unsigned)(seqs * s.K * s.G * s.nblk);
+  return dim3((s.tasks + kScanWaves - 1) / kScanWaves);
+}
 
 template <int NL, bool WHOLE>
 hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
-  const int64_t blocks = (a.B * a.K * a.G * a.nblk + kScanWaves - 1) / kScanWaves;
+  const int64_t waves = (int64_t)a.K * a.G * a.nblk;
   if (a.K > 1) {
-    hipError_t e = launches(a, blocks, 256, [&](const ScanArgs& s, dim3 n) {
-      hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, true>), n, dim3(256), 0, stream, s);
+    hipError_t e = sequences(a, waves, [&](ScanArgs s, int64_t n) {
+      const dim3 g = wave_blocks(s, n);
+      hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, true>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
-    e = launches(a, (a.B * a.cols * 4 * NL + 255) / 256, 256, [&](const ScanArgs& s, dim3 n) {
-      hipLaunchKernelGGL(eql_scan_carry_kernel<false>, n, dim3(256), 0, stream, s, 4 * NL);
+    e = sequences(a, a.cols * NL / 16, [&](const ScanArgs& s, int64_t n) {
+      hipLaunchKernelGGL(eql_scan_carry_kernel<false>, dim3((unsigned)(n * (a.cols * NL / 16))), dim3(64), 0, stream, s, 4 * NL);
     });
     if (e != hipSuccess) return e;
   }
-  return launches(a, blocks, 256, [&](const ScanArgs& s, dim3 n) {
-    hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, false>), n, dim3(256), 0, stream, s);
+  return sequences(a, waves, [&](ScanArgs s, int64_t n) {
+    const dim3 g = wave_blocks(s, n);
+    hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, false>), g, dim3(64 * kScanWaves), 0, stream, s);
   });
 }
 
@@ -43,12 +62,13 @@ template <int NL, bool WHOLE>
 hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
   hipError_t e;
   if (a.K > 1) {
-    e = launches(a, (a.B * a.K * a.G * a.nblk + kScanWaves - 1) / kScanWaves, 256, [&](const ScanArgs& s, dim3 n) {
-      hipLaunchKernelGGL((eql_scan_back_kernel<DT, NL, WHOLE>), n, dim3(256), 0, stream, s);
+    e = sequences(a, (int64_t)a.K * a.G * a.nblk, [&](ScanArgs s, int64_t n) {
+      const dim3 g = wave_blocks(s, n);
+      hipLaunchKernelGGL((eql_scan_back_kernel<DT, NL, WHOLE>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
-    e = launches(a, (a.B * a.cols * 4 * NL + 255) / 256, 256, [&](const ScanArgs& s, dim3 n) {
-      hipLaunchKernelGGL(eql_scan_carry_kernel<true>, n, dim3(256), 0, stream, s, 4 * NL);
+    e = sequences(a, a.cols * NL / 16, [&](const ScanArgs& s, int64_t n) {
+      hipLaunchKernelGGL(eql_scan_carry_kernel<true>, dim3((unsigned)(n * (a.cols * NL / 16))), dim3(64), 0, stream, s, 4 * NL);
     });
     if (e != hipSuccess) return e;
   }
@@ -59,17 +79,18 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
     e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
   }
-  e = launches(a, a.B * a.K * a.G * a.P, 64 * waves, [&](const ScanArgs& s, dim3 n) {
-    hipLaunchKernelGGL(k, n, dim3(64 * waves), lds, stream, s, waves);
+  const int64_t per = (int64_t)a.K * a.G * a.P;
+  e = sequences(a, per * waves, [&](const ScanArgs& s, int64_t n) {
+    hipLaunchKernelGGL(k, dim3((unsigned)(n * per)), dim3(64 * waves), lds, stream, s, waves);
   });
   if (e != hipSuccess) return e;
   if (a.P > 1) {
-    e = launches(a, (a.B * a.L * a.G * 8 * NL + 255) / 256, 256, [&](const ScanArgs& s, dim3 n) {
+    e = elements(a, a.B * a.L * a.G * 8 * NL, 256, [&](const ScanArgs& s, dim3 n) {
       hipLaunchKernelGGL(eql_scan_bc_kernel<DT>, n, dim3(256), 0, stream, s, 4 * NL);
     });
     if (e != hipSuccess) return e;
   }
-  return launches(a, (int64_t)a.C * (a.N + 2), 256, [&](const ScanArgs& s, dim3 n) {
+  return elements(a, (int64_t)a.C * (a.N + 2), 1, [&](const ScanArgs& s, dim3 n) {
     hipLaunchKernelGGL(eql_scan_params_kernel<>, n, dim3(256), 0, stream, s, scan_cols(NL));
   });
 }
