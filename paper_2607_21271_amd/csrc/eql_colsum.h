@@ -6,28 +6,28 @@
 
 namespace eqk {
 
-// A workgroup of 256 takes up to 64 columns of one kind j of rows [rows][J][K], whole channels of T columns each; its
-// four waves add every fourth row, then a thread a channel adds the waves and the channel's columns.
-// f(channel, sum) for each.
-constexpr int kColsumWidth = 64;
-inline int colsum_channels(int T) { return T < kColsumWidth ? kColsumWidth / T : 1; }
+// A workgroup of kColsumThreads takes up to 64 columns of one kind of rows [rows][.. K ..], `step` apart, whole channels of T
+// columns each; its waves add every sixteenth row, four at a time, then a thread a channel adds the waves and the
+// channel's columns.  f(channel, sum) for each.
+constexpr int kColsumWidth = 64, kColsumWaves = 16, kColsumThreads = 64 * kColsumWaves;
+inline int colsum_channels(int T) { return kColsumWidth / T; }  // (T <= 16)
 inline int colsum_blocks(int C, int T) { return (C + colsum_channels(T) - 1) / colsum_channels(T); }
 
 template <typename F>
 __device__ __forceinline__ void column_sums(const float* part, int64_t rows, int64_t step, int C, int T, int block, F&& f) {
-  __shared__ float red[4][kColsumWidth];
-  const int per = kColsumWidth / T, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;  // (T <= 16)
+  __shared__ float red[kColsumWaves][kColsumWidth];
+  const int per = kColsumWidth / T, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int c0 = block * per, n = min(per, C - c0) * T;
   float v = 0.0f;
   if (lane < n) {
     const float* p = part + c0 * T + lane;
-    float w[4] = {0.f, 0.f, 0.f, 0.f};  // four rows in flight
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
     int64_t r = wave;
-    for (; r + 12 < rows; r += 16) {
+    for (; r + 3 * kColsumWaves < rows; r += 4 * kColsumWaves) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] += p[(r + 4 * k) * step];
+      for (int k = 0; k < 4; ++k) w[k] += p[(r + kColsumWaves * k) * step];
     }
-    for (; r < rows; r += 4) w[0] += p[r * step];
+    for (; r < rows; r += kColsumWaves) w[0] += p[r * step];
     v = (w[0] + w[1]) + (w[2] + w[3]);
   }
   red[wave][lane] = v;
@@ -35,8 +35,8 @@ __device__ __forceinline__ void column_sums(const float* part, int64_t rows, int
   if ((int)threadIdx.x < n / T) {
     float s = 0.0f;
     for (int t = 0; t < T; ++t) {
-      const int i = threadIdx.x * T + t;
-      s += (red[0][i] + red[1][i]) + (red[2][i] + red[3][i]);
+#pragma unroll
+      for (int k = 0; k < kColsumWaves; ++k) s += red[k][threadIdx.x * T + t];
     }
     f(c0 + (int)threadIdx.x, s);
   }

@@ -322,7 +322,7 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
 
 // dweight and dbias from the workgroups' sums.
 template <int DT>
-__global__ __launch_bounds__(256) void eql_conv_params_kernel(const ConvArgs a, int GR) {
+__global__ __launch_bounds__(kColsumThreads) void eql_conv_params_kernel(const ConvArgs a, int GR) {
   using E = typename Elem<DT>::T;
   const int j = (int)(blockIdx.x % (a.W + 1)), block = (int)(blockIdx.x / (a.W + 1));
   const int T = a.T / GR, K = a.C * T;

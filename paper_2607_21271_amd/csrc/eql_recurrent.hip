@@ -40,7 +40,7 @@ hipError_t conv_gr(const ConvArgs& a, hipStream_t stream) {
       else hipLaunchKernelGGL((eql_conv_fwd_kernel<DT, W, VEC, GR, WHOLE>), n, dim3(256), 0, stream, s);
     });
     if (e != hipSuccess || !BACK) return e;
-    hipLaunchKernelGGL(eql_conv_params_kernel<DT>, dim3((unsigned)((W + 1) * colsum_blocks(a.C, a.T / GR))), dim3(256), 0, stream, a, GR);
+    hipLaunchKernelGGL(eql_conv_params_kernel<DT>, dim3((unsigned)((W + 1) * colsum_blocks(a.C, a.T / GR))), dim3(kColsumThreads), 0, stream, a, GR);
     return hipGetLastError();
   }
 }
@@ -110,11 +110,12 @@ hipError_t res_backward<DT>(const ResArgs& a, hipStream_t stream) {
   const hipError_t e = res(a, true, stream);
   if (e != hipSuccess || a.J == 0) return e;
   const int gr = res_gr(a), blocks = colsum_blocks(a.C, a.T / gr);
-  const hipError_t f = launches(a, a.seqs, (int64_t)a.J * blocks, 256, [&](const ResArgs& s, dim3 n) {
-    hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(256), 0, stream, s, gr, blocks);
+  const hipError_t f = launches(a, a.seqs, (int64_t)a.J * blocks, kColsumThreads, [&](const ResArgs& s, dim3 n) {
+    hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(kColsumThreads), 0, stream, s, gr, blocks);
   });
   if (f != hipSuccess) return f;
-  hipLaunchKernelGGL(eql_res_params_kernel<DT>, dim3((unsigned)((a.C + 63) / 64)), dim3(256), 0, stream, a);
+  hipLaunchKernelGGL(eql_res_params_kernel<DT>, dim3((unsigned)((a.C + kResParamChannels - 1) / kResParamChannels)),
+                     dim3(kResParamThreads), 0, stream, a);
   return hipGetLastError();
 }
 

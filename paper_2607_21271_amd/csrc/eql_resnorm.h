@@ -334,7 +334,7 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
 
 // sums[q, j, c]: the strips and group elements of a sequence's column sums.
 template <int UNUSED = 0>
-__global__ __launch_bounds__(256) void eql_res_strips_kernel(const ResArgs a, int GR, int blocks) {
+__global__ __launch_bounds__(kColsumThreads) void eql_res_strips_kernel(const ResArgs a, int GR, int blocks) {
   unsigned id = a.first + blockIdx.x;
   const int block = (int)(id % (unsigned)blocks);
   id /= (unsigned)blocks;
@@ -343,17 +343,19 @@ __global__ __launch_bounds__(256) void eql_res_strips_kernel(const ResArgs a, in
   column_sums(a.part + (q * a.strips * a.J + j) * K, a.strips, (int64_t)a.J * K, a.C, T, block,
               [&](int c, float v) { a.sums[(q * a.J + j) * a.C + c] = v; });
 }
-// The parameters' gradients: a workgroup takes 64 channels, its waves every fourth sequence.
+// The parameters' gradients: a workgroup takes 16 channels, its 64 threads of each every 64th sequence.
+constexpr int kResParamThreads = 1024, kResParamChannels = 16;
 template <int DT>
-__global__ __launch_bounds__(256) void eql_res_params_kernel(const ResArgs a) {
+__global__ __launch_bounds__(kResParamThreads) void eql_res_params_kernel(const ResArgs a) {
   using E = typename Elem<DT>::T;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)blockIdx.x * 64 + lane;
-  __shared__ float red[5][4][64];
+  constexpr int NC = kResParamChannels, NQ = kResParamThreads / NC;
+  const int cc = threadIdx.x % NC, turn = threadIdx.x / NC, c = (int)blockIdx.x * NC + cc;
+  __shared__ float red[5][NQ][NC];
   auto at = [&](const void* p, int64_t i) { return (float)reinterpret_cast<const E*>(p)[i]; };
   float sum[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // dw, db, dscale, dpw, dpb
   if (c < a.C) {
     const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
-    for (int64_t q = wave; q < a.seqs; q += 4) {
+    for (int64_t q = turn; q < a.seqs; q += NQ) {
       const float* s = a.sums + q * a.J * a.C + c;
       if (a.w) {
         sum[0] += s[0];
@@ -370,13 +372,17 @@ __global__ __launch_bounds__(256) void eql_res_params_kernel(const ResArgs a) {
     }
   }
 #pragma unroll
-  for (int i = 0; i < 5; ++i) red[i][wave][lane] = sum[i];
+  for (int i = 0; i < 5; ++i) red[i][turn][cc] = sum[i];
   __syncthreads();
-  if (c >= a.C || wave != 0) return;
+  if (c >= a.C || turn >= 5) return;
   void* const dst[5] = {a.dw, a.db, a.dscale, a.dpw, a.dpb};
+  float v = 0.0f;
+#pragma unroll 8
+  for (int q = 0; q < NQ; ++q) v += red[turn][q][cc];
+  void* p = nullptr;
 #pragma unroll
-  for (int i = 0; i < 5; ++i)
-    if (dst[i]) reinterpret_cast<E*>(dst[i])[c] = (E)((red[i][0][lane] + red[i][1][lane]) + (red[i][2][lane] + red[i][3][lane]));
+  for (int i = 0; i < 5; ++i) p = turn == i ? dst[i] : p;
+  if (p) reinterpret_cast<E*>(p)[c] = (E)v;
 }
 
 }  // namespace eqk

@@ -17,8 +17,9 @@
 // zero and its sum of d, a small kernel carries the states over the chunks (a chunk multiplies what
 // comes in by exp(A sum d)), and the main pass starts every chunk from its own.
 #pragma once
+#include <type_traits>
+
 #include "eql_common.h"
-#include "eql_colsum.h"
 #include "eql_config.h"
 #include "eql_lanes.h"
 #include "eql_recurrent.h"
@@ -377,7 +378,7 @@ __device__ __forceinline__ void scan_step(float (&h)[4][4], const float (&e)[4][
 }
 // End of a token in the loops over them: the next one's decays and words from LDS are on their way by then, so that one
 // wave on a SIMD waits for neither (left to itself the compiler uses an exponential two instructions
-// after it is issued: 980 cycles a token instead of SCAN_CYCLES).
+// after it is issued: 980 cycles a token of 64 columns, 16 states, instead of 780).
 __device__ __forceinline__ void token_end() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---- forward ---------------------------------------------------------------
@@ -460,43 +461,55 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * CH + c0); };
     auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * NP + n0); };
     float part[4] = {0.f, 0.f, 0.f, 0.f}, e0[4][4], e1[4][4];
-    floatx4 d = cols(ds, 0), u = cols(us, 0), bb = rows(bs, 0), cc = {};
-    if constexpr (!STATES) cc = rows(cs, 0);
-    scan_exp(e0, A2, d);
-    floatx4 d1 = cols(ds, 1);
+    // y of a token, in place of its d x, which every lane of these columns has read; all of them write what all of them hold
+    // (a branch here would keep the next token's reads behind it)
+    auto output = [&](int t, const floatx4& cc) {
+      floatx4 y;
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
-      const floatx4 d2 = cols(ds, t + 2), u1 = cols(us, t + 1), b1 = rows(bs, t + 1);
-      floatx4 c1 = {};
-      if constexpr (!STATES) c1 = rows(cs, t + 1);
-      if (t + 1 < TT) scan_exp(e1, A2, d1);
-      scan_step(h, e0, u, bb);
-      if constexpr (STATES) {
+      for (int q = 0; q < 4; ++q) {
+        float s = h[q][0] * cc[0];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) part[q] += d[q];
-      } else {
-        floatx4 y;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          float s = h[q][0] * cc[0];
-#pragma unroll
-          for (int n = 1; n < 4; ++n) s = __builtin_fmaf(h[q][n], cc[n], s);
-          y[q] = lanes_sum<NL>(s);
-        }
-        // in place of d x, which every lane of these columns has read; all of them write what all of them hold (a
-        // branch here would keep the next token's reads behind it)
-        *reinterpret_cast<floatx4*>(us + t * CH + c0) = y;
+        for (int n = 1; n < 4; ++n) s = __builtin_fmaf(h[q][n], cc[n], s);
+        y[q] = lanes_sum<NL>(s);
       }
-      d = d1;
-      d1 = d2;
-      u = u1;
-      bb = b1;
-      cc = c1;
+      *reinterpret_cast<floatx4*>(us + t * CH + c0) = y;
+    };
+    if (STATES || nt == TT) {
+      floatx4 d = cols(ds, 0), u = cols(us, 0), bb = rows(bs, 0), cc = {};
+      if constexpr (!STATES) cc = rows(cs, 0);
+      scan_exp(e0, A2, d);
+      floatx4 d1 = cols(ds, 1);
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int t = 0; t < TT; ++t) {
+        const floatx4 d2 = cols(ds, t + 2), u1 = cols(us, t + 1), b1 = rows(bs, t + 1);
+        floatx4 c1 = {};
+        if constexpr (!STATES) c1 = rows(cs, t + 1);
+        if (t + 1 < TT) scan_exp(e1, A2, d1);
+        scan_step(h, e0, u, bb);
+        if constexpr (STATES) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
-      token_end();
+          for (int q = 0; q < 4; ++q) part[q] += d[q];
+        } else {
+          output(t, cc);
+        }
+        d = d1;
+        d1 = d2;
+        u = u1;
+        bb = b1;
+        cc = c1;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
+        token_end();
+      }
+    } else {  // a sequence's last tokens, or a call over few
+#pragma unroll 1
+      for (int t = 0; t < nt; ++t) {
+        scan_exp(e0, A2, cols(ds, t));
+        scan_step(h, e0, cols(us, t), rows(bs, t));
+        output(t, rows(cs, t));
+      }
     }
     if constexpr (STATES) {
 #pragma unroll
@@ -553,24 +566,28 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
   float* c = a.carry + ((b * a.K + from) * a.cols + col) * NP + n;
   const float* s = a.sums + (b * a.K + from) * a.cols + col;
   // the first chunk of the way has nothing before it; the last one's own result is not wanted
-  for (int j = 0; j < a.K - 1; j += kScanAhead) {
-    float v[kScanAhead], d[kScanAhead];
-    const int m = min(a.K - 1 - j, kScanAhead);
+  auto chunks = [&](auto count) {
+    constexpr int n = decltype(count)::value;
+    float v[n], d[n];
 #pragma unroll
-    for (int k = 0; k < kScanAhead; ++k)
-      if (k < m) {
-        v[k] = c[k * cstep];
-        d[k] = s[k * sstep];
-      }
+    for (int k = 0; k < n; ++k) {
+      v[k] = c[k * cstep];
+      d[k] = s[k * sstep];
+    }
 #pragma unroll
-    for (int k = 0; k < kScanAhead; ++k)
-      if (k < m) {
-        c[k * cstep] = h;
-        h = __builtin_fmaf(__builtin_amdgcn_exp2f(d[k] * A2), h, v[k]);
-      }
-    c += m * cstep;
-    s += m * sstep;
-  }
+    for (int k = 0; k < n; ++k) d[k] = __builtin_amdgcn_exp2f(d[k] * A2);
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      c[k * cstep] = h;
+      h = __builtin_fmaf(d[k], h, v[k]);
+    }
+    c += n * cstep;
+    s += n * sstep;
+  };
+  int left = a.K - 1;
+  for (; left >= kScanAhead; left -= kScanAhead) chunks(std::integral_constant<int, kScanAhead>{});
+  for (; left >= 4; left -= 4) chunks(std::integral_constant<int, 4>{});
+  for (; left > 0; --left) chunks(std::integral_constant<int, 1>{});
   *c = h;
 }
 
