@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void eql_conv_fwd_kernel(const ConvArgs a) {
 
 // dx of the strip's tokens; its sums for dweight and dbias.  du of the W - 1 tokens behind the strip is formed again:
 // rows + W - 1 tokens are walked, a multiple of eight.
-constexpr int kConvBatch = 8;
+constexpr int kConvBatch = 4;
 
 template <int DT, int W, int VEC, int GR, bool WHOLE>
 __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {

@@ -14,8 +14,9 @@ namespace eqk {
 constexpr int kScanMaxN = 64;
 constexpr int scan_lanes(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 constexpr int scan_cols(int NL) { return 256 / NL; }
-// tokens of a tile, whose first state training keeps
+// tokens of a tile, and of a run, whose first state training keeps
 constexpr int scan_tile(int NL) { return NL == 1 ? 4 : NL == 2 ? 8 : 16; }
+constexpr int scan_run(int NL) { return NL == 1 ? 4 : 8; }
 constexpr int scan_ept(int NL) { return scan_tile(NL) * scan_cols(NL) / 64; }  // elements of a lane
 constexpr int scan_vec(int dt, int NL) {
   return (dt == kF32 ? 4 : 8) < scan_ept(NL) ? (dt == kF32 ? 4 : 8) : scan_ept(NL);
@@ -28,7 +29,7 @@ struct ScanArgs {
   void *y, *dx, *ddelta, *dz, *db, *dc;
   float *hT, *dh0, *dA, *dD, *dbias;
   const int* lengths;
-  float* states;  // [B, tiles, cols, NP]: the state before each tile
+  float* states;  // [B, runs, cols, NP]: the state before each run
   float* carry;   // [B, K, cols, NP]: the state before each chunk (backward: the gradient behind it)
   float* sums;    // [B, K, cols]: the chunk's sum of d
   float* part;    // [B * K, N + 2, cols]: sums of dA, dD, ddelta_bias
@@ -38,7 +39,7 @@ struct ScanArgs {
   int64_t first;         // what a launch starts with: a sequence (an element or workgroup of the small kernels)
   unsigned tasks;        // waves of a launch
   unsigned mT;           // ceil(2^32 / T), 0 for T = 1: the high half of column * mT is the channel
-  int64_t chunk, tiles;  // tokens of a chunk (whole tiles), tiles of a sequence
+  int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
   int whole;  // every vector of a wave's columns is aligned and inside its group
 };

@@ -91,7 +91,7 @@ int scan_args(const eqlinear_scan_shape* s, eqk::ScanArgs& a, bool bwd) {
 }
 
 int64_t scan_np(const eqk::ScanArgs& a) { return 4 * eqk::scan_lanes(a.N); }
-size_t scan_states(const eqk::ScanArgs& a) { return (size_t)a.B * a.tiles * a.cols * scan_np(a) * sizeof(float); }
+size_t scan_states(const eqk::ScanArgs& a) { return (size_t)a.B * a.runs * a.cols * scan_np(a) * sizeof(float); }
 size_t scan_carry(const eqk::ScanArgs& a) {
   return a.K > 1 ? align256((size_t)a.B * a.K * a.cols * scan_np(a) * sizeof(float)) : 0;
 }
@@ -164,6 +164,7 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.nblk = (a.CTg + CH - 1) / CH;
   a.cols = a.G * a.nblk * CH;
   a.tiles = (a.L + TT - 1) / TT;
+  a.runs = (a.L + scan_run(NL) - 1) / scan_run(NL);
   a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
   const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves;
   a.P = (a.nblk + waves - 1) / waves;

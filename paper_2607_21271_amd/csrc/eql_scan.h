@@ -391,6 +391,7 @@ template <int DT, int NL, bool WHOLE, bool STATES>
 __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const ScanArgs a) {
   using TL = ScanTile<DT, NL, WHOLE>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
+  constexpr int RUN = scan_run(NL);
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned id = blockIdx.x * kScanWaves + wave;
@@ -456,7 +457,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     }
     if (l0 + TT < stop) fetch(l0 + TT);
     if constexpr (!STATES)
-      if (a.states) store_padded<NL>(a.states + ((p.b * a.tiles + l0 / TT) * a.cols + p.col0) * NP, h);
+      if (a.states) store_padded<NL>(a.states + ((p.b * a.runs + l0 / RUN) * a.cols + p.col0) * NP, h);
     wave_order();
     auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * CH + c0); };
     auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * NP + n0); };
@@ -481,6 +482,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
       floatx4 d1 = cols(ds, 1);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
+        if constexpr (!STATES)
+          if (t > 0 && t % RUN == 0 && a.states)
+            store_padded<NL>(a.states + ((p.b * a.runs + (l0 + t) / RUN) * a.cols + p.col0) * NP, h);
         const floatx4 d2 = cols(ds, t + 2), u1 = cols(us, t + 1), b1 = rows(bs, t + 1);
         floatx4 c1 = {};
         if constexpr (!STATES) c1 = rows(cs, t + 1);
@@ -506,6 +510,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     } else {  // a sequence's last tokens, or a call over few
 #pragma unroll 1
       for (int t = 0; t < nt; ++t) {
+        if constexpr (!STATES)
+          if (t > 0 && t % RUN == 0 && a.states)
+            store_padded<NL>(a.states + ((p.b * a.runs + (l0 + t) / RUN) * a.cols + p.col0) * NP, h);
         scan_exp(e0, A2, cols(ds, t));
         scan_step(h, e0, cols(us, t), rows(bs, t));
         output(t, rows(cs, t));
@@ -691,7 +698,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 
 // The gradients.  The waves of a workgroup take neighbouring column blocks of one group and chunk, so that db
 // and dc are summed over them before they leave; a tile is walked from its last run of SUB tokens to the
-// first: the states of a run are formed again from the tile's first one and kept in registers.
+// first: the states of a run are formed again from the one before it, which the forward kept, and held in registers.
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave
   return 3 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
@@ -704,10 +711,11 @@ template <int NL>
 constexpr int scan_bwd_bytes(int waves) {
   return waves * (scan_bwd_lds<NL>() + scan_red_lds<NL>()) * 4;
 }
-template <int DT, int NL, bool WHOLE, int SUB>
+template <int DT, int NL, bool WHOLE>
 __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
   using TL = ScanTile<DT, NL, WHOLE>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
+  constexpr int SUB = scan_run(NL);
   using E = typename TL::E;
   extern __shared__ __attribute__((aligned(16))) float smem[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -780,12 +788,15 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     TL::load_bc(cr, a.c, p.b * a.cs[0] + l0 * a.cs[1] + p.g * a.cs[2], a.cs[1], nt, a.N);
   };
   const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
-  auto start = [&](int64_t tile) { return a.states + ((p.b * a.tiles + p.begin / TT + tile) * a.cols + p.col0) * NP; };
-  float hs[4][4] = {};  // the state before the tile
+  // the state before the run of tokens from l on, the next one on the way back
+  float hs[4][4] = {};
+  auto start = [&](int64_t l) {
+    if (on) load_padded<NL>(a.states + ((p.b * a.runs + l / SUB) * a.cols + p.col0) * NP, hs);
+  };
   if (tiles > 0) {
     fetch(p.begin + (tiles - 1) * TT);
     fetch_bc(p.begin + (tiles - 1) * TT);
-    if (on) load_padded<NL>(start(tiles - 1), hs);
+    start((stop - 1) / SUB * SUB);
   }
   for (int64_t tile = tiles - 1; tile >= 0; --tile, odd ^= 1) {
     const int64_t l0 = p.begin + tile * TT;
@@ -828,23 +839,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     auto token = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * CH + c0); };
     auto states = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * NP + n0); };
 #pragma unroll 1
-    for (int s0 = TT - SUB; s0 >= 0; s0 -= SUB) {
+    for (int s0 = (nt - 1) / SUB * SUB; s0 >= 0; s0 -= SUB) {
       float h[4][4], H[SUB][4][4], e0[4][4], e1[4][4];  // H[i]: the state before token s0 + i
 #pragma unroll
       for (int q = 0; q < 4; ++q)
 #pragma unroll
         for (int n = 0; n < 4; ++n) h[q][n] = hs[q][n];
-      if (s0 == 0 && tile > 0 && on) load_padded<NL>(start(tile - 1), hs);  // for the next tile, while this run is worked on
-      scan_exp(e0, A2, token(ds, 0));
-#pragma unroll 2
-      for (int t = 0; t < s0; ++t) {
-        scan_exp(e1, A2, token(ds, t + 1));
-        scan_step(h, e0, token(us, t), states(bs, t));
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-#pragma unroll
-          for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
-      }
+      if (l0 + s0 > p.begin) start(l0 + s0 - SUB);  // while this run is worked on
+      scan_exp(e0, A2, token(ds, s0));
       {
         floatx4 u = token(us, s0), bb = states(bs, s0), d1 = token(ds, s0 + 1);
 #pragma unroll

@@ -72,8 +72,7 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
     });
     if (e != hipSuccess) return e;
   }
-  constexpr int SUB = scan_tile(NL) < 8 ? scan_tile(NL) : 8;
-  auto k = eql_scan_bwd_kernel<DT, NL, WHOLE, SUB>;
+  auto k = eql_scan_bwd_kernel<DT, NL, WHOLE>;
   const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves, lds = scan_bwd_bytes<NL>(waves);
   if (lds > 65536) {
     e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);

@@ -72,7 +72,8 @@ def test_scan_arguments(kw, status, back):
     (dict(state_in=P + 9 * STEP + 1), ALI), (dict(states=P + 12 * STEP + 4), ALI), (dict(ws=P + 24 * STEP + 8), ALI),
     (dict(y=P + 100), INV), (dict(y=P + 3 * STEP), INV), (dict(state_out=P + 10 * STEP), INV), (dict(states=P + 11 * STEP), INV),
     (dict(state_out=P + 9 * STEP + 16), INV), (dict(y=P + 9 * STEP), INV), (dict(states=P + 9 * STEP), INV),
-    (dict(ws=P), INV), (dict(ws=P + 9 * STEP), INV), (dict(lengths=P + 10 * STEP + 8), INV), (dict(ws=None), WS), (dict(need=64), WS)])
+    (dict(ws=P, L_=5000), INV), (dict(ws=P + 9 * STEP, L_=5000), INV), (dict(lengths=P + 10 * STEP + 8), INV), (dict(ws=None, L_=5000), WS),
+    (dict(need=64, L_=5000), WS)])
 def test_scan_forward_arguments(kw, status):
     assert scan(**kw) == status
 
@@ -110,9 +111,9 @@ def test_scan_sizes():
     st = lambda **k: L.eqlinear_selective_scan_states_bytes(ctypes.byref(scan_shape(**k)))
     assert ws(L_=1) == 0 and ws(B=0) == 0  # few tokens are one chunk
     assert ws(L_=5000) > 0  # few columns and many tokens are split
-    # a state of 4-byte values, N rounded up, each tile of 16 tokens
-    assert st(C=32, T=2, G=1, N=16, L_=32) == 2 * 2 * 64 * 16 * 4
-    assert st(C=32, T=2, G=1, N=16, L_=33) == 2 * 3 * 64 * 16 * 4
+    # a state of 4-byte values, N rounded up, each run of 8 tokens
+    assert st(C=32, T=2, G=1, N=16, L_=32) == 2 * 4 * 64 * 16 * 4
+    assert st(C=32, T=2, G=1, N=16, L_=33) == 2 * 5 * 64 * 16 * 4
     assert bw(L_=5000) > ws(L_=5000) and bw() % 256 == 0
     for bad in (dict(N=65), dict(T=17), dict(dt=4), dict(G=7)):
         assert ws(**bad) == bw(**bad) == st(**bad) == 0
