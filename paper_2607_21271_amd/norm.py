@@ -120,60 +120,17 @@ class GroupNormAct(torch.nn.Module):
 KINDS = {"layer": _lib.EQL_NORM_LAYER, "rms": _lib.EQL_NORM_RMS}
 
 
-@functools.lru_cache(maxsize=1024)
-def _residual_plan(shape, kind, eps, dtype):
-    """The C shape of a call (a pointer that keeps it) and the bytes of its backward workspace."""
-    ref = ctypes.pointer(_lib.ResidualShape(shape[0], math.prod(shape[1:-2]), shape[-2], shape[-1], kind, ops._DT[dtype], eps, 0))
-    return ref, _lib.eqlinear_residual_norm_backward_workspace_bytes(ref)
-
-
-def _residual_forward(x, branch, weight, bias, scale, gate, post_weight, post_bias, kind, eps):
-    ref, _ = _residual_plan(x.shape, kind, eps, x.dtype)
-    r = None if branch is None else torch.empty_like(x)
-    h = None if weight is None else torch.empty_like(x)
-    p = ops._ptr
-    ops._launch("eqlinear_residual_norm", x, ref, p(x), p(branch), p(weight), p(bias), p(scale), p(gate), p(post_weight),
-                p(post_bias), p(r), p(h))
-    return r, h
-
-
-class ResidualNormFunction(torch.autograd.Function):
-    """Autograd: gradients of x, the branch and every parameter; r is formed again from x and the branch."""
-
-    @staticmethod
-    def forward(ctx, x, branch, weight, bias, scale, gate, post_weight, post_bias, kind, eps):
-        ctx.set_materialize_grads(False)
-        given = tuple(None if t is None else t.contiguous()
-                      for t in (x, branch, weight, bias, scale, gate, post_weight, post_bias))
-        ctx.save_for_backward(*given)
-        ctx.args = (kind, eps)
-        r, h = _residual_forward(*given, kind, eps)
-        return h if r is None else r if h is None else (r, h)
-
-    @staticmethod
-    @once_differentiable
-    def backward(ctx, *grads):
-        given = ctx.saved_tensors
-        x, branch, weight, bias, scale, gate, post_weight, post_bias = given
-        ref, need = _residual_plan(x.shape, *ctx.args, x.dtype)
-        if all(g is None for g in grads):
-            return (None,) * 10
-        gr, gh = grads if len(grads) == 2 else (None, grads[0]) if branch is None else (grads[0], None)
-        gr, gh = (None if g is None else g.contiguous() for g in (gr, gh))
-        new = torch.empty_like if x.numel() else torch.zeros_like
-        dx, du, dw, db, ds, dg, dpw, dpb = (new(t) if t is not None and need else None
-                                            for t, need in zip(given, ctx.needs_input_grad))
-        if x.numel():
-            ws = x.new_empty((need,), dtype=torch.uint8)
-            p = ops._ptr
-            ops._launch("eqlinear_residual_norm_backward", x, ref, p(x), p(branch), p(weight), p(scale), p(gate),
-                        p(post_weight), p(post_bias), p(gr), p(gh), p(dx), p(du), p(dw), p(db), p(ds), p(dg), p(dpw), p(dpb),
-                        p(ws), need)
-        return dx, du, dw, db, ds, dg, dpw, dpb, None, None
+_RESIDUAL = ("branch", "weight", "bias", "scale", "gate", "post_weight", "post_bias")
 
 
 @functools.lru_cache(maxsize=1024)
-def _check_residual_shapes(x, branch, weight, bias, scale, gate, post_weight, post_bias, kind):
+def _residual_plan(kind, eps, dtype, x, types, branch, weight, bias, scale, gate, post_weight, post_bias):
+    """Checks shapes and types; the C shape of a call (a pointer that keeps it) and the bytes of its backward workspace."""
+    if dtype not in ops._DT:
+        raise TypeError("eqlinear supports float32, float16 and bfloat16, got %s" % dtype)
+    for name, t in zip(_RESIDUAL, types):
+        if t is not None and t != dtype:
+            raise TypeError("%s has dtype %s, expected %s (one dtype per call)" % (name, t, dtype))
     if len(x) < 3 or x[-1] < 1 or x[-2] < 1:
         raise ValueError("x must be [B, ..., C, T], got %s" % (tuple(x),))
     if kind not in KINDS:
@@ -189,6 +146,55 @@ def _check_residual_shapes(x, branch, weight, bias, scale, gate, post_weight, po
                           ("post_bias", post_bias, x[-2:-1])):
         if s is not None and tuple(s) != tuple(want):
             raise ValueError("%s must be %s, got %s" % (name, list(want), tuple(s)))
+    ref = ctypes.pointer(_lib.ResidualShape(x[0], math.prod(x[1:-2]), x[-2], x[-1], KINDS[kind], ops._DT[dtype], eps, 0))
+    return ref, _lib.eqlinear_residual_norm_backward_workspace_bytes(ref)
+
+
+def _residual_check(kind, eps, x, *given):
+    return _residual_plan(kind, eps, x.dtype, x.shape, tuple([None if t is None else t.dtype for t in given]),
+                          *[None if t is None else t.shape for t in given])
+
+
+def _residual_forward(ref, given):
+    x = given[0]
+    r = None if given[1] is None else torch.empty_like(x)
+    h = None if given[2] is None else torch.empty_like(x)
+    ops._launch("eqlinear_residual_norm", x, ref, *[None if t is None else t.data_ptr() for t in (*given, r, h)])
+    return r, h
+
+
+class ResidualNormFunction(torch.autograd.Function):
+    """Autograd: gradients of x, the branch and every parameter; r is formed again from x and the branch."""
+
+    @staticmethod
+    def forward(ctx, x, branch, weight, bias, scale, gate, post_weight, post_bias, kind, eps):
+        ctx.set_materialize_grads(False)
+        given = tuple(None if t is None else t.contiguous()
+                      for t in (x, branch, weight, bias, scale, gate, post_weight, post_bias))
+        ctx.save_for_backward(*given)
+        ctx.plan = _residual_check(kind, eps, *given)
+        r, h = _residual_forward(ctx.plan[0], given)
+        return h if r is None else r if h is None else (r, h)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, *grads):
+        given = ctx.saved_tensors
+        x, branch, weight, _, scale, gate, post_weight, post_bias = given
+        ref, need = ctx.plan
+        if all(g is None for g in grads):
+            return (None,) * 10
+        gr, gh = grads if len(grads) == 2 else (None, grads[0]) if branch is None else (grads[0], None)
+        gr, gh = (None if g is None else g.contiguous() for g in (gr, gh))
+        empty = x.numel() == 0
+        new = torch.zeros_like if empty else torch.empty_like
+        out = [new(t) if t is not None and want else None for t, want in zip(given, ctx.needs_input_grad)]
+        if not empty:
+            ws = x.new_empty((need,), dtype=torch.uint8)
+            ops._launch("eqlinear_residual_norm_backward", x, ref,
+                        *[None if t is None else t.data_ptr()
+                          for t in (x, branch, weight, scale, gate, post_weight, post_bias, gr, gh, *out, ws)], need)
+        return (*out, None, None)
 
 
 def residual_norm(x: torch.Tensor, branch: torch.Tensor | None = None, weight: torch.Tensor | None = None,
@@ -205,15 +211,13 @@ def residual_norm(x: torch.Tensor, branch: torch.Tensor | None = None, weight: t
     ``kind`` layer (mean and variance) or rms.  Parameters are per channel, shared over T, of x's type; ``gate`` [B, C] is per
     sequence (a conditioned gate, or 0 and 1 / (1 - p) of a branch dropped at random).  Either result may be the one that has
     a gradient."""
-    ops._dtype_code(x)
-    ops._check_same_dtype(x, branch=branch, weight=weight, bias=bias, scale=scale, gate=gate, post_weight=post_weight,
-                          post_bias=post_bias)
     given = (x, branch, weight, bias, scale, gate, post_weight, post_bias)
-    _check_residual_shapes(*(None if t is None else t.shape for t in given), kind)
+    eps = float(eps)
+    ref, _ = _residual_check(kind, eps, *given)
     ops._check_dev(*given)
-    if ops._no_node(*(t for t in given if t is not None)):
-        r, h = _residual_forward(*(None if t is None else t.contiguous() for t in given), KINDS[kind], float(eps))
+    if ops._no_node(*[t for t in given if t is not None]):
+        r, h = _residual_forward(ref, [None if t is None else t.contiguous() for t in given])
     else:
-        out = ResidualNormFunction.apply(*given, KINDS[kind], float(eps))
+        out = ResidualNormFunction.apply(*given, kind, eps)
         r, h = (None, out) if branch is None else (out, None) if weight is None else out
     return x if branch is None else r, h

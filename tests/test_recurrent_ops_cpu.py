@@ -100,7 +100,74 @@ def test_encoder_chooses_its_mixer():
 def test_strided_views_are_described():
     """Views of a packed buffer keep their strides; tensors whose tokens are not contiguous are copied."""
     t = torch.zeros(2, 5, 12, 2)
+    assert scan._tokens_ready((2, 5, 6, 2), t[:, :, 6:].stride()) and not scan._tokens_ready((2, 5, 6, 2), t[:, :, ::2].stride())
     assert scan._tokens(t[:, :, 6:]).data_ptr() == t[:, :, 6:].data_ptr()
     assert scan._tokens(t[:, :, ::2]).is_contiguous()
     assert scan._tokens(t.transpose(0, 1)).stride() == (24, 120, 2, 1)
     assert scan._steps((1, 5, 3), (7, 8, 9), 3) == (0, 8, 9)
+
+
+class Launches:
+    """The library's entry points replaced by fills: each output that is not NULL holds 3 where a kernel would have written."""
+
+    def __init__(self, monkeypatch, n):
+        import ctypes
+
+        from paper_2607_21271_amd import _lib, ops
+        self.calls = []
+
+        def fill(name, outs):
+            def launch(*args):
+                self.calls.append(name)
+                for o in outs:
+                    if args[o]:
+                        (ctypes.c_float * n).from_address(args[o])[:] = [3.0] * n
+                return 0
+            return launch
+        for name, outs in (("eqlinear_selective_scan", (11,)), ("eqlinear_causal_conv", (6,)), ("eqlinear_residual_norm", (9, 10))):
+            monkeypatch.setattr(_lib, name, fill(name, outs))
+        monkeypatch.setattr(ops, "_check_dev", lambda *ts: None)
+        monkeypatch.setattr(ops, "_stream_of", lambda t: 0)
+
+
+def operators():
+    A, w = -torch.ones(3, 4), torch.ones(3)
+    bc = torch.ones(2, 5, 1, 4)
+    return {"scan": lambda x: scan.selective_scan(x, x, A, bc, bc), "conv": lambda x: scan.causal_conv(x, torch.ones(3, 4)),
+            "norm": lambda x: norm.residual_norm(x, x, w)[1], "norm alone": lambda x: norm.residual_norm(x, weight=w)[1]}
+
+
+@pytest.mark.parametrize("name", list(operators()))
+def test_forward_mode_is_refused_not_dropped(name, monkeypatch):
+    """No forward-mode derivative: a dual tensor is refused and never comes back without its tangent."""
+    launches = Launches(monkeypatch, 2 * 5 * 3 * 8)
+    f, x = operators()[name], torch.randn(2, 5, 3, 8)
+    with torch.no_grad(), torch.autograd.forward_ad.dual_level():
+        with pytest.raises((RuntimeError, NotImplementedError)):
+            f(torch.autograd.forward_ad.make_dual(x, torch.ones_like(x)))
+        assert (f(x) == 3.0).all() and launches.calls
+
+
+@pytest.mark.parametrize("name", list(operators()))
+def test_a_traced_call_runs_again(name, monkeypatch):
+    launches = Launches(monkeypatch, 2 * 5 * 3 * 8)
+    f, x = operators()[name], torch.randn(2, 5, 3, 8)
+    with torch.no_grad():
+        traced = torch.jit.trace(f, x, check_trace=False)
+        launches.calls = []
+        assert (traced(x) == 3.0).all() and launches.calls
+
+
+def test_a_state_in_place_is_not_traced_or_transformed(monkeypatch):
+    Launches(monkeypatch, 1)
+    state = torch.zeros(2, 3, 3, 8)
+    f = lambda x: scan.causal_conv(x, torch.ones(3, 4), state=state, state_out=state)[0]
+    x = torch.randn(2, 5, 3, 8)
+    with torch.no_grad(), pytest.raises(ValueError):
+        torch.jit.trace(f, x, check_trace=False)
+    with pytest.raises(ValueError):
+        f(x.requires_grad_())
+    with torch.no_grad():
+        before = state._version
+        f(x)
+    assert state._version > before
