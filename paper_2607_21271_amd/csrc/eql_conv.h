@@ -100,8 +100,7 @@ __device__ __forceinline__ void conv_weights(const ConvArgs& a, const ConvPlace&
   using E = typename Elem<DT>::T;
 #pragma unroll
   for (int i = 0; i < VEC / GR; ++i) {
-    const unsigned col = (unsigned)min(p.col + i * GR, a.CT - 1);
-    const int c = a.mT ? (int)__umulhi(col, a.mT) : (int)col;
+    const int c = channel_of(min(p.col + i * GR, a.CT - 1), a.mT);
     bias[i] = a.bias ? (float)reinterpret_cast<const E*>(a.bias)[c] : 0.0f;
 #pragma unroll
     for (int j = 0; j < W; ++j) w[j][i] = (float)reinterpret_cast<const E*>(a.w)[c * W + j];

@@ -8,6 +8,11 @@
 
 namespace eqk {
 
+// The channel of column ct <= 65536 in rows of T group elements, T <= 16: ct m / 2^21 with m = ceil(2^21 / T), which is
+// off by less than the 1 / T that it may be.
+constexpr unsigned channel_factor(int T) { return (unsigned)(((1 << 21) + T - 1) / T); }
+__device__ __forceinline__ int channel_of(int ct, unsigned m) { return (int)__umulhi((unsigned)ct << 11, m); }
+
 // ---- selective scan ----
 // A wave takes `scan_cols(NL)` neighbouring columns (channel, group element) of one group:
 // NL lanes share four columns and hold four states of each.
@@ -38,7 +43,7 @@ struct ScanArgs {
   int64_t B, L;
   int64_t first;         // what a launch starts with: a sequence (an element or workgroup of the small kernels)
   unsigned tasks;        // waves of a launch
-  unsigned mT;           // ceil(2^32 / T), 0 for T = 1: the high half of column * mT is the channel
+  unsigned mT;           // channel_factor(T)
   int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
   int whole;  // every vector of a wave's columns is aligned and inside its group
@@ -69,7 +74,7 @@ struct ConvArgs {
   int64_t B, L, strips, groups;
   int64_t seq;           // what a launch starts with: a sequence, and a workgroup from it on
   unsigned first;
-  unsigned mT;           // ceil(2^32 / T), 0 for T = 1: the high half of column * mT is the channel
+  unsigned mT;           // channel_factor(T)
   int C, T, W, CT, silu, vec;
   int rows;              // tokens of a strip
   int width, cblocks;    // vectors of columns of a workgroup, workgroups side by side
@@ -102,7 +107,7 @@ struct ResArgs {
   int64_t strips, strip; // workgroups of a sequence and tokens of each
   int64_t seq;     // what a launch starts with: a sequence, and a workgroup from it on
   unsigned first;
-  unsigned mT;     // ceil(2^32 / T), 0 for T = 1
+  unsigned mT;           // channel_factor(T)
   int C, T, K, rms, J;
   float eps;
   int whole, lanes, ept;  // threads of a row and elements of each

@@ -138,7 +138,7 @@ int scan_whole(const eqk::ScanArgs& a, int dtype) {
   const int64_t steps[6] = {a.CT, a.xs[1], a.ds[1], a.z ? a.zs[1] : 0, a.bs[1], a.cs[1]};
   for (int64_t st : steps)
     if (st >= ((int64_t)1 << 31) / 128) return 0;
-  if (a.N % 4 != 0 || !vectors(a.b, a.bs, 3, e, 4) || !vectors(a.c, a.cs, 3, e, 4)) return 0;
+  if (a.N % 4 != 0 || !aligned(a.A, 16) || !vectors(a.b, a.bs, 3, e, 4) || !vectors(a.c, a.cs, 3, e, 4)) return 0;
   return a.CTg % vec == 0 && vectors(a.x, a.xs, 2, e, vec) && vectors(a.delta, a.ds, 2, e, vec) &&
          vectors(a.z, a.zs, 2, e, vec) && vectors(a.y, none, 1, e, vec) && vectors(a.dy, none, 1, e, vec) &&
          vectors(a.dx, none, 1, e, vec) && vectors(a.ddelta, none, 1, e, vec) && vectors(a.dz, none, 1, e, vec);
@@ -165,7 +165,7 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.cols = a.G * a.nblk * CH;
   a.tiles = (a.L + TT - 1) / TT;
   a.runs = (a.L + scan_run(NL) - 1) / scan_run(NL);
-  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
+  a.mT = channel_factor(a.T);
   const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves;
   a.P = (a.nblk + waves - 1) / waves;
   const int64_t simds = 4 * (int64_t)cus, one = a.B * a.G * (bwd ? (int64_t)a.P * waves : a.nblk);
@@ -194,7 +194,7 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
 void conv_plan(ConvArgs& a, int dt, int cus, bool bwd) {
   const int vec = conv_vec(dt, a.W, bwd);
   a.CT = a.C * a.T;
-  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
+  a.mT = channel_factor(a.T);
   const int nv = (a.CT + vec - 1) / vec;
   a.width = nv < 256 ? nv : 256;
   a.cblocks = (nv + a.width - 1) / a.width;
@@ -214,7 +214,7 @@ void conv_plan(ConvArgs& a, int dt, int cus, bool bwd) {
 void res_plan(ResArgs& a, int dt, int cus, bool bwd) {
   (void)dt;
   a.K = a.C * a.T;
-  a.mT = a.T == 1 ? 0 : (unsigned)((((uint64_t)1 << 32) + a.T - 1) / a.T);
+  a.mT = channel_factor(a.T);
   a.lanes = a.K <= 128 ? 16 : a.K <= 1024 ? 64 : a.K <= 4096 ? 256 : 512;
   a.ept = a.K <= 8 * a.lanes ? 8 : 16;
   a.seqs = a.gate ? a.B : 1;

@@ -82,7 +82,8 @@ struct ResRow {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int c = at(i * GR / VEC) + i * GR % VEC;
-      f[i] = p && c < a.K ? (float)q[a.mT ? (int)__umulhi((unsigned)c, a.mT) : c] : none;
+      const float v = p ? (float)q[c < a.K ? channel_of(c, a.mT) : 0] : none;
+      f[i] = c < a.K ? v : none;
     }
   }
   // the sum over a row's threads

@@ -111,7 +111,7 @@ __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, unsigned id) 
   p.end = min(p.begin + a.chunk, a.L);
   return p;
 }
-__device__ __forceinline__ int scan_channel(const ScanArgs& a, int ct) { return a.mT ? (int)__umulhi((unsigned)ct, a.mT) : ct; }
+__device__ __forceinline__ int scan_channel(const ScanArgs& a, int ct) { return channel_of(ct, a.mT); }
 
 constexpr uint32_t kScanDrop = 0x80000000u;  // an offset past every resource: loads give 0, stores go nowhere
 
@@ -291,16 +291,23 @@ struct ScanTile {
   }
 };
 
-// A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.
-template <int NL>
+// A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.  WHOLE: four states are all
+// inside or all outside, and rows of A whole 16-byte words (what lies outside is read from A's start instead).
+template <int NL, bool WHOLE>
 __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    const float* s = a.A + (int64_t)scan_channel(a, p.ct0 + c0 + q) * a.N + n0;
     const int m = c0 + q < p.left ? a.N - n0 : 0;
+    const float* s = a.A + (m > 0 ? scan_channel(a, p.ct0 + c0 + q) * a.N + n0 : 0);
+    if constexpr (WHOLE) {
+      const floatx4 v = *reinterpret_cast<const floatx4*>(s);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) A2[q][n] = n < m ? s[n] * kLog2e : 0.0f;
+      for (int n = 0; n < 4; ++n) A2[q][n] = m > 0 ? v[n] * kLog2e : 0.0f;
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) A2[q][n] = n < m ? s[n] * kLog2e : 0.0f;
+    }
   }
 }
 // The lane's states in [cols][NP] or, for the caller, [CT][N].
@@ -330,9 +337,9 @@ __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p
   for (int q = 0; q < 4; ++q) {
     const float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
     if (whole) {
-      const floatx4 v = c0 + q < p.left ? *reinterpret_cast<const floatx4*>(s) : floatx4{0.f, 0.f, 0.f, 0.f};
+      const floatx4 v = *reinterpret_cast<const floatx4*>(c0 + q < p.left ? s : base);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) h[q][n] = v[n];
+      for (int n = 0; n < 4; ++n) h[q][n] = c0 + q < p.left ? v[n] : 0.0f;
     } else {
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[q][n] = c0 + q < p.left && n0 + n < a.N ? s[n] : 0.0f;
@@ -357,10 +364,22 @@ __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& 
   }
 }
 // The parameter of the channels of the lane's vector, 0 outside and where src is NULL.
-template <int VEC>
+template <int VEC, bool WHOLE>
 __device__ __forceinline__ void scan_param(const ScanArgs& a, const ScanPlace& p, const float* src, int at, float (&f)[VEC]) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) f[i] = src && at + i < p.left ? src[scan_channel(a, p.ct0 + at + i)] : 0.0f;
+  for (int i = 0; i < VEC; ++i) f[i] = 0.0f;
+  if (!src) return;
+  if (WHOLE && a.T % VEC == 0) {  // one channel
+    const float v = src[at < p.left ? scan_channel(a, p.ct0 + at) : 0];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) f[i] = at < p.left ? v : 0.0f;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    const float v = src[at + i < p.left ? scan_channel(a, p.ct0 + at + i) : 0];
+    f[i] = at + i < p.left ? v : 0.0f;
+  }
 }
 
 // The decays of a token: exp(d A).
@@ -420,9 +439,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   };
   if (p.begin < stop) fetch(p.begin);
   float A2[4][4], h[4][4], bias[VEC], skip[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
-  scan_decay<NL>(a, p, A2);
-  scan_param<VEC>(a, p, a.bias, at, bias);
-  if constexpr (!STATES) scan_param<VEC>(a, p, a.D, at, skip);
+  scan_decay<NL, WHOLE>(a, p, A2);
+  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
+  if constexpr (!STATES) scan_param<VEC, WHOLE>(a, p, a.D, at, skip);
   const int64_t slot = (p.b * a.K + p.k) * a.cols + p.col0;
   if (!STATES && a.K > 1) load_padded<NL>(a.carry + slot * NP, h);
   else if (!STATES && a.h0) load_state<NL>(a, p, a.h0, h);
@@ -629,8 +648,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
   const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
   if (tiles > 0) fetch(p.begin + (tiles - 1) * TT);
   float A2[4][4], r[4][4], bias[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
-  scan_decay<NL>(a, p, A2);
-  scan_param<VEC>(a, p, a.bias, at, bias);
+  scan_decay<NL, WHOLE>(a, p, A2);
+  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -741,9 +760,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     return v;
   };
   float A2[4][4], g[4][4], dA[4][4], bias[VEC], skip[VEC], dskip[VEC], dbias[VEC];
-  scan_decay<NL>(a, p, A2);
-  scan_param<VEC>(a, p, a.bias, at, bias);
-  scan_param<VEC>(a, p, a.D, at, skip);
+  scan_decay<NL, WHOLE>(a, p, A2);
+  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
+  scan_param<VEC, WHOLE>(a, p, a.D, at, skip);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) dskip[i] = dbias[i] = 0.0f;
 #pragma unroll
@@ -1062,14 +1081,12 @@ __global__ __launch_bounds__(256) void eql_scan_params_kernel(const ScanArgs a, 
   const int ch = (int)(id / (a.N + 2)), j = (int)(id % (a.N + 2));
   float* const dst = j < a.N ? a.dA + (int64_t)ch * a.N + j : j == a.N ? (a.dD ? a.dD + ch : nullptr) : (a.dbias ? a.dbias + ch : nullptr);
   if (!dst) return;
-  const int64_t n = a.B * a.K * a.T;
+  const int64_t n = a.B * a.K;
   float v = 0.0f;
-  const int ct = ch * a.T, g = ct / a.CTg;
-  const float* const from = a.part + (int64_t)j * a.cols + g * a.nblk * CH + (ct - g * a.CTg);
-  for (int64_t i = threadIdx.x; i < n; i += 256) {
-    const int64_t k = n < (1 << 27) ? scan_channel(a, (int)i) : i / a.T;
-    v += from[k * (a.N + 2) * a.cols + (i - k * a.T)];
-  }
+  const int ct = ch * a.T, g = ct / a.CTg, step = 256 / a.T, first = channel_of(threadIdx.x, a.mT);
+  const float* const from = a.part + (int64_t)j * a.cols + g * a.nblk * CH + (ct - g * a.CTg) + (threadIdx.x - first * a.T);
+  if (first < step)
+    for (int64_t i = first; i < n; i += step) v += from[i * (a.N + 2) * a.cols];
   __shared__ float red[4];
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
