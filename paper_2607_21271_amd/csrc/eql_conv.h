@@ -5,12 +5,13 @@
 // of its neighbours, W - 1 tokens, is read again, from the caches.  Runs of GR columns that share a channel share their
 // weights and their sums for dweight and dbias.
 // Bound: memory, and the loads that a thread has in flight: the forward reads its whole strip before it starts, the
-// backward eight tokens while it works on the eight before.
+// backward four tokens while it works on the four before.
 #pragma once
 #include "eql_colsum.h"
 #include "eql_common.h"
 #include "eql_config.h"
 #include "eql_recurrent.h"
+#include "eql_vectors.h"
 
 namespace eqk {
 
@@ -18,64 +19,31 @@ __device__ __forceinline__ float conv_sigmoid(float v) {  // (exp(-v) of inf giv
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
 }
 
-// VEC elements as raw words; WHOLE: one aligned vector, else the first n of them, the others 0.
+// VEC elements as raw words.
 template <int DT, int VEC>
 struct ConvVec {
   static constexpr int EB = Elem<DT>::bytes, W = VEC * EB / 4;
   uint32_t w[W];
 };
-template <int DT, int VEC, bool WHOLE>
+template <int DT, int VEC, int MODE>
 __device__ __forceinline__ void conv_load(const void* p, int n, ConvVec<DT, VEC>& r) {
-  constexpr int W = ConvVec<DT, VEC>::W;
-  if constexpr (WHOLE && W == 4) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.w[i] = v[i];
-  } else if constexpr (WHOLE) {
-    const u32x2 v = *reinterpret_cast<const u32x2*>(p);
-    r.w[0] = v[0];
-    r.w[1] = v[1];
-  } else if constexpr (DT == kF32) {
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) r.w[i] = i < n ? q[i] : 0u;
-  } else {
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      const uint32_t lo = 2 * i < n ? q[2 * i] : 0u, hi = 2 * i + 1 < n ? q[2 * i + 1] : 0u;
-      r.w[i] = lo | hi << 16;
-    }
-  }
+  load_vector<DT, VEC, MODE>(p, n, r.w);
 }
 template <int DT, int VEC>
 __device__ __forceinline__ void conv_floats(const ConvVec<DT, VEC>& r, float (&f)[VEC]) {
   raw_to_floats<DT, ConvVec<DT, VEC>::W>(r.w, f);
 }
-template <int DT, int VEC, bool WHOLE>
-__device__ __forceinline__ void conv_store(void* p, int n, const float (&f)[VEC]) {
-  using E = typename Elem<DT>::T;
-  if constexpr (WHOLE) {
-    constexpr int EB = Elem<DT>::bytes, W = VEC * EB / 4;
-    uint32_t w[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = pack2<DT>(f[i * (4 / EB)], f[i * (4 / EB) + (EB == 2)]);
-    if constexpr (W == 4) *reinterpret_cast<u32x4*>(p) = u32x4{w[0], w[1], w[2], w[3]};
-    else *reinterpret_cast<u32x2*>(p) = u32x2{w[0], w[1]};
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i)
-      if (i < n) reinterpret_cast<E*>(p)[i] = (E)f[i];
-  }
-}
-
-// Where a thread stands: columns col .. col + n, tokens l0 .. l1 of sequence b (none where it has no work).
+// Where a thread stands: columns col + skip .. col + n, tokens l0 .. l1 of sequence b (none where it has no work).
 struct ConvPlace {
   int64_t b, group, l0, l1, len;
-  int col, n, vector, turn;  // vector: among its workgroup's; turn: strip of the workgroup's
-  bool on;
+  int col, skip, n, vector, turn;  // vector: among its workgroup's; turn: strip of the workgroup's
+  bool has, on;                    // whether there is such a vector, and such a strip
 };
-template <int VEC>
+template <int DT, int VEC, int MODE>
+__device__ __forceinline__ void conv_store(void* p, const ConvPlace& at, const float (&f)[VEC]) {
+  store_vector<DT, VEC, MODE>(p, at.skip, at.n, f);
+}
+template <int VEC, int MODE>
 __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& a) {
   ConvPlace p;
   const int nv = (a.CT + VEC - 1) / VEC;
@@ -86,10 +54,16 @@ __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& a) {
   p.b = a.first + id / (unsigned)a.groups;
   p.vector = (int)threadIdx.x % a.width;
   p.turn = (int)threadIdx.x / a.width;
+  p.has = cb * a.width + p.vector < nv;
   p.col = (cb * a.width + p.vector) * VEC;
-  p.n = min(VEC, a.CT - p.col);
+  p.skip = 0;
+  p.n = MODE == kTiny ? a.CT : VEC;
+  if constexpr (MODE == kLoose) {
+    p.skip = max(p.col - (a.CT - VEC), 0);
+    p.col -= p.skip;
+  }
   const int64_t strip = p.group * a.turns + p.turn;
-  p.on = p.turn < a.turns && strip < a.strips && cb * a.width + p.vector < nv;
+  p.on = p.turn < a.turns && strip < a.strips && p.has;
   p.len = a.lengths ? min(max((int64_t)a.lengths[p.b], (int64_t)0), a.L) : a.L;
   p.l0 = p.on ? strip * a.rows : 0;
   p.l1 = p.on ? min(p.l0 + a.rows, a.L) : 0;
@@ -107,13 +81,13 @@ __device__ __forceinline__ void conv_weights(const ConvArgs& a, const ConvPlace&
   }
 }
 // Token l of sequence b, from the state before token 0; 0 from len on, before the state, and for a thread without work.
-template <int DT, int W, int VEC, bool WHOLE>
+template <int DT, int W, int VEC, int MODE>
 __device__ __forceinline__ void conv_token(const ConvArgs& a, const ConvPlace& p, int64_t l, ConvVec<DT, VEC>& r) {
   constexpr int EB = Elem<DT>::bytes;
   if (p.on && l >= 0 && l < p.len) {
-    conv_load<DT, VEC, WHOLE>((const char*)a.x + (p.b * a.xs[0] + l * a.xs[1] + p.col) * EB, p.n, r);
+    conv_load<DT, VEC, MODE>((const char*)a.x + (p.b * a.xs[0] + l * a.xs[1] + p.col) * EB, p.n, r);
   } else if (p.on && l < 0 && a.h0) {
-    conv_load<DT, VEC, WHOLE>((const char*)a.h0 + ((p.b * (W - 1) + l + W - 1) * a.CT + p.col) * EB, p.n, r);
+    conv_load<DT, VEC, MODE>((const char*)a.h0 + ((p.b * (W - 1) + l + W - 1) * a.CT + p.col) * EB, p.n, r);
   } else {
 #pragma unroll
     for (int i = 0; i < ConvVec<DT, VEC>::W; ++i) r.w[i] = 0u;
@@ -122,20 +96,20 @@ __device__ __forceinline__ void conv_token(const ConvArgs& a, const ConvPlace& p
 
 constexpr int kConvRows = 16;  // of a forward strip
 
-template <int DT, int W, int VEC, int GR, bool WHOLE>
+template <int DT, int W, int VEC, int GR, int MODE>
 __global__ __launch_bounds__(256) void eql_conv_fwd_kernel(const ConvArgs a) {
   constexpr int EB = Elem<DT>::bytes;
-  const ConvPlace p = conv_place<VEC>(a);
+  const ConvPlace p = conv_place<VEC, MODE>(a);
   if (!p.on) return;
   ConvVec<DT, VEC> raw[kConvRows + W - 1];  // tokens l0 - (W - 1) ..
   const bool inner = p.l0 >= W - 1 && p.l0 + kConvRows <= p.len;
   if (inner) {
     const char* q = (const char*)a.x + (p.b * a.xs[0] + (p.l0 - (W - 1)) * a.xs[1] + p.col) * EB;
 #pragma unroll
-    for (int j = 0; j < kConvRows + W - 1; ++j) conv_load<DT, VEC, WHOLE>(q + j * a.xs[1] * EB, p.n, raw[j]);
+    for (int j = 0; j < kConvRows + W - 1; ++j) conv_load<DT, VEC, MODE>(q + j * a.xs[1] * EB, p.n, raw[j]);
   } else {
 #pragma unroll
-    for (int j = 0; j < kConvRows + W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, raw[j]);
+    for (int j = 0; j < kConvRows + W - 1; ++j) conv_token<DT, W, VEC, MODE>(a, p, p.l0 - (W - 1) + j, raw[j]);
   }
   float w[W][VEC / GR], bias[VEC / GR], x[W][VEC];  // x[W - 1]: the newest token
   conv_weights<DT, W, VEC, GR>(a, p, w, bias);
@@ -161,30 +135,30 @@ __global__ __launch_bounds__(256) void eql_conv_fwd_kernel(const ConvArgs a) {
     if (p.l0 + r >= p.len)
 #pragma unroll
       for (int i = 0; i < VEC; ++i) y[i] = 0.0f;
-    conv_store<DT, VEC, WHOLE>(out + (int64_t)r * a.CT * EB, p.n, y);
+    conv_store<DT, VEC, MODE>(out + (int64_t)r * a.CT * EB, p, y);
   }
   // the last W - 1 tokens: the first strip alone reads the state, so it may be updated in place
   if (W > 1 && a.hT && p.l0 == 0) {
     ConvVec<DT, VEC> s[W];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.len - (W - 1) + j, s[j]);
+    for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, MODE>(a, p, p.len - (W - 1) + j, s[j]);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
       float f[VEC];
       conv_floats(s[j], f);
-      conv_store<DT, VEC, WHOLE>((char*)a.hT + ((p.b * (W - 1) + j) * a.CT + p.col) * EB, p.n, f);
+      conv_store<DT, VEC, MODE>((char*)a.hT + ((p.b * (W - 1) + j) * a.CT + p.col) * EB, p, f);
     }
   }
 }
 
 // dx of the strip's tokens; its sums for dweight and dbias.  du of the W - 1 tokens behind the strip is formed again:
-// rows + W - 1 tokens are walked, a multiple of eight.
+// rows + W - 1 tokens are walked, a multiple of eight, in batches.
 constexpr int kConvBatch = 4;
 
-template <int DT, int W, int VEC, int GR, bool WHOLE>
+template <int DT, int W, int VEC, int GR, int MODE>
 __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
   constexpr int EB = Elem<DT>::bytes, NG = VEC / GR;
-  const ConvPlace p = conv_place<VEC>(a);
+  const ConvPlace p = conv_place<VEC, MODE>(a);
   const int steps = a.rows + W - 1;
   const bool inner = p.on && p.l0 >= W - 1 && p.l0 + steps <= p.len;
   ConvVec<DT, VEC> xr[kConvBatch], gr[kConvBatch], before[W];
@@ -194,14 +168,14 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
     if (inner) {
 #pragma unroll
       for (int j = 0; j < kConvBatch; ++j) {
-        conv_load<DT, VEC, WHOLE>(xp + (int64_t)(s + j) * a.xs[1] * EB, p.n, xr[j]);
-        conv_load<DT, VEC, WHOLE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
+        conv_load<DT, VEC, MODE>(xp + (int64_t)(s + j) * a.xs[1] * EB, p.n, xr[j]);
+        conv_load<DT, VEC, MODE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
       }
     } else {
 #pragma unroll
       for (int j = 0; j < kConvBatch; ++j) {
-        conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 + s + j, xr[j]);
-        if (p.on && p.l0 + s + j < p.len) conv_load<DT, VEC, WHOLE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
+        conv_token<DT, W, VEC, MODE>(a, p, p.l0 + s + j, xr[j]);
+        if (p.on && p.l0 + s + j < p.len) conv_load<DT, VEC, MODE>(gp + (int64_t)(s + j) * a.CT * EB, p.n, gr[j]);
         else
 #pragma unroll
           for (int i = 0; i < ConvVec<DT, VEC>::W; ++i) gr[j].w[i] = 0u;
@@ -209,7 +183,7 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
     }
   };
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, WHOLE>(a, p, p.l0 - (W - 1) + j, before[j]);
+  for (int j = 0; j < W - 1; ++j) conv_token<DT, W, VEC, MODE>(a, p, p.l0 - (W - 1) + j, before[j]);
   fetch(0);
   float w[W][NG], bias[NG], x[W][VEC], du[W][VEC], dw[W][NG], db[NG];
   conv_weights<DT, W, VEC, GR>(a, p, w, bias);
@@ -284,7 +258,7 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
         if (W > 1 && a.dhT && at >= p.len - (W - 1) && at < p.len) {  // a token of the last ones
           ConvVec<DT, VEC> hr;
           float h[VEC];
-          conv_load<DT, VEC, WHOLE>((const char*)a.dhT + ((p.b * (W - 1) + at - p.len + W - 1) * a.CT + p.col) * EB, p.n, hr);
+          conv_load<DT, VEC, MODE>((const char*)a.dhT + ((p.b * (W - 1) + at - p.len + W - 1) * a.CT + p.col) * EB, p.n, hr);
           conv_floats(hr, h);
 #pragma unroll
           for (int i = 0; i < VEC; ++i) d[i] += h[i];
@@ -293,8 +267,8 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
 #pragma unroll
           for (int i = 0; i < VEC; ++i) d[i] = 0.0f;
       }
-      if (at >= 0) conv_store<DT, VEC, WHOLE>((char*)a.dx + ((p.b * a.L + at) * a.CT + p.col) * EB, p.n, d);
-      else conv_store<DT, VEC, WHOLE>((char*)a.dh0 + ((p.b * (W - 1) + at + W - 1) * a.CT + p.col) * EB, p.n, d);
+      if (at >= 0) conv_store<DT, VEC, MODE>((char*)a.dx + ((p.b * a.L + at) * a.CT + p.col) * EB, p, d);
+      else conv_store<DT, VEC, MODE>((char*)a.dh0 + ((p.b * (W - 1) + at + W - 1) * a.CT + p.col) * EB, p, d);
     }
   }
   // the sums of the workgroup's strips, in order
@@ -307,10 +281,10 @@ __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
 #pragma unroll
     for (int i = 0; i < NG; ++i) red[threadIdx.x][i] = j < W ? dw[j < W ? j : 0][i] : db[i];
     __syncthreads();
-    if (p.turn == 0 && p.col < a.CT) {
+    if (p.turn == 0 && p.has) {
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        if (i * GR >= p.n) break;
+        if (i * GR < p.skip || i * GR >= p.n) continue;
         float v = red[p.vector][i];
         for (int t = 1; t < a.turns; ++t) v += red[t * a.width + p.vector][i];
         part[(int64_t)j * K + i] = v;

@@ -13,6 +13,9 @@ namespace eqk {
 constexpr unsigned channel_factor(int T) { return (unsigned)(((1 << 21) + T - 1) / T); }
 __device__ __forceinline__ int channel_of(int ct, unsigned m) { return (int)__umulhi((unsigned)ct << 11, m); }
 
+// How rows of the convolution and the residual norm are read and written (eql_vectors.h).
+constexpr int kWhole = 0, kLoose = 1, kTiny = 2;
+
 // ---- selective scan ----
 // A wave takes `scan_cols(NL)` neighbouring columns (channel, group element) of one group:
 // NL lanes share four columns and hold four states of each.
@@ -75,7 +78,7 @@ struct ConvArgs {
   int64_t seq;           // what a launch starts with: a sequence, and a workgroup from it on
   unsigned first;
   unsigned mT;           // channel_factor(T)
-  int C, T, W, CT, silu, vec;
+  int C, T, W, CT, silu, mode;
   int rows;              // tokens of a strip
   int width, cblocks;    // vectors of columns of a workgroup, workgroups side by side
   int turns;             // strips of a workgroup; `groups` of them are a sequence's
@@ -110,7 +113,7 @@ struct ResArgs {
   unsigned mT;           // channel_factor(T)
   int C, T, K, rms, J;
   float eps;
-  int whole, lanes, ept;  // threads of a row and elements of each
+  int mode, lanes, ept;  // threads of a row and elements of each
 };
 
 void res_plan(ResArgs& a, int dt, int cus, bool bwd);

@@ -29,15 +29,15 @@ hipError_t launches(const A& a, int64_t seqs, int64_t per, int threads, F&& f) {
   return hipSuccess;
 }
 
-template <int W, bool BACK, int GR, bool WHOLE>
+template <int W, bool BACK, int GR, int MODE>
 hipError_t conv_gr(const ConvArgs& a, hipStream_t stream) {
   constexpr int VEC = conv_vec(DT, W, BACK);
   if constexpr (GR > VEC) {
     return hipErrorInvalidValue;
   } else {
     const hipError_t e = launches(a, a.B, a.groups * a.cblocks, 256, [&](const ConvArgs& s, dim3 n) {
-      if constexpr (BACK) hipLaunchKernelGGL((eql_conv_bwd_kernel<DT, W, VEC, GR, WHOLE>), n, dim3(256), 0, stream, s);
-      else hipLaunchKernelGGL((eql_conv_fwd_kernel<DT, W, VEC, GR, WHOLE>), n, dim3(256), 0, stream, s);
+      if constexpr (BACK) hipLaunchKernelGGL((eql_conv_bwd_kernel<DT, W, VEC, GR, MODE>), n, dim3(256), 0, stream, s);
+      else hipLaunchKernelGGL((eql_conv_fwd_kernel<DT, W, VEC, GR, MODE>), n, dim3(256), 0, stream, s);
     });
     if (e != hipSuccess || !BACK) return e;
     hipLaunchKernelGGL(eql_conv_params_kernel<DT>, dim3((unsigned)((W + 1) * colsum_blocks(a.C, a.T / GR))), dim3(kColsumThreads), 0, stream, a, GR);
@@ -47,11 +47,12 @@ hipError_t conv_gr(const ConvArgs& a, hipStream_t stream) {
 template <int W, bool BACK>
 hipError_t conv_w(const ConvArgs& a, hipStream_t stream) {
   constexpr int VEC = conv_vec(DT, W, BACK);
-  if (a.vec == 1) return conv_gr<W, BACK, 1, false>(a, stream);
-  if (a.T % VEC == 0) return conv_gr<W, BACK, VEC, true>(a, stream);
+  if (a.mode == kTiny) return conv_gr<W, BACK, 1, kTiny>(a, stream);
+  if (a.mode == kLoose) return conv_gr<W, BACK, 1, kLoose>(a, stream);
+  if (a.T % VEC == 0) return conv_gr<W, BACK, VEC, kWhole>(a, stream);
   if constexpr (VEC == 8)
-    if (a.T % 4 == 0) return conv_gr<W, BACK, 4, true>(a, stream);
-  return conv_gr<W, BACK, 1, true>(a, stream);
+    if (a.T % 4 == 0) return conv_gr<W, BACK, 4, kWhole>(a, stream);
+  return conv_gr<W, BACK, 1, kWhole>(a, stream);
 }
 template <bool BACK, int W = 1>
 hipError_t conv(const ConvArgs& a, hipStream_t stream) {
@@ -62,33 +63,37 @@ hipError_t conv(const ConvArgs& a, hipStream_t stream) {
   }
 }
 
-template <int LANES, int EPT, bool WHOLE, int GR>
+template <int LANES, int EPT, int MODE, int GR>
 hipError_t res_row(const ResArgs& a, bool back, hipStream_t stream) {
-  constexpr int threads = ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS;
+  constexpr int threads = ResRow<DT, LANES, EPT, MODE, GR>::THREADS;
   return launches(a, a.seqs, a.strips, threads, [&](const ResArgs& s, dim3 n) {
-    if (back) hipLaunchKernelGGL((eql_res_bwd_kernel<DT, LANES, EPT, WHOLE, GR>), n, dim3(threads), 0, stream, s);
-    else hipLaunchKernelGGL((eql_res_fwd_kernel<DT, LANES, EPT, WHOLE, GR>), n, dim3(threads), 0, stream, s);
+    if (back) hipLaunchKernelGGL((eql_res_bwd_kernel<DT, LANES, EPT, MODE, GR>), n, dim3(threads), 0, stream, s);
+    else hipLaunchKernelGGL((eql_res_fwd_kernel<DT, LANES, EPT, MODE, GR>), n, dim3(threads), 0, stream, s);
   });
 }
-template <bool WHOLE, int GR>
+template <int MODE, int GR>
 hipError_t res_lanes(const ResArgs& a, bool back, hipStream_t stream) {
-  if (a.lanes == 16) return res_row<16, 8, WHOLE, GR>(a, back, stream);
-  if (a.lanes == 64) return a.ept == 8 ? res_row<64, 8, WHOLE, GR>(a, back, stream) : res_row<64, 16, WHOLE, GR>(a, back, stream);
-  if (a.lanes == 256) return a.ept == 8 ? res_row<256, 8, WHOLE, GR>(a, back, stream) : res_row<256, 16, WHOLE, GR>(a, back, stream);
-  return res_row<512, 16, WHOLE, GR>(a, back, stream);
+  if (a.lanes == 8) return res_row<8, 8, MODE, GR>(a, back, stream);
+  if (a.lanes == 32) return res_row<32, 8, MODE, GR>(a, back, stream);
+  if (a.lanes == 4) return res_row<4, 8, MODE, GR>(a, back, stream);
+  if (a.lanes == 16) return res_row<16, 8, MODE, GR>(a, back, stream);
+  if (a.lanes == 64) return a.ept == 8 ? res_row<64, 8, MODE, GR>(a, back, stream) : res_row<64, 16, MODE, GR>(a, back, stream);
+  if (a.lanes == 256) return a.ept == 8 ? res_row<256, 8, MODE, GR>(a, back, stream) : res_row<256, 16, MODE, GR>(a, back, stream);
+  return res_row<1024, 8, MODE, GR>(a, back, stream);
 }
 // columns that share a channel, of a vector
 int res_gr(const ResArgs& a) {
-  if (!a.whole) return 1;
+  if (a.mode != kWhole) return 1;
   if (DT != kF32 && a.T % 8 == 0) return 8;
   return a.T % 4 == 0 ? 4 : 1;
 }
 hipError_t res(const ResArgs& a, bool back, hipStream_t stream) {
   const int gr = res_gr(a);
   if constexpr (DT != kF32)
-    if (gr == 8) return res_lanes<true, 8>(a, back, stream);
-  if (gr == 4) return res_lanes<true, 4>(a, back, stream);
-  return a.whole ? res_lanes<true, 1>(a, back, stream) : res_lanes<false, 1>(a, back, stream);
+    if (gr == 8) return res_lanes<kWhole, 8>(a, back, stream);
+  if (gr == 4) return res_lanes<kWhole, 4>(a, back, stream);
+  if (a.mode == kTiny) return res_row<4, 8, kTiny, 1>(a, back, stream);
+  return a.mode == kWhole ? res_lanes<kWhole, 1>(a, back, stream) : res_lanes<kLoose, 1>(a, back, stream);
 }
 
 }  // namespace

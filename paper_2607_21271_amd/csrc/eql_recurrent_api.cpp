@@ -215,7 +215,11 @@ void res_plan(ResArgs& a, int dt, int cus, bool bwd) {
   (void)dt;
   a.K = a.C * a.T;
   a.mT = channel_factor(a.T);
-  a.lanes = a.K <= 128 ? 16 : a.K <= 1024 ? 64 : a.K <= 4096 ? 256 : 512;
+  // The fewest threads that hold a row in eight elements each: 32 MiB of f16 rows of 16 elements take 72 us with 4 threads
+  // and 252 with 16, of 256 elements 46 us with 32 and 76 with 64.  Up to 4096 elements 16 each save barriers; above, 1024
+  // threads of eight (512 of 16 spill in the backward: training passes over 8192 f16 columns 281 us instead of 395).
+  a.lanes = a.K <= 256 ? 4 : a.K <= 1024 ? 64 : a.K <= 4096 ? 256 : 1024;
+  while (8 * a.lanes < a.K && a.K <= 256) a.lanes *= 2;
   a.ept = a.K <= 8 * a.lanes ? 8 : 16;
   a.seqs = a.gate ? a.B : 1;
   a.rows = a.gate ? a.L : a.B * a.L;
@@ -398,14 +402,14 @@ int conv_inputs(const eqlinear_conv_shape* s, const eqk::ConvArgs& a, const void
   return EQL_OK;
 }
 
-int conv_whole(const eqk::ConvArgs& a, int dtype, bool bwd) {
+int conv_mode(const eqk::ConvArgs& a, int dtype, bool bwd) {
   const int vec = eqk::conv_vec(dtype, a.W, bwd);
   const size_t e = elem_bytes(dtype);
   const int64_t none[1] = {0};
   const void* dense[7] = {a.h0, a.y, a.hT, a.dy, a.dx, a.dhT, a.dh0};
   bool ok = a.CT % vec == 0 && vectors(a.x, a.xs, 2, e, vec);
   for (const void* p : dense) ok = ok && vectors(p, none, 1, e, vec);
-  return ok ? vec : 1;
+  return ok ? eqk::kWhole : a.CT < vec ? eqk::kTiny : eqk::kLoose;
 }
 
 }  // namespace
@@ -433,7 +437,7 @@ int eqlinear_causal_conv(const eqlinear_conv_shape* s, const void* x, const void
   a.h0 = state_in;
   a.y = y;
   a.hT = state_out;
-  a.vec = conv_whole(a, s->dtype, false);
+  a.mode = conv_mode(a, s->dtype, false);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::conv_forward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::conv_forward<eqk::kF16>(a, st));
@@ -479,7 +483,7 @@ int eqlinear_causal_conv_backward(const eqlinear_conv_shape* s, const void* x, c
   a.db = dbias;
   a.dh0 = d_state_in;
   a.part = (float*)workspace;
-  a.vec = conv_whole(a, s->dtype, true);
+  a.mode = conv_mode(a, s->dtype, true);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::conv_backward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::conv_backward<eqk::kF16>(a, st));
@@ -510,12 +514,12 @@ int res_args(const eqlinear_residual_shape* s, eqk::ResArgs& a) {
   return EQL_OK;
 }
 
-int res_whole(const eqk::ResArgs& a, int dtype) {
+int res_mode(const eqk::ResArgs& a, int dtype) {
   const size_t e = elem_bytes(dtype);
   bool ok = (size_t)a.K * e % 16 == 0;
   const void* rows[8] = {a.x, a.u, a.r, a.h, a.dr, a.dh, a.dx, a.du};
   for (const void* p : rows) ok = ok && aligned(p, 16);
-  return ok;
+  return ok ? eqk::kWhole : (size_t)a.K * e < 16 ? eqk::kTiny : eqk::kLoose;
 }
 
 // rows of column sums: dw and db of a norm after, one or two of a branch
@@ -557,7 +561,7 @@ int eqlinear_residual_norm(const eqlinear_residual_shape* s, const void* x, cons
   a.r = r;
   a.h = h;
   eqk::res_plan(a, s->dtype, kPlanCus, false);
-  a.whole = res_whole(a, s->dtype);
+  a.mode = res_mode(a, s->dtype);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::res_forward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::res_forward<eqk::kF16>(a, st));
@@ -624,7 +628,7 @@ int eqlinear_residual_norm_backward(const eqlinear_residual_shape* s, const void
   if (n == 0) return EQL_OK;
   a.part = (float*)workspace;
   a.sums = (float*)((char*)workspace + align256((size_t)a.seqs * a.strips * a.J * a.K * sizeof(float)));
-  a.whole = res_whole(a, s->dtype);
+  a.mode = res_mode(a, s->dtype);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::res_backward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::res_backward<eqk::kF16>(a, st));

@@ -18,85 +18,82 @@
 #include "eql_config.h"
 #include "eql_lanes.h"
 #include "eql_recurrent.h"
+#include "eql_vectors.h"
 
 namespace eqk {
 
-template <int DT, int LANES, int EPT, bool WHOLE, int GR>
+template <int DT, int LANES, int EPT, int MODE, int GR>
 struct ResRow {
   using E = typename Elem<DT>::T;
-  static constexpr int EB = Elem<DT>::bytes, VEC = WHOLE ? 16 / EB : 1, NV = EPT / VEC;
+  static constexpr int EB = Elem<DT>::bytes, VEC = 16 / EB, NV = EPT / VEC;
   static constexpr int NP = EPT / GR;  // parameters of a thread: of runs of GR columns that share a channel
-  static constexpr int W = WHOLE ? 4 : 1;
+  static_assert(LANES >= 4 && (LANES & (LANES - 1)) == 0);
   static constexpr int ROWS = LANES < 256 ? 256 / LANES : 1;   // rows of a workgroup at a time
   static constexpr int THREADS = LANES < 256 ? 256 : LANES;
   struct Raw {
-    uint32_t w[NV * W];
+    uint32_t w[NV * 4];
   };
-  // first element of vector v
-  static __device__ __forceinline__ int at(int v) { return (v * LANES + (int)(threadIdx.x % LANES)) * VEC; }
+  // first element of vector v, where it would be in a row of whole vectors and where it is
+  static __device__ __forceinline__ int place(int v) { return (v * LANES + (int)(threadIdx.x % LANES)) * VEC; }
+  static __device__ __forceinline__ int at(int v, int K) { return MODE == kLoose ? min(place(v), K - VEC) : place(v); }
+  // whether the thread's element e is its own
+  static __device__ __forceinline__ bool own(int e, int K) {
+    if constexpr (MODE == kLoose) return e % VEC >= place(e / VEC) - (K - VEC);
+    return place(e / VEC) + (MODE == kTiny ? e % VEC : 0) < K;
+  }
   static __device__ __forceinline__ void load(Raw& r, const void* base, int64_t row, int K, bool on) {
     const E* p = reinterpret_cast<const E*>(base) + row * K;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      const bool ok = on && at(v) < K;
-      if constexpr (WHOLE) {
-        const u32x4 q = ok ? *reinterpret_cast<const u32x4*>(p + at(v)) : u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[v * 4 + i] = q[i];
-      } else if constexpr (EB == 4) {
-        r.w[v] = ok ? __builtin_bit_cast(uint32_t, p[at(v)]) : 0u;
+      if (on && place(v) < K) {
+        load_vector<DT, VEC, MODE>(p + at(v, K), K, r.w + v * 4);
       } else {
-        r.w[v] = ok ? __builtin_bit_cast(uint16_t, p[at(v)]) : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[v * 4 + i] = 0u;
       }
     }
   }
-  static __device__ __forceinline__ void floats(const Raw& r, float (&f)[EPT]) {
-    if constexpr (WHOLE) {
-      raw_to_floats<DT, NV * 4>(r.w, f);
-    } else {
+  static __device__ __forceinline__ void floats(const Raw& r, int K, float (&f)[EPT]) {  // 0 where they are not its own
+    raw_to_floats<DT, NV * 4>(r.w, f);
+    if constexpr (MODE == kLoose)
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if constexpr (EB == 4) f[v] = __builtin_bit_cast(float, r.w[v]);
-        else f[v] = (float)__builtin_bit_cast(E, (uint16_t)r.w[v]);
-      }
-    }
+      for (int e = 0; e < EPT; ++e) f[e] = own(e, K) ? f[e] : 0.0f;
   }
   static __device__ __forceinline__ void store(const float (&f)[EPT], void* base, int64_t row, int K) {
     E* p = reinterpret_cast<E*>(base) + row * K;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      if (at(v) >= K) continue;
-      if constexpr (WHOLE) {
-        u32x4 q;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = pack2<DT>(f[v * VEC + i * (4 / EB)], f[v * VEC + i * (4 / EB) + (EB == 2)]);
-        *reinterpret_cast<u32x4*>(p + at(v)) = q;
-      } else {
-        p[at(v)] = (E)f[v];
-      }
-    }
+    for (int v = 0; v < NV; ++v)
+      if (place(v) < K) store_vector<DT, VEC, MODE>(p + at(v, K), place(v) - at(v, K), K, f + v * VEC);
   }
   // a parameter of the thread's columns, `none` outside and where p is NULL
   static __device__ __forceinline__ void param(const void* p, const ResArgs& a, float none, float (&f)[NP]) {
     const E* q = reinterpret_cast<const E*>(p);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int c = at(i * GR / VEC) + i * GR % VEC;
-      const float v = p ? (float)q[c < a.K ? channel_of(c, a.mT) : 0] : none;
-      f[i] = c < a.K ? v : none;
+      const bool mine = own(i * GR, a.K);
+      const float v = p ? (float)q[mine ? channel_of(at(i * GR / VEC, a.K) + i * GR % VEC, a.mT) : 0] : none;
+      f[i] = mine ? v : none;
     }
   }
   // the sum over a row's threads
   static __device__ __forceinline__ float total(float s, float* red, int& slot) {
-    s += dpp<0x128>(s);  // rows of 16 lanes rotated by 8, 4, 2, 1
-    s += dpp<0x124>(s);
-    s += dpp<0x122>(s);
-    s += dpp<0x121>(s);
-    if constexpr (LANES >= 64) {
+    if constexpr (LANES < 16) {
+      s += dpp<0xB1>(s);  // quad_perm 1 0 3 2, then 2 3 0 1
+      s += dpp<0x4E>(s);
+      if constexpr (LANES == 8) s += dpp<0x141>(s);  // half row mirrored: the other quad
+    } else {
+      s += dpp<0x128>(s);  // rows of 16 lanes rotated by 8, 4, 2, 1
+      s += dpp<0x124>(s);
+      s += dpp<0x122>(s);
+      s += dpp<0x121>(s);
+    }
+    if constexpr (LANES >= 32) {
       float t = s;
       swap16(s, t);
       s += t;
-      t = s;
+    }
+    if constexpr (LANES >= 64) {
+      float t = s;
       swap32(s, t);
       s += t;
     }
@@ -120,7 +117,7 @@ struct ResRow {
       for (int e = 0; e < EPT; ++e) s += f[e];
       const float mean = total(s, red, slot) / (float)a.K;
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) f[e] = at(e / VEC) + e % VEC < a.K ? f[e] - mean : 0.0f;
+      for (int e = 0; e < EPT; ++e) f[e] = own(e, a.K) ? f[e] - mean : 0.0f;
       s = 0.0f;
     }
 #pragma unroll
@@ -143,7 +140,7 @@ struct ResRow {
     m = a.rms ? 0.0f : total(m, red, slot) / (float)a.K;
 #pragma unroll
     for (int e = 0; e < EPT; ++e)
-      g[e] = at(e / VEC) + e % VEC < a.K ? k * (g[e] - __builtin_fmaf(f[e], s, m)) : 0.0f;
+      g[e] = own(e, a.K) ? k * (g[e] - __builtin_fmaf(f[e], s, m)) : 0.0f;
   }
 };
 
@@ -171,9 +168,9 @@ __device__ __forceinline__ void res_scale(const ResArgs& a, const ResPlace& p, f
   for (int i = 0; i < R::NP; ++i) k[i] *= g[i];
 }
 
-template <int DT, int LANES, int EPT, bool WHOLE, int GR>
-__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void eql_res_fwd_kernel(const ResArgs a) {
-  using R = ResRow<DT, LANES, EPT, WHOLE, GR>;
+template <int DT, int LANES, int EPT, int MODE, int GR>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, MODE, GR>::THREADS)) void eql_res_fwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, MODE, GR>;
   __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
   const ResPlace p = res_place(a);
   int slot = 0;
@@ -194,8 +191,8 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
   for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
     const int64_t row = p.q * a.rows + i;
     float x[EPT], u[EPT];
-    R::floats(xr, x);
-    if (a.u) R::floats(ur, u);
+    R::floats(xr, a.K, x);
+    if (a.u) R::floats(ur, a.K, u);
     if (i + R::ROWS < p.last) fetch(i + R::ROWS);
     if (a.u) {
       if (a.pw) {
@@ -217,12 +214,30 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
 }
 
 // Rows of column sums: dw, db (where there is a norm after), then E, or P and S.
-template <int DT, int LANES, int EPT, bool WHOLE, int GR>
-__global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void eql_res_bwd_kernel(const ResArgs a) {
-  using R = ResRow<DT, LANES, EPT, WHOLE, GR>;
+template <int DT, int LANES, int EPT, int MODE, int GR>
+__global__ __launch_bounds__((ResRow<DT, LANES, EPT, MODE, GR>::THREADS)) void eql_res_bwd_kernel(const ResArgs a) {
+  using R = ResRow<DT, LANES, EPT, MODE, GR>;
   constexpr int NP = R::NP;
   __shared__ float red[2 * (LANES > 64 ? LANES / 64 : 1)];
   __shared__ float cols[R::ROWS > 1 ? R::ROWS * LANES * NP : 1];
+  // Parameters of a thread's own in LDS where 1024 threads leave each 128 registers: a row's are read as it needs them
+  // (kept in registers they go to scratch memory with every row).
+  constexpr bool PARK = LANES == 1024 && GR == 1;
+  __shared__ floatx4 parked[PARK ? NP * LANES : 1];
+  auto park = [&](int j, const float (&f)[NP]) {
+    if constexpr (PARK)
+#pragma unroll
+      for (int i = 0; i < NP; i += 4) parked[(j * NP + i) / 4 * LANES + threadIdx.x] = floatx4{f[i], f[i + 1], f[i + 2], f[i + 3]};
+  };
+  auto again = [&](int j, float (&f)[NP]) {
+    if constexpr (PARK)
+#pragma unroll
+      for (int i = 0; i < NP; i += 4) {
+        const floatx4 v = parked[(j * NP + i) / 4 * LANES + threadIdx.x];
+#pragma unroll
+        for (int o = 0; o < 4; ++o) f[i + o] = v[o];
+      }
+  };
   const ResPlace p = res_place(a);
   int slot = 0;
   const int mine = LANES < 256 ? threadIdx.x / LANES : 0;
@@ -235,25 +250,33 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
     if (a.dh) R::load(hr, a.dh, row, a.K, on);
     if (a.dr) R::load(rr, a.dr, row, a.K, on);
   };
-  fetch(p.first + mine);
+  if (!PARK) fetch(p.first + mine);  // (PARK: no registers for two rows)
   float k[NP], w[NP], pw[NP], pb[NP];
   res_scale<R>(a, p, k);
   R::param(a.w, a, 0.0f, w);
   R::param(a.pw, a, 0.0f, pw);
   R::param(a.pb, a, 0.0f, pb);
+  park(0, k);
+  park(1, w);
+  park(2, pw);
+  park(3, pb);
   float s0[NP], s1[NP], s2[NP], s3[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) s0[i] = s1[i] = s2[i] = s3[i] = 0.0f;
   for (int64_t i = p.first + mine; i < p.last; i += R::ROWS) {
     const int64_t row = p.q * a.rows + i;
     float x[EPT], u[EPT], g[EPT], d[EPT], fu = 1.0f;
-    R::floats(xr, x);
-    if (a.u) R::floats(ur, u);
-    if (a.dh) R::floats(hr, g);
-    if (a.dr) R::floats(rr, d);
-    if (i + R::ROWS < p.last) fetch(i + R::ROWS);
+    if (PARK) fetch(i);
+    R::floats(xr, a.K, x);
+    if (a.u) R::floats(ur, a.K, u);
+    if (a.dh && !PARK) R::floats(hr, a.K, g);
+    if (a.dr && !PARK) R::floats(rr, a.K, d);
+    if (!PARK && i + R::ROWS < p.last) fetch(i + R::ROWS);
     if (a.u) {
+      again(0, k);
       if (a.pw) {
+        again(2, pw);
+        again(3, pb);
         fu = R::normed(u, a, red, slot);  // u: uh
 #pragma unroll
         for (int e = 0; e < EPT; ++e) x[e] = __builtin_fmaf(k[e / GR], __builtin_fmaf(u[e], pw[e / GR], pb[e / GR]), x[e]);
@@ -264,6 +287,8 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
     }
     if (a.dh) {
       const float fr = R::normed(x, a, red, slot);  // x: rh
+      again(1, w);
+      if (PARK) R::floats(hr, a.K, g);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) {
         s0[e / GR] = __builtin_fmaf(g[e], x[e], s0[e / GR]);
@@ -271,10 +296,12 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
         g[e] *= w[e / GR];
       }
       R::back(g, x, fr, a, red, slot);
+      if (a.dr && PARK) R::floats(rr, a.K, d);
       if (a.dr)
 #pragma unroll
         for (int e = 0; e < EPT; ++e) g[e] += d[e];
     } else {
+      if (a.dr && PARK) R::floats(rr, a.K, d);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) g[e] = a.dr ? d[e] : 0.0f;
     }
@@ -282,7 +309,9 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
     if (a.u) {
 #pragma unroll
       for (int e = 0; e < EPT; ++e) s2[e / GR] = __builtin_fmaf(g[e], u[e], s2[e / GR]);
+      again(0, k);
       if (a.pw) {
+        again(2, pw);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
           s3[e / GR] += g[e];
@@ -304,8 +333,8 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
       if (j) __syncthreads();
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int c = (R::at(i * GR / R::VEC) + i * GR % R::VEC) / GR;
-        if (c < K) cols[mine * (LANES * NP) + c] = s[i];
+        const int c = (R::at(i * GR / R::VEC, a.K) + i * GR % R::VEC) / GR;
+        if (R::own(i * GR, a.K)) cols[mine * (LANES * NP) + c] = s[i];
       }
       __syncthreads();
       for (int c = threadIdx.x; c < K; c += R::THREADS) {
@@ -317,8 +346,8 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, WHOLE, GR>::THREADS)) void 
     } else {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int c = (R::at(i * GR / R::VEC) + i * GR % R::VEC) / GR;
-        if (c < K) part[(int64_t)j * K + c] = s[i];
+        const int c = (R::at(i * GR / R::VEC, a.K) + i * GR % R::VEC) / GR;
+        if (R::own(i * GR, a.K)) part[(int64_t)j * K + c] = s[i];
       }
     }
     ++j;

@@ -46,7 +46,7 @@ def grads(seed, t):
 @pytest.mark.parametrize("W", range(1, 9))
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 def test_widths(W, dt):
-    for B, L, C, T in ((2, 1, 8, 4), (1, 3, 5, 3), (2, 70, 24, 8), (3, 130, 7, 1)):
+    for B, L, C, T in ((2, 1, 8, 4), (1, 3, 5, 3), (2, 70, 24, 8), (3, 130, 7, 1), (2, 40, 3, 1), (1, 33, 2053, 1)):
         t = make(W + L, B, L, C, T, W, dt)
         for act in ("none", "silu"):
             check(t, activation=act)
@@ -104,10 +104,11 @@ def test_layouts(dt, cut):
 
 @pytest.mark.parametrize("dt", ["f32", "f16"])
 @pytest.mark.parametrize("W", [2, 4, 8])
-def test_carrying_on(dt, W):
+@pytest.mark.parametrize("C,T", [(6, 4), (7, 3), (3, 1), (2053, 1)])
+def test_carrying_on(dt, W, C, T):
     """Pieces of 1, 2, 17 and 60 tokens with the state updated in place, against the whole sequence."""
     from paper_2607_21271_amd.scan import causal_conv
-    t = make(9, 2, 80, 6, 4, W, dt)
+    t = make(9, 2, 80, C, T, W, dt)
     want = R.conv(**t, activation="silu")
     state, at, ys = t["state"].clone(), 0, []
     for n in (1, 2, 17, 60):

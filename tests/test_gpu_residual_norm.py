@@ -55,7 +55,7 @@ def grads(seed, t):
 
 # rows of one element up to the largest, on and off whole vectors, of every number of threads a row
 ROWS = [(2, 3, 1, 1), (3, 5, 5, 3), (2, 9, 16, 8), (1, 7, 130, 1), (2, 40, 96, 8), (1, 5, 115, 3), (2, 6, 129, 8), (1, 4, 1025, 2), (2, 3, 4096, 1),
-        (1, 3, 1024, 8), (1, 2, 8191, 1), (2, 1, 520, 8)]
+        (1, 3, 1024, 8), (1, 2, 8191, 1), (2, 1, 520, 8), (3, 70, 9, 1), (2, 40, 11, 5), (2, 70, 67, 3), (1, 2, 8192, 1), (2, 3, 1365, 3), (1, 700, 2, 3)]
 
 
 @pytest.mark.parametrize("size", ROWS, ids=lambda s: "x".join(map(str, s)))
