@@ -13,7 +13,7 @@ namespace eqk {
 constexpr unsigned channel_factor(int T) { return (unsigned)(((1 << 21) + T - 1) / T); }
 __device__ __forceinline__ int channel_of(int ct, unsigned m) { return (int)__umulhi((unsigned)ct << 11, m); }
 
-// How rows of the convolution and the residual norm are read and written (eql_vectors.h).
+// How rows are read and written (eql_vectors.h, ScanTile).
 constexpr int kWhole = 0, kLoose = 1, kTiny = 2;
 
 // ---- selective scan ----
@@ -49,7 +49,7 @@ struct ScanArgs {
   unsigned mT;           // channel_factor(T)
   int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
-  int whole;  // every vector of a wave's columns is aligned and inside its group
+  int mode;  // how rows are read and written (ScanTile)
 };
 
 // Fills CT .. P, chunk and tiles for the forward or the backward pass.

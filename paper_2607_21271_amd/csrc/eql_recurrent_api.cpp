@@ -129,19 +129,14 @@ int scan_inputs(const eqlinear_scan_shape* s, const eqk::ScanArgs& a, const void
   return EQL_OK;
 }
 
-// Whether the column blocks of every tensor can be read and written in whole vectors.
-int scan_whole(const eqk::ScanArgs& a, int dtype) {
+// How the kernels read and write: a tile's tokens are addressed by 31 bits from its first.
+int scan_mode(const eqk::ScanArgs& a, int dtype) {
   const int vec = eqk::scan_vec(dtype, eqk::scan_lanes(a.N));
-  const size_t e = elem_bytes(dtype);
-  const int64_t none[1] = {0};
-  // a tile's tokens are addressed by 31 bits from its first
   const int64_t steps[6] = {a.CT, a.xs[1], a.ds[1], a.z ? a.zs[1] : 0, a.bs[1], a.cs[1]};
   for (int64_t st : steps)
-    if (st >= ((int64_t)1 << 31) / 128) return 0;
-  if (a.N % 4 != 0 || !aligned(a.A, 16) || !vectors(a.b, a.bs, 3, e, 4) || !vectors(a.c, a.cs, 3, e, 4)) return 0;
-  return a.CTg % vec == 0 && vectors(a.x, a.xs, 2, e, vec) && vectors(a.delta, a.ds, 2, e, vec) &&
-         vectors(a.z, a.zs, 2, e, vec) && vectors(a.y, none, 1, e, vec) && vectors(a.dy, none, 1, e, vec) &&
-         vectors(a.dx, none, 1, e, vec) && vectors(a.ddelta, none, 1, e, vec) && vectors(a.dz, none, 1, e, vec);
+    if (st >= ((int64_t)1 << 31) / 128) return eqk::kTiny;
+  if (a.CTg < vec) return eqk::kTiny;
+  return a.CTg % vec == 0 && a.N % 4 == 0 && aligned(a.A, 16) ? eqk::kWhole : eqk::kLoose;
 }
 
 }  // namespace
@@ -287,7 +282,7 @@ int eqlinear_selective_scan(const eqlinear_scan_shape* s, const void* x, const v
   a.states = states;
   a.carry = (float*)workspace;
   a.sums = (float*)((char*)workspace + scan_carry(a));
-  a.whole = scan_whole(a, s->dtype);
+  a.mode = scan_mode(a, s->dtype);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::scan_forward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::scan_forward<eqk::kF16>(a, st));
@@ -350,7 +345,7 @@ int eqlinear_selective_scan_backward(const eqlinear_scan_shape* s, const void* x
   a.sums = (float*)((char*)workspace + scan_carry(a));
   a.part = (float*)((char*)workspace + scan_carry(a) + scan_sums(a));
   a.bcpart = (float*)((char*)workspace + scan_carry(a) + scan_sums(a) + scan_part(a));
-  a.whole = scan_whole(a, s->dtype);
+  a.mode = scan_mode(a, s->dtype);
   hipStream_t st = (hipStream_t)stream;
   if (s->dtype == EQL_F32) return launched(eqk::scan_backward<eqk::kF32>(a, st));
   if (s->dtype == EQL_F16) return launched(eqk::scan_backward<eqk::kF16>(a, st));

@@ -116,14 +116,18 @@ __device__ __forceinline__ int scan_channel(const ScanArgs& a, int ct) { return 
 constexpr uint32_t kScanDrop = 0x80000000u;  // an offset past every resource: loads give 0, stores go nowhere
 
 // The lane's elements of a tile of [TT][CH]: NV vectors of VEC, vector v at token tok(v), column at.
-// WHOLE: vectors through a buffer resource that ends behind the tile's last token, else single elements.
-template <int DT, int NL, bool WHOLE>
+// kWhole, kLoose: vectors through a buffer resource that ends behind the tile's last token, at the elements' own
+// alignment.  kLoose: a group's last vector, where it is not full, is read so that it ends where the group does, and moved
+// to its place as it is used (which would cost kWhole 5 %); so are the last run of a token's b and c.  kTiny (groups
+// shorter than a vector, tokens further apart than 31 bits reach): single elements.
+template <int DT, int NL, int MODE>
 struct ScanTile {
   static constexpr int CH = scan_cols(NL), TT = scan_tile(NL), EPT = scan_ept(NL), VEC = scan_vec(DT, NL);
   static constexpr int NV = EPT / VEC, VT = CH / VEC, EB = DT == kF32 ? 4 : 2;
   static constexpr int W = VEC * EB / 4;  // 32-bit words of a vector
   static constexpr int NP = 4 * NL;
   static constexpr int NB = (TT * NL + 63) / 64;  // runs of four of b, and of c, that a lane loads
+  static constexpr int BW = MODE == kLoose && NL == 1 ? 4 : EB;  // words of such a run (N < 4: one for each element)
   using E = typename Elem<DT>::T;
   struct Raw {
     uint32_t w[NV * W];
@@ -131,29 +135,39 @@ struct ScanTile {
   static __device__ __forceinline__ int at() { return (threadIdx.x & 63) % VT * VEC; }
   static __device__ __forceinline__ int tok(int v) { return v * (64 / VT) + (threadIdx.x & 63) / VT; }
 
+  // whether a vector of the wave's is partly outside its group, the same for all lanes; columns of the lane's that are
+  static __device__ __forceinline__ bool part(int left) { return MODE == kLoose && left < CH && left % VEC != 0; }
+  static __device__ __forceinline__ int beyond(int left) { return at() < left ? max(at() + VEC - left, 0) : 0; }
+  // columns before the wave's first that its resources begin with: a vector that is moved back may start there
+  static __device__ __forceinline__ int lead(int left) { return part(left) ? VEC : 0; }
+
   // A tensor's place in the tile: the lane's byte offsets and the tokens' stride.
   struct View {
-    const char* p;  // of the wave's first column, sequence and token 0
+    const char* p;  // of the wave's first column, less `lead`, sequence and token 0
     int64_t stride;
-    uint32_t off[WHOLE ? NV : 1];
+    uint32_t off[MODE != kTiny ? NV : 1];
   };
   static __device__ __forceinline__ View view(const void* p, int64_t first, int64_t stride, int left) {
     View r;
-    r.p = reinterpret_cast<const char*>(p) + first * EB;
     r.stride = stride;
-    if constexpr (WHOLE) {
+    if constexpr (MODE != kTiny) {
+      const int back = part(left) ? VEC - beyond(left) : 0;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) r.off[v] = at() < left ? (uint32_t)((tok(v) * (int)stride + at()) * EB) : kScanDrop;
+      for (int v = 0; v < NV; ++v) r.off[v] = at() < left ? (uint32_t)((tok(v) * (int)stride + at() + back) * EB) : kScanDrop;
     }
+    return rebased(r, p, first, left);
+  }
+  static __device__ __forceinline__ View rebased(View r, const void* p, int64_t first, int left) {
+    r.p = reinterpret_cast<const char*>(p) + (first - lead(left)) * EB;
     return r;
   }
   static __device__ __forceinline__ __amdgpu_buffer_rsrc_t resource(const View& w, int64_t l, int rows, int left) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(w.p + l * w.stride * EB), (short)0,
-                                             ((rows - 1) * (int)w.stride + left) * EB, 0x00020000);
+                                             ((rows - 1) * (int)w.stride + left + lead(left)) * EB, 0x00020000);
   }
   // tokens l .. l + nt (nt > 0); what lies behind them may be anything
   static __device__ __forceinline__ void load(Raw& r, const View& w, int64_t l, int nt, int left) {
-    if constexpr (WHOLE) {
+    if constexpr (MODE != kTiny) {
       const auto rs = resource(w, l, nt, left);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -187,7 +201,25 @@ struct ScanTile {
       }
     }
   }
-  static __device__ __forceinline__ void floats(const Raw& r, float (&f)[EPT]) { raw_to_floats<DT, NV * W>(r.w, f); }
+  static __device__ __forceinline__ void floats(const Raw& r, int left, float (&f)[EPT]) {
+    Raw q = r;
+    if (part(left)) {  // elements down by what is beyond, 0 there
+      const int by = beyond(left), words = EB == 4 ? by : by / 2;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        uint32_t* const w = q.w + v * W;
+#pragma unroll
+        for (int d = 1; d < W; d *= 2)
+#pragma unroll
+          for (int i = 0; i < W; ++i) w[i] = words & d ? (i + d < W ? w[i + d] : 0u) : w[i];
+        if constexpr (EB == 2)
+#pragma unroll
+          for (int i = 0; i < W; ++i) w[i] = __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : 0u, w[i], by % 2 * 16);
+      }
+    }
+    // (one conversion behind the branch: with one on either side of it the compiler lost an element of the gradients' f16 tiles)
+    raw_to_floats<DT, NV * W>(q.w, f);
+  }
   // the same words, whose conversion is not kept from an earlier one
   static __device__ __forceinline__ void again(Raw& r) {
 #pragma unroll
@@ -200,15 +232,25 @@ struct ScanTile {
 
   // stores tokens l .. l + rows
   static __device__ __forceinline__ void store(const float (&f)[EPT], const View& w, int64_t l, int rows, int left) {
-    if constexpr (WHOLE) {
+    if constexpr (MODE != kTiny) {
       const auto rs = resource(w, l, rows, left);
+      const int by = part(left) ? beyond(left) : 0;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         uint32_t q[W];
 #pragma unroll
         for (int i = 0; i < W; ++i) q[i] = pack2<DT>(f[v * VEC + i * (4 / EB)], f[v * VEC + i * (4 / EB) + (EB == 2)]);
-        if constexpr (W == 4) __builtin_amdgcn_raw_buffer_store_b128(u32x4{q[0], q[1], q[2], q[3]}, rs, w.off[v], 0, 0);
-        else __builtin_amdgcn_raw_buffer_store_b64(u32x2{q[0], q[1]}, rs, w.off[v], 0, 0);
+        const uint32_t off = by > 0 ? kScanDrop : w.off[v];
+        if constexpr (W == 4) __builtin_amdgcn_raw_buffer_store_b128(u32x4{q[0], q[1], q[2], q[3]}, rs, off, 0, 0);
+        else __builtin_amdgcn_raw_buffer_store_b64(u32x2{q[0], q[1]}, rs, off, 0, 0);
+        if (part(left)) {  // one element after the other
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const uint32_t o = by > 0 && i + by < VEC ? w.off[v] + (i + by) * EB : kScanDrop;
+            if constexpr (EB == 4) __builtin_amdgcn_raw_buffer_store_b32(q[i], rs, o, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(q[i / 2] >> i % 2 * 16), rs, o, 0, 0);
+          }
+        }
       }
     } else {
       E* p = reinterpret_cast<E*>(const_cast<char*>(w.p)) + l * w.stride;
@@ -243,70 +285,108 @@ struct ScanTile {
   }
   // b or c of a tile: runs of four, i * 64 + lane of [TT][NP / 4]
   struct Bc {
-    uint32_t w[NB * EB];
+    uint32_t w[NB * BW];
   };
   static __device__ __forceinline__ void load_bc(Bc& r, const void* base, int64_t first, int64_t stride, int nt, int N) {
     const char* p = reinterpret_cast<const char*>(base) + first * EB;
+    if constexpr (MODE != kTiny) {
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, ((nt - 1) * (int)stride + N) * EB, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int j = i * 64 + (threadIdx.x & 63), t = j / NL, n = j % NL * 4;
-      if constexpr (WHOLE) {
-        const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, ((nt - 1) * (int)stride + N) * EB, 0x00020000);
-        const uint32_t off = n < N && t < nt ? (uint32_t)((t * (int)stride + n) * EB) : kScanDrop;
+      for (int i = 0; i < NB; ++i) {
+        const int j = i * 64 + (threadIdx.x & 63), t = j / NL, n = j % NL * 4;
+        const bool on = n < N && t < nt;
+        if (MODE == kLoose && NL == 1 && N < 4) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t off = on && q < N ? (uint32_t)((t * (int)stride + q) * EB) : kScanDrop;
+            if constexpr (EB == 4) r.w[i * BW + q] = __builtin_amdgcn_raw_buffer_load_b32(rs, off, 0, 0);
+            else r.w[i * BW + q] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, off, 0, 0);
+          }
+          continue;
+        }
+        // (a last run that is not full ends where the row does)
+        const uint32_t off = on ? (uint32_t)((t * (int)stride + (MODE == kLoose ? min(n, N - 4) : n)) * EB) : kScanDrop;
         if constexpr (EB == 4) {
           const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0));
 #pragma unroll
-          for (int q = 0; q < 4; ++q) r.w[i * 4 + q] = x[q];
+          for (int q = 0; q < 4; ++q) r.w[i * BW + q] = x[q];
         } else {
           const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0));
-          r.w[i * 2] = x[0];
-          r.w[i * 2 + 1] = x[1];
+          r.w[i * BW] = x[0];
+          r.w[i * BW + 1] = x[1];
         }
-      } else {
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int j = i * 64 + (threadIdx.x & 63), t = j / NL, n = j % NL * 4;
         const E* q = reinterpret_cast<const E*>(p) + t * stride + n;
         const int m = t < nt ? N - n : 0;
         if constexpr (EB == 4) {
 #pragma unroll
-          for (int o = 0; o < 4; ++o) r.w[i * 4 + o] = o < m ? __builtin_bit_cast(uint32_t, q[o]) : 0u;
+          for (int o = 0; o < 4; ++o) r.w[i * BW + o] = o < m ? __builtin_bit_cast(uint32_t, q[o]) : 0u;
         } else {
           const uint16_t* h = reinterpret_cast<const uint16_t*>(q);
 #pragma unroll
           for (int o = 0; o < 2; ++o) {
             const uint32_t lo = 2 * o < m ? h[2 * o] : 0u, hi = 2 * o + 1 < m ? h[2 * o + 1] : 0u;
-            r.w[i * 2 + o] = lo | hi << 16;
+            r.w[i * BW + o] = lo | hi << 16;
           }
         }
       }
     }
   }
-  static __device__ __forceinline__ void put_bc(float* tile, const Bc& r) {
-    float f[NB * 4];
-    raw_to_floats<DT, NB * EB>(r.w, f);
+  static __device__ __forceinline__ void put_bc(float* tile, const Bc& r, int N) {
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int j = i * 64 + (threadIdx.x & 63);
-      if (TT * NL >= 64 || j < TT * NL)
-        *reinterpret_cast<floatx4*>(tile + j * 4) = floatx4{f[i * 4], f[i * 4 + 1], f[i * 4 + 2], f[i * 4 + 3]};
+      const int j = i * 64 + (threadIdx.x & 63), n = j % NL * 4;
+      uint32_t w[EB];
+#pragma unroll
+      for (int q = 0; q < EB; ++q) w[q] = r.w[i * BW + q];
+      if (MODE == kLoose && NL == 1 && N < 4) {
+        if constexpr (EB == 2 && BW == 4) {
+          w[0] = r.w[i * BW] | r.w[i * BW + 1] << 16;
+          w[1] = r.w[i * BW + 2];
+        }
+      } else if (MODE == kLoose && N % 4 != 0) {  // the last run's states down to their places, 0 behind them
+        const int by = n < N ? max(n + 4 - N, 0) : 0;
+        if constexpr (EB == 4) {
+#pragma unroll
+          for (int d = 1; d < 4; d *= 2)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = by & d ? (q + d < 4 ? w[q + d] : 0u) : w[q];
+        } else {
+          const uint32_t lo = by & 2 ? w[1] : w[0], hi = by & 2 ? 0u : w[1];
+          w[0] = __builtin_amdgcn_alignbit(hi, lo, by % 2 * 16);
+          w[1] = hi >> by % 2 * 16;
+        }
+      }
+      float f[4];
+      raw_to_floats<DT, EB>(w, f);
+      if (TT * NL >= 64 || j < TT * NL) *reinterpret_cast<floatx4*>(tile + j * 4) = floatx4{f[0], f[1], f[2], f[3]};
     }
   }
 };
 
-// A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.  WHOLE: four states are all
+// A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.  kWhole: four states are all
 // inside or all outside, and rows of A whole 16-byte words (what lies outside is read from A's start instead).
-template <int NL, bool WHOLE>
+template <int NL, int MODE>
 __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int m = c0 + q < p.left ? a.N - n0 : 0;
     const float* s = a.A + (m > 0 ? scan_channel(a, p.ct0 + c0 + q) * a.N + n0 : 0);
-    if constexpr (WHOLE) {
+    if constexpr (MODE == kWhole) {
       const floatx4 v = *reinterpret_cast<const floatx4*>(s);
 #pragma unroll
       for (int n = 0; n < 4; ++n) A2[q][n] = m > 0 ? v[n] * kLog2e : 0.0f;
     } else {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) A2[q][n] = n < m ? s[n] * kLog2e : 0.0f;
+      for (int n = 0; n < 4; ++n) {
+        const float v = s[n < m ? n : 0];
+        A2[q][n] = n < m ? v * kLog2e : 0.0f;
+      }
     }
   }
 }
@@ -332,27 +412,32 @@ __device__ __forceinline__ void store_padded(float* base, const float (&h)[4][4]
 template <int NL>
 __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* base, float (&h)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
-  const bool whole = a.N == 4 * NL && ((uintptr_t)base & 15) == 0;
+  const bool whole = a.N % 4 == 0 && ((uintptr_t)base & 15) == 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
     if (whole) {
-      const floatx4 v = *reinterpret_cast<const floatx4*>(c0 + q < p.left ? s : base);
+      const bool on = c0 + q < p.left && n0 < a.N;
+      const floatx4 v = *reinterpret_cast<const floatx4*>(on ? s : base);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) h[q][n] = c0 + q < p.left ? v[n] : 0.0f;
+      for (int n = 0; n < 4; ++n) h[q][n] = on ? v[n] : 0.0f;
     } else {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) h[q][n] = c0 + q < p.left && n0 + n < a.N ? s[n] : 0.0f;
+      for (int n = 0; n < 4; ++n) {
+        const bool on = c0 + q < p.left && n0 + n < a.N;
+        const float v = *(on ? s + n : base);
+        h[q][n] = on ? v : 0.0f;
+      }
     }
   }
 }
 template <int NL>
 __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& p, float* base, const float (&h)[4][4]) {
   const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
-  const bool whole = a.N == 4 * NL && ((uintptr_t)base & 15) == 0;
+  const bool whole = a.N % 4 == 0 && ((uintptr_t)base & 15) == 0;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
-    if (c0 + q >= p.left) continue;
+    if (c0 + q >= p.left || n0 >= a.N) continue;
     float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
     if (whole) {
       *reinterpret_cast<floatx4*>(s) = floatx4{h[q][0], h[q][1], h[q][2], h[q][3]};
@@ -364,12 +449,12 @@ __device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& 
   }
 }
 // The parameter of the channels of the lane's vector, 0 outside and where src is NULL.
-template <int VEC, bool WHOLE>
+template <int VEC, int MODE>
 __device__ __forceinline__ void scan_param(const ScanArgs& a, const ScanPlace& p, const float* src, int at, float (&f)[VEC]) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) f[i] = 0.0f;
   if (!src) return;
-  if (WHOLE && a.T % VEC == 0) {  // one channel
+  if (MODE == kWhole && a.T % VEC == 0) {  // one channel
     const float v = src[at < p.left ? scan_channel(a, p.ct0 + at) : 0];
 #pragma unroll
     for (int i = 0; i < VEC; ++i) f[i] = at < p.left ? v : 0.0f;
@@ -406,9 +491,9 @@ template <int NL>
 constexpr int scan_fwd_lds() {  // floats of a wave
   return 2 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
 }
-template <int DT, int NL, bool WHOLE, bool STATES>
+template <int DT, int NL, int MODE, bool STATES>
 __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL, WHOLE>;
+  using TL = ScanTile<DT, NL, MODE>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   constexpr int RUN = scan_run(NL);
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
@@ -439,9 +524,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   };
   if (p.begin < stop) fetch(p.begin);
   float A2[4][4], h[4][4], bias[VEC], skip[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
-  scan_decay<NL, WHOLE>(a, p, A2);
-  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
-  if constexpr (!STATES) scan_param<VEC, WHOLE>(a, p, a.D, at, skip);
+  scan_decay<NL, MODE>(a, p, A2);
+  scan_param<VEC, MODE>(a, p, a.bias, at, bias);
+  if constexpr (!STATES) scan_param<VEC, MODE>(a, p, a.D, at, skip);
   const int64_t slot = (p.b * a.K + p.k) * a.cols + p.col0;
   if (!STATES && a.K > 1) load_padded<NL>(a.carry + slot * NP, h);
   else if (!STATES && a.h0) load_state<NL>(a, p, a.h0, h);
@@ -455,8 +540,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     typename TL::Raw xc = xr, zc = zr;  // of this tile, while the next one's are on their way
     {
       float xf[EPT], df[EPT];
-      TL::floats(dr, df);
-      TL::floats(xr, xf);
+      TL::floats(dr, p.left, df);
+      TL::floats(xr, p.left, xf);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) df[e] += bias[e % VEC];
       if (a.softplus)
@@ -471,8 +556,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
 #pragma unroll
       for (int e = 0; e < EPT; ++e) df[e] *= xf[e];
       TL::put(us, df);
-      TL::put_bc(bs, br);
-      if constexpr (!STATES) TL::put_bc(cs, cr);
+      TL::put_bc(bs, br, a.N);
+      if constexpr (!STATES) TL::put_bc(cs, cr, a.N);
     }
     if (l0 + TT < stop) fetch(l0 + TT);
     if constexpr (!STATES)
@@ -545,12 +630,12 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
       float xf[EPT], yf[EPT];
       TL::get(us, yf);
       TL::again(xc);
-      TL::floats(xc, xf);
+      TL::floats(xc, p.left, xf);
 #pragma unroll
       for (int e = 0; e < EPT; ++e) yf[e] = __builtin_fmaf(skip[e % VEC], xf[e], yf[e]);
       if (a.z) {
         TL::again(zc);
-        TL::floats(zc, xf);
+        TL::floats(zc, p.left, xf);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) yf[e] *= xf[e] * sigmoid(xf[e]);
       }
@@ -619,9 +704,9 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
 
 // ---- gradients ---------------------------------------------------------------
 // r behind a chunk from zero, and its sum of d (chunks 1 .. K - 1): r = a (c s + r) from the last token to the first.
-template <int DT, int NL, bool WHOLE>
+template <int DT, int NL, int MODE>
 __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL, WHOLE>;
+  using TL = ScanTile<DT, NL, MODE>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -648,8 +733,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
   const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
   if (tiles > 0) fetch(p.begin + (tiles - 1) * TT);
   float A2[4][4], r[4][4], bias[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
-  scan_decay<NL, WHOLE>(a, p, A2);
-  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
+  scan_decay<NL, MODE>(a, p, A2);
+  scan_param<VEC, MODE>(a, p, a.bias, at, bias);
 #pragma unroll
   for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -659,11 +744,11 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
     const int nt = (int)min(stop - l0, (int64_t)TT);
     {
       float sf[EPT], df[EPT];
-      TL::floats(yr, sf);
-      TL::floats(dr, df);
+      TL::floats(yr, p.left, sf);
+      TL::floats(dr, p.left, df);
       if (a.z) {
         float zf[EPT];
-        TL::floats(zr, zf);
+        TL::floats(zr, p.left, zf);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
       }
@@ -679,7 +764,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
       wave_order();
       TL::put(ds, df);
       TL::put(ss, sf);
-      TL::put_bc(cs, cr);
+      TL::put_bc(cs, cr, a.N);
     }
     if (tile > 0) fetch(l0 - TT);
     wave_order();
@@ -730,9 +815,9 @@ template <int NL>
 constexpr int scan_bwd_bytes(int waves) {
   return waves * (scan_bwd_lds<NL>() + scan_red_lds<NL>()) * 4;
 }
-template <int DT, int NL, bool WHOLE>
+template <int DT, int NL, int MODE>
 __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
-  using TL = ScanTile<DT, NL, WHOLE>;
+  using TL = ScanTile<DT, NL, MODE>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   constexpr int SUB = scan_run(NL);
   using E = typename TL::E;
@@ -753,16 +838,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   const int64_t stop = min(p.len, p.end);
   const auto xv = TL::view(a.x, p.b * a.xs[0] + p.ct0, a.xs[1], p.left), dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left);
   const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left);
-  auto gv = TL::view(a.dy, p.b * a.L * a.CT + p.ct0, a.CT, p.left);  // the dense tensors
+  const auto gv = TL::view(a.dy, p.b * a.L * a.CT + p.ct0, a.CT, p.left);  // the dense tensors
   auto dense = [&](const void* q) {
-    auto v = gv;
-    v.p = (const char*)q + (p.b * a.L * a.CT + p.ct0) * TL::EB;
-    return v;
+    return TL::rebased(gv, q, p.b * a.L * a.CT + p.ct0, p.left);
   };
   float A2[4][4], g[4][4], dA[4][4], bias[VEC], skip[VEC], dskip[VEC], dbias[VEC];
-  scan_decay<NL, WHOLE>(a, p, A2);
-  scan_param<VEC, WHOLE>(a, p, a.bias, at, bias);
-  scan_param<VEC, WHOLE>(a, p, a.D, at, skip);
+  scan_decay<NL, MODE>(a, p, A2);
+  scan_param<VEC, MODE>(a, p, a.bias, at, bias);
+  scan_param<VEC, MODE>(a, p, a.D, at, skip);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) dskip[i] = dbias[i] = 0.0f;
 #pragma unroll
@@ -822,12 +905,12 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     const int nt = (int)min(stop - l0, (int64_t)TT);
     {
       float xf[EPT], df[EPT], sf[EPT];
-      TL::floats(xr, xf);
-      TL::floats(dr, df);
-      TL::floats(yr, sf);
+      TL::floats(xr, p.left, xf);
+      TL::floats(dr, p.left, df);
+      TL::floats(yr, p.left, sf);
       if (a.z) {
         float zf[EPT];
-        TL::floats(zr, zf);
+        TL::floats(zr, p.left, zf);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
       }
@@ -849,8 +932,8 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
 #pragma unroll
       for (int e = 0; e < EPT; ++e) df[e] *= xf[e];
       TL::put(us, df);
-      TL::put_bc(bs, br);
-      TL::put_bc(cs, cr);
+      TL::put_bc(bs, br, a.N);
+      TL::put_bc(cs, cr, a.N);
     }
     if (tile > 0) fetch_bc(l0 - TT);
     wave_order();
@@ -967,14 +1050,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
       TL::again(xr);
       TL::again(dr);
       TL::again(yr);
-      TL::floats(xr, xf);
+      TL::floats(xr, p.left, xf);
       const int rows = (int)min(p.end - l0, (int64_t)TT);
       float sf[EPT];
-      TL::floats(yr, sf);
+      TL::floats(yr, p.left, sf);
       if (a.z) {
         float zf[EPT], ch[EPT];
         TL::again(zr);
-        TL::floats(zr, zf);
+        TL::floats(zr, p.left, zf);
         TL::get(ss, ch);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -985,7 +1068,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
         if (nt < TT) TL::behind(ch, nt);
         if (a.dz) TL::store(ch, dense(a.dz), l0, rows, p.left);
       }
-      TL::floats(dr, o);
+      TL::floats(dr, p.left, o);
       TL::get(us, f);  // sum_n g b
       float sa[EPT];
       TL::get(ds, sa);  // sum_n A a g h, times log2(e)

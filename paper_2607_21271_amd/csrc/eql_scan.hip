@@ -38,13 +38,13 @@ dim3 wave_blocks(ScanArgs& s, int64_t seqs) {
   return dim3((s.tasks + kScanWaves - 1) / kScanWaves);
 }
 
-template <int NL, bool WHOLE>
+template <int NL, int MODE>
 hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
   const int64_t waves = (int64_t)a.K * a.G * a.nblk;
   if (a.K > 1) {
     hipError_t e = sequences(a, waves, [&](ScanArgs s, int64_t n) {
       const dim3 g = wave_blocks(s, n);
-      hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, true>), g, dim3(64 * kScanWaves), 0, stream, s);
+      hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, MODE, true>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
     e = sequences(a, a.cols * NL / 16, [&](const ScanArgs& s, int64_t n) {
@@ -54,17 +54,17 @@ hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
   }
   return sequences(a, waves, [&](ScanArgs s, int64_t n) {
     const dim3 g = wave_blocks(s, n);
-    hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, WHOLE, false>), g, dim3(64 * kScanWaves), 0, stream, s);
+    hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, MODE, false>), g, dim3(64 * kScanWaves), 0, stream, s);
   });
 }
 
-template <int NL, bool WHOLE>
+template <int NL, int MODE>
 hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
   hipError_t e;
   if (a.K > 1) {
     e = sequences(a, (int64_t)a.K * a.G * a.nblk, [&](ScanArgs s, int64_t n) {
       const dim3 g = wave_blocks(s, n);
-      hipLaunchKernelGGL((eql_scan_back_kernel<DT, NL, WHOLE>), g, dim3(64 * kScanWaves), 0, stream, s);
+      hipLaunchKernelGGL((eql_scan_back_kernel<DT, NL, MODE>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
     e = sequences(a, a.cols * NL / 16, [&](const ScanArgs& s, int64_t n) {
@@ -72,7 +72,7 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
     });
     if (e != hipSuccess) return e;
   }
-  auto k = eql_scan_bwd_kernel<DT, NL, WHOLE>;
+  auto k = eql_scan_bwd_kernel<DT, NL, MODE>;
   const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves, lds = scan_bwd_bytes<NL>(waves);
   if (lds > 65536) {
     e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -96,8 +96,9 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
 
 template <int NL>
 hipError_t pass(const ScanArgs& a, bool back, hipStream_t stream) {
-  if (a.whole) return back ? bwd<NL, true>(a, stream) : fwd<NL, true>(a, stream);
-  return back ? bwd<NL, false>(a, stream) : fwd<NL, false>(a, stream);
+  if (a.mode == kWhole) return back ? bwd<NL, kWhole>(a, stream) : fwd<NL, kWhole>(a, stream);
+  if (a.mode == kLoose) return back ? bwd<NL, kLoose>(a, stream) : fwd<NL, kLoose>(a, stream);
+  return back ? bwd<NL, kTiny>(a, stream) : fwd<NL, kTiny>(a, stream);
 }
 
 hipError_t run(const ScanArgs& a, bool back, hipStream_t stream) {

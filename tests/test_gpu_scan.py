@@ -57,7 +57,10 @@ def grads(seed, t, L):
 # vectors, chunks of tokens
 SIZES = [(1, 1, 1, 1, 1, 1), (2, 1, 8, 4, 16, 1), (3, 5, 6, 1, 4, 2), (2, 17, 12, 8, 16, 1), (1, 16, 3, 5, 7, 3), (2, 33, 40, 8, 16, 2),
          (1, 64, 9, 2, 64, 1), (2, 15, 64, 8, 8, 1), (1, 31, 70, 4, 33, 1), (2, 40, 150, 2, 3, 1), (1, 300, 16, 4, 16, 2), (1, 700, 5, 1, 20, 1),
-         (1, 520, 8, 1, 2, 1), (1, 130, 80, 4, 12, 1), (2, 8, 200, 8, 16, 1)]
+         (1, 520, 8, 1, 2, 1), (1, 130, 80, 4, 12, 1), (2, 8, 200, 8, 16, 1),
+         # a group's last vector not full, in its first block and in a later one; runs of four states not full
+         (2, 37, 75, 3, 7, 3), (1, 70, 131, 5, 13, 1), (2, 40, 67, 1, 1, 1), (1, 50, 261, 1, 3, 1), (1, 90, 33, 1, 62, 1), (2, 25, 105, 3, 21, 3),
+         (3, 2, 205, 5, 11, 1)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
@@ -127,6 +130,20 @@ def test_layouts(dt, cut):
     t = {k: lay(v) for k, v in t.items()}
     t["state"] = state
     check(t, lay(dy), ds)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16"])
+def test_tokens_far_apart(dt):
+    """Tokens 2^24 elements apart, as in a buffer of many sequences side by side."""
+    t = make(13, 1, 3, 6, 3, 7, 1, dt)
+    dy, ds = grads(14, t, 3)
+    wide = torch.zeros(1, 3, (1 << 24) + 5, dtype=t["x"].dtype, device="cuda")
+    for i, k in enumerate(("x", "delta", "z", "Bt", "Ct")):
+        v = t[k].flatten(2)
+        wide[:, :, 100 * i:100 * i + v.shape[2]] = v
+        t[k] = wide[:, :, 100 * i:100 * i + v.shape[2]].unflatten(2, t[k].shape[2:])
+    check(t)
+    check(t, dy, ds)
 
 
 def test_gradient_of_a_broadcast_sum():
