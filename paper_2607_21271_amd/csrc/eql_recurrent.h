@@ -48,7 +48,8 @@ struct ScanArgs {
   unsigned tasks;        // waves of a launch
   unsigned mT;           // channel_factor(T)
   int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
-  int C, T, N, G, CT, CTg, nblk, cols, K, P, softplus;
+  int C, T, N, G, CT, CTg, nblk, cols, K, softplus;
+  int waves, P;  // of a workgroup of the gradients, and those side by side for a group's columns
   int mode;  // how rows are read and written (ScanTile)
 };
 

@@ -143,15 +143,17 @@ int scan_mode(const eqk::ScanArgs& a, int dtype) {
 
 namespace eqk {
 
-// Time of `waves` waves that walk `tiles` tiles each, in tiles of a wave alone on its SIMD: the forward's kernels fit two on
-// one, which hide each other's waiting (a tile of one wave 0.37 us, of two 0.55 us together), the gradients' one.
-static double scan_time(int64_t waves, int64_t tiles, int64_t simds, bool bwd) {
+// Time of `waves` waves that walk `tokens` tokens each, in tokens of a wave alone on its SIMD: the forward's kernels fit two
+// on one, which hide each other's waiting (a token of one wave 0.37 us, of two 0.55 us together), the gradients' one (1.1 us).
+static double scan_time(int64_t waves, int64_t tokens, int64_t simds, bool bwd) {
   const int64_t w = (waves + simds - 1) / simds;
-  return (double)(tiles + 1) * (bwd ? (double)w : 0.75 * w + (w % 2 ? 0.25 : 0.0));
+  return (double)(tokens + 8) * (bwd ? (double)w : 0.75 * w + (w % 2 ? 0.25 : 0.0));
 }
 
-// Chunks of tokens where the columns alone do not fill the device: the number of waves (one to four a SIMD) for
-// which the pass over the states or gradients, half to three quarters of the main one, and the main one take least.
+// Chunks of tokens where the columns alone do not fill the device: the number of waves (one to four a SIMD) for which the
+// pass over the states or gradients, half to three quarters of the main one, and the main one take least.
+// Gradients: workgroups of four, two or one wave, which fill a CU's four SIMDs alike (three where there are no more); smaller
+// ones leave fewer waves without columns, and more sums of db and dc to memory.
 void scan_plan(ScanArgs& a, int cus, bool bwd) {
   const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL);
   a.CT = a.C * a.T;
@@ -161,29 +163,36 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.tiles = (a.L + TT - 1) / TT;
   a.runs = (a.L + scan_run(NL) - 1) / scan_run(NL);
   a.mT = channel_factor(a.T);
-  const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves;
-  a.P = (a.nblk + waves - 1) / waves;
-  const int64_t simds = 4 * (int64_t)cus, one = a.B * a.G * (bwd ? (int64_t)a.P * waves : a.nblk);
-  int64_t per = a.tiles > 0 ? a.tiles : 1;
-  if (one > 0 && one < simds && a.tiles > 1) {
-    const int64_t whole = per;
-    double least = scan_time(one, whole, simds, bwd);
-    for (int w = 1; w <= 4; ++w) {
+  const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1;
+  int64_t per = tiles;
+  double least = -1.0;
+  for (int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves; waves > 0; --waves) {
+    if (waves == 3 && a.nblk > 3) continue;
+    const int P = (a.nblk + waves - 1) / waves;
+    const int64_t one = a.B * a.G * (bwd ? (int64_t)P * waves : a.nblk);
+    // the sums' way out and back in, in tokens of 1.1 us at 5 TB/s
+    const double sums = bwd && P > 1 ? (double)a.B * a.L * a.G * P * 16 * 4 * NL / 5.5e6 + 4.0 : 0.0;
+    auto take = [&](int64_t n, double t) {
+      if (least >= 0.0 && t + sums >= least) return;
+      least = t + sums;
+      per = n;
+      a.P = P;
+      a.waves = waves;
+    };
+    take(tiles, scan_time(one, tiles * TT, simds, bwd));
+    for (int w = 1; w <= 4 && one > 0 && one < simds; ++w) {
       int64_t K = w * simds / one;
-      if (K > whole) K = whole;
+      if (K > tiles) K = tiles;
       if (K < 2) continue;
-      const int64_t n = (whole + K - 1) / K;
-      K = (whole + n - 1) / n;
+      const int64_t n = (tiles + K - 1) / K;
+      K = (tiles + n - 1) / n;
       // (two more launches, and the states between the passes: about ten microseconds)
-      const double t = scan_time(one * K, n, simds, bwd) * (bwd ? 1.3 : 1.7) + (bwd ? 8.0 : 25.0);
-      if (t < least) {
-        least = t;
-        per = n;
-      }
+      take(n, scan_time(one * K, n * TT, simds, bwd) * (bwd ? 1.3 : 1.7) + (bwd ? 8.0 : 25.0));
     }
+    if (!bwd) break;
   }
   a.chunk = per * TT;
-  a.K = (int)(a.tiles > 0 ? (a.tiles + per - 1) / per : 1);
+  a.K = (int)((tiles + per - 1) / per);
 }
 
 void conv_plan(ConvArgs& a, int dt, int cus, bool bwd) {

@@ -73,7 +73,7 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   auto k = eql_scan_bwd_kernel<DT, NL, MODE>;
-  const int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves, lds = scan_bwd_bytes<NL>(waves);
+  const int waves = a.waves, lds = scan_bwd_bytes<NL>(waves);
   if (lds > 65536) {
     e = hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
