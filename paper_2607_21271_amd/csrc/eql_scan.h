@@ -656,6 +656,145 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   }
 }
 
+// A call over few tokens, without kept states: a wave takes its columns one token at a time, and a lane's four columns lie
+// 64 / NL apart, so that states come and go in whole cache lines.  Bound by them: 256 sequences of 2048 columns of 64 f32
+// states take one token in 56 us, 4.8 TB/s; the kernel of tiles, whose registers leave two waves a SIMD, in 95.  Few waves wait
+// for their loads one after the other: one token of 32 sequences of 768 columns of 16 states, 5.3 us, with tiles 6.7.  From
+// 6 tokens on (3 where a lane has all of a column's states) the tiles are faster there: 8 tokens 10.2 us, with tiles 8.8.
+constexpr int scan_few(int NL) { return NL == 1 ? 2 : 4; }  // tokens
+template <int DT, int NL>
+__global__ __launch_bounds__(64 * kScanWaves) void eql_scan_few_kernel(const ScanArgs a) {
+  using E = typename Elem<DT>::T;
+  constexpr int CH = scan_cols(NL), NP = 4 * NL, STEP = 64 / NL, EC = CH >= 64 ? CH / 64 : 1;
+  __shared__ __attribute__((aligned(16))) float lds[kScanWaves][2 * CH + 2 * NP];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const unsigned id = blockIdx.x * kScanWaves + wave;
+  if (id >= a.tasks) return;  // (no barrier follows)
+  const ScanPlace p = scan_place<NL>(a, id);
+  const int n0 = lane % NL * 4, c0 = lane / NL, cols = min(p.left, CH);
+  const bool quads = a.N % 4 == 0 && ((uintptr_t)a.h0 & 15) == 0 && ((uintptr_t)a.hT & 15) == 0 && ((uintptr_t)a.A & 15) == 0;
+  // four states of column c0 + q STEP, none where m <= 0
+  auto states = [&](const float* base, int64_t at, int m, float (&f)[4]) {
+    if (quads) {
+      const floatx4 v = *reinterpret_cast<const floatx4*>(base + (m > 0 ? at : 0));
+#pragma unroll
+      for (int n = 0; n < 4; ++n) f[n] = m > 0 ? v[n] : 0.0f;
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const float v = base[n < m ? at + n : 0];
+        f[n] = n < m ? v : 0.0f;
+      }
+    }
+  };
+  float h[4][4], A2[4][4];
+  const int64_t row = (p.b * a.CT + p.ct0) * a.N;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int c = c0 + q * STEP, m = c < cols ? a.N - n0 : 0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) h[q][n] = 0.0f;
+    if (a.h0) states(a.h0, row + c * a.N + n0, m, h[q]);
+    states(a.A, (int64_t)(m > 0 ? scan_channel(a, p.ct0 + c) : 0) * a.N + n0, m, A2[q]);
+  }
+  // the elements of a token: column lane + 64 i, and b and c of state `lane`
+  float xn[EC], dn[EC], zn[EC], bn = 0.0f, cn = 0.0f, bias[EC], skip[EC];
+  auto fetch = [&](int64_t l) {
+    auto at = [&](const void* t, const int64_t* st, int64_t i) { return (float)reinterpret_cast<const E*>(t)[p.b * st[0] + l * st[1] + i]; };
+#pragma unroll
+    for (int i = 0; i < EC; ++i) {
+      const int c = p.ct0 + (lane + 64 * i < cols ? lane + 64 * i : 0);
+      xn[i] = at(a.x, a.xs, c);
+      dn[i] = at(a.delta, a.ds, c);
+      zn[i] = a.z ? at(a.z, a.zs, c) : 0.0f;
+    }
+    const int n = lane < a.N ? lane : 0;
+    bn = at(a.b, a.bs, p.g * a.bs[2] + n);
+    cn = at(a.c, a.cs, p.g * a.cs[2] + n);
+    if (lane >= a.N) bn = cn = 0.0f;
+  };
+  if (p.len > 0) fetch(0);
+#pragma unroll
+  for (int i = 0; i < EC; ++i) {
+    const int ch = scan_channel(a, p.ct0 + (lane + 64 * i < cols ? lane + 64 * i : 0));
+    bias[i] = a.bias ? a.bias[ch] : 0.0f;
+    skip[i] = a.D ? a.D[ch] : 0.0f;
+  }
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+#pragma unroll
+    for (int n = 0; n < 4; ++n) A2[q][n] *= kLog2e;
+  float* const ds = lds[wave];
+  float* const us = ds + CH;
+  float* const bs = us + CH;
+  float* const cs = bs + NP;
+  E* const y = reinterpret_cast<E*>(a.y) + p.b * a.L * a.CT + p.ct0;
+  for (int64_t l = 0; l < a.L; ++l) {
+    float f[EC], x[EC], z[EC];
+    if (l < p.len) {
+#pragma unroll
+      for (int i = 0; i < EC; ++i) {
+        x[i] = xn[i];
+        z[i] = zn[i];
+        float d = dn[i] + bias[i];
+        if (a.softplus) d = softplus(d);
+        if (lane + 64 * i < CH) {
+          ds[lane + 64 * i] = d;
+          us[lane + 64 * i] = d * x[i];
+        }
+      }
+      if (lane < NP) {
+        bs[lane] = bn;
+        cs[lane] = cn;
+      }
+      if (l + 1 < p.len) fetch(l + 1);
+      wave_order();
+      const floatx4 bb = *reinterpret_cast<const floatx4*>(bs + n0), cc = *reinterpret_cast<const floatx4*>(cs + n0);
+      float out[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float d = ds[c0 + q * STEP], u = us[c0 + q * STEP];
+        float s = 0.0f;
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          h[q][n] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2[q][n]), h[q][n], u * bb[n]);
+          s = __builtin_fmaf(h[q][n], cc[n], s);
+        }
+        out[q] = lanes_sum<NL>(s);
+      }
+      wave_order();
+#pragma unroll
+      for (int q = 0; q < 4; ++q) us[c0 + q * STEP] = out[q];  // (lanes of a column hold the same sum)
+      wave_order();
+#pragma unroll
+      for (int i = 0; i < EC; ++i) {
+        f[i] = __builtin_fmaf(skip[i], x[i], lane + 64 * i < CH ? us[lane + 64 * i] : 0.0f);
+        if (a.z) f[i] *= z[i] * sigmoid(z[i]);
+      }
+      wave_order();
+    } else {
+#pragma unroll
+      for (int i = 0; i < EC; ++i) f[i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < EC; ++i)
+      if (lane + 64 * i < cols) y[l * a.CT + lane + 64 * i] = (E)f[i];
+  }
+  if (!a.hT) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int c = c0 + q * STEP, m = c < cols ? a.N - n0 : 0;
+    float* const s = a.hT + row + c * a.N + n0;
+    if (quads) {
+      if (m > 0) *reinterpret_cast<floatx4*>(s) = floatx4{h[q][0], h[q][1], h[q][2], h[q][3]};
+    } else {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+        if (n < m) s[n] = h[q][n];
+    }
+  }
+}
+
 // Carries the states over the chunks of a sequence, in place: what a chunk formed from zero becomes what it
 // starts from.  BACK: from the last chunk to the first, the gradient behind a chunk.  A thread takes one
 // column's state and reads kScanAhead chunks before it needs the first.

@@ -95,7 +95,16 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
 }
 
 template <int NL>
+hipError_t few(const ScanArgs& a, hipStream_t stream) {
+  return sequences(a, (int64_t)a.G * a.nblk, [&](ScanArgs s, int64_t n) {
+    const dim3 g = wave_blocks(s, n);
+    hipLaunchKernelGGL((eql_scan_few_kernel<DT, NL>), g, dim3(64 * kScanWaves), 0, stream, s);
+  });
+}
+
+template <int NL>
 hipError_t pass(const ScanArgs& a, bool back, hipStream_t stream) {
+  if (!back && a.L <= scan_few(NL) && !a.states) return few<NL>(a, stream);
   if (a.mode == kWhole) return back ? bwd<NL, kWhole>(a, stream) : fwd<NL, kWhole>(a, stream);
   if (a.mode == kLoose) return back ? bwd<NL, kLoose>(a, stream) : fwd<NL, kLoose>(a, stream);
   return back ? bwd<NL, kTiny>(a, stream) : fwd<NL, kTiny>(a, stream);

@@ -60,7 +60,9 @@ SIZES = [(1, 1, 1, 1, 1, 1), (2, 1, 8, 4, 16, 1), (3, 5, 6, 1, 4, 2), (2, 17, 12
          (1, 520, 8, 1, 2, 1), (1, 130, 80, 4, 12, 1), (2, 8, 200, 8, 16, 1),
          # a group's last vector not full, in its first block and in a later one; runs of four states not full
          (2, 37, 75, 3, 7, 3), (1, 70, 131, 5, 13, 1), (2, 40, 67, 1, 1, 1), (1, 50, 261, 1, 3, 1), (1, 90, 33, 1, 62, 1), (2, 25, 105, 3, 21, 3),
-         (3, 2, 205, 5, 11, 1)]
+         (3, 2, 205, 5, 11, 1),
+         # few tokens
+         (2, 4, 37, 3, 62, 1), (5, 3, 9, 8, 5, 3), (2, 2, 300, 1, 3, 1), (3, 4, 17, 8, 32, 1)]
 
 
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
@@ -81,7 +83,7 @@ def test_what_may_be_left_out(D, z, bias, state, softplus):
 
 
 @pytest.mark.parametrize("dt", ["f32", "f16"])
-@pytest.mark.parametrize("L", [1, 40, 400])
+@pytest.mark.parametrize("L", [1, 3, 40, 400])
 def test_lengths(dt, L):
     """Sequences of no token, one, all but one, all; what lies behind them is NaN and reaches nothing."""
     lengths = torch.tensor([0, 1, L - 1, L, -3, L + 7], dtype=torch.int32)
