@@ -110,7 +110,8 @@ int eqlinear_residual_norm(const eqlinear_residual_shape* shape, const void* x, 
                            const void* post_bias, void* r, void* h, void* stream);
 
 /* Gradients from dr and dh (each may be NULL: 0; dh only with weight).  dx, dbranch [B, L, C, T], dweight .. dpost_bias
- * [C], dgate [B, C]; a gradient may be NULL where it is not wanted.  r is formed again from x and branch. */
+ * [C], dgate [B, C]; a gradient may be NULL where it is not wanted, and is 0 where there are no tokens.  r is formed again
+ * from x and branch. */
 size_t eqlinear_residual_norm_backward_workspace_bytes(const eqlinear_residual_shape* shape);
 int eqlinear_residual_norm_backward(const eqlinear_residual_shape* shape, const void* x, const void* branch,
                                     const void* weight, const void* scale, const void* gate, const void* post_weight,

@@ -112,13 +112,15 @@ hipError_t res_forward<DT>(const ResArgs& a, hipStream_t stream) {
 }
 template <>
 hipError_t res_backward<DT>(const ResArgs& a, hipStream_t stream) {
-  const hipError_t e = res(a, true, stream);
-  if (e != hipSuccess || a.J == 0) return e;
-  const int gr = res_gr(a), blocks = colsum_blocks(a.C, a.T / gr);
-  const hipError_t f = launches(a, a.seqs, (int64_t)a.J * blocks, kColsumThreads, [&](const ResArgs& s, dim3 n) {
-    hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(kColsumThreads), 0, stream, s, gr, blocks);
-  });
-  if (f != hipSuccess) return f;
+  if (a.seqs > 0 && a.rows > 0) {  // (else the parameters' gradients are 0)
+    hipError_t e = res(a, true, stream);
+    if (e != hipSuccess || a.J == 0) return e;
+    const int gr = res_gr(a), blocks = colsum_blocks(a.C, a.T / gr);
+    e = launches(a, a.seqs, (int64_t)a.J * blocks, kColsumThreads, [&](const ResArgs& s, dim3 n) {
+      hipLaunchKernelGGL(eql_res_strips_kernel<>, n, dim3(kColsumThreads), 0, stream, s, gr, blocks);
+    });
+    if (e != hipSuccess) return e;
+  }
   hipLaunchKernelGGL(eql_res_params_kernel<DT>, dim3((unsigned)((a.C + kResParamChannels - 1) / kResParamChannels)),
                      dim3(kResParamThreads), 0, stream, a);
   return hipGetLastError();

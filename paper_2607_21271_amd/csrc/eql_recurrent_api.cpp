@@ -593,7 +593,7 @@ int eqlinear_residual_norm_backward(const eqlinear_residual_shape* s, const void
   eqk::ResArgs a;
   if (int st = res_args(s, a)) return st;
   const size_t e = elem_bytes(s->dtype), n = (size_t)a.B * a.L * a.C * a.T * e, p = (size_t)a.C * e;
-  if (!branch && (scale || gate || post_weight || dbranch)) return EQL_ERR_INVALID_ARG;
+  if (!branch && (scale || gate || post_weight || dbranch) && n > 0) return EQL_ERR_INVALID_ARG;
   if ((post_bias && !post_weight) || (dh && !weight) || ((dweight || dbias) && !weight) || (dscale && !scale) ||
       (dgate && !gate) || ((dpost_weight || dpost_bias) && !post_weight) || (n > 0 && !x))
     return EQL_ERR_INVALID_ARG;
@@ -627,9 +627,8 @@ int eqlinear_residual_norm_backward(const eqlinear_residual_shape* s, const void
   const Range in[9] = {{x, n}, {branch, n}, {weight, p}, {scale, p}, {gate, (size_t)a.B * p}, {post_weight, p}, {post_bias, p},
                        {dr, n}, {dh, n}};
   if (!apart(out, 9, in, 9)) return EQL_ERR_INVALID_ARG;
-  if (need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
+  if (n > 0 && need > 0 && (!workspace || workspace_bytes < need)) return EQL_ERR_WORKSPACE;
   if (int st = check_device()) return st;
-  if (n == 0) return EQL_OK;
   a.part = (float*)workspace;
   a.sums = (float*)((char*)workspace + align256((size_t)a.seqs * a.strips * a.J * a.K * sizeof(float)));
   a.mode = res_mode(a, s->dtype);

@@ -386,6 +386,10 @@ __global__ __launch_bounds__(kResParamThreads) void eql_res_params_kernel(const 
   if (c < a.C) {
     const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
     for (int64_t q = turn; q < a.seqs; q += NQ) {
+      if (a.rows == 0) {  // no tokens: nothing was summed
+        if (a.dgate) reinterpret_cast<E*>(a.dgate)[q * a.C + c] = (E)0.0f;
+        continue;
+      }
       const float* s = a.sums + q * a.J * a.C + c;
       if (a.w) {
         sum[0] += s[0];

@@ -186,14 +186,11 @@ class ResidualNormFunction(torch.autograd.Function):
             return (None,) * 10
         gr, gh = grads if len(grads) == 2 else (None, grads[0]) if branch is None else (grads[0], None)
         gr, gh = (None if g is None else g.contiguous() for g in (gr, gh))
-        empty = x.numel() == 0
-        new = torch.zeros_like if empty else torch.empty_like
-        out = [new(t) if t is not None and want else None for t, want in zip(given, ctx.needs_input_grad)]
-        if not empty:
-            ws = x.new_empty((need,), dtype=torch.uint8)
-            ops._launch("eqlinear_residual_norm_backward", x, ref,
-                        *[None if t is None else t.data_ptr()
-                          for t in (x, branch, weight, scale, gate, post_weight, post_bias, gr, gh, *out, ws)], need)
+        out = [torch.empty_like(t) if t is not None and want else None for t, want in zip(given, ctx.needs_input_grad)]
+        ws = x.new_empty((need,), dtype=torch.uint8)
+        ops._launch("eqlinear_residual_norm_backward", x, ref,
+                    *[None if t is None else t.data_ptr() for t in (x, branch, weight, scale, gate, post_weight, post_bias, gr, gh, *out, ws)],
+                    need)
         return (*out, None, None)
 
 

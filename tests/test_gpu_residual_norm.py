@@ -148,6 +148,8 @@ def test_dropped_branch():
 def test_empty():
     for B, L in ((0, 5), (2, 0)):
         t = make(11, B, L, 4, 2, "f32")
+        junk = [torch.full((n,), float("nan"), device="cuda") for n in (4, 4, 4, 4, 4, 4, 8, 8)]
+        del junk  # what is allocated next holds NaN
         got = run(t, *grads(1, t))
         assert got["r"].shape == (B, L, 4, 2) and all((got["d" + k] == 0).all() for k in NAMES[2:])
 
@@ -159,3 +161,33 @@ def test_same_bits_every_time():
     for _ in range(3):
         for k, v in run(t, *g).items():
             assert torch.equal(v, first[k]), k
+
+
+def test_branch_is_x():
+    from paper_2607_21271_amd.norm import residual_norm
+    t = make(14, 2, 9, 12, 4, "f32")
+    dr, dh = grads(5, t)
+    want = R.residual(**{**t, "branch": t["x"]}, dr=dr, dh=dh)
+    x = t["x"].detach().requires_grad_()
+    r, h = residual_norm(**{**t, "x": x, "branch": x})
+    torch.autograd.backward((r, h), (dr, dh))
+    R.within("r", r.detach(), *want["r"])
+    R.within("h", h.detach(), *want["h"])
+    # a sum of two rounded gradients: its own rounding, half a step of f32, beside their bounds
+    both = want["dx"][0] + want["dbranch"][0]
+    R.within("dx", x.grad, both, want["dx"][1] + want["dbranch"][1] + both.abs() * 2.0 ** -24 + 2.0 ** -126)
+
+
+def test_more_sequences_than_a_launch_takes():
+    """17 million sequences with gates of their own: workgroups are numbered from each launch's first sequence."""
+    B, C = 17_000_003, 8
+    t = make(15, 5, 1, C, 1, "f16", bias=False, post=False)
+    many = {k: v if v is None or v.shape[0] != 5 else v.repeat(B // 5 + 1, *[1] * (v.dim() - 1))[:B] for k, v in t.items()}
+    dr, dh = grads(6, t)
+    got, want = run(many), run(t)
+    for k in ("r", "h"):
+        assert torch.equal(got[k], want[k].repeat(B // 5 + 1, 1, 1, 1)[:B]), k
+    more = lambda v: v.repeat(B // 5 + 1, 1, 1, 1)[:B]
+    got, want = run(many, more(dr), more(dh)), run(t, dr, dh)
+    for k in ("dx", "dbranch", "dgate"):
+        assert torch.equal(got[k], want[k].repeat(B // 5 + 1, *[1] * (want[k].dim() - 1))[:B]), k

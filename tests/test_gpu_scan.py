@@ -238,3 +238,16 @@ def test_state_out_is_not_differentiable():
     assert h is out and not y.requires_grad
     with pytest.raises(ValueError):
         selective_scan(**{k: None if v is None else v.detach() for k, v in t.items()}, state_out=out[:, :2])
+
+
+@pytest.mark.parametrize("L", [1, 5])
+def test_more_waves_than_a_launch_takes(L):
+    """4100 sequences of 4096 column blocks: more waves than one launch has, all sequences alike."""
+    from paper_2607_21271_amd.scan import selective_scan
+    t = make(31, 1, L, 4096, 16, 64, 1, "f16", state=False)
+    with torch.no_grad():
+        want = selective_scan(**t)
+        many = {k: v.expand(4100, *v.shape[1:]) if v is not None and v.dim() == 4 else v for k, v in t.items()}
+        got = selective_scan(**many)
+    for part in got.split(100):
+        assert torch.equal(part, want.expand_as(part))
