@@ -44,6 +44,11 @@ LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang",
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 DEVICE_FLAGS = LINK_FLAGS + VGPR_FORM
 ACC_REG_UNITS = {"eql_big", "attn_f32"}
+# Arrays stay arrays until loops over them are unrolled, and then become registers of their own.  Made into vectors
+# before that, f16 elements were lost: in a scan's gradients an element's register was written by another
+# tensor's before it had been read.
+SCALARS = ["-mllvm", "-disable-promote-alloca-to-vector"]
+SCALAR_UNITS = ("scan_", "recurrent_")
 COMMON_FLAGS = ["-O3", "-std=c++20", "-fPIC", "-Wall", "-Wno-unused-function",
                 "-I" + os.path.join(os.path.dirname(HERE), "include")]
 
@@ -55,6 +60,7 @@ def _compile(unit) -> str:
     obj = os.path.join(wd, stem + ".o")
     lang = ["-x", "hip"] if src.endswith(".cpp") else []
     dev = LINK_FLAGS if stem in ACC_REG_UNITS else DEVICE_FLAGS
+    dev = dev + SCALARS if stem.startswith(SCALAR_UNITS) else dev
     cmd = [HIPCC, *dev, *COMMON_FLAGS, *defs, "-save-temps", *lang, "-c",
            os.path.join(CSRC, src), "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True, cwd=wd)

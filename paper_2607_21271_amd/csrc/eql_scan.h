@@ -944,7 +944,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 // first: the states of a run are formed again from the one before it, which the forward kept, and held in registers.
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave
-  return 3 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
+  return 7 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
 }
 template <int NL>
 constexpr int scan_red_lds() {  // floats of a wave's db and dc, twice
@@ -970,7 +970,11 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   float* const ds = smem + wave * scan_bwd_lds<NL>();
   float* const us = ds + TT * CH;
   float* const ss = us + TT * CH;
-  float* const bs = ss + TT * CH;
+  float* const as = ss + TT * CH;  // sum_n A a g h, sum_n c h, the step's slope, sigmoid(z)
+  float* const hc = as + TT * CH;
+  float* const ls = hc + TT * CH;
+  float* const gs = ls + TT * CH;
+  float* const bs = gs + TT * CH;
   float* const cs = bs + TT * NP;
   float* const red = smem + waves * scan_bwd_lds<NL>();  // [2][waves][TT][2][NP]
   const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
@@ -1048,16 +1052,25 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
       TL::floats(dr, p.left, df);
       TL::floats(yr, p.left, sf);
       if (a.z) {
-        float zf[EPT];
+        float zf[EPT], sg[EPT];
         TL::floats(zr, p.left, zf);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) sf[e] *= zf[e] * sigmoid(zf[e]);
+        for (int e = 0; e < EPT; ++e) {
+          sg[e] = sigmoid(zf[e]);
+          sf[e] *= zf[e] * sg[e];
+        }
+        wave_order();
+        TL::put(gs, sg);
       }
 #pragma unroll
       for (int e = 0; e < EPT; ++e) df[e] += bias[e % VEC];
-      if (a.softplus)
+      if (a.softplus) {
+        float slope[EPT];
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) df[e] = softplus(df[e]);
+        for (int e = 0; e < EPT; ++e) df[e] = softplus(df[e], slope[e]);
+        wave_order();
+        TL::put(ls, slope);
+      }
       if (nt < TT) {
         TL::behind(df, nt);
         TL::behind(xf, nt);
@@ -1127,15 +1140,15 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
         floatx4 v;
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(gb[q]);
-        // d, d x and s of this token have been read by every lane of these columns; lanes that hold the same sums write
-        // them alike, without a branch
+        // d x of this token has been read by every lane of these columns; lanes that hold the same sums write them alike,
+        // without a branch
         *reinterpret_cast<floatx4*>(us + t * CH + c0) = v;
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ga[q]);
-        *reinterpret_cast<floatx4*>(ds + t * CH + c0) = v;
+        *reinterpret_cast<floatx4*>(as + t * CH + c0) = v;
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ch[q]);
-        *reinterpret_cast<floatx4*>(ss + t * CH + c0) = v;
+        *reinterpret_cast<floatx4*>(hc + t * CH + c0) = v;
         mine[(t * 2) * NP + n0 + lane / 16] = columns_sum<NL>(db[0], db[1], db[2], db[3]);  // state n0 + row
         mine[(t * 2 + 1) * NP + n0 + lane / 16] = columns_sum<NL>(dc[0], dc[1], dc[2], dc[3]);
       };
@@ -1185,40 +1198,40 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     }
     wave_order();
     {
-      float xf[EPT], f[EPT], o[EPT];
+      float xf[EPT], f[EPT], o[EPT], sf[EPT];
       TL::again(xr);
-      TL::again(dr);
-      TL::again(yr);
       TL::floats(xr, p.left, xf);
       const int rows = (int)min(p.end - l0, (int64_t)TT);
-      float sf[EPT];
-      TL::floats(yr, p.left, sf);
-      if (a.z) {
-        float zf[EPT], ch[EPT];
+      if (a.z && a.dz) {
+        float zf[EPT], ch[EPT], sg[EPT];
+        TL::again(yr);
         TL::again(zr);
+        TL::floats(yr, p.left, sf);
         TL::floats(zr, p.left, zf);
-        TL::get(ss, ch);
+        TL::get(hc, ch);
+        TL::get(gs, sg);
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-          const float sg = sigmoid(zf[e]), y0 = __builtin_fmaf(skip[e % VEC], xf[e], ch[e]);
-          ch[e] = sf[e] * y0 * sg * __builtin_fmaf(zf[e], 1.0f - sg, 1.0f);
-          sf[e] *= zf[e] * sg;
+          const float y0 = __builtin_fmaf(skip[e % VEC], xf[e], ch[e]);
+          ch[e] = sf[e] * y0 * sg[e] * __builtin_fmaf(zf[e], 1.0f - sg[e], 1.0f);
         }
         if (nt < TT) TL::behind(ch, nt);
-        if (a.dz) TL::store(ch, dense(a.dz), l0, rows, p.left);
+        TL::store(ch, dense(a.dz), l0, rows, p.left);
       }
-      TL::floats(dr, p.left, o);
       TL::get(us, f);  // sum_n g b
       float sa[EPT];
-      TL::get(ds, sa);  // sum_n A a g h, times log2(e)
+      TL::get(as, sa);  // sum_n A a g h, times log2(e)
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        const float v = o[e] + bias[e % VEC];
-        float slope = 1.0f;
-        const float d = a.softplus ? softplus(v, slope) : v;
-        o[e] = __builtin_fmaf(kLn2, sa[e], xf[e] * f[e]) * slope;
-        f[e] = __builtin_fmaf(skip[e % VEC], sf[e], d * f[e]);
+      for (int e = 0; e < EPT; ++e) o[e] = __builtin_fmaf(kLn2, sa[e], xf[e] * f[e]);
+      if (a.softplus) {
+        TL::get(ls, sa);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) o[e] *= sa[e];
       }
+      TL::get(ds, sa);
+      TL::get(ss, sf);
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) f[e] = __builtin_fmaf(skip[e % VEC], sf[e], sa[e] * f[e]);
       if (nt < TT) {
         TL::behind(o, nt);
         TL::behind(f, nt);
