@@ -39,7 +39,9 @@ ARCH = "gfx950"
 # bytes a lane) and the attention's key gradient at heads above 96 (64 in bf16,
 # 352 in fp16; 164 in full precision, one wave).  The large-tile unit (one wave per SIMD, T * 64
 # accumulators per lane) and full-precision attention keep them in the
-# accumulation registers instead.
+# accumulation registers instead.  Of the recurrent kernels, scratch is used by some scans whose
+# columns or states are no whole vectors (32 to 48 bytes a lane) and by the residual norm's gradients over rows of
+# more than 4096 elements (16 to 60 bytes; 208 in fp32 where the rows are no whole vectors).
 LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 DEVICE_FLAGS = LINK_FLAGS + VGPR_FORM

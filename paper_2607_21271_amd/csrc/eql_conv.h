@@ -5,7 +5,9 @@
 // of its neighbours, W - 1 tokens, is read again, from the caches.  Runs of GR columns that share a channel share their
 // weights and their sums for dweight and dbias.
 // Bound: memory, and the loads that a thread has in flight: the forward reads its whole strip before it starts, the
-// backward four tokens while it works on the four before.
+// backward four tokens while it works on the four before (with eight at a time 36 us below, not 25: fewer waves fit).
+// Measured, four taps, silu: 16,389 tokens of 768 f16 columns 16 us (3.1 TB/s), 8 x 4,096 of 1,024 28 us (4.7 TB/s);
+// 25,092 tokens of 512 bf16 columns 15 us forward, 25 back (3.1 TB/s) and 5 for the parameters.
 #pragma once
 #include "eql_colsum.h"
 #include "eql_common.h"

@@ -205,7 +205,8 @@ void conv_plan(ConvArgs& a, int dt, int cus, bool bwd) {
   a.turns = 256 / a.width;
   a.rows = 16;
   if (bwd) {
-    // strips of 8 m tokens with their halo: longer ones where the device is full of waves anyway
+    // strips of 8 m tokens with their halo: longer ones, which read less of it twice, where the device has two waves a
+    // SIMD anyway
     int64_t m = a.B * nv * a.L / (8 * 64 * 8 * (int64_t)cus);
     m = m < 2 ? 2 : m > 8 ? 8 : m;
     a.rows = (int)(8 * m) - (a.W - 1);

@@ -11,7 +11,9 @@
 // registers.  The backward forms r again from x and u: what it reads is the inputs and the two gradients, and
 // no rounding of r enters.  Column sums stay in registers over a strip, then one row of sums a workgroup goes to
 // memory, and two small kernels add them in a fixed order.
-// Bound: memory (forward 4, backward 6 rows an element).
+// Bound: memory (forward 4, backward 6 rows an element), in the backward with the waves that its sums leave.
+// Measured: 12,608 rows of 768 f16 17 us forward (4.6 TB/s), 26 back (4.5 TB/s) and 9 for the parameters; 25,092
+// rows of 1,024 bf16 with a norm before and after 40 and 66 us (5.1 and 4.7 TB/s).
 #pragma once
 #include "eql_colsum.h"
 #include "eql_common.h"
