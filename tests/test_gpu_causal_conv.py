@@ -46,7 +46,7 @@ def grads(seed, t):
 @pytest.mark.parametrize("W", range(1, 9))
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 def test_widths(W, dt):
-    for B, L, C, T in ((2, 1, 8, 4), (1, 3, 5, 3), (2, 70, 24, 8), (3, 130, 7, 1), (2, 40, 3, 1), (1, 33, 2053, 1)):
+    for B, L, C, T in ((2, 1, 8, 4), (1, 3, 5, 3), (2, 70, 24, 8), (3, 130, 7, 1), (2, 40, 3, 1), (1, 33, 2053, 1), (2, 40, 16, 3)):
         t = make(W + L, B, L, C, T, W, dt)
         for act in ("none", "silu"):
             check(t, activation=act)
@@ -143,3 +143,24 @@ def test_large_values():
     t = make(13, 1, 40, 8, 2, 2, "f32")
     t["x"] = t["x"] * 60
     check(t, *grads(5, t), activation="silu")
+
+
+@pytest.mark.parametrize("C,T", [(64, 8), (513, 1)])
+def test_long_strips(C, T):
+    """Enough tokens for strips of more than 16 in the gradients: dx has the bits that it has sequence by sequence; dw is the
+    64-bit sum.  A sum of n products in fp32, one after the other, is off by n / 2^24 of its magnitude at most; here a thread
+    adds 64 tokens of 4 columns, and a few hundred partial sums follow."""
+    B, L, W = 13, 4096, 4
+    t = make(21, B, L, C, T, W, "f32", state=False)
+    dy = grads(6, t)[0]
+    got = run(t, dy)
+    for b in (0, 7, 12):
+        one = run(dict(t, x=t["x"][b:b + 1]), dy[b:b + 1])
+        assert torch.equal(got["dx"][b:b + 1], one["dx"]) and torch.equal(got["y"][b:b + 1], one["y"])
+    x, g = t["x"].double(), dy.double()
+    for w in range(W):
+        n = L - (W - 1 - w)
+        terms = g[:, L - n:] * x[:, :n]
+        want, bound = terms.sum((0, 1, 3)), 1000 * 2.0 ** -24 * terms.abs().sum((0, 1, 3))
+        assert ((got["dw"][:, w].double() - want).abs() <= bound).all()
+    assert ((got["db"].double() - g.sum((0, 1, 3))).abs() <= 1000 * 2.0 ** -24 * g.abs().sum((0, 1, 3))).all()

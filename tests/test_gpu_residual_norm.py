@@ -55,7 +55,8 @@ def grads(seed, t):
 
 # rows of one element up to the largest, on and off whole vectors, of every number of threads a row
 ROWS = [(2, 3, 1, 1), (3, 5, 5, 3), (2, 9, 16, 8), (1, 7, 130, 1), (2, 40, 96, 8), (1, 5, 115, 3), (2, 6, 129, 8), (1, 4, 1025, 2), (2, 3, 4096, 1),
-        (1, 3, 1024, 8), (1, 2, 8191, 1), (2, 1, 520, 8), (3, 70, 9, 1), (2, 40, 11, 5), (2, 70, 67, 3), (1, 2, 8192, 1), (2, 3, 1365, 3), (1, 700, 2, 3)]
+        (1, 3, 1024, 8), (1, 2, 8191, 1), (2, 1, 520, 8), (3, 70, 9, 1), (2, 40, 11, 5), (2, 70, 67, 3), (1, 2, 8192, 1), (2, 3, 1365, 3), (1, 700, 2, 3),
+        (2, 33, 16, 1), (1, 9, 40, 2), (2, 9, 50, 4), (3, 5, 100, 5), (1, 8, 400, 2), (1, 3, 300, 4), (2, 3, 620, 4), (2, 5, 1030, 4)]
 
 
 @pytest.mark.parametrize("size", ROWS, ids=lambda s: "x".join(map(str, s)))

@@ -73,6 +73,28 @@ def test_scan(size, dt):
     check(t, *grads(5, t, size[1]))
 
 
+# gradients in workgroups of one, two, three and four waves, several side by side for a group's columns, chunks of several tiles
+@pytest.mark.parametrize("size", [(64, 33, 520, 1, 5, 1), (33, 50, 520, 1, 5, 1), (40, 33, 520, 1, 2, 1), (17, 100, 520, 1, 5, 1),
+                                  (130, 9, 65, 1, 33, 1)], ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dt", ["f32", "f16"])
+def test_workgroups(size, dt):
+    t = make(sum(size), *size, dt)
+    lengths = torch.randint(0, size[1] + 1, (size[0],), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    check(t, *grads(5, t, size[1]), lengths=lengths.cuda())
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("C", [8, 9, 3], ids=["whole", "loose", "tiny"])
+@pytest.mark.parametrize("N", [4, 8, 16, 32, 64])
+def test_ways_to_read(N, C, dt):
+    """Whole vectors, rows that are none, rows shorter than one, for every number of lanes that share columns, two or three tiles
+    of one wave."""
+    L = 10 if N == 4 else 20
+    t = make(N + C, 1030, L, C, 1, N if C == 8 else N - 1, 1, dt)
+    check(t)
+    check(t, *grads(7, t, L))
+
+
 @pytest.mark.parametrize("D,z,bias,state,softplus", [c for c in itertools.product([0, 1], repeat=5) if sum(c) in (0, 1, 4)])
 def test_what_may_be_left_out(D, z, bias, state, softplus):
     t = make(7, 2, 21, 8, 4, 16, 1, "bf16", D, z, bias, state, bool(softplus))
