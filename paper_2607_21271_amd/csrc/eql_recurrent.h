@@ -18,16 +18,18 @@ constexpr int kWhole = 0, kLoose = 1, kTiny = 2;
 
 // ---- selective scan ----
 // A wave takes `scan_cols(NL)` neighbouring columns (channel, group element) of one group:
-// NL lanes share four columns and hold four states of each.
+// NL lanes share four columns (the gradients: two, where Q says so) and hold four states of each.
 constexpr int kScanMaxN = 64;
 constexpr int scan_lanes(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
-constexpr int scan_cols(int NL) { return 256 / NL; }
+constexpr int scan_cols(int NL, int Q = 4) { return 64 * Q / NL; }
+// columns of a lane in the gradients (eql_scan_bwd_kernel)
+constexpr int scan_bwd_columns(int NL) { return NL == 16 ? 4 : 2; }
 // tokens of a tile, and of a run, whose first state training keeps
 constexpr int scan_tile(int NL) { return NL == 1 ? 4 : NL == 2 ? 8 : 16; }
 constexpr int scan_run(int NL) { return NL == 1 ? 4 : 8; }
-constexpr int scan_ept(int NL) { return scan_tile(NL) * scan_cols(NL) / 64; }  // elements of a lane
-constexpr int scan_vec(int dt, int NL) {
-  return (dt == kF32 ? 4 : 8) < scan_ept(NL) ? (dt == kF32 ? 4 : 8) : scan_ept(NL);
+constexpr int scan_ept(int NL, int Q = 4) { return scan_tile(NL) * scan_cols(NL, Q) / 64; }  // elements of a lane
+constexpr int scan_vec(int dt, int NL, int Q = 4) {
+  return (dt == kF32 ? 4 : 8) < scan_ept(NL, Q) ? (dt == kF32 ? 4 : 8) : scan_ept(NL, Q);
 }
 constexpr int kScanWaves = 4;  // of a workgroup
 
@@ -49,6 +51,7 @@ struct ScanArgs {
   unsigned mT;           // channel_factor(T)
   int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, softplus;
+  int bblk;      // blocks of a group's columns in the gradients
   int waves, P;  // of a workgroup of the gradients, and those side by side for a group's columns
   int mode;  // how rows are read and written (ScanTile)
 };

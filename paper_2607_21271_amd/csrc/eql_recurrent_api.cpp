@@ -143,35 +143,39 @@ int scan_mode(const eqk::ScanArgs& a, int dtype) {
 
 namespace eqk {
 
-// Time of `waves` waves that walk `tokens` tokens each, in tokens of a wave alone on its SIMD: the forward's kernels fit two
-// on one, which hide each other's waiting (a token of one wave 0.37 us, of two 0.55 us together), the gradients' one (1.1 us).
-static double scan_time(int64_t waves, int64_t tokens, int64_t simds, bool bwd) {
+// Microseconds of `waves` waves that walk `tokens` tokens each, at `one` a token for a wave alone on its SIMD (and eight
+// tokens' time before the first).  half: two on a SIMD hide half of each other's time, else none.
+static double scan_time(int64_t waves, int64_t tokens, int64_t simds, double one, bool half) {
   const int64_t w = (waves + simds - 1) / simds;
-  return (double)(tokens + 8) * (bwd ? (double)w : 0.75 * w + (w % 2 ? 0.25 : 0.0));
+  return one * (double)(tokens + 8) * (half ? 0.75 * w + (w % 2 ? 0.25 : 0.0) : (double)w);
 }
 
 // Chunks of tokens where the columns alone do not fill the device: the number of waves (one to four a SIMD) for which the
-// pass over the states or gradients, half to three quarters of the main one, and the main one take least.
+// pass over the states or gradients and the main one take least, by what a token of theirs takes: 0.26 and 0.37 us
+// forward, back 0.25 and 0.51 (1.1 with four columns a lane).
 // Gradients: workgroups of four, two or one wave, which fill a CU's four SIMDs alike (three where there are no more); smaller
 // ones leave fewer waves without columns, and more sums of db and dc to memory.
 void scan_plan(ScanArgs& a, int cus, bool bwd) {
-  const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL);
+  const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL), back = scan_cols(NL, scan_bwd_columns(NL));
   a.CT = a.C * a.T;
   a.CTg = a.CT / a.G;
   a.nblk = (a.CTg + CH - 1) / CH;
+  a.bblk = (a.CTg + back - 1) / back;
   a.cols = a.G * a.nblk * CH;
   a.tiles = (a.L + TT - 1) / TT;
   a.runs = (a.L + scan_run(NL) - 1) / scan_run(NL);
   a.mT = channel_factor(a.T);
-  const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1;
+  const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1, first = a.B * a.G * a.nblk;
+  const int nblk = bwd ? a.bblk : a.nblk;
+  const double token = !bwd ? 0.37 : back == CH ? 1.1 : 0.51;
   int64_t per = tiles;
   double least = -1.0;
-  for (int waves = a.nblk < kScanWaves ? a.nblk : kScanWaves; waves > 0; --waves) {
-    if (waves == 3 && a.nblk > 3) continue;
-    const int P = (a.nblk + waves - 1) / waves;
-    const int64_t one = a.B * a.G * (bwd ? (int64_t)P * waves : a.nblk);
-    // the sums' way out and back in, in tokens of 1.1 us at 5 TB/s
-    const double sums = bwd && P > 1 ? (double)a.B * a.L * a.G * P * 16 * 4 * NL / 5.5e6 + 4.0 : 0.0;
+  for (int waves = nblk < kScanWaves ? nblk : kScanWaves; waves > 0; --waves) {
+    if (waves == 3 && nblk > 3) continue;
+    const int P = (nblk + waves - 1) / waves;
+    const int64_t one = a.B * a.G * (bwd ? (int64_t)P * waves : nblk);
+    // the sums' way out and back in, at 5 TB/s, and a launch
+    const double sums = bwd && P > 1 ? (double)a.B * a.L * a.G * P * 16 * 4 * NL / 5e6 + 4.0 : 0.0;
     auto take = [&](int64_t n, double t) {
       if (least >= 0.0 && t + sums >= least) return;
       least = t + sums;
@@ -179,15 +183,15 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
       a.P = P;
       a.waves = waves;
     };
-    take(tiles, scan_time(one, tiles * TT, simds, bwd));
-    for (int w = 1; w <= 4 && one > 0 && one < simds; ++w) {
+    take(tiles, scan_time(one, tiles * TT, simds, token, !bwd));
+    for (int w = 1; w <= 4 && one > 0 && one < 2 * simds; ++w) {
       int64_t K = w * simds / one;
       if (K > tiles) K = tiles;
       if (K < 2) continue;
       const int64_t n = (tiles + K - 1) / K;
       K = (tiles + n - 1) / n;
       // (two more launches, and the states between the passes: about ten microseconds)
-      take(n, scan_time(one * K, n * TT, simds, bwd) * (bwd ? 1.3 : 1.7) + (bwd ? 8.0 : 25.0));
+      take(n, scan_time(one * K, n * TT, simds, token, !bwd) + scan_time(first * K, n * TT, simds, bwd ? 0.25 : 0.26, true) + 10.0);
     }
     if (!bwd) break;
   }

@@ -39,6 +39,10 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// Q floats: one of each of a lane's columns
+template <int Q>
+using Cols = float __attribute__((ext_vector_type(Q)));
+
 // Sum over the NL neighbouring lanes that share columns.
 template <int NL>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -98,18 +102,20 @@ struct ScanPlace {
   int64_t len;     // tokens that hold data
   int64_t begin, end;
 };
-template <int NL>
+template <int NL, int Q = 4>
 __device__ __forceinline__ ScanPlace scan_place(const ScanArgs& a, unsigned id) {
+  constexpr int CH = scan_cols(NL, Q);
   ScanPlace p;
-  p.blk = (int)(id % (unsigned)a.nblk);
-  id /= (unsigned)a.nblk;
+  const unsigned nblk = Q == 4 ? a.nblk : a.bblk;
+  p.blk = (int)(id % nblk);
+  id /= nblk;
   p.g = (int)(id % (unsigned)a.G);
   id /= (unsigned)a.G;
   p.k = (int)(id % (unsigned)a.K);
   p.b = a.first + id / (unsigned)a.K;
-  p.col0 = (p.g * a.nblk + p.blk) * scan_cols(NL);
-  p.ct0 = p.g * a.CTg + p.blk * scan_cols(NL);
-  p.left = a.CTg - p.blk * scan_cols(NL);
+  p.col0 = p.g * a.nblk * scan_cols(NL) + p.blk * CH;
+  p.ct0 = p.g * a.CTg + p.blk * CH;
+  p.left = a.CTg - p.blk * CH;
   p.len = a.lengths ? min(max((int64_t)a.lengths[p.b], (int64_t)0), a.L) : a.L;
   p.begin = p.k * a.chunk;
   p.end = min(p.begin + a.chunk, a.L);
@@ -124,9 +130,9 @@ constexpr uint32_t kScanDrop = 0x80000000u;  // an offset past every resource: l
 // alignment.  kLoose: a group's last vector, where it is not full, is read so that it ends where the group does, and moved
 // to its place as it is used (which would cost kWhole 5 %); so are the last run of a token's b and c.  kTiny (groups
 // shorter than a vector, tokens further apart than 31 bits reach): single elements.
-template <int DT, int NL, int MODE>
+template <int DT, int NL, int MODE, int Q = 4>
 struct ScanTile {
-  static constexpr int CH = scan_cols(NL), TT = scan_tile(NL), EPT = scan_ept(NL), VEC = scan_vec(DT, NL);
+  static constexpr int CH = scan_cols(NL, Q), TT = scan_tile(NL), EPT = scan_ept(NL, Q), VEC = scan_vec(DT, NL, Q);
   static constexpr int NV = EPT / VEC, VT = CH / VEC, EB = DT == kF32 ? 4 : 2;
   static constexpr int W = VEC * EB / 4;  // 32-bit words of a vector
   static constexpr int NP = 4 * NL;
@@ -374,11 +380,11 @@ struct ScanTile {
 
 // A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.  kWhole: four states are all
 // inside or all outside, and rows of A whole 16-byte words (what lies outside is read from A's start instead).
-template <int NL, int MODE>
-__device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[4][4]) {
-  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
+template <int NL, int MODE, int Q>
+__device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[Q][4]) {
+  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * Q;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < Q; ++q) {
     const int m = c0 + q < p.left ? a.N - n0 : 0;
     const float* s = a.A + (m > 0 ? scan_channel(a, p.ct0 + c0 + q) * a.N + n0 : 0);
     if constexpr (MODE == kWhole) {
@@ -395,12 +401,12 @@ __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p
   }
 }
 // The lane's states in [cols][NP] or, for the caller, [CT][N].
-template <int NL>
-__device__ __forceinline__ void load_padded(const float* base, float (&h)[4][4]) {
+template <int NL, int Q>
+__device__ __forceinline__ void load_padded(const float* base, float (&h)[Q][4]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const floatx4 v = *reinterpret_cast<const floatx4*>(base + (lane / NL * 4 + q) * (4 * NL) + lane % NL * 4);
+  for (int q = 0; q < Q; ++q) {
+    const floatx4 v = *reinterpret_cast<const floatx4*>(base + (lane / NL * Q + q) * (4 * NL) + lane % NL * 4);
 #pragma unroll
     for (int n = 0; n < 4; ++n) h[q][n] = v[n];
   }
@@ -413,12 +419,12 @@ __device__ __forceinline__ void store_padded(float* base, const float (&h)[4][4]
     *reinterpret_cast<floatx4*>(base + (lane / NL * 4 + q) * (4 * NL) + lane % NL * 4) =
         floatx4{h[q][0], h[q][1], h[q][2], h[q][3]};
 }
-template <int NL>
-__device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* base, float (&h)[4][4]) {
-  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
+template <int NL, int Q>
+__device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p, const float* base, float (&h)[Q][4]) {
+  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * Q;
   const bool whole = a.N % 4 == 0 && ((uintptr_t)base & 15) == 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < Q; ++q) {
     const float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
     if (whole) {
       const bool on = c0 + q < p.left && n0 < a.N;
@@ -435,12 +441,12 @@ __device__ __forceinline__ void load_state(const ScanArgs& a, const ScanPlace& p
     }
   }
 }
-template <int NL>
-__device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& p, float* base, const float (&h)[4][4]) {
-  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * 4;
+template <int NL, int Q>
+__device__ __forceinline__ void store_state(const ScanArgs& a, const ScanPlace& p, float* base, const float (&h)[Q][4]) {
+  const int lane = threadIdx.x & 63, n0 = lane % NL * 4, c0 = lane / NL * Q;
   const bool whole = a.N % 4 == 0 && ((uintptr_t)base & 15) == 0;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
+  for (int q = 0; q < Q; ++q) {
     if (c0 + q >= p.left || n0 >= a.N) continue;
     float* s = base + (p.b * a.CT + p.ct0 + c0 + q) * a.N + n0;
     if (whole) {
@@ -472,15 +478,17 @@ __device__ __forceinline__ void scan_param(const ScanArgs& a, const ScanPlace& p
 }
 
 // The decays of a token: exp(d A).
-__device__ __forceinline__ void scan_exp(float (&e)[4][4], const float (&A2)[4][4], const floatx4& d) {
+template <int Q>
+__device__ __forceinline__ void scan_exp(float (&e)[Q][4], const float (&A2)[Q][4], const Cols<Q>& d) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int n = 0; n < 4; ++n) e[q][n] = __builtin_amdgcn_exp2f(d[q] * A2[q][n]);
 }
-__device__ __forceinline__ void scan_step(float (&h)[4][4], const float (&e)[4][4], const floatx4& dx, const floatx4& bb) {
+template <int Q>
+__device__ __forceinline__ void scan_step(float (&h)[Q][4], const float (&e)[Q][4], const Cols<Q>& dx, const floatx4& bb) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int n = 0; n < 4; ++n) h[q][n] = __builtin_fmaf(e[q][n], h[q][n], dx[q] * bb[n]);
 }
@@ -951,11 +959,13 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 // and dc are summed over them before they leave; a tile is walked from its last run of SUB tokens to the
 // first: the states of a run are formed again from the one before it, which the forward kept, and held in registers.
 // What a tile's elements need twice (step, slope, gate, dy silu(z)) waits in LDS beside the scan's sums.
-// One wave a SIMD: a run's states take 128 registers (two waves, with spills: 476 us against 217).
-// Measured, f16, 16 states: 64 x 197 tokens of 768 columns 205 us, 1.3 ps a state of a token, the vector pipe 75 % busy.
+// Two columns a lane (four above 32 states): a run's states take 64 registers, and two waves fit a SIMD, 205 us below with four
+// columns and one wave.  Bound by the vector pipe: a wave alone needs 0.51 us a token, two 0.97 together.  What is spilled
+// (20 to 40 registers) is used once a tile.
+// Measured, f16, 16 states: 64 x 197 tokens of 768 columns 174 us, 1.1 ps a state of a token.
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave
-  return 7 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
+  return 7 * scan_tile(NL) * scan_cols(NL, scan_bwd_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
 }
 template <int NL>
 constexpr int scan_red_lds() {  // floats of a wave's db and dc, twice
@@ -966,8 +976,10 @@ constexpr int scan_bwd_bytes(int waves) {
   return waves * (scan_bwd_lds<NL>() + scan_red_lds<NL>()) * 4;
 }
 template <int DT, int NL, int MODE>
-__global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
-  using TL = ScanTile<DT, NL, MODE>;
+__global__ __launch_bounds__(64 * kScanWaves, scan_bwd_columns(NL) == 4 ? 1 : 2) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
+  constexpr int Q = scan_bwd_columns(NL);
+  using TL = ScanTile<DT, NL, MODE, Q>;
+  using Col = Cols<Q>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   constexpr int SUB = scan_run(NL);
   using E = typename TL::E;
@@ -975,8 +987,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // workgroup: (sequence, chunk, group, run of `waves` blocks)
   const int run = (int)(blockIdx.x % (unsigned)a.P);
-  const bool on = run * waves + wave < a.nblk;
-  ScanPlace p = scan_place<NL>(a, blockIdx.x / (unsigned)a.P * (unsigned)a.nblk + (unsigned)min(run * waves + wave, a.nblk - 1));
+  const int blocks = Q == 4 ? a.nblk : a.bblk;
+  const bool on = run * waves + wave < blocks;
+  ScanPlace p = scan_place<NL, Q>(a, blockIdx.x / (unsigned)a.P * (unsigned)blocks + (unsigned)min(run * waves + wave, blocks - 1));
   if (!on) p.left = 0;
   float* const ds = smem + wave * scan_bwd_lds<NL>();
   float* const us = ds + TT * CH;
@@ -988,7 +1001,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   float* const bs = gs + TT * CH;
   float* const cs = bs + TT * NP;
   float* const red = smem + waves * scan_bwd_lds<NL>();  // [2][waves][TT][2][NP]
-  const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int n0 = lane % NL * 4, c0 = lane / NL * Q, at = TL::at();
   const int64_t stop = min(p.len, p.end);
   const auto xv = TL::view(a.x, p.b * a.xs[0] + p.ct0, a.xs[1], p.left), dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left);
   const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left);
@@ -996,14 +1009,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   auto dense = [&](const void* q) {
     return TL::rebased(gv, q, p.b * a.L * a.CT + p.ct0, p.left);
   };
-  float A2[4][4], g[4][4], dA[4][4], bias[VEC], skip[VEC], dskip[VEC], dbias[VEC];
+  float A2[Q][4], g[Q][4], dA[Q][4], bias[VEC], skip[VEC], dskip[VEC], dbias[VEC];
   scan_decay<NL, MODE>(a, p, A2);
   scan_param<VEC, MODE>(a, p, a.bias, at, bias);
   scan_param<VEC, MODE>(a, p, a.D, at, skip);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) dskip[i] = dbias[i] = 0.0f;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int n = 0; n < 4; ++n) g[q][n] = dA[q][n] = 0.0f;
   const int64_t slot = (p.b * a.K + p.k) * a.cols + p.col0;
@@ -1017,14 +1030,16 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       if (n0 + n >= a.N) continue;
-      floatx4* const q = reinterpret_cast<floatx4*>(part + (int64_t)(n0 + n) * a.cols + c0);
-      floatx4 v = floatx4{dA[0][n], dA[1][n], dA[2][n], dA[3][n]};
+      Col* const q = reinterpret_cast<Col*>(part + (int64_t)(n0 + n) * a.cols + c0);
+      Col v;
+#pragma unroll
+      for (int i = 0; i < Q; ++i) v[i] = dA[i][n];
       if (flushed) v += *q;
       *q = v;
     }
     flushed = true;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int n = 0; n < 4; ++n) dA[q][n] = 0.0f;
   };
@@ -1045,7 +1060,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
   };
   const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
   // the state before the run of tokens from l on, the next one on the way back
-  float hs[4][4] = {};
+  float hs[Q][4] = {};
   auto start = [&](int64_t l) {
     if (on) load_padded<NL>(a.states + ((p.b * a.runs + l / SUB) * a.cols + p.col0) * NP, hs);
   };
@@ -1101,31 +1116,33 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
     if (tile > 0) fetch_bc(l0 - TT);
     wave_order();
     float* const mine = red + ((odd * waves + wave) * TT * 2) * NP;
-    auto token = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * CH + c0); };
+    auto token = [&](const float* tile_, int t) { return *reinterpret_cast<const Col*>(tile_ + t * CH + c0); };
     auto states = [&](const float* tile_, int t) { return *reinterpret_cast<const floatx4*>(tile_ + t * NP + n0); };
 #pragma unroll 1
     for (int s0 = (nt - 1) / SUB * SUB; s0 >= 0; s0 -= SUB) {
-      float h[4][4], H[SUB][4][4], e0[4][4], e1[4][4];  // H[i]: the state before token s0 + i
+      float h[Q][4], H[SUB][Q][4], e0[Q][4], e1[Q][4];  // H[i]: the state before token s0 + i
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int n = 0; n < 4; ++n) h[q][n] = hs[q][n];
       if (l0 + s0 > p.begin) start(l0 + s0 - SUB);  // while this run is worked on
       scan_exp(e0, A2, token(ds, s0));
       {
-        floatx4 u = token(us, s0), bb = states(bs, s0), d1 = token(ds, s0 + 1);
+        floatx4 bb = states(bs, s0);
+        Col u = token(us, s0), d1 = token(ds, s0 + 1);
 #pragma unroll
         for (int i = 0; i < SUB; ++i) {
           const int t1 = s0 + (i + 1 < SUB ? i + 1 : i), t2 = s0 + (i + 2 < SUB ? i + 2 : SUB - 1);
-          const floatx4 u1 = token(us, t1), b1 = states(bs, t1), d2 = token(ds, t2);
+          const floatx4 b1 = states(bs, t1);
+          const Col u1 = token(us, t1), d2 = token(ds, t2);
           if (i + 1 < SUB) scan_exp(e1, A2, d1);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int n = 0; n < 4; ++n) H[i][q][n] = h[q][n];
           scan_step(h, e0, u, bb);
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
+          for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
           u = u1;
@@ -1138,28 +1155,28 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
       // as the states
       asm volatile("" ::: "memory");
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int n = 0; n < 4; ++n) asm volatile("" : "+v"(A2[q][n]));
-      floatx4 d = token(ds, s0 + SUB - 1), u = token(us, s0 + SUB - 1), s = token(ss, s0 + SUB - 1);
-      floatx4 bb = states(bs, s0 + SUB - 1), cc = states(cs, s0 + SUB - 1), d1 = token(ds, s0 + SUB - 2);
+      Col d = token(ds, s0 + SUB - 1), u = token(us, s0 + SUB - 1), s = token(ss, s0 + SUB - 1), d1 = token(ds, s0 + SUB - 2);
+      floatx4 bb = states(bs, s0 + SUB - 1), cc = states(cs, s0 + SUB - 1);
       scan_exp(e0, A2, d);
-      floatx4 gb = {}, ga = {}, ch = {};
+      Col gb = {}, ga = {}, ch = {};
       float db[4] = {}, dc[4] = {};
       // the sums over lanes of a token are taken beside the next one's products
       auto sums = [&](int t) {
-        floatx4 v;
+        Col v;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(gb[q]);
+        for (int q = 0; q < Q; ++q) v[q] = lanes_sum<NL>(gb[q]);
         // d x of this token has been read by every lane of these columns; lanes that hold the same sums write them alike,
         // without a branch
-        *reinterpret_cast<floatx4*>(us + t * CH + c0) = v;
+        *reinterpret_cast<Col*>(us + t * CH + c0) = v;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ga[q]);
-        *reinterpret_cast<floatx4*>(as + t * CH + c0) = v;
+        for (int q = 0; q < Q; ++q) v[q] = lanes_sum<NL>(ga[q]);
+        *reinterpret_cast<Col*>(as + t * CH + c0) = v;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = lanes_sum<NL>(ch[q]);
-        *reinterpret_cast<floatx4*>(hc + t * CH + c0) = v;
+        for (int q = 0; q < Q; ++q) v[q] = lanes_sum<NL>(ch[q]);
+        *reinterpret_cast<Col*>(hc + t * CH + c0) = v;
         mine[(t * 2) * NP + n0 + lane / 16] = columns_sum<NL>(db[0], db[1], db[2], db[3]);  // state n0 + row
         mine[(t * 2 + 1) * NP + n0 + lane / 16] = columns_sum<NL>(dc[0], dc[1], dc[2], dc[3]);
       };
@@ -1167,13 +1184,14 @@ __global__ __launch_bounds__(64 * kScanWaves, 1) void eql_scan_bwd_kernel(const 
       for (int i = SUB - 1; i >= 0; --i) {
         const int t = s0 + i, before = i ? t - 1 : t, before2 = i > 1 ? t - 2 : s0;
         // the tokens before are read while this one is worked on
-        const floatx4 d2 = token(ds, before2), u1 = token(us, before), s1 = token(ss, before), b1 = states(bs, before), c1 = states(cs, before);
+        const Col d2 = token(ds, before2), u1 = token(us, before), s1 = token(ss, before);
+        const floatx4 b1 = states(bs, before), c1 = states(cs, before);
         if (i > 0) scan_exp(e1, A2, d1);
         if (i + 1 < SUB) sums(t + 1);
 #pragma unroll
         for (int n = 0; n < 4; ++n) db[n] = dc[n] = 0.0f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < Q; ++q) {
           float sb = 0.0f, sa = 0.0f, sc = 0.0f;
 #pragma unroll
           for (int n = 0; n < 4; ++n) {
