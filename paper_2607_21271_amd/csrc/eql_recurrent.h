@@ -22,8 +22,8 @@ constexpr int kWhole = 0, kLoose = 1, kTiny = 2;
 constexpr int kScanMaxN = 64;
 constexpr int scan_lanes(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 constexpr int scan_cols(int NL, int Q = 4) { return 64 * Q / NL; }
-// columns of a lane in the gradients (eql_scan_bwd_kernel)
-constexpr int scan_bwd_columns(int NL) { return NL == 16 ? 4 : 2; }
+// columns of a lane in the kernels of tiles
+constexpr int scan_columns(int NL) { return NL == 16 ? 4 : 2; }
 // tokens of a tile, and of a run, whose first state training keeps
 constexpr int scan_tile(int NL) { return NL == 1 ? 4 : NL == 2 ? 8 : 16; }
 constexpr int scan_run(int NL) { return NL == 1 ? 4 : 8; }

@@ -156,7 +156,7 @@ static double scan_time(int64_t waves, int64_t tokens, int64_t simds, double one
 // Gradients: workgroups of four, two or one wave, which fill a CU's four SIMDs alike (three where there are no more); smaller
 // ones leave fewer waves without columns, and more sums of db and dc to memory.
 void scan_plan(ScanArgs& a, int cus, bool bwd) {
-  const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL), back = scan_cols(NL, scan_bwd_columns(NL));
+  const int NL = scan_lanes(a.N), CH = scan_cols(NL), TT = scan_tile(NL), back = scan_cols(NL, scan_columns(NL));
   a.CT = a.C * a.T;
   a.CTg = a.CT / a.G;
   a.nblk = (a.CTg + CH - 1) / CH;
@@ -165,8 +165,8 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.tiles = (a.L + TT - 1) / TT;
   a.runs = (a.L + scan_run(NL) - 1) / scan_run(NL);
   a.mT = channel_factor(a.T);
-  const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1, first = a.B * a.G * a.nblk;
-  const int nblk = bwd ? a.bblk : a.nblk;
+  const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1, first = a.B * a.G * a.bblk;
+  const int nblk = a.bblk;
   const double token = !bwd ? 0.37 : back == CH ? 1.1 : 0.51;
   int64_t per = tiles;
   double least = -1.0;

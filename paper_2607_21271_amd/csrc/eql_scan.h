@@ -411,12 +411,12 @@ __device__ __forceinline__ void load_padded(const float* base, float (&h)[Q][4])
     for (int n = 0; n < 4; ++n) h[q][n] = v[n];
   }
 }
-template <int NL>
-__device__ __forceinline__ void store_padded(float* base, const float (&h)[4][4]) {
+template <int NL, int Q>
+__device__ __forceinline__ void store_padded(float* base, const float (&h)[Q][4]) {
   const int lane = threadIdx.x & 63;
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
-    *reinterpret_cast<floatx4*>(base + (lane / NL * 4 + q) * (4 * NL) + lane % NL * 4) =
+  for (int q = 0; q < Q; ++q)
+    *reinterpret_cast<floatx4*>(base + (lane / NL * Q + q) * (4 * NL) + lane % NL * 4) =
         floatx4{h[q][0], h[q][1], h[q][2], h[q][3]};
 }
 template <int NL, int Q>
@@ -504,24 +504,26 @@ __device__ __forceinline__ void token_end() { __builtin_amdgcn_sched_barrier(0);
 // its SIMD, 646 with a second, against 550 of instructions.  A third wave a SIMD (168 registers) spills.
 template <int NL>
 constexpr int scan_fwd_lds() {  // floats of a wave
-  return 2 * scan_tile(NL) * scan_cols(NL) + 2 * scan_tile(NL) * 4 * NL;
+  return 2 * scan_tile(NL) * scan_cols(NL, scan_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
 }
 template <int DT, int NL, int MODE, bool STATES>
 __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL, MODE>;
+  constexpr int Q = scan_columns(NL);
+  using TL = ScanTile<DT, NL, MODE, Q>;
+  using Col = Cols<Q>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   constexpr int RUN = scan_run(NL);
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned id = blockIdx.x * kScanWaves + wave;
   if (id >= a.tasks) return;  // (no barrier follows)
-  const ScanPlace p = scan_place<NL>(a, id);
+  const ScanPlace p = scan_place<NL, Q>(a, id);
   if (STATES && p.k == a.K - 1) return;
   float* const ds = lds + wave * scan_fwd_lds<NL>();
   float* const us = ds + TT * CH;
   float* const bs = us + TT * CH;
   float* const cs = bs + TT * NP;
-  const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int n0 = lane % NL * 4, c0 = lane / NL * Q, at = TL::at();
   const int64_t stop = min(p.len, p.end);
   const auto xv = TL::view(a.x, p.b * a.xs[0] + p.ct0, a.xs[1], p.left), dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left);
   const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left), yv = TL::view(a.y, p.b * a.L * a.CT + p.ct0, a.CT, p.left);
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     }
   };
   if (p.begin < stop) fetch(p.begin);
-  float A2[4][4], h[4][4], bias[VEC], skip[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
+  float A2[Q][4], h[Q][4], bias[VEC], skip[VEC], total[Q] = {};
   scan_decay<NL, MODE>(a, p, A2);
   scan_param<VEC, MODE>(a, p, a.bias, at, bias);
   if constexpr (!STATES) scan_param<VEC, MODE>(a, p, a.D, at, skip);
@@ -547,7 +549,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   else if (!STATES && a.h0) load_state<NL>(a, p, a.h0, h);
   else
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
       for (int n = 0; n < 4; ++n) h[q][n] = 0.0f;
   for (int64_t l0 = p.begin; l0 < stop; l0 += TT) {
@@ -578,40 +580,42 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     if constexpr (!STATES)
       if (a.states) store_padded<NL>(a.states + ((p.b * a.runs + l0 / RUN) * a.cols + p.col0) * NP, h);
     wave_order();
-    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * CH + c0); };
+    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const Col*>(tile + min(t, TT - 1) * CH + c0); };
     auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + min(t, TT - 1) * NP + n0); };
-    float part[4] = {0.f, 0.f, 0.f, 0.f}, e0[4][4], e1[4][4];
+    float part[Q] = {}, e0[Q][4], e1[Q][4];
     // y of a token, in place of its d x, which every lane of these columns has read; all of them write what all of them hold
     // (a branch here would keep the next token's reads behind it)
     auto output = [&](int t, const floatx4& cc) {
-      floatx4 y;
+      Col y;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < Q; ++q) {
         float s = h[q][0] * cc[0];
 #pragma unroll
         for (int n = 1; n < 4; ++n) s = __builtin_fmaf(h[q][n], cc[n], s);
         y[q] = lanes_sum<NL>(s);
       }
-      *reinterpret_cast<floatx4*>(us + t * CH + c0) = y;
+      *reinterpret_cast<Col*>(us + t * CH + c0) = y;
     };
     if (STATES || nt == TT) {
-      floatx4 d = cols(ds, 0), u = cols(us, 0), bb = rows(bs, 0), cc = {};
+      Col d = cols(ds, 0), u = cols(us, 0);
+      floatx4 bb = rows(bs, 0), cc = {};
       if constexpr (!STATES) cc = rows(cs, 0);
       scan_exp(e0, A2, d);
-      floatx4 d1 = cols(ds, 1);
+      Col d1 = cols(ds, 1);
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
         if constexpr (!STATES)
           if (t > 0 && t % RUN == 0 && a.states)
             store_padded<NL>(a.states + ((p.b * a.runs + (l0 + t) / RUN) * a.cols + p.col0) * NP, h);
-        const floatx4 d2 = cols(ds, t + 2), u1 = cols(us, t + 1), b1 = rows(bs, t + 1);
+        const Col d2 = cols(ds, t + 2), u1 = cols(us, t + 1);
+        const floatx4 b1 = rows(bs, t + 1);
         floatx4 c1 = {};
         if constexpr (!STATES) c1 = rows(cs, t + 1);
         if (t + 1 < TT) scan_exp(e1, A2, d1);
         scan_step(h, e0, u, bb);
         if constexpr (STATES) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) part[q] += d[q];
+          for (int q = 0; q < Q; ++q) part[q] += d[q];
         } else {
           output(t, cc);
         }
@@ -621,7 +625,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
         bb = b1;
         cc = c1;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < Q; ++q)
 #pragma unroll
           for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
         token_end();
@@ -639,7 +643,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
     }
     if constexpr (STATES) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) total[q] += part[q];
+      for (int q = 0; q < Q; ++q) total[q] += part[q];
     } else {
       wave_order();
       float xf[EPT], yf[EPT];
@@ -660,7 +664,9 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   }
   if constexpr (STATES) {
     store_padded<NL>(a.carry + slot * NP, h);
-    if (lane % NL == 0) *reinterpret_cast<floatx4*>(a.sums + slot + c0) = floatx4{total[0], total[1], total[2], total[3]};
+    if (lane % NL == 0)
+#pragma unroll
+      for (int q = 0; q < Q; ++q) a.sums[slot + c0 + q] = total[q];
   } else {
     float zero[EPT];
 #pragma unroll
@@ -861,18 +867,20 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
 // r behind a chunk from zero, and its sum of d (chunks 1 .. K - 1): r = a (c s + r) from the last token to the first.
 template <int DT, int NL, int MODE>
 __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const ScanArgs a) {
-  using TL = ScanTile<DT, NL, MODE>;
+  constexpr int Q = scan_columns(NL);
+  using TL = ScanTile<DT, NL, MODE, Q>;
+  using Col = Cols<Q>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;
   __shared__ __attribute__((aligned(16))) float lds[kScanWaves * scan_fwd_lds<NL>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned id = blockIdx.x * kScanWaves + wave;
   if (id >= a.tasks) return;  // (no barrier follows)
-  const ScanPlace p = scan_place<NL>(a, id);
+  const ScanPlace p = scan_place<NL, Q>(a, id);
   if (p.k == 0) return;
   float* const ds = lds + wave * scan_fwd_lds<NL>();
   float* const ss = ds + TT * CH;
   float* const cs = ss + TT * CH;
-  const int n0 = lane % NL * 4, c0 = lane / NL * 4, at = TL::at();
+  const int n0 = lane % NL * 4, c0 = lane / NL * Q, at = TL::at();
   const int64_t stop = min(p.len, p.end);
   const auto dv = TL::view(a.delta, p.b * a.ds[0] + p.ct0, a.ds[1], p.left), gv = TL::view(a.dy, p.b * a.L * a.CT + p.ct0, a.CT, p.left);
   const auto zv = TL::view(a.z, p.b * a.zs[0] + p.ct0, a.zs[1], p.left);
@@ -887,11 +895,11 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
   };
   const int64_t tiles = (max(stop - p.begin, (int64_t)0) + TT - 1) / TT;
   if (tiles > 0) fetch(p.begin + (tiles - 1) * TT);
-  float A2[4][4], r[4][4], bias[VEC], total[4] = {0.f, 0.f, 0.f, 0.f};
+  float A2[Q][4], r[Q][4], bias[VEC], total[Q] = {};
   scan_decay<NL, MODE>(a, p, A2);
   scan_param<VEC, MODE>(a, p, a.bias, at, bias);
 #pragma unroll
-  for (int q = 0; q < 4; ++q)
+  for (int q = 0; q < Q; ++q)
 #pragma unroll
     for (int n = 0; n < 4; ++n) r[q][n] = 0.0f;
   for (int64_t tile = tiles - 1; tile >= 0; --tile) {
@@ -923,17 +931,19 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
     }
     if (tile > 0) fetch(l0 - TT);
     wave_order();
-    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + max(t, 0) * CH + c0); };
+    auto cols = [&](const float* tile, int t) { return *reinterpret_cast<const Col*>(tile + max(t, 0) * CH + c0); };
     auto rows = [&](const float* tile, int t) { return *reinterpret_cast<const floatx4*>(tile + max(t, 0) * NP + n0); };
-    float part[4] = {0.f, 0.f, 0.f, 0.f}, e0[4][4], e1[4][4];
-    floatx4 d = cols(ds, TT - 1), s = cols(ss, TT - 1), cc = rows(cs, TT - 1), d1 = cols(ds, TT - 2);
+    float part[Q] = {}, e0[Q][4], e1[Q][4];
+    Col d = cols(ds, TT - 1), s = cols(ss, TT - 1), d1 = cols(ds, TT - 2);
+    floatx4 cc = rows(cs, TT - 1);
     scan_exp(e0, A2, d);
 #pragma unroll
     for (int t = TT - 1; t >= 0; --t) {
-      const floatx4 d2 = cols(ds, t - 2), s1 = cols(ss, t - 1), c1 = rows(cs, t - 1);
+      const Col d2 = cols(ds, t - 2), s1 = cols(ss, t - 1);
+      const floatx4 c1 = rows(cs, t - 1);
       if (t > 0) scan_exp(e1, A2, d1);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < Q; ++q) {
         part[q] += d[q];
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
@@ -948,11 +958,13 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
       token_end();
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) total[q] += part[q];
+    for (int q = 0; q < Q; ++q) total[q] += part[q];
   }
   const int64_t slot = (p.b * a.K + p.k) * a.cols + p.col0;
   store_padded<NL>(a.carry + slot * NP, r);
-  if (lane % NL == 0) *reinterpret_cast<floatx4*>(a.sums + slot + c0) = floatx4{total[0], total[1], total[2], total[3]};
+  if (lane % NL == 0)
+#pragma unroll
+    for (int q = 0; q < Q; ++q) a.sums[slot + c0 + q] = total[q];
 }
 
 // The gradients.  The waves of a workgroup take neighbouring column blocks of one group and chunk, so that db
@@ -965,7 +977,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 // Measured, f16, 16 states: 64 x 197 tokens of 768 columns 174 us, 1.1 ps a state of a token.
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave
-  return 7 * scan_tile(NL) * scan_cols(NL, scan_bwd_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
+  return 7 * scan_tile(NL) * scan_cols(NL, scan_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
 }
 template <int NL>
 constexpr int scan_red_lds() {  // floats of a wave's db and dc, twice
@@ -976,8 +988,8 @@ constexpr int scan_bwd_bytes(int waves) {
   return waves * (scan_bwd_lds<NL>() + scan_red_lds<NL>()) * 4;
 }
 template <int DT, int NL, int MODE>
-__global__ __launch_bounds__(64 * kScanWaves, scan_bwd_columns(NL) == 4 ? 1 : 2) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
-  constexpr int Q = scan_bwd_columns(NL);
+__global__ __launch_bounds__(64 * kScanWaves, scan_columns(NL) == 4 ? 1 : 2) void eql_scan_bwd_kernel(const ScanArgs a, int waves) {
+  constexpr int Q = scan_columns(NL);
   using TL = ScanTile<DT, NL, MODE, Q>;
   using Col = Cols<Q>;
   constexpr int TT = TL::TT, CH = TL::CH, EPT = TL::EPT, VEC = TL::VEC, NP = TL::NP;

@@ -33,17 +33,17 @@ hipError_t elements(const ScanArgs& a, int64_t n, int per, F&& f) {
   }
   return hipSuccess;
 }
-dim3 wave_blocks(ScanArgs& s, int64_t seqs) {
-  s.tasks = (unsigned)(seqs * s.K * s.G * s.nblk);
+dim3 wave_blocks(ScanArgs& s, int64_t seqs, int blocks) {
+  s.tasks = (unsigned)(seqs * s.K * s.G * blocks);
   return dim3((s.tasks + kScanWaves - 1) / kScanWaves);
 }
 
 template <int NL, int MODE>
 hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
-  const int64_t waves = (int64_t)a.K * a.G * a.nblk;
+  const int64_t waves = (int64_t)a.K * a.G * a.bblk;
   if (a.K > 1) {
     hipError_t e = sequences(a, waves, [&](ScanArgs s, int64_t n) {
-      const dim3 g = wave_blocks(s, n);
+      const dim3 g = wave_blocks(s, n, s.bblk);
       hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, MODE, true>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
@@ -53,7 +53,7 @@ hipError_t fwd(const ScanArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   return sequences(a, waves, [&](ScanArgs s, int64_t n) {
-    const dim3 g = wave_blocks(s, n);
+    const dim3 g = wave_blocks(s, n, s.bblk);
     hipLaunchKernelGGL((eql_scan_fwd_kernel<DT, NL, MODE, false>), g, dim3(64 * kScanWaves), 0, stream, s);
   });
 }
@@ -62,8 +62,8 @@ template <int NL, int MODE>
 hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
   hipError_t e;
   if (a.K > 1) {
-    e = sequences(a, (int64_t)a.K * a.G * a.nblk, [&](ScanArgs s, int64_t n) {
-      const dim3 g = wave_blocks(s, n);
+    e = sequences(a, (int64_t)a.K * a.G * a.bblk, [&](ScanArgs s, int64_t n) {
+      const dim3 g = wave_blocks(s, n, s.bblk);
       hipLaunchKernelGGL((eql_scan_back_kernel<DT, NL, MODE>), g, dim3(64 * kScanWaves), 0, stream, s);
     });
     if (e != hipSuccess) return e;
@@ -97,7 +97,7 @@ hipError_t bwd(const ScanArgs& a, hipStream_t stream) {
 template <int NL>
 hipError_t few(const ScanArgs& a, hipStream_t stream) {
   return sequences(a, (int64_t)a.G * a.nblk, [&](ScanArgs s, int64_t n) {
-    const dim3 g = wave_blocks(s, n);
+    const dim3 g = wave_blocks(s, n, s.nblk);
     hipLaunchKernelGGL((eql_scan_few_kernel<DT, NL>), g, dim3(64 * kScanWaves), 0, stream, s);
   });
 }

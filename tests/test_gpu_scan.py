@@ -75,7 +75,8 @@ def test_scan(size, dt):
 
 # gradients in workgroups of one, two, three and four waves, several side by side for a group's columns, chunks of several tiles
 @pytest.mark.parametrize("size", [(64, 33, 520, 1, 5, 1), (33, 50, 520, 1, 5, 1), (40, 33, 520, 1, 2, 1), (17, 100, 520, 1, 5, 1),
-                                  (130, 9, 65, 1, 33, 1)], ids=lambda s: "x".join(map(str, s)))
+                                  (130, 9, 65, 1, 33, 1), (130, 33, 5, 1, 2, 1), (33, 50, 257, 1, 5, 1), (40, 33, 257, 1, 2, 1),
+                                  (17, 100, 257, 1, 5, 1), (130, 9, 257, 1, 5, 1), (40, 50, 129, 1, 2, 1), (1, 33, 97, 1, 16, 1)], ids=lambda s: "x".join(map(str, s)))
 @pytest.mark.parametrize("dt", ["f32", "f16"])
 def test_workgroups(size, dt):
     t = make(sum(size), *size, dt)
