@@ -143,16 +143,21 @@ int scan_mode(const eqk::ScanArgs& a, int dtype) {
 
 namespace eqk {
 
-// Microseconds of `waves` waves that walk `tokens` tokens each, at `one` a token for a wave alone on its SIMD (and eight
-// tokens' time before the first).  half: two on a SIMD hide half of each other's time, else none.
-static double scan_time(int64_t waves, int64_t tokens, int64_t simds, double one, bool half) {
+// Microseconds of a kernel whose waves, w to a SIMD, walk `tokens` tokens each: its start, and for a token `each` a wave and
+// `round` where `slots` of them hide the rest of each other's time.  Measured at 16 states: forward 0.19, 0.31 and 0.55 us a
+// token with 1, 2 and 4 waves a SIMD, gradients 0.60, 0.90 and 1.80; above 32 states, with four columns a lane, 0.31 and 0.50
+// and, gradients, 1.2 a wave.
+struct ScanRate {
+  double start, round, each;
+  int slots;
+};
+static double scan_time(int64_t waves, int64_t tokens, int64_t simds, const ScanRate& r) {
   const int64_t w = (waves + simds - 1) / simds;
-  return one * (double)(tokens + 8) * (half ? 0.75 * w + (w % 2 ? 0.25 : 0.0) : (double)w);
+  return r.start + (double)tokens * (r.round * (double)((w + r.slots - 1) / r.slots) + r.each * (double)w);
 }
 
 // Chunks of tokens where the columns alone do not fill the device: the number of waves (one to four a SIMD) for which the
-// pass over the states or gradients and the main one take least, by what a token of theirs takes: 0.26 and 0.37 us
-// forward, back 0.25 and 0.51 (1.1 with four columns a lane).
+// main pass and the one before it over states or gradients, 0.7 of the forward's main one, take least.
 // Gradients: workgroups of four, two or one wave, which fill a CU's four SIMDs alike (three where there are no more); smaller
 // ones leave fewer waves without columns, and more sums of db and dc to memory.
 void scan_plan(ScanArgs& a, int cus, bool bwd) {
@@ -167,7 +172,9 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
   a.mT = channel_factor(a.T);
   const int64_t simds = 4 * (int64_t)cus, tiles = a.tiles > 0 ? a.tiles : 1, first = a.B * a.G * a.bblk;
   const int nblk = a.bblk;
-  const double token = !bwd ? 0.37 : back == CH ? 1.1 : 0.51;
+  const bool two = back < CH;
+  const ScanRate forward = two ? ScanRate{7.0, 0.065, 0.122, 4} : ScanRate{7.0, 0.11, 0.195, 2};
+  const ScanRate main = !bwd ? forward : two ? ScanRate{12.0, 0.3, 0.3, 2} : ScanRate{12.0, 0.0, 1.2, 1};
   int64_t per = tiles;
   double least = -1.0;
   for (int waves = nblk < kScanWaves ? nblk : kScanWaves; waves > 0; --waves) {
@@ -183,15 +190,16 @@ void scan_plan(ScanArgs& a, int cus, bool bwd) {
       a.P = P;
       a.waves = waves;
     };
-    take(tiles, scan_time(one, tiles * TT, simds, token, !bwd));
+    take(tiles, scan_time(one, tiles * TT, simds, main));
     for (int w = 1; w <= 4 && one > 0 && one < 2 * simds; ++w) {
       int64_t K = w * simds / one;
       if (K > tiles) K = tiles;
       if (K < 2) continue;
       const int64_t n = (tiles + K - 1) / K;
       K = (tiles + n - 1) / n;
-      // (two more launches, and the states between the passes: about ten microseconds)
-      take(n, scan_time(one * K, n * TT, simds, token, !bwd) + scan_time(first * K, n * TT, simds, bwd ? 0.25 : 0.26, true) + 10.0);
+      // two more launches, and the states between the passes: written, carried over the chunks and read
+      const double carry = 7.0 + (double)(a.B * K) * a.cols * 4 * NL * 16 / 5e6;
+      take(n, scan_time(one * K, n * TT, simds, main) + 0.7 * scan_time(first * K, n * TT, simds, forward) + carry);
     }
     if (!bwd) break;
   }
