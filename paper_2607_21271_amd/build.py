@@ -39,9 +39,10 @@ ARCH = "gfx950"
 # bytes a lane) and the attention's key gradient at heads above 96 (64 in bf16,
 # 352 in fp16; 164 in full precision, one wave).  The large-tile unit (one wave per SIMD, T * 64
 # accumulators per lane) and full-precision attention keep them in the
-# accumulation registers instead.  Of the recurrent kernels, scratch is used by some scans whose
-# columns or states are no whole vectors (32 to 48 bytes a lane) and by the residual norm's gradients over rows of
-# more than 4096 elements (16 to 60 bytes; 208 in fp32 where the rows are no whole vectors).
+# accumulation registers instead.  Of the recurrent kernels, scratch is used by the scan's
+# gradients at 5 to 16 states (72 to 172 bytes a lane, 124 to 212 in fp32; some others 20 to 112), outside the loops over
+# tokens, and by the residual norm's over rows of more than 4096 elements (16 to 60 bytes; 208 in fp32 where the rows are
+# no whole vectors).
 LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 DEVICE_FLAGS = LINK_FLAGS + VGPR_FORM

@@ -8,8 +8,8 @@
 //   dd = sum_n A a g h_{l-1} + x sum_n g b,  dA[n] = sum d a g h_{l-1},  dz = dy (sum_n c h + D x) silu'(z).
 //
 // A wave takes a block of columns (channel, group element) of one group and walks the tokens in tiles.
-// NL lanes share four columns and hold four states of each in registers: a token costs a lane two 16-byte
-// reads of d and d x and two of b and c from LDS for 16 states.  Element by element work (softplus, the gate, loads and
+// NL lanes share Q columns, two (four above 32 states), and hold four states of each in registers: a token costs a lane two
+// reads of d and d x and two of b and c from LDS for 4 Q states.  Element by element work (softplus, the gate, loads and
 // stores in whole vectors) runs on the tile's elements spread over all lanes; d and d x go to the
 // scan through LDS, y comes back the same way.  No barrier in the forward: a wave's LDS is its own.
 //
@@ -499,9 +499,9 @@ __device__ __forceinline__ void token_end() { __builtin_amdgcn_sched_barrier(0);
 
 // ---- forward ---------------------------------------------------------------
 // STATES: only the state that a chunk forms from zero and its sum of d (chunks 0 .. K - 2).
-// Measured, f16, 16 states: 16,389 tokens of 768 columns in 147 chunks 49 us + 9 for the carry + 67; 64 x 197 tokens
-// without chunks, states kept for the gradients, 74 us (0.48 ps a state of a token): a wave's 780 cycles a token alone on
-// its SIMD, 646 with a second, against 550 of instructions.  A third wave a SIMD (168 registers) spills.
+// Measured, f16, 16 states: 16,389 tokens of 768 columns in 114 chunks 46 us + 8 for the carry + 64; 64 x 197 tokens
+// without chunks, states kept for the gradients, 62 to 67 us (0.41 ps a state of a token).  A token takes 0.19 us with one wave
+// on a SIMD, 0.30 with two and 0.55 with four (with four columns a lane, for twice the work, 0.36 and 0.60, and no more fit).
 template <int NL>
 constexpr int scan_fwd_lds() {  // floats of a wave
   return 2 * scan_tile(NL) * scan_cols(NL, scan_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
@@ -971,10 +971,10 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 // and dc are summed over them before they leave; a tile is walked from its last run of SUB tokens to the
 // first: the states of a run are formed again from the one before it, which the forward kept, and held in registers.
 // What a tile's elements need twice (step, slope, gate, dy silu(z)) waits in LDS beside the scan's sums.
-// Two columns a lane (four above 32 states): a run's states take 64 registers, and two waves fit a SIMD, 205 us below with four
-// columns and one wave.  Bound by the vector pipe: a wave alone needs 0.51 us a token, two 0.97 together.  What is spilled
-// (20 to 40 registers) is used once a tile.
-// Measured, f16, 16 states: 64 x 197 tokens of 768 columns 174 us, 1.1 ps a state of a token.
+// Two columns a lane (four above 32 states): a run's states take 64 registers, and two waves fit a SIMD.  Bound by the vector
+// pipe: a wave alone takes 0.6 us a token, two 0.9 together (with four columns, for twice the work, 1.1 us, and no second
+// wave fits).  What is spilled (17 to 52 registers) is used once a tile, not in the loops over tokens.
+// Measured, f16, 16 states: 64 x 197 tokens of 768 columns 172 to 187 us, 1.1 to 1.2 ps a state of a token (205 with four).
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave
   return 7 * scan_tile(NL) * scan_cols(NL, scan_columns(NL)) + 2 * scan_tile(NL) * 4 * NL;
