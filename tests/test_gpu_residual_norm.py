@@ -75,8 +75,9 @@ OPTIONS = [dict(zip(("weight", "bias", "scale", "gate", "post", "post_bias"), c)
 
 
 @pytest.mark.parametrize("option", OPTIONS, ids=lambda o: "".join(str(v) for v in o.values()))
-def test_what_may_be_left_out(option):
-    t = make(5, 3, 20, 12, 4, "f16", **option)
+@pytest.mark.parametrize("C", [12, 11])
+def test_what_may_be_left_out(option, C):
+    t = make(5, 3, 20, C, 4, "f16", **option)
     dr, dh = grads(4, t)
     check(t)
     check(t, dr, None)

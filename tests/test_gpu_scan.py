@@ -90,10 +90,14 @@ def test_workgroups(size, dt):
 def test_ways_to_read(N, C, dt):
     """Whole vectors, rows that are none, rows shorter than one, for every number of lanes that share columns, two or three tiles
     of one wave."""
-    L = 10 if N == 4 else 20
-    t = make(N + C, 1030, L, C, 1, N if C == 8 else N - 1, 1, dt)
+    L, n = 10 if N == 4 else 20, N if C == 8 else N - 1
+    t = make(N + C, 1030, L, C, 1, n, 1, dt)
     check(t)
     check(t, *grads(7, t, L))
+    # without the gate and the softplus
+    t = make(N + C, 1030, L, C, 1, n, 1, dt, 1, 0, 1, 0, False)
+    check(t, softplus=False)
+    check(t, grads(7, t, L)[0], None, softplus=False)
 
 
 @pytest.mark.parametrize("D,z,bias,state,softplus", [c for c in itertools.product([0, 1], repeat=5) if sum(c) in (0, 1, 4)])
