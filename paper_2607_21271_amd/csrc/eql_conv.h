@@ -13,6 +13,7 @@
 #include "eql_common.h"
 #include "eql_config.h"
 #include "eql_recurrent.h"
+#include "eql_slices.h"
 #include "eql_vectors.h"
 
 namespace eqk {
@@ -46,29 +47,29 @@ __device__ __forceinline__ void conv_store(void* p, const ConvPlace& at, const f
   store_vector<DT, VEC, MODE>(p, at.skip, at.n, f);
 }
 template <int VEC, int MODE>
-__device__ __forceinline__ ConvPlace conv_place(const ConvArgs& a) {
+__host__ __device__ __forceinline__ ConvPlace conv_place(const ConvArgs& a, unsigned block, int thread) {
   ConvPlace p;
   const int nv = (a.CT + VEC - 1) / VEC;
-  unsigned id = blockIdx.x;
-  const int cb = (int)(id % (unsigned)a.cblocks);
-  id /= (unsigned)a.cblocks;
-  p.group = id % (unsigned)a.groups;
-  p.b = a.first + id / (unsigned)a.groups;
-  p.vector = (int)threadIdx.x % a.width;
-  p.turn = (int)threadIdx.x / a.width;
+  const SlicePlace at = slice_place(a.seq, a.first, block, (unsigned)(a.groups * a.cblocks));
+  const int cb = (int)(at.at % (unsigned)a.cblocks);
+  p.group = at.at / (unsigned)a.cblocks;
+  p.b = at.seq;
+  p.vector = thread % a.width;
+  p.turn = thread / a.width;
   p.has = cb * a.width + p.vector < nv;
   p.col = (cb * a.width + p.vector) * VEC;
   p.skip = 0;
   p.n = MODE == kTiny ? a.CT : VEC;
   if constexpr (MODE == kLoose) {
-    p.skip = max(p.col - (a.CT - VEC), 0);
+    p.skip = p.col > a.CT - VEC ? p.col - (a.CT - VEC) : 0;
     p.col -= p.skip;
   }
   const int64_t strip = p.group * a.turns + p.turn;
   p.on = p.turn < a.turns && strip < a.strips && p.has;
-  p.len = a.lengths ? min(max((int64_t)a.lengths[p.b], (int64_t)0), a.L) : a.L;
+  const int64_t n = a.lengths ? a.lengths[p.b] : a.L;
+  p.len = n < 0 ? 0 : n > a.L ? a.L : n;
   p.l0 = p.on ? strip * a.rows : 0;
-  p.l1 = p.on ? min(p.l0 + a.rows, a.L) : 0;
+  p.l1 = !p.on ? 0 : p.l0 + a.rows < a.L ? p.l0 + a.rows : a.L;
   return p;
 }
 template <int DT, int W, int VEC, int GR>
@@ -101,7 +102,7 @@ constexpr int kConvRows = 16;  // of a forward strip
 template <int DT, int W, int VEC, int GR, int MODE>
 __global__ __launch_bounds__(256) void eql_conv_fwd_kernel(const ConvArgs a) {
   constexpr int EB = Elem<DT>::bytes;
-  const ConvPlace p = conv_place<VEC, MODE>(a);
+  const ConvPlace p = conv_place<VEC, MODE>(a, blockIdx.x, (int)threadIdx.x);
   if (!p.on) return;
   ConvVec<DT, VEC> raw[kConvRows + W - 1];  // tokens l0 - (W - 1) ..
   const bool inner = p.l0 >= W - 1 && p.l0 + kConvRows <= p.len;
@@ -160,7 +161,7 @@ constexpr int kConvBatch = 4;
 template <int DT, int W, int VEC, int GR, int MODE>
 __global__ __launch_bounds__(256) void eql_conv_bwd_kernel(const ConvArgs a) {
   constexpr int EB = Elem<DT>::bytes, NG = VEC / GR;
-  const ConvPlace p = conv_place<VEC, MODE>(a);
+  const ConvPlace p = conv_place<VEC, MODE>(a, blockIdx.x, (int)threadIdx.x);
   const int steps = a.rows + W - 1;
   const bool inner = p.on && p.l0 >= W - 1 && p.l0 + steps <= p.len;
   ConvVec<DT, VEC> xr[kConvBatch], gr[kConvBatch], before[W];

@@ -3,6 +3,7 @@
 #include "eql_conv.h"
 #include "eql_launch.h"
 #include "eql_resnorm.h"
+#include "eql_slices.h"
 
 namespace eqk {
 namespace {
@@ -10,23 +11,20 @@ namespace {
 constexpr int DT = EQK_DT;
 
 // f(slice of the call that one launch takes, its workgroups) for `per` workgroups a sequence: fewer than 2^32
-// threads a launch, and numbers of workgroups below 2^31 from its first sequence on.
+// threads a launch.
 template <typename A, typename F>
 hipError_t launches(const A& a, int64_t seqs, int64_t per, int threads, F&& f) {
+  if (per < 1 || per > kSliceReach) return hipErrorInvalidValue;
   A s = a;
-  const int64_t some = ((int64_t)1 << 31) - 1, most = launch_blocks(threads);
-  if (per < 1 || per > some) return hipErrorInvalidValue;
-  const int64_t step = some / per;
-  for (s.seq = 0; s.seq < seqs; s.seq += step) {
-    const int64_t n = (seqs - s.seq < step ? seqs - s.seq : step) * per;
-    for (int64_t first = 0; first < n; first += most) {
-      s.first = (unsigned)first;
-      f(s, dim3((unsigned)(n - first < most ? n - first : most)));
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  }
-  return hipSuccess;
+  hipError_t e = hipSuccess;
+  slices(seqs, per, launch_blocks(threads), kSliceReach, [&](int64_t seq, unsigned first, unsigned blocks) {
+    s.seq = seq;
+    s.first = first;
+    f(s, dim3(blocks));
+    e = hipGetLastError();
+    return e == hipSuccess;
+  });
+  return e;
 }
 
 template <int W, bool BACK, int GR, int MODE>

@@ -20,6 +20,7 @@
 #include "eql_config.h"
 #include "eql_lanes.h"
 #include "eql_recurrent.h"
+#include "eql_slices.h"
 #include "eql_vectors.h"
 
 namespace eqk {
@@ -152,9 +153,9 @@ struct ResPlace {
 };
 __device__ __forceinline__ ResPlace res_place(const ResArgs& a) {
   ResPlace p;
-  const unsigned id = a.first + blockIdx.x;
-  p.q = a.seq + id / (unsigned)a.strips;
-  p.strip = id % (unsigned)a.strips;
+  const SlicePlace at = slice_place(a.seq, a.first, blockIdx.x, (unsigned)a.strips);
+  p.q = at.seq;
+  p.strip = at.at;
   p.first = p.strip * a.strip;
   p.last = min(p.first + a.strip, a.rows);
   return p;
@@ -367,11 +368,9 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, MODE, GR>::THREADS)) void e
 // sums[q, j, c]: the strips and group elements of a sequence's column sums.
 template <int UNUSED = 0>
 __global__ __launch_bounds__(kColsumThreads) void eql_res_strips_kernel(const ResArgs a, int GR, int blocks) {
-  unsigned id = a.first + blockIdx.x;
-  const int block = (int)(id % (unsigned)blocks);
-  id /= (unsigned)blocks;
-  const int j = (int)(id % (unsigned)a.J), T = a.T / GR, K = a.K / GR;
-  const int64_t q = a.seq + id / (unsigned)a.J;
+  const SlicePlace at = slice_place(a.seq, a.first, blockIdx.x, (unsigned)(a.J * blocks));
+  const int block = (int)(at.at % (unsigned)blocks), j = (int)(at.at / (unsigned)blocks), T = a.T / GR, K = a.K / GR;
+  const int64_t q = at.seq;
   column_sums(a.part + (q * a.strips * a.J + j) * K, a.strips, (int64_t)a.J * K, a.C, T, block,
               [&](int c, float v) { a.sums[(q * a.J + j) * a.C + c] = v; });
 }
