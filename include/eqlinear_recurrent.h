@@ -35,7 +35,8 @@ extern "C" {
  * sums and exponents in fp32, one rounding of y.  states (fp32, _states_bytes, or NULL) keeps
  * what the backward starts its runs of tokens from.  1 <= N <= 64, T <= 16,
  * C * T <= 65536, groups <= C, B <= 2^20, L <= 2^30, 2^46 elements a tensor (EQL_ERR_UNSUPPORTED above).
- * Elements need only their own alignment; 16-byte aligned addresses and strides run faster. */
+ * Elements need only their own alignment; 16-byte aligned addresses and strides run faster.  Infinities and NaN inside a
+ * sequence do to y and the states what they do in the formulas; a gradient that is infinite there may come as NaN. */
 typedef struct {
   int64_t B, L;
   int32_t C, T, N, groups;

@@ -378,7 +378,9 @@ struct ScanTile {
   }
 };
 
-// A of the lane's four columns and four states, times log2(e); 0 outside, where a state stays 0.  kWhole: four states are all
+// A of states and columns that do not exist: their decay is 1 for every finite step, and 0, not NaN, for an infinite one.
+constexpr float kNoDecay = -0x1p-126f;
+// A of the lane's columns and four states, times log2(e); kNoDecay outside, where a state stays 0.  kWhole: four states are all
 // inside or all outside, and rows of A whole 16-byte words (what lies outside is read from A's start instead).
 template <int NL, int MODE, int Q>
 __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p, float (&A2)[Q][4]) {
@@ -390,12 +392,12 @@ __device__ __forceinline__ void scan_decay(const ScanArgs& a, const ScanPlace& p
     if constexpr (MODE == kWhole) {
       const floatx4 v = *reinterpret_cast<const floatx4*>(s);
 #pragma unroll
-      for (int n = 0; n < 4; ++n) A2[q][n] = m > 0 ? v[n] * kLog2e : 0.0f;
+      for (int n = 0; n < 4; ++n) A2[q][n] = m > 0 ? v[n] * kLog2e : kNoDecay;
     } else {
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
         const float v = s[n < m ? n : 0];
-        A2[q][n] = n < m ? v * kLog2e : 0.0f;
+        A2[q][n] = n < m ? v * kLog2e : kNoDecay;
       }
     }
   }
@@ -477,6 +479,17 @@ __device__ __forceinline__ void scan_param(const ScanArgs& a, const ScanPlace& p
   }
 }
 
+// States past N have b = c = 0 and stay 0 as long as d x is finite: 0 times infinity is NaN, and with c = 0 that would reach
+// y.  Tiles with an infinite or NaN d x are walked with those states set to 0 after each token.  In the gradients such states,
+// and the columns past a group's, turn infinities to NaN only in sums that are infinite anyway.
+template <int EPT>
+__device__ __forceinline__ bool scan_wild(const float (&u)[EPT]) {
+  float v = 0.0f;
+#pragma unroll
+  for (int e = 0; e < EPT; ++e) v = __builtin_fmaf(u[e], 0.0f, v);
+  return __builtin_amdgcn_ballot_w64(v != v) != 0;
+}
+
 // The decays of a token: exp(d A).
 template <int Q>
 __device__ __forceinline__ void scan_exp(float (&e)[Q][4], const float (&A2)[Q][4], const Cols<Q>& d) {
@@ -555,6 +568,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
   for (int64_t l0 = p.begin; l0 < stop; l0 += TT) {
     const int nt = (int)min(stop - l0, (int64_t)TT);
     typename TL::Raw xc = xr, zc = zr;  // of this tile, while the next one's are on their way
+    bool wild = false;
     {
       float xf[EPT], df[EPT];
       TL::floats(dr, p.left, df);
@@ -573,6 +587,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
 #pragma unroll
       for (int e = 0; e < EPT; ++e) df[e] *= xf[e];
       TL::put(us, df);
+      if (!STATES && a.N < NP) wild = scan_wild(df);  // (of a chunk's own states the carry drops those past N)
       TL::put_bc(bs, br, a.N);
       if constexpr (!STATES) TL::put_bc(cs, cr, a.N);
     }
@@ -596,7 +611,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
       }
       *reinterpret_cast<Col*>(us + t * CH + c0) = y;
     };
-    if (STATES || nt == TT) {
+    if (STATES || (nt == TT && !wild)) {
       Col d = cols(ds, 0), u = cols(us, 0);
       floatx4 bb = rows(bs, 0), cc = {};
       if constexpr (!STATES) cc = rows(cs, 0);
@@ -630,7 +645,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
           for (int n = 0; n < 4; ++n) e0[q][n] = e1[q][n];
         token_end();
       }
-    } else {  // a sequence's last tokens, or a call over few
+    } else {  // a sequence's last tokens, a call over few, infinities
 #pragma unroll 1
       for (int t = 0; t < nt; ++t) {
         if constexpr (!STATES)
@@ -638,6 +653,11 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_fwd_kernel(const 
             store_padded<NL>(a.states + ((p.b * a.runs + (l0 + t) / RUN) * a.cols + p.col0) * NP, h);
         scan_exp(e0, A2, cols(ds, t));
         scan_step(h, e0, cols(us, t), rows(bs, t));
+        if (wild)
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) h[q][n] = n0 + n < a.N ? h[q][n] : 0.0f;
         output(t, rows(cs, t));
       }
     }
@@ -778,7 +798,8 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_few_kernel(const Sca
         float s = 0.0f;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          h[q][n] = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2[q][n]), h[q][n], u * bb[n]);
+          const float next = __builtin_fmaf(__builtin_amdgcn_exp2f(d * A2[q][n]), h[q][n], u * bb[n]);
+          h[q][n] = n0 + n < a.N ? next : 0.0f;  // (0 times an infinite u)
           s = __builtin_fmaf(h[q][n], cc[n], s);
         }
         out[q] = lanes_sum<NL>(s);
@@ -830,16 +851,18 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
   const int g = col / (a.nblk * CH), in = col - g * a.nblk * CH;
   const bool real = in < a.CTg && n < a.N;
   const int ct = g * a.CTg + in;
-  const float A2 = real ? a.A[(int64_t)scan_channel(a, ct) * a.N + n] * kLog2e : 0.0f;
   const float* first = BACK ? a.dhT : a.h0;
-  float h = first && real ? first[(b * a.CT + ct) * a.N + n] : 0.0f;
   const int64_t cstep = (BACK ? -1 : 1) * (int64_t)a.cols * NP, sstep = (BACK ? -1 : 1) * (int64_t)a.cols;
   const int from = BACK ? a.K - 1 : 0;
   float* c = a.carry + ((b * a.K + from) * a.cols + col) * NP + n;
   const float* s = a.sums + (b * a.K + from) * a.cols + col;
-  // the first chunk of the way has nothing before it; the last one's own result is not wanted
-  auto chunks = [&](auto count) {
+  const float A2 = real ? a.A[(int64_t)scan_channel(a, ct) * a.N + n] * kLog2e : 0.0f;
+  float h = first && real ? first[(b * a.CT + ct) * a.N + n] : 0.0f;
+  // the first chunk of the way has nothing before it; the last one's own result is not wanted; what a chunk formed of
+  // states and columns that do not exist may be NaN and ends here (ALL: the wave has none of them)
+  auto chunks = [&](auto count, auto all) {
     constexpr int n = decltype(count)::value;
+    constexpr bool ALL = decltype(all)::value;
     float v[n], d[n];
 #pragma unroll
     for (int k = 0; k < n; ++k) {
@@ -850,17 +873,21 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
     for (int k = 0; k < n; ++k) d[k] = __builtin_amdgcn_exp2f(d[k] * A2);
 #pragma unroll
     for (int k = 0; k < n; ++k) {
-      c[k * cstep] = h;
+      c[k * cstep] = ALL || real ? h : 0.0f;
       h = __builtin_fmaf(d[k], h, v[k]);
     }
     c += n * cstep;
     s += n * sstep;
   };
-  int left = a.K - 1;
-  for (; left >= kScanAhead; left -= kScanAhead) chunks(std::integral_constant<int, kScanAhead>{});
-  for (; left >= 4; left -= 4) chunks(std::integral_constant<int, 4>{});
-  for (; left > 0; --left) chunks(std::integral_constant<int, 1>{});
-  *c = h;
+  auto walk = [&](auto all) {
+    int left = a.K - 1;
+    for (; left >= kScanAhead; left -= kScanAhead) chunks(std::integral_constant<int, kScanAhead>{}, all);
+    for (; left >= 4; left -= 4) chunks(std::integral_constant<int, 4>{}, all);
+    for (; left > 0; --left) chunks(std::integral_constant<int, 1>{}, all);
+  };
+  if (__builtin_amdgcn_ballot_w64(!real) == 0) walk(std::true_type{});
+  else walk(std::false_type{});
+  *c = real ? h : 0.0f;
 }
 
 // ---- gradients ---------------------------------------------------------------
