@@ -837,6 +837,14 @@ __global__ __launch_bounds__(64 * kScanWaves) void eql_scan_few_kernel(const Sca
   }
 }
 
+// 2^e h + v for any finite e whose product with h is in range, 0 and infinite h too: beyond 2^126 either way the whole part of e
+// goes to h's exponent.
+__device__ __forceinline__ float carried(float e, float h, float v) {
+  const float m = __builtin_fabsf(e);
+  const float w = m <= 126.0f || m == __builtin_inff() ? 0.0f : __builtin_floorf(fminf(fmaxf(e, -1000.0f), 1000.0f));
+  return __builtin_fmaf(__builtin_amdgcn_exp2f(w == 0.0f ? e : fminf(fmaxf(e - w, 0.0f), 1.0f)), __builtin_ldexpf(h, (int)w), v);
+}
+
 // Carries the states over the chunks of a sequence, in place: what a chunk formed from zero becomes what it
 // starts from.  BACK: from the last chunk to the first, the gradient behind a chunk.  A thread takes one
 // column's state and reads kScanAhead chunks before it needs the first.  Bound by the way through memory, once for so many
@@ -863,18 +871,32 @@ __global__ __launch_bounds__(64) void eql_scan_carry_kernel(const ScanArgs a, in
   auto chunks = [&](auto count, auto all) {
     constexpr int n = decltype(count)::value;
     constexpr bool ALL = decltype(all)::value;
-    float v[n], d[n];
+    const float start = h;
+    float v[n], e[n], d[n];
 #pragma unroll
     for (int k = 0; k < n; ++k) {
       v[k] = c[k * cstep];
-      d[k] = s[k * sstep];
+      e[k] = s[k * sstep];
     }
 #pragma unroll
-    for (int k = 0; k < n; ++k) d[k] = __builtin_amdgcn_exp2f(d[k] * A2);
+    for (int k = 0; k < n; ++k) {
+      e[k] *= A2;
+      d[k] = __builtin_amdgcn_exp2f(e[k]);
+    }
 #pragma unroll
     for (int k = 0; k < n; ++k) {
       c[k * cstep] = ALL || real ? h : 0.0f;
       h = __builtin_fmaf(d[k], h, v[k]);
+    }
+    // Token by token a state may stay 0, finite or infinite where a chunk's decay is infinite or 0, and their product would be
+    // NaN or infinite: those chunks again, with the decay in two factors
+    if (__builtin_amdgcn_ballot_w64(real && !(__builtin_fabsf(h) < __builtin_inff())) != 0) {
+      h = start;
+#pragma unroll
+      for (int k = 0; k < n; ++k) {
+        c[k * cstep] = ALL || real ? h : 0.0f;
+        h = carried(e[k], h, v[k]);
+      }
     }
     c += n * cstep;
     s += n * sstep;
