@@ -134,7 +134,8 @@ class EQScanBlock(torch.nn.Module):
         last, state = cache or (None, None)
         x = scan.causal_conv(x, self.conv_weight, self.conv_bias, "silu", lengths, last, state_out=last)
         x = x if cache is None else x[0]
-        bc = self.bc(x.mean(3)).view(B, L, 2 * self.groups, self.states)
+        with torch.autocast(x.device.type, enabled=False):  # (a dense layer: it would give Bt and Ct a type that x has not)
+            bc = self.bc(x.mean(3)).view(B, L, 2 * self.groups, self.states)
         y = scan.selective_scan(x, self.delta_up(self.delta_down(x)), -torch.exp(self.A_log), bc[:, :, :self.groups],
                                 bc[:, :, self.groups:], self.D, z, self.delta_bias, lengths=lengths, state=state,
                                 state_out=state)
