@@ -1086,8 +1086,31 @@ __global__ __launch_bounds__(64 * kScanWaves, scan_columns(NL) == 4 ? 1 : 2) voi
   float* const part = a.part + (p.b * a.K + p.k) * (a.N + 2) * a.cols + p.col0;
   int odd = 0, turns = 0;
   bool flushed = false;
-  auto flush = [&] {  // the lane's sums of dA to memory
+  auto flush = [&] {  // the lane's sums of dA, dD and ddelta_bias to memory
     if (!on) return;
+    // (lanes with the same columns lie VT apart)
+    auto add = [&](float* row, float (&f)[VEC]) {
+      if constexpr (TL::VT <= 16) {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) {
+          const float v = columns_sum<TL::VT>(f[i], f[i + 1], f[i + 2], f[i + 3]);  // column i + row of 16 lanes
+          float* const q = row + at + i + lane / 16;
+          if (lane % 16 < TL::VT) *q = flushed ? *q + v : v;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          float u = f[i], v = f[i];
+          swap32(u, v);
+          float* const q = row + at + i;
+          if (lane < TL::VT) *q = flushed ? *q + (u + v) : u + v;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) f[i] = 0.0f;
+    };
+    add(part + (int64_t)a.N * a.cols, dskip);
+    add(part + (int64_t)(a.N + 1) * a.cols, dbias);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       if (n0 + n >= a.N) continue;
@@ -1282,10 +1305,6 @@ __global__ __launch_bounds__(64 * kScanWaves, scan_columns(NL) == 4 ? 1 : 2) voi
       }
       sums(s0);
     }
-    if (++turns == 32) {  // sums of no more than 32 tiles in registers, so that long ones lose no digits
-      turns = 0;
-      flush();
-    }
     wave_order();
     {
       float xf[EPT], f[EPT], o[EPT], sf[EPT];
@@ -1331,6 +1350,11 @@ __global__ __launch_bounds__(64 * kScanWaves, scan_columns(NL) == 4 ? 1 : 2) voi
       TL::store(o, dense(a.ddelta), l0, rows, p.left);
       TL::store(f, dense(a.dx), l0, rows, p.left);
     }
+    // sums of no more than 32 tiles in registers, so that long ones lose no digits
+    if (__builtin_expect(++turns == 32 || tile == 0, 0)) {
+      turns = 0;
+      flush();
+    }
     if (tile > 0) fetch(l0 - TT);
     __syncthreads();  // (every wave of the workgroup walks the same tiles)
     for (int i = threadIdx.x; i < nt * 2 * NP; i += 64 * waves) {
@@ -1363,21 +1387,8 @@ __global__ __launch_bounds__(64 * kScanWaves, scan_columns(NL) == 4 ? 1 : 2) voi
     }
   }
   if (a.dh0 && p.k == 0) store_state<NL>(a, p, a.dh0, g);
-  if (!on) return;
-  flush();
-  // lanes with the same columns lie VT apart
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) {
-#pragma unroll
-    for (int d = TL::VT; d < 64; d *= 2) {
-      dskip[i] += __shfl_xor(dskip[i], d);
-      dbias[i] += __shfl_xor(dbias[i], d);
-    }
-    if (lane < TL::VT) {
-      part[(int64_t)a.N * a.cols + at + i] = dskip[i];
-      part[(int64_t)(a.N + 1) * a.cols + at + i] = dbias[i];
-    }
-  }
+  if (tiles == 0 && on)
+    for (int i = lane; i < (a.N + 2) * CH; i += 64) part[(int64_t)(i / CH) * a.cols + i % CH] = 0.0f;
 }
 
 // db and dc: the parts of a token's P workgroups in order.
@@ -1411,7 +1422,11 @@ __global__ __launch_bounds__(256) void eql_scan_params_kernel(const ScanArgs a, 
   const int ct = ch * a.T, g = ct / a.CTg, step = 256 / a.T, first = channel_of(threadIdx.x, a.mT);
   const float* const from = a.part + (int64_t)j * a.cols + g * a.nblk * CH + (ct - g * a.CTg) + (threadIdx.x - first * a.T);
   if (first < step)
-    for (int64_t i = first; i < n; i += step) v += from[i * (a.N + 2) * a.cols];
+    for (int64_t i = first; i < n;) {  // 64 rows, then the sums of so many, so that many rows lose no digits
+      float w = 0.0f;
+      for (int k = 0; k < 64 && i < n; ++k, i += step) w += from[i * (a.N + 2) * a.cols];
+      v += w;
+    }
   __shared__ float red[4];
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
