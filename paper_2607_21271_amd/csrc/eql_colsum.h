@@ -7,8 +7,8 @@
 namespace eqk {
 
 // A workgroup of kColsumThreads takes up to 64 columns of one kind of rows [rows][.. K ..], `step` apart, whole channels of T
-// columns each; its waves add every sixteenth row, four at a time, then a thread a channel adds the waves and the
-// channel's columns.  f(channel, sum) for each.
+// columns each; its waves add every sixteenth row, four at a time (64 of these, then the sums of so many: thousands of rows
+// one after the other would lose digits), then a thread a channel adds the waves and the channel's columns.  f(channel, sum) for each.
 constexpr int kColsumWidth = 64, kColsumWaves = 16, kColsumThreads = 64 * kColsumWaves;
 inline int colsum_channels(int T) { return kColsumWidth / T; }  // (T <= 16)
 inline int colsum_blocks(int C, int T) { return (C + colsum_channels(T) - 1) / colsum_channels(T); }
@@ -23,9 +23,14 @@ __device__ __forceinline__ void column_sums(const float* part, int64_t rows, int
     const float* p = part + c0 * T + lane;
     float w[4] = {0.f, 0.f, 0.f, 0.f};
     int64_t r = wave;
-    for (; r + 3 * kColsumWaves < rows; r += 4 * kColsumWaves) {
+    while (r + 3 * kColsumWaves < rows) {
+      float u[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < 64 && r + 3 * kColsumWaves < rows; ++i, r += 4 * kColsumWaves) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] += p[(r + kColsumWaves * k) * step];
+        for (int k = 0; k < 4; ++k) u[k] += p[(r + kColsumWaves * k) * step];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] += u[k];
     }
     for (; r < rows; r += kColsumWaves) w[0] += p[r * step];
     v = (w[0] + w[1]) + (w[2] + w[3]);
