@@ -244,6 +244,9 @@ void res_plan(ResArgs& a, int dt, int cus, bool bwd) {
   // four workgroups a CU (two in the backward, whose sums take registers), each at least two turns long
   int64_t strips = a.seqs > 0 ? ((bwd ? 2 : 4) * (int64_t)cus + a.seqs - 1) / a.seqs : 1;
   const int64_t most = (a.rows + 2 * turn - 1) / (2 * turn);
+  // gradients: no more than 256 turns, which a thread adds up one after the other
+  const int64_t least = bwd ? (a.rows + 256 * turn - 1) / (256 * turn) : 1;
+  if (strips < least) strips = least;
   if (strips > most) strips = most;
   if (strips < 1) strips = 1;
   a.strip = (a.rows + strips - 1) / strips;

@@ -112,6 +112,20 @@ struct ResRow {
     }
     return s;
   }
+  // s and the sum of f, or f h, over run i of columns; a run adds to s as one, which keeps the digits of many rows
+  static __device__ __forceinline__ float values(const float (&f)[EPT], int i, float s) {
+    float t = f[i * GR];
+#pragma unroll
+    for (int j = 1; j < GR; ++j) t += f[i * GR + j];
+    return s + t;
+  }
+  static __device__ __forceinline__ float products(const float (&f)[EPT], const float (&h)[EPT], int i, float s) {
+    if constexpr (GR == 1) return __builtin_fmaf(f[i], h[i], s);
+    float t = f[i * GR] * h[i * GR];
+#pragma unroll
+    for (int j = 1; j < GR; ++j) t = __builtin_fmaf(f[i * GR + j], h[i * GR + j], t);
+    return s + t;
+  }
   // f normalised in place (0 outside the row); returns the factor
   static __device__ __forceinline__ float normed(float (&f)[EPT], const ResArgs& a, float* red, int& slot) {
     float s = 0.0f;
@@ -293,11 +307,12 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, MODE, GR>::THREADS)) void e
       again(1, w);
       if (PARK) R::floats(hr, a.K, g);
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) {
-        s0[e / GR] = __builtin_fmaf(g[e], x[e], s0[e / GR]);
-        s1[e / GR] += g[e];
-        g[e] *= w[e / GR];
+      for (int i = 0; i < NP; ++i) {
+        s0[i] = R::products(g, x, i, s0[i]);
+        s1[i] = R::values(g, i, s1[i]);
       }
+#pragma unroll
+      for (int e = 0; e < EPT; ++e) g[e] *= w[e / GR];
       R::back(g, x, fr, a, red, slot);
       if (a.dr && PARK) R::floats(rr, a.K, d);
       if (a.dr)
@@ -311,15 +326,14 @@ __global__ __launch_bounds__((ResRow<DT, LANES, EPT, MODE, GR>::THREADS)) void e
     if (a.dx) R::store(g, a.dx, row, a.K);
     if (a.u) {
 #pragma unroll
-      for (int e = 0; e < EPT; ++e) s2[e / GR] = __builtin_fmaf(g[e], u[e], s2[e / GR]);
+      for (int i = 0; i < NP; ++i) s2[i] = R::products(g, u, i, s2[i]);
       again(0, k);
       if (a.pw) {
         again(2, pw);
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-          s3[e / GR] += g[e];
-          g[e] *= k[e / GR] * pw[e / GR];
-        }
+        for (int i = 0; i < NP; ++i) s3[i] = R::values(g, i, s3[i]);
+#pragma unroll
+        for (int e = 0; e < EPT; ++e) g[e] *= k[e / GR] * pw[e / GR];
         if (a.du) R::back(g, u, fu, a, red, slot);
       } else {
 #pragma unroll
@@ -384,6 +398,8 @@ __global__ __launch_bounds__(kResParamThreads) void eql_res_params_kernel(const 
   __shared__ float red[5][NQ][NC];
   auto at = [&](const void* p, int64_t i) { return (float)reinterpret_cast<const E*>(p)[i]; };
   float sum[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // dw, db, dscale, dpw, dpb
+  float many[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // of 64 sequences each, so that thousands lose no digits
+  int turns = 0;
   if (c < a.C) {
     const float scale = a.scale ? at(a.scale, c) : 1.0f, pw = a.pw ? at(a.pw, c) : 1.0f, pb = a.pb ? at(a.pb, c) : 0.0f;
     for (int64_t q = turn; q < a.seqs; q += NQ) {
@@ -392,6 +408,14 @@ __global__ __launch_bounds__(kResParamThreads) void eql_res_params_kernel(const 
         continue;
       }
       const float* s = a.sums + q * a.J * a.C + c;
+      if (++turns == 64) {
+        turns = 0;
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+          many[i] += sum[i];
+          sum[i] = 0.0f;
+        }
+      }
       if (a.w) {
         sum[0] += s[0];
         sum[1] += s[a.C];
@@ -407,7 +431,7 @@ __global__ __launch_bounds__(kResParamThreads) void eql_res_params_kernel(const 
     }
   }
 #pragma unroll
-  for (int i = 0; i < 5; ++i) red[i][turn][cc] = sum[i];
+  for (int i = 0; i < 5; ++i) red[i][turn][cc] = many[i] + sum[i];
   __syncthreads();
   if (c >= a.C || turn >= 5) return;
   void* const dst[5] = {a.dw, a.db, a.dscale, a.dpw, a.dpb};
