@@ -131,7 +131,7 @@ int scan_inputs(const eqlinear_scan_shape* s, const eqk::ScanArgs& a, const void
 
 // How the kernels read and write: a tile's tokens are addressed by 31 bits from its first.
 int scan_mode(const eqk::ScanArgs& a, int dtype) {
-  const int vec = eqk::scan_vec(dtype, eqk::scan_lanes(a.N));
+  const int NL = eqk::scan_lanes(a.N), vec = eqk::scan_vec(dtype, NL, eqk::scan_columns(NL));
   const int64_t steps[6] = {a.CT, a.xs[1], a.ds[1], a.z ? a.zs[1] : 0, a.bs[1], a.cs[1]};
   for (int64_t st : steps)
     if (st >= ((int64_t)1 << 31) / 128) return eqk::kTiny;
