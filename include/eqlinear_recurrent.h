@@ -33,7 +33,9 @@ extern "C" {
  *   y_l = (sum_n c_l[n] h[n] + D x_l) * silu(z_l)
  * state_out (fp32 [B, C, T, N], may be state_in or NULL) is h after the last token.  States,
  * sums and exponents in fp32, one rounding of y.  states (fp32, _states_bytes, or NULL) keeps
- * what the backward starts its runs of tokens from.  1 <= N <= 64, T <= 16,
+ * what the backward starts its runs of tokens from: 4 NP / 8 bytes for each element of x, NP the states rounded up to 4, 8, 16,
+ * 32 or 64 (8 bytes at 16 states, 32 at 64; NP bytes up to 4 states), and the columns of a group, C / groups * T, rounded up to a
+ * multiple of 1024 / NP: many narrow groups multiply it, and the workspaces.  1 <= N <= 64, T <= 16,
  * C * T <= 65536, groups <= C, B <= 2^20, L <= 2^30, 2^46 elements a tensor (EQL_ERR_UNSUPPORTED above).
  * Elements need only their own alignment; 16-byte aligned addresses and strides run faster.  Infinities and NaN inside a
  * sequence do to y and the states what they do in the formulas; a gradient that is infinite there may come as NaN. */

@@ -40,7 +40,7 @@ ARCH = "gfx950"
 # 352 in fp16; 164 in full precision, one wave).  The large-tile unit (one wave per SIMD, T * 64
 # accumulators per lane) and full-precision attention keep them in the
 # accumulation registers instead.  Of the recurrent kernels, scratch is used by the scan's
-# gradients at 5 to 16 states (72 to 172 bytes a lane, 124 to 212 in fp32; some others 20 to 112), outside the loops over
+# gradients at 5 to 16 states (72 to 136 bytes a lane, 104 to 208 in fp32; some others 20 to 104), outside the loops over
 # tokens, and by the residual norm's over rows of more than 4096 elements (16 to 60 bytes; 208 in fp32 where the rows are
 # no whole vectors).
 LINK_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -49,7 +49,7 @@ DEVICE_FLAGS = LINK_FLAGS + VGPR_FORM
 ACC_REG_UNITS = {"eql_big", "attn_f32"}
 # Arrays stay arrays until loops over them are unrolled, and then become registers of their own.  Made into vectors
 # before that, f16 elements were lost: in a scan's gradients an element's register was written by another
-# tensor's before it had been read.
+# tensor's before it had been read (the post-build check finds such elements).
 SCALARS = ["-mllvm", "-disable-promote-alloca-to-vector"]
 SCALAR_UNITS = ("scan_", "recurrent_")
 COMMON_FLAGS = ["-O3", "-std=c++20", "-fPIC", "-Wall", "-Wno-unused-function",

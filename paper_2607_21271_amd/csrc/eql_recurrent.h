@@ -17,8 +17,9 @@ __device__ __forceinline__ int channel_of(int ct, unsigned m) { return (int)__um
 constexpr int kWhole = 0, kLoose = 1, kTiny = 2;
 
 // ---- selective scan ----
-// A wave takes `scan_cols(NL)` neighbouring columns (channel, group element) of one group:
-// NL lanes share four columns (the gradients: two, where Q says so) and hold four states of each.
+// A wave takes `scan_cols(NL, Q)` neighbouring columns (channel, group element) of one group: NL lanes share Q columns and
+// hold four states of each.  Q is scan_columns(NL) in the kernels of tiles, forward and gradients, four in the one of few
+// tokens.  A group's columns are padded to whole scan_cols(NL) in what is kept for them (states, carry, sums).
 constexpr int kScanMaxN = 64;
 constexpr int scan_lanes(int N) { return N <= 4 ? 1 : N <= 8 ? 2 : N <= 16 ? 4 : N <= 32 ? 8 : 16; }
 constexpr int scan_cols(int NL, int Q = 4) { return 64 * Q / NL; }
@@ -51,7 +52,7 @@ struct ScanArgs {
   unsigned mT;           // channel_factor(T)
   int64_t chunk, tiles, runs;  // tokens of a chunk (whole tiles), tiles and runs of a sequence
   int C, T, N, G, CT, CTg, nblk, cols, K, softplus;
-  int bblk;      // blocks of a group's columns in the gradients
+  int bblk;      // blocks of a group's columns in the kernels of tiles (nblk: of few tokens)
   int waves, P;  // of a workgroup of the gradients, and those side by side for a group's columns
   int mode;  // how rows are read and written (ScanTile)
 };

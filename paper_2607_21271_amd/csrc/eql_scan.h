@@ -1022,7 +1022,7 @@ __global__ __launch_bounds__(64 * kScanWaves, 2) void eql_scan_back_kernel(const
 // What a tile's elements need twice (step, slope, gate, dy silu(z)) waits in LDS beside the scan's sums.
 // Two columns a lane (four above 32 states): a run's states take 64 registers, and two waves fit a SIMD.  Bound by the vector
 // pipe: a wave alone takes 0.6 us a token, two 0.9 together (with four columns, for twice the work, 1.1 us, and no second
-// wave fits).  What is spilled (17 to 52 registers) is used once a tile, not in the loops over tokens.
+// wave fits).  What is spilled (18 to 52 registers) is used once a tile, not in the loops over tokens.
 // Measured, f16, 16 states: 64 x 197 tokens of 768 columns 172 to 187 us, 1.1 to 1.2 ps a state of a token (205 with four).
 template <int NL>
 constexpr int scan_bwd_lds() {  // floats of a wave

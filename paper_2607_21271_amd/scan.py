@@ -198,7 +198,11 @@ def selective_scan(x: torch.Tensor, delta: torch.Tensor, A: torch.Tensor, Bt: to
     ``lengths`` int32 [B]: tokens of each sequence that hold data (None: L); the others give zeros and no gradient, and
     leave the state.  ``state`` float32 [B, C, T, N]: h before the first token (None: 0).  ``return_state``: (y, h after the last
     token).  ``state_out``: a buffer for that h, which may be ``state`` itself (updated in place); the call is then not
-    differentiable and gives (y, state_out)."""
+    differentiable and gives (y, state_out).
+
+    Training keeps, until its backward pass, a float32 state before every eight tokens: 8 bytes for each element of x at 9 to 16
+    states, 32 at 33 to 64, more where groups have few columns (C / groups * T is rounded up to 64 columns at 9 to 16
+    states)."""
     softplus = bool(softplus)
     plan = _scan_check(x, delta, A, Bt, Ct, D, z, delta_bias, softplus, state)
     ops._check_dev(x, delta, A, Bt, Ct, D, z, delta_bias, state)
