@@ -148,7 +148,7 @@ def _written_and_read(op, operands):
         read |= written
     if "swap" in op:
         written |= read
-    if op.startswith("buffer_load") and operands.endswith(" lds"):  # (its first operand is an address)
+    if "load_lds" in op or (op.startswith("buffer_load") and operands.endswith(" lds")):  # (the first operand is an address)
         written, read = 0, read | written
     return written, read
 

@@ -47,7 +47,8 @@ def test_flags_an_element_whose_register_is_taken():
 
 @pytest.mark.parametrize("reader", ["v_mov_b32_e32 v60, v43", "v_fmac_f32_e32 v43, v1, v2", "v_cmp_lt_f32_e32 vcc, 0, v43", "ds_write_b32 v9, v43",
                                     "scratch_store_dword off, v43, off offset:4", "v_cvt_pkrtz_f16_f32 v8, v[42:43], v2",
-                                    "v_permlane32_swap_b32_e32 v43, v44", "v_add_f32_dpp v43, v1, v1 quad_perm:[1,0,3,2]", "s_swappc_b64 s[30:31], s[4:5]"])
+                                    "v_permlane32_swap_b32_e32 v43, v44", "v_add_f32_dpp v43, v1, v1 quad_perm:[1,0,3,2]", "s_swappc_b64 s[30:31], s[4:5]", "buffer_load_dwordx4 v43, s[0:3], 0 offen lds",
+                                    "global_load_lds_dwordx4 v[42:43], off"])
 def test_passes_where_it_is_read(reader):
     """On either way to where the register is written again."""
     assert _scan(LOST.replace("\ts_and_b64 vcc", "\t%s\n\ts_and_b64 vcc" % reader)) == []
